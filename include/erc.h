@@ -284,6 +284,131 @@ erc_status erc_saint_counts(const erc_graph* g, const int32_t* nodes, int32_t n_
 erc_status erc_saint_norm(const erc_graph* g, const int32_t* node_count, const int32_t* edge_count,
                           int32_t N, float* lambda, float* alpha, erc_stream s);
 
+/* =============================================================================================
+ * Row-wise choices (no counterpart in the paper): draws from rows of scores, and experts chosen
+ * per row, for models that are trained on or answer over the graph's nodes.
+ *
+ * Whole-number results are the same on every machine.  The weight of a score l in a row with
+ * maximum m and temperature T is round(2^t 2^40), half up, an integer, with t = (l - m) c,
+ * c = log2(e) / T and 2^t = p(t - e) 2^e, e = rint(t); p is the degree-5 polynomial with float32
+ * coefficients 1, 0.693147, 0.24022242, 0.055507336, 0.009671513, 0.0013264727 in Horner's form.
+ * Every step is one float32 operation rounded to nearest.  t = 0 at the maximum, whatever c is;
+ * entries with e < -41 weigh 0.  Scores are read as float32; NaN and -inf are masked entries; -0
+ * equals +0; where the maximum is +inf, only the entries that equal it weigh anything.  The
+ * lowest finite value of a type is a score like any other.
+ * Score rows have unit element stride and `stride` elements (any >= 0) from row to row.
+ * ========================================================================================== */
+enum { ERC_F32 = 0, ERC_BF16 = 1, ERC_F16 = 2 };
+
+#define ERC_SAMPLE_ROWS_MAX_N 4194304 /* 2^22 entries: a row's weight sum stays below 2^63 */
+
+/* Rule of erc_sample_rows: a value for every row, or a device array [rows] where the pointer is
+ * not NULL (the value is then not used, but must still be valid). */
+typedef struct erc_sample_rule {
+  float temperature;             /* 0: the best entry; finite, >= 0 */
+  int32_t top_k;                 /* 0: off */
+  float top_p;                   /* 1: off; in (0, 1] */
+  float min_p;                   /* 0: off; in [0, 1] */
+  const float* temperature_rows; /* entries that are not > 0 (NaN too) mean the best entry */
+  const int32_t* top_k_rows;     /* entries <= 0 mean off */
+  const float* top_p_rows;       /* entries that are not < 1 mean off, those <= 0 the best entry */
+  const float* min_p_rows;       /* entries that are not > 0 mean off, those > 1 mean 1 */
+} erc_sample_rule;
+
+/* ---------------------------------------------------------------------------------------------
+ * erc_sample_rows -- one draw from each row of scores.
+ *
+ * With the row's weights w_i, in this order:
+ *   min-p  keeps w_i >= max(1, floor(min_p 2^40)) (2^40 is the weight of the maximum);
+ *   top-k  keeps the first top_k of these, ordered by score descending, then index ascending;
+ *   top-p  keeps, in that order and with W the sum of what is left, the entries that have less
+ *          than max(1, floor(W floor(top_p 2^31) / 2^31)) before them.
+ * The draw takes x = words[row], W the kept sum, and picks the first kept index, in index order,
+ * whose inclusive weight sum exceeds floor(x W / 2^64): the same exact inverse distribution
+ * function as erc_sample_subgraph's.
+ * In : logits [rows x n] of `type`, n <= ERC_SAMPLE_ROWS_MAX_N; words [rows]; rule (host).
+ * Out: ids [rows] int32 (-1 where nothing can be drawn: n = 0 or every entry masked); logp [rows]
+ *      float32 natural logarithm of the draw's probability among the kept entries (-inf where
+ *      there is none); kept [rows] int32 number of kept entries.
+ * Errors: INVALID_ARG for sizes, types, pointers or rule values out of range.  Deterministic.
+ * ------------------------------------------------------------------------------------------- */
+erc_status erc_sample_rows(int64_t rows, int64_t n, const void* logits, int32_t type,
+                           int64_t stride, const uint64_t* words, const erc_sample_rule* rule,
+                           int32_t* ids, float* logp, int32_t* kept, erc_stream s);
+
+enum { ERC_SCORE_SOFTMAX = 0, ERC_SCORE_SIGMOID = 1 };
+#define ERC_ROUTE_MAX_EXPERTS 1024
+#define ERC_ROUTE_MAX_K 32
+
+typedef struct erc_route_rule {
+  int32_t experts;    /* E, 1 .. ERC_ROUTE_MAX_EXPERTS */
+  int32_t k;          /* experts of a row, 1 .. min(ERC_ROUTE_MAX_K, E) */
+  int32_t score;      /* ERC_SCORE_SOFTMAX or ERC_SCORE_SIGMOID */
+  int32_t groups;     /* equal groups of consecutive experts; 1: none */
+  int32_t top_groups; /* groups a row may choose from */
+  int32_t group_best; /* a group's score is the sum of its 1 or 2 best choices */
+  int32_t renorm;     /* not 0: the chosen weights are divided by their sum */
+  float scale;        /* factor of every weight; finite */
+} erc_route_rule;
+
+/* ---------------------------------------------------------------------------------------------
+ * erc_route -- k experts for each row of scores, with their weights.
+ *
+ * s_i is the softmax over the row (2^t divided by the sum of the row's integer weights, as
+ * 2^t (1 / Z), T = 1) or the sigmoid ((l >= 0 ? 1 : e) / (1 + e), e = 2^(-|l| log2(e)), 0 below
+ * 2^-126).  Experts are chosen by s_i + bias_i (bias [E] float32 or NULL; it balances the load
+ * and has no part in the weights): first the top_groups best groups, then the k best experts in
+ * them, ties to the lowest index.  A masked score, or a choice that is -inf or NaN, is never
+ * chosen, and neither is a group with no other; a group's missing second best adds nothing.
+ * Out: experts [rows x k] int32, best first, -1 where fewer than k can be chosen; weights
+ *      [rows x k] float32: scale s_i, or scale s_i / (sum of the row's chosen s) with renorm (0
+ *      where that sum is 0); 0 for -1.
+ * erc_route_backward -- the gradient with respect to the logits for fixed choices: from dweights
+ *      [rows x k] to dlogits [rows x E] of `type`, dense rows.  Entries of `experts` outside
+ *      [0, E) contribute nothing; a row must not name an expert twice.  Of the rule it uses
+ *      experts, k, score, renorm and scale; the bias has no gradient.
+ * Errors: INVALID_ARG for sizes, types, pointers or rule values out of range.  Deterministic.
+ * ------------------------------------------------------------------------------------------- */
+erc_status erc_route(int64_t rows, const void* logits, int32_t type, int64_t stride,
+                     const float* bias, const erc_route_rule* rule, int32_t* experts,
+                     float* weights, erc_stream s);
+erc_status erc_route_backward(int64_t rows, const void* logits, int32_t type, int64_t stride,
+                              const int32_t* experts, const float* dweights,
+                              const erc_route_rule* rule, void* dlogits, erc_stream s);
+
+/* ---------------------------------------------------------------------------------------------
+ * erc_expert_plan -- the pairs (row, choice) of `experts` [rows x k] in expert order.
+ *
+ * A pair's number is row * k + choice; entries outside [0, n_experts) are no pairs.
+ * Out: offsets [n_experts + 1] int64, expert e's pairs take slots offsets[e] .. offsets[e+1]-1, in
+ *      ascending pair number; order [rows * k] int32, the pair of each slot, -1 from
+ *      offsets[n_experts] on; slot [rows x k] int32, the slot of each pair, -1 for no pair.
+ * Errors: INVALID_ARG for sizes (rows * k < 2^31) and pointers; CAPACITY if ws_bytes <
+ *      erc_expert_plan_workspace_size(rows, k, n_experts).  Deterministic.
+ *
+ * erc_expert_gather  -- xs[slot[t, j]] = x[t] for every pair: x [rows x width] to xs
+ *      [rows * k x width]; the slots from *placed on (device; pass offsets + n_experts) are zeroed.
+ *      Its gradient is erc_expert_combine of xs' gradient with weights NULL.
+ * erc_expert_combine -- out[t] = sum_j weights[t, j] y[slot[t, j]] over the row's pairs (weights
+ *      NULL: 1), summed in float32 in the order of j and rounded once; 0 for a row without pairs.
+ * erc_expert_combine_backward -- dy[slot[t, j]] = weights[t, j] dout[t], zeros from *placed on, and
+ *      dweights[t, j] = dout[t] . y[slot[t, j]] (float32 sums; 0 for no pair).
+ * slot must come from erc_expert_plan (every value below rows * k, none twice).  Row-major dense
+ * arrays of `type`; weights and dweights float32.  Errors: INVALID_ARG.  Deterministic.
+ * ------------------------------------------------------------------------------------------- */
+size_t erc_expert_plan_workspace_size(int64_t rows, int32_t k, int32_t n_experts);
+erc_status erc_expert_plan(int64_t rows, int32_t k, int32_t n_experts, const int32_t* experts,
+                           int64_t* offsets, int32_t* order, int32_t* slot, void* ws,
+                           size_t ws_bytes, erc_stream s);
+erc_status erc_expert_gather(int64_t rows, int32_t k, int64_t width, const void* x, int32_t type,
+                             const int32_t* slot, const int64_t* placed, void* xs, erc_stream s);
+erc_status erc_expert_combine(int64_t rows, int32_t k, int64_t width, const void* y, int32_t type,
+                              const int32_t* slot, const float* weights, void* out, erc_stream s);
+erc_status erc_expert_combine_backward(int64_t rows, int32_t k, int64_t width, const void* dout,
+                                       const void* y, int32_t type, const int32_t* slot,
+                                       const int64_t* placed, const float* weights, void* dy,
+                                       float* dweights, erc_stream s);
+
 /* ---------------------------------------------------------------------------------------------
  * erc_laplacian_apply -- AP = L_eps P for an n x ld block (the CG operator of Eq. 5), and, when
  * pAp is not NULL, pAp[c] = sum_u P[u,c] AP[u,c] as float64 (device [kc]).  Exposed for testing

@@ -47,6 +47,17 @@ class ErcGraphC(ctypes.Structure):
                 ("deg", _c_p), ("csr_eid", _c_p), ("eu", _c_p), ("ev", _c_p), ("ew", _c_p)]
 
 
+class ErcSampleRuleC(ctypes.Structure):
+    _fields_ = [("temperature", _f32), ("top_k", _i32), ("top_p", _f32), ("min_p", _f32),
+                ("temperature_rows", _c_p), ("top_k_rows", _c_p), ("top_p_rows", _c_p),
+                ("min_p_rows", _c_p)]
+
+
+class ErcRouteRuleC(ctypes.Structure):
+    _fields_ = [("experts", _i32), ("k", _i32), ("score", _i32), ("groups", _i32),
+                ("top_groups", _i32), ("group_best", _i32), ("renorm", _i32), ("scale", _f32)]
+
+
 class ErcParamsC(ctypes.Structure):
     _fields_ = [("seed", _u64), ("K", _i32), ("kc", _i32), ("eps", _f32), ("tol", _f32),
                 ("max_iter", _i32), ("eta", _f32), ("dup_policy", _i32), ("precond", _i32)]
@@ -104,6 +115,18 @@ _SIGS = {
     "erc_run_host": (_i32, [ctypes.POINTER(ErcParamsC), _i32, _c_p, _c_p, _c_p, _i64,
                             ctypes.POINTER(_i64), _c_p, _c_p, _c_p, _c_p, _c_p, _c_p, _c_p, _c_p,
                             _c_p, _c_p, _sz, _c_p]),
+    "erc_sample_rows": (_i32, [_i64, _i64, _c_p, _i32, _i64, _c_p, ctypes.POINTER(ErcSampleRuleC),
+                               _c_p, _c_p, _c_p, _c_p]),
+    "erc_route": (_i32, [_i64, _c_p, _i32, _i64, _c_p, ctypes.POINTER(ErcRouteRuleC), _c_p, _c_p,
+                         _c_p]),
+    "erc_route_backward": (_i32, [_i64, _c_p, _i32, _i64, _c_p, _c_p,
+                                  ctypes.POINTER(ErcRouteRuleC), _c_p, _c_p]),
+    "erc_expert_plan_workspace_size": (_sz, [_i64, _i32, _i32]),
+    "erc_expert_plan": (_i32, [_i64, _i32, _i32, _c_p, _c_p, _c_p, _c_p, _c_p, _sz, _c_p]),
+    "erc_expert_gather": (_i32, [_i64, _i32, _i64, _c_p, _i32, _c_p, _c_p, _c_p, _c_p]),
+    "erc_expert_combine": (_i32, [_i64, _i32, _i64, _c_p, _i32, _c_p, _c_p, _c_p, _c_p]),
+    "erc_expert_combine_backward": (_i32, [_i64, _i32, _i64, _c_p, _c_p, _i32, _c_p, _c_p, _c_p,
+                                           _c_p, _c_p, _c_p]),
 }
 
 _lib = None
@@ -462,3 +485,177 @@ def erc_run_host(n, src, dst, w, params, ws=None, out=None):
     res = _trim(dict(o), m.value)
     res["status"] = st
     return res
+
+
+# ------------------------------------------------------------------------------------------------
+# row-wise choices: the argument checks that need the tensors' types, shapes and devices are made
+# here (the C entry points see raw pointers), and raise ErcError with ERC_ERR_INVALID_ARG
+# ------------------------------------------------------------------------------------------------
+ERC_F32, ERC_BF16, ERC_F16 = 0, 1, 2
+ERC_SCORE_SOFTMAX, ERC_SCORE_SIGMOID = 0, 1
+_TYPES = {torch.float32: ERC_F32, torch.bfloat16: ERC_BF16, torch.float16: ERC_F16}
+
+
+def _require(ok, message):
+    if not ok:
+        raise ErcError(ERC_ERR_INVALID_ARG, message)
+
+
+def _need(t, name, dtype, shape, device):
+    """`t` is a dense tensor of this type and shape on `device`."""
+    _require(isinstance(t, torch.Tensor) and t.dtype == dtype and tuple(t.shape) == tuple(shape)
+             and t.device == device and t.is_contiguous(),
+             f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)} on {device}")
+
+
+def _rows_of(t, name):
+    """(rows, n, type, row stride) of a matrix of scores with unit element stride."""
+    _require(isinstance(t, torch.Tensor) and t.is_cuda and t.dim() == 2 and t.dtype in _TYPES,
+             f"{name} must be a 2-d float32, bfloat16 or float16 CUDA tensor")
+    rows, n = t.shape
+    _require(n <= 1 or t.stride(1) == 1, f"the rows of {name} must have unit element stride")
+    return rows, n, _TYPES[t.dtype], t.stride(0) if rows > 1 else n
+
+
+def _stream_of(t):
+    return ctypes.c_void_p(torch.cuda.current_stream(t.device).cuda_stream)
+
+
+def erc_sample_rows(logits, words, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
+    """One draw from each row of logits [rows, n] (see include/erc.h): (ids int32, logp float32,
+    kept int32), each [rows].
+
+    words int64 [rows] holds 64 random bits a row; temperature, top_k, top_p and min_p are numbers,
+    or tensors [rows] (float32, int32, float32, float32) with a value for each row.
+    """
+    rows, n, kind, stride = _rows_of(logits, "logits")
+    dev = logits.device
+    _need(words, "words", torch.int64, (rows,), dev)
+    rule = ErcSampleRuleC(1.0, 0, 1.0, 0.0)
+    for name, v, dtype in (("temperature", temperature, torch.float32),
+                           ("top_k", top_k, torch.int32), ("top_p", top_p, torch.float32),
+                           ("min_p", min_p, torch.float32)):
+        if isinstance(v, torch.Tensor):
+            _need(v, name, dtype, (rows,), dev)
+            setattr(rule, name + "_rows", v.data_ptr())
+        elif name == "top_k":
+            rule.top_k = min(int(v), 2**31 - 1)
+        else:
+            setattr(rule, name, float(v))
+    out = torch.empty(3, rows, dtype=torch.int32, device=dev)
+    ids, logp, kept = out[0], out[1].view(torch.float32), out[2]
+    _check(lib().erc_sample_rows(rows, n, _ptr(logits), kind, stride, _ptr(words),
+                                 ctypes.byref(rule), _ptr(ids), _ptr(logp), _ptr(kept),
+                                 _stream_of(logits)))
+    return ids, logp, kept
+
+
+def erc_route(logits, k, score=ERC_SCORE_SOFTMAX, bias=None, groups=1, top_groups=1, group_best=2,
+              renorm=True, scale=1.0):
+    """k experts of each row of logits [rows, E] (see include/erc.h): (experts int32, weights
+    float32), each [rows, k]; bias float32 [E] or None."""
+    rows, E, kind, stride = _rows_of(logits, "logits")
+    dev = logits.device
+    if bias is not None:
+        _need(bias, "bias", torch.float32, (E,), dev)
+    rule = ErcRouteRuleC(E, k, score, groups, top_groups, group_best, int(bool(renorm)), scale)
+    experts = torch.empty(rows, max(k, 0), dtype=torch.int32, device=dev)
+    weights = torch.empty(rows, max(k, 0), dtype=torch.float32, device=dev)
+    _check(lib().erc_route(rows, _ptr(logits), kind, stride, _ptr(bias), ctypes.byref(rule),
+                           _ptr(experts), _ptr(weights), _stream_of(logits)))
+    return experts, weights
+
+
+def erc_route_backward(logits, experts, dweights, score=ERC_SCORE_SOFTMAX, renorm=True, scale=1.0):
+    """The gradient of erc_route's weights with respect to logits, for the experts it chose."""
+    rows, E, kind, stride = _rows_of(logits, "logits")
+    dev = logits.device
+    _require(isinstance(experts, torch.Tensor) and experts.dim() == 2, "experts must be [rows, k]")
+    k = experts.shape[1]
+    _need(experts, "experts", torch.int32, (rows, k), dev)
+    _need(dweights, "dweights", torch.float32, (rows, k), dev)
+    rule = ErcRouteRuleC(E, k, score, 1, 1, 1, int(bool(renorm)), scale)
+    dlogits = torch.empty(rows, E, dtype=logits.dtype, device=dev)
+    _check(lib().erc_route_backward(rows, _ptr(logits), kind, stride, _ptr(experts),
+                                    _ptr(dweights), ctypes.byref(rule), _ptr(dlogits),
+                                    _stream_of(logits)))
+    return dlogits
+
+
+def erc_expert_plan(experts, n_experts, ws=None):
+    """The pairs of experts int32 [rows, k] in expert order (see include/erc.h): (offsets int64
+    [n_experts + 1], order int32 [rows * k], slot int32 [rows, k])."""
+    _require(isinstance(experts, torch.Tensor) and experts.is_cuda and experts.dim() == 2,
+             "experts must be a CUDA tensor [rows, k]")
+    rows, k = experts.shape
+    dev = experts.device
+    _need(experts, "experts", torch.int32, (rows, k), dev)
+    _require(0 < n_experts < 2**31, "n_experts out of range")
+    offsets = torch.empty(n_experts + 1, dtype=torch.int64, device=dev)
+    order = torch.empty(rows * k, dtype=torch.int32, device=dev)
+    slot = torch.empty(rows, k, dtype=torch.int32, device=dev)
+    if ws is None:
+        ws = _workspace(lib().erc_expert_plan_workspace_size(rows, k, n_experts), dev)
+    _check(lib().erc_expert_plan(rows, k, n_experts, _ptr(experts), _ptr(offsets), _ptr(order),
+                                 _ptr(slot), _ptr(ws), ws.numel(), _stream_of(experts)))
+    return offsets, order, slot
+
+
+def _matrix(t, name):
+    _require(isinstance(t, torch.Tensor) and t.is_cuda and t.dim() == 2 and t.dtype in _TYPES
+             and t.is_contiguous(),
+             f"{name} must be a contiguous 2-d float32, bfloat16 or float16 CUDA tensor")
+    return t.shape[0], t.shape[1], _TYPES[t.dtype]
+
+
+def _slots(slot, rows, dev):
+    _require(isinstance(slot, torch.Tensor) and slot.dim() == 2, "slot must be [rows, k]")
+    rows = slot.shape[0] if rows is None else rows
+    _need(slot, "slot", torch.int32, (rows, slot.shape[1]), dev)
+    return rows, slot.shape[1]
+
+
+def _placed(offsets, dev):
+    _require(isinstance(offsets, torch.Tensor) and offsets.dim() == 1 and offsets.numel() > 0,
+             "offsets must be [n_experts + 1]")
+    _need(offsets, "offsets", torch.int64, offsets.shape, dev)
+    return ctypes.c_void_p(offsets.data_ptr() + 8 * (offsets.numel() - 1))
+
+
+def erc_expert_gather(x, slot, offsets):
+    """Rows of x [rows, width] at the slots of their pairs: xs [rows * k, width], zeros from
+    offsets[-1] on.  The gradient is erc_expert_combine(dxs, slot)."""
+    rows, width, kind = _matrix(x, "x")
+    _, k = _slots(slot, rows, x.device)
+    xs = torch.empty(rows * k, width, dtype=x.dtype, device=x.device)
+    _check(lib().erc_expert_gather(rows, k, width, _ptr(x), kind, _ptr(slot),
+                                   _placed(offsets, x.device), _ptr(xs), _stream_of(x)))
+    return xs
+
+
+def erc_expert_combine(y, slot, weights=None):
+    """The weighted sum over each row's pairs of y [rows * k, width]: out [rows, width]."""
+    slots, width, kind = _matrix(y, "y")
+    rows, k = _slots(slot, None, y.device)
+    _require(slots == rows * k, "y must have rows * k rows")
+    if weights is not None:
+        _need(weights, "weights", torch.float32, (rows, k), y.device)
+    out = torch.empty(rows, width, dtype=y.dtype, device=y.device)
+    _check(lib().erc_expert_combine(rows, k, width, _ptr(y), kind, _ptr(slot), _ptr(weights),
+                                    _ptr(out), _stream_of(y)))
+    return out
+
+
+def erc_expert_combine_backward(dout, y, slot, offsets, weights):
+    """The gradient of erc_expert_combine: (dy [rows * k, width], dweights float32 [rows, k])."""
+    rows, width, kind = _matrix(dout, "dout")
+    dev = dout.device
+    _, k = _slots(slot, rows, dev)
+    _need(y, "y", dout.dtype, (rows * k, width), dev)
+    _need(weights, "weights", torch.float32, (rows, k), dev)
+    dy = torch.empty_like(y)
+    dweights = torch.empty(rows, k, dtype=torch.float32, device=dev)
+    _check(lib().erc_expert_combine_backward(rows, k, width, _ptr(dout), _ptr(y), kind, _ptr(slot),
+                                             _placed(offsets, dev), _ptr(weights), _ptr(dy),
+                                             _ptr(dweights), _stream_of(dout)))
+    return dy, dweights
