@@ -76,6 +76,152 @@ __device__ __forceinline__ float order_value(unsigned k) {
   return __uint_as_float(k ^ ((k >> 31) ? 0x80000000u : 0xffffffffu));
 }
 
+// ---- the same weights for many entries of a thread, as two sums of 32 bits
+//
+// For t >= -60 (smaller t are raised to it: their weights are 0 all the same) v = p 2^e is an exact
+// float, hi = floor(v 2^20) and lo = round_half_up of the rest in 20 bits, so w = hi 2^20 + lo.
+// floor() comes from adding 2^23 with rounding toward zero: the sum's low bits are the integer,
+// and the sums of bit patterns carry a known multiple of 2^23's pattern.  Products and sums of two
+// entries are issued as one packed instruction.
+__device__ __forceinline__ uint64_t pair(float a, float b) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ void unpair(uint64_t p, float& a, float& b) {
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(p));
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+// a * b rounded by itself: the assembler fuses a packed product with the sum that takes it (1.6 of
+// 16.8 million polynomial values then differ), so the product is an fma with a -0 that it cannot see
+__constant__ uint64_t minus_zeros = 0x8000000080000000ull;
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) { return fma2(a, b, minus_zeros); }
+__device__ __forceinline__ uint64_t fma2_rz(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rz.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+
+constexpr unsigned HI_BIAS = 0x4B000000u, LO_BIAS = 0x25800000u;  // 2^23's pattern, and its half
+
+// weights of two scaled scores: hi and lo with their biases, and 2^t itself
+__device__ __forceinline__ void weight_parts(float t0, float t1, unsigned hi[2], unsigned lo[2],
+                                             float v[2]) {
+  const uint64_t t = pair(fmaxf(t0, -60.f), fmaxf(t1, -60.f));
+  const uint64_t shifter = pair(12582912.f, 12582912.f);  // 1.5 2^23: adding it rounds to an integer
+  const uint64_t r = add2(t, shifter);
+  const uint64_t e = add2(r, pair(-12582912.f, -12582912.f));
+  const uint64_t f = add2(t, e ^ 0x8000000080000000ull);
+  uint64_t p = add2(mul2(f, pair(0.0013264727f, 0.0013264727f)), pair(0.009671513f, 0.009671513f));
+  p = add2(mul2(p, f), pair(0.055507336f, 0.055507336f));
+  p = add2(mul2(p, f), pair(0.24022242f, 0.24022242f));
+  p = add2(mul2(p, f), pair(0.693147f, 0.693147f));
+  p = add2(mul2(p, f), pair(1.f, 1.f));
+  float p0, p1, r0, r1;
+  unpair(p, p0, p1);
+  unpair(r, r0, r1);
+  v[0] = __uint_as_float(__float_as_uint(p0) + (__float_as_uint(r0) << 23));
+  v[1] = __uint_as_float(__float_as_uint(p1) + (__float_as_uint(r1) << 23));
+  const uint64_t vv = pair(v[0], v[1]);
+  const uint64_t two20 = pair(1048576.f, 1048576.f), two23 = pair(8388608.f, 8388608.f);
+  const uint64_t h = fma2_rz(vv, two20, two23);
+  const uint64_t rest = fma2(vv, two20, add2(two23, h ^ 0x8000000080000000ull));
+  const uint64_t l = fma2_rz(rest, pair(2097152.f, 2097152.f), two23);
+  float a, b;
+  unpair(h, a, b);
+  hi[0] = __float_as_uint(a);
+  hi[1] = __float_as_uint(b);
+  unpair(l, a, b);
+  lo[0] = (__float_as_uint(a) + 1) >> 1;
+  lo[1] = (__float_as_uint(b) + 1) >> 1;
+}
+__device__ __forceinline__ unsigned long long join_parts(unsigned hi, unsigned lo) {
+  return ((unsigned long long)(hi - HI_BIAS) << 20) + (lo - LO_BIAS);
+}
+
+// 16 bytes of scores as floats; NaN becomes -inf (the maximum of a number and NaN is the number)
+template <class T>
+struct ScoreVec {
+  static constexpr int N = 16 / sizeof(T);
+};
+__device__ __forceinline__ void unpack_scores(uint4 u, float* l, float) {
+  l[0] = fmaxf(__uint_as_float(u.x), -INFINITY);
+  l[1] = fmaxf(__uint_as_float(u.y), -INFINITY);
+  l[2] = fmaxf(__uint_as_float(u.z), -INFINITY);
+  l[3] = fmaxf(__uint_as_float(u.w), -INFINITY);
+}
+__device__ __forceinline__ void unpack_scores(uint4 u, float* l, __nv_bfloat16) {
+  const unsigned w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const __nv_bfloat162 c = __hmax2(*reinterpret_cast<const __nv_bfloat162*>(&w[i]),
+                                     __nv_bfloat162(__ushort_as_bfloat16(0xff80), __ushort_as_bfloat16(0xff80)));
+    const unsigned b = *reinterpret_cast<const unsigned*>(&c);
+    l[2 * i] = __uint_as_float(b << 16);
+    l[2 * i + 1] = __uint_as_float(b & 0xffff0000u);
+  }
+}
+__device__ __forceinline__ void unpack_scores(uint4 u, float* l, __half) {
+  const unsigned w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const __half2 c = __hmax2(*reinterpret_cast<const __half2*>(&w[i]),
+                              __half2(__ushort_as_half(0xfc00), __ushort_as_half(0xfc00)));
+    const float2 f = __half22float2(c);
+    l[2 * i] = f.x;
+    l[2 * i + 1] = f.y;
+  }
+}
+// the pattern of -inf in each lane of a 32-bit word
+template <class T>
+__device__ __forceinline__ unsigned masked_word();
+template <>
+__device__ __forceinline__ unsigned masked_word<float>() { return 0xff800000u; }
+template <>
+__device__ __forceinline__ unsigned masked_word<__nv_bfloat16>() { return 0xff80ff80u; }
+template <>
+__device__ __forceinline__ unsigned masked_word<__half>() { return 0xfc00fc00u; }
+
+// a row's scores as aligned 16-byte vectors: vector v holds entries v N - skew .. v N - skew + N - 1,
+// those outside [0, n) read as masked.  No address outside the row is touched.
+template <class T>
+struct RowView {
+  const T* base;  // aligned, `skew` entries before the row
+  int skew;
+  int n;
+  int vectors;
+  __device__ __forceinline__ RowView(const T* row, int64_t n_)
+      : skew((int)((reinterpret_cast<uintptr_t>(row) & 15) / sizeof(T))), n((int)n_) {
+    base = row - skew;
+    vectors = (skew + n + ScoreVec<T>::N - 1) / ScoreVec<T>::N;
+  }
+  __device__ __forceinline__ uint4 fetch(int v) const {
+    constexpr int N = ScoreVec<T>::N;
+    const int first = v * N - skew;
+    if (first >= 0 && first + N <= n) return __ldg(reinterpret_cast<const uint4*>(base) + v);
+    union {
+      uint4 u;
+      T t[N];
+      unsigned w[4];
+    } x;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x.w[i] = masked_word<T>();
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (first + i >= 0 && first + i < n) x.t[i] = base[skew + first + i];
+    return x.u;
+  }
+};
+
 inline int type_bytes(int32_t type) { return type == ERC_F32 ? 4 : 2; }
 
 // calls f with a value of the C++ type behind an erc_type (checked by the caller)

@@ -4,13 +4,20 @@
 // With integer weights w_i (choice.cuh) every filter is a threshold in the order (score descending,
 // index ascending): the kept set is {score > theta} and the first `ties` entries at theta.  A row's
 // draw is the first kept index whose inclusive weight sum in index order exceeds floor(x W / 2^64).
+#include <atomic>
+
 #include "choice.cuh"
 
 namespace erc {
 namespace {
 
-constexpr int RT = 512;  // threads of a row's block
-constexpr int RW = RT / 32;
+constexpr int RT = 512;       // threads of a block
+constexpr int RW = RT / 32;   // its warps
+constexpr int MAX_C = 16;     // blocks of a row's cluster
+constexpr int LIST = 4096;    // candidates ranked in one block's shared memory
+constexpr int BINS = 2048;    // bins of one level of the descent
+constexpr int CBINS = 1024;   // bins of the threads' maxima
+constexpr int ROOM = 80 * 1024;  // bytes of a row in a block's shared memory (two blocks an SM)
 
 struct RowRule {
   float scale;               // log2(e) / T
@@ -35,17 +42,35 @@ __device__ __forceinline__ RowRule row_rule(const erc_sample_rule& r, int64_t ro
   return o;
 }
 
+__device__ __forceinline__ unsigned cluster_rank() {
+  unsigned r;
+  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ void cluster_barrier() {
+  asm volatile(
+      "barrier.cluster.arrive.release.aligned;\n\t"
+      "barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// address of the same shared variable in block `rank` of this cluster
 template <class V>
-__device__ __forceinline__ V block_sum(V v, V* part) {
-#pragma unroll
-  for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-  __syncthreads();
-  if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = v;
-  __syncthreads();
-  V s = 0;
-#pragma unroll
-  for (int i = 0; i < RW; ++i) s += part[i];
-  return s;
+__device__ __forceinline__ unsigned peer(const V* local, unsigned rank) {
+  unsigned a = (unsigned)__cvta_generic_to_shared(local), r;
+  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(rank));
+  return r;
+}
+__device__ __forceinline__ unsigned ld_peer(const unsigned* p, unsigned rank) {
+  unsigned v;
+  asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(peer(p, rank)) : "memory");
+  return v;
+}
+__device__ __forceinline__ unsigned long long ld_peer(const unsigned long long* p, unsigned rank) {
+  unsigned long long v;
+  asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(peer(p, rank)) : "memory");
+  return v;
+}
+__device__ __forceinline__ void add_peer(unsigned* p, unsigned rank, unsigned v) {
+  asm volatile("red.shared::cluster.add.u32 [%0], %1;" ::"r"(peer(p, rank)), "r"(v) : "memory");
 }
 
 // exclusive sum over the block's threads; *total receives the block's sum
@@ -61,189 +86,643 @@ __device__ __forceinline__ V block_exclusive(V v, V* part, V* total) {
   __syncthreads();
   if (lane == 31) part[warp] = x;
   __syncthreads();
-  V base = 0, all = 0;
+  V s = lane < RW ? part[lane] : V(0);
 #pragma unroll
-  for (int i = 0; i < RW; ++i) {
-    if (i == warp) base = all;
-    all += part[i];
+  for (int o = 1; o < RW; o <<= 1) {
+    const V y = __shfl_up_sync(0xffffffffu, s, o);
+    if (lane >= o) s += y;
   }
-  *total = all;
-  return base + x - v;
+  *total = __shfl_sync(0xffffffffu, s, RW - 1);
+  const V base = __shfl_sync(0xffffffffu, s, warp ? warp - 1 : 0);
+  return (warp ? base : V(0)) + x - v;
 }
 
-template <class T>
-__global__ void __launch_bounds__(RT) k_sample_rows(int64_t n, const T* __restrict__ logits,
-                                                    int64_t stride,
-                                                    const uint64_t* __restrict__ words,
-                                                    erc_sample_rule rule, int32_t* __restrict__ ids,
-                                                    float* __restrict__ logp,
-                                                    int32_t* __restrict__ kept) {
-  __shared__ unsigned long long mass[256];
-  __shared__ unsigned count[256];
-  __shared__ unsigned long long part64[RW];
-  __shared__ unsigned part32[RW];
-  __shared__ unsigned s_digit, s_count;
-  __shared__ unsigned long long s_mass;
-  __shared__ int s_found;
-  const int tid = threadIdx.x;
-  const int64_t row = blockIdx.x;
-  const T* x = logits + row * stride;
-  const RowRule r = row_rule(rule, row);
+struct Part {  // what a stretch of the row holds: mass and number above theta, entries at theta
+  unsigned long long mass;
+  unsigned above, tied;
+};
 
-  float m = -INFINITY;
-  for (int64_t i = tid; i < n; i += RT) m = fmaxf(m, clean_score(to_f32(x[i])));
-  {
-    unsigned k = order_key(m);
-    k = __reduce_max_sync(0xffffffffu, k);
-    if ((tid & 31) == 0) part32[tid >> 5] = k;
-    __syncthreads();
-    for (int i = 0; i < RW; ++i) k = max(k, part32[i]);
-    m = order_value(k);
-    __syncthreads();
-  }
-  if (m == -INFINITY) {
-    if (tid == 0) {
-      ids[row] = -1;
-      logp[row] = -INFINITY;
-      kept[row] = 0;
-    }
-    return;
-  }
-  auto weight = [&](float l) -> unsigned long long {
-    if (l == -INFINITY) return 0ull;
-    const unsigned long long w = fixed_weight(below_max(l, m, r.scale));
-    return w >= r.least ? w : 0ull;
+struct Shared {
+  unsigned long long part64[RW], mass[RW], total64;
+  unsigned part32[RW], above[RW], tied[RW];
+  unsigned long long sub_mass[RW];  // of the parts of the drawn region
+  unsigned sub_tied[RW];
+  unsigned top, low;          // the block's largest entry and smallest thread maximum, as keys
+  unsigned number;            // candidates of this block
+  unsigned theta, ties, some; // what block 0 decided from the list
+  unsigned digit;             // a level's bin
+  unsigned long long over;    // a level's sum before that bin
+  union {
+    unsigned bins[3][BINS];
+    unsigned list[LIST];
+    unsigned count[CBINS];
   };
+};
 
-  // radix descent, eight bits of the key at a time: theta is the key at which the running count
-  // (top-k) or the running mass (top-p) over larger entries reaches its bound
-  unsigned theta = 0, ties = 0xffffffffu;
-  if (r.top_k != 0xffffffffu) {
-    unsigned prefix = 0, left = r.top_k;
-    bool all = false;
-    for (int shift = 24; shift >= 0 && !all; shift -= 8) {
-      for (int b = tid; b < 256; b += RT) count[b] = 0;
-      __syncthreads();
-      for (int64_t i = tid; i < n; i += RT) {
-        const float l = clean_score(to_f32(x[i]));
-        const unsigned key = order_key(l);
-        if ((shift == 24 || (key >> (shift + 8)) == prefix) && weight(l))
-          atomicAdd(&count[(key >> shift) & 255], 1u);
-      }
-      __syncthreads();
-      if (tid == 0) {
-        unsigned c = 0;
-        int b = 255;
-        for (; b >= 0 && c + count[b] < left; --b) c += count[b];
-        s_found = b >= 0;
-        s_digit = b < 0 ? 0 : b;
-        s_count = c;
-      }
-      __syncthreads();
-      all = !s_found;
-      prefix = prefix << 8 | s_digit;
-      left -= s_count;
-      __syncthreads();
+template <class T>
+struct Row {
+  static constexpr int N = ScoreVec<T>::N;
+  RowView<T> view;
+  uint4* buffer;  // the first `resident` vectors of each warp's region
+  int resident;
+  int first, last, region;  // this block's vectors, and vectors of a warp's region
+  float max, scale;
+  bool odd;  // a maximum of +inf or an infinite scale
+  unsigned long long least;
+  float tmin;  // entries with t below this weigh less than `least`
+
+  __device__ __forceinline__ int begin(int warp) const { return first + warp * region; }
+  __device__ __forceinline__ int end(int warp) const { return min(last, begin(warp) + region); }
+  // vector `at` of warp `warp`'s region; masked from `stop` on
+  __device__ __forceinline__ uint4 get(int warp, int at, int stop) const {
+    if (at >= stop) {
+      const unsigned w = masked_word<T>();
+      return make_uint4(w, w, w, w);
     }
-    if (!all) {
-      theta = prefix;
-      ties = left;
+    const int i = at - begin(warp);
+    return i < resident ? buffer[warp * resident + i] : view.fetch(at);
+  }
+  __device__ __forceinline__ void scores(uint4 u, float* l) const { unpack_scores(u, l, T()); }
+  __device__ __forceinline__ float scaled(float l) const {
+    return odd ? below_max(l, max, scale) : __fmul_rn(__fsub_rn(l, max), scale);
+  }
+  // the weight of a score, 0 if it is not eligible
+  __device__ __forceinline__ unsigned long long weight(float l) const {
+    if (l == -INFINITY) return 0ull;
+    const unsigned long long w = fixed_weight(below_max(l, max, scale));
+    return w >= least ? w : 0ull;
+  }
+};
+
+// mass, numbers and ties of vectors [from, to) of a warp's region, over its lanes
+template <class T>
+__device__ Part measure(const Row<T>& r, int warp, int from, int to, float theta) {
+  constexpr int N = Row<T>::N;
+  const int lane = threadIdx.x & 31;
+  Part p = {0, 0, 0};
+  unsigned hi = 0, lo = 0, parts = 0;
+  for (int at = from + lane; at - lane < to; at += 32) {
+    float l[N], t[N];
+    r.scores(r.get(warp, at, to), l);
+    float best = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < N; ++i) best = fmaxf(best, l[i]);
+    if (!(best >= theta) || best == -INFINITY) continue;
+    best = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      t[i] = r.scaled(l[i]);
+      best = fmaxf(best, t[i]);
+    }
+    if (!(best >= r.tmin)) continue;
+    if (r.least == 1 && theta == -INFINITY) {
+#pragma unroll
+      for (int i = 0; i < N; i += 2) {
+        unsigned h[2], w[2];
+        float v[2];
+        weight_parts(t[i], t[i + 1], h, w, v);
+        hi += h[0] + h[1];
+        lo += w[0] + w[1];
+        p.above += (v[0] >= 0x1p-41f) + (v[1] >= 0x1p-41f);
+      }
+      parts += N;
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; i += 2) {
+        unsigned h[2], w[2];
+        float v[2];
+        weight_parts(t[i], t[i + 1], h, w, v);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const unsigned long long x = join_parts(h[j], w[j]);
+          const bool in = x >= r.least && l[i + j] >= theta;
+          if (in && l[i + j] > theta) {
+            p.mass += x;
+            ++p.above;
+          } else if (in) {
+            ++p.tied;
+          }
+        }
+      }
     }
   }
-  if (r.part != 0xffffffffu) {
-    // entries at theta all weigh the same, so top-k's own cut is a bound on their number
-    unsigned long long above = 0, tied = 0, wt = 0;
-    for (int64_t i = tid; i < n; i += RT) {
-      const float l = clean_score(to_f32(x[i]));
-      const unsigned key = order_key(l);
-      const unsigned long long w = weight(l);
-      if (key > theta) above += w;
-      else if (key == theta && w) ++tied;
+  p.mass += ((unsigned long long)(hi - parts * HI_BIAS) << 20) + (lo - parts * LO_BIAS);
+  p.above = __reduce_add_sync(0xffffffffu, p.above);
+  p.tied = __reduce_add_sync(0xffffffffu, p.tied);
+#pragma unroll
+  for (int o = 16; o; o >>= 1) p.mass += __shfl_xor_sync(0xffffffffu, p.mass, o);
+  return p;
+}
+
+// The row's kept mass by warps of the cluster: every thread i < C * RW gets the place of warp i's
+// region in it.  theta = -inf: no threshold.
+struct Measured {
+  unsigned long long before, kept, total, above_mass;
+  unsigned ties_before, number, tied;
+};
+template <class T>
+__device__ Measured measure_row(Shared& s, const Row<T>& r, int C, float theta, unsigned ties) {
+  const int tid = threadIdx.x, warp = tid >> 5;
+  const Part p = measure(r, warp, r.begin(warp), r.end(warp), theta);
+  if ((tid & 31) == 0) {
+    s.mass[warp] = p.mass;
+    s.above[warp] = p.above;
+    s.tied[warp] = p.tied;
+  }
+  cluster_barrier();
+  Part q = {0, 0, 0};
+  if (tid < C * RW) {
+    q.mass = ld_peer(&s.mass[tid % RW], tid / RW);
+    q.above = ld_peer(&s.above[tid % RW], tid / RW);
+    q.tied = ld_peer(&s.tied[tid % RW], tid / RW);
+  }
+  Measured m;
+  unsigned tied, above;
+  m.ties_before = block_exclusive(q.tied, s.part32, &tied);
+  block_exclusive(q.above, s.part32, &above);
+  block_exclusive(q.mass, s.part64, &m.above_mass);
+  m.kept = q.mass;
+  if (q.tied && m.ties_before < ties)
+    m.kept += min(q.tied, ties - m.ties_before) * r.weight(theta);
+  m.before = block_exclusive(m.kept, s.part64, &m.total);
+  m.tied = tied;
+  m.number = above + min(tied, ties);
+  return m;
+}
+
+// Descent to the key at which the running count (MASS: weight) over entries with keys in
+// [klo, khi], largest first, reaches `left` (> 0).  Returns false where it does not; else khi is
+// that key and `left` what is still wanted from the entries at it.  A level splits the keys into
+// at most BINS bins; a bin's weights are summed as three limbs of 14 bits, at most 2^18 of them in
+// a block, and the blocks of the cluster each add up a part of the bins.
+template <bool MASS, class T>
+__device__ bool descend(Shared& s, const Row<T>& r, unsigned rank, int C, unsigned klo,
+                        unsigned& khi, unsigned long long& left) {
+  constexpr int N = Row<T>::N;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int B = BINS / C;
+  for (;;) {
+    const unsigned span = khi - klo;
+    const int shift = span < BINS ? 0 : 21 - __clz(span);
+    const float lo_value = order_value(klo);
+    for (int b = tid; b < (MASS ? 3 : 1) * BINS; b += RT) s.bins[0][b] = 0;
+    __syncthreads();
+    const int stop = r.end(warp);
+    for (int at = r.begin(warp) + lane; at - lane < stop; at += 32) {
+      float l[N];
+      r.scores(r.get(warp, at, stop), l);
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+        if (l[i] >= lo_value) {
+          const unsigned d = khi - order_key(__fadd_rn(l[i], 0.f));
+          const unsigned long long w = d <= span ? r.weight(l[i]) : 0ull;
+          if (w) {
+            const unsigned b = d >> shift;
+            if (MASS) {
+              atomicAdd(&s.bins[0][b], (unsigned)w & 0x3fff);
+              atomicAdd(&s.bins[1][b], (unsigned)(w >> 14) & 0x3fff);
+              atomicAdd(&s.bins[2][b], (unsigned)(w >> 28));
+            } else {
+              atomicAdd(&s.bins[0][b], 1u);
+            }
+          }
+        }
     }
-    above = block_sum(above, part64);
-    tied = block_sum(tied, part64);
-    if (tied > ties) tied = ties;
-    if (tied) wt = weight(order_value(theta));
-    const unsigned long long total = above + tied * wt;
-    const unsigned long long want =
-        (total >> 31) * r.part + (((total & 0x7fffffffull) * r.part) >> 31);
-    const unsigned long long target = want ? want : 1ull;
-    if (above < target) {
-      const unsigned long long need = (target - above + wt - 1) / wt;
-      if (need < ties) ties = (unsigned)need;
-    } else {
-      unsigned prefix = 0;
-      unsigned long long left = target;
-      for (int shift = 24; shift >= 0; shift -= 8) {
-        for (int b = tid; b < 256; b += RT) mass[b] = 0;
-        __syncthreads();
-        for (int64_t i = tid; i < n; i += RT) {
-          const float l = clean_score(to_f32(x[i]));
-          const unsigned key = order_key(l);
-          if (key > theta && (shift == 24 || (key >> (shift + 8)) == prefix)) {
-            const unsigned long long w = weight(l);
-            if (w) atomicAdd(&mass[(key >> shift) & 255], w);
+    cluster_barrier();
+    // this block's share of the bins: bins rank * B .., BINS / RT of them a thread at most
+    unsigned long long v[BINS / RT], mine = 0;
+    const int per = (B + RT - 1) / RT;
+#pragma unroll
+    for (int i = 0; i < BINS / RT; ++i) {
+      v[i] = 0;
+      const int b = tid * per + i;
+      if (i < per && b < B)
+        for (int c = 0; c < C; ++c) {
+          v[i] += ld_peer(&s.bins[0][rank * B + b], c);
+          if (MASS)
+            v[i] += ((unsigned long long)ld_peer(&s.bins[1][rank * B + b], c) << 14) +
+                    ((unsigned long long)ld_peer(&s.bins[2][rank * B + b], c) << 28);
+        }
+      mine += v[i];
+    }
+    unsigned long long sum;
+    unsigned long long before = block_exclusive(mine, s.part64, &sum);
+    if (tid == 0) s.total64 = sum;
+    cluster_barrier();
+    unsigned long long base = 0;
+    int owner = -1;
+    for (int c = 0; c < C; ++c) {
+      const unsigned long long q = ld_peer(&s.total64, c);
+      if (owner < 0) {
+        if (base + q >= left) owner = c;
+        else base += q;
+      }
+    }
+    if (owner == (int)rank) {
+      before += base;
+#pragma unroll
+      for (int i = 0; i < BINS / RT; ++i) {
+        if (v[i] && before < left && left <= before + v[i]) {
+          s.digit = rank * B + tid * per + i;
+          s.over = before;
+        }
+        before += v[i];
+      }
+    }
+    cluster_barrier();
+    if (owner < 0) return false;
+    const unsigned digit = ld_peer(&s.digit, owner);
+    left -= ld_peer(&s.over, owner);
+    khi -= digit << shift;
+    const unsigned width = (1u << shift) - 1;
+    if (khi - klo > width) klo = khi - width;
+    cluster_barrier();
+    if (klo == khi) return true;
+  }
+}
+
+// Ranks at most LIST candidates in block 0: top-k, then top-p, to (theta, ties).  Returns false,
+// with nothing decided, where there are more.  Candidates are the eligible entries whose distance
+// from the maximum is below `reach` (all of them: reach = inf).
+template <class T>
+__device__ bool rank_list(Shared& s, const Row<T>& r, const RowRule& rule, unsigned rank, int C,
+                          float inv, float reach, float& theta, unsigned& ties) {
+  constexpr int N = Row<T>::N;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  if (tid == 0) s.number = 0;
+  __syncthreads();
+  const int stop = r.end(warp);
+  for (int at = r.begin(warp) + lane; at - lane < stop; at += 32) {
+    float l[N];
+    r.scores(r.get(warp, at, stop), l);
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (__fmul_rn(__fsub_rn(r.max, l[i]), inv) < reach && r.weight(l[i])) {
+        const unsigned p = atomicAdd(&s.number, 1u);
+        if (p < LIST) s.list[p] = order_key(__fadd_rn(l[i], 0.f));
+      }
+  }
+  cluster_barrier();
+  unsigned all = 0, mine = 0;
+  for (int c = 0; c < C; ++c) {
+    const unsigned q = ld_peer(&s.number, c);
+    if (c == 0) mine = q;
+    all += q;
+  }
+  if (all > LIST) {
+    cluster_barrier();
+    return false;
+  }
+  if (rank == 0) {
+    unsigned at = mine;
+    for (int c = 1; c < C; ++c) {
+      const unsigned q = ld_peer(&s.number, c);
+      for (unsigned i = tid; i < q; i += RT) s.list[at + i] = ld_peer(&s.list[i], c);
+      at += q;
+    }
+    unsigned size = 2;
+    while (size < all) size *= 2;
+    for (unsigned i = all + tid; i < size; i += RT) s.list[i] = 0;
+    __syncthreads();
+    for (unsigned k = 2; k <= size; k *= 2)  // bitonic sort, largest first
+      for (unsigned j = k / 2; j; j /= 2) {
+        for (unsigned i = tid; i < size / 2; i += RT) {
+          const unsigned a = 2 * i - (i & (j - 1)), b = a + j;
+          const unsigned x = s.list[a], y = s.list[b];
+          if ((x < y) == ((a & k) == 0)) {
+            s.list[a] = y;
+            s.list[b] = x;
           }
         }
         __syncthreads();
-        if (tid == 0) {
-          unsigned long long c = 0;
-          int b = 255;
-          for (; b > 0 && c + mass[b] < left; --b) c += mass[b];
-          s_digit = b;
-          s_mass = c;
-        }
-        __syncthreads();
-        prefix = prefix << 8 | s_digit;
-        left -= s_mass;
-        __syncthreads();
       }
-      theta = prefix;
-      wt = weight(order_value(theta));
-      ties = (unsigned)((left + wt - 1) / wt);
+    // each thread takes LIST / RT consecutive candidates
+    const unsigned keep = min(all, rule.top_k);
+    unsigned long long w[LIST / RT], sum = 0, total;
+#pragma unroll
+    for (int i = 0; i < LIST / RT; ++i) {
+      const unsigned at_i = tid * (LIST / RT) + i;
+      w[i] = at_i < keep ? r.weight(order_value(s.list[at_i])) : 0ull;
+      sum += w[i];
+    }
+    unsigned long long before = block_exclusive(sum, s.part64, &total);
+    unsigned long long target = ~0ull;
+    if (rule.part != 0xffffffffu) {
+      target = (total >> 31) * rule.part + (((total & 0x7fffffffull) * rule.part) >> 31);
+      if (!target) target = 1;
+    }
+    unsigned kept = 0;
+#pragma unroll
+    for (int i = 0; i < LIST / RT; ++i) {
+      if (w[i] && before < target) ++kept;
+      before += w[i];
+    }
+    unsigned number;
+    block_exclusive(kept, s.part32, &number);
+    if (tid == 0) {
+      // (theta, ties): the last kept key, and how many of the kept ones have it
+      const unsigned key = number ? s.list[number - 1] : 0u;
+      unsigned lo = 0, hi = number;  // first of the kept with that key
+      while (lo < hi) {
+        const unsigned mid = (lo + hi) / 2;
+        if (s.list[mid] > key) lo = mid + 1;
+        else hi = mid;
+      }
+      s.theta = key;
+      s.ties = number - lo;
+    }
+  }
+  cluster_barrier();
+  theta = order_value(ld_peer(&s.theta, 0));
+  ties = ld_peer(&s.ties, 0);
+  return true;
+}
+
+template <class T>
+__device__ void sample_row(Shared& s, Row<T>& r, const RowRule& rule, unsigned rank, int C,
+                           uint64_t word, int32_t* id, float* logp, int32_t* kept) {
+  constexpr int N = Row<T>::N;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  // one pass over memory: the row's entries into shared memory, each thread's maximum
+  float tm = -INFINITY;
+  {
+    const int b = r.begin(warp), e = r.end(warp);
+    uint4* mine = r.buffer + warp * r.resident;
+#pragma unroll 4
+    for (int at = b + lane; at < e; at += 32) {
+      const uint4 u = r.view.fetch(at);
+      if (at - b < r.resident) mine[at - b] = u;
+      float l[N];
+      r.scores(u, l);
+#pragma unroll
+      for (int i = 0; i < N; ++i) tm = fmaxf(tm, l[i]);
+    }
+  }
+  tm = __fadd_rn(tm, 0.f);
+  {
+    const unsigned k = order_key(tm);
+    const unsigned hi = __reduce_max_sync(0xffffffffu, k);
+    const unsigned lo = __reduce_min_sync(0xffffffffu, tm == -INFINITY ? 0xffffffffu : k);
+    if (lane == 0) {
+      s.part32[warp] = hi;
+      s.above[warp] = lo;
+    }
+    for (int b = tid; b < CBINS; b += RT) s.count[b] = 0;
+    __syncthreads();
+    if (warp == 0) {
+      const unsigned h = __reduce_max_sync(0xffffffffu, lane < RW ? s.part32[lane] : 0u);
+      const unsigned w = __reduce_min_sync(0xffffffffu, lane < RW ? s.above[lane] : 0xffffffffu);
+      if (lane == 0) {
+        s.top = h;
+        s.low = w;
+      }
+    }
+  }
+  cluster_barrier();
+  unsigned top = 0, low = 0xffffffffu;
+  {
+    const unsigned t = lane < C ? ld_peer(&s.top, lane) : 0u;
+    const unsigned w = lane < C ? ld_peer(&s.low, lane) : 0xffffffffu;
+    top = __reduce_max_sync(0xffffffffu, t);
+    low = __reduce_min_sync(0xffffffffu, w);
+  }
+  r.max = order_value(top);
+  if (r.max == -INFINITY) {  // the same in every block of the cluster
+    if (rank == 0 && tid == 0) {
+      *id = -1;
+      *logp = -INFINITY;
+      *kept = 0;
+    }
+    return;
+  }
+  r.scale = rule.scale;
+  r.least = rule.least;
+  r.odd = r.max == INFINITY || r.scale > 3.4028234e38f;
+  r.tmin = rule.least <= 1 ? -41.5f : log2f((float)rule.least - 0.5f) - 40.01f;
+
+  float theta = -INFINITY;
+  unsigned ties = 0xffffffffu;
+  const bool by_k = rule.top_k < (unsigned)r.view.n, by_p = rule.part != 0xffffffffu;
+  bool done = false, limited = false;
+  if (by_k && !r.odd) {
+    // At least top_k entries lie no lower than the top_k-th best of the threads' maxima: those down
+    // to its bin are the candidates.
+    const float inv = __fdiv_rn(1023.f, __fsub_rn(r.max, order_value(low)));
+    if (inv < 1e30f) {
+      if (r.weight(tm)) {
+        const unsigned b = min((unsigned)(int)__fmul_rn(__fsub_rn(r.max, tm), inv), CBINS - 1u);
+        add_peer(&s.count[b], 0, 1u);
+      }
+      cluster_barrier();
+      unsigned c[CBINS / RT], sum = 0, all;
+#pragma unroll
+      for (int i = 0; i < CBINS / RT; ++i) {
+        c[i] = ld_peer(&s.count[tid * (CBINS / RT) + i], 0);
+        sum += c[i];
+      }
+      unsigned before = block_exclusive(sum, s.part32, &all);
+#pragma unroll
+      for (int i = 0; i < CBINS / RT; ++i) {
+        if (before < rule.top_k && rule.top_k <= before + c[i]) s.digit = tid * (CBINS / RT) + i;
+        before += c[i];
+      }
+      cluster_barrier();
+      if (all >= rule.top_k)
+        done = rank_list(s, r, rule, rank, C, inv, (float)s.digit + 1.f, theta, ties);
+      else if (rule.least > 1)
+        done = rank_list(s, r, rule, rank, C, 0.f, 1.f, theta, ties);
+      limited = done;
+    }
+  }
+  if (!done) {
+    // keys an eligible entry can have: t >= tmin, with room for its roundings
+    const float edge = r.odd ? -INFINITY
+                             : __fadd_rn(r.max, __fdiv_rn(r.tmin - 0.5f, r.scale)) - 1e-5f * fabsf(r.max);
+    unsigned klo = order_key(fmaxf(edge, -3.4028235e38f));
+    if (by_k) {
+      unsigned khi = top;
+      unsigned long long left = rule.top_k;
+      if (descend<false>(s, r, rank, C, klo, khi, left)) {
+        theta = order_value(khi);
+        ties = (unsigned)left;
+        limited = true;
+      }
+    }
+    if (by_p) {
+      const Measured m = measure_row(s, r, C, theta, ties);
+      cluster_barrier();
+      unsigned long long target =
+          (m.total >> 31) * rule.part + (((m.total & 0x7fffffffull) * rule.part) >> 31);
+      if (!target) target = 1;
+      if (m.above_mass < target) {
+        const unsigned long long wt = r.weight(theta);
+        ties = (unsigned)((target - m.above_mass + wt - 1) / wt);
+      } else {
+        if (limited) klo = order_key(theta) + 1;
+        unsigned khi = top;
+        unsigned long long left = target;
+        descend<true>(s, r, rank, C, klo, khi, left);
+        theta = order_value(khi);
+        const unsigned long long wt = r.weight(theta);
+        ties = (unsigned)((left + wt - 1) / wt);
+      }
     }
   }
 
-  // the kept entries in index order: their total, then the draw
-  unsigned long long total = 0;
-  unsigned number = 0;
-  int found = -1;
-  unsigned long long at = 0, mine = 0;
-  for (int pass = 0; pass < 2; ++pass) {
-    unsigned long long before = 0;
-    unsigned tied = 0, some = 0;
-    for (int64_t base = 0; base < n; base += RT) {
-      const int64_t i = base + tid;
-      const float l = i < n ? clean_score(to_f32(x[i])) : -INFINITY;
-      const unsigned key = order_key(l);
-      unsigned long long w = key >= theta ? weight(l) : 0ull;
-      unsigned all;
-      const unsigned mytie = w && key == theta;
-      const unsigned rank = tied + block_exclusive(mytie, part32, &all);
-      tied += all;
-      if (mytie && rank >= ties) w = 0;
-      unsigned long long sum;
-      const unsigned long long ex = before + block_exclusive(w, part64, &sum);
-      if (pass == 1 && w && ex <= at && at < ex + w) {
-        found = (int)i;
-        mine = w;
+  // the draw: the warp's region it falls in, then a sixteenth of that region, then a vector
+  const Measured m = measure_row(s, r, C, theta, ties);
+  const unsigned long long at = __umul64hi(word, m.total);
+  if (tid < C * RW && at >= m.before && at - m.before < m.kept) {
+    s.digit = tid;
+    s.over = m.before;
+    s.some = m.ties_before;
+  }
+  __syncthreads();
+  const int owner = (int)s.digit;
+  if (owner / RW == (int)rank) {
+    const unsigned long long wt = theta == -INFINITY ? 0ull : r.weight(theta);
+    const int ow = owner % RW, ob = r.begin(ow), oe = r.end(ow);
+    const int step = ((oe - ob + 31) / 32 + RW - 1) / RW * 32;  // vectors of a sixteenth
+    const int from = min(oe, ob + warp * step), to = min(oe, from + step);
+    unsigned long long before = s.over;
+    unsigned ties_before = s.some;
+    const Part p = measure(r, ow, from, to, theta);
+    if (lane == 0) {
+      s.sub_mass[warp] = p.mass;
+      s.sub_tied[warp] = p.tied;
+    }
+    __syncthreads();
+    auto with_ties = [&](unsigned long long mass, unsigned tied, unsigned earlier) {
+      return tied && earlier < ties ? mass + min(tied, ties - earlier) * wt : mass;
+    };
+    for (int w = 0; w < warp; ++w) {
+      before += with_ties(s.sub_mass[w], s.sub_tied[w], ties_before);
+      ties_before += s.sub_tied[w];
+    }
+    const unsigned long long here = with_ties(p.mass, p.tied, ties_before);
+    if (at >= before && at - before < here) {  // one warp: 32 vectors at a time
+      for (int v0 = from; v0 < to; v0 += 32) {
+        float l[N];
+        r.scores(r.get(ow, v0 + lane, to), l);
+        unsigned long long mass = 0;
+        unsigned tied = 0;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          const unsigned long long w = l[i] >= theta ? r.weight(l[i]) : 0ull;
+          if (w && l[i] == theta) ++tied;
+          else mass += w;
+        }
+        unsigned tied_to = tied;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+          const unsigned y = __shfl_up_sync(0xffffffffu, tied_to, o);
+          if (lane >= o) tied_to += y;
+        }
+        unsigned mine_before = ties_before + tied_to - tied;
+        const unsigned long long k = with_ties(mass, tied, mine_before);
+        unsigned long long k_to = k;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+          const unsigned long long y = __shfl_up_sync(0xffffffffu, k_to, o);
+          if (lane >= o) k_to += y;
+        }
+        unsigned long long b = before + k_to - k;
+        if (at >= b && at - b < k) {
+#pragma unroll
+          for (int i = 0; i < N; ++i) {
+            unsigned long long w = l[i] >= theta ? r.weight(l[i]) : 0ull;
+            if (w && l[i] == theta && mine_before++ >= ties) w = 0;
+            if (at >= b && at - b < w) {
+              const unsigned long long rest = m.total - w;
+              *id = (v0 + lane) * N - r.view.skew + i;
+              *kept = (int32_t)m.number;
+              *logp = w > rest ? log1pf(-__fdiv_rn(__ull2float_rn(rest), __ull2float_rn(m.total)))
+                               : logf(__fdiv_rn(__ull2float_rn(w), __ull2float_rn(m.total)));
+            }
+            b += w;
+          }
+        }
+        before += __shfl_sync(0xffffffffu, k_to, 31);
+        ties_before += __shfl_sync(0xffffffffu, tied_to, 31);
+        if (at < before) break;
       }
-      before += sum;
-      some += w != 0;
-    }
-    if (pass == 0) {
-      total = before;
-      number = block_sum(some, part32);
-      at = __umul64hi(words[row], total);
     }
   }
-  if (found >= 0) {
-    ids[row] = found;
-    kept[row] = (int32_t)number;
-    const unsigned long long rest = total - mine;
-    logp[row] = mine > rest ? log1pf(-__fdiv_rn(__ull2float_rn(rest), __ull2float_rn(total)))
-                            : logf(__fdiv_rn(__ull2float_rn(mine), __ull2float_rn(total)));
+}
+
+// A cluster of C blocks takes a row: block c its c-th contiguous part, each of the block's warps a
+// contiguous region of that, so that the index order is the order of (block, warp, vector, lane).
+template <class T>
+__global__ void __launch_bounds__(RT, 2)
+    k_sample_rows(int64_t rows, int64_t n, const T* __restrict__ logits, int64_t stride,
+                  const uint64_t* __restrict__ words, erc_sample_rule rule, int C, int resident,
+                  int32_t* __restrict__ ids, float* __restrict__ logp, int32_t* __restrict__ kept) {
+  extern __shared__ uint4 buffer[];
+  __shared__ Shared s;
+  const unsigned rank = cluster_rank();
+  for (int64_t row = blockIdx.x / C; row < rows; row += gridDim.x / C) {
+    Row<T> r = {RowView<T>(logits + row * stride, n)};
+    const int part = (r.view.vectors + C - 1) / C;
+    r.buffer = buffer;
+    r.resident = resident;
+    r.first = min(r.view.vectors, (int)rank * part);
+    r.last = min(r.view.vectors, r.first + part);
+    r.region = (part + RT - 1) / RT * 32;
+    sample_row(s, r, row_rule(rule, row), rank, C, words[row], &ids[row], &logp[row], &kept[row]);
+    cluster_barrier();
   }
+}
+
+// Vectors of a warp's region kept in shared memory, blocks of a cluster, and the dynamic bytes.
+// C is the smallest power of two whose blocks can hold the row (16 at most), then as many more as
+// the machine has room for at two blocks an SM, while a block still gets 4096 entries.
+struct Shape {
+  int C, resident;
+  size_t bytes;
+};
+Shape shape_of(int64_t rows, int64_t n, int elt) {
+  const int64_t vectors = (n * elt + 15) / 16 + 1;
+  auto region = [&](int C) { return ((vectors + C - 1) / C + RT - 1) / RT * 32; };
+  Shape h;
+  h.C = 1;
+  while (h.C < MAX_C && region(h.C) * RW * 16 > ROOM) h.C *= 2;
+  while (h.C < MAX_C && rows * h.C * 2 <= 2 * sm_count() && n >= h.C * 2 * 4096) h.C *= 2;
+  const int64_t most = ROOM / (RW * 16) / 32 * 32;
+  h.resident = (int)(region(h.C) < most ? region(h.C) : most);
+  h.bytes = (size_t)h.resident * RW * 16;
+  return h;
+}
+
+template <class T>
+erc_status launch_rows(int64_t rows, int64_t n, const T* logits, int64_t stride,
+                       const uint64_t* words, const erc_sample_rule& rule, int32_t* ids,
+                       float* logp, int32_t* kept, cudaStream_t s) {
+  const Shape h = shape_of(rows, n, (int)sizeof(T));
+  static std::atomic<uint64_t> ready{0};  // devices whose kernel has its attributes, one bit each
+  int dev = 0;
+  ERC_CUDA(cudaGetDevice(&dev));
+  if (dev >= 64 || !(ready.load(std::memory_order_acquire) >> dev & 1)) {
+    ERC_CUDA(cudaFuncSetAttribute(k_sample_rows<T>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                  ROOM));
+    ERC_CUDA(cudaFuncSetAttribute(k_sample_rows<T>, cudaFuncAttributeNonPortableClusterSizeAllowed,
+                                  1));
+    if (dev < 64) ready.fetch_or(1ull << dev, std::memory_order_release);
+  }
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(rows < 65535 ? rows : 65535) * h.C);
+  cfg.blockDim = dim3(RT);
+  cfg.dynamicSmemBytes = h.bytes;
+  cfg.stream = s;
+  cudaLaunchAttribute at = {};
+  at.id = cudaLaunchAttributeClusterDimension;
+  at.val.clusterDim.x = h.C;
+  at.val.clusterDim.y = at.val.clusterDim.z = 1;
+  cfg.attrs = &at;
+  cfg.numAttrs = 1;
+  ERC_CUDA(cudaLaunchKernelEx(&cfg, k_sample_rows<T>, rows, n, logits, stride, words, rule, h.C,
+                              h.resident, ids, logp, kept));
+  count_launches(1);
+  return ERC_OK;
 }
 
 }  // namespace
@@ -271,10 +750,7 @@ extern "C" erc_status erc_sample_rows(int64_t rows, int64_t n, const void* logit
   ERC_REQUIRE(reinterpret_cast<uintptr_t>(logits) % type_bytes(type) == 0, "misaligned logits");
   return with_type(type, [&](auto t) {
     using T = decltype(t);
-    k_sample_rows<T><<<(unsigned)rows, RT, 0, as_stream(stream)>>>(
-        n, static_cast<const T*>(logits), stride, words, *rule, ids, logp, kept);
-    count_launches(1);
-    ERC_CUDA(cudaGetLastError());
-    return ERC_OK;
+    return launch_rows<T>(rows, n, static_cast<const T*>(logits), stride, words, *rule, ids, logp,
+                          kept, as_stream(stream));
   });
 }
