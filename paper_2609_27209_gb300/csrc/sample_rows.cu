@@ -693,10 +693,191 @@ Shape shape_of(int64_t rows, int64_t n, int elt) {
   return h;
 }
 
+// ------------------------------------------------------------------------------------------------
+// short rows: a warp takes a row, `q` consecutive entries a lane (odd: no bank conflicts)
+// ------------------------------------------------------------------------------------------------
+constexpr int SW = 8;          // warps of a block
+constexpr int SHORT = 1024;    // longest row
+inline int short_q(int64_t n) { return (int)((n + 31) / 32) | 1; }
+
+__device__ __forceinline__ unsigned long long warp_sum(unsigned long long v) {
+#pragma unroll
+  for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  return v;
+}
+template <class V>
+__device__ __forceinline__ V warp_inclusive(V v) {
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const V y = __shfl_up_sync(0xffffffffu, v, o);
+    if ((int)(threadIdx.x & 31) >= o) v += y;
+  }
+  return v;
+}
+
+// The largest key K in [floor, top] with sum(K) >= want, where sum(K) is what entries with keys of
+// at least K sum to and sum(floor) >= want: the bits below the highest one in which the two ends
+// differ, one by one.
+template <class F>
+__device__ __forceinline__ unsigned largest_key(unsigned floor, unsigned top,
+                                                unsigned long long want, F&& sum) {
+  const unsigned differ = floor ^ top;
+  if (!differ) return top;
+  int bit = 31 - __clz(differ);
+  unsigned key = top >> bit >> 1 << 1 << bit;  // the shared bits (bit may be 31)
+  for (; bit >= 0; --bit) {
+    const unsigned c = key | 1u << bit;
+    if (c <= floor || (c <= top && sum(c) >= want)) key = c;
+  }
+  return key;
+}
+
+template <class T, bool MASS>
+__global__ void __launch_bounds__(SW * 32)
+    k_sample_short(int64_t rows, int n, int q, const T* __restrict__ logits, int64_t stride,
+                   const uint64_t* __restrict__ words, erc_sample_rule rule,
+                   int32_t* __restrict__ ids, float* __restrict__ logp,
+                   int32_t* __restrict__ kept) {
+  extern __shared__ uint64_t short_buffer[];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  uint64_t* weights = short_buffer + (MASS ? warp * q * 32 : 0);  // MASS only
+  unsigned* keys = reinterpret_cast<unsigned*>(short_buffer + (MASS ? SW * q * 32 : 0)) + warp * q * 32;
+  for (int64_t row = (int64_t)blockIdx.x * SW + warp; row < rows; row += (int64_t)gridDim.x * SW) {
+    const T* x = logits + row * stride;
+    const RowRule r = row_rule(rule, row);
+    float m = -INFINITY;
+    for (int i = lane; i < q * 32; i += 32) {
+      const float l = i < n ? clean_score(to_f32(x[i])) : -INFINITY;
+      m = fmaxf(m, l);
+      keys[i] = __float_as_uint(l);
+    }
+    const unsigned top = __reduce_max_sync(0xffffffffu, order_key(__fadd_rn(m, 0.f)));
+    m = order_value(top);
+    if (m == -INFINITY) {
+      if (lane == 0) {
+        ids[row] = -1;
+        logp[row] = -INFINITY;
+        kept[row] = 0;
+      }
+      __syncwarp();
+      continue;
+    }
+    const float least_t = r.least <= 1 ? -41.5f : log2f((float)r.least - 0.5f) - 40.01f;
+    __syncwarp();
+    // a lane's own entries: keys (0: not eligible) and their weights
+    unsigned* mine = keys + lane * q;
+    unsigned long long mass = 0;
+    unsigned above = 0, low = 0xffffffffu;
+    for (int i = 0; i < q; ++i) {
+      const float l = __uint_as_float(mine[i]);
+      const float t = l == -INFINITY ? -INFINITY : below_max(l, m, r.scale);
+      unsigned long long w = 0;
+      if (t >= least_t) {
+        w = fixed_weight(t);
+        if (w < r.least) w = 0;
+      }
+      const unsigned k = w ? order_key(l) : 0u;
+      mine[i] = k;
+      if (MASS) weights[lane * q + i] = w;
+      mass += w;
+      above += w != 0;
+      if (w) low = min(low, k);
+    }
+    auto weight_of = [&](unsigned k) {
+      return k ? fixed_weight(below_max(order_value(k), m, r.scale)) : 0ull;
+    };
+    unsigned theta = 0, ties = 0xffffffffu, tied = 0;
+    unsigned number = __reduce_add_sync(0xffffffffu, above);
+    const bool by_k = r.top_k < number;
+    if (by_k || (MASS && r.part != 0xffffffffu)) {
+      low = __reduce_min_sync(0xffffffffu, low);
+      auto count = [&](unsigned k) {
+        unsigned c = 0;
+        for (int i = 0; i < q; ++i) c += mine[i] >= k;
+        return __reduce_add_sync(0xffffffffu, c);
+      };
+      auto mass_of = [&](unsigned k) {
+        unsigned long long s = 0;
+        for (int i = 0; i < q; ++i)
+          if (mine[i] >= k) s += weights[lane * q + i];
+        return warp_sum(s);
+      };
+      if (by_k) {
+        theta = largest_key(low, top, r.top_k, [&](unsigned k) { return (unsigned long long)count(k); });
+        ties = r.top_k - (theta == 0xffffffffu ? 0u : count(theta + 1));
+        number = r.top_k;
+      }
+      if (MASS && r.part != 0xffffffffu) {
+        const unsigned long long wt = by_k ? weight_of(theta) : 0ull;
+        const unsigned long long over = by_k ? mass_of(theta + 1) : warp_sum(mass);
+        const unsigned long long total = over + (by_k ? ties * wt : 0ull);
+        unsigned long long target =
+            (total >> 31) * r.part + (((total & 0x7fffffffull) * r.part) >> 31);
+        if (!target) target = 1;
+        if (over < target) {
+          ties = (unsigned)((target - over + wt - 1) / wt);
+        } else {
+          theta = largest_key(by_k ? theta + 1 : low, top, target, mass_of);
+          const unsigned long long more = mass_of(theta + 1), w = weight_of(theta);
+          ties = (unsigned)((target - more + w - 1) / w);
+        }
+        number = count(theta + 1) + ties;
+      }
+      mass = 0;
+      const unsigned long long wt = weight_of(theta);
+      for (int i = 0; i < q; ++i) {
+        if (mine[i] > theta) mass += MASS ? weights[lane * q + i] : weight_of(mine[i]);
+        tied += mine[i] == theta;
+      }
+      const unsigned earlier = warp_inclusive(tied) - tied;
+      tied = earlier < ties ? min(tied, ties - earlier) : 0u;  // of the lane's ties, those kept
+      mass += tied * wt;
+    }
+    const unsigned long long to = warp_inclusive(mass);
+    const unsigned long long total = __shfl_sync(0xffffffffu, to, 31);
+    const unsigned long long at = __umul64hi(words[row], total);
+    const int owner = 31 - __clz(__ballot_sync(0xffffffffu, to - mass <= at && mass));
+    unsigned long long before = __shfl_sync(0xffffffffu, to - mass, owner);
+    unsigned left = __shfl_sync(0xffffffffu, tied, owner);  // ties of the owner's that are kept
+    __syncwarp();
+    for (int i0 = 0; i0 < q; i0 += 32) {  // the owner's entries, one a lane
+      const unsigned k = i0 + lane < q ? keys[owner * q + i0 + lane] : 0u;
+      const bool tie = theta && k == theta;
+      const unsigned earlier = __popc(__ballot_sync(0xffffffffu, tie) & ((1u << lane) - 1));
+      const unsigned long long w = k > theta || (tie && earlier < left) ? weight_of(k) : 0ull;
+      const unsigned long long in = before + warp_inclusive(w);
+      if (at < in && in - w <= at) {
+        const unsigned long long rest = total - w;
+        ids[row] = owner * q + i0 + lane;
+        kept[row] = (int32_t)number;
+        logp[row] = w > rest ? log1pf(-__fdiv_rn(__ull2float_rn(rest), __ull2float_rn(total)))
+                             : logf(__fdiv_rn(__ull2float_rn(w), __ull2float_rn(total)));
+      }
+      left -= min(left, (unsigned)__popc(__ballot_sync(0xffffffffu, tie)));
+      before = __shfl_sync(0xffffffffu, in, 31);
+    }
+    __syncwarp();
+  }
+}
+
 template <class T>
 erc_status launch_rows(int64_t rows, int64_t n, const T* logits, int64_t stride,
                        const uint64_t* words, const erc_sample_rule& rule, int32_t* ids,
                        float* logp, int32_t* kept, cudaStream_t s) {
+  if (n <= SHORT) {
+    const int q = short_q(n);
+    const bool mass = rule.top_p < 1.f || rule.top_p_rows;
+    const size_t bytes = (size_t)SW * q * 32 * (mass ? 12 : 4);
+    auto kernel = mass ? k_sample_short<T, true> : k_sample_short<T, false>;
+    if (bytes > 48 * 1024)
+      ERC_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes));
+    const int64_t blocks = (rows + SW - 1) / SW;
+    kernel<<<(unsigned)(blocks < 0x7fffffff ? blocks : 0x7fffffff), SW * 32, bytes, s>>>(
+        rows, (int)n, q, logits, stride, words, rule, ids, logp, kept);
+    count_launches(1);
+    ERC_CUDA(cudaGetLastError());
+    return ERC_OK;
+  }
   const Shape h = shape_of(rows, n, (int)sizeof(T));
   static std::atomic<uint64_t> ready{0};  // devices whose kernel has its attributes, one bit each
   int dev = 0;
