@@ -96,6 +96,11 @@ __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
   asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
   return r;
 }
+__device__ __forceinline__ uint64_t add2_rz(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rz.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
 __device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
   uint64_t r;
   asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
@@ -111,7 +116,7 @@ __device__ __forceinline__ uint64_t fma2_rz(uint64_t a, uint64_t b, uint64_t c) 
   return r;
 }
 
-constexpr unsigned HI_BIAS = 0x4B000000u, LO_BIAS = 0x25800000u;  // 2^23's pattern, and its half
+constexpr unsigned BIAS = 0x4B000000u;  // 2^23's pattern
 
 // weights of two scaled scores: hi and lo with their biases, and 2^t itself
 __device__ __forceinline__ void weight_parts(float t0, float t1, unsigned hi[2], unsigned lo[2],
@@ -135,17 +140,22 @@ __device__ __forceinline__ void weight_parts(float t0, float t1, unsigned hi[2],
   const uint64_t two20 = pair(1048576.f, 1048576.f), two23 = pair(8388608.f, 8388608.f);
   const uint64_t h = fma2_rz(vv, two20, two23);
   const uint64_t rest = fma2(vv, two20, add2(two23, h ^ 0x8000000080000000ull));
-  const uint64_t l = fma2_rz(rest, pair(2097152.f, 2097152.f), two23);
+  // rounded half up: half a unit is added, toward zero, before the floor
+  const uint64_t l = fma2_rz(add2_rz(rest, pair(0x1p-21f, 0x1p-21f)), two20, two23);
   float a, b;
   unpair(h, a, b);
   hi[0] = __float_as_uint(a);
   hi[1] = __float_as_uint(b);
   unpair(l, a, b);
-  lo[0] = (__float_as_uint(a) + 1) >> 1;
-  lo[1] = (__float_as_uint(b) + 1) >> 1;
+  lo[0] = __float_as_uint(a);
+  lo[1] = __float_as_uint(b);
 }
 __device__ __forceinline__ unsigned long long join_parts(unsigned hi, unsigned lo) {
-  return ((unsigned long long)(hi - HI_BIAS) << 20) + (lo - LO_BIAS);
+  return ((unsigned long long)(hi - BIAS) << 20) + (lo - BIAS);
+}
+// the sum of `count` weights from the sums of their parts
+__device__ __forceinline__ unsigned long long join_sums(unsigned hi, unsigned lo, unsigned count) {
+  return join_parts(hi - (count - 1) * BIAS, lo - (count - 1) * BIAS);
 }
 
 // 16 bytes of scores as floats; NaN becomes -inf (the maximum of a number and NaN is the number)

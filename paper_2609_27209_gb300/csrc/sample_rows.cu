@@ -15,9 +15,11 @@ constexpr int RT = 512;       // threads of a block
 constexpr int RW = RT / 32;   // its warps
 constexpr int MAX_C = 16;     // blocks of a row's cluster
 constexpr int LIST = 4096;    // candidates ranked in one block's shared memory
-constexpr int BINS = 2048;    // bins of one level of the descent
+constexpr int BINS = 1024;    // bins of one level of the descent
+constexpr int STEPS = 64;     // bins an octave of the weights' histogram
+constexpr int WBINS = 2048;   // its bins
 constexpr int CBINS = 1024;   // bins of the threads' maxima
-constexpr int ROOM = 80 * 1024;  // bytes of a row in a block's shared memory (two blocks an SM)
+constexpr int ROOM = 72 * 1024;  // bytes of a row in a block's shared memory (two blocks an SM)
 
 struct RowRule {
   float scale;               // log2(e) / T
@@ -103,7 +105,7 @@ struct Part {  // what a stretch of the row holds: mass and number above theta, 
 };
 
 struct Shared {
-  unsigned long long part64[RW], mass[RW], total64;
+  unsigned long long part64[RW], mass[RW], total64, sure64;
   unsigned part32[RW], above[RW], tied[RW];
   unsigned long long sub_mass[RW];  // of the parts of the drawn region
   unsigned sub_tied[RW];
@@ -111,12 +113,15 @@ struct Shared {
   unsigned number;            // candidates of this block
   unsigned theta, ties, some; // what block 0 decided from the list
   unsigned digit;             // a level's bin
+  unsigned first_bin, last_bin;  // of the weights' histogram
   unsigned long long over;    // a level's sum before that bin
   union {
     unsigned bins[3][BINS];
-    unsigned list[LIST];
     unsigned count[CBINS];
+    unsigned wbins[WBINS];
   };
+  unsigned list[LIST];        // candidates' keys
+  uint8_t from[LIST];         // and the warps whose regions hold them
 };
 
 template <class T>
@@ -206,7 +211,7 @@ __device__ Part measure(const Row<T>& r, int warp, int from, int to, float theta
       }
     }
   }
-  p.mass += ((unsigned long long)(hi - parts * HI_BIAS) << 20) + (lo - parts * LO_BIAS);
+  p.mass += join_sums(hi, lo, parts);
   p.above = __reduce_add_sync(0xffffffffu, p.above);
   p.tied = __reduce_add_sync(0xffffffffu, p.tied);
 #pragma unroll
@@ -221,14 +226,8 @@ struct Measured {
   unsigned ties_before, number, tied;
 };
 template <class T>
-__device__ Measured measure_row(Shared& s, const Row<T>& r, int C, float theta, unsigned ties) {
-  const int tid = threadIdx.x, warp = tid >> 5;
-  const Part p = measure(r, warp, r.begin(warp), r.end(warp), theta);
-  if ((tid & 31) == 0) {
-    s.mass[warp] = p.mass;
-    s.above[warp] = p.above;
-    s.tied[warp] = p.tied;
-  }
+__device__ Measured by_regions(Shared& s, const Row<T>& r, int C, float theta, unsigned ties) {
+  const int tid = threadIdx.x;
   cluster_barrier();
   Part q = {0, 0, 0};
   if (tid < C * RW) {
@@ -249,45 +248,66 @@ __device__ Measured measure_row(Shared& s, const Row<T>& r, int C, float theta, 
   m.number = above + min(tied, ties);
   return m;
 }
+template <class T>
+__device__ Measured measure_row(Shared& s, const Row<T>& r, int C, float theta, unsigned ties) {
+  const int warp = threadIdx.x >> 5;
+  const Part p = measure(r, warp, r.begin(warp), r.end(warp), theta);
+  if ((threadIdx.x & 31) == 0) {
+    s.mass[warp] = p.mass;
+    s.above[warp] = p.above;
+    s.tied[warp] = p.tied;
+  }
+  return by_regions(s, r, C, theta, ties);
+}
+
+// f(score) for every entry of the block: of its regions, or (LISTED) of its candidate list
+template <bool LISTED, class T, class F>
+__device__ __forceinline__ void each_score(const Shared& s, const Row<T>& r, float floor, F&& f) {
+  constexpr int N = Row<T>::N;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  if (LISTED) {
+    for (unsigned i = tid; i < s.number; i += RT) f(order_value(s.list[i]));
+    return;
+  }
+  const int stop = r.end(warp);
+  for (int at = r.begin(warp) + lane; at - lane < stop; at += 32) {
+    float l[N];
+    r.scores(r.get(warp, at, stop), l);
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (l[i] >= floor) f(l[i]);
+  }
+}
 
 // Descent to the key at which the running count (MASS: weight) over entries with keys in
 // [klo, khi], largest first, reaches `left` (> 0).  Returns false where it does not; else khi is
 // that key and `left` what is still wanted from the entries at it.  A level splits the keys into
 // at most BINS bins; a bin's weights are summed as three limbs of 14 bits, at most 2^18 of them in
 // a block, and the blocks of the cluster each add up a part of the bins.
-template <bool MASS, class T>
+template <bool MASS, bool LISTED, class T>
 __device__ bool descend(Shared& s, const Row<T>& r, unsigned rank, int C, unsigned klo,
                         unsigned& khi, unsigned long long& left) {
-  constexpr int N = Row<T>::N;
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int tid = threadIdx.x;
   const int B = BINS / C;
   for (;;) {
     const unsigned span = khi - klo;
-    const int shift = span < BINS ? 0 : 21 - __clz(span);
-    const float lo_value = order_value(klo);
+    const int shift = span < BINS ? 0 : 22 - __clz(span);
     for (int b = tid; b < (MASS ? 3 : 1) * BINS; b += RT) s.bins[0][b] = 0;
     __syncthreads();
-    const int stop = r.end(warp);
-    for (int at = r.begin(warp) + lane; at - lane < stop; at += 32) {
-      float l[N];
-      r.scores(r.get(warp, at, stop), l);
-#pragma unroll
-      for (int i = 0; i < N; ++i)
-        if (l[i] >= lo_value) {
-          const unsigned d = khi - order_key(__fadd_rn(l[i], 0.f));
-          const unsigned long long w = d <= span ? r.weight(l[i]) : 0ull;
-          if (w) {
-            const unsigned b = d >> shift;
-            if (MASS) {
-              atomicAdd(&s.bins[0][b], (unsigned)w & 0x3fff);
-              atomicAdd(&s.bins[1][b], (unsigned)(w >> 14) & 0x3fff);
-              atomicAdd(&s.bins[2][b], (unsigned)(w >> 28));
-            } else {
-              atomicAdd(&s.bins[0][b], 1u);
-            }
-          }
+    each_score<LISTED>(s, r, order_value(klo), [&](float l) {
+      const unsigned d = khi - order_key(__fadd_rn(l, 0.f));
+      const unsigned long long w = d <= span ? r.weight(l) : 0ull;
+      if (w) {
+        const unsigned b = d >> shift;
+        if (MASS) {
+          atomicAdd(&s.bins[0][b], (unsigned)w & 0x3fff);
+          atomicAdd(&s.bins[1][b], (unsigned)(w >> 14) & 0x3fff);
+          atomicAdd(&s.bins[2][b], (unsigned)(w >> 28));
+        } else {
+          atomicAdd(&s.bins[0][b], 1u);
         }
-    }
+      }
+    });
     cluster_barrier();
     // this block's share of the bins: bins rank * B .., BINS / RT of them a thread at most
     unsigned long long v[BINS / RT], mine = 0;
@@ -438,6 +458,203 @@ __device__ bool rank_list(Shared& s, const Row<T>& r, const RowRule& rule, unsig
   return true;
 }
 
+// Sum over the cluster of a value of each thread.
+__device__ unsigned long long cluster_sum(Shared& s, unsigned long long v, unsigned long long* slot,
+                                          int C) {
+  const int lane = threadIdx.x & 31;
+  unsigned long long sum;
+  block_exclusive(v, s.part64, &sum);
+  if (threadIdx.x == 0) *slot = sum;
+  cluster_barrier();
+  sum = lane < C ? ld_peer(slot, lane) : 0ull;
+#pragma unroll
+  for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+  return sum;
+}
+
+// Top-p alone over long rows.  One pass weighs the row and counts its entries by weight, STEPS bins
+// an octave: a bin's entries weigh within 1.1% of each other, so the counts bound the running mass
+// from both sides and leave a few bins in which theta lies.  A second pass weighs what is above
+// them, which is kept, and lists their entries; theta is found in the list.  Bins are stretches of
+// t (floor(-t STEPS), an exact product), and so are all comparisons.  Returns false, with nothing
+// decided, where a block's list overflows.
+// `m` receives the kept row by regions (see Measured).
+template <class T>
+__device__ bool nucleus(Shared& s, const Row<T>& r, const RowRule& rule, unsigned rank, int C,
+                        float& theta, unsigned& ties, Measured& m) {
+  constexpr int N = Row<T>::N;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int stop = r.end(warp);
+  // the maximum alone weighs 2^40: all entries below `cut` together weigh less than an eighth of
+  // 1 - top_p of that, so theta is above it (or below the last bin)
+  const float rest = 1.f - __fmul_rn((float)rule.part, 0x1p-31f);
+  const float cut = fmaxf(log2f(__fdiv_rn(rest, (float)r.view.n)) - 3.01f, -(float)WBINS / STEPS);
+  const float low = fmaxf(cut, r.tmin - 1.f);
+  for (int b = tid; b < WBINS; b += RT) s.wbins[b] = 0;
+  if (tid == 0) s.number = 0;
+  __syncthreads();
+  unsigned long long mass = 0;
+  {
+    unsigned hi = 0, lo = 0, parts = 0;
+    for (int at = r.begin(warp) + lane; at - lane < stop; at += 32) {
+      float l[N];
+      r.scores(r.get(warp, at, stop), l);
+#pragma unroll
+      for (int i = 0; i < N; i += 2) {
+        const float t0 = __fmul_rn(__fsub_rn(l[i], r.max), r.scale);
+        const float t1 = __fmul_rn(__fsub_rn(l[i + 1], r.max), r.scale);
+        unsigned h[2], w[2];
+        float v[2];
+        weight_parts(t0, t1, h, w, v);
+        bool in0 = t0 > low, in1 = t1 > low;
+        if (r.least > 1) {
+          const unsigned long long a = join_parts(h[0], w[0]), b = join_parts(h[1], w[1]);
+          const bool e0 = a >= r.least, e1 = b >= r.least;
+          mass += (e0 ? a : 0ull) + (e1 ? b : 0ull);
+          in0 = in0 && e0;
+          in1 = in1 && e1;
+        } else {
+          hi += h[0] + h[1];
+          lo += w[0] + w[1];
+        }
+        if (in0) atomicAdd(&s.wbins[__float_as_uint(__fmaf_rz(t0, -(float)STEPS, 8388608.f)) - BIAS], 1u);
+        if (in1) atomicAdd(&s.wbins[__float_as_uint(__fmaf_rz(t1, -(float)STEPS, 8388608.f)) - BIAS], 1u);
+      }
+      parts += N;
+    }
+    if (r.least <= 1 && parts) mass = join_sums(hi, lo, parts);
+  }
+  const unsigned long long total = cluster_sum(s, mass, &s.total64, C);  // also closes the counting
+  unsigned long long target =
+      (total >> 31) * rule.part + (((total & 0x7fffffffull) * rule.part) >> 31);
+  if (!target) target = 1;
+  // bounds of the running mass through each bin, from the bins before it and from those after it
+  float from_t, to_t;  // theta lies in to_t < t <= from_t
+  {
+    constexpr int P = WBINS / RT;
+    unsigned c[P] = {};
+    for (int k = 0; k < C; ++k)
+#pragma unroll
+      for (int i = 0; i < P; ++i) c[i] += ld_peer(&s.wbins[tid * P + i], k);
+    unsigned long long least[P], most[P], ls = 0, ms = 0, all_least, all_most;
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+      const float top = exp2f(40.f - (float)(tid * P + i) * (1.f / STEPS));
+      const float bottom = top * (1.f - 0.01089f - 2e-5f);  // 2^(-1/64) = 1 - 0.010772
+      least[i] = c[i] * (bottom > 1.f ? (unsigned long long)(bottom - 1.f) : 0ull);
+      most[i] = c[i] * ((unsigned long long)(top * (1.f + 2e-5f)) + 1ull);
+      ls += least[i];
+      ms += most[i];
+    }
+    unsigned long long lb = block_exclusive(ls, s.part64, &all_least);
+    unsigned long long mb = block_exclusive(ms, s.part64, &all_most);
+    const unsigned long long below =  // what is not counted weighs at most this
+        low > cut ? 0ull : (unsigned long long)(exp2f(40.f + low) * 1.001f * (float)r.view.n) + r.view.n;
+    if (tid == 0) {
+      s.first_bin = WBINS;
+      s.last_bin = WBINS;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+      const unsigned long long l0 = lb, m0 = mb;
+      lb += least[i];
+      mb += most[i];
+      auto upper = [&](unsigned long long most_to, unsigned long long least_to) {
+        return min(most_to, total - min(total, all_least - least_to));
+      };
+      auto lower = [&](unsigned long long most_to, unsigned long long least_to) {
+        const unsigned long long after = all_most - most_to + below;
+        return max(least_to, total - min(total, after));
+      };
+      const bool start = tid == 0 && i == 0;
+      if (upper(mb, lb) >= target && (start || upper(m0, l0) < target)) s.first_bin = tid * P + i;
+      if (lower(mb, lb) >= target && (start || lower(m0, l0) < target)) s.last_bin = tid * P + i;
+    }
+    __syncthreads();
+    from_t = -(float)s.first_bin * (1.f / STEPS);
+    to_t = s.last_bin < WBINS ? -(float)(s.last_bin + 1) * (1.f / STEPS) : -INFINITY;
+  }
+  // what lies above the bins, by regions, and the list of what lies in them
+  Part p = {0, 0, 0};
+  {
+    unsigned hi = 0, lo = 0, parts = 0;
+    for (int at = r.begin(warp) + lane; at - lane < stop; at += 32) {
+      float l[N], t[N];
+      r.scores(r.get(warp, at, stop), l);
+      float best = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        t[i] = __fmul_rn(__fsub_rn(l[i], r.max), r.scale);
+        best = fmaxf(best, t[i]);
+      }
+      if (!(best > to_t)) continue;
+      bool listed = false;
+      if (best > from_t) {
+#pragma unroll
+        for (int i = 0; i < N; i += 2) {
+          unsigned h[2], w[2];
+          float v[2];
+          weight_parts(t[i], t[i + 1], h, w, v);
+#pragma unroll
+          for (int j = 0; j < 2; ++j)
+            if (t[i + j] > from_t && (r.least <= 1 || join_parts(h[j], w[j]) >= r.least)) {
+              hi += h[j];
+              lo += w[j];
+              ++parts;
+            }
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < N; ++i) listed = listed || (t[i] <= from_t && t[i] > to_t);
+      if (listed) {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+          if (t[i] <= from_t && t[i] > to_t && r.weight(l[i])) {
+            const unsigned q = atomicAdd(&s.number, 1u);
+            if (q < LIST) {
+              s.list[q] = order_key(__fadd_rn(l[i], 0.f));
+              s.from[q] = (uint8_t)warp;
+            }
+          }
+      }
+    }
+    p.above = parts;
+    if (parts) p.mass = join_sums(hi, lo, parts);
+  }
+  p.above = __reduce_add_sync(0xffffffffu, p.above);
+#pragma unroll
+  for (int o = 16; o; o >>= 1) p.mass += __shfl_xor_sync(0xffffffffu, p.mass, o);
+  if (lane == 0) {
+    s.mass[warp] = p.mass;
+    s.above[warp] = p.above;
+    s.tied[warp] = 0;
+  }
+  const unsigned long long sure = cluster_sum(s, lane == 0 ? p.mass : 0ull, &s.sure64, C);
+  bool over = false;
+  for (int k = 0; k < C; ++k) over = over || ld_peer(&s.number, k) > LIST;
+  cluster_barrier();
+  if (over) return false;
+  // sure < target: theta is in the list
+  unsigned long long left = target - sure;
+  unsigned klo = order_key(-3.4028235e38f), khi = order_key(r.max);
+  descend<true, true>(s, r, rank, C, klo, khi, left);
+  theta = order_value(khi);
+  const unsigned long long wt = r.weight(theta);
+  ties = (unsigned)((left + wt - 1) / wt);
+  for (unsigned i = tid; i < s.number; i += RT) {
+    const unsigned k = s.list[i];
+    if (k > khi) {
+      atomicAdd(&s.mass[s.from[i]], r.weight(order_value(k)));
+      atomicAdd(&s.above[s.from[i]], 1u);
+    } else if (k == khi) {
+      atomicAdd(&s.tied[s.from[i]], 1u);
+    }
+  }
+  m = by_regions(s, r, C, theta, ties);
+  return true;
+}
+
 template <class T>
 __device__ void sample_row(Shared& s, Row<T>& r, const RowRule& rule, unsigned rank, int C,
                            uint64_t word, int32_t* id, float* logp, int32_t* kept) {
@@ -503,7 +720,8 @@ __device__ void sample_row(Shared& s, Row<T>& r, const RowRule& rule, unsigned r
   float theta = -INFINITY;
   unsigned ties = 0xffffffffu;
   const bool by_k = rule.top_k < (unsigned)r.view.n, by_p = rule.part != 0xffffffffu;
-  bool done = false, limited = false;
+  bool done = false, limited = false, measured = false;
+  Measured m;
   if (by_k && !r.odd) {
     // At least top_k entries lie no lower than the top_k-th best of the threads' maxima: those down
     // to its bin are the candidates.
@@ -534,6 +752,7 @@ __device__ void sample_row(Shared& s, Row<T>& r, const RowRule& rule, unsigned r
       limited = done;
     }
   }
+  if (!by_k && by_p && !r.odd) done = measured = nucleus(s, r, rule, rank, C, theta, ties, m);
   if (!done) {
     // keys an eligible entry can have: t >= tmin, with room for its roundings
     const float edge = r.odd ? -INFINITY
@@ -542,14 +761,14 @@ __device__ void sample_row(Shared& s, Row<T>& r, const RowRule& rule, unsigned r
     if (by_k) {
       unsigned khi = top;
       unsigned long long left = rule.top_k;
-      if (descend<false>(s, r, rank, C, klo, khi, left)) {
+      if (descend<false, false>(s, r, rank, C, klo, khi, left)) {
         theta = order_value(khi);
         ties = (unsigned)left;
         limited = true;
       }
     }
     if (by_p) {
-      const Measured m = measure_row(s, r, C, theta, ties);
+      m = measure_row(s, r, C, theta, ties);
       cluster_barrier();
       unsigned long long target =
           (m.total >> 31) * rule.part + (((m.total & 0x7fffffffull) * rule.part) >> 31);
@@ -561,7 +780,7 @@ __device__ void sample_row(Shared& s, Row<T>& r, const RowRule& rule, unsigned r
         if (limited) klo = order_key(theta) + 1;
         unsigned khi = top;
         unsigned long long left = target;
-        descend<true>(s, r, rank, C, klo, khi, left);
+        descend<true, false>(s, r, rank, C, klo, khi, left);
         theta = order_value(khi);
         const unsigned long long wt = r.weight(theta);
         ties = (unsigned)((left + wt - 1) / wt);
@@ -570,7 +789,7 @@ __device__ void sample_row(Shared& s, Row<T>& r, const RowRule& rule, unsigned r
   }
 
   // the draw: the warp's region it falls in, then a sixteenth of that region, then a vector
-  const Measured m = measure_row(s, r, C, theta, ties);
+  if (!measured) m = measure_row(s, r, C, theta, ties);
   const unsigned long long at = __umul64hi(word, m.total);
   if (tid < C * RW && at >= m.before && at - m.before < m.kept) {
     s.digit = tid;
