@@ -191,6 +191,14 @@ __device__ __forceinline__ void unpack_scores(uint4 u, float* l, __half) {
     l[2 * i + 1] = f.y;
   }
 }
+// the same as pairs for the packed instructions
+template <class T>
+__device__ __forceinline__ void unpack_pairs(uint4 u, uint64_t* p) {
+  float l[ScoreVec<T>::N];
+  unpack_scores(u, l, T());
+#pragma unroll
+  for (int i = 0; i < ScoreVec<T>::N / 2; ++i) p[i] = pair(l[2 * i], l[2 * i + 1]);
+}
 // the pattern of -inf in each lane of a 32-bit word
 template <class T>
 __device__ __forceinline__ unsigned masked_word();
@@ -214,10 +222,17 @@ struct RowView {
     base = row - skew;
     vectors = (skew + n + ScoreVec<T>::N - 1) / ScoreVec<T>::N;
   }
+  // vectors that lie wholly inside the row: (v > 0 or no skew) and v < whole()
+  __device__ __forceinline__ int whole() const { return (skew + n) / ScoreVec<T>::N; }
+  __device__ __forceinline__ uint4 inner(int v) const {
+    return __ldg(reinterpret_cast<const uint4*>(base) + v);
+  }
   __device__ __forceinline__ uint4 fetch(int v) const {
+    const int first = v * ScoreVec<T>::N - skew;
+    return first >= 0 && first + ScoreVec<T>::N <= n ? inner(v) : edge(base, skew, n, first);
+  }
+  static __device__ __noinline__ uint4 edge(const T* base, int skew, int n, int first) {
     constexpr int N = ScoreVec<T>::N;
-    const int first = v * N - skew;
-    if (first >= 0 && first + N <= n) return __ldg(reinterpret_cast<const uint4*>(base) + v);
     union {
       uint4 u;
       T t[N];

@@ -16,8 +16,8 @@ constexpr int RW = RT / 32;   // its warps
 constexpr int MAX_C = 16;     // blocks of a row's cluster
 constexpr int LIST = 4096;    // candidates ranked in one block's shared memory
 constexpr int BINS = 1024;    // bins of one level of the descent
-constexpr int STEPS = 64;     // bins an octave of the weights' histogram
-constexpr int WBINS = 2048;   // its bins
+constexpr int STEPS = 128;    // bins an octave of the weights' histogram
+constexpr int WBINS = 4096;   // its bins
 constexpr int CBINS = 1024;   // bins of the threads' maxima
 constexpr int ROOM = 72 * 1024;  // bytes of a row in a block's shared memory (two blocks an SM)
 
@@ -44,36 +44,59 @@ __device__ __forceinline__ RowRule row_rule(const erc_sample_rule& r, int64_t ro
   return o;
 }
 
-__device__ __forceinline__ unsigned cluster_rank() {
-  unsigned r;
-  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-  return r;
-}
-__device__ __forceinline__ void cluster_barrier() {
-  asm volatile(
-      "barrier.cluster.arrive.release.aligned;\n\t"
-      "barrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-// address of the same shared variable in block `rank` of this cluster
-template <class V>
-__device__ __forceinline__ unsigned peer(const V* local, unsigned rank) {
-  unsigned a = (unsigned)__cvta_generic_to_shared(local), r;
-  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(rank));
-  return r;
-}
-__device__ __forceinline__ unsigned ld_peer(const unsigned* p, unsigned rank) {
-  unsigned v;
-  asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(peer(p, rank)) : "memory");
-  return v;
-}
-__device__ __forceinline__ unsigned long long ld_peer(const unsigned long long* p, unsigned rank) {
-  unsigned long long v;
-  asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(peer(p, rank)) : "memory");
-  return v;
-}
-__device__ __forceinline__ void add_peer(unsigned* p, unsigned rank, unsigned v) {
-  asm volatile("red.shared::cluster.add.u32 [%0], %1;" ::"r"(peer(p, rank)), "r"(v) : "memory");
-}
+// The blocks of a row: a thread-block cluster, or (SOLO) one block, for which the cluster's barrier
+// and remote accesses become the block's own.
+template <bool SOLO>
+struct Team {
+  int blocks;
+  unsigned rank;
+  __device__ __forceinline__ explicit Team(int C) : blocks(SOLO ? 1 : C), rank(0) {
+    if (!SOLO) asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+  }
+  __device__ __forceinline__ int size() const { return SOLO ? 1 : blocks; }
+  __device__ __forceinline__ void barrier() const {
+    if (SOLO)
+      __syncthreads();
+    else
+      asm volatile(
+          "barrier.cluster.arrive.release.aligned;\n\t"
+          "barrier.cluster.wait.acquire.aligned;" ::: "memory");
+  }
+  // the same shared variable in block `at`
+  __device__ __forceinline__ static unsigned address(const void* local, unsigned at) {
+    unsigned a = (unsigned)__cvta_generic_to_shared(local), r;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(at));
+    return r;
+  }
+  __device__ __forceinline__ unsigned load(const unsigned* p, unsigned at) const {
+    if (SOLO) return *p;
+    unsigned v;
+    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(address(p, at)) : "memory");
+    return v;
+  }
+  __device__ __forceinline__ uint4 load(const uint4* p, unsigned at) const {
+    if (SOLO) return *p;
+    uint4 v;
+    asm volatile("ld.shared::cluster.v4.u32 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+                 : "r"(address(p, at))
+                 : "memory");
+    return v;
+  }
+  __device__ __forceinline__ unsigned long long load(const unsigned long long* p,
+                                                     unsigned at) const {
+    if (SOLO) return *p;
+    unsigned long long v;
+    asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(address(p, at)) : "memory");
+    return v;
+  }
+  __device__ __forceinline__ void add(unsigned* p, unsigned at, unsigned v) const {
+    if (SOLO)
+      atomicAdd(p, v);
+    else
+      asm volatile("red.shared::cluster.add.u32 [%0], %1;" ::"r"(address(p, at)), "r"(v) : "memory");
+  }
+};
 
 // exclusive sum over the block's threads; *total receives the block's sum
 template <class V>
@@ -118,7 +141,7 @@ struct Shared {
   union {
     unsigned bins[3][BINS];
     unsigned count[CBINS];
-    unsigned wbins[WBINS];
+    alignas(16) unsigned wbins[WBINS];
   };
   unsigned list[LIST];        // candidates' keys
   uint8_t from[LIST];         // and the warps whose regions hold them
@@ -158,6 +181,19 @@ struct Row {
     return w >= least ? w : 0ull;
   }
 };
+
+// f(vector) for vectors [from, to) of a warp's region, 32 at a time (lanes past the end get masked
+// vectors), the next one loaded meanwhile
+template <class T, class F>
+__device__ __forceinline__ void each_vector(const Row<T>& r, int warp, int from, int to, F&& f) {
+  const int lane = threadIdx.x & 31;
+  uint4 u = r.get(warp, from + lane, to);
+  for (int at = from; at < to; at += 32) {
+    const uint4 next = r.get(warp, at + 32 + lane, to);
+    f(u);
+    u = next;
+  }
+}
 
 // mass, numbers and ties of vectors [from, to) of a warp's region, over its lanes
 template <class T>
@@ -225,15 +261,17 @@ struct Measured {
   unsigned long long before, kept, total, above_mass;
   unsigned ties_before, number, tied;
 };
-template <class T>
-__device__ Measured by_regions(Shared& s, const Row<T>& r, int C, float theta, unsigned ties) {
+template <class T, bool SOLO>
+__device__ Measured by_regions(Shared& s, const Row<T>& r, const Team<SOLO>& team, float theta,
+                               unsigned ties) {
+  const int C = team.size();
   const int tid = threadIdx.x;
-  cluster_barrier();
+  team.barrier();
   Part q = {0, 0, 0};
   if (tid < C * RW) {
-    q.mass = ld_peer(&s.mass[tid % RW], tid / RW);
-    q.above = ld_peer(&s.above[tid % RW], tid / RW);
-    q.tied = ld_peer(&s.tied[tid % RW], tid / RW);
+    q.mass = team.load(&s.mass[tid % RW], tid / RW);
+    q.above = team.load(&s.above[tid % RW], tid / RW);
+    q.tied = team.load(&s.tied[tid % RW], tid / RW);
   }
   Measured m;
   unsigned tied, above;
@@ -248,8 +286,9 @@ __device__ Measured by_regions(Shared& s, const Row<T>& r, int C, float theta, u
   m.number = above + min(tied, ties);
   return m;
 }
-template <class T>
-__device__ Measured measure_row(Shared& s, const Row<T>& r, int C, float theta, unsigned ties) {
+template <class T, bool SOLO>
+__device__ Measured measure_row(Shared& s, const Row<T>& r, const Team<SOLO>& team, float theta,
+                                unsigned ties) {
   const int warp = threadIdx.x >> 5;
   const Part p = measure(r, warp, r.begin(warp), r.end(warp), theta);
   if ((threadIdx.x & 31) == 0) {
@@ -257,36 +296,45 @@ __device__ Measured measure_row(Shared& s, const Row<T>& r, int C, float theta, 
     s.above[warp] = p.above;
     s.tied[warp] = p.tied;
   }
-  return by_regions(s, r, C, theta, ties);
+  return by_regions(s, r, team, theta, ties);
 }
 
-// f(score) for every entry of the block: of its regions, or (LISTED) of its candidate list
+// f(score, warp of its region) for the entries of the block that are no lower than `floor`: those of
+// its regions, or (LISTED) of its candidate list
 template <bool LISTED, class T, class F>
 __device__ __forceinline__ void each_score(const Shared& s, const Row<T>& r, float floor, F&& f) {
   constexpr int N = Row<T>::N;
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int tid = threadIdx.x, warp = tid >> 5;
   if (LISTED) {
-    for (unsigned i = tid; i < s.number; i += RT) f(order_value(s.list[i]));
+    for (unsigned i = tid; i < s.number; i += RT) {
+      const float l = order_value(s.list[i]);
+      if (l >= floor) f(l, s.from[i]);
+    }
     return;
   }
-  const int stop = r.end(warp);
-  for (int at = r.begin(warp) + lane; at - lane < stop; at += 32) {
-    float l[N];
-    r.scores(r.get(warp, at, stop), l);
+  each_vector(r, warp, r.begin(warp), r.end(warp), [&](uint4 u) {
+    float l[N], best = -INFINITY;
+    r.scores(u, l);
 #pragma unroll
-    for (int i = 0; i < N; ++i)
-      if (l[i] >= floor) f(l[i]);
-  }
+    for (int i = 0; i < N; ++i) best = fmaxf(best, l[i]);
+    if (best >= floor) {
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+        if (l[i] >= floor) f(l[i], warp);
+    }
+  });
 }
 
 // Descent to the key at which the running count (MASS: weight) over entries with keys in
-// [klo, khi], largest first, reaches `left` (> 0).  Returns false where it does not; else khi is
+// [klo, khi] and t of at most `limit`, largest first, reaches `left` (> 0).  Returns false where it does not; else khi is
 // that key and `left` what is still wanted from the entries at it.  A level splits the keys into
 // at most BINS bins; a bin's weights are summed as three limbs of 14 bits, at most 2^18 of them in
 // a block, and the blocks of the cluster each add up a part of the bins.
-template <bool MASS, bool LISTED, class T>
-__device__ bool descend(Shared& s, const Row<T>& r, unsigned rank, int C, unsigned klo,
-                        unsigned& khi, unsigned long long& left) {
+template <bool MASS, bool LISTED, class T, bool SOLO>
+__device__ bool descend(Shared& s, const Row<T>& r, const Team<SOLO>& team, unsigned klo,
+                        unsigned& khi, unsigned long long& left, float limit = INFINITY) {
+  const int C = team.size();
+  const unsigned rank = team.rank;
   const int tid = threadIdx.x;
   const int B = BINS / C;
   for (;;) {
@@ -294,9 +342,10 @@ __device__ bool descend(Shared& s, const Row<T>& r, unsigned rank, int C, unsign
     const int shift = span < BINS ? 0 : 22 - __clz(span);
     for (int b = tid; b < (MASS ? 3 : 1) * BINS; b += RT) s.bins[0][b] = 0;
     __syncthreads();
-    each_score<LISTED>(s, r, order_value(klo), [&](float l) {
+    each_score<LISTED>(s, r, order_value(klo), [&](float l, int) {
       const unsigned d = khi - order_key(__fadd_rn(l, 0.f));
-      const unsigned long long w = d <= span ? r.weight(l) : 0ull;
+      const bool in = d <= span && (LISTED || limit == INFINITY || r.scaled(l) <= limit);
+      const unsigned long long w = in ? r.weight(l) : 0ull;
       if (w) {
         const unsigned b = d >> shift;
         if (MASS) {
@@ -308,7 +357,7 @@ __device__ bool descend(Shared& s, const Row<T>& r, unsigned rank, int C, unsign
         }
       }
     });
-    cluster_barrier();
+    team.barrier();
     // this block's share of the bins: bins rank * B .., BINS / RT of them a thread at most
     unsigned long long v[BINS / RT], mine = 0;
     const int per = (B + RT - 1) / RT;
@@ -318,21 +367,21 @@ __device__ bool descend(Shared& s, const Row<T>& r, unsigned rank, int C, unsign
       const int b = tid * per + i;
       if (i < per && b < B)
         for (int c = 0; c < C; ++c) {
-          v[i] += ld_peer(&s.bins[0][rank * B + b], c);
+          v[i] += team.load(&s.bins[0][rank * B + b], c);
           if (MASS)
-            v[i] += ((unsigned long long)ld_peer(&s.bins[1][rank * B + b], c) << 14) +
-                    ((unsigned long long)ld_peer(&s.bins[2][rank * B + b], c) << 28);
+            v[i] += ((unsigned long long)team.load(&s.bins[1][rank * B + b], c) << 14) +
+                    ((unsigned long long)team.load(&s.bins[2][rank * B + b], c) << 28);
         }
       mine += v[i];
     }
     unsigned long long sum;
     unsigned long long before = block_exclusive(mine, s.part64, &sum);
     if (tid == 0) s.total64 = sum;
-    cluster_barrier();
+    team.barrier();
     unsigned long long base = 0;
     int owner = -1;
     for (int c = 0; c < C; ++c) {
-      const unsigned long long q = ld_peer(&s.total64, c);
+      const unsigned long long q = team.load(&s.total64, c);
       if (owner < 0) {
         if (base + q >= left) owner = c;
         else base += q;
@@ -349,14 +398,14 @@ __device__ bool descend(Shared& s, const Row<T>& r, unsigned rank, int C, unsign
         before += v[i];
       }
     }
-    cluster_barrier();
+    team.barrier();
     if (owner < 0) return false;
-    const unsigned digit = ld_peer(&s.digit, owner);
-    left -= ld_peer(&s.over, owner);
+    const unsigned digit = team.load(&s.digit, owner);
+    left -= team.load(&s.over, owner);
     khi -= digit << shift;
     const unsigned width = (1u << shift) - 1;
     if (khi - klo > width) klo = khi - width;
-    cluster_barrier();
+    team.barrier();
     if (klo == khi) return true;
   }
 }
@@ -364,9 +413,12 @@ __device__ bool descend(Shared& s, const Row<T>& r, unsigned rank, int C, unsign
 // Ranks at most LIST candidates in block 0: top-k, then top-p, to (theta, ties).  Returns false,
 // with nothing decided, where there are more.  Candidates are the eligible entries whose distance
 // from the maximum is below `reach` (all of them: reach = inf).
-template <class T>
-__device__ bool rank_list(Shared& s, const Row<T>& r, const RowRule& rule, unsigned rank, int C,
-                          float inv, float reach, float& theta, unsigned& ties) {
+template <class T, bool SOLO>
+__device__ bool rank_list(Shared& s, const Row<T>& r, const RowRule& rule,
+                          const Team<SOLO>& team, float inv, float reach, float& theta,
+                          unsigned& ties) {
+  const int C = team.size();
+  const unsigned rank = team.rank;
   constexpr int N = Row<T>::N;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   if (tid == 0) s.number = 0;
@@ -382,22 +434,22 @@ __device__ bool rank_list(Shared& s, const Row<T>& r, const RowRule& rule, unsig
         if (p < LIST) s.list[p] = order_key(__fadd_rn(l[i], 0.f));
       }
   }
-  cluster_barrier();
+  team.barrier();
   unsigned all = 0, mine = 0;
   for (int c = 0; c < C; ++c) {
-    const unsigned q = ld_peer(&s.number, c);
+    const unsigned q = team.load(&s.number, c);
     if (c == 0) mine = q;
     all += q;
   }
   if (all > LIST) {
-    cluster_barrier();
+    team.barrier();
     return false;
   }
   if (rank == 0) {
     unsigned at = mine;
     for (int c = 1; c < C; ++c) {
-      const unsigned q = ld_peer(&s.number, c);
-      for (unsigned i = tid; i < q; i += RT) s.list[at + i] = ld_peer(&s.list[i], c);
+      const unsigned q = team.load(&s.number, c);
+      for (unsigned i = tid; i < q; i += RT) s.list[at + i] = team.load(&s.list[i], c);
       at += q;
     }
     unsigned size = 2;
@@ -452,36 +504,39 @@ __device__ bool rank_list(Shared& s, const Row<T>& r, const RowRule& rule, unsig
       s.ties = number - lo;
     }
   }
-  cluster_barrier();
-  theta = order_value(ld_peer(&s.theta, 0));
-  ties = ld_peer(&s.ties, 0);
+  team.barrier();
+  theta = order_value(team.load(&s.theta, 0));
+  ties = team.load(&s.ties, 0);
   return true;
 }
 
 // Sum over the cluster of a value of each thread.
-__device__ unsigned long long cluster_sum(Shared& s, unsigned long long v, unsigned long long* slot,
-                                          int C) {
+template <bool SOLO>
+__device__ unsigned long long team_sum(Shared& s, unsigned long long v, unsigned long long* slot,
+                                       const Team<SOLO>& team) {
+  const int C = team.size();
   const int lane = threadIdx.x & 31;
   unsigned long long sum;
   block_exclusive(v, s.part64, &sum);
   if (threadIdx.x == 0) *slot = sum;
-  cluster_barrier();
-  sum = lane < C ? ld_peer(slot, lane) : 0ull;
+  team.barrier();
+  sum = lane < C ? team.load(slot, lane) : 0ull;
 #pragma unroll
   for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
   return sum;
 }
 
 // Top-p alone over long rows.  One pass weighs the row and counts its entries by weight, STEPS bins
-// an octave: a bin's entries weigh within 1.1% of each other, so the counts bound the running mass
+// an octave: a bin's entries weigh within 0.55% of each other, so the counts bound the running mass
 // from both sides and leave a few bins in which theta lies.  A second pass weighs what is above
-// them, which is kept, and lists their entries; theta is found in the list.  Bins are stretches of
-// t (floor(-t STEPS), an exact product), and so are all comparisons.  Returns false, with nothing
-// decided, where a block's list overflows.
+// them, which is kept, and lists their entries; theta is found in the list (in
+// the row itself where a block's list overflows).  Bins are stretches of t (floor(-t STEPS), an
+// exact product), and so are all comparisons.
 // `m` receives the kept row by regions (see Measured).
-template <class T>
-__device__ bool nucleus(Shared& s, const Row<T>& r, const RowRule& rule, unsigned rank, int C,
+template <class T, bool SOLO>
+__device__ void nucleus(Shared& s, const Row<T>& r, const RowRule& rule, const Team<SOLO>& team,
                         float& theta, unsigned& ties, Measured& m) {
+  const int C = team.size();
   constexpr int N = Row<T>::N;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int stop = r.end(warp);
@@ -494,37 +549,50 @@ __device__ bool nucleus(Shared& s, const Row<T>& r, const RowRule& rule, unsigne
   if (tid == 0) s.number = 0;
   __syncthreads();
   unsigned long long mass = 0;
-  {
+  const uint64_t m2 = pair(-r.max, -r.max), s2 = pair(r.scale, r.scale);
+  if (r.least <= 1) {
+    const unsigned bins = (unsigned)__cvta_generic_to_shared(s.wbins) - (BIAS << 2);
     unsigned hi = 0, lo = 0, parts = 0;
-    for (int at = r.begin(warp) + lane; at - lane < stop; at += 32) {
-      float l[N];
-      r.scores(r.get(warp, at, stop), l);
+    each_vector(r, warp, r.begin(warp), stop, [&](uint4 u) {
+      uint64_t l[N / 2];
+      unpack_pairs<T>(u, l);
 #pragma unroll
-      for (int i = 0; i < N; i += 2) {
-        const float t0 = __fmul_rn(__fsub_rn(l[i], r.max), r.scale);
-        const float t1 = __fmul_rn(__fsub_rn(l[i + 1], r.max), r.scale);
+      for (int i = 0; i < N / 2; ++i) {
+        float t[2], v[2];
         unsigned h[2], w[2];
-        float v[2];
-        weight_parts(t0, t1, h, w, v);
-        bool in0 = t0 > low, in1 = t1 > low;
-        if (r.least > 1) {
-          const unsigned long long a = join_parts(h[0], w[0]), b = join_parts(h[1], w[1]);
-          const bool e0 = a >= r.least, e1 = b >= r.least;
-          mass += (e0 ? a : 0ull) + (e1 ? b : 0ull);
-          in0 = in0 && e0;
-          in1 = in1 && e1;
-        } else {
-          hi += h[0] + h[1];
-          lo += w[0] + w[1];
+        unpair(mul2(add2(l[i], m2), s2), t[0], t[1]);
+        weight_parts(t[0], t[1], h, w, v);
+        hi += h[0] + h[1];
+        lo += w[0] + w[1];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const unsigned bin = __float_as_uint(__fmaf_rz(t[j], -(float)STEPS, 8388608.f));
+          asm volatile(
+              "{\n\t.reg .pred p;\n\tsetp.gt.f32 p, %0, %1;\n\t@p red.shared.add.u32 [%2], 1;\n\t}" ::"f"(t[j]),
+              "f"(low), "r"(bins + (bin << 2))
+              : "memory");
         }
-        if (in0) atomicAdd(&s.wbins[__float_as_uint(__fmaf_rz(t0, -(float)STEPS, 8388608.f)) - BIAS], 1u);
-        if (in1) atomicAdd(&s.wbins[__float_as_uint(__fmaf_rz(t1, -(float)STEPS, 8388608.f)) - BIAS], 1u);
       }
       parts += N;
-    }
-    if (r.least <= 1 && parts) mass = join_sums(hi, lo, parts);
+    });
+    if (parts) mass = join_sums(hi, lo, parts);
+  } else {
+    each_vector(r, warp, r.begin(warp), stop, [&](uint4 u) {
+      float l[N], best = -INFINITY;
+      r.scores(u, l);
+#pragma unroll
+      for (int i = 0; i < N; ++i) best = fmaxf(best, l[i]);
+      if (!(r.scaled(best) > low)) return;
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const float t = r.scaled(l[i]);
+        const unsigned long long w = t > low ? r.weight(l[i]) : 0ull;
+        mass += w;
+        if (w) atomicAdd(&s.wbins[__float_as_uint(__fmaf_rz(t, -(float)STEPS, 8388608.f)) - BIAS], 1u);
+      }
+    });
   }
-  const unsigned long long total = cluster_sum(s, mass, &s.total64, C);  // also closes the counting
+  const unsigned long long total = team_sum(s, mass, &s.total64, team);  // also closes the counting
   unsigned long long target =
       (total >> 31) * rule.part + (((total & 0x7fffffffull) * rule.part) >> 31);
   if (!target) target = 1;
@@ -533,14 +601,21 @@ __device__ bool nucleus(Shared& s, const Row<T>& r, const RowRule& rule, unsigne
   {
     constexpr int P = WBINS / RT;
     unsigned c[P] = {};
+#pragma unroll 4
     for (int k = 0; k < C; ++k)
 #pragma unroll
-      for (int i = 0; i < P; ++i) c[i] += ld_peer(&s.wbins[tid * P + i], k);
+      for (int i = 0; i < P; i += 4) {
+        const uint4 q = team.load(reinterpret_cast<const uint4*>(&s.wbins[tid * P + i]), k);
+        c[i] += q.x;
+        c[i + 1] += q.y;
+        c[i + 2] += q.z;
+        c[i + 3] += q.w;
+      }
     unsigned long long least[P], most[P], ls = 0, ms = 0, all_least, all_most;
 #pragma unroll
     for (int i = 0; i < P; ++i) {
       const float top = exp2f(40.f - (float)(tid * P + i) * (1.f / STEPS));
-      const float bottom = top * (1.f - 0.01089f - 2e-5f);  // 2^(-1/64) = 1 - 0.010772
+      const float bottom = top * (1.f - 0.005402f - 2e-5f);  // 2^(-1/128) = 1 - 0.0054005
       least[i] = c[i] * (bottom > 1.f ? (unsigned long long)(bottom - 1.f) : 0ull);
       most[i] = c[i] * ((unsigned long long)(top * (1.f + 2e-5f)) + 1ull);
       ls += least[i];
@@ -579,48 +654,58 @@ __device__ bool nucleus(Shared& s, const Row<T>& r, const RowRule& rule, unsigne
   Part p = {0, 0, 0};
   {
     unsigned hi = 0, lo = 0, parts = 0;
-    for (int at = r.begin(warp) + lane; at - lane < stop; at += 32) {
-      float l[N], t[N];
-      r.scores(r.get(warp, at, stop), l);
-      float best = -INFINITY;
+    each_vector(r, warp, r.begin(warp), stop, [&](uint4 u) {
+      uint64_t l[N / 2];
+      float t[N], best = -INFINITY;
+      unpack_pairs<T>(u, l);
+#pragma unroll
+      for (int i = 0; i < N / 2; ++i) {
+        unpair(mul2(add2(l[i], m2), s2), t[2 * i], t[2 * i + 1]);
+        best = fmaxf(best, fmaxf(t[2 * i], t[2 * i + 1]));
+      }
+      if (!__any_sync(0xffffffffu, best > to_t)) return;
 #pragma unroll
       for (int i = 0; i < N; ++i) {
-        t[i] = __fmul_rn(__fsub_rn(l[i], r.max), r.scale);
-        best = fmaxf(best, t[i]);
+        const unsigned who = __ballot_sync(0xffffffffu, t[i] <= from_t && t[i] > to_t);
+        if (!who) continue;
+        float x0, x1;
+        unpair(l[i / 2], x0, x1);
+        const float x = i & 1 ? x1 : x0;
+        const bool in = (who >> lane & 1) && (r.least <= 1 || r.weight(x));
+        const unsigned those = __ballot_sync(0xffffffffu, in);
+        unsigned q = 0;
+        if (lane == 0) q = atomicAdd(&s.number, (unsigned)__popc(those));
+        q = __shfl_sync(0xffffffffu, q, 0) + __popc(those & ((1u << lane) - 1));
+        if (in && q < LIST) {
+          s.list[q] = order_key(__fadd_rn(x, 0.f));
+          s.from[q] = (uint8_t)warp;
+        }
       }
-      if (!(best > to_t)) continue;
-      bool listed = false;
-      if (best > from_t) {
+      if (!__any_sync(0xffffffffu, best > from_t)) return;
+      if (r.least <= 1) {
 #pragma unroll
         for (int i = 0; i < N; i += 2) {
           unsigned h[2], w[2];
           float v[2];
-          weight_parts(t[i], t[i + 1], h, w, v);
+          const bool k0 = t[i] > from_t, k1 = t[i + 1] > from_t;
+          weight_parts(k0 ? t[i] : -60.f, k1 ? t[i + 1] : -60.f, h, w, v);
+          hi += h[0] + h[1];
+          lo += w[0] + w[1];
+          p.above += k0 + k1;
+        }
+        parts += N;
+      } else {
 #pragma unroll
-          for (int j = 0; j < 2; ++j)
-            if (t[i + j] > from_t && (r.least <= 1 || join_parts(h[j], w[j]) >= r.least)) {
-              hi += h[j];
-              lo += w[j];
-              ++parts;
-            }
+        for (int i = 0; i < N; ++i) {
+          float x0, x1;
+          unpair(l[i / 2], x0, x1);
+          const unsigned long long w = t[i] > from_t ? r.weight(i & 1 ? x1 : x0) : 0ull;
+          p.mass += w;
+          p.above += w != 0;
         }
       }
-#pragma unroll
-      for (int i = 0; i < N; ++i) listed = listed || (t[i] <= from_t && t[i] > to_t);
-      if (listed) {
-#pragma unroll
-        for (int i = 0; i < N; ++i)
-          if (t[i] <= from_t && t[i] > to_t && r.weight(l[i])) {
-            const unsigned q = atomicAdd(&s.number, 1u);
-            if (q < LIST) {
-              s.list[q] = order_key(__fadd_rn(l[i], 0.f));
-              s.from[q] = (uint8_t)warp;
-            }
-          }
-      }
-    }
-    p.above = parts;
-    if (parts) p.mass = join_sums(hi, lo, parts);
+    });
+    if (parts) p.mass += join_sums(hi, lo, parts);
   }
   p.above = __reduce_add_sync(0xffffffffu, p.above);
 #pragma unroll
@@ -630,50 +715,72 @@ __device__ bool nucleus(Shared& s, const Row<T>& r, const RowRule& rule, unsigne
     s.above[warp] = p.above;
     s.tied[warp] = 0;
   }
-  const unsigned long long sure = cluster_sum(s, lane == 0 ? p.mass : 0ull, &s.sure64, C);
+  const unsigned long long sure = team_sum(s, lane == 0 ? p.mass : 0ull, &s.sure64, team);
   bool over = false;
-  for (int k = 0; k < C; ++k) over = over || ld_peer(&s.number, k) > LIST;
-  cluster_barrier();
-  if (over) return false;
-  // sure < target: theta is in the list
+  for (int k = 0; k < C; ++k) over = over || team.load(&s.number, k) > LIST;
+  team.barrier();
+  // sure < target: theta is among the bins' entries
   unsigned long long left = target - sure;
-  unsigned klo = order_key(-3.4028235e38f), khi = order_key(r.max);
-  descend<true, true>(s, r, rank, C, klo, khi, left);
+  // the listed entries' scores, with room for the roundings of t
+  auto score_at = [&](float t, float room) {
+    return __fadd_rn(r.max, __fdiv_rn(t + room, r.scale)) + room * 1e-4f * fabsf(r.max);
+  };
+  unsigned klo = order_key(fmaxf(score_at(to_t, -0.01f), -3.4028235e38f));
+  unsigned khi = order_key(fminf(score_at(from_t, 0.01f), r.max));
+  auto settle = [&](auto listed) {  // theta, and what the bins' entries add to the regions
+    constexpr bool L = decltype(listed)::value;
+    descend<true, L>(s, r, team, klo, khi, left, from_t);
+    each_score<L>(s, r, order_value(khi), [&](float l, int region) {
+      if (!L && r.scaled(l) > from_t) return;
+      const unsigned long long w = r.weight(l);
+      if (!w) return;
+      const bool tie = order_key(__fadd_rn(l, 0.f)) == khi;
+      if (!tie) atomicAdd(&s.mass[region], w);
+      atomicAdd(tie ? &s.tied[region] : &s.above[region], 1u);
+    });
+  };
+  if (over)
+    settle(std::false_type());
+  else
+    settle(std::true_type());
   theta = order_value(khi);
   const unsigned long long wt = r.weight(theta);
   ties = (unsigned)((left + wt - 1) / wt);
-  for (unsigned i = tid; i < s.number; i += RT) {
-    const unsigned k = s.list[i];
-    if (k > khi) {
-      atomicAdd(&s.mass[s.from[i]], r.weight(order_value(k)));
-      atomicAdd(&s.above[s.from[i]], 1u);
-    } else if (k == khi) {
-      atomicAdd(&s.tied[s.from[i]], 1u);
-    }
-  }
-  m = by_regions(s, r, C, theta, ties);
-  return true;
+  m = by_regions(s, r, team, theta, ties);
 }
 
-template <class T>
-__device__ void sample_row(Shared& s, Row<T>& r, const RowRule& rule, unsigned rank, int C,
+template <class T, bool SOLO>
+__device__ void sample_row(Shared& s, Row<T>& r, const RowRule& rule, const Team<SOLO>& team,
                            uint64_t word, int32_t* id, float* logp, int32_t* kept) {
+  const int C = team.size();
+  const unsigned rank = team.rank;
   constexpr int N = Row<T>::N;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   // one pass over memory: the row's entries into shared memory, each thread's maximum
   float tm = -INFINITY;
   {
-    const int b = r.begin(warp), e = r.end(warp);
+    const int b = r.begin(warp), e = r.end(warp), whole = r.view.whole();
     uint4* mine = r.buffer + warp * r.resident;
-#pragma unroll 4
-    for (int at = b + lane; at < e; at += 32) {
-      const uint4 u = r.view.fetch(at);
+    auto take = [&](uint4 u, int at) {
       if (at - b < r.resident) mine[at - b] = u;
       float l[N];
       r.scores(u, l);
 #pragma unroll
       for (int i = 0; i < N; ++i) tm = fmaxf(tm, l[i]);
+    };
+    int at = b + lane;
+    if (b == 0) {  // the row's first vector may be a part of one
+      if (at < e) take(r.view.fetch(at), at);
+      at += 32;
     }
+    for (; at - lane + 128 <= min(e, whole); at += 128) {  // four loads in flight
+      uint4 u[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) u[k] = r.view.inner(at + 32 * k);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) take(u[k], at + 32 * k);
+    }
+    for (; at < e; at += 32) take(r.view.fetch(at), at);
   }
   tm = __fadd_rn(tm, 0.f);
   {
@@ -695,11 +802,11 @@ __device__ void sample_row(Shared& s, Row<T>& r, const RowRule& rule, unsigned r
       }
     }
   }
-  cluster_barrier();
+  team.barrier();
   unsigned top = 0, low = 0xffffffffu;
   {
-    const unsigned t = lane < C ? ld_peer(&s.top, lane) : 0u;
-    const unsigned w = lane < C ? ld_peer(&s.low, lane) : 0xffffffffu;
+    const unsigned t = lane < C ? team.load(&s.top, lane) : 0u;
+    const unsigned w = lane < C ? team.load(&s.low, lane) : 0xffffffffu;
     top = __reduce_max_sync(0xffffffffu, t);
     low = __reduce_min_sync(0xffffffffu, w);
   }
@@ -729,13 +836,13 @@ __device__ void sample_row(Shared& s, Row<T>& r, const RowRule& rule, unsigned r
     if (inv < 1e30f) {
       if (r.weight(tm)) {
         const unsigned b = min((unsigned)(int)__fmul_rn(__fsub_rn(r.max, tm), inv), CBINS - 1u);
-        add_peer(&s.count[b], 0, 1u);
+        team.add(&s.count[b], 0, 1u);
       }
-      cluster_barrier();
+      team.barrier();
       unsigned c[CBINS / RT], sum = 0, all;
 #pragma unroll
       for (int i = 0; i < CBINS / RT; ++i) {
-        c[i] = ld_peer(&s.count[tid * (CBINS / RT) + i], 0);
+        c[i] = team.load(&s.count[tid * (CBINS / RT) + i], 0);
         sum += c[i];
       }
       unsigned before = block_exclusive(sum, s.part32, &all);
@@ -744,15 +851,18 @@ __device__ void sample_row(Shared& s, Row<T>& r, const RowRule& rule, unsigned r
         if (before < rule.top_k && rule.top_k <= before + c[i]) s.digit = tid * (CBINS / RT) + i;
         before += c[i];
       }
-      cluster_barrier();
+      team.barrier();
       if (all >= rule.top_k)
-        done = rank_list(s, r, rule, rank, C, inv, (float)s.digit + 1.f, theta, ties);
+        done = rank_list(s, r, rule, team, inv, (float)s.digit + 1.f, theta, ties);
       else if (rule.least > 1)
-        done = rank_list(s, r, rule, rank, C, 0.f, 1.f, theta, ties);
+        done = rank_list(s, r, rule, team, 0.f, 1.f, theta, ties);
       limited = done;
     }
   }
-  if (!by_k && by_p && !r.odd) done = measured = nucleus(s, r, rule, rank, C, theta, ties, m);
+  if (!by_k && by_p && !r.odd) {
+    nucleus(s, r, rule, team, theta, ties, m);
+    done = measured = true;
+  }
   if (!done) {
     // keys an eligible entry can have: t >= tmin, with room for its roundings
     const float edge = r.odd ? -INFINITY
@@ -761,15 +871,15 @@ __device__ void sample_row(Shared& s, Row<T>& r, const RowRule& rule, unsigned r
     if (by_k) {
       unsigned khi = top;
       unsigned long long left = rule.top_k;
-      if (descend<false, false>(s, r, rank, C, klo, khi, left)) {
+      if (descend<false, false>(s, r, team, klo, khi, left)) {
         theta = order_value(khi);
         ties = (unsigned)left;
         limited = true;
       }
     }
     if (by_p) {
-      m = measure_row(s, r, C, theta, ties);
-      cluster_barrier();
+      m = measure_row(s, r, team, theta, ties);
+      team.barrier();
       unsigned long long target =
           (m.total >> 31) * rule.part + (((m.total & 0x7fffffffull) * rule.part) >> 31);
       if (!target) target = 1;
@@ -780,7 +890,7 @@ __device__ void sample_row(Shared& s, Row<T>& r, const RowRule& rule, unsigned r
         if (limited) klo = order_key(theta) + 1;
         unsigned khi = top;
         unsigned long long left = target;
-        descend<true, false>(s, r, rank, C, klo, khi, left);
+        descend<true, false>(s, r, team, klo, khi, left);
         theta = order_value(khi);
         const unsigned long long wt = r.weight(theta);
         ties = (unsigned)((left + wt - 1) / wt);
@@ -789,7 +899,7 @@ __device__ void sample_row(Shared& s, Row<T>& r, const RowRule& rule, unsigned r
   }
 
   // the draw: the warp's region it falls in, then a sixteenth of that region, then a vector
-  if (!measured) m = measure_row(s, r, C, theta, ties);
+  if (!measured) m = measure_row(s, r, team, theta, ties);
   const unsigned long long at = __umul64hi(word, m.total);
   if (tid < C * RW && at >= m.before && at - m.before < m.kept) {
     s.digit = tid;
@@ -871,30 +981,33 @@ __device__ void sample_row(Shared& s, Row<T>& r, const RowRule& rule, unsigned r
 
 // A cluster of C blocks takes a row: block c its c-th contiguous part, each of the block's warps a
 // contiguous region of that, so that the index order is the order of (block, warp, vector, lane).
-template <class T>
+template <class T, bool SOLO>
 __global__ void __launch_bounds__(RT, 2)
     k_sample_rows(int64_t rows, int64_t n, const T* __restrict__ logits, int64_t stride,
                   const uint64_t* __restrict__ words, erc_sample_rule rule, int C, int resident,
                   int32_t* __restrict__ ids, float* __restrict__ logp, int32_t* __restrict__ kept) {
   extern __shared__ uint4 buffer[];
   __shared__ Shared s;
-  const unsigned rank = cluster_rank();
+  const Team<SOLO> team(C);
+  C = team.size();
   for (int64_t row = blockIdx.x / C; row < rows; row += gridDim.x / C) {
     Row<T> r = {RowView<T>(logits + row * stride, n)};
     const int part = (r.view.vectors + C - 1) / C;
     r.buffer = buffer;
     r.resident = resident;
-    r.first = min(r.view.vectors, (int)rank * part);
+    r.first = min(r.view.vectors, (int)team.rank * part);
     r.last = min(r.view.vectors, r.first + part);
     r.region = (part + RT - 1) / RT * 32;
-    sample_row(s, r, row_rule(rule, row), rank, C, words[row], &ids[row], &logp[row], &kept[row]);
-    cluster_barrier();
+    sample_row(s, r, row_rule(rule, row), team, words[row], &ids[row], &logp[row], &kept[row]);
+    team.barrier();
   }
 }
 
-// Vectors of a warp's region kept in shared memory, blocks of a cluster, and the dynamic bytes.
-// C is the smallest power of two whose blocks can hold the row (16 at most), then as many more as
-// the machine has room for at two blocks an SM, while a block still gets 4096 entries.
+// Vectors of a warp's region kept in shared memory, blocks of a row, and the dynamic bytes.
+// A block holds at most 2^18 entries (sums of 14-bit limbs and of weight parts stay in 32 bits).
+// Beyond that, blocks are added to a row while the machine has room for them (two blocks an SM)
+// and a block still gets 4096 entries; rows that fill the machine by themselves take one block
+// each and read what shared memory does not hold again from L2.
 struct Shape {
   int C, resident;
   size_t bytes;
@@ -904,7 +1017,7 @@ Shape shape_of(int64_t rows, int64_t n, int elt) {
   auto region = [&](int C) { return ((vectors + C - 1) / C + RT - 1) / RT * 32; };
   Shape h;
   h.C = 1;
-  while (h.C < MAX_C && region(h.C) * RW * 16 > ROOM) h.C *= 2;
+  while (h.C < MAX_C && n > ((int64_t)h.C << 18)) h.C *= 2;
   while (h.C < MAX_C && rows * h.C * 2 <= 2 * sm_count() && n >= h.C * 2 * 4096) h.C *= 2;
   const int64_t most = ROOM / (RW * 16) / 32 * 32;
   h.resident = (int)(region(h.C) < most ? region(h.C) : most);
@@ -1098,14 +1211,16 @@ erc_status launch_rows(int64_t rows, int64_t n, const T* logits, int64_t stride,
     return ERC_OK;
   }
   const Shape h = shape_of(rows, n, (int)sizeof(T));
-  static std::atomic<uint64_t> ready{0};  // devices whose kernel has its attributes, one bit each
+  static std::atomic<uint64_t> ready{0};  // devices whose kernels have their attributes, one bit each
   int dev = 0;
   ERC_CUDA(cudaGetDevice(&dev));
   if (dev >= 64 || !(ready.load(std::memory_order_acquire) >> dev & 1)) {
-    ERC_CUDA(cudaFuncSetAttribute(k_sample_rows<T>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                  ROOM));
-    ERC_CUDA(cudaFuncSetAttribute(k_sample_rows<T>, cudaFuncAttributeNonPortableClusterSizeAllowed,
-                                  1));
+    ERC_CUDA(cudaFuncSetAttribute(k_sample_rows<T, true>,
+                                  cudaFuncAttributeMaxDynamicSharedMemorySize, ROOM));
+    ERC_CUDA(cudaFuncSetAttribute(k_sample_rows<T, false>,
+                                  cudaFuncAttributeMaxDynamicSharedMemorySize, ROOM));
+    ERC_CUDA(cudaFuncSetAttribute(k_sample_rows<T, false>,
+                                  cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
     if (dev < 64) ready.fetch_or(1ull << dev, std::memory_order_release);
   }
   cudaLaunchConfig_t cfg = {};
@@ -1118,9 +1233,9 @@ erc_status launch_rows(int64_t rows, int64_t n, const T* logits, int64_t stride,
   at.val.clusterDim.x = h.C;
   at.val.clusterDim.y = at.val.clusterDim.z = 1;
   cfg.attrs = &at;
-  cfg.numAttrs = 1;
-  ERC_CUDA(cudaLaunchKernelEx(&cfg, k_sample_rows<T>, rows, n, logits, stride, words, rule, h.C,
-                              h.resident, ids, logp, kept));
+  cfg.numAttrs = h.C > 1;
+  ERC_CUDA(cudaLaunchKernelEx(&cfg, h.C > 1 ? k_sample_rows<T, false> : k_sample_rows<T, true>, rows,
+                              n, logits, stride, words, rule, h.C, h.resident, ids, logp, kept));
   count_launches(1);
   return ERC_OK;
 }

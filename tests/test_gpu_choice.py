@@ -80,6 +80,18 @@ def test_sample_long_rows(n, rows, rule):
 
 
 @pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("n", [60001, 250007])
+def test_sample_top_p_that_ends_inside_a_long_flat_tail(kind, n):
+    rng = np.random.default_rng(n)
+    rows = 4
+    x = rng.uniform(-0.3, 0.3, (rows, n)).astype(np.float32)  # a tail of nearly equal weights
+    x[np.arange(rows), rng.integers(0, n, rows)] = np.log(n) + np.array([2, 3, 1, 0], np.float32)  # 0.88, 0.95, ..
+    for p in (0.9, 0.96, 0.999):
+        check_sample(torch.from_numpy(x).to(dev()).to(TYPES[kind]), words_of(rng, rows), top_p=p)
+        check_sample(torch.from_numpy(x).to(dev()).to(TYPES[kind]), words_of(rng, rows), top_p=p, min_p=1e-6)
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
 def test_sample_the_largest_rows(kind):
     n = 1 << 22  # ERC_SAMPLE_ROWS_MAX_N
     rng = np.random.default_rng(5)
