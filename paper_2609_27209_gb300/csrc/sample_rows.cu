@@ -14,12 +14,13 @@ namespace {
 constexpr int RT = 512;       // threads of a block
 constexpr int RW = RT / 32;   // its warps
 constexpr int MAX_C = 16;     // blocks of a row's cluster
-constexpr int LIST = 4096;    // candidates ranked in one block's shared memory
+constexpr int LIST = 8192;    // candidates listed in a block's shared memory
+constexpr int RANK = 4096;    // candidates of a row that one block ranks
 constexpr int BINS = 1024;    // bins of one level of the descent
 constexpr int STEPS = 128;    // bins an octave of the weights' histogram
 constexpr int WBINS = 4096;   // its bins
 constexpr int CBINS = 1024;   // bins of the threads' maxima
-constexpr int ROOM = 72 * 1024;  // bytes of a row in a block's shared memory (two blocks an SM)
+constexpr int ROOM = 48 * 1024;  // bytes of a row in a block's shared memory (two blocks an SM)
 
 struct RowRule {
   float scale;               // log2(e) / T
@@ -199,54 +200,45 @@ __device__ __forceinline__ void each_vector(const Row<T>& r, int warp, int from,
 template <class T>
 __device__ Part measure(const Row<T>& r, int warp, int from, int to, float theta) {
   constexpr int N = Row<T>::N;
-  const int lane = threadIdx.x & 31;
   Part p = {0, 0, 0};
   unsigned hi = 0, lo = 0, parts = 0;
-  for (int at = from + lane; at - lane < to; at += 32) {
-    float l[N], t[N];
-    r.scores(r.get(warp, at, to), l);
-    float best = -INFINITY;
+  if (r.least == 1 && theta == -INFINITY && !r.odd) {
+    const uint64_t m2 = pair(-r.max, -r.max), s2 = pair(r.scale, r.scale);
+    each_vector(r, warp, from, to, [&](uint4 u) {
+      uint64_t l[N / 2];
+      unpack_pairs<T>(u, l);
 #pragma unroll
-    for (int i = 0; i < N; ++i) best = fmaxf(best, l[i]);
-    if (!(best >= theta) || best == -INFINITY) continue;
-    best = -INFINITY;
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      t[i] = r.scaled(l[i]);
-      best = fmaxf(best, t[i]);
-    }
-    if (!(best >= r.tmin)) continue;
-    if (r.least == 1 && theta == -INFINITY) {
-#pragma unroll
-      for (int i = 0; i < N; i += 2) {
+      for (int i = 0; i < N / 2; ++i) {
+        float t[2], v[2];
         unsigned h[2], w[2];
-        float v[2];
-        weight_parts(t[i], t[i + 1], h, w, v);
+        unpair(mul2(add2(l[i], m2), s2), t[0], t[1]);
+        weight_parts(t[0], t[1], h, w, v);
         hi += h[0] + h[1];
         lo += w[0] + w[1];
         p.above += (v[0] >= 0x1p-41f) + (v[1] >= 0x1p-41f);
       }
       parts += N;
-    } else {
+    });
+  } else {
+    each_vector(r, warp, from, to, [&](uint4 u) {
+      float l[N], best = -INFINITY;
+      r.scores(u, l);
 #pragma unroll
-      for (int i = 0; i < N; i += 2) {
-        unsigned h[2], w[2];
-        float v[2];
-        weight_parts(t[i], t[i + 1], h, w, v);
+      for (int i = 0; i < N; ++i) best = fmaxf(best, l[i]);
+      if (!(best >= theta) || !(r.scaled(best) >= r.tmin)) return;
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          const unsigned long long x = join_parts(h[j], w[j]);
-          const bool in = x >= r.least && l[i + j] >= theta;
-          if (in && l[i + j] > theta) {
-            p.mass += x;
-            ++p.above;
-          } else if (in) {
-            ++p.tied;
-          }
+      for (int i = 0; i < N; ++i) {
+        const unsigned long long w = l[i] >= theta && r.scaled(l[i]) >= r.tmin ? r.weight(l[i]) : 0ull;
+        if (w && l[i] == theta) {
+          ++p.tied;
+        } else if (w) {
+          p.mass += w;
+          ++p.above;
         }
       }
-    }
+    });
   }
+  if (parts)
   p.mass += join_sums(hi, lo, parts);
   p.above = __reduce_add_sync(0xffffffffu, p.above);
   p.tied = __reduce_add_sync(0xffffffffu, p.tied);
@@ -410,7 +402,7 @@ __device__ bool descend(Shared& s, const Row<T>& r, const Team<SOLO>& team, unsi
   }
 }
 
-// Ranks at most LIST candidates in block 0: top-k, then top-p, to (theta, ties).  Returns false,
+// Ranks at most RANK candidates in block 0: top-k, then top-p, to (theta, ties).  Returns false,
 // with nothing decided, where there are more.  Candidates are the eligible entries whose distance
 // from the maximum is below `reach` (all of them: reach = inf).
 template <class T, bool SOLO>
@@ -420,20 +412,22 @@ __device__ bool rank_list(Shared& s, const Row<T>& r, const RowRule& rule,
   const int C = team.size();
   const unsigned rank = team.rank;
   constexpr int N = Row<T>::N;
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int tid = threadIdx.x, warp = tid >> 5;
   if (tid == 0) s.number = 0;
   __syncthreads();
-  const int stop = r.end(warp);
-  for (int at = r.begin(warp) + lane; at - lane < stop; at += 32) {
-    float l[N];
-    r.scores(r.get(warp, at, stop), l);
+  each_vector(r, warp, r.begin(warp), r.end(warp), [&](uint4 u) {
+    float l[N], best = -INFINITY;
+    r.scores(u, l);
+#pragma unroll
+    for (int i = 0; i < N; ++i) best = fmaxf(best, l[i]);
+    if (!(__fmul_rn(__fsub_rn(r.max, best), inv) < reach)) return;
 #pragma unroll
     for (int i = 0; i < N; ++i)
       if (__fmul_rn(__fsub_rn(r.max, l[i]), inv) < reach && r.weight(l[i])) {
         const unsigned p = atomicAdd(&s.number, 1u);
-        if (p < LIST) s.list[p] = order_key(__fadd_rn(l[i], 0.f));
+        if (p < RANK) s.list[p] = order_key(__fadd_rn(l[i], 0.f));
       }
-  }
+  });
   team.barrier();
   unsigned all = 0, mine = 0;
   for (int c = 0; c < C; ++c) {
@@ -441,7 +435,7 @@ __device__ bool rank_list(Shared& s, const Row<T>& r, const RowRule& rule,
     if (c == 0) mine = q;
     all += q;
   }
-  if (all > LIST) {
+  if (all > RANK) {
     team.barrier();
     return false;
   }
@@ -468,12 +462,12 @@ __device__ bool rank_list(Shared& s, const Row<T>& r, const RowRule& rule,
         }
         __syncthreads();
       }
-    // each thread takes LIST / RT consecutive candidates
+    // each thread takes RANK / RT consecutive candidates
     const unsigned keep = min(all, rule.top_k);
-    unsigned long long w[LIST / RT], sum = 0, total;
+    unsigned long long w[RANK / RT], sum = 0, total;
 #pragma unroll
-    for (int i = 0; i < LIST / RT; ++i) {
-      const unsigned at_i = tid * (LIST / RT) + i;
+    for (int i = 0; i < RANK / RT; ++i) {
+      const unsigned at_i = tid * (RANK / RT) + i;
       w[i] = at_i < keep ? r.weight(order_value(s.list[at_i])) : 0ull;
       sum += w[i];
     }
@@ -485,7 +479,7 @@ __device__ bool rank_list(Shared& s, const Row<T>& r, const RowRule& rule,
     }
     unsigned kept = 0;
 #pragma unroll
-    for (int i = 0; i < LIST / RT; ++i) {
+    for (int i = 0; i < RANK / RT; ++i) {
       if (w[i] && before < target) ++kept;
       before += w[i];
     }
@@ -524,6 +518,38 @@ __device__ unsigned long long team_sum(Shared& s, unsigned long long v, unsigned
 #pragma unroll
   for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
   return sum;
+}
+
+// whether a block's list holds more than it can
+template <bool SOLO>
+__device__ bool overflowed(Shared& s, const Team<SOLO>& team) {
+  bool over = false;
+  for (int k = 0; k < team.size(); ++k) over = over || team.load(&s.number, k) > LIST;
+  return over;
+}
+
+// the keys of entries with to_t < t <= from_t, with room for the roundings of t
+template <class T>
+__device__ __forceinline__ void bin_keys(const Row<T>& r, float to_t, float from_t, unsigned& klo,
+                                         unsigned& khi) {
+  auto score_at = [&](float t, float room) {
+    return __fadd_rn(r.max, __fdiv_rn(t + room, r.scale)) + room * 1e-4f * fabsf(r.max);
+  };
+  klo = order_key(fmaxf(score_at(to_t, -0.01f), -3.4028235e38f));
+  khi = order_key(fminf(score_at(from_t, 0.01f), r.max));
+}
+
+// appends the lanes' entries to the block's list
+__device__ __forceinline__ void append(Shared& s, bool in, float l, int warp) {
+  const int lane = threadIdx.x & 31;
+  const unsigned those = __ballot_sync(0xffffffffu, in);
+  unsigned q = 0;
+  if (lane == 0) q = atomicAdd(&s.number, (unsigned)__popc(those));
+  q = __shfl_sync(0xffffffffu, q, 0) + __popc(those & ((1u << lane) - 1));
+  if (in && q < LIST) {
+    s.list[q] = order_key(__fadd_rn(l, 0.f));
+    s.from[q] = (uint8_t)warp;
+  }
 }
 
 // Top-p alone over long rows.  One pass weighs the row and counts its entries by weight, STEPS bins
@@ -671,15 +697,7 @@ __device__ void nucleus(Shared& s, const Row<T>& r, const RowRule& rule, const T
         float x0, x1;
         unpair(l[i / 2], x0, x1);
         const float x = i & 1 ? x1 : x0;
-        const bool in = (who >> lane & 1) && (r.least <= 1 || r.weight(x));
-        const unsigned those = __ballot_sync(0xffffffffu, in);
-        unsigned q = 0;
-        if (lane == 0) q = atomicAdd(&s.number, (unsigned)__popc(those));
-        q = __shfl_sync(0xffffffffu, q, 0) + __popc(those & ((1u << lane) - 1));
-        if (in && q < LIST) {
-          s.list[q] = order_key(__fadd_rn(x, 0.f));
-          s.from[q] = (uint8_t)warp;
-        }
+        append(s, (who >> lane & 1) && (r.least <= 1 || r.weight(x)), x, warp);
       }
       if (!__any_sync(0xffffffffu, best > from_t)) return;
       if (r.least <= 1) {
@@ -716,17 +734,12 @@ __device__ void nucleus(Shared& s, const Row<T>& r, const RowRule& rule, const T
     s.tied[warp] = 0;
   }
   const unsigned long long sure = team_sum(s, lane == 0 ? p.mass : 0ull, &s.sure64, team);
-  bool over = false;
-  for (int k = 0; k < C; ++k) over = over || team.load(&s.number, k) > LIST;
+  const bool over = overflowed(s, team);
   team.barrier();
   // sure < target: theta is among the bins' entries
   unsigned long long left = target - sure;
-  // the listed entries' scores, with room for the roundings of t
-  auto score_at = [&](float t, float room) {
-    return __fadd_rn(r.max, __fdiv_rn(t + room, r.scale)) + room * 1e-4f * fabsf(r.max);
-  };
-  unsigned klo = order_key(fmaxf(score_at(to_t, -0.01f), -3.4028235e38f));
-  unsigned khi = order_key(fminf(score_at(from_t, 0.01f), r.max));
+  unsigned klo, khi;
+  bin_keys(r, to_t, from_t, klo, khi);
   auto settle = [&](auto listed) {  // theta, and what the bins' entries add to the regions
     constexpr bool L = decltype(listed)::value;
     descend<true, L>(s, r, team, klo, khi, left, from_t);
@@ -749,6 +762,91 @@ __device__ void nucleus(Shared& s, const Row<T>& r, const RowRule& rule, const T
   m = by_regions(s, r, team, theta, ties);
 }
 
+// Top-k with more entries than the threads' maxima can bound: a pass counts the entries by the bins
+// of nucleus(), which gives the bin of the top_k-th exactly.  Where the entries down to that bin
+// can be ranked, they are (done: true).  Else the bin's entries are listed and theta found among
+// them, without top-p (limited).  Neither, where fewer than top_k entries lie in the bins.
+template <class T, bool SOLO>
+__device__ bool tally(Shared& s, const Row<T>& r, const RowRule& rule, const Team<SOLO>& team,
+                      float& theta, unsigned& ties, bool& limited) {
+  constexpr int N = Row<T>::N;
+  constexpr int P = WBINS / RT;
+  const int tid = threadIdx.x, warp = tid >> 5;
+  const float low = fmaxf(r.tmin - 1.f, -(float)WBINS / STEPS);
+  team.barrier();  // the bins share memory with counts that other blocks read
+  for (int b = tid; b < WBINS; b += RT) s.wbins[b] = 0;
+  if (tid == 0) s.number = 0;
+  __syncthreads();
+  each_vector(r, warp, r.begin(warp), r.end(warp), [&](uint4 u) {
+    float l[N];
+    r.scores(u, l);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const float t = r.scaled(l[i]);
+      if (t > low && (r.least <= 1 || r.weight(l[i])))
+        atomicAdd(&s.wbins[__float_as_uint(__fmaf_rz(t, -(float)STEPS, 8388608.f)) - BIAS], 1u);
+    }
+  });
+  team.barrier();
+  unsigned c[P] = {}, sum = 0, all;
+#pragma unroll 4
+  for (int k = 0; k < team.size(); ++k)
+#pragma unroll
+    for (int i = 0; i < P; i += 4) {
+      const uint4 q = team.load(reinterpret_cast<const uint4*>(&s.wbins[tid * P + i]), k);
+      c[i] += q.x;
+      c[i + 1] += q.y;
+      c[i + 2] += q.z;
+      c[i + 3] += q.w;
+    }
+#pragma unroll
+  for (int i = 0; i < P; ++i) sum += c[i];
+  unsigned before = block_exclusive(sum, s.part32, &all);
+#pragma unroll
+  for (int i = 0; i < P; ++i) {
+    if (before < rule.top_k && rule.top_k <= before + c[i]) {
+      s.first_bin = tid * P + i;
+      s.some = before;
+      s.digit = c[i];
+    }
+    before += c[i];
+  }
+  team.barrier();
+  if (all < rule.top_k) {
+    // every eligible entry, where all of them lie in the bins and can be ranked
+    return r.tmin - 1.f > -(float)WBINS / STEPS && all <= RANK &&
+           rank_list(s, r, rule, team, r.scale, -low, theta, ties);
+  }
+  const unsigned bin = s.first_bin;
+  const float from_t = -(float)bin * (1.f / STEPS), to_t = -(float)(bin + 1) * (1.f / STEPS);
+  unsigned long long left = rule.top_k - s.some;
+  if (s.some + s.digit <= RANK) return rank_list(s, r, rule, team, r.scale, -to_t, theta, ties);
+  __syncthreads();
+  each_vector(r, warp, r.begin(warp), r.end(warp), [&](uint4 u) {
+    float l[N];
+    r.scores(u, l);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const float t = r.scaled(l[i]);
+      if (__any_sync(0xffffffffu, t <= from_t && t > to_t))
+        append(s, t <= from_t && t > to_t && r.weight(l[i]), l[i], warp);
+    }
+  });
+  team.barrier();
+  const bool over = overflowed(s, team);
+  team.barrier();
+  unsigned klo, khi;
+  bin_keys(r, to_t, from_t, klo, khi);
+  if (over)
+    descend<false, false>(s, r, team, klo, khi, left, from_t);
+  else
+    descend<false, true>(s, r, team, klo, khi, left, from_t);
+  theta = order_value(khi);
+  ties = (unsigned)left;
+  limited = true;
+  return rule.part == 0xffffffffu;
+}
+
 template <class T, bool SOLO>
 __device__ void sample_row(Shared& s, Row<T>& r, const RowRule& rule, const Team<SOLO>& team,
                            uint64_t word, int32_t* id, float* logp, int32_t* kept) {
@@ -757,20 +855,23 @@ __device__ void sample_row(Shared& s, Row<T>& r, const RowRule& rule, const Team
   constexpr int N = Row<T>::N;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   // one pass over memory: the row's entries into shared memory, each thread's maximum
-  float tm = -INFINITY;
+  constexpr int TM = 4;  // maxima a thread keeps
+  float tm[TM];
+#pragma unroll
+  for (int k = 0; k < TM; ++k) tm[k] = -INFINITY;
   {
     const int b = r.begin(warp), e = r.end(warp), whole = r.view.whole();
     uint4* mine = r.buffer + warp * r.resident;
-    auto take = [&](uint4 u, int at) {
+    auto take = [&](uint4 u, int at, float& m) {
       if (at - b < r.resident) mine[at - b] = u;
       float l[N];
       r.scores(u, l);
 #pragma unroll
-      for (int i = 0; i < N; ++i) tm = fmaxf(tm, l[i]);
+      for (int i = 0; i < N; ++i) m = fmaxf(m, l[i]);
     };
     int at = b + lane;
     if (b == 0) {  // the row's first vector may be a part of one
-      if (at < e) take(r.view.fetch(at), at);
+      if (at < e) take(r.view.fetch(at), at, tm[0]);
       at += 32;
     }
     for (; at - lane + 128 <= min(e, whole); at += 128) {  // four loads in flight
@@ -778,15 +879,23 @@ __device__ void sample_row(Shared& s, Row<T>& r, const RowRule& rule, const Team
 #pragma unroll
       for (int k = 0; k < 4; ++k) u[k] = r.view.inner(at + 32 * k);
 #pragma unroll
-      for (int k = 0; k < 4; ++k) take(u[k], at + 32 * k);
+      for (int k = 0; k < 4; ++k) take(u[k], at + 32 * k, tm[k]);
     }
-    for (; at < e; at += 32) take(r.view.fetch(at), at);
+#pragma unroll
+    for (int k = 1; k < TM; ++k, at += 32)
+      if (at < e) take(r.view.fetch(at), at, tm[k]);
+    if (at < e) take(r.view.fetch(at), at, tm[0]);
   }
-  tm = __fadd_rn(tm, 0.f);
   {
-    const unsigned k = order_key(tm);
-    const unsigned hi = __reduce_max_sync(0xffffffffu, k);
-    const unsigned lo = __reduce_min_sync(0xffffffffu, tm == -INFINITY ? 0xffffffffu : k);
+    unsigned hi = 0, lo = 0xffffffffu;
+#pragma unroll
+    for (int k = 0; k < TM; ++k) {
+      tm[k] = __fadd_rn(tm[k], 0.f);
+      hi = max(hi, order_key(tm[k]));
+      if (tm[k] != -INFINITY) lo = min(lo, order_key(tm[k]));
+    }
+    hi = __reduce_max_sync(0xffffffffu, hi);
+    lo = __reduce_min_sync(0xffffffffu, lo);
     if (lane == 0) {
       s.part32[warp] = hi;
       s.above[warp] = lo;
@@ -833,11 +942,13 @@ __device__ void sample_row(Shared& s, Row<T>& r, const RowRule& rule, const Team
     // At least top_k entries lie no lower than the top_k-th best of the threads' maxima: those down
     // to its bin are the candidates.
     const float inv = __fdiv_rn(1023.f, __fsub_rn(r.max, order_value(low)));
-    if (inv < 1e30f) {
-      if (r.weight(tm)) {
-        const unsigned b = min((unsigned)(int)__fmul_rn(__fsub_rn(r.max, tm), inv), CBINS - 1u);
-        team.add(&s.count[b], 0, 1u);
-      }
+    if (inv < 1e30f && rule.top_k <= (unsigned)(RT * TM / 4 * C)) {
+#pragma unroll
+      for (int k = 0; k < TM; ++k)
+        if (r.weight(tm[k])) {
+          const unsigned b = min((unsigned)(int)__fmul_rn(__fsub_rn(r.max, tm[k]), inv), CBINS - 1u);
+          team.add(&s.count[b], 0, 1u);
+        }
       team.barrier();
       unsigned c[CBINS / RT], sum = 0, all;
 #pragma unroll
@@ -854,10 +965,8 @@ __device__ void sample_row(Shared& s, Row<T>& r, const RowRule& rule, const Team
       team.barrier();
       if (all >= rule.top_k)
         done = rank_list(s, r, rule, team, inv, (float)s.digit + 1.f, theta, ties);
-      else if (rule.least > 1)
-        done = rank_list(s, r, rule, team, 0.f, 1.f, theta, ties);
-      limited = done;
     }
+    if (!done) done = tally(s, r, rule, team, theta, ties, limited);
   }
   if (!by_k && by_p && !r.odd) {
     nucleus(s, r, rule, team, theta, ties, m);
@@ -868,7 +977,7 @@ __device__ void sample_row(Shared& s, Row<T>& r, const RowRule& rule, const Team
     const float edge = r.odd ? -INFINITY
                              : __fadd_rn(r.max, __fdiv_rn(r.tmin - 0.5f, r.scale)) - 1e-5f * fabsf(r.max);
     unsigned klo = order_key(fmaxf(edge, -3.4028235e38f));
-    if (by_k) {
+    if (by_k && !limited) {
       unsigned khi = top;
       unsigned long long left = rule.top_k;
       if (descend<false, false>(s, r, team, klo, khi, left)) {
