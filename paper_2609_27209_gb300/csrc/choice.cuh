@@ -118,10 +118,9 @@ __device__ __forceinline__ uint64_t fma2_rz(uint64_t a, uint64_t b, uint64_t c) 
 
 constexpr unsigned BIAS = 0x4B000000u;  // 2^23's pattern
 
-// weights of two scaled scores: hi and lo with their biases, and 2^t itself
-__device__ __forceinline__ void weight_parts(float t0, float t1, unsigned hi[2], unsigned lo[2],
-                                             float v[2]) {
-  const uint64_t t = pair(fmaxf(t0, -60.f), fmaxf(t1, -60.f));
+// the polynomial of two scaled scores (|t| < 2^22), and t + 1.5 2^23, whose low bits are rint(t)
+__device__ __forceinline__ void pow2_pair(float t0, float t1, float p_out[2], float r_out[2]) {
+  const uint64_t t = pair(t0, t1);
   const uint64_t shifter = pair(12582912.f, 12582912.f);  // 1.5 2^23: adding it rounds to an integer
   const uint64_t r = add2(t, shifter);
   const uint64_t e = add2(r, pair(-12582912.f, -12582912.f));
@@ -131,11 +130,16 @@ __device__ __forceinline__ void weight_parts(float t0, float t1, unsigned hi[2],
   p = add2(mul2(p, f), pair(0.24022242f, 0.24022242f));
   p = add2(mul2(p, f), pair(0.693147f, 0.693147f));
   p = add2(mul2(p, f), pair(1.f, 1.f));
-  float p0, p1, r0, r1;
-  unpair(p, p0, p1);
-  unpair(r, r0, r1);
-  v[0] = __uint_as_float(__float_as_uint(p0) + (__float_as_uint(r0) << 23));
-  v[1] = __uint_as_float(__float_as_uint(p1) + (__float_as_uint(r1) << 23));
+  unpair(p, p_out[0], p_out[1]);
+  unpair(r, r_out[0], r_out[1]);
+}
+// weights of two scaled scores: hi and lo with their biases, and 2^t itself
+__device__ __forceinline__ void weight_parts(float t0, float t1, unsigned hi[2], unsigned lo[2],
+                                             float v[2]) {
+  float p[2], r[2];
+  pow2_pair(fmaxf(t0, -60.f), fmaxf(t1, -60.f), p, r);
+  v[0] = __uint_as_float(__float_as_uint(p[0]) + (__float_as_uint(r[0]) << 23));
+  v[1] = __uint_as_float(__float_as_uint(p[1]) + (__float_as_uint(r[1]) << 23));
   const uint64_t vv = pair(v[0], v[1]);
   const uint64_t two20 = pair(1048576.f, 1048576.f), two23 = pair(8388608.f, 8388608.f);
   const uint64_t h = fma2_rz(vv, two20, two23);

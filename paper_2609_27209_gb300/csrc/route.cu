@@ -121,44 +121,316 @@ __global__ void __launch_bounds__(QW * 32) k_route(int64_t rows, const T* __rest
   }
 }
 
-template <class T>
-__global__ void __launch_bounds__(QW * 32)
-    k_route_backward(int64_t rows, const T* __restrict__ logits, int64_t stride,
-                     const int32_t* __restrict__ experts, const float* __restrict__ dweights,
-                     erc_route_rule rule, T* __restrict__ dlogits) {
-  extern __shared__ float smem[];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int E = rule.experts, k = rule.k;
-  const int64_t row = (int64_t)blockIdx.x * QW + warp;
-  if (row >= rows) return;
-  float* sc = smem + warp * 2 * E;
-  float* ds = sc + E;
-  row_scores(logits + row * stride, E, rule.score, sc, lane);
-  for (int i = lane; i < E; i += 32) ds[i] = 0.f;
-  __syncwarp();
-  const int at = lane < k ? experts[row * k + lane] : -1;
-  const bool some = at >= 0 && at < E;
-  const float s = some ? fmaxf(sc[at], 0.f) : 0.f;
-  float g = some ? dweights[row * k + lane] * rule.scale : 0.f;
-  auto sum = [](float v) {
+// ------------------------------------------------------------------------------------------------
+// rows in registers: L lanes take a row, each V consecutive experts, so a warp takes 32 / L rows and
+// the lowest index among equals is the lowest (lane, place).
+// ------------------------------------------------------------------------------------------------
+constexpr int FW = 8;  // warps of a block
+
+template <int L>
+__device__ __forceinline__ unsigned lanes_max(unsigned v) {
+  if constexpr (L == 32) {
+    return __reduce_max_sync(0xffffffffu, v);
+  } else {
 #pragma unroll
-    for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    for (int o = L / 2; o; o >>= 1) v = max(v, __shfl_xor_sync(0xffffffffu, v, o));
     return v;
-  };
-  if (rule.renorm) {
-    const float D = sum(s);
-    const float p = D > 0.f ? s / D : 0.f;
-    const float gp = sum(g * p);
-    g = some && D > 0.f ? (g - gp) / D : 0.f;
   }
-  const float gs = sum(g * s);
-  if (some) atomicAdd(&ds[at], g);
+}
+template <int L>
+__device__ __forceinline__ unsigned lanes_sum(unsigned v) {
+  if constexpr (L == 32) {
+    return __reduce_add_sync(0xffffffffu, v);
+  } else {
+#pragma unroll
+    for (int o = L / 2; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+  }
+}
+template <int L>
+__device__ __forceinline__ float lanes_sum(float v) {
+#pragma unroll
+  for (int o = L / 2; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  return v;
+}
+
+// V scores of a lane from `first` on; masked from E on.  `wide`: 16-byte loads are aligned and V
+// divides E.
+template <class T, int V>
+__device__ __forceinline__ void load_scores(const T* x, int first, int E, bool wide, bool row,
+                                            float* l) {
+  constexpr int N = ScoreVec<T>::N;
+  if (!row || first >= E) {
+#pragma unroll
+    for (int j = 0; j < V; ++j) l[j] = -INFINITY;
+  } else if (wide) {
+#pragma unroll
+    for (int j = 0; j < V / N; ++j)
+      unpack_scores(__ldg(reinterpret_cast<const uint4*>(x + first) + j), l + j * N, T());
+  } else {
+#pragma unroll
+    for (int j = 0; j < V; ++j)
+      l[j] = first + j < E ? fmaxf(to_f32(x[first + j]), -INFINITY) : -INFINITY;
+  }
+}
+
+// the scores s_j of a lane's logits, -1 where masked
+template <int L, int V, bool SIGMOID>
+__device__ __forceinline__ void lane_scores(const float* l, float* s) {
+  if (SIGMOID) {
+#pragma unroll
+    for (int j = 0; j < V; j += 2) {
+      float t[2], p[2], r[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) t[i] = fmaxf(-__fmul_rn(fabsf(l[j + i]), LOG2E), -200.f);
+      pow2_pair(t[0], t[1], p, r);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const float x = l[j + i];
+        const float e = t[i] >= -126.5f
+                            ? __uint_as_float(__float_as_uint(p[i]) + (__float_as_uint(r[i]) << 23))
+                            : 0.f;
+        s[j + i] = x == -INFINITY ? -1.f : __fdiv_rn(x >= 0.f ? 1.f : e, __fadd_rn(1.f, e));
+      }
+    }
+  } else {
+    float m = l[0];
+#pragma unroll
+    for (int j = 1; j < V; ++j) m = fmaxf(m, l[j]);
+    m = order_value(lanes_max<L>(order_key(__fadd_rn(m, 0.f))));
+    unsigned hi = 0, lo = 0;
+#pragma unroll
+    for (int j = 0; j < V; j += 2) {
+      float t[2];
+      unsigned h[2], w[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) t[i] = l[j + i] == -INFINITY ? -60.f : below_max(l[j + i], m, LOG2E);
+      weight_parts(t[0], t[1], h, w, s + j);
+      hi += h[0] + h[1];
+      lo += w[0] + w[1];
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        if (!(t[i] > -41.5f)) s[j + i] = 0.f;
+    }
+    hi = lanes_sum<L>(hi - V * BIAS);
+    lo = lanes_sum<L>(lo - V * BIAS);
+    const unsigned long long z = ((unsigned long long)hi << 20) + lo;
+    const float inv = __frcp_rn(__fmul_rn(__ull2float_rn(z ? z : 1ull), 9.094947017729282e-13f));
+#pragma unroll
+    for (int j = 0; j < V; ++j) s[j] = l[j] == -INFINITY ? -1.f : __fmul_rn(s[j], inv);
+  }
+}
+
+template <class T, int L, int V, bool SIGMOID>
+__global__ void __launch_bounds__(FW * 32)
+    k_route_lanes(int64_t rows, const T* __restrict__ logits, int64_t stride,
+                  const float* __restrict__ bias, erc_route_rule rule, bool wide,
+                  int32_t* __restrict__ experts, float* __restrict__ weights) {
+  constexpr int R = 32 / L;  // rows of a warp
+  __shared__ float picked[FW * R][ERC_ROUTE_MAX_K];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, sub = lane / L, at = lane % L;
+  const int E = rule.experts, k = rule.k;
+  const int64_t row = ((int64_t)blockIdx.x * FW + warp) * R + sub;
+  const bool live = row < rows;
+  const unsigned mates = (L == 32 ? 0xffffffffu : ((1u << L) - 1)) << (sub * L);
+  const int first = at * V;
+  float l[V], s[V];
+  load_scores<T, V>(logits + (live ? row : 0) * stride, first, E, wide, live, l);
+  lane_scores<L, V, SIGMOID>(l, s);
+  unsigned key[V];  // 0: not to be chosen
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
+    float c = s[j];
+    if (bias) c = __fadd_rn(c, first + j < E ? __ldg(bias + first + j) : 0.f);
+    key[j] = s[j] < 0.f || c != c || c == -INFINITY ? 0u : order_key(__fadd_rn(c, 0.f));
+  }
+  if (rule.groups > 1 && rule.top_groups < rule.groups) {
+    // a group is `span` lanes; its best two, then its rank among the groups
+    const int span = E / rule.groups / V;
+    unsigned a = 0, b = 0;
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      b = max(b, min(a, key[j]));
+      a = max(a, key[j]);
+    }
+    for (int o = 1; o < span; o <<= 1) {
+      const unsigned a2 = __shfl_xor_sync(0xffffffffu, a, o), b2 = __shfl_xor_sync(0xffffffffu, b, o);
+      b = max(max(b, b2), min(a, a2));
+      a = max(a, a2);
+    }
+    float g = a ? order_value(a) : -INFINITY;
+    if (b && rule.group_best == 2) g = __fadd_rn(g, order_value(b));
+    const unsigned mine = a ? order_key(__fadd_rn(g, 0.f)) : 0u;
+    int better = 0;
+    for (int o = 0; o < rule.groups; ++o) {
+      const unsigned other = __shfl_sync(0xffffffffu, mine, sub * L + o * span);
+      better += other > mine || (other == mine && o < at / span);
+    }
+    if (better >= rule.top_groups) {
+#pragma unroll
+      for (int j = 0; j < V; ++j) key[j] = 0u;
+    }
+  }
+  float sum = 0.f;
+  unsigned top = 0;
+#pragma unroll
+  for (int j = 0; j < V; ++j) top = max(top, key[j]);
+  for (int c = 0; c < k; ++c) {
+    const unsigned best = lanes_max<L>(top);
+    const unsigned who = __ballot_sync(0xffffffffu, top == best) & mates;
+    const int owner = __ffs(who) - 1;
+    // the owner takes its first entry with that key away
+    const unsigned want = lane == owner && best ? best : 0xffffffffu;
+    int place = V;
+    float score = 0.f;
+    top = 0;
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      const bool hit = key[j] == want && place == V;
+      if (hit) {
+        place = j;
+        score = s[j];
+        key[j] = 0u;
+      }
+      top = max(top, key[j]);
+    }
+    score = __shfl_sync(0xffffffffu, score, owner);
+    sum = __fadd_rn(sum, score);
+    if (lane == owner && live) {
+      picked[warp * R + sub][c] = score;
+      experts[row * k + c] = best ? first + place : -1;
+    }
+  }
   __syncwarp();
-  for (int i = lane; i < E; i += 32) {
-    const float v = fmaxf(sc[i], 0.f);
-    const float d = rule.score == ERC_SCORE_SIGMOID ? ds[i] * v * (1.f - v) : v * (ds[i] - gs);
-    dlogits[row * E + i] = from_f32<T>(d);
+  for (int c = at; c < k && live; c += L) {
+    float w = picked[warp * R + sub][c];
+    if (rule.renorm) w = sum > 0.f ? __fdiv_rn(w, sum) : 0.f;
+    weights[row * k + c] = __fmul_rn(w, rule.scale);
   }
+}
+
+// The gradient of the row's weights.  Where nothing is chosen it is -s_i gs for softmax, with
+// gs = sum ds s (0 in exact arithmetic when renormalised), and 0 for sigmoid, whose rows are then not
+// read at all; the lanes that hold a chosen expert's gradient store it over that.  Results here are
+// rounded to the output's type, so the exponential is the hardware's.
+template <class T, int L, int V, bool SIGMOID>
+__global__ void __launch_bounds__(FW * 32)
+    k_route_lanes_backward(int64_t rows, const T* __restrict__ logits, int64_t stride,
+                           const int32_t* __restrict__ experts, const float* __restrict__ dweights,
+                           erc_route_rule rule, bool wide, bool wide_out, T* __restrict__ dlogits) {
+  constexpr int R = 32 / L, N = ScoreVec<T>::N, KL = (ERC_ROUTE_MAX_K + L - 1) / L;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, sub = lane / L, at = lane % L;
+  const int E = rule.experts, k = rule.k;
+  const int64_t row = ((int64_t)blockIdx.x * FW + warp) * R + sub;
+  const bool live = row < rows;
+  const T* x = logits + (live ? row : 0) * stride;
+  const int first = at * V;
+  auto power = [](float t) {  // 2^t, 0 where the forward pass has 0
+    float e;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(t));
+    return t > -41.5f ? e : 0.f;
+  };
+  float v[V], m = 0.f, inv = 0.f;
+  if (!SIGMOID) {
+    load_scores<T, V>(x, first, E, wide, live, v);
+    m = v[0];
+#pragma unroll
+    for (int j = 1; j < V; ++j) m = fmaxf(m, v[j]);
+#pragma unroll
+    for (int o = L / 2; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+    float z = 0.f;
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      v[j] = v[j] == -INFINITY ? 0.f : power(below_max(v[j], m, LOG2E));
+      z += v[j];
+    }
+    z = lanes_sum<L>(z);
+    inv = z > 0.f ? __frcp_rn(z) : 0.f;
+  }
+  // the row's choices, one or more a lane
+  int place[KL];
+  float s[KL], g[KL], D = 0.f;
+#pragma unroll
+  for (int i = 0; i < KL; ++i) {
+    const int c = at + i * L;
+    place[i] = -1;
+    s[i] = g[i] = 0.f;
+    if (c < k && live) {
+      const int e = experts[row * k + c];
+      if (e >= 0 && e < E) {
+        place[i] = e;
+        g[i] = dweights[row * k + c] * rule.scale;
+        const float l = clean_score(to_f32(x[e]));
+        if (l == -INFINITY)
+          s[i] = 0.f;
+        else if (SIGMOID) {
+          const float q = pow2_float(-__fmul_rn(fabsf(l), LOG2E), -126.f);
+          s[i] = __fdiv_rn(l >= 0.f ? 1.f : q, 1.f + q);
+        } else {
+          s[i] = power(below_max(l, m, LOG2E)) * inv;
+        }
+      }
+    }
+    D += s[i];
+  }
+  if (rule.renorm) {
+    D = lanes_sum<L>(D);
+    const float r = D > 0.f ? __frcp_rn(D) : 0.f;
+    float gp = 0.f;
+#pragma unroll
+    for (int i = 0; i < KL; ++i) gp += g[i] * (D > 0.f ? __fdiv_rn(s[i], D) : 0.f);
+    gp = lanes_sum<L>(gp);
+#pragma unroll
+    for (int i = 0; i < KL; ++i) g[i] = place[i] >= 0 ? (g[i] - gp) * r : 0.f;
+  }
+  float gs = 0.f;
+  if (!SIGMOID && !rule.renorm) {
+#pragma unroll
+    for (int i = 0; i < KL; ++i) gs += g[i] * s[i];
+    gs = lanes_sum<L>(gs);
+  }
+  T* out = dlogits + row * E;
+  if (live && first < E) {
+    const float q = SIGMOID ? 0.f : 0.f - gs * inv;
+    if (wide_out) {
+#pragma unroll
+      for (int j = 0; j < V / N; ++j) {
+        union {
+          uint4 u;
+          T t[N];
+        } o;
+#pragma unroll
+        for (int i = 0; i < N; ++i) o.t[i] = from_f32<T>(SIGMOID ? 0.f : v[j * N + i] * q);
+        reinterpret_cast<uint4*>(out + first)[j] = o.u;
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < V; ++j)
+        if (first + j < E) out[first + j] = from_f32<T>(SIGMOID ? 0.f : v[j] * q);
+    }
+  }
+  __syncwarp();
+#pragma unroll
+  for (int i = 0; i < KL; ++i)
+    if (place[i] >= 0)
+      out[place[i]] = from_f32<T>(SIGMOID ? g[i] * s[i] * (1.f - s[i]) : s[i] * (g[i] - gs));
+}
+
+// calls f(L, V) for the fewest lanes that hold E experts, eight a lane up to 256
+template <class F>
+erc_status with_lanes(int E, F&& f) {
+  using I8 = std::integral_constant<int, 8>;
+  using I16 = std::integral_constant<int, 16>;
+  using I32 = std::integral_constant<int, 32>;
+  if (E <= 64) return f(I8(), I8());
+  if (E <= 128) return f(I16(), I8());
+  if (E <= 256) return f(I32(), I8());
+  if (E <= 512) return f(I32(), I16());
+  return f(I32(), I32());
+}
+template <class T>
+bool aligned16(const T* p, int64_t stride, int64_t rows) {
+  return reinterpret_cast<uintptr_t>(p) % 16 == 0 && (rows <= 1 || stride * sizeof(T) % 16 == 0);
 }
 
 erc_status check_rule(const erc_route_rule* r, int32_t type, int64_t rows, int64_t stride) {
@@ -193,12 +465,29 @@ extern "C" erc_status erc_route(int64_t rows, const void* logits, int32_t type, 
   ERC_REQUIRE(reinterpret_cast<uintptr_t>(logits) % type_bytes(type) == 0, "misaligned logits");
   return with_type(type, [&](auto t) {
     using T = decltype(t);
-    const size_t sh = QW * (2 * rule->experts + rule->groups) * sizeof(float);
-    k_route<T><<<(unsigned)((rows + QW - 1) / QW), QW * 32, sh, as_stream(stream)>>>(
-        rows, static_cast<const T*>(logits), stride, bias, *rule, experts, weights);
-    count_launches(1);
-    ERC_CUDA(cudaGetLastError());
-    return ERC_OK;
+    const T* x = static_cast<const T*>(logits);
+    cudaStream_t s = as_stream(stream);
+    const bool grouped = rule->groups > 1 && rule->top_groups < rule->groups;
+    return with_lanes(rule->experts, [&](auto l, auto v) {
+      constexpr int L = decltype(l)::value, V = decltype(v)::value;
+      const int size = rule->experts / rule->groups, span = size / V;
+      if (grouped && (size % V || (span & (span - 1)))) {
+        // groups that no power of two of lanes holds: the row in shared memory
+        const size_t sh = QW * (2 * rule->experts + rule->groups) * sizeof(float);
+        k_route<T><<<(unsigned)((rows + QW - 1) / QW), QW * 32, sh, s>>>(rows, x, stride, bias, *rule,
+                                                                         experts, weights);
+      } else {
+        const bool wide = aligned16(x, stride, rows) && rule->experts % V == 0;
+        const int64_t per = FW * (32 / L);
+        auto kernel = rule->score == ERC_SCORE_SIGMOID ? k_route_lanes<T, L, V, true>
+                                                       : k_route_lanes<T, L, V, false>;
+        kernel<<<(unsigned)((rows + per - 1) / per), FW * 32, 0, s>>>(rows, x, stride, bias, *rule,
+                                                                      wide, experts, weights);
+      }
+      count_launches(1);
+      ERC_CUDA(cudaGetLastError());
+      return ERC_OK;
+    });
   });
 }
 
@@ -215,12 +504,21 @@ extern "C" erc_status erc_route_backward(int64_t rows, const void* logits, int32
               "misaligned logits or dlogits");
   return with_type(type, [&](auto t) {
     using T = decltype(t);
-    const size_t sh = QW * 2 * rule->experts * sizeof(float);
-    k_route_backward<T><<<(unsigned)((rows + QW - 1) / QW), QW * 32, sh, as_stream(stream)>>>(
-        rows, static_cast<const T*>(logits), stride, experts, dweights, *rule,
-        static_cast<T*>(dlogits));
-    count_launches(1);
-    ERC_CUDA(cudaGetLastError());
-    return ERC_OK;
+    const T* x = static_cast<const T*>(logits);
+    T* dx = static_cast<T*>(dlogits);
+    return with_lanes(rule->experts, [&](auto l, auto v) {
+      constexpr int L = decltype(l)::value, V = decltype(v)::value;
+      const bool even = rule->experts % V == 0;
+      const bool wide = even && aligned16(x, stride, rows);
+      const bool wide_out = even && aligned16(dx, rule->experts, rows);
+      const int64_t per = FW * (32 / L);
+      auto kernel = rule->score == ERC_SCORE_SIGMOID ? k_route_lanes_backward<T, L, V, true>
+                                                     : k_route_lanes_backward<T, L, V, false>;
+      kernel<<<(unsigned)((rows + per - 1) / per), FW * 32, 0, as_stream(stream)>>>(
+          rows, x, stride, experts, dweights, *rule, wide, wide_out, dx);
+      count_launches(1);
+      ERC_CUDA(cudaGetLastError());
+      return ERC_OK;
+    });
   });
 }

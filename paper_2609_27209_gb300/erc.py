@@ -496,29 +496,32 @@ ERC_SCORE_SOFTMAX, ERC_SCORE_SIGMOID = 0, 1
 _TYPES = {torch.float32: ERC_F32, torch.bfloat16: ERC_BF16, torch.float16: ERC_F16}
 
 
-def _require(ok, message):
-    if not ok:
-        raise ErcError(ERC_ERR_INVALID_ARG, message)
+def _refuse(message):
+    raise ErcError(ERC_ERR_INVALID_ARG, message)
 
 
 def _need(t, name, dtype, shape, device):
     """`t` is a dense tensor of this type and shape on `device`."""
-    _require(isinstance(t, torch.Tensor) and t.dtype == dtype and tuple(t.shape) == tuple(shape)
-             and t.device == device and t.is_contiguous(),
-             f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)} on {device}")
+    if not (isinstance(t, torch.Tensor) and t.dtype is dtype and t.shape == shape
+            and t.device == device and t.is_contiguous()):
+        _refuse(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)} on {device}")
 
 
 def _rows_of(t, name):
     """(rows, n, type, row stride) of a matrix of scores with unit element stride."""
-    _require(isinstance(t, torch.Tensor) and t.is_cuda and t.dim() == 2 and t.dtype in _TYPES,
-             f"{name} must be a 2-d float32, bfloat16 or float16 CUDA tensor")
+    kind = _TYPES.get(t.dtype) if isinstance(t, torch.Tensor) and t.is_cuda else None
+    if kind is None or t.dim() != 2:
+        _refuse(f"{name} must be a 2-d float32, bfloat16 or float16 CUDA tensor")
     rows, n = t.shape
-    _require(n <= 1 or t.stride(1) == 1, f"the rows of {name} must have unit element stride")
-    return rows, n, _TYPES[t.dtype], t.stride(0) if rows > 1 else n
+    stride, unit = t.stride()
+    if n > 1 and unit != 1:
+        _refuse(f"the rows of {name} must have unit element stride")
+    return rows, n, kind, stride if rows > 1 else n
 
 
 def _stream_of(t):
-    return ctypes.c_void_p(torch.cuda.current_stream(t.device).cuda_stream)
+    # the raw handle: the Stream object of torch.cuda.current_stream costs 2 us a call
+    return torch._C._cuda_getCurrentRawStream(t.device.index)
 
 
 def erc_sample_rows(logits, words, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
@@ -542,11 +545,12 @@ def erc_sample_rows(logits, words, temperature=1.0, top_k=0, top_p=1.0, min_p=0.
             rule.top_k = min(int(v), 2**31 - 1)
         else:
             setattr(rule, name, float(v))
-    out = torch.empty(3, rows, dtype=torch.int32, device=dev)
-    ids, logp, kept = out[0], out[1].view(torch.float32), out[2]
-    _check(lib().erc_sample_rows(rows, n, _ptr(logits), kind, stride, _ptr(words),
-                                 ctypes.byref(rule), _ptr(ids), _ptr(logp), _ptr(kept),
-                                 _stream_of(logits)))
+    ids = torch.empty(rows, dtype=torch.int32, device=dev)
+    logp = torch.empty(rows, dtype=torch.float32, device=dev)
+    kept = torch.empty(rows, dtype=torch.int32, device=dev)
+    _check(lib().erc_sample_rows(rows, n, logits.data_ptr(), kind, stride, words.data_ptr(),
+                                 ctypes.byref(rule), ids.data_ptr(), logp.data_ptr(),
+                                 kept.data_ptr(), _stream_of(logits)))
     return ids, logp, kept
 
 
@@ -561,8 +565,8 @@ def erc_route(logits, k, score=ERC_SCORE_SOFTMAX, bias=None, groups=1, top_group
     rule = ErcRouteRuleC(E, k, score, groups, top_groups, group_best, int(bool(renorm)), scale)
     experts = torch.empty(rows, max(k, 0), dtype=torch.int32, device=dev)
     weights = torch.empty(rows, max(k, 0), dtype=torch.float32, device=dev)
-    _check(lib().erc_route(rows, _ptr(logits), kind, stride, _ptr(bias), ctypes.byref(rule),
-                           _ptr(experts), _ptr(weights), _stream_of(logits)))
+    _check(lib().erc_route(rows, logits.data_ptr(), kind, stride, _ptr(bias), ctypes.byref(rule),
+                           experts.data_ptr(), _ptr(weights), _stream_of(logits)))
     return experts, weights
 
 
@@ -570,14 +574,15 @@ def erc_route_backward(logits, experts, dweights, score=ERC_SCORE_SOFTMAX, renor
     """The gradient of erc_route's weights with respect to logits, for the experts it chose."""
     rows, E, kind, stride = _rows_of(logits, "logits")
     dev = logits.device
-    _require(isinstance(experts, torch.Tensor) and experts.dim() == 2, "experts must be [rows, k]")
+    if not (isinstance(experts, torch.Tensor) and experts.dim() == 2):
+        _refuse("experts must be [rows, k]")
     k = experts.shape[1]
     _need(experts, "experts", torch.int32, (rows, k), dev)
     _need(dweights, "dweights", torch.float32, (rows, k), dev)
     rule = ErcRouteRuleC(E, k, score, 1, 1, 1, int(bool(renorm)), scale)
     dlogits = torch.empty(rows, E, dtype=logits.dtype, device=dev)
-    _check(lib().erc_route_backward(rows, _ptr(logits), kind, stride, _ptr(experts),
-                                    _ptr(dweights), ctypes.byref(rule), _ptr(dlogits),
+    _check(lib().erc_route_backward(rows, logits.data_ptr(), kind, stride, experts.data_ptr(),
+                                    dweights.data_ptr(), ctypes.byref(rule), dlogits.data_ptr(),
                                     _stream_of(logits)))
     return dlogits
 
@@ -585,41 +590,43 @@ def erc_route_backward(logits, experts, dweights, score=ERC_SCORE_SOFTMAX, renor
 def erc_expert_plan(experts, n_experts, ws=None):
     """The pairs of experts int32 [rows, k] in expert order (see include/erc.h): (offsets int64
     [n_experts + 1], order int32 [rows * k], slot int32 [rows, k])."""
-    _require(isinstance(experts, torch.Tensor) and experts.is_cuda and experts.dim() == 2,
-             "experts must be a CUDA tensor [rows, k]")
+    if not (isinstance(experts, torch.Tensor) and experts.is_cuda and experts.dim() == 2):
+        _refuse("experts must be a CUDA tensor [rows, k]")
     rows, k = experts.shape
     dev = experts.device
     _need(experts, "experts", torch.int32, (rows, k), dev)
-    _require(0 < n_experts < 2**31, "n_experts out of range")
+    if not 0 < n_experts < 2**31:
+        _refuse("n_experts out of range")
     offsets = torch.empty(n_experts + 1, dtype=torch.int64, device=dev)
     order = torch.empty(rows * k, dtype=torch.int32, device=dev)
     slot = torch.empty(rows, k, dtype=torch.int32, device=dev)
     if ws is None:
         ws = _workspace(lib().erc_expert_plan_workspace_size(rows, k, n_experts), dev)
-    _check(lib().erc_expert_plan(rows, k, n_experts, _ptr(experts), _ptr(offsets), _ptr(order),
-                                 _ptr(slot), _ptr(ws), ws.numel(), _stream_of(experts)))
+    _check(lib().erc_expert_plan(rows, k, n_experts, experts.data_ptr(), offsets.data_ptr(), order.data_ptr(),
+                                 slot.data_ptr(), ws.data_ptr(), ws.numel(), _stream_of(experts)))
     return offsets, order, slot
 
 
 def _matrix(t, name):
-    _require(isinstance(t, torch.Tensor) and t.is_cuda and t.dim() == 2 and t.dtype in _TYPES
-             and t.is_contiguous(),
-             f"{name} must be a contiguous 2-d float32, bfloat16 or float16 CUDA tensor")
-    return t.shape[0], t.shape[1], _TYPES[t.dtype]
+    kind = _TYPES.get(t.dtype) if isinstance(t, torch.Tensor) and t.is_cuda else None
+    if kind is None or t.dim() != 2 or not t.is_contiguous():
+        _refuse(f"{name} must be a contiguous 2-d float32, bfloat16 or float16 CUDA tensor")
+    return t.shape[0], t.shape[1], kind
 
 
 def _slots(slot, rows, dev):
-    _require(isinstance(slot, torch.Tensor) and slot.dim() == 2, "slot must be [rows, k]")
+    if not (isinstance(slot, torch.Tensor) and slot.dim() == 2):
+        _refuse("slot must be [rows, k]")
     rows = slot.shape[0] if rows is None else rows
     _need(slot, "slot", torch.int32, (rows, slot.shape[1]), dev)
     return rows, slot.shape[1]
 
 
 def _placed(offsets, dev):
-    _require(isinstance(offsets, torch.Tensor) and offsets.dim() == 1 and offsets.numel() > 0,
-             "offsets must be [n_experts + 1]")
+    if not (isinstance(offsets, torch.Tensor) and offsets.dim() == 1 and offsets.numel() > 0):
+        _refuse("offsets must be [n_experts + 1]")
     _need(offsets, "offsets", torch.int64, offsets.shape, dev)
-    return ctypes.c_void_p(offsets.data_ptr() + 8 * (offsets.numel() - 1))
+    return offsets.data_ptr() + 8 * (offsets.numel() - 1)
 
 
 def erc_expert_gather(x, slot, offsets):
@@ -628,8 +635,8 @@ def erc_expert_gather(x, slot, offsets):
     rows, width, kind = _matrix(x, "x")
     _, k = _slots(slot, rows, x.device)
     xs = torch.empty(rows * k, width, dtype=x.dtype, device=x.device)
-    _check(lib().erc_expert_gather(rows, k, width, _ptr(x), kind, _ptr(slot),
-                                   _placed(offsets, x.device), _ptr(xs), _stream_of(x)))
+    _check(lib().erc_expert_gather(rows, k, width, x.data_ptr(), kind, slot.data_ptr(),
+                                   _placed(offsets, x.device), xs.data_ptr(), _stream_of(x)))
     return xs
 
 
@@ -637,12 +644,13 @@ def erc_expert_combine(y, slot, weights=None):
     """The weighted sum over each row's pairs of y [rows * k, width]: out [rows, width]."""
     slots, width, kind = _matrix(y, "y")
     rows, k = _slots(slot, None, y.device)
-    _require(slots == rows * k, "y must have rows * k rows")
+    if slots != rows * k:
+        _refuse("y must have rows * k rows")
     if weights is not None:
         _need(weights, "weights", torch.float32, (rows, k), y.device)
     out = torch.empty(rows, width, dtype=y.dtype, device=y.device)
-    _check(lib().erc_expert_combine(rows, k, width, _ptr(y), kind, _ptr(slot), _ptr(weights),
-                                    _ptr(out), _stream_of(y)))
+    _check(lib().erc_expert_combine(rows, k, width, y.data_ptr(), kind, slot.data_ptr(), _ptr(weights),
+                                    out.data_ptr(), _stream_of(y)))
     return out
 
 
@@ -655,7 +663,7 @@ def erc_expert_combine_backward(dout, y, slot, offsets, weights):
     _need(weights, "weights", torch.float32, (rows, k), dev)
     dy = torch.empty_like(y)
     dweights = torch.empty(rows, k, dtype=torch.float32, device=dev)
-    _check(lib().erc_expert_combine_backward(rows, k, width, _ptr(dout), _ptr(y), kind, _ptr(slot),
-                                             _placed(offsets, dev), _ptr(weights), _ptr(dy),
-                                             _ptr(dweights), _stream_of(dout)))
+    _check(lib().erc_expert_combine_backward(rows, k, width, dout.data_ptr(), y.data_ptr(), kind, slot.data_ptr(),
+                                             _placed(offsets, dev), _ptr(weights), dy.data_ptr(),
+                                             dweights.data_ptr(), _stream_of(dout)))
     return dy, dweights
