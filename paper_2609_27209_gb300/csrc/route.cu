@@ -174,21 +174,35 @@ __device__ __forceinline__ void load_scores(const T* x, int first, int E, bool w
   }
 }
 
+struct RowScale {  // of a softmax row: its maximum and 1 / Z
+  float max, inv;
+};
+
+// one logit's score, -1 where masked
+template <bool SIGMOID>
+__device__ __forceinline__ float one_score(float l, const RowScale& r) {
+  if (l == -INFINITY) return -1.f;
+  if (!SIGMOID) return __fmul_rn(pow2_float(below_max(l, r.max, LOG2E), -41.f), r.inv);
+  const float e = pow2_float(-__fmul_rn(fabsf(l), LOG2E), -126.f);
+  return __fdiv_rn(l >= 0.f ? 1.f : e, __fadd_rn(1.f, e));
+}
+
 // the scores s_j of a lane's logits, -1 where masked
 template <int L, int V, bool SIGMOID>
-__device__ __forceinline__ void lane_scores(const float* l, float* s) {
+__device__ __forceinline__ RowScale lane_scores(const float* l, float* s) {
+  RowScale r = {};
   if (SIGMOID) {
 #pragma unroll
     for (int j = 0; j < V; j += 2) {
-      float t[2], p[2], r[2];
+      float t[2], p[2], k[2];
 #pragma unroll
       for (int i = 0; i < 2; ++i) t[i] = fmaxf(-__fmul_rn(fabsf(l[j + i]), LOG2E), -200.f);
-      pow2_pair(t[0], t[1], p, r);
+      pow2_pair(t[0], t[1], p, k);
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         const float x = l[j + i];
         const float e = t[i] >= -126.5f
-                            ? __uint_as_float(__float_as_uint(p[i]) + (__float_as_uint(r[i]) << 23))
+                            ? __uint_as_float(__float_as_uint(p[i]) + (__float_as_uint(k[i]) << 23))
                             : 0.f;
         s[j + i] = x == -INFINITY ? -1.f : __fdiv_rn(x >= 0.f ? 1.f : e, __fadd_rn(1.f, e));
       }
@@ -218,9 +232,112 @@ __device__ __forceinline__ void lane_scores(const float* l, float* s) {
     const float inv = __frcp_rn(__fmul_rn(__ull2float_rn(z ? z : 1ull), 9.094947017729282e-13f));
 #pragma unroll
     for (int j = 0; j < V; ++j) s[j] = l[j] == -INFINITY ? -1.f : __fmul_rn(s[j], inv);
+    r.max = m;
+    r.inv = inv;
+  }
+  return r;
+}
+
+// the choice of an expert from its score (negative: masked): -inf where it is not to be chosen.  A score
+// is never -0, so neither is its sum with a bias.
+__device__ __forceinline__ float choice(float s, float bias) {
+  return s < 0.f ? -INFINITY : fmaxf(__fadd_rn(s, bias), -INFINITY);
+}
+template <int V>
+__device__ __forceinline__ void lane_bias(const float* bias, int first, int E, float* b) {
+#pragma unroll
+  for (int j = 0; j < V; ++j) b[j] = bias && first + j < E ? __ldg(bias + first + j) : 0.f;
+}
+
+template <int L>
+__device__ __forceinline__ float lanes_max(float v) {
+  if constexpr (L == 32) {
+    float r;
+    asm("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
+    return r;
+  } else {
+#pragma unroll
+    for (int o = L / 2; o; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
+    return v;
   }
 }
 
+// the score of a lane's group (a power of two of lanes): its best choice, or the sum of its best two
+template <int V>
+__device__ __forceinline__ float group_score(const erc_route_rule& rule, int span, const float* c) {
+  float a = -INFINITY, b = -INFINITY;
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
+    b = fmaxf(b, fminf(a, c[j]));
+    a = fmaxf(a, c[j]);
+  }
+  for (int o = 1; o < span; o <<= 1) {
+    const float a2 = __shfl_xor_sync(0xffffffffu, a, o), b2 = __shfl_xor_sync(0xffffffffu, b, o);
+    b = fmaxf(fmaxf(b, b2), fminf(a, a2));
+    a = fmaxf(a, a2);
+  }
+  return b > -INFINITY && rule.group_best == 2 ? __fadd_rn(a, b) : a;
+}
+
+// The choices of the groups passed over become -inf; ties go to the lowest group.
+template <int L, int V>
+__device__ __forceinline__ void keep_groups(const erc_route_rule& rule, int lane, float* c) {
+  const int at = lane % L, span = rule.experts / rule.groups / V;
+  const float mine = group_score<V>(rule, span, c);
+  int better = 0;
+  for (int o = 0; o < rule.groups; ++o) {
+    const float other = __shfl_sync(0xffffffffu, mine, lane - at + o * span);
+    better += other > mine || (other == mine && o < at / span);
+  }
+  if (better >= rule.top_groups) {
+#pragma unroll
+    for (int j = 0; j < V; ++j) c[j] = -INFINITY;
+  }
+}
+
+// k rounds over a row of L lanes: the best choice, by its first owner, is taken away
+template <int L, int V>
+__device__ __forceinline__ void pick_in_rounds(const erc_route_rule& rule, int lane, bool live,
+                                               int64_t row, const float* s, float* c, float* picked,
+                                               int32_t* experts, float* weights) {
+  const int at = lane % L, k = rule.k;
+  const unsigned mates = (L == 32 ? 0xffffffffu : ((1u << (L & 31)) - 1)) << (lane - at);
+  float sum = 0.f, top = -INFINITY;
+#pragma unroll
+  for (int j = 0; j < V; ++j) top = fmaxf(top, c[j]);
+  for (int i = 0; i < k; ++i) {
+    const float best = lanes_max<L>(top);
+    const int owner = __ffs(__ballot_sync(0xffffffffu, top == best) & mates) - 1;
+    const bool take = lane == owner && best > -INFINITY;
+    int place = V;
+    float score = 0.f;
+    top = -INFINITY;
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      if (take && c[j] == best && place == V) {
+        place = j;
+        score = s[j];
+        c[j] = -INFINITY;
+      }
+      top = fmaxf(top, c[j]);
+    }
+    score = __shfl_sync(0xffffffffu, score, owner);
+    sum = __fadd_rn(sum, score);
+    if (lane == owner && live) {
+      picked[i] = score;
+      experts[row * k + i] = take ? at * V + place : -1;
+    }
+  }
+  __syncwarp();
+  for (int i = at; i < k && live; i += L) {
+    float w = picked[i];
+    if (rule.renorm) w = sum > 0.f ? __fdiv_rn(w, sum) : 0.f;
+    weights[row * k + i] = __fmul_rn(w, rule.scale);
+  }
+  __syncwarp();
+}
+
+// rows of at most 128 experts: L = 8 or 16 lanes a row
 template <class T, int L, int V, bool SIGMOID>
 __global__ void __launch_bounds__(FW * 32)
     k_route_lanes(int64_t rows, const T* __restrict__ logits, int64_t stride,
@@ -228,84 +345,152 @@ __global__ void __launch_bounds__(FW * 32)
                   int32_t* __restrict__ experts, float* __restrict__ weights) {
   constexpr int R = 32 / L;  // rows of a warp
   __shared__ float picked[FW * R][ERC_ROUTE_MAX_K];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, sub = lane / L, at = lane % L;
-  const int E = rule.experts, k = rule.k;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, sub = lane / L;
+  const int E = rule.experts, first = lane % L * V;
   const int64_t row = ((int64_t)blockIdx.x * FW + warp) * R + sub;
   const bool live = row < rows;
-  const unsigned mates = (L == 32 ? 0xffffffffu : ((1u << L) - 1)) << (sub * L);
-  const int first = at * V;
-  float l[V], s[V];
+  float l[V], s[V], c[V];
   load_scores<T, V>(logits + (live ? row : 0) * stride, first, E, wide, live, l);
   lane_scores<L, V, SIGMOID>(l, s);
-  unsigned key[V];  // 0: not to be chosen
+  lane_bias<V>(bias, first, E, c);
 #pragma unroll
-  for (int j = 0; j < V; ++j) {
-    float c = s[j];
-    if (bias) c = __fadd_rn(c, first + j < E ? __ldg(bias + first + j) : 0.f);
-    key[j] = s[j] < 0.f || c != c || c == -INFINITY ? 0u : order_key(__fadd_rn(c, 0.f));
+  for (int j = 0; j < V; ++j) c[j] = choice(s[j], c[j]);
+  if (rule.groups > 1 && rule.top_groups < rule.groups) keep_groups<L, V>(rule, lane, c);
+  pick_in_rounds<L, V>(rule, lane, live, row, s, c, picked[warp * R + sub], experts, weights);
+}
+
+// The places of the choices that can be among the k best into `list`, in ascending order: those no
+// lower than the k-th distinct best of the lanes' best, less `margin` times (1 + its value).  Returns
+// their number; more than 32 are not listed.
+template <int V>
+__device__ __forceinline__ int candidates(const float* c, int k, int first, float margin,
+                                          uint16_t* list) {
+  float top = -INFINITY, theta = -INFINITY;
+#pragma unroll
+  for (int j = 0; j < V; ++j) top = fmaxf(top, c[j]);
+  for (int i = 0; i < k; ++i) {
+    theta = lanes_max<32>(top);
+    if (theta == -INFINITY) break;
+    if (top == theta) top = -INFINITY;
   }
-  if (rule.groups > 1 && rule.top_groups < rule.groups) {
-    // a group is `span` lanes; its best two, then its rank among the groups
-    const int span = E / rule.groups / V;
-    unsigned a = 0, b = 0;
+  const float least = margin > 0.f && theta > -INFINITY ? theta - margin * (1.f + fabsf(theta)) : theta;
+  if (least != least) return 33;  // a choice of +inf has no margin
+  unsigned mask = 0;
 #pragma unroll
-    for (int j = 0; j < V; ++j) {
-      b = max(b, min(a, key[j]));
-      a = max(a, key[j]);
-    }
-    for (int o = 1; o < span; o <<= 1) {
-      const unsigned a2 = __shfl_xor_sync(0xffffffffu, a, o), b2 = __shfl_xor_sync(0xffffffffu, b, o);
-      b = max(max(b, b2), min(a, a2));
-      a = max(a, a2);
-    }
-    float g = a ? order_value(a) : -INFINITY;
-    if (b && rule.group_best == 2) g = __fadd_rn(g, order_value(b));
-    const unsigned mine = a ? order_key(__fadd_rn(g, 0.f)) : 0u;
-    int better = 0;
-    for (int o = 0; o < rule.groups; ++o) {
-      const unsigned other = __shfl_sync(0xffffffffu, mine, sub * L + o * span);
-      better += other > mine || (other == mine && o < at / span);
-    }
-    if (better >= rule.top_groups) {
+  for (int j = 0; j < V; ++j)
+    if (c[j] >= least && c[j] > -INFINITY) mask |= 1u << j;
+  int to = __popc(mask);
 #pragma unroll
-      for (int j = 0; j < V; ++j) key[j] = 0u;
-    }
+  for (int o = 1; o < 32; o <<= 1) {
+    const int y = __shfl_up_sync(0xffffffffu, to, o);
+    if ((int)(threadIdx.x & 31) >= o) to += y;
   }
-  float sum = 0.f;
-  unsigned top = 0;
-#pragma unroll
-  for (int j = 0; j < V; ++j) top = max(top, key[j]);
-  for (int c = 0; c < k; ++c) {
-    const unsigned best = lanes_max<L>(top);
-    const unsigned who = __ballot_sync(0xffffffffu, top == best) & mates;
-    const int owner = __ffs(who) - 1;
-    // the owner takes its first entry with that key away
-    const unsigned want = lane == owner && best ? best : 0xffffffffu;
-    int place = V;
-    float score = 0.f;
-    top = 0;
-#pragma unroll
-    for (int j = 0; j < V; ++j) {
-      const bool hit = key[j] == want && place == V;
-      if (hit) {
-        place = j;
-        score = s[j];
-        key[j] = 0u;
-      }
-      top = max(top, key[j]);
-    }
-    score = __shfl_sync(0xffffffffu, score, owner);
-    sum = __fadd_rn(sum, score);
-    if (lane == owner && live) {
-      picked[warp * R + sub][c] = score;
-      experts[row * k + c] = best ? first + place : -1;
-    }
-  }
+  const int n = __shfl_sync(0xffffffffu, to, 31);
+  if (n > 32) return n;
+  for (to -= __popc(mask); mask; mask &= mask - 1) list[to++] = (uint16_t)(first + __ffs(mask) - 1);
   __syncwarp();
-  for (int c = at; c < k && live; c += L) {
-    float w = picked[warp * R + sub][c];
-    if (rule.renorm) w = sum > 0.f ? __fdiv_rn(w, sum) : 0.f;
-    weights[row * k + c] = __fmul_rn(w, rule.scale);
+  return n;
+}
+
+// Rows of more than 128 experts: a warp a row, the k best ranked among at most 32 candidates, one a
+// lane, by their exact choices.  For sigmoid scores the candidates come from the hardware's
+// exponential and reciprocal: with |t| as computed here their scores are within 1.1e-6 of the exact
+// ones (2^-22 for ex2, 1.9e-7 for the polynomial, an ulp for rcp, three roundings), so 4e-6 (1 + |c|)
+// covers twice that and the rounding of the sum with the bias.  Rows whose groups are not told apart
+// by twice as much, or with more candidates, take exact choices and, if need be, k rounds.
+//
+// A warp takes rows in turn, its biases in registers and the next row on its way.
+//
+// E = 256, k = 8, four of eight groups, sigmoid with bias, 32,768 rows of bf16: k rounds over exact
+// scores took 55 us (1505 instructions a row, issue-bound).
+template <class T, int V, bool SIGMOID>
+__global__ void __launch_bounds__(FW * 32, V == 8 ? 4 : V == 16 ? 2 : 1)
+    k_route_warp(int64_t rows, const T* __restrict__ logits, int64_t stride,
+                 const float* __restrict__ bias, erc_route_rule rule, bool wide,
+                 int32_t* __restrict__ experts, float* __restrict__ weights) {
+  __shared__ float picked[FW][ERC_ROUTE_MAX_K];
+  __shared__ uint16_t lists[FW][32];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int E = rule.experts, k = rule.k, first = lane * V;
+  const bool grouped = rule.groups > 1 && rule.top_groups < rule.groups;
+  const int span = grouped ? E / rule.groups / V : 32;
+  const int64_t step = (int64_t)gridDim.x * FW;
+  float b[V], next[V];
+  lane_bias<V>(bias, first, E, b);
+  int64_t row = (int64_t)blockIdx.x * FW + warp;
+  load_scores<T, V>(logits + row * stride, first, E, wide, row < rows, next);
+  for (; row < rows; row += step) {
+    const T* x = logits + row * stride;
+    float l[V], s[V], c[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) l[j] = next[j];
+    if (row + step < rows) load_scores<T, V>(x + step * stride, first, E, wide, true, next);
+    int n = 33;
+    RowScale scale = {};
+    if (SIGMOID) {
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        float e, r;
+        asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(-__fmul_rn(fabsf(l[j]), LOG2E)));
+        asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + e));
+        c[j] = fmaxf((l[j] >= 0.f ? r : e * r) + b[j], -INFINITY);
+        if (l[j] == -INFINITY) c[j] = -INFINITY;
+      }
+      bool clear = true;
+      if (grouped) {
+        // the top_groups distinct best groups' scores, and the best of the rest
+        const float mine = group_score<V>(rule, span, c);
+        float rest = mine, worst = -INFINITY;
+        for (int i = 0; i < rule.top_groups; ++i) {
+          worst = lanes_max<32>(rest);
+          if (rest == worst) rest = -INFINITY;
+        }
+        rest = lanes_max<32>(rest);
+        const int in = __popc(__ballot_sync(0xffffffffu, mine >= worst && first < E));
+        clear = in == rule.top_groups * span && worst - rest > 8e-6f * (1.f + fabsf(worst));
+        if (mine < worst) {
+#pragma unroll
+          for (int j = 0; j < V; ++j) c[j] = -INFINITY;
+        }
+      }
+      if (clear) n = candidates<V>(c, k, first, 4e-6f, lists[warp]);
+    }
+    if (n > 32) {
+      scale = lane_scores<32, V, SIGMOID>(l, s);
+#pragma unroll
+      for (int j = 0; j < V; ++j) c[j] = choice(s[j], b[j]);
+      if (grouped) keep_groups<32, V>(rule, lane, c);
+      n = candidates<V>(c, k, first, 0.f, lists[warp]);
+      if (n > 32) {
+        pick_in_rounds<32, V>(rule, lane, true, row, s, c, picked[warp], experts, weights);
+        continue;
+      }
+    }
+    // one candidate a lane, in ascending order of experts
+    int e = -1;
+    float score = 0.f, mine = -INFINITY;
+    if (lane < n) {
+      e = lists[warp][lane];
+      score = one_score<SIGMOID>(fmaxf(to_f32(x[e]), -INFINITY), scale);
+      mine = choice(score, bias ? __ldg(bias + e) : 0.f);
+    }
+    int rank = 0;
+    for (int i = 0; i < n; ++i) {
+      const float other = __shfl_sync(0xffffffffu, mine, i);
+      rank += i < lane ? other >= mine : other > mine;
+    }
+    const bool in = lane < n && rank < k;
+    const float sum = rule.renorm ? lanes_sum<32>(in ? score : 0.f) : 0.f;
+    if (in) {
+      if (rule.renorm) score = sum > 0.f ? __fdiv_rn(score, sum) : 0.f;
+      experts[row * k + rank] = e;
+      weights[row * k + rank] = __fmul_rn(score, rule.scale);
+    }
+    if (lane >= n && lane < k) {  // fewer than k can be chosen
+      experts[row * k + lane] = -1;
+      weights[row * k + lane] = 0.f;
+    }
+    __syncwarp();
   }
 }
 
@@ -476,6 +661,13 @@ extern "C" erc_status erc_route(int64_t rows, const void* logits, int32_t type, 
         const size_t sh = QW * (2 * rule->experts + rule->groups) * sizeof(float);
         k_route<T><<<(unsigned)((rows + QW - 1) / QW), QW * 32, sh, s>>>(rows, x, stride, bias, *rule,
                                                                          experts, weights);
+      } else if constexpr (L == 32) {
+        const bool wide = aligned16(x, stride, rows) && rule->experts % V == 0;
+        const int64_t most = 4LL * sm_count(), need = (rows + FW - 1) / FW;
+        auto kernel = rule->score == ERC_SCORE_SIGMOID ? k_route_warp<T, V, true>
+                                                       : k_route_warp<T, V, false>;
+        kernel<<<(unsigned)(need < most ? need : most), FW * 32, 0, s>>>(rows, x, stride, bias, *rule,
+                                                                         wide, experts, weights);
       } else {
         const bool wide = aligned16(x, stride, rows) && rule->experts % V == 0;
         const int64_t per = FW * (32 / L);
