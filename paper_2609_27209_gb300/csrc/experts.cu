@@ -1,149 +1,319 @@
 // experts.cu -- the chosen (row, choice) pairs in expert order, rows copied into that order, and
 // the weighted sum back, with its gradient.
+#include <initializer_list>
+
 #include "choice.cuh"
 
 namespace erc {
 namespace {
 
-constexpr int PT = 256;     // threads of a plan tile
-constexpr int PTILE = 1024;  // pairs of a plan tile
+constexpr int PT = 256;        // threads of a plan tile
+constexpr int PW = PT / 32;    // its warps
+constexpr int PTILE = 4096;    // pairs of a plan tile: a warp takes PTILE / PW consecutive ones
 constexpr int MAX_E = ERC_ROUTE_MAX_EXPERTS;
 
 struct Plan {
-  int32_t* tile;  // [tiles][E] pairs of each expert, then their exclusive sums over tiles
+  int32_t* tile;   // [E][tiles] pairs of each expert, then their exclusive sums over the tiles
+  int32_t* total;  // [E]
 };
+int64_t plan_tiles(int64_t pairs) { return (pairs + PTILE - 1) / PTILE; }
 void plan_experts(Arena& a, Plan& p, int64_t pairs, int E) {
-  p.tile = a.take<int32_t>((size_t)((pairs + PTILE - 1) / PTILE) * E);
+  p.tile = a.take<int32_t>((size_t)plan_tiles(pairs) * E);
+  p.total = a.take<int32_t>(E);
 }
 
 __global__ void __launch_bounds__(PT) k_plan_count(const int32_t* __restrict__ experts,
-                                                   int64_t pairs, int E,
+                                                   int64_t pairs, int E, int tiles,
                                                    int32_t* __restrict__ tile) {
   __shared__ int32_t c[MAX_E];
   for (int e = threadIdx.x; e < E; e += PT) c[e] = 0;
   __syncthreads();
   const int64_t base = (int64_t)blockIdx.x * PTILE;
-  for (int i = threadIdx.x; i < PTILE && base + i < pairs; i += PT) {
-    const int e = experts[base + i];
+#pragma unroll 4
+  for (int i = threadIdx.x; i < PTILE; i += PT) {
+    const int e = base + i < pairs ? experts[base + i] : -1;
     if (e >= 0 && e < E) atomicAdd(&c[e], 1);
   }
   __syncthreads();
-  for (int e = threadIdx.x; e < E; e += PT) tile[(int64_t)blockIdx.x * E + e] = c[e];
+  for (int e = threadIdx.x; e < E; e += PT) tile[(int64_t)e * tiles + blockIdx.x] = c[e];
 }
 
-__global__ void __launch_bounds__(MAX_E) k_plan_scan(int32_t* __restrict__ tile, int tiles, int E,
-                                                     int64_t* __restrict__ offsets) {
-  __shared__ int32_t total[MAX_E];
-  const int e = threadIdx.x;
-  int32_t sum = 0;
-  if (e < E)
-    for (int t = 0; t < tiles; ++t) {
-      const int32_t v = tile[(int64_t)t * E + e];
-      tile[(int64_t)t * E + e] = sum;
-      sum += v;
-    }
-  total[e] = e < E ? sum : 0;
-  __syncthreads();
-  if (e == 0) {
-    int64_t s = 0;
-    for (int i = 0; i < E; ++i) {
-      offsets[i] = s;
-      s += total[i];
-    }
-    offsets[E] = s;
-  }
-}
-
-// a pair's slot: its expert's offset, the pairs of that expert in earlier tiles, and those before
-// it in its tile
-__global__ void __launch_bounds__(PT) k_plan_place(const int32_t* __restrict__ experts,
-                                                   int64_t pairs, int E,
-                                                   const int32_t* __restrict__ tile,
-                                                   const int64_t* __restrict__ offsets,
-                                                   int32_t* __restrict__ order,
-                                                   int32_t* __restrict__ slot) {
-  __shared__ int32_t next[MAX_E];
+// a block scans an expert's counts over the tiles
+__global__ void __launch_bounds__(PT) k_plan_scan(int32_t* __restrict__ tile, int tiles,
+                                                  int32_t* __restrict__ total) {
+  __shared__ int32_t part[PW];
+  int32_t* t = tile + (int64_t)blockIdx.x * tiles;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int64_t base = (int64_t)blockIdx.x * PTILE;
-  for (int e = threadIdx.x; e < E; e += PT)
-    next[e] = (int32_t)offsets[e] + tile[(int64_t)blockIdx.x * E + e];
-  const int64_t placed = offsets[E];
-  for (int i = threadIdx.x; i < PTILE && base + i < pairs; i += PT)
-    if (base + i >= placed) order[base + i] = -1;
-  __syncthreads();
-  for (int g = 0; g < PTILE / 32; ++g) {  // 32 pairs at a time, in order
-    if (g % (PT / 32) == warp) {
-      const int64_t i = base + g * 32 + lane;
-      const int e = i < pairs ? experts[i] : -1;
-      const bool some = e >= 0 && e < E;
-      const unsigned same = __match_any_sync(0xffffffffu, some ? e : -1);
-      int32_t at = 0;
-      if (some) at = next[e] + __popc(same & ((1u << lane) - 1));
-      __syncwarp();
-      if (some && lane == 31 - __clz(same)) next[e] = at + 1;
-      if (some) order[at] = (int32_t)i;
-      if (i < pairs) slot[i] = some ? at : -1;
+  int32_t before = 0;
+  for (int base = 0; base < tiles; base += PT) {
+    const int i = base + threadIdx.x;
+    const int32_t v = i < tiles ? t[i] : 0;
+    int32_t x = v;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int32_t y = __shfl_up_sync(0xffffffffu, x, o);
+      if (lane >= o) x += y;
     }
+    if (lane == 31) part[warp] = x;
+    __syncthreads();
+    int32_t mine = before;
+#pragma unroll
+    for (int w = 0; w < PW; ++w) {
+      if (w < warp) mine += part[w];
+      before += part[w];
+    }
+    if (i < tiles) t[i] = mine + x - v;
     __syncthreads();
   }
+  if (threadIdx.x == 0) total[blockIdx.x] = before;
 }
 
-template <class T>
-__global__ void __launch_bounds__(256) k_combine(int64_t rows, int k, int64_t width,
-                                                 const T* __restrict__ y,
-                                                 const int32_t* __restrict__ slot,
-                                                 const float* __restrict__ weights,
-                                                 T* __restrict__ out) {
-  for (int64_t t = blockIdx.x; t < rows; t += gridDim.x)
-    for (int64_t d = threadIdx.x; d < width; d += 256) {
-      float s = 0.f;
-      for (int j = 0; j < k; ++j) {
-        const int32_t p = slot[t * k + j];
-        if (p < 0 || p >= rows * k) continue;
-        const float v = to_f32(y[p * width + d]);
-        s = weights ? fmaf(weights[t * k + j], v, s) : s + v;
-      }
-      out[t * width + d] = from_f32<T>(s);
-    }
-}
-
-// dy[slot] = weight * g[row] (weights NULL: a copy) and dweights = g[row] . y[slot]
-template <class T>
-__global__ void __launch_bounds__(256) k_expand(int64_t rows, int k, int64_t width,
-                                                const T* __restrict__ g, const T* __restrict__ y,
-                                                const int32_t* __restrict__ slot,
-                                                const int64_t* __restrict__ placed,
-                                                const float* __restrict__ weights,
-                                                T* __restrict__ dy, float* __restrict__ dweights) {
-  __shared__ float part[8];
-  const int tid = threadIdx.x;
-  const int64_t from = *placed < 0 ? 0 : *placed;  // slots without a pair
-  for (int64_t u = from + blockIdx.x; u < rows * k; u += gridDim.x)
-    for (int64_t d = tid; d < width; d += 256) dy[u * width + d] = from_f32<T>(0.f);
-  for (int64_t u = blockIdx.x; u < rows * k; u += gridDim.x) {
-    const int32_t p = slot[u];
-    const int64_t t = u / k;
-    const float w = weights ? weights[u] : 1.f;
-    float s = 0.f;
-    if (p >= 0 && p < rows * k)
-      for (int64_t d = tid; d < width; d += 256) {
-        const float v = to_f32(g[t * width + d]);
-        dy[p * width + d] = from_f32<T>(weights ? w * v : v);
-        if (dweights) s = fmaf(v, to_f32(y[p * width + d]), s);
-      }
-    if (dweights) {
+// A pair's slot: its expert's offset, the expert's pairs in earlier tiles, in earlier warps of its
+// tile, and before it in its warp.  Every block adds up the experts' totals (one tile: its own).
+//
+// 169,343 x 8 pairs, 256 experts: a tile of 4096 keeps the per-tile counts (0.3 MB) in L2; a tile of
+// 1024 with a single block scanning them took 179 us in all.
+__global__ void __launch_bounds__(PT) k_plan_place(const int32_t* __restrict__ experts,
+                                                   int64_t pairs, int E, int tiles,
+                                                   const int32_t* __restrict__ tile,
+                                                   const int32_t* __restrict__ total,
+                                                   int64_t* __restrict__ offsets,
+                                                   int32_t* __restrict__ order,
+                                                   int32_t* __restrict__ slot) {
+  extern __shared__ int32_t next[];  // [PW][E]: pairs of each warp, then their next slots
+  __shared__ int32_t part[PW];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  constexpr int PER = PTILE / PW;
+  const int64_t base = (int64_t)blockIdx.x * PTILE + warp * PER;
+  for (int e = tid; e < PW * E; e += PT) next[e] = 0;
+  __syncthreads();
+#pragma unroll 4
+  for (int i = lane; i < PER; i += 32) {
+    const int e = base + i < pairs ? experts[base + i] : -1;
+    if (e >= 0 && e < E) atomicAdd(&next[warp * E + e], 1);
+  }
+  __syncthreads();
+  // offsets: each thread takes MAX_E / PT consecutive experts at most
+  constexpr int Q = MAX_E / PT;
+  const int q = (E + PT - 1) / PT;
+  int32_t count[Q], sum = 0;
 #pragma unroll
-      for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-      __syncthreads();
-      if ((tid & 31) == 0) part[tid >> 5] = s;
-      __syncthreads();
-      if (tid == 0) {
-        s = 0.f;
-        for (int i = 0; i < 8; ++i) s += part[i];
-        dweights[u] = s;
+  for (int j = 0; j < Q; ++j) {
+    const int e = tid * q + j;
+    count[j] = 0;
+    if (j < q && e < E) {
+      if (tiles > 1)
+        count[j] = total[e];
+      else
+        for (int w = 0; w < PW; ++w) count[j] += next[w * E + e];
+    }
+    sum += count[j];
+  }
+  int32_t to = sum;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int32_t y = __shfl_up_sync(0xffffffffu, to, o);
+    if (lane >= o) to += y;
+  }
+  if (lane == 31) part[warp] = to;
+  __syncthreads();
+  int32_t at = to - sum, placed = 0;
+#pragma unroll
+  for (int w = 0; w < PW; ++w) {
+    if (w < warp) at += part[w];
+    placed += part[w];
+  }
+#pragma unroll
+  for (int j = 0; j < Q; ++j) {
+    const int e = tid * q + j;
+    if (j < q && e < E) {
+      if (blockIdx.x == 0) offsets[e] = at;
+      int32_t first = at + (tiles > 1 ? tile[(int64_t)e * tiles + blockIdx.x] : 0);
+      for (int w = 0; w < PW; ++w) {
+        const int32_t c = next[w * E + e];
+        next[w * E + e] = first;
+        first += c;
       }
+    }
+    at += count[j];
+  }
+  if (blockIdx.x == 0 && tid == 0) offsets[E] = placed;
+  __syncthreads();
+  for (int i0 = 0; i0 < PER && base + i0 < pairs; i0 += 32) {  // 32 pairs at a time, in order
+    const int64_t i = base + i0 + lane;
+    const int e = i < pairs ? experts[i] : -1;
+    const bool some = e >= 0 && e < E;
+    const unsigned same = __match_any_sync(0xffffffffu, some ? e : -1);
+    int32_t p = -1;
+    if (some) p = next[warp * E + e] + __popc(same & ((1u << lane) - 1));
+    __syncwarp();
+    if (some && lane == 31 - __clz(same)) next[warp * E + e] = p + 1;
+    __syncwarp();
+    if (some) order[p] = (int32_t)i;
+    if (i < pairs) {
+      slot[i] = p;
+      if (i >= placed) order[i] = -1;
     }
   }
+}
+
+// ------------------------------------------------------------------------------------------------
+// rows of vectors: B bytes (16 where every row starts on 16 bytes, down to one element) at a time
+// ------------------------------------------------------------------------------------------------
+template <int B>
+struct Bytes;
+template <>
+struct Bytes<16> { using type = uint4; };
+template <>
+struct Bytes<8> { using type = uint2; };
+template <>
+struct Bytes<4> { using type = unsigned; };
+template <>
+struct Bytes<2> { using type = unsigned short; };
+
+template <class T, int B>
+union Piece {
+  static constexpr int N = B / sizeof(T);
+  typename Bytes<B>::type raw;
+  T t[N];
+  __device__ __forceinline__ Piece() {}
+};
+
+constexpr int XT = 256;  // threads of a block
+
+// A thread takes a piece of a row, all the row's pairs in flight: the combined row is written once and
+// every y row read once.
+template <class T, int B, int K>
+__global__ void __launch_bounds__(XT) k_combine(int64_t rows, int k, int pieces, int wide,
+                                                const T* __restrict__ y,
+                                                const int32_t* __restrict__ slot,
+                                                const float* __restrict__ weights,
+                                                T* __restrict__ out) {
+  using P = Piece<T, B>;
+  const int per = XT / wide, tr = threadIdx.x / wide, tc = threadIdx.x % wide;
+  if (tr >= per) return;
+  const int64_t pairs = rows * k;
+  const auto* src = reinterpret_cast<const typename Bytes<B>::type*>(y);
+  for (int64_t t = (int64_t)blockIdx.x * per + tr; t < rows; t += (int64_t)gridDim.x * per)
+    for (int c = tc; c < pieces; c += wide) {
+      float s[P::N];
+#pragma unroll
+      for (int i = 0; i < P::N; ++i) s[i] = 0.f;
+      for (int j0 = 0; j0 < k; j0 += K) {
+        P v[K];
+        float w[K];
+        bool some[K];
+#pragma unroll
+        for (int j = 0; j < K; ++j) {
+          const int32_t p = j0 + j < k ? __ldg(slot + t * k + j0 + j) : -1;
+          some[j] = p >= 0 && p < pairs;
+          if (some[j]) {
+            v[j].raw = __ldg(src + (int64_t)p * pieces + c);
+            w[j] = weights ? __ldg(weights + t * k + j0 + j) : 1.f;
+          }
+        }
+#pragma unroll
+        for (int j = 0; j < K; ++j)
+          if (some[j]) {
+#pragma unroll
+            for (int i = 0; i < P::N; ++i)
+              s[i] = weights ? fmaf(w[j], to_f32(v[j].t[i]), s[i]) : s[i] + to_f32(v[j].t[i]);
+          }
+      }
+      P o;
+#pragma unroll
+      for (int i = 0; i < P::N; ++i) o.t[i] = from_f32<T>(s[i]);
+      reinterpret_cast<typename Bytes<B>::type*>(out)[t * pieces + c] = o.raw;
+    }
+}
+
+template <class T, int B>
+__device__ __forceinline__ void zero_rows(int64_t pairs, int pieces, const int64_t* placed, T* out) {
+  using V = typename Bytes<B>::type;
+  const int64_t from = *placed < 0 ? 0 : *placed;
+  if (from >= pairs) return;
+  Piece<T, B> z;
+#pragma unroll
+  for (int i = 0; i < Piece<T, B>::N; ++i) z.t[i] = from_f32<T>(0.f);
+  const int64_t end = pairs * pieces;
+  for (int64_t i = from * pieces + (int64_t)blockIdx.x * XT + threadIdx.x; i < end;
+       i += (int64_t)gridDim.x * XT)
+    reinterpret_cast<V*>(out)[i] = z.raw;
+}
+
+// xs[slot] = x[row]: a row is read once and written to each of its slots
+template <class T, int B>
+__global__ void __launch_bounds__(XT) k_gather(int64_t rows, int k, int pieces, int wide,
+                                               const T* __restrict__ x,
+                                               const int32_t* __restrict__ slot,
+                                               const int64_t* __restrict__ placed,
+                                               T* __restrict__ xs) {
+  using V = typename Bytes<B>::type;
+  const int per = XT / wide, tr = threadIdx.x / wide, tc = threadIdx.x % wide;
+  const int64_t pairs = rows * k;
+  if (tr < per)
+    for (int64_t t = (int64_t)blockIdx.x * per + tr; t < rows; t += (int64_t)gridDim.x * per)
+      for (int c = tc; c < pieces; c += wide) {
+        const V v = __ldg(reinterpret_cast<const V*>(x) + t * pieces + c);
+        for (int j = 0; j < k; ++j) {
+          const int32_t p = __ldg(slot + t * k + j);
+          if (p >= 0 && p < pairs) reinterpret_cast<V*>(xs)[(int64_t)p * pieces + c] = v;
+        }
+      }
+  zero_rows<T, B>(pairs, pieces, placed, xs);
+}
+
+// dy[slot] = weight dout[row] and dweights = dout[row] . y[slot]: a warp takes a row, KG of its pairs
+// at a time, so dout is read once (from L1 for more pairs) and each y row is read where its dy row is
+// written.
+template <class T, int B, int KG>
+__global__ void __launch_bounds__(XT) k_combine_backward(
+    int64_t rows, int k, int pieces, const T* __restrict__ dout, const T* __restrict__ y,
+    const int32_t* __restrict__ slot, const int64_t* __restrict__ placed,
+    const float* __restrict__ weights, T* __restrict__ dy, float* __restrict__ dweights) {
+  using P = Piece<T, B>;
+  using V = typename Bytes<B>::type;
+  const int lane = threadIdx.x & 31;
+  const int64_t pairs = rows * k;
+  for (int64_t t = ((int64_t)blockIdx.x * XT + threadIdx.x) >> 5; t < rows;
+       t += (int64_t)gridDim.x * (XT / 32))
+    for (int j0 = 0; j0 < k; j0 += KG) {
+      int64_t at[KG];
+      float w[KG], s[KG];
+#pragma unroll
+      for (int j = 0; j < KG; ++j) {
+        const int32_t p = j0 + j < k ? __ldg(slot + t * k + j0 + j) : -1;
+        at[j] = p >= 0 && p < pairs ? (int64_t)p * pieces : -1;
+        w[j] = at[j] >= 0 ? __ldg(weights + t * k + j0 + j) : 0.f;
+        s[j] = 0.f;
+      }
+      for (int c = lane; c < pieces; c += 32) {
+        P g, v[KG];
+        g.raw = __ldg(reinterpret_cast<const V*>(dout) + t * pieces + c);
+#pragma unroll
+        for (int j = 0; j < KG; ++j)
+          if (at[j] >= 0) v[j].raw = __ldg(reinterpret_cast<const V*>(y) + at[j] + c);
+#pragma unroll
+        for (int j = 0; j < KG; ++j)
+          if (at[j] >= 0) {
+            P o;
+#pragma unroll
+            for (int i = 0; i < P::N; ++i) {
+              const float f = to_f32(g.t[i]);
+              s[j] = fmaf(f, to_f32(v[j].t[i]), s[j]);
+              o.t[i] = from_f32<T>(w[j] * f);
+            }
+            reinterpret_cast<V*>(dy)[at[j] + c] = o.raw;
+          }
+      }
+#pragma unroll
+      for (int j = 0; j < KG; ++j) {
+#pragma unroll
+        for (int o = 16; o; o >>= 1) s[j] += __shfl_xor_sync(0xffffffffu, s[j], o);
+        if (lane == 0 && j0 + j < k) dweights[t * k + j0 + j] = s[j];
+      }
+    }
+  zero_rows<T, B>(pairs, pieces, placed, dy);
 }
 
 erc_status check_sizes(int64_t rows, int32_t k, int64_t width, int32_t type) {
@@ -156,9 +326,30 @@ erc_status check_sizes(int64_t rows, int32_t k, int64_t width, int32_t type) {
 bool aligned(const void* p, int32_t type) {
   return reinterpret_cast<uintptr_t>(p) % type_bytes(type) == 0;
 }
-unsigned row_grid(int64_t rows) {
-  const int64_t most = 64LL * sm_count();
-  return (unsigned)(rows < most ? rows : most);
+// blocks for `work` units of a block each, as many as a few waves of full SMs
+unsigned grid_of(int64_t work) {
+  const int64_t most = 32LL * sm_count();
+  return (unsigned)(work < most ? (work > 0 ? work : 1) : most);
+}
+// threads that share a row of `pieces`: whole warps, or a power of two below one
+int threads_wide(int64_t pieces) {
+  if (pieces >= XT) return XT;
+  if (pieces > 32) return (int)((pieces + 31) / 32 * 32);
+  int w = 1;
+  while (w < pieces) w *= 2;
+  return w;
+}
+// calls f(B) for the largest piece of at most 16 bytes that divides a row and every base address
+template <class T, class F>
+erc_status with_bytes(int64_t width, std::initializer_list<const void*> bases, F&& f) {
+  uintptr_t all = (uintptr_t)(width * sizeof(T));
+  for (const void* p : bases) all |= reinterpret_cast<uintptr_t>(p);
+  if (all % 16 == 0) return f(std::integral_constant<int, 16>());
+  if (all % 8 == 0) return f(std::integral_constant<int, 8>());
+  if constexpr (sizeof(T) == 2) {
+    if (all % 4 != 0) return f(std::integral_constant<int, 2>());
+  }
+  return f(std::integral_constant<int, 4>());
 }
 
 }  // namespace
@@ -170,6 +361,7 @@ extern "C" size_t erc_expert_plan_workspace_size(int64_t rows, int32_t k, int32_
   if (rows < 0 || k < 1 || k > ERC_ROUTE_MAX_K || rows > 0x7fffffffLL / k || experts < 1 ||
       experts > MAX_E)
     return 0;
+  if (plan_tiles(rows * k) <= 1) return 0;  // a single block plans them
   Arena a(nullptr);
   Plan p;
   plan_experts(a, p, rows * k, experts);
@@ -191,16 +383,20 @@ extern "C" erc_status erc_expert_plan(int64_t rows, int32_t k, int32_t n_experts
     return ERC_OK;
   }
   ERC_REQUIRE(experts && order && slot, "null pointer");
-  if (!ws || ws_bytes < erc_expert_plan_workspace_size(rows, k, n_experts))
+  const int64_t tiles = plan_tiles(pairs);
+  if (tiles > 1 && (!ws || ws_bytes < erc_expert_plan_workspace_size(rows, k, n_experts)))
     return set_error(ERC_ERR_CAPACITY, "workspace too small");
-  Arena ar(reinterpret_cast<void*>((reinterpret_cast<uintptr_t>(ws) + 255) & ~uintptr_t(255)));
-  Plan p;
-  plan_experts(ar, p, pairs, n_experts);
-  const unsigned tiles = (unsigned)((pairs + PTILE - 1) / PTILE);
-  k_plan_count<<<tiles, PT, 0, s>>>(experts, pairs, n_experts, p.tile);
-  k_plan_scan<<<1, MAX_E, 0, s>>>(p.tile, (int)tiles, n_experts, offsets);
-  k_plan_place<<<tiles, PT, 0, s>>>(experts, pairs, n_experts, p.tile, offsets, order, slot);
-  count_launches(3);
+  Plan p = {};
+  if (tiles > 1) {
+    Arena ar(reinterpret_cast<void*>((reinterpret_cast<uintptr_t>(ws) + 255) & ~uintptr_t(255)));
+    plan_experts(ar, p, pairs, n_experts);
+    k_plan_count<<<(unsigned)tiles, PT, 0, s>>>(experts, pairs, n_experts, (int)tiles, p.tile);
+    k_plan_scan<<<n_experts, PT, 0, s>>>(p.tile, (int)tiles, p.total);
+    count_launches(2);
+  }
+  k_plan_place<<<(unsigned)tiles, PT, PW * n_experts * sizeof(int32_t), s>>>(
+      experts, pairs, n_experts, (int)tiles, p.tile, p.total, offsets, order, slot);
+  count_launches(1);
   ERC_CUDA(cudaGetLastError());
   return ERC_OK;
 }
@@ -215,29 +411,19 @@ extern "C" erc_status erc_expert_combine(int64_t rows, int32_t k, int64_t width,
   ERC_REQUIRE(aligned(y, type) && aligned(out, type), "misaligned y or out");
   return with_type(type, [&](auto t) {
     using T = decltype(t);
-    k_combine<T><<<row_grid(rows), 256, 0, as_stream(stream)>>>(
-        rows, k, width, static_cast<const T*>(y), slot, weights, static_cast<T*>(out));
-    count_launches(1);
-    ERC_CUDA(cudaGetLastError());
-    return ERC_OK;
+    return with_bytes<T>(width, {y, out}, [&](auto bytes) {
+      constexpr int B = decltype(bytes)::value;
+      const int pieces = (int)(width * sizeof(T) / B), wide = threads_wide(pieces);
+      const unsigned grid = grid_of((rows + XT / wide - 1) / (XT / wide));
+      auto kernel = k <= 2 ? k_combine<T, B, 2> : k <= 4 ? k_combine<T, B, 4> : k_combine<T, B, 8>;
+      kernel<<<grid, XT, 0, as_stream(stream)>>>(rows, k, pieces, wide, static_cast<const T*>(y), slot,
+                                                 weights, static_cast<T*>(out));
+      count_launches(1);
+      ERC_CUDA(cudaGetLastError());
+      return ERC_OK;
+    });
   });
 }
-
-namespace {
-erc_status expand(int64_t rows, int32_t k, int64_t width, const void* g, const void* y,
-                  int32_t type, const int32_t* slot, const int64_t* placed, const float* weights,
-                  void* dy, float* dweights, erc_stream stream) {
-  return with_type(type, [&](auto t) {
-    using T = decltype(t);
-    k_expand<T><<<row_grid(rows * k), 256, 0, as_stream(stream)>>>(
-        rows, k, width, static_cast<const T*>(g), static_cast<const T*>(y), slot, placed, weights,
-        static_cast<T*>(dy), dweights);
-    count_launches(1);
-    ERC_CUDA(cudaGetLastError());
-    return ERC_OK;
-  });
-}
-}  // namespace
 
 extern "C" erc_status erc_expert_gather(int64_t rows, int32_t k, int64_t width, const void* x,
                                         int32_t type, const int32_t* slot, const int64_t* placed,
@@ -247,7 +433,20 @@ extern "C" erc_status erc_expert_gather(int64_t rows, int32_t k, int64_t width, 
   if (rows == 0 || width == 0) return ERC_OK;
   ERC_REQUIRE(x && slot && placed && xs, "null pointer");
   ERC_REQUIRE(aligned(x, type) && aligned(xs, type), "misaligned x or xs");
-  return expand(rows, k, width, x, nullptr, type, slot, placed, nullptr, xs, nullptr, stream);
+  return with_type(type, [&](auto t) {
+    using T = decltype(t);
+    return with_bytes<T>(width, {x, xs}, [&](auto bytes) {
+      constexpr int B = decltype(bytes)::value;
+      const int pieces = (int)(width * sizeof(T) / B), wide = threads_wide(pieces);
+      const unsigned grid = grid_of((rows + XT / wide - 1) / (XT / wide));
+      k_gather<T, B><<<grid, XT, 0, as_stream(stream)>>>(rows, k, pieces, wide,
+                                                         static_cast<const T*>(x), slot, placed,
+                                                         static_cast<T*>(xs));
+      count_launches(1);
+      ERC_CUDA(cudaGetLastError());
+      return ERC_OK;
+    });
+  });
 }
 
 extern "C" erc_status erc_expert_combine_backward(int64_t rows, int32_t k, int64_t width,
@@ -266,5 +465,20 @@ extern "C" erc_status erc_expert_combine_backward(int64_t rows, int32_t k, int64
   ERC_REQUIRE(dout && y && dy, "null pointer");
   ERC_REQUIRE(aligned(dout, type) && aligned(y, type) && aligned(dy, type),
               "misaligned dout, y or dy");
-  return expand(rows, k, width, dout, y, type, slot, placed, weights, dy, dweights, stream);
+  return with_type(type, [&](auto t) {
+    using T = decltype(t);
+    return with_bytes<T>(width, {dout, y, dy}, [&](auto bytes) {
+      constexpr int B = decltype(bytes)::value;
+      const int pieces = (int)(width * sizeof(T) / B);
+      auto kernel = k == 1   ? k_combine_backward<T, B, 1>
+                    : k <= 2 ? k_combine_backward<T, B, 2>
+                             : k_combine_backward<T, B, 4>;
+      kernel<<<grid_of((rows + XT / 32 - 1) / (XT / 32)), XT, 0, as_stream(stream)>>>(
+          rows, k, pieces, static_cast<const T*>(dout), static_cast<const T*>(y), slot, placed, weights,
+          static_cast<T*>(dy), dweights);
+      count_launches(1);
+      ERC_CUDA(cudaGetLastError());
+      return ERC_OK;
+    });
+  });
 }

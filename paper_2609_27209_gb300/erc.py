@@ -601,9 +601,11 @@ def erc_expert_plan(experts, n_experts, ws=None):
     order = torch.empty(rows * k, dtype=torch.int32, device=dev)
     slot = torch.empty(rows, k, dtype=torch.int32, device=dev)
     if ws is None:
-        ws = _workspace(lib().erc_expert_plan_workspace_size(rows, k, n_experts), dev)
-    _check(lib().erc_expert_plan(rows, k, n_experts, experts.data_ptr(), offsets.data_ptr(), order.data_ptr(),
-                                 slot.data_ptr(), ws.data_ptr(), ws.numel(), _stream_of(experts)))
+        need = lib().erc_expert_plan_workspace_size(rows, k, n_experts)
+        ws = _workspace(need, dev) if need else None
+    _check(lib().erc_expert_plan(rows, k, n_experts, experts.data_ptr(), offsets.data_ptr(),
+                                 order.data_ptr(), slot.data_ptr(), _ptr(ws),
+                                 0 if ws is None else ws.numel(), _stream_of(experts)))
     return offsets, order, slot
 
 
