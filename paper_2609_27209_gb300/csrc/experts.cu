@@ -9,7 +9,7 @@ namespace {
 
 constexpr int PT = 256;        // threads of a plan tile
 constexpr int PW = PT / 32;    // its warps
-constexpr int PTILE = 4096;    // pairs of a plan tile: a warp takes PTILE / PW consecutive ones
+constexpr int PTILE = 2048;    // pairs of a plan tile: a warp takes PTILE / PW consecutive ones
 constexpr int MAX_E = ERC_ROUTE_MAX_EXPERTS;
 
 struct Plan {
@@ -29,11 +29,15 @@ __global__ void __launch_bounds__(PT) k_plan_count(const int32_t* __restrict__ e
   for (int e = threadIdx.x; e < E; e += PT) c[e] = 0;
   __syncthreads();
   const int64_t base = (int64_t)blockIdx.x * PTILE;
-#pragma unroll 4
-  for (int i = threadIdx.x; i < PTILE; i += PT) {
-    const int e = base + i < pairs ? experts[base + i] : -1;
-    if (e >= 0 && e < E) atomicAdd(&c[e], 1);
+  int mine[PTILE / PT];
+#pragma unroll
+  for (int j = 0; j < PTILE / PT; ++j) {
+    const int64_t i = base + j * PT + threadIdx.x;
+    mine[j] = i < pairs ? experts[i] : -1;
   }
+#pragma unroll
+  for (int j = 0; j < PTILE / PT; ++j)
+    if (mine[j] >= 0 && mine[j] < E) atomicAdd(&c[mine[j]], 1);
   __syncthreads();
   for (int e = threadIdx.x; e < E; e += PT) tile[(int64_t)e * tiles + blockIdx.x] = c[e];
 }
@@ -71,8 +75,8 @@ __global__ void __launch_bounds__(PT) k_plan_scan(int32_t* __restrict__ tile, in
 // A pair's slot: its expert's offset, the expert's pairs in earlier tiles, in earlier warps of its
 // tile, and before it in its warp.  Every block adds up the experts' totals (one tile: its own).
 //
-// 169,343 x 8 pairs, 256 experts: a tile of 4096 keeps the per-tile counts (0.3 MB) in L2; a tile of
-// 1024 with a single block scanning them took 179 us in all.
+// 169,343 x 8 pairs, 256 experts: the pairs of a warp stay in registers between
+// its counting and its placing, eight loads in flight.
 __global__ void __launch_bounds__(PT) k_plan_place(const int32_t* __restrict__ experts,
                                                    int64_t pairs, int E, int tiles,
                                                    const int32_t* __restrict__ tile,
@@ -85,13 +89,18 @@ __global__ void __launch_bounds__(PT) k_plan_place(const int32_t* __restrict__ e
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   constexpr int PER = PTILE / PW;
   const int64_t base = (int64_t)blockIdx.x * PTILE + warp * PER;
+  int mine[PER / 32];  // the warp's pairs, 32 consecutive ones at a time; -1: none
+#pragma unroll
+  for (int j = 0; j < PER / 32; ++j) {
+    const int64_t i = base + j * 32 + lane;
+    mine[j] = i < pairs ? experts[i] : -1;
+    if (mine[j] < 0 || mine[j] >= E) mine[j] = -1;
+  }
   for (int e = tid; e < PW * E; e += PT) next[e] = 0;
   __syncthreads();
-#pragma unroll 4
-  for (int i = lane; i < PER; i += 32) {
-    const int e = base + i < pairs ? experts[base + i] : -1;
-    if (e >= 0 && e < E) atomicAdd(&next[warp * E + e], 1);
-  }
+#pragma unroll
+  for (int j = 0; j < PER / 32; ++j)
+    if (mine[j] >= 0) atomicAdd(&next[warp * E + mine[j]], 1);
   __syncthreads();
   // offsets: each thread takes MAX_E / PT consecutive experts at most
   constexpr int Q = MAX_E / PT;
@@ -139,15 +148,15 @@ __global__ void __launch_bounds__(PT) k_plan_place(const int32_t* __restrict__ e
   }
   if (blockIdx.x == 0 && tid == 0) offsets[E] = placed;
   __syncthreads();
-  for (int i0 = 0; i0 < PER && base + i0 < pairs; i0 += 32) {  // 32 pairs at a time, in order
-    const int64_t i = base + i0 + lane;
-    const int e = i < pairs ? experts[i] : -1;
-    const bool some = e >= 0 && e < E;
-    const unsigned same = __match_any_sync(0xffffffffu, some ? e : -1);
+#pragma unroll
+  for (int j = 0; j < PER / 32; ++j) {  // in order
+    const int64_t i = base + j * 32 + lane;
+    const bool some = mine[j] >= 0;
+    const unsigned same = __match_any_sync(0xffffffffu, some ? mine[j] : -1);
     int32_t p = -1;
-    if (some) p = next[warp * E + e] + __popc(same & ((1u << lane) - 1));
+    if (some) p = next[warp * E + mine[j]] + __popc(same & ((1u << lane) - 1));
     __syncwarp();
-    if (some && lane == 31 - __clz(same)) next[warp * E + e] = p + 1;
+    if (some && lane == 31 - __clz(same)) next[warp * E + mine[j]] = p + 1;
     __syncwarp();
     if (some) order[p] = (int32_t)i;
     if (i < pairs) {
@@ -181,8 +190,8 @@ union Piece {
 
 constexpr int XT = 256;  // threads of a block
 
-// A thread takes a piece of a row, all the row's pairs in flight: the combined row is written once and
-// every y row read once.
+// A thread takes a piece of a row, K of the row's pairs in flight and the next row's slots and
+// weights on their way: the combined row is written once and every y row read once.
 template <class T, int B, int K>
 __global__ void __launch_bounds__(XT) k_combine(int64_t rows, int k, int pieces, int wide,
                                                 const T* __restrict__ y,
@@ -190,41 +199,53 @@ __global__ void __launch_bounds__(XT) k_combine(int64_t rows, int k, int pieces,
                                                 const float* __restrict__ weights,
                                                 T* __restrict__ out) {
   using P = Piece<T, B>;
+  using V = typename Bytes<B>::type;
   const int per = XT / wide, tr = threadIdx.x / wide, tc = threadIdx.x % wide;
   if (tr >= per) return;
-  const int64_t pairs = rows * k;
-  const auto* src = reinterpret_cast<const typename Bytes<B>::type*>(y);
-  for (int64_t t = (int64_t)blockIdx.x * per + tr; t < rows; t += (int64_t)gridDim.x * per)
+  const unsigned pairs = (unsigned)(rows * k);
+  const int64_t step = (int64_t)gridDim.x * per;
+  int64_t t = (int64_t)blockIdx.x * per + tr;
+  unsigned p[K], pn[K];  // a pair that is none has a slot of at least `pairs`
+  float w[K], wn[K];
+  auto fetch = [&](int64_t row, int j0, unsigned* q, float* f) {
+#pragma unroll
+    for (int j = 0; j < K; ++j) {
+      const bool in = row < rows && j0 + j < k;
+      q[j] = in ? (unsigned)__ldg(slot + row * k + j0 + j) : 0xffffffffu;
+      f[j] = in && weights ? __ldg(weights + row * k + j0 + j) : 1.f;
+    }
+  };
+  fetch(t, 0, pn, wn);
+  for (; t < rows; t += step) {
+#pragma unroll
+    for (int j = 0; j < K; ++j) {
+      p[j] = pn[j];
+      w[j] = wn[j];
+    }
+    fetch(t + step, 0, pn, wn);
     for (int c = tc; c < pieces; c += wide) {
       float s[P::N];
 #pragma unroll
       for (int i = 0; i < P::N; ++i) s[i] = 0.f;
       for (int j0 = 0; j0 < k; j0 += K) {
+        if (k > K) fetch(t, j0, p, w);
         P v[K];
-        float w[K];
-        bool some[K];
-#pragma unroll
-        for (int j = 0; j < K; ++j) {
-          const int32_t p = j0 + j < k ? __ldg(slot + t * k + j0 + j) : -1;
-          some[j] = p >= 0 && p < pairs;
-          if (some[j]) {
-            v[j].raw = __ldg(src + (int64_t)p * pieces + c);
-            w[j] = weights ? __ldg(weights + t * k + j0 + j) : 1.f;
-          }
-        }
 #pragma unroll
         for (int j = 0; j < K; ++j)
-          if (some[j]) {
+          if (p[j] < pairs) v[j].raw = __ldcs(reinterpret_cast<const V*>(y) + (int64_t)p[j] * pieces + c);
 #pragma unroll
-            for (int i = 0; i < P::N; ++i)
-              s[i] = weights ? fmaf(w[j], to_f32(v[j].t[i]), s[i]) : s[i] + to_f32(v[j].t[i]);
+        for (int j = 0; j < K; ++j)
+          if (p[j] < pairs) {
+#pragma unroll
+            for (int i = 0; i < P::N; ++i) s[i] = fmaf(w[j], to_f32(v[j].t[i]), s[i]);
           }
       }
       P o;
 #pragma unroll
       for (int i = 0; i < P::N; ++i) o.t[i] = from_f32<T>(s[i]);
-      reinterpret_cast<typename Bytes<B>::type*>(out)[t * pieces + c] = o.raw;
+      reinterpret_cast<V*>(out)[t * pieces + c] = o.raw;
     }
+  }
 }
 
 template <class T, int B>
@@ -326,9 +347,9 @@ erc_status check_sizes(int64_t rows, int32_t k, int64_t width, int32_t type) {
 bool aligned(const void* p, int32_t type) {
   return reinterpret_cast<uintptr_t>(p) % type_bytes(type) == 0;
 }
-// blocks for `work` units of a block each, as many as a few waves of full SMs
-unsigned grid_of(int64_t work) {
-  const int64_t most = 32LL * sm_count();
+// blocks for `work` units of a block each, at most so many an SM
+unsigned grid_of(int64_t work, int blocks_an_sm) {
+  const int64_t most = (int64_t)blocks_an_sm * sm_count();
   return (unsigned)(work < most ? (work > 0 ? work : 1) : most);
 }
 // threads that share a row of `pieces`: whole warps, or a power of two below one
@@ -414,7 +435,7 @@ extern "C" erc_status erc_expert_combine(int64_t rows, int32_t k, int64_t width,
     return with_bytes<T>(width, {y, out}, [&](auto bytes) {
       constexpr int B = decltype(bytes)::value;
       const int pieces = (int)(width * sizeof(T) / B), wide = threads_wide(pieces);
-      const unsigned grid = grid_of((rows + XT / wide - 1) / (XT / wide));
+      const unsigned grid = grid_of((rows + XT / wide - 1) / (XT / wide), 4);
       auto kernel = k <= 2 ? k_combine<T, B, 2> : k <= 4 ? k_combine<T, B, 4> : k_combine<T, B, 8>;
       kernel<<<grid, XT, 0, as_stream(stream)>>>(rows, k, pieces, wide, static_cast<const T*>(y), slot,
                                                  weights, static_cast<T*>(out));
@@ -438,7 +459,7 @@ extern "C" erc_status erc_expert_gather(int64_t rows, int32_t k, int64_t width, 
     return with_bytes<T>(width, {x, xs}, [&](auto bytes) {
       constexpr int B = decltype(bytes)::value;
       const int pieces = (int)(width * sizeof(T) / B), wide = threads_wide(pieces);
-      const unsigned grid = grid_of((rows + XT / wide - 1) / (XT / wide));
+      const unsigned grid = grid_of((rows + XT / wide - 1) / (XT / wide), 32);
       k_gather<T, B><<<grid, XT, 0, as_stream(stream)>>>(rows, k, pieces, wide,
                                                          static_cast<const T*>(x), slot, placed,
                                                          static_cast<T*>(xs));
@@ -473,7 +494,7 @@ extern "C" erc_status erc_expert_combine_backward(int64_t rows, int32_t k, int64
       auto kernel = k == 1   ? k_combine_backward<T, B, 1>
                     : k <= 2 ? k_combine_backward<T, B, 2>
                              : k_combine_backward<T, B, 4>;
-      kernel<<<grid_of((rows + XT / 32 - 1) / (XT / 32)), XT, 0, as_stream(stream)>>>(
+      kernel<<<grid_of((rows + XT / 32 - 1) / (XT / 32), 32), XT, 0, as_stream(stream)>>>(
           rows, k, pieces, static_cast<const T*>(dout), static_cast<const T*>(y), slot, placed, weights,
           static_cast<T*>(dy), dweights);
       count_launches(1);
