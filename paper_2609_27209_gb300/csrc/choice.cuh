@@ -133,14 +133,8 @@ __device__ __forceinline__ void pow2_pair(float t0, float t1, float p_out[2], fl
   unpair(p, p_out[0], p_out[1]);
   unpair(r, r_out[0], r_out[1]);
 }
-// weights of two scaled scores: hi and lo with their biases, and 2^t itself
-__device__ __forceinline__ void weight_parts(float t0, float t1, unsigned hi[2], unsigned lo[2],
-                                             float v[2]) {
-  float p[2], r[2];
-  pow2_pair(fmaxf(t0, -60.f), fmaxf(t1, -60.f), p, r);
-  v[0] = __uint_as_float(__float_as_uint(p[0]) + (__float_as_uint(r[0]) << 23));
-  v[1] = __uint_as_float(__float_as_uint(p[1]) + (__float_as_uint(r[1]) << 23));
-  const uint64_t vv = pair(v[0], v[1]);
+// hi and lo, with their biases, of two values of 2^t
+__device__ __forceinline__ void split_weights(uint64_t vv, unsigned hi[2], unsigned lo[2]) {
   const uint64_t two20 = pair(1048576.f, 1048576.f), two23 = pair(8388608.f, 8388608.f);
   const uint64_t h = fma2_rz(vv, two20, two23);
   const uint64_t rest = fma2(vv, two20, add2(two23, h ^ 0x8000000080000000ull));
@@ -153,6 +147,15 @@ __device__ __forceinline__ void weight_parts(float t0, float t1, unsigned hi[2],
   unpair(l, a, b);
   lo[0] = __float_as_uint(a);
   lo[1] = __float_as_uint(b);
+}
+// weights of two scaled scores: hi and lo with their biases, and 2^t itself
+__device__ __forceinline__ void weight_parts(float t0, float t1, unsigned hi[2], unsigned lo[2],
+                                             float v[2]) {
+  float p[2], r[2];
+  pow2_pair(fmaxf(t0, -60.f), fmaxf(t1, -60.f), p, r);
+  v[0] = __uint_as_float(__float_as_uint(p[0]) + (__float_as_uint(r[0]) << 23));
+  v[1] = __uint_as_float(__float_as_uint(p[1]) + (__float_as_uint(r[1]) << 23));
+  split_weights(pair(v[0], v[1]), hi, lo);
 }
 __device__ __forceinline__ unsigned long long join_parts(unsigned hi, unsigned lo) {
   return ((unsigned long long)(hi - BIAS) << 20) + (lo - BIAS);

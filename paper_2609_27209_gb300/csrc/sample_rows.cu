@@ -5,6 +5,7 @@
 // index ascending): the kept set is {score > theta} and the first `ties` entries at theta.  A row's
 // draw is the first kept index whose inclusive weight sum in index order exceeds floor(x W / 2^64).
 #include <atomic>
+#include <type_traits>
 
 #include "choice.cuh"
 
@@ -19,6 +20,10 @@ constexpr int RANK = 4096;    // candidates of a row that one block ranks
 constexpr int BINS = 1024;    // bins of one level of the descent
 constexpr int STEPS = 128;    // bins an octave of the weights' histogram
 constexpr int WBINS = 4096;   // its bins
+constexpr int CODE_LOW = 103 << 7, CODE_HIGH = 134 << 7;  // bfloat16 codes of 2^-24 and 2^7
+constexpr int CODE_ZERO = CODE_HIGH - CODE_LOW + 1;        // place of 0 in the table
+constexpr int CODES = 8192;   // its length; 2 CODE_ZERO + 1 places can be met
+constexpr int CODES_FROM = 8192;  // shortest row that is worth a table
 constexpr int CBINS = 1024;   // bins of the threads' maxima
 constexpr int ROOM = 48 * 1024;  // bytes of a row in a block's shared memory (two blocks an SM)
 
@@ -139,13 +144,19 @@ struct Shared {
   unsigned digit;             // a level's bin
   unsigned first_bin, last_bin;  // of the weights' histogram
   unsigned long long over;    // a level's sum before that bin
+  unsigned odd;               // entries that the code table has no place for
   union {
-    unsigned bins[3][BINS];
-    unsigned count[CBINS];
-    alignas(16) unsigned wbins[WBINS];
+    struct {
+      union {
+        unsigned bins[3][BINS];
+        unsigned count[CBINS];
+        alignas(16) unsigned wbins[WBINS];
+      };
+      unsigned list[LIST];    // candidates' keys
+      uint8_t from[LIST];     // and the warps whose regions hold them
+    };
+    alignas(16) unsigned codes[CODES];  // entries of each bfloat16 code, then its 2^t if it is kept
   };
-  unsigned list[LIST];        // candidates' keys
-  uint8_t from[LIST];         // and the warps whose regions hold them
 };
 
 template <class T>
@@ -160,6 +171,13 @@ struct Row {
   unsigned long long least;
   float tmin;  // entries with t below this weigh less than `least`
 
+  // with the maximum set: the row's scale and eligibility
+  __device__ __forceinline__ void rules(const RowRule& rule) {
+    scale = rule.scale;
+    least = rule.least;
+    odd = max == INFINITY || scale > 3.4028234e38f;
+    tmin = rule.least <= 1 ? -41.5f : log2f((float)rule.least - 0.5f) - 40.01f;
+  }
   __device__ __forceinline__ int begin(int warp) const { return first + warp * region; }
   __device__ __forceinline__ int end(int warp) const { return min(last, begin(warp) + region); }
   // vector `at` of warp `warp`'s region; masked from `stop` on
@@ -182,6 +200,34 @@ struct Row {
     return w >= least ? w : 0ull;
   }
 };
+
+// f(vector, k) for the vectors of the block, each on its way into shared memory too: four loads in
+// flight, of which k is the number
+template <class T, class F>
+__device__ __forceinline__ void stage(const Row<T>& r, F&& f) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int b = r.begin(warp), e = r.end(warp), whole = r.view.whole();
+  uint4* mine = r.buffer + warp * r.resident;
+  auto take = [&](uint4 u, int at, int k) {
+    if (at - b < r.resident) mine[at - b] = u;
+    f(u, k);
+  };
+  int at = b + lane;
+  if (b == 0) {  // the row's first vector may be a part of one
+    if (at < e) take(r.view.fetch(at), at, 0);
+    at += 32;
+  }
+  for (; at - lane + 128 <= min(e, whole); at += 128) {
+    uint4 u[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) u[k] = r.view.inner(at + 32 * k);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) take(u[k], at + 32 * k, k);
+  }
+#pragma unroll
+  for (int k = 0; k < 4; ++k, at += 32)
+    if (at < e) take(r.view.fetch(at), at, k);
+}
 
 // f(vector) for vectors [from, to) of a warp's region, 32 at a time (lanes past the end get masked
 // vectors), the next one loaded meanwhile
@@ -847,168 +893,204 @@ __device__ bool tally(Shared& s, const Row<T>& r, const RowRule& rule, const Tea
   return rule.part == 0xffffffffu;
 }
 
+// ------------------------------------------------------------------------------------------------
+// bfloat16 rows by their codes
+// ------------------------------------------------------------------------------------------------
+// The 16 bits of a score say its weight, so one pass that counts the row's entries by code holds all
+// that the filters need: a place of the table for every magnitude in [2^-24, 2^7) of either sign, and
+// for 0, in descending order of the scores.  Each thread takes 16 places, weighs those that have
+// entries, and running sums over the threads give theta and its ties exactly.  A second pass adds up
+// the kept weights of each region, read from the table (as 2^t, whose parts give the integer).
+// Returns 1, or 0 for a row with nothing to draw, or -1 where an entry has no place in the table.
+//
+// 256 rows of 232,965, top-p: 264 us by weighing every entry twice (issue-bound, 81 instructions an
+// entry); both passes here take about a quarter of the instructions.
+
+// four times the place of the bfloat16 in the upper half of `t` (a: its magnitude): 0's for magnitudes
+// below the table, one past the last of their sign for those above it
+__device__ __forceinline__ int code_place4(unsigned t, int& a) {
+  a = (int)(t >> 16) & 0x7fff;
+  const int i = min(max(a, CODE_LOW - 1), CODE_HIGH) - (CODE_LOW - 1);
+  const int negative = (int)t >> 31;  // -1 or 0
+  return (CODE_ZERO + ((i ^ ~negative) + 1 + negative)) << 2;
+}
+__device__ __forceinline__ float place_value(int place) {
+  const int i = place - CODE_ZERO;
+  if (i == 0) return 0.f;
+  const unsigned a = (unsigned)(abs(i) + CODE_LOW - 1) << 16;
+  return __uint_as_float(i > 0 ? a | 0x80000000u : a);
+}
+
 template <class T, bool SOLO>
-__device__ void sample_row(Shared& s, Row<T>& r, const RowRule& rule, const Team<SOLO>& team,
-                           uint64_t word, int32_t* id, float* logp, int32_t* kept) {
+__device__ int by_codes(Shared& s, Row<T>& r, const RowRule& rule, const Team<SOLO>& team,
+                        float& theta, unsigned& ties, Measured& m) {
+  constexpr int P = CODES / RT;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  for (int b = tid; b < CODES; b += RT) s.codes[b] = 0;
+  if (tid == 0) {
+    s.odd = 0;
+    s.top = CODES;
+    s.last_bin = 0;
+    s.some = 0;
+  }
+  __syncthreads();
+  const unsigned table = (unsigned)__cvta_generic_to_shared(s.codes);
+  bool odd = false;
+  stage(r, [&](uint4 u, int) {
+    const unsigned w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const unsigned t = i & 1 ? w[i / 2] : w[i / 2] << 16;
+      int a;
+      const unsigned at = table + code_place4(t, a);
+      asm volatile(
+          "{\n\t.reg .pred p;\n\tsetp.lt.s32 p, %0, %1;\n\t@p red.shared.add.u32 [%2], 1;\n\t}" ::"r"(a),
+          "n"(CODE_HIGH), "r"(at)
+          : "memory");
+      if ((unsigned)(a - CODE_LOW) >= CODE_HIGH - CODE_LOW)  // neither 0 nor masked: no place
+        odd = odd || !(a == 0 || a > 0x7f80 || (t >> 16) == 0xff80);
+    }
+  });
+  if (odd) s.odd = 1;
+  team.barrier();
+  bool any = false;
+  for (int c = 0; c < team.size(); ++c) any = any || team.load(&s.odd, c);
+  unsigned count[P];
+#pragma unroll
+  for (int i = 0; i < P; ++i) count[i] = 0;
+  for (int c = 0; c < team.size(); ++c)
+#pragma unroll
+    for (int i = 0; i < P; i += 4) {
+      const uint4 q = team.load(reinterpret_cast<const uint4*>(&s.codes[tid * P + i]), c);
+      count[i] += q.x;
+      count[i + 1] += q.y;
+      count[i + 2] += q.z;
+      count[i + 3] += q.w;
+    }
+  unsigned first = CODES;
+#pragma unroll
+  for (int i = P - 1; i >= 0; --i)
+    if (count[i]) first = tid * P + i;
+  first = __reduce_min_sync(0xffffffffu, first);
+  if (lane == 0) atomicMin(&s.top, first);
+  team.barrier();  // the counts have been read everywhere
+  if (any) return -1;
+  if (s.top == CODES) return 0;
+  r.max = place_value((int)s.top);
+  r.rules(rule);
+
+  // 2^t of each place, and its integer weight where it is eligible
+  float v[P];
+#pragma unroll
+  for (int i = 0; i < P; ++i) v[i] = 0.f;
+  auto weight = [&](float x) {
+    unsigned hi[2], lo[2];
+    split_weights(pair(x, x), hi, lo);
+    return join_parts(hi[0], lo[0]);
+  };
+  unsigned entries = 0, all;
+#pragma unroll
+  for (int i = 0; i < P; ++i)
+    if (count[i]) {
+      const float t = r.scaled(place_value(tid * P + i));
+      v[i] = t > -41.5f ? pow2_float(t, -41.f) : 0.f;
+      if (weight(v[i]) < r.least) count[i] = 0;
+      entries += count[i];
+    }
+  const unsigned entries_before = block_exclusive(entries, s.part32, &all);
+  auto left_by_k = [&](unsigned before, unsigned n) {
+    return before < rule.top_k ? min(n, rule.top_k - before) : 0u;
+  };
+  unsigned before = entries_before;
+  unsigned long long mass = 0, total;
+#pragma unroll
+  for (int i = 0; i < P; ++i) {
+    if (count[i]) mass += left_by_k(before, count[i]) * weight(v[i]);
+    before += count[i];
+  }
+  unsigned long long mass_before = block_exclusive(mass, s.part64, &total);
+  unsigned long long target = ~0ull;
+  if (rule.part != 0xffffffffu) {
+    target = (total >> 31) * rule.part + (((total & 0x7fffffffull) * rule.part) >> 31);
+    if (!target) target = 1;
+  }
+  unsigned number = 0, last = 0;
+  before = entries_before;
+#pragma unroll
+  for (int i = 0; i < P; ++i) {
+    const unsigned n = left_by_k(before, count[i]);
+    float keep = 0.f;
+    if (n && mass_before < target) {
+      const unsigned long long w = weight(v[i]);
+      unsigned kept = n;
+      if (target - mass_before < n * w) kept = (unsigned)((target - mass_before + w - 1) / w);
+      if (kept < count[i])
+        s.some = kept;  // only the last kept place is kept in part
+      else
+        keep = v[i];
+      number += kept;
+      last = tid * P + i;
+      mass_before += n * w;
+    }
+    before += count[i];
+    s.codes[tid * P + i] = __float_as_uint(keep);
+  }
+  last = __reduce_max_sync(0xffffffffu, last);
+  if (lane == 0) atomicMax(&s.last_bin, last);
+  unsigned all_kept;
+  block_exclusive(number, s.part32, &all_kept);  // also orders what the block's threads wrote
+  __syncthreads();
+  theta = place_value((int)s.last_bin);
+  ties = s.some ? s.some : 0xffffffffu;
+
+  // the regions' kept mass, and their entries at a theta kept in part
+  const int theta4 = s.some ? (int)s.last_bin << 2 : -1;
+  Part p = {0, 0, 0};
+  unsigned hi = 0, lo = 0, parts = 0;
+  each_vector(r, warp, r.begin(warp), r.end(warp), [&](uint4 u) {
+    const unsigned w[4] = {u.x, u.y, u.z, u.w};
+    float l[8], best = -INFINITY;
+    r.scores(u, l);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) best = fmaxf(best, l[i]);
+    if (!(best >= theta)) return;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      int a;
+      const int p0 = code_place4(w[i] << 16, a), p1 = code_place4(w[i], a);
+      const float v0 = *reinterpret_cast<const float*>(reinterpret_cast<const char*>(s.codes) + p0);
+      const float v1 = *reinterpret_cast<const float*>(reinterpret_cast<const char*>(s.codes) + p1);
+      unsigned h[2], q[2];
+      split_weights(pair(v0, v1), h, q);
+      hi += h[0] + h[1];
+      lo += q[0] + q[1];
+      p.tied += (p0 == theta4) + (p1 == theta4);
+    }
+    parts += 8;
+  });
+  if (parts) p.mass = join_sums(hi, lo, parts);
+  p.tied = __reduce_add_sync(0xffffffffu, p.tied);
+#pragma unroll
+  for (int o = 16; o; o >>= 1) p.mass += __shfl_xor_sync(0xffffffffu, p.mass, o);
+  if (lane == 0) {
+    s.mass[warp] = p.mass;
+    s.above[warp] = 0;
+    s.tied[warp] = p.tied;
+  }
+  m = by_regions(s, r, team, theta, ties);
+  m.number = all_kept;
+  return 1;
+}
+
+// The draw from the kept row: the warp's region it falls in, then a sixteenth of that region, then a
+// vector.
+template <class T, bool SOLO>
+__device__ void draw(Shared& s, const Row<T>& r, const Team<SOLO>& team, float theta, unsigned ties,
+                     const Measured& m, uint64_t word, int32_t* id, float* logp, int32_t* kept) {
+  constexpr int N = Row<T>::N;
   const int C = team.size();
   const unsigned rank = team.rank;
-  constexpr int N = Row<T>::N;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  // one pass over memory: the row's entries into shared memory, each thread's maximum
-  constexpr int TM = 4;  // maxima a thread keeps
-  float tm[TM];
-#pragma unroll
-  for (int k = 0; k < TM; ++k) tm[k] = -INFINITY;
-  {
-    const int b = r.begin(warp), e = r.end(warp), whole = r.view.whole();
-    uint4* mine = r.buffer + warp * r.resident;
-    auto take = [&](uint4 u, int at, float& m) {
-      if (at - b < r.resident) mine[at - b] = u;
-      float l[N];
-      r.scores(u, l);
-#pragma unroll
-      for (int i = 0; i < N; ++i) m = fmaxf(m, l[i]);
-    };
-    int at = b + lane;
-    if (b == 0) {  // the row's first vector may be a part of one
-      if (at < e) take(r.view.fetch(at), at, tm[0]);
-      at += 32;
-    }
-    for (; at - lane + 128 <= min(e, whole); at += 128) {  // four loads in flight
-      uint4 u[4];
-#pragma unroll
-      for (int k = 0; k < 4; ++k) u[k] = r.view.inner(at + 32 * k);
-#pragma unroll
-      for (int k = 0; k < 4; ++k) take(u[k], at + 32 * k, tm[k]);
-    }
-#pragma unroll
-    for (int k = 1; k < TM; ++k, at += 32)
-      if (at < e) take(r.view.fetch(at), at, tm[k]);
-    if (at < e) take(r.view.fetch(at), at, tm[0]);
-  }
-  {
-    unsigned hi = 0, lo = 0xffffffffu;
-#pragma unroll
-    for (int k = 0; k < TM; ++k) {
-      tm[k] = __fadd_rn(tm[k], 0.f);
-      hi = max(hi, order_key(tm[k]));
-      if (tm[k] != -INFINITY) lo = min(lo, order_key(tm[k]));
-    }
-    hi = __reduce_max_sync(0xffffffffu, hi);
-    lo = __reduce_min_sync(0xffffffffu, lo);
-    if (lane == 0) {
-      s.part32[warp] = hi;
-      s.above[warp] = lo;
-    }
-    for (int b = tid; b < CBINS; b += RT) s.count[b] = 0;
-    __syncthreads();
-    if (warp == 0) {
-      const unsigned h = __reduce_max_sync(0xffffffffu, lane < RW ? s.part32[lane] : 0u);
-      const unsigned w = __reduce_min_sync(0xffffffffu, lane < RW ? s.above[lane] : 0xffffffffu);
-      if (lane == 0) {
-        s.top = h;
-        s.low = w;
-      }
-    }
-  }
-  team.barrier();
-  unsigned top = 0, low = 0xffffffffu;
-  {
-    const unsigned t = lane < C ? team.load(&s.top, lane) : 0u;
-    const unsigned w = lane < C ? team.load(&s.low, lane) : 0xffffffffu;
-    top = __reduce_max_sync(0xffffffffu, t);
-    low = __reduce_min_sync(0xffffffffu, w);
-  }
-  r.max = order_value(top);
-  if (r.max == -INFINITY) {  // the same in every block of the cluster
-    if (rank == 0 && tid == 0) {
-      *id = -1;
-      *logp = -INFINITY;
-      *kept = 0;
-    }
-    return;
-  }
-  r.scale = rule.scale;
-  r.least = rule.least;
-  r.odd = r.max == INFINITY || r.scale > 3.4028234e38f;
-  r.tmin = rule.least <= 1 ? -41.5f : log2f((float)rule.least - 0.5f) - 40.01f;
-
-  float theta = -INFINITY;
-  unsigned ties = 0xffffffffu;
-  const bool by_k = rule.top_k < (unsigned)r.view.n, by_p = rule.part != 0xffffffffu;
-  bool done = false, limited = false, measured = false;
-  Measured m;
-  if (by_k && !r.odd) {
-    // At least top_k entries lie no lower than the top_k-th best of the threads' maxima: those down
-    // to its bin are the candidates.
-    const float inv = __fdiv_rn(1023.f, __fsub_rn(r.max, order_value(low)));
-    if (inv < 1e30f && rule.top_k <= (unsigned)(RT * TM / 4 * C)) {
-#pragma unroll
-      for (int k = 0; k < TM; ++k)
-        if (r.weight(tm[k])) {
-          const unsigned b = min((unsigned)(int)__fmul_rn(__fsub_rn(r.max, tm[k]), inv), CBINS - 1u);
-          team.add(&s.count[b], 0, 1u);
-        }
-      team.barrier();
-      unsigned c[CBINS / RT], sum = 0, all;
-#pragma unroll
-      for (int i = 0; i < CBINS / RT; ++i) {
-        c[i] = team.load(&s.count[tid * (CBINS / RT) + i], 0);
-        sum += c[i];
-      }
-      unsigned before = block_exclusive(sum, s.part32, &all);
-#pragma unroll
-      for (int i = 0; i < CBINS / RT; ++i) {
-        if (before < rule.top_k && rule.top_k <= before + c[i]) s.digit = tid * (CBINS / RT) + i;
-        before += c[i];
-      }
-      team.barrier();
-      if (all >= rule.top_k)
-        done = rank_list(s, r, rule, team, inv, (float)s.digit + 1.f, theta, ties);
-    }
-    if (!done) done = tally(s, r, rule, team, theta, ties, limited);
-  }
-  if (!by_k && by_p && !r.odd) {
-    nucleus(s, r, rule, team, theta, ties, m);
-    done = measured = true;
-  }
-  if (!done) {
-    // keys an eligible entry can have: t >= tmin, with room for its roundings
-    const float edge = r.odd ? -INFINITY
-                             : __fadd_rn(r.max, __fdiv_rn(r.tmin - 0.5f, r.scale)) - 1e-5f * fabsf(r.max);
-    unsigned klo = order_key(fmaxf(edge, -3.4028235e38f));
-    if (by_k && !limited) {
-      unsigned khi = top;
-      unsigned long long left = rule.top_k;
-      if (descend<false, false>(s, r, team, klo, khi, left)) {
-        theta = order_value(khi);
-        ties = (unsigned)left;
-        limited = true;
-      }
-    }
-    if (by_p) {
-      m = measure_row(s, r, team, theta, ties);
-      team.barrier();
-      unsigned long long target =
-          (m.total >> 31) * rule.part + (((m.total & 0x7fffffffull) * rule.part) >> 31);
-      if (!target) target = 1;
-      if (m.above_mass < target) {
-        const unsigned long long wt = r.weight(theta);
-        ties = (unsigned)((target - m.above_mass + wt - 1) / wt);
-      } else {
-        if (limited) klo = order_key(theta) + 1;
-        unsigned khi = top;
-        unsigned long long left = target;
-        descend<true, false>(s, r, team, klo, khi, left);
-        theta = order_value(khi);
-        const unsigned long long wt = r.weight(theta);
-        ties = (unsigned)((left + wt - 1) / wt);
-      }
-    }
-  }
-
-  // the draw: the warp's region it falls in, then a sixteenth of that region, then a vector
-  if (!measured) m = measure_row(s, r, team, theta, ties);
   const unsigned long long at = __umul64hi(word, m.total);
   if (tid < C * RW && at >= m.before && at - m.before < m.kept) {
     s.digit = tid;
@@ -1086,6 +1168,164 @@ __device__ void sample_row(Shared& s, Row<T>& r, const RowRule& rule, const Team
       }
     }
   }
+}
+
+template <class T, bool SOLO>
+__device__ void sample_row(Shared& s, Row<T>& r, const RowRule& rule, const Team<SOLO>& team,
+                           uint64_t word, int32_t* id, float* logp, int32_t* kept) {
+  const int C = team.size();
+  const unsigned rank = team.rank;
+  constexpr int N = Row<T>::N;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  float theta = -INFINITY;
+  unsigned ties = 0xffffffffu;
+  Measured m;
+  if constexpr (std::is_same<T, __nv_bfloat16>::value) {
+    if (r.view.n >= CODES_FROM) {
+      const int found = by_codes(s, r, rule, team, theta, ties, m);
+      if (found == 0) {
+        if (rank == 0 && tid == 0) {
+          *id = -1;
+          *logp = -INFINITY;
+          *kept = 0;
+        }
+        return;
+      }
+      if (found > 0) {
+        draw(s, r, team, theta, ties, m, word, id, logp, kept);
+        return;
+      }
+    }
+  }
+
+  // one pass over memory: the row's entries into shared memory, each thread's maxima
+  constexpr int TM = 4;
+  float tm[TM];
+#pragma unroll
+  for (int k = 0; k < TM; ++k) tm[k] = -INFINITY;
+  stage(r, [&](uint4 u, int k) {
+    float l[N];
+    r.scores(u, l);
+#pragma unroll
+    for (int i = 0; i < N; ++i) tm[k] = fmaxf(tm[k], l[i]);
+  });
+  {
+    unsigned hi = 0, lo = 0xffffffffu;
+#pragma unroll
+    for (int k = 0; k < TM; ++k) {
+      tm[k] = __fadd_rn(tm[k], 0.f);
+      hi = max(hi, order_key(tm[k]));
+      if (tm[k] != -INFINITY) lo = min(lo, order_key(tm[k]));
+    }
+    hi = __reduce_max_sync(0xffffffffu, hi);
+    lo = __reduce_min_sync(0xffffffffu, lo);
+    if (lane == 0) {
+      s.part32[warp] = hi;
+      s.above[warp] = lo;
+    }
+    for (int b = tid; b < CBINS; b += RT) s.count[b] = 0;
+    __syncthreads();
+    if (warp == 0) {
+      const unsigned h = __reduce_max_sync(0xffffffffu, lane < RW ? s.part32[lane] : 0u);
+      const unsigned w = __reduce_min_sync(0xffffffffu, lane < RW ? s.above[lane] : 0xffffffffu);
+      if (lane == 0) {
+        s.top = h;
+        s.low = w;
+      }
+    }
+  }
+  team.barrier();
+  unsigned top = 0, low = 0xffffffffu;
+  {
+    const unsigned t = lane < C ? team.load(&s.top, lane) : 0u;
+    const unsigned w = lane < C ? team.load(&s.low, lane) : 0xffffffffu;
+    top = __reduce_max_sync(0xffffffffu, t);
+    low = __reduce_min_sync(0xffffffffu, w);
+  }
+  r.max = order_value(top);
+  if (r.max == -INFINITY) {  // the same in every block of the cluster
+    if (rank == 0 && tid == 0) {
+      *id = -1;
+      *logp = -INFINITY;
+      *kept = 0;
+    }
+    return;
+  }
+  r.rules(rule);
+
+  const bool by_k = rule.top_k < (unsigned)r.view.n, by_p = rule.part != 0xffffffffu;
+  bool done = false, limited = false, measured = false;
+  if (by_k && !r.odd) {
+    // At least top_k entries lie no lower than the top_k-th best of the threads' maxima: those down
+    // to its bin are the candidates.
+    const float inv = __fdiv_rn(1023.f, __fsub_rn(r.max, order_value(low)));
+    if (inv < 1e30f && rule.top_k <= (unsigned)(RT * TM / 4 * C)) {
+#pragma unroll
+      for (int k = 0; k < TM; ++k)
+        if (r.weight(tm[k])) {
+          const unsigned b = min((unsigned)(int)__fmul_rn(__fsub_rn(r.max, tm[k]), inv), CBINS - 1u);
+          team.add(&s.count[b], 0, 1u);
+        }
+      team.barrier();
+      unsigned c[CBINS / RT], sum = 0, all;
+#pragma unroll
+      for (int i = 0; i < CBINS / RT; ++i) {
+        c[i] = team.load(&s.count[tid * (CBINS / RT) + i], 0);
+        sum += c[i];
+      }
+      unsigned before = block_exclusive(sum, s.part32, &all);
+#pragma unroll
+      for (int i = 0; i < CBINS / RT; ++i) {
+        if (before < rule.top_k && rule.top_k <= before + c[i]) s.digit = tid * (CBINS / RT) + i;
+        before += c[i];
+      }
+      team.barrier();
+      if (all >= rule.top_k)
+        done = rank_list(s, r, rule, team, inv, (float)s.digit + 1.f, theta, ties);
+    }
+    if (!done) done = tally(s, r, rule, team, theta, ties, limited);
+  }
+  if (!by_k && by_p && !r.odd) {
+    nucleus(s, r, rule, team, theta, ties, m);
+    done = measured = true;
+  }
+  if (!done) {
+    // keys an eligible entry can have: t >= tmin, with room for its roundings
+    const float edge = r.odd ? -INFINITY
+                             : __fadd_rn(r.max, __fdiv_rn(r.tmin - 0.5f, r.scale)) - 1e-5f * fabsf(r.max);
+    unsigned klo = order_key(fmaxf(edge, -3.4028235e38f));
+    if (by_k && !limited) {
+      unsigned khi = top;
+      unsigned long long left = rule.top_k;
+      if (descend<false, false>(s, r, team, klo, khi, left)) {
+        theta = order_value(khi);
+        ties = (unsigned)left;
+        limited = true;
+      }
+    }
+    if (by_p) {
+      m = measure_row(s, r, team, theta, ties);
+      team.barrier();
+      unsigned long long target =
+          (m.total >> 31) * rule.part + (((m.total & 0x7fffffffull) * rule.part) >> 31);
+      if (!target) target = 1;
+      if (m.above_mass < target) {
+        const unsigned long long wt = r.weight(theta);
+        ties = (unsigned)((target - m.above_mass + wt - 1) / wt);
+      } else {
+        if (limited) klo = order_key(theta) + 1;
+        unsigned khi = top;
+        unsigned long long left = target;
+        descend<true, false>(s, r, team, klo, khi, left);
+        theta = order_value(khi);
+        const unsigned long long wt = r.weight(theta);
+        ties = (unsigned)((left + wt - 1) / wt);
+      }
+    }
+  }
+
+  if (!measured) m = measure_row(s, r, team, theta, ties);
+  draw(s, r, team, theta, ties, m, word, id, logp, kept);
 }
 
 // A cluster of C blocks takes a row: block c its c-th contiguous part, each of the block's warps a

@@ -91,6 +91,25 @@ def test_sample_top_p_that_ends_inside_a_long_flat_tail(kind, n):
         check_sample(torch.from_numpy(x).to(dev()).to(TYPES[kind]), words_of(rng, rows), top_p=p, min_p=1e-6)
 
 
+@pytest.mark.parametrize("rule", RULES, ids=str)
+@pytest.mark.parametrize("n", [8193, 20011, 300007])
+def test_sample_long_bfloat16_rows_of_every_kind(n, rule):
+    rng = np.random.default_rng(n)
+    x = rng.normal(size=(10, n)).astype(np.float32) * 2
+    x[1] = rng.integers(-3, 4, n) * 0.25  # seven values, zeros of both signs
+    x[1][x[1] == 0] *= np.where(rng.random((x[1] == 0).sum()) < 0.5, -1, 1)
+    x[2] = -np.inf
+    x[3] = np.where(rng.random(n) < 0.7, -np.inf, x[3])
+    x[3, ::97] = np.nan
+    x[4, 5] = 300.0  # magnitudes that a table of codes may not hold
+    x[5, ::1001] = 1e-9
+    x[6, 77], x[6, 78] = np.inf, -np.inf
+    x[7] = x[7] * 1e-3 + 100
+    x[8] = -np.abs(x[8]) - 1
+    x[9] = np.finfo(np.float32).min / 2
+    check_sample(torch.from_numpy(x).to(dev()).to(torch.bfloat16), words_of(rng, 10), **rule)
+
+
 @pytest.mark.parametrize("kind", ["f32", "bf16"])
 def test_sample_the_largest_rows(kind):
     n = 1 << 22  # ERC_SAMPLE_ROWS_MAX_N
