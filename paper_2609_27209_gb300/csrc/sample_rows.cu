@@ -25,7 +25,8 @@ constexpr int CODE_ZERO = CODE_HIGH - CODE_LOW + 1;        // place of 0 in the 
 constexpr int CODES = 8192;   // its length; 2 CODE_ZERO + 1 places can be met
 constexpr int CODES_FROM = 8192;  // shortest row that is worth a table
 constexpr int CBINS = 1024;   // bins of the threads' maxima
-constexpr int ROOM = 48 * 1024;  // bytes of a row in a block's shared memory (two blocks an SM)
+constexpr int DEPTH = 6;      // stages of a warp's ring of vectors
+constexpr int RING = RW * DEPTH * 512;  // its bytes for a block (two blocks an SM)
 
 struct RowRule {
   float scale;               // log2(e) / T
@@ -163,8 +164,7 @@ template <class T>
 struct Row {
   static constexpr int N = ScoreVec<T>::N;
   RowView<T> view;
-  uint4* buffer;  // the first `resident` vectors of each warp's region
-  int resident;
+  uint4* ring;  // DEPTH stages of 32 vectors for each warp
   int first, last, region;  // this block's vectors, and vectors of a warp's region
   float max, scale;
   bool odd;  // a maximum of +inf or an infinite scale
@@ -180,18 +180,14 @@ struct Row {
   }
   __device__ __forceinline__ int begin(int warp) const { return first + warp * region; }
   __device__ __forceinline__ int end(int warp) const { return min(last, begin(warp) + region); }
-  // vector `at` of warp `warp`'s region; masked from `stop` on
-  __device__ __forceinline__ uint4 get(int warp, int at, int stop) const {
-    if (at >= stop) {
-      const unsigned w = masked_word<T>();
-      return make_uint4(w, w, w, w);
-    }
-    const int i = at - begin(warp);
-    return i < resident ? buffer[warp * resident + i] : view.fetch(at);
-  }
   __device__ __forceinline__ void scores(uint4 u, float* l) const { unpack_scores(u, l, T()); }
   __device__ __forceinline__ float scaled(float l) const {
     return odd ? below_max(l, max, scale) : __fmul_rn(__fsub_rn(l, max), scale);
+  }
+  __device__ __forceinline__ bool eligible(float l) const {
+    const float t = scaled(l);
+    if (!(t >= tmin)) return false;
+    return (least <= 1 && t > -40.9f) || weight(l);  // t near the edge is weighed
   }
   // the weight of a score, 0 if it is not eligible
   __device__ __forceinline__ unsigned long long weight(float l) const {
@@ -201,56 +197,53 @@ struct Row {
   }
 };
 
-// f(vector, k) for the vectors of the block, each on its way into shared memory too: four loads in
-// flight, of which k is the number
+// f(vector) for vectors [from, to) of the row, 32 at a time (lanes past the end get masked vectors).
+// Each lane's vectors arrive in the warp's ring of shared memory, DEPTH - 1 ahead, and are read by
+// that lane alone.
 template <class T, class F>
-__device__ __forceinline__ void stage(const Row<T>& r, F&& f) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int b = r.begin(warp), e = r.end(warp), whole = r.view.whole();
-  uint4* mine = r.buffer + warp * r.resident;
-  auto take = [&](uint4 u, int at, int k) {
-    if (at - b < r.resident) mine[at - b] = u;
-    f(u, k);
+__device__ __forceinline__ void each_vector(const Row<T>& r, int from, int to, F&& f) {
+  const int lane = threadIdx.x & 31, whole = r.view.whole(), head = r.view.skew ? 1 : 0;
+  const uint4* src = reinterpret_cast<const uint4*>(r.view.base);
+  uint4* mine = r.ring + (threadIdx.x >> 5) * (DEPTH * 32) + lane;
+  const unsigned dst = (unsigned)__cvta_generic_to_shared(mine);
+  auto inside = [&](int at) { return at >= head && at < whole && at < to; };
+  auto issue = [&](int at, unsigned stage) {
+    if (inside(at))
+      asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + stage), "l"(src + at)
+                   : "memory");
+    asm volatile("cp.async.commit_group;" ::: "memory");
   };
-  int at = b + lane;
-  if (b == 0) {  // the row's first vector may be a part of one
-    if (at < e) take(r.view.fetch(at), at, 0);
-    at += 32;
-  }
-  for (; at - lane + 128 <= min(e, whole); at += 128) {
-    uint4 u[4];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) u[k] = r.view.inner(at + 32 * k);
-#pragma unroll
-    for (int k = 0; k < 4; ++k) take(u[k], at + 32 * k, k);
-  }
-#pragma unroll
-  for (int k = 0; k < 4; ++k, at += 32)
-    if (at < e) take(r.view.fetch(at), at, k);
-}
-
-// f(vector) for vectors [from, to) of a warp's region, 32 at a time (lanes past the end get masked
-// vectors), the next one loaded meanwhile
-template <class T, class F>
-__device__ __forceinline__ void each_vector(const Row<T>& r, int warp, int from, int to, F&& f) {
-  const int lane = threadIdx.x & 31;
-  uint4 u = r.get(warp, from + lane, to);
-  for (int at = from; at < to; at += 32) {
-    const uint4 next = r.get(warp, at + 32 + lane, to);
+  for (int d = 0; d < DEPTH - 1; ++d) issue(from + lane + 32 * d, d * 512);
+  unsigned stage = 0, ahead = (DEPTH - 1) * 512;
+  for (int at = from + lane; at - lane < to; at += 32) {
+    issue(at + 32 * (DEPTH - 1), ahead);
+    asm volatile("cp.async.wait_group %0;" ::"n"(DEPTH - 1) : "memory");
+    uint4 u;
+    if (inside(at)) {
+      u = *reinterpret_cast<const uint4*>(reinterpret_cast<const char*>(mine) + stage);
+    } else if (at < to) {
+      u = r.view.fetch(at);  // a vector that the row shares with its neighbours
+    } else {
+      const unsigned w = masked_word<T>();
+      u = make_uint4(w, w, w, w);
+    }
     f(u);
-    u = next;
+    stage = stage == (DEPTH - 1) * 512 ? 0 : stage + 512;
+    ahead = ahead == (DEPTH - 1) * 512 ? 0 : ahead + 512;
   }
+  asm volatile("cp.async.wait_group 0;" ::: "memory");
 }
 
-// mass, numbers and ties of vectors [from, to) of a warp's region, over its lanes
+// mass, numbers and ties of vectors [from, to), over the lanes
 template <class T>
-__device__ Part measure(const Row<T>& r, int warp, int from, int to, float theta) {
+__device__ Part measure(const Row<T>& r, int from, int to, float theta) {
   constexpr int N = Row<T>::N;
   Part p = {0, 0, 0};
   unsigned hi = 0, lo = 0, parts = 0;
   if (r.least == 1 && theta == -INFINITY && !r.odd) {
     const uint64_t m2 = pair(-r.max, -r.max), s2 = pair(r.scale, r.scale);
-    each_vector(r, warp, from, to, [&](uint4 u) {
+    each_vector(r, from, to, [&](uint4 u) {
       uint64_t l[N / 2];
       unpack_pairs<T>(u, l);
 #pragma unroll
@@ -266,26 +259,39 @@ __device__ Part measure(const Row<T>& r, int warp, int from, int to, float theta
       parts += N;
     });
   } else {
-    each_vector(r, warp, from, to, [&](uint4 u) {
+    each_vector(r, from, to, [&](uint4 u) {
       float l[N], best = -INFINITY;
       r.scores(u, l);
 #pragma unroll
       for (int i = 0; i < N; ++i) best = fmaxf(best, l[i]);
       if (!(best >= theta) || !(r.scaled(best) >= r.tmin)) return;
 #pragma unroll
-      for (int i = 0; i < N; ++i) {
-        const unsigned long long w = l[i] >= theta && r.scaled(l[i]) >= r.tmin ? r.weight(l[i]) : 0ull;
-        if (w && l[i] == theta) {
-          ++p.tied;
-        } else if (w) {
-          p.mass += w;
-          ++p.above;
+      for (int i = 0; i < N; i += 2) {
+        unsigned h[2], w[2];
+        float v[2], t[2];
+        if (!(fmaxf(l[i], l[i + 1]) >= theta)) continue;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) t[j] = l[i + j] > theta ? r.scaled(l[i + j]) : -60.f;
+        if (!(fmaxf(t[0], t[1]) >= r.tmin) && theta == -INFINITY) continue;
+        weight_parts(t[0], t[1], h, w, v);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          if (r.least <= 1) {
+            hi += h[j];
+            lo += w[j];
+            ++parts;
+            p.above += v[j] >= 0x1p-41f;
+          } else {
+            const unsigned long long x = join_parts(h[j], w[j]);
+            p.mass += x >= r.least ? x : 0ull;
+            p.above += x >= r.least;
+          }
+          p.tied += l[i + j] == theta && theta > -INFINITY;  // theta itself is eligible
         }
       }
     });
   }
-  if (parts)
-  p.mass += join_sums(hi, lo, parts);
+  if (parts) p.mass += join_sums(hi, lo, parts);
   p.above = __reduce_add_sync(0xffffffffu, p.above);
   p.tied = __reduce_add_sync(0xffffffffu, p.tied);
 #pragma unroll
@@ -328,7 +334,7 @@ template <class T, bool SOLO>
 __device__ Measured measure_row(Shared& s, const Row<T>& r, const Team<SOLO>& team, float theta,
                                 unsigned ties) {
   const int warp = threadIdx.x >> 5;
-  const Part p = measure(r, warp, r.begin(warp), r.end(warp), theta);
+  const Part p = measure(r, r.begin(warp), r.end(warp), theta);
   if ((threadIdx.x & 31) == 0) {
     s.mass[warp] = p.mass;
     s.above[warp] = p.above;
@@ -350,7 +356,7 @@ __device__ __forceinline__ void each_score(const Shared& s, const Row<T>& r, flo
     }
     return;
   }
-  each_vector(r, warp, r.begin(warp), r.end(warp), [&](uint4 u) {
+  each_vector(r, r.begin(warp), r.end(warp), [&](uint4 u) {
     float l[N], best = -INFINITY;
     r.scores(u, l);
 #pragma unroll
@@ -461,7 +467,7 @@ __device__ bool rank_list(Shared& s, const Row<T>& r, const RowRule& rule,
   const int tid = threadIdx.x, warp = tid >> 5;
   if (tid == 0) s.number = 0;
   __syncthreads();
-  each_vector(r, warp, r.begin(warp), r.end(warp), [&](uint4 u) {
+  each_vector(r, r.begin(warp), r.end(warp), [&](uint4 u) {
     float l[N], best = -INFINITY;
     r.scores(u, l);
 #pragma unroll
@@ -469,7 +475,7 @@ __device__ bool rank_list(Shared& s, const Row<T>& r, const RowRule& rule,
     if (!(__fmul_rn(__fsub_rn(r.max, best), inv) < reach)) return;
 #pragma unroll
     for (int i = 0; i < N; ++i)
-      if (__fmul_rn(__fsub_rn(r.max, l[i]), inv) < reach && r.weight(l[i])) {
+      if (__fmul_rn(__fsub_rn(r.max, l[i]), inv) < reach && r.eligible(l[i])) {
         const unsigned p = atomicAdd(&s.number, 1u);
         if (p < RANK) s.list[p] = order_key(__fadd_rn(l[i], 0.f));
       }
@@ -625,7 +631,7 @@ __device__ void nucleus(Shared& s, const Row<T>& r, const RowRule& rule, const T
   if (r.least <= 1) {
     const unsigned bins = (unsigned)__cvta_generic_to_shared(s.wbins) - (BIAS << 2);
     unsigned hi = 0, lo = 0, parts = 0;
-    each_vector(r, warp, r.begin(warp), stop, [&](uint4 u) {
+    each_vector(r, r.begin(warp), stop, [&](uint4 u) {
       uint64_t l[N / 2];
       unpack_pairs<T>(u, l);
 #pragma unroll
@@ -649,7 +655,7 @@ __device__ void nucleus(Shared& s, const Row<T>& r, const RowRule& rule, const T
     });
     if (parts) mass = join_sums(hi, lo, parts);
   } else {
-    each_vector(r, warp, r.begin(warp), stop, [&](uint4 u) {
+    each_vector(r, r.begin(warp), stop, [&](uint4 u) {
       float l[N], best = -INFINITY;
       r.scores(u, l);
 #pragma unroll
@@ -726,7 +732,7 @@ __device__ void nucleus(Shared& s, const Row<T>& r, const RowRule& rule, const T
   Part p = {0, 0, 0};
   {
     unsigned hi = 0, lo = 0, parts = 0;
-    each_vector(r, warp, r.begin(warp), stop, [&](uint4 u) {
+    each_vector(r, r.begin(warp), stop, [&](uint4 u) {
       uint64_t l[N / 2];
       float t[N], best = -INFINITY;
       unpack_pairs<T>(u, l);
@@ -823,13 +829,13 @@ __device__ bool tally(Shared& s, const Row<T>& r, const RowRule& rule, const Tea
   for (int b = tid; b < WBINS; b += RT) s.wbins[b] = 0;
   if (tid == 0) s.number = 0;
   __syncthreads();
-  each_vector(r, warp, r.begin(warp), r.end(warp), [&](uint4 u) {
+  each_vector(r, r.begin(warp), r.end(warp), [&](uint4 u) {
     float l[N];
     r.scores(u, l);
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const float t = r.scaled(l[i]);
-      if (t > low && (r.least <= 1 || r.weight(l[i])))
+      if (t > low && (r.least <= 1 || r.eligible(l[i])))
         atomicAdd(&s.wbins[__float_as_uint(__fmaf_rz(t, -(float)STEPS, 8388608.f)) - BIAS], 1u);
     }
   });
@@ -868,7 +874,7 @@ __device__ bool tally(Shared& s, const Row<T>& r, const RowRule& rule, const Tea
   unsigned long long left = rule.top_k - s.some;
   if (s.some + s.digit <= RANK) return rank_list(s, r, rule, team, r.scale, -to_t, theta, ties);
   __syncthreads();
-  each_vector(r, warp, r.begin(warp), r.end(warp), [&](uint4 u) {
+  each_vector(r, r.begin(warp), r.end(warp), [&](uint4 u) {
     float l[N];
     r.scores(u, l);
 #pragma unroll
@@ -901,7 +907,8 @@ __device__ bool tally(Shared& s, const Row<T>& r, const RowRule& rule, const Tea
 // for 0, in descending order of the scores.  Each thread takes 16 places, weighs those that have
 // entries, and running sums over the threads give theta and its ties exactly.  A second pass adds up
 // the kept weights of each region, read from the table (as 2^t, whose parts give the integer).
-// Returns 1, or 0 for a row with nothing to draw, or -1 where an entry has no place in the table.
+// Returns 1, or 0 for a row with nothing to draw, or -1 where entries without a place of their own
+// could change the result.
 //
 // 256 rows of 232,965, top-p: 264 us by weighing every entry twice (issue-bound, 81 instructions an
 // entry); both passes here take about a quarter of the instructions.
@@ -935,8 +942,8 @@ __device__ int by_codes(Shared& s, Row<T>& r, const RowRule& rule, const Team<SO
   }
   __syncthreads();
   const unsigned table = (unsigned)__cvta_generic_to_shared(s.codes);
-  bool odd = false;
-  stage(r, [&](uint4 u, int) {
+  bool odd = false, tiny = false;
+  each_vector(r, r.begin(warp), r.end(warp), [&](uint4 u) {
     const unsigned w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
@@ -947,14 +954,17 @@ __device__ int by_codes(Shared& s, Row<T>& r, const RowRule& rule, const Team<SO
           "{\n\t.reg .pred p;\n\tsetp.lt.s32 p, %0, %1;\n\t@p red.shared.add.u32 [%2], 1;\n\t}" ::"r"(a),
           "n"(CODE_HIGH), "r"(at)
           : "memory");
-      if ((unsigned)(a - CODE_LOW) >= CODE_HIGH - CODE_LOW)  // neither 0 nor masked: no place
-        odd = odd || !(a == 0 || a > 0x7f80 || (t >> 16) == 0xff80);
+      if ((unsigned)(a - CODE_LOW) >= CODE_HIGH - CODE_LOW) {  // 0, masked, or no place of its own
+        tiny = tiny || (a != 0 && a < CODE_LOW);
+        odd = odd || !(a < CODE_LOW || a > 0x7f80 || (t >> 16) == 0xff80);
+      }
     }
   });
-  if (odd) s.odd = 1;
+  if (odd) atomicOr(&s.odd, 1u);
+  if (tiny) atomicOr(&s.odd, 2u);
   team.barrier();
-  bool any = false;
-  for (int c = 0; c < team.size(); ++c) any = any || team.load(&s.odd, c);
+  unsigned any = 0;
+  for (int c = 0; c < team.size(); ++c) any |= team.load(&s.odd, c);
   unsigned count[P];
 #pragma unroll
   for (int i = 0; i < P; ++i) count[i] = 0;
@@ -974,9 +984,12 @@ __device__ int by_codes(Shared& s, Row<T>& r, const RowRule& rule, const Team<SO
   first = __reduce_min_sync(0xffffffffu, first);
   if (lane == 0) atomicMin(&s.top, first);
   team.barrier();  // the counts have been read everywhere
-  if (any) return -1;
+  if (any & 1) return -1;
   if (s.top == CODES) return 0;
   r.max = place_value((int)s.top);
+  // magnitudes below 2^-24 were counted as 0: beside a maximum of at least 2 their difference from it
+  // rounds to the same float, so they weigh the same
+  if (any && fabsf(r.max) < 2.f) return -1;
   r.rules(rule);
 
   // 2^t of each place, and its integer weight where it is eligible
@@ -1040,14 +1053,17 @@ __device__ int by_codes(Shared& s, Row<T>& r, const RowRule& rule, const Team<SO
   unsigned all_kept;
   block_exclusive(number, s.part32, &all_kept);  // also orders what the block's threads wrote
   __syncthreads();
+  if (any && s.some && s.last_bin == CODE_ZERO) return -1;  // but they are no ties of 0
   theta = place_value((int)s.last_bin);
   ties = s.some ? s.some : 0xffffffffu;
+  // (where 0 is the last place kept, so are the smaller magnitudes below it)
+  if (any && s.last_bin == CODE_ZERO) theta = -0x1.fep-25f;
 
   // the regions' kept mass, and their entries at a theta kept in part
   const int theta4 = s.some ? (int)s.last_bin << 2 : -1;
   Part p = {0, 0, 0};
   unsigned hi = 0, lo = 0, parts = 0;
-  each_vector(r, warp, r.begin(warp), r.end(warp), [&](uint4 u) {
+  each_vector(r, r.begin(warp), r.end(warp), [&](uint4 u) {
     const unsigned w[4] = {u.x, u.y, u.z, u.w};
     float l[8], best = -INFINITY;
     r.scores(u, l);
@@ -1106,7 +1122,7 @@ __device__ void draw(Shared& s, const Row<T>& r, const Team<SOLO>& team, float t
     const int from = min(oe, ob + warp * step), to = min(oe, from + step);
     unsigned long long before = s.over;
     unsigned ties_before = s.some;
-    const Part p = measure(r, ow, from, to, theta);
+    const Part p = measure(r, from, to, theta);
     if (lane == 0) {
       s.sub_mass[warp] = p.mass;
       s.sub_tied[warp] = p.tied;
@@ -1121,9 +1137,11 @@ __device__ void draw(Shared& s, const Row<T>& r, const Team<SOLO>& team, float t
     }
     const unsigned long long here = with_ties(p.mass, p.tied, ties_before);
     if (at >= before && at - before < here) {  // one warp: 32 vectors at a time
+      const unsigned mw = masked_word<T>();
+      const uint4 masked = make_uint4(mw, mw, mw, mw);
       for (int v0 = from; v0 < to; v0 += 32) {
         float l[N];
-        r.scores(r.get(ow, v0 + lane, to), l);
+        r.scores(v0 + lane < to ? r.view.fetch(v0 + lane) : masked, l);
         unsigned long long mass = 0;
         unsigned tied = 0;
 #pragma unroll
@@ -1177,11 +1195,14 @@ __device__ void sample_row(Shared& s, Row<T>& r, const RowRule& rule, const Team
   const unsigned rank = team.rank;
   constexpr int N = Row<T>::N;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  constexpr int TM = 4;  // maxima of a thread
+  const bool by_k = rule.top_k < (unsigned)r.view.n, by_p = rule.part != 0xffffffffu;
   float theta = -INFINITY;
   unsigned ties = 0xffffffffu;
   Measured m;
   if constexpr (std::is_same<T, __nv_bfloat16>::value) {
-    if (r.view.n >= CODES_FROM) {
+    const bool k_by_maxima = by_k && rule.top_k <= (unsigned)min(RT * TM / 4 * C, 512);
+    if (r.view.n >= CODES_FROM && (by_k || by_p) && !k_by_maxima) {
       const int found = by_codes(s, r, rule, team, theta, ties, m);
       if (found == 0) {
         if (rank == 0 && tid == 0) {
@@ -1198,17 +1219,23 @@ __device__ void sample_row(Shared& s, Row<T>& r, const RowRule& rule, const Team
     }
   }
 
-  // one pass over memory: the row's entries into shared memory, each thread's maxima
-  constexpr int TM = 4;
+  // the row's maximum, and each thread's maxima over a quarter of its vectors
   float tm[TM];
 #pragma unroll
   for (int k = 0; k < TM; ++k) tm[k] = -INFINITY;
-  stage(r, [&](uint4 u, int k) {
-    float l[N];
-    r.scores(u, l);
+  {
+    int k = 0;
+    each_vector(r, r.begin(warp), r.end(warp), [&](uint4 u) {
+      float l[N], best = -INFINITY;
+      r.scores(u, l);
 #pragma unroll
-    for (int i = 0; i < N; ++i) tm[k] = fmaxf(tm[k], l[i]);
-  });
+      for (int i = 0; i < N; ++i) best = fmaxf(best, l[i]);
+#pragma unroll
+      for (int i = 0; i < TM; ++i)
+        if (k == i) tm[i] = fmaxf(tm[i], best);
+      k = (k + 1) % TM;
+    });
+  }
   {
     unsigned hi = 0, lo = 0xffffffffu;
 #pragma unroll
@@ -1253,7 +1280,6 @@ __device__ void sample_row(Shared& s, Row<T>& r, const RowRule& rule, const Team
   }
   r.rules(rule);
 
-  const bool by_k = rule.top_k < (unsigned)r.view.n, by_p = rule.part != 0xffffffffu;
   bool done = false, limited = false, measured = false;
   if (by_k && !r.odd) {
     // At least top_k entries lie no lower than the top_k-th best of the threads' maxima: those down
@@ -1262,7 +1288,7 @@ __device__ void sample_row(Shared& s, Row<T>& r, const RowRule& rule, const Team
     if (inv < 1e30f && rule.top_k <= (unsigned)(RT * TM / 4 * C)) {
 #pragma unroll
       for (int k = 0; k < TM; ++k)
-        if (r.weight(tm[k])) {
+        if (r.eligible(tm[k])) {
           const unsigned b = min((unsigned)(int)__fmul_rn(__fsub_rn(r.max, tm[k]), inv), CBINS - 1u);
           team.add(&s.count[b], 0, 1u);
         }
@@ -1333,17 +1359,16 @@ __device__ void sample_row(Shared& s, Row<T>& r, const RowRule& rule, const Team
 template <class T, bool SOLO>
 __global__ void __launch_bounds__(RT, 2)
     k_sample_rows(int64_t rows, int64_t n, const T* __restrict__ logits, int64_t stride,
-                  const uint64_t* __restrict__ words, erc_sample_rule rule, int C, int resident,
+                  const uint64_t* __restrict__ words, erc_sample_rule rule, int C,
                   int32_t* __restrict__ ids, float* __restrict__ logp, int32_t* __restrict__ kept) {
-  extern __shared__ uint4 buffer[];
+  extern __shared__ uint4 ring[];
   __shared__ Shared s;
   const Team<SOLO> team(C);
   C = team.size();
   for (int64_t row = blockIdx.x / C; row < rows; row += gridDim.x / C) {
     Row<T> r = {RowView<T>(logits + row * stride, n)};
     const int part = (r.view.vectors + C - 1) / C;
-    r.buffer = buffer;
-    r.resident = resident;
+    r.ring = ring;
     r.first = min(r.view.vectors, (int)team.rank * part);
     r.last = min(r.view.vectors, r.first + part);
     r.region = (part + RT - 1) / RT * 32;
@@ -1352,26 +1377,15 @@ __global__ void __launch_bounds__(RT, 2)
   }
 }
 
-// Vectors of a warp's region kept in shared memory, blocks of a row, and the dynamic bytes.
-// A block holds at most 2^18 entries (sums of 14-bit limbs and of weight parts stay in 32 bits).
-// Beyond that, blocks are added to a row while the machine has room for them (two blocks an SM)
-// and a block still gets 4096 entries; rows that fill the machine by themselves take one block
-// each and read what shared memory does not hold again from L2.
-struct Shape {
-  int C, resident;
-  size_t bytes;
-};
-Shape shape_of(int64_t rows, int64_t n, int elt) {
-  const int64_t vectors = (n * elt + 15) / 16 + 1;
-  auto region = [&](int C) { return ((vectors + C - 1) / C + RT - 1) / RT * 32; };
-  Shape h;
-  h.C = 1;
-  while (h.C < MAX_C && n > ((int64_t)h.C << 18)) h.C *= 2;
-  while (h.C < MAX_C && rows * h.C * 2 <= 2 * sm_count() && n >= h.C * 2 * 4096) h.C *= 2;
-  const int64_t most = ROOM / (RW * 16) / 32 * 32;
-  h.resident = (int)(region(h.C) < most ? region(h.C) : most);
-  h.bytes = (size_t)h.resident * RW * 16;
-  return h;
+// Blocks of a row.  A block holds at most 2^18 entries (sums of 14-bit limbs and of weight parts stay
+// in 32 bits).  Beyond that, blocks are added to a row while the machine has room for them (two
+// blocks an SM) and a block still gets 4096 entries; rows that fill the machine by themselves take
+// one block each.  Passes after the first find the row in L2.
+int blocks_of(int64_t rows, int64_t n) {
+  int C = 1;
+  while (C < MAX_C && n > ((int64_t)C << 18)) C *= 2;
+  while (C < MAX_C && rows * C * 2 <= 2 * sm_count() && n >= C * 2 * 4096) C *= 2;
+  return C;
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -1559,32 +1573,32 @@ erc_status launch_rows(int64_t rows, int64_t n, const T* logits, int64_t stride,
     ERC_CUDA(cudaGetLastError());
     return ERC_OK;
   }
-  const Shape h = shape_of(rows, n, (int)sizeof(T));
+  const int C = blocks_of(rows, n);
   static std::atomic<uint64_t> ready{0};  // devices whose kernels have their attributes, one bit each
   int dev = 0;
   ERC_CUDA(cudaGetDevice(&dev));
   if (dev >= 64 || !(ready.load(std::memory_order_acquire) >> dev & 1)) {
     ERC_CUDA(cudaFuncSetAttribute(k_sample_rows<T, true>,
-                                  cudaFuncAttributeMaxDynamicSharedMemorySize, ROOM));
+                                  cudaFuncAttributeMaxDynamicSharedMemorySize, RING));
     ERC_CUDA(cudaFuncSetAttribute(k_sample_rows<T, false>,
-                                  cudaFuncAttributeMaxDynamicSharedMemorySize, ROOM));
+                                  cudaFuncAttributeMaxDynamicSharedMemorySize, RING));
     ERC_CUDA(cudaFuncSetAttribute(k_sample_rows<T, false>,
                                   cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
     if (dev < 64) ready.fetch_or(1ull << dev, std::memory_order_release);
   }
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(rows < 65535 ? rows : 65535) * h.C);
+  cfg.gridDim = dim3((unsigned)(rows < 65535 ? rows : 65535) * C);
   cfg.blockDim = dim3(RT);
-  cfg.dynamicSmemBytes = h.bytes;
+  cfg.dynamicSmemBytes = RING;
   cfg.stream = s;
   cudaLaunchAttribute at = {};
   at.id = cudaLaunchAttributeClusterDimension;
-  at.val.clusterDim.x = h.C;
+  at.val.clusterDim.x = C;
   at.val.clusterDim.y = at.val.clusterDim.z = 1;
   cfg.attrs = &at;
-  cfg.numAttrs = h.C > 1;
-  ERC_CUDA(cudaLaunchKernelEx(&cfg, h.C > 1 ? k_sample_rows<T, false> : k_sample_rows<T, true>, rows,
-                              n, logits, stride, words, rule, h.C, h.resident, ids, logp, kept));
+  cfg.numAttrs = C > 1;
+  ERC_CUDA(cudaLaunchKernelEx(&cfg, C > 1 ? k_sample_rows<T, false> : k_sample_rows<T, true>, rows,
+                              n, logits, stride, words, rule, C, ids, logp, kept));
   count_launches(1);
   return ERC_OK;
 }

@@ -110,6 +110,19 @@ def test_sample_long_bfloat16_rows_of_every_kind(n, rule):
     check_sample(torch.from_numpy(x).to(dev()).to(torch.bfloat16), words_of(rng, 10), **rule)
 
 
+@pytest.mark.parametrize("top", [3.0, 1.0, 0.0])
+@pytest.mark.parametrize("rule", [dict(top_p=0.3), dict(top_p=0.999), dict(top_k=7000), dict(top_k=4000, top_p=0.9), dict(top_p=0.5)], ids=str)
+def test_sample_bfloat16_rows_of_zeros_and_tiny_magnitudes(top, rule):
+    rng = np.random.default_rng(int(top))
+    n = 9001
+    x = rng.choice(np.array([0.0, -0.0, 1e-9, -1e-9, 2e-8, -3e-8, 2.0**-24, -(2.0**-24)], np.float32), (6, n))
+    x[:, ::300] = top
+    x[3, 1::2] = -1.0
+    x[4] = np.where(rng.random(n) < 0.5, x[4], 1.0)
+    x[5] = rng.choice(np.array([0.0, -0.0], np.float32), n)
+    check_sample(torch.from_numpy(x).to(dev()).to(torch.bfloat16), words_of(rng, 6), **rule)
+
+
 @pytest.mark.parametrize("kind", ["f32", "bf16"])
 def test_sample_the_largest_rows(kind):
     n = 1 << 22  # ERC_SAMPLE_ROWS_MAX_N
