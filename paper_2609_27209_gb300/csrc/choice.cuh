@@ -198,6 +198,21 @@ __device__ __forceinline__ void unpack_scores(uint4 u, float* l, __half) {
     l[2 * i + 1] = f.y;
   }
 }
+// the largest of 16 bytes of scores, -inf where all are masked
+__device__ __forceinline__ float max_score(uint4 u, float) {
+  return fmaxf(fmaxf(fmaxf(__uint_as_float(u.x), __uint_as_float(u.y)),
+                     fmaxf(__uint_as_float(u.z), __uint_as_float(u.w))), -INFINITY);
+}
+__device__ __forceinline__ float max_score(uint4 u, __nv_bfloat16) {
+  const __nv_bfloat162* p = reinterpret_cast<const __nv_bfloat162*>(&u);
+  const __nv_bfloat162 m = __hmax2(__hmax2(p[0], p[1]), __hmax2(p[2], p[3]));
+  return fmaxf(fmaxf(__low2float(m), __high2float(m)), -INFINITY);
+}
+__device__ __forceinline__ float max_score(uint4 u, __half) {
+  const __half2* p = reinterpret_cast<const __half2*>(&u);
+  const __half2 m = __hmax2(__hmax2(p[0], p[1]), __hmax2(p[2], p[3]));
+  return fmaxf(fmaxf(__low2float(m), __high2float(m)), -INFINITY);
+}
 // the same as pairs for the packed instructions
 template <class T>
 __device__ __forceinline__ void unpack_pairs(uint4 u, uint64_t* p) {

@@ -12,8 +12,6 @@
 namespace erc {
 namespace {
 
-constexpr int RT = 512;       // threads of a block
-constexpr int RW = RT / 32;   // its warps
 constexpr int MAX_C = 16;     // blocks of a row's cluster
 constexpr int LIST = 8192;    // candidates listed in a block's shared memory
 constexpr int RANK = 4096;    // candidates of a row that one block ranks
@@ -26,7 +24,7 @@ constexpr int CODES = 8192;   // its length; 2 CODE_ZERO + 1 places can be met
 constexpr int CODES_FROM = 8192;  // shortest row that is worth a table
 constexpr int CBINS = 1024;   // bins of the threads' maxima
 constexpr int DEPTH = 6;      // stages of a warp's ring of vectors
-constexpr int RING = RW * DEPTH * 512;  // its bytes for a block (two blocks an SM)
+constexpr int ring_bytes(int threads) { return threads / 32 * DEPTH * 512; }
 
 struct RowRule {
   float scale;               // log2(e) / T
@@ -106,8 +104,8 @@ struct Team {
 };
 
 // exclusive sum over the block's threads; *total receives the block's sum
-template <class V>
-__device__ __forceinline__ V block_exclusive(V v, V* part, V* total) {
+template <class V, int RW>
+__device__ __forceinline__ V block_exclusive(V v, V (&part)[RW], V* total) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   V x = v;
 #pragma unroll
@@ -134,7 +132,10 @@ struct Part {  // what a stretch of the row holds: mass and number above theta, 
   unsigned above, tied;
 };
 
+template <int THREADS>
 struct Shared {
+  static constexpr int RT = THREADS;     // threads of a block
+  static constexpr int RW = THREADS / 32;  // its warps
   unsigned long long part64[RW], mass[RW], total64, sure64;
   unsigned part32[RW], above[RW], tied[RW];
   unsigned long long sub_mass[RW];  // of the parts of the drawn region
@@ -202,35 +203,39 @@ struct Row {
 // that lane alone.
 template <class T, class F>
 __device__ __forceinline__ void each_vector(const Row<T>& r, int from, int to, F&& f) {
-  const int lane = threadIdx.x & 31, whole = r.view.whole(), head = r.view.skew ? 1 : 0;
-  const uint4* src = reinterpret_cast<const uint4*>(r.view.base);
+  const int lane = threadIdx.x & 31;
+  auto masked = [] {
+    const unsigned w = masked_word<T>();
+    return make_uint4(w, w, w, w);
+  };
+  if (from == 0 && r.view.skew) {  // the first vector is shared with the row before
+    f(lane < to ? r.view.fetch(lane) : masked());
+    from = 32;
+  }
+  const int whole = min(to, r.view.whole());  // vectors up to here are the row's own
+  const uint4* src = reinterpret_cast<const uint4*>(r.view.base) + lane;
   uint4* mine = r.ring + (threadIdx.x >> 5) * (DEPTH * 32) + lane;
   const unsigned dst = (unsigned)__cvta_generic_to_shared(mine);
-  auto inside = [&](int at) { return at >= head && at < whole && at < to; };
-  auto issue = [&](int at, unsigned stage) {
-    if (inside(at))
-      asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + stage), "l"(src + at)
+  auto issue = [&](int base, unsigned stage) {
+    if (base + 32 <= whole || base + lane < whole)
+      asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + stage), "l"(src + base)
                    : "memory");
     asm volatile("cp.async.commit_group;" ::: "memory");
   };
 #pragma unroll
-  for (int d = 0; d < DEPTH - 1; ++d) issue(from + lane + 32 * d, d * 512);
-  unsigned stage = 0, ahead = (DEPTH - 1) * 512;
-  for (int at = from + lane; at - lane < to; at += 32) {
-    issue(at + 32 * (DEPTH - 1), ahead);
+  for (int d = 0; d < DEPTH - 1; ++d) issue(from + 32 * d, d * 512);
+  unsigned stage = 0, last = (DEPTH - 1) * 512;
+  for (int base = from; base < to; base += 32) {
+    issue(base + 32 * (DEPTH - 1), last);
     asm volatile("cp.async.wait_group %0;" ::"n"(DEPTH - 1) : "memory");
     uint4 u;
-    if (inside(at)) {
+    if (base + 32 <= whole || base + lane < whole)
       u = *reinterpret_cast<const uint4*>(reinterpret_cast<const char*>(mine) + stage);
-    } else if (at < to) {
-      u = r.view.fetch(at);  // a vector that the row shares with its neighbours
-    } else {
-      const unsigned w = masked_word<T>();
-      u = make_uint4(w, w, w, w);
-    }
+    else
+      u = base + lane < to ? r.view.fetch(base + lane) : masked();
     f(u);
+    last = stage;
     stage = stage == (DEPTH - 1) * 512 ? 0 : stage + 512;
-    ahead = ahead == (DEPTH - 1) * 512 ? 0 : ahead + 512;
   }
   asm volatile("cp.async.wait_group 0;" ::: "memory");
 }
@@ -260,11 +265,10 @@ __device__ Part measure(const Row<T>& r, int from, int to, float theta) {
     });
   } else {
     each_vector(r, from, to, [&](uint4 u) {
-      float l[N], best = -INFINITY;
-      r.scores(u, l);
-#pragma unroll
-      for (int i = 0; i < N; ++i) best = fmaxf(best, l[i]);
+      const float best = max_score(u, T());
       if (!(best >= theta) || !(r.scaled(best) >= r.tmin)) return;
+      float l[N];
+      r.scores(u, l);
 #pragma unroll
       for (int i = 0; i < N; i += 2) {
         unsigned h[2], w[2];
@@ -305,9 +309,10 @@ struct Measured {
   unsigned long long before, kept, total, above_mass;
   unsigned ties_before, number, tied;
 };
-template <class T, bool SOLO>
-__device__ Measured by_regions(Shared& s, const Row<T>& r, const Team<SOLO>& team, float theta,
+template <class T, bool SOLO, class S>
+__device__ Measured by_regions(S& s, const Row<T>& r, const Team<SOLO>& team, float theta,
                                unsigned ties) {
+  constexpr int RW = S::RW;
   const int C = team.size();
   const int tid = threadIdx.x;
   team.barrier();
@@ -330,8 +335,8 @@ __device__ Measured by_regions(Shared& s, const Row<T>& r, const Team<SOLO>& tea
   m.number = above + min(tied, ties);
   return m;
 }
-template <class T, bool SOLO>
-__device__ Measured measure_row(Shared& s, const Row<T>& r, const Team<SOLO>& team, float theta,
+template <class T, bool SOLO, class S>
+__device__ Measured measure_row(S& s, const Row<T>& r, const Team<SOLO>& team, float theta,
                                 unsigned ties) {
   const int warp = threadIdx.x >> 5;
   const Part p = measure(r, r.begin(warp), r.end(warp), theta);
@@ -345,8 +350,9 @@ __device__ Measured measure_row(Shared& s, const Row<T>& r, const Team<SOLO>& te
 
 // f(score, warp of its region) for the entries of the block that are no lower than `floor`: those of
 // its regions, or (LISTED) of its candidate list
-template <bool LISTED, class T, class F>
-__device__ __forceinline__ void each_score(const Shared& s, const Row<T>& r, float floor, F&& f) {
+template <bool LISTED, class T, class F, class S>
+__device__ __forceinline__ void each_score(const S& s, const Row<T>& r, float floor, F&& f) {
+  constexpr int RT = S::RT;
   constexpr int N = Row<T>::N;
   const int tid = threadIdx.x, warp = tid >> 5;
   if (LISTED) {
@@ -357,11 +363,9 @@ __device__ __forceinline__ void each_score(const Shared& s, const Row<T>& r, flo
     return;
   }
   each_vector(r, r.begin(warp), r.end(warp), [&](uint4 u) {
-    float l[N], best = -INFINITY;
-    r.scores(u, l);
-#pragma unroll
-    for (int i = 0; i < N; ++i) best = fmaxf(best, l[i]);
-    if (best >= floor) {
+    if (max_score(u, T()) >= floor) {
+      float l[N];
+      r.scores(u, l);
 #pragma unroll
       for (int i = 0; i < N; ++i)
         if (l[i] >= floor) f(l[i], warp);
@@ -374,9 +378,10 @@ __device__ __forceinline__ void each_score(const Shared& s, const Row<T>& r, flo
 // that key and `left` what is still wanted from the entries at it.  A level splits the keys into
 // at most BINS bins; a bin's weights are summed as three limbs of 14 bits, at most 2^18 of them in
 // a block, and the blocks of the cluster each add up a part of the bins.
-template <bool MASS, bool LISTED, class T, bool SOLO>
-__device__ bool descend(Shared& s, const Row<T>& r, const Team<SOLO>& team, unsigned klo,
+template <bool MASS, bool LISTED, class T, bool SOLO, class S>
+__device__ bool descend(S& s, const Row<T>& r, const Team<SOLO>& team, unsigned klo,
                         unsigned& khi, unsigned long long& left, float limit = INFINITY) {
+  constexpr int RT = S::RT;
   const int C = team.size();
   const unsigned rank = team.rank;
   const int tid = threadIdx.x;
@@ -457,10 +462,11 @@ __device__ bool descend(Shared& s, const Row<T>& r, const Team<SOLO>& team, unsi
 // Ranks at most RANK candidates in block 0: top-k, then top-p, to (theta, ties).  Returns false,
 // with nothing decided, where there are more.  Candidates are the eligible entries whose distance
 // from the maximum is below `reach` (all of them: reach = inf).
-template <class T, bool SOLO>
-__device__ bool rank_list(Shared& s, const Row<T>& r, const RowRule& rule,
+template <class T, bool SOLO, class S>
+__device__ bool rank_list(S& s, const Row<T>& r, const RowRule& rule,
                           const Team<SOLO>& team, float inv, float reach, float& theta,
                           unsigned& ties) {
+  constexpr int RT = S::RT;
   const int C = team.size();
   const unsigned rank = team.rank;
   constexpr int N = Row<T>::N;
@@ -468,11 +474,10 @@ __device__ bool rank_list(Shared& s, const Row<T>& r, const RowRule& rule,
   if (tid == 0) s.number = 0;
   __syncthreads();
   each_vector(r, r.begin(warp), r.end(warp), [&](uint4 u) {
-    float l[N], best = -INFINITY;
-    r.scores(u, l);
-#pragma unroll
-    for (int i = 0; i < N; ++i) best = fmaxf(best, l[i]);
+    const float best = max_score(u, T());
     if (!(__fmul_rn(__fsub_rn(r.max, best), inv) < reach)) return;
+    float l[N];
+    r.scores(u, l);
 #pragma unroll
     for (int i = 0; i < N; ++i)
       if (__fmul_rn(__fsub_rn(r.max, l[i]), inv) < reach && r.eligible(l[i])) {
@@ -557,8 +562,8 @@ __device__ bool rank_list(Shared& s, const Row<T>& r, const RowRule& rule,
 }
 
 // Sum over the cluster of a value of each thread.
-template <bool SOLO>
-__device__ unsigned long long team_sum(Shared& s, unsigned long long v, unsigned long long* slot,
+template <bool SOLO, class S>
+__device__ unsigned long long team_sum(S& s, unsigned long long v, unsigned long long* slot,
                                        const Team<SOLO>& team) {
   const int C = team.size();
   const int lane = threadIdx.x & 31;
@@ -573,8 +578,8 @@ __device__ unsigned long long team_sum(Shared& s, unsigned long long v, unsigned
 }
 
 // whether a block's list holds more than it can
-template <bool SOLO>
-__device__ bool overflowed(Shared& s, const Team<SOLO>& team) {
+template <bool SOLO, class S>
+__device__ bool overflowed(S& s, const Team<SOLO>& team) {
   bool over = false;
   for (int k = 0; k < team.size(); ++k) over = over || team.load(&s.number, k) > LIST;
   return over;
@@ -592,7 +597,8 @@ __device__ __forceinline__ void bin_keys(const Row<T>& r, float to_t, float from
 }
 
 // appends the lanes' entries to the block's list
-__device__ __forceinline__ void append(Shared& s, bool in, float l, int warp) {
+template <class S>
+__device__ __forceinline__ void append(S& s, bool in, float l, int warp) {
   const int lane = threadIdx.x & 31;
   const unsigned those = __ballot_sync(0xffffffffu, in);
   unsigned q = 0;
@@ -611,9 +617,10 @@ __device__ __forceinline__ void append(Shared& s, bool in, float l, int warp) {
 // the row itself where a block's list overflows).  Bins are stretches of t (floor(-t STEPS), an
 // exact product), and so are all comparisons.
 // `m` receives the kept row by regions (see Measured).
-template <class T, bool SOLO>
-__device__ void nucleus(Shared& s, const Row<T>& r, const RowRule& rule, const Team<SOLO>& team,
+template <class T, bool SOLO, class S>
+__device__ void nucleus(S& s, const Row<T>& r, const RowRule& rule, const Team<SOLO>& team,
                         float& theta, unsigned& ties, Measured& m) {
+  constexpr int RT = S::RT;
   const int C = team.size();
   constexpr int N = Row<T>::N;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -656,11 +663,10 @@ __device__ void nucleus(Shared& s, const Row<T>& r, const RowRule& rule, const T
     if (parts) mass = join_sums(hi, lo, parts);
   } else {
     each_vector(r, r.begin(warp), stop, [&](uint4 u) {
-      float l[N], best = -INFINITY;
-      r.scores(u, l);
-#pragma unroll
-      for (int i = 0; i < N; ++i) best = fmaxf(best, l[i]);
+      const float best = max_score(u, T());
       if (!(r.scaled(best) > low)) return;
+      float l[N];
+      r.scores(u, l);
 #pragma unroll
       for (int i = 0; i < N; ++i) {
         const float t = r.scaled(l[i]);
@@ -818,9 +824,10 @@ __device__ void nucleus(Shared& s, const Row<T>& r, const RowRule& rule, const T
 // of nucleus(), which gives the bin of the top_k-th exactly.  Where the entries down to that bin
 // can be ranked, they are (done: true).  Else the bin's entries are listed and theta found among
 // them, without top-p (limited).  Neither, where fewer than top_k entries lie in the bins.
-template <class T, bool SOLO>
-__device__ bool tally(Shared& s, const Row<T>& r, const RowRule& rule, const Team<SOLO>& team,
+template <class T, bool SOLO, class S>
+__device__ bool tally(S& s, const Row<T>& r, const RowRule& rule, const Team<SOLO>& team,
                       float& theta, unsigned& ties, bool& limited) {
+  constexpr int RT = S::RT;
   constexpr int N = Row<T>::N;
   constexpr int P = WBINS / RT;
   const int tid = threadIdx.x, warp = tid >> 5;
@@ -928,9 +935,10 @@ __device__ __forceinline__ float place_value(int place) {
   return __uint_as_float(i > 0 ? a | 0x80000000u : a);
 }
 
-template <class T, bool SOLO>
-__device__ int by_codes(Shared& s, Row<T>& r, const RowRule& rule, const Team<SOLO>& team,
+template <class T, bool SOLO, class S>
+__device__ int by_codes(S& s, Row<T>& r, const RowRule& rule, const Team<SOLO>& team,
                         float& theta, unsigned& ties, Measured& m) {
+  constexpr int RT = S::RT;
   constexpr int P = CODES / RT;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   for (int b = tid; b < CODES; b += RT) s.codes[b] = 0;
@@ -1065,11 +1073,10 @@ __device__ int by_codes(Shared& s, Row<T>& r, const RowRule& rule, const Team<SO
   unsigned hi = 0, lo = 0, parts = 0;
   each_vector(r, r.begin(warp), r.end(warp), [&](uint4 u) {
     const unsigned w[4] = {u.x, u.y, u.z, u.w};
-    float l[8], best = -INFINITY;
-    r.scores(u, l);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) best = fmaxf(best, l[i]);
+    const float best = max_score(u, T());
     if (!(best >= theta)) return;
+    float l[8];
+    r.scores(u, l);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       int a;
@@ -1100,9 +1107,10 @@ __device__ int by_codes(Shared& s, Row<T>& r, const RowRule& rule, const Team<SO
 
 // The draw from the kept row: the warp's region it falls in, then a sixteenth of that region, then a
 // vector.
-template <class T, bool SOLO>
-__device__ void draw(Shared& s, const Row<T>& r, const Team<SOLO>& team, float theta, unsigned ties,
+template <class T, bool SOLO, class S>
+__device__ void draw(S& s, const Row<T>& r, const Team<SOLO>& team, float theta, unsigned ties,
                      const Measured& m, uint64_t word, int32_t* id, float* logp, int32_t* kept) {
+  constexpr int RW = S::RW;
   constexpr int N = Row<T>::N;
   const int C = team.size();
   const unsigned rank = team.rank;
@@ -1188,9 +1196,10 @@ __device__ void draw(Shared& s, const Row<T>& r, const Team<SOLO>& team, float t
   }
 }
 
-template <class T, bool SOLO>
-__device__ void sample_row(Shared& s, Row<T>& r, const RowRule& rule, const Team<SOLO>& team,
+template <class T, bool SOLO, class S>
+__device__ void sample_row(S& s, Row<T>& r, const RowRule& rule, const Team<SOLO>& team,
                            uint64_t word, int32_t* id, float* logp, int32_t* kept) {
+  constexpr int RT = S::RT, RW = S::RW;
   const int C = team.size();
   const unsigned rank = team.rank;
   constexpr int N = Row<T>::N;
@@ -1224,16 +1233,11 @@ __device__ void sample_row(Shared& s, Row<T>& r, const RowRule& rule, const Team
 #pragma unroll
   for (int k = 0; k < TM; ++k) tm[k] = -INFINITY;
   {
-    int k = 0;
     each_vector(r, r.begin(warp), r.end(warp), [&](uint4 u) {
-      float l[N], best = -INFINITY;
-      r.scores(u, l);
+      const float best = fmaxf(tm[0], max_score(u, T()));
 #pragma unroll
-      for (int i = 0; i < N; ++i) best = fmaxf(best, l[i]);
-#pragma unroll
-      for (int i = 0; i < TM; ++i)
-        if (k == i) tm[i] = fmaxf(tm[i], best);
-      k = (k + 1) % TM;
+      for (int i = 1; i < TM; ++i) tm[i - 1] = tm[i];  // each fourth vector's maximum
+      tm[TM - 1] = best;
     });
   }
   {
@@ -1356,13 +1360,13 @@ __device__ void sample_row(Shared& s, Row<T>& r, const RowRule& rule, const Team
 
 // A cluster of C blocks takes a row: block c its c-th contiguous part, each of the block's warps a
 // contiguous region of that, so that the index order is the order of (block, warp, vector, lane).
-template <class T, bool SOLO>
-__global__ void __launch_bounds__(RT, 2)
+template <class T, bool SOLO, int RT>
+__global__ void __launch_bounds__(RT, RT == 512 ? 2 : 1)
     k_sample_rows(int64_t rows, int64_t n, const T* __restrict__ logits, int64_t stride,
                   const uint64_t* __restrict__ words, erc_sample_rule rule, int C,
                   int32_t* __restrict__ ids, float* __restrict__ logp, int32_t* __restrict__ kept) {
   extern __shared__ uint4 ring[];
-  __shared__ Shared s;
+  __shared__ Shared<RT> s;
   const Team<SOLO> team(C);
   C = team.size();
   for (int64_t row = blockIdx.x / C; row < rows; row += gridDim.x / C) {
@@ -1573,23 +1577,30 @@ erc_status launch_rows(int64_t rows, int64_t n, const T* logits, int64_t stride,
     ERC_CUDA(cudaGetLastError());
     return ERC_OK;
   }
+  // Blocks of 512 threads, two an SM; where the rows give an SM no second block, blocks of 1024 take
+  // long parts.  112: seven clusters of 16 such blocks fit the machine at once.
   const int C = blocks_of(rows, n);
+  const bool many = C > 1 && rows * C <= 112 && n >= (int64_t)C * 512 * 64;
   static std::atomic<uint64_t> ready{0};  // devices whose kernels have their attributes, one bit each
   int dev = 0;
   ERC_CUDA(cudaGetDevice(&dev));
   if (dev >= 64 || !(ready.load(std::memory_order_acquire) >> dev & 1)) {
-    ERC_CUDA(cudaFuncSetAttribute(k_sample_rows<T, true>,
-                                  cudaFuncAttributeMaxDynamicSharedMemorySize, RING));
-    ERC_CUDA(cudaFuncSetAttribute(k_sample_rows<T, false>,
-                                  cudaFuncAttributeMaxDynamicSharedMemorySize, RING));
-    ERC_CUDA(cudaFuncSetAttribute(k_sample_rows<T, false>,
+    ERC_CUDA(cudaFuncSetAttribute(k_sample_rows<T, true, 512>,
+                                  cudaFuncAttributeMaxDynamicSharedMemorySize, ring_bytes(512)));
+    ERC_CUDA(cudaFuncSetAttribute(k_sample_rows<T, false, 512>,
+                                  cudaFuncAttributeMaxDynamicSharedMemorySize, ring_bytes(512)));
+    ERC_CUDA(cudaFuncSetAttribute(k_sample_rows<T, false, 1024>,
+                                  cudaFuncAttributeMaxDynamicSharedMemorySize, ring_bytes(1024)));
+    ERC_CUDA(cudaFuncSetAttribute(k_sample_rows<T, false, 512>,
+                                  cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
+    ERC_CUDA(cudaFuncSetAttribute(k_sample_rows<T, false, 1024>,
                                   cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
     if (dev < 64) ready.fetch_or(1ull << dev, std::memory_order_release);
   }
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(rows < 65535 ? rows : 65535) * C);
-  cfg.blockDim = dim3(RT);
-  cfg.dynamicSmemBytes = RING;
+  cfg.blockDim = dim3(many ? 1024 : 512);
+  cfg.dynamicSmemBytes = ring_bytes(many ? 1024 : 512);
   cfg.stream = s;
   cudaLaunchAttribute at = {};
   at.id = cudaLaunchAttributeClusterDimension;
@@ -1597,8 +1608,10 @@ erc_status launch_rows(int64_t rows, int64_t n, const T* logits, int64_t stride,
   at.val.clusterDim.y = at.val.clusterDim.z = 1;
   cfg.attrs = &at;
   cfg.numAttrs = C > 1;
-  ERC_CUDA(cudaLaunchKernelEx(&cfg, C > 1 ? k_sample_rows<T, false> : k_sample_rows<T, true>, rows,
-                              n, logits, stride, words, rule, C, ids, logp, kept));
+  auto kernel = C == 1 ? k_sample_rows<T, true, 512>
+                : many ? k_sample_rows<T, false, 1024>
+                       : k_sample_rows<T, false, 512>;
+  ERC_CUDA(cudaLaunchKernelEx(&cfg, kernel, rows, n, logits, stride, words, rule, C, ids, logp, kept));
   count_launches(1);
   return ERC_OK;
 }
