@@ -14,17 +14,12 @@
 namespace erc {
 namespace {
 
+constexpr int SMALL = 16384;   // longest row of a block of 128 threads
 constexpr int MAX_C = 16;     // blocks of a row's cluster
-constexpr int LIST = 8192;    // candidates listed in a block's shared memory
-constexpr int RANK = 4096;    // candidates of a row that one block ranks
-constexpr int BINS = 1024;    // bins of one level of the descent
-constexpr int STEPS = 128;    // bins an octave of the weights' histogram
-constexpr int WBINS = 4096;   // its bins
 constexpr int CODE_LOW = 103 << 7, CODE_HIGH = 134 << 7;  // bfloat16 codes of 2^-24 and 2^7
 constexpr int CODE_ZERO = CODE_HIGH - CODE_LOW + 1;        // place of 0 in the table
 constexpr int CODES = 8192;   // its length; 2 CODE_ZERO + 1 places can be met
 constexpr int CODES_FROM = 8192;  // shortest row that is worth a table
-constexpr int CBINS = 1024;   // bins of the threads' maxima
 constexpr int DEPTH = 6;      // stages of a warp's ring of vectors
 constexpr int ring_bytes(int threads) { return threads / 32 * DEPTH * 512; }
 
@@ -132,6 +127,15 @@ template <int THREADS>
 struct Shared {
   static constexpr int RT = THREADS;     // threads of a block
   static constexpr int RW = THREADS / 32;  // its warps
+  // blocks of 128 threads take rows of at most SMALL entries, several an SM
+  static constexpr bool LARGE = THREADS > 128;
+  static constexpr int LIST = LARGE ? 8192 : 2048;   // candidates listed in a block's memory
+  static constexpr int RANK = LARGE ? 4096 : 1024;   // candidates of a row that one block ranks
+  static constexpr int BIN_BITS = LARGE ? 10 : 9;    // of the bins of one level of the descent
+  static constexpr int BINS = 1 << BIN_BITS;
+  static constexpr int STEPS = LARGE ? 128 : 16;     // bins an octave of the weights' histogram
+  static constexpr int WBINS = 32 * STEPS;           // its bins
+  static constexpr int CBINS = LARGE ? 1024 : 256;   // bins of the threads' maxima
   unsigned long long part64[RW], mass[RW], total64, sure64;
   unsigned part32[RW], above[RW], tied[RW];
   unsigned long long sub_mass[RW];  // of the parts of the drawn region
@@ -153,7 +157,7 @@ struct Shared {
       unsigned list[LIST];    // candidates' keys
       uint8_t from[LIST];     // and the warps whose regions hold them
     };
-    alignas(16) unsigned codes[CODES];  // entries of each bfloat16 code, then its 2^t if it is kept
+    alignas(16) unsigned codes[LARGE ? CODES : 4];  // entries of each bfloat16 code, then its 2^t if it is kept
   };
 };
 
@@ -381,11 +385,11 @@ __device__ bool descend(S& s, const Row<T>& r, const Team<SOLO>& team, unsigned 
   const int C = team.size();
   const unsigned rank = team.rank;
   const int tid = threadIdx.x;
-  const int B = BINS / C;
+  const int B = S::BINS / C;
   for (;;) {
     const unsigned span = khi - klo;
-    const int shift = span < BINS ? 0 : 22 - __clz(span);
-    for (int b = tid; b < (MASS ? 3 : 1) * BINS; b += RT) s.bins[0][b] = 0;
+    const int shift = span < S::BINS ? 0 : 32 - S::BIN_BITS - __clz(span);
+    for (int b = tid; b < (MASS ? 3 : 1) * S::BINS; b += RT) s.bins[0][b] = 0;
     __syncthreads();
     each_score<LISTED>(s, r, order_value(klo), [&](float l, int) {
       const unsigned d = khi - order_key(__fadd_rn(l, 0.f));
@@ -404,10 +408,10 @@ __device__ bool descend(S& s, const Row<T>& r, const Team<SOLO>& team, unsigned 
     });
     team.barrier();
     // this block's share of the bins: bins rank * B .., BINS / RT of them a thread at most
-    unsigned long long v[BINS / RT], mine = 0;
+    unsigned long long v[S::BINS / RT], mine = 0;
     const int per = (B + RT - 1) / RT;
 #pragma unroll
-    for (int i = 0; i < BINS / RT; ++i) {
+    for (int i = 0; i < S::BINS / RT; ++i) {
       v[i] = 0;
       const int b = tid * per + i;
       if (i < per && b < B)
@@ -435,7 +439,7 @@ __device__ bool descend(S& s, const Row<T>& r, const Team<SOLO>& team, unsigned 
     if (owner == (int)rank) {
       before += base;
 #pragma unroll
-      for (int i = 0; i < BINS / RT; ++i) {
+      for (int i = 0; i < S::BINS / RT; ++i) {
         if (v[i] && before < left && left <= before + v[i]) {
           s.digit = rank * B + tid * per + i;
           s.over = before;
@@ -478,7 +482,7 @@ __device__ bool rank_list(S& s, const Row<T>& r, const RowRule& rule,
     for (int i = 0; i < N; ++i)
       if (__fmul_rn(__fsub_rn(r.max, l[i]), inv) < reach && r.eligible(l[i])) {
         const unsigned p = atomicAdd(&s.number, 1u);
-        if (p < RANK) s.list[p] = order_key(__fadd_rn(l[i], 0.f));
+        if (p < S::RANK) s.list[p] = order_key(__fadd_rn(l[i], 0.f));
       }
   });
   team.barrier();
@@ -488,7 +492,7 @@ __device__ bool rank_list(S& s, const Row<T>& r, const RowRule& rule,
     if (c == 0) mine = q;
     all += q;
   }
-  if (all > RANK) {
+  if (all > S::RANK) {
     team.barrier();
     return false;
   }
@@ -517,10 +521,10 @@ __device__ bool rank_list(S& s, const Row<T>& r, const RowRule& rule,
       }
     // each thread takes RANK / RT consecutive candidates
     const unsigned keep = min(all, rule.top_k);
-    unsigned long long w[RANK / RT], sum = 0, total;
+    unsigned long long w[S::RANK / RT], sum = 0, total;
 #pragma unroll
-    for (int i = 0; i < RANK / RT; ++i) {
-      const unsigned at_i = tid * (RANK / RT) + i;
+    for (int i = 0; i < S::RANK / RT; ++i) {
+      const unsigned at_i = tid * (S::RANK / RT) + i;
       w[i] = at_i < keep ? r.weight(order_value(s.list[at_i])) : 0ull;
       sum += w[i];
     }
@@ -532,7 +536,7 @@ __device__ bool rank_list(S& s, const Row<T>& r, const RowRule& rule,
     }
     unsigned kept = 0;
 #pragma unroll
-    for (int i = 0; i < RANK / RT; ++i) {
+    for (int i = 0; i < S::RANK / RT; ++i) {
       if (w[i] && before < target) ++kept;
       before += w[i];
     }
@@ -577,7 +581,7 @@ __device__ unsigned long long team_sum(S& s, unsigned long long v, unsigned long
 template <bool SOLO, class S>
 __device__ bool overflowed(S& s, const Team<SOLO>& team) {
   bool over = false;
-  for (int k = 0; k < team.size(); ++k) over = over || team.load(&s.number, k) > LIST;
+  for (int k = 0; k < team.size(); ++k) over = over || team.load(&s.number, k) > S::LIST;
   return over;
 }
 
@@ -600,7 +604,7 @@ __device__ __forceinline__ void append(S& s, bool in, float l, int warp) {
   unsigned q = 0;
   if (lane == 0) q = atomicAdd(&s.number, (unsigned)__popc(those));
   q = __shfl_sync(0xffffffffu, q, 0) + __popc(those & ((1u << lane) - 1));
-  if (in && q < LIST) {
+  if (in && q < S::LIST) {
     s.list[q] = order_key(__fadd_rn(l, 0.f));
     s.from[q] = (uint8_t)warp;
   }
@@ -624,9 +628,9 @@ __device__ void nucleus(S& s, const Row<T>& r, const RowRule& rule, const Team<S
   // the maximum alone weighs 2^40: all entries below `cut` together weigh less than an eighth of
   // 1 - top_p of that, so theta is above it (or below the last bin)
   const float rest = 1.f - __fmul_rn((float)rule.part, 0x1p-31f);
-  const float cut = fmaxf(log2f(__fdiv_rn(rest, (float)r.view.n)) - 3.01f, -(float)WBINS / STEPS);
+  const float cut = fmaxf(log2f(__fdiv_rn(rest, (float)r.view.n)) - 3.01f, -(float)S::WBINS / S::STEPS);
   const float low = fmaxf(cut, r.tmin - 1.f);
-  for (int b = tid; b < WBINS; b += RT) s.wbins[b] = 0;
+  for (int b = tid; b < S::WBINS; b += RT) s.wbins[b] = 0;
   if (tid == 0) s.number = 0;
   __syncthreads();
   unsigned long long mass = 0;
@@ -647,7 +651,7 @@ __device__ void nucleus(S& s, const Row<T>& r, const RowRule& rule, const Team<S
         lo += w[0] + w[1];
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-          const unsigned bin = __float_as_uint(__fmaf_rz(t[j], -(float)STEPS, 8388608.f));
+          const unsigned bin = __float_as_uint(__fmaf_rz(t[j], -(float)S::STEPS, 8388608.f));
           asm volatile(
               "{\n\t.reg .pred p;\n\tsetp.gt.f32 p, %0, %1;\n\t@p red.shared.add.u32 [%2], 1;\n\t}" ::"f"(t[j]),
               "f"(low), "r"(bins + (bin << 2))
@@ -668,7 +672,7 @@ __device__ void nucleus(S& s, const Row<T>& r, const RowRule& rule, const Team<S
         const float t = r.scaled(l[i]);
         const unsigned long long w = t > low ? r.weight(l[i]) : 0ull;
         mass += w;
-        if (w) atomicAdd(&s.wbins[__float_as_uint(__fmaf_rz(t, -(float)STEPS, 8388608.f)) - BIAS], 1u);
+        if (w) atomicAdd(&s.wbins[__float_as_uint(__fmaf_rz(t, -(float)S::STEPS, 8388608.f)) - BIAS], 1u);
       }
     });
   }
@@ -679,7 +683,7 @@ __device__ void nucleus(S& s, const Row<T>& r, const RowRule& rule, const Team<S
   // bounds of the running mass through each bin, from the bins before it and from those after it
   float from_t, to_t;  // theta lies in to_t < t <= from_t
   {
-    constexpr int P = WBINS / RT;
+    constexpr int P = S::WBINS / RT;
     unsigned c[P] = {};
 #pragma unroll 4
     for (int k = 0; k < C; ++k)
@@ -694,8 +698,8 @@ __device__ void nucleus(S& s, const Row<T>& r, const RowRule& rule, const Team<S
     unsigned long long least[P], most[P], ls = 0, ms = 0, all_least, all_most;
 #pragma unroll
     for (int i = 0; i < P; ++i) {
-      const float top = exp2f(40.f - (float)(tid * P + i) * (1.f / STEPS));
-      const float bottom = top * (1.f - 0.005402f - 2e-5f);  // 2^(-1/128) = 1 - 0.0054005
+      const float top = exp2f(40.f - (float)(tid * P + i) * (1.f / S::STEPS));
+      const float bottom = top * exp2f(-1.f / S::STEPS) * (1.f - 2e-5f);
       least[i] = c[i] * (bottom > 1.f ? (unsigned long long)(bottom - 1.f) : 0ull);
       most[i] = c[i] * ((unsigned long long)(top * (1.f + 2e-5f)) + 1ull);
       ls += least[i];
@@ -706,8 +710,8 @@ __device__ void nucleus(S& s, const Row<T>& r, const RowRule& rule, const Team<S
     const unsigned long long below =  // what is not counted weighs at most this
         low > cut ? 0ull : (unsigned long long)(exp2f(40.f + low) * 1.001f * (float)r.view.n) + r.view.n;
     if (tid == 0) {
-      s.first_bin = WBINS;
-      s.last_bin = WBINS;
+      s.first_bin = S::WBINS;
+      s.last_bin = S::WBINS;
     }
     __syncthreads();
 #pragma unroll
@@ -727,8 +731,8 @@ __device__ void nucleus(S& s, const Row<T>& r, const RowRule& rule, const Team<S
       if (lower(mb, lb) >= target && (start || lower(m0, l0) < target)) s.last_bin = tid * P + i;
     }
     __syncthreads();
-    from_t = -(float)s.first_bin * (1.f / STEPS);
-    to_t = s.last_bin < WBINS ? -(float)(s.last_bin + 1) * (1.f / STEPS) : -INFINITY;
+    from_t = -(float)s.first_bin * (1.f / S::STEPS);
+    to_t = s.last_bin < S::WBINS ? -(float)(s.last_bin + 1) * (1.f / S::STEPS) : -INFINITY;
   }
   // what lies above the bins, by regions, and the list of what lies in them
   Part p = {0, 0, 0};
@@ -825,11 +829,11 @@ __device__ bool tally(S& s, const Row<T>& r, const RowRule& rule, const Team<SOL
                       float& theta, unsigned& ties, bool& limited) {
   constexpr int RT = S::RT;
   constexpr int N = Row<T>::N;
-  constexpr int P = WBINS / RT;
+  constexpr int P = S::WBINS / RT;
   const int tid = threadIdx.x, warp = tid >> 5;
-  const float low = fmaxf(r.tmin - 1.f, -(float)WBINS / STEPS);
+  const float low = fmaxf(r.tmin - 1.f, -(float)S::WBINS / S::STEPS);
   team.barrier();  // the bins share memory with counts that other blocks read
-  for (int b = tid; b < WBINS; b += RT) s.wbins[b] = 0;
+  for (int b = tid; b < S::WBINS; b += RT) s.wbins[b] = 0;
   if (tid == 0) s.number = 0;
   __syncthreads();
   each_vector(r, r.begin(warp), r.end(warp), [&](uint4 u) {
@@ -839,7 +843,7 @@ __device__ bool tally(S& s, const Row<T>& r, const RowRule& rule, const Team<SOL
     for (int i = 0; i < N; ++i) {
       const float t = r.scaled(l[i]);
       if (t > low && (r.least <= 1 || r.eligible(l[i])))
-        atomicAdd(&s.wbins[__float_as_uint(__fmaf_rz(t, -(float)STEPS, 8388608.f)) - BIAS], 1u);
+        atomicAdd(&s.wbins[__float_as_uint(__fmaf_rz(t, -(float)S::STEPS, 8388608.f)) - BIAS], 1u);
     }
   });
   team.barrier();
@@ -869,13 +873,13 @@ __device__ bool tally(S& s, const Row<T>& r, const RowRule& rule, const Team<SOL
   team.barrier();
   if (all < rule.top_k) {
     // every eligible entry, where all of them lie in the bins and can be ranked
-    return r.tmin - 1.f > -(float)WBINS / STEPS && all <= RANK &&
+    return r.tmin - 1.f > -(float)S::WBINS / S::STEPS && all <= S::RANK &&
            rank_list(s, r, rule, team, r.scale, -low, theta, ties);
   }
   const unsigned bin = s.first_bin;
-  const float from_t = -(float)bin * (1.f / STEPS), to_t = -(float)(bin + 1) * (1.f / STEPS);
+  const float from_t = -(float)bin * (1.f / S::STEPS), to_t = -(float)(bin + 1) * (1.f / S::STEPS);
   unsigned long long left = rule.top_k - s.some;
-  if (s.some + s.digit <= RANK) return rank_list(s, r, rule, team, r.scale, -to_t, theta, ties);
+  if (s.some + s.digit <= S::RANK) return rank_list(s, r, rule, team, r.scale, -to_t, theta, ties);
   __syncthreads();
   each_vector(r, r.begin(warp), r.end(warp), [&](uint4 u) {
     float l[N];
@@ -1204,7 +1208,7 @@ __device__ void sample_row(S& s, Row<T>& r, const RowRule& rule, const Team<SOLO
   float theta = -INFINITY;
   unsigned ties = 0xffffffffu;
   Measured m;
-  if constexpr (std::is_same<T, __nv_bfloat16>::value) {
+  if constexpr (std::is_same<T, __nv_bfloat16>::value && S::LARGE) {
     const bool k_by_maxima = by_k && rule.top_k <= (unsigned)min(RT * TM / 4 * C, 512);
     if (r.view.n >= CODES_FROM && (by_k || by_p) && !k_by_maxima) {
       const int found = by_codes(s, r, rule, team, theta, ties, m);
@@ -1249,7 +1253,7 @@ __device__ void sample_row(S& s, Row<T>& r, const RowRule& rule, const Team<SOLO
       s.part32[warp] = hi;
       s.above[warp] = lo;
     }
-    for (int b = tid; b < CBINS; b += RT) s.count[b] = 0;
+    for (int b = tid; b < S::CBINS; b += RT) s.count[b] = 0;
     __syncthreads();
     if (warp == 0) {
       const unsigned h = __reduce_max_sync(0xffffffffu, lane < RW ? s.part32[lane] : 0u);
@@ -1283,27 +1287,27 @@ __device__ void sample_row(S& s, Row<T>& r, const RowRule& rule, const Team<SOLO
   if (by_k && !r.odd) {
     // At least top_k entries lie no lower than the top_k-th best of the threads' maxima: those down
     // to its bin are the candidates.
-    const float inv = __fdiv_rn(1023.f, __fsub_rn(r.max, order_value(low)));
+    const float inv = __fdiv_rn((float)(S::CBINS - 1), __fsub_rn(r.max, order_value(low)));
     if (inv < 1e30f && rule.top_k <= (unsigned)(RT * TM / 4 * C)) {
 #pragma unroll
       for (int k = 0; k < TM; ++k)
         if (r.eligible(tm[k])) {
-          const unsigned b = min((unsigned)(int)__fmul_rn(__fsub_rn(r.max, tm[k]), inv), CBINS - 1u);
+          const unsigned b = min((unsigned)(int)__fmul_rn(__fsub_rn(r.max, tm[k]), inv), S::CBINS - 1u);
           atomicAdd(&s.count[b], 1u);
         }
       team.barrier();
-      unsigned c[CBINS / RT], sum = 0, all;
+      unsigned c[S::CBINS / RT], sum = 0, all;
 #pragma unroll
-      for (int i = 0; i < CBINS / RT; ++i) {
+      for (int i = 0; i < S::CBINS / RT; ++i) {
         c[i] = 0;
 #pragma unroll 4
-        for (int q = 0; q < C; ++q) c[i] += team.load(&s.count[tid * (CBINS / RT) + i], q);
+        for (int q = 0; q < C; ++q) c[i] += team.load(&s.count[tid * (S::CBINS / RT) + i], q);
         sum += c[i];
       }
       unsigned before = block_exclusive(sum, s.part32, &all);
 #pragma unroll
-      for (int i = 0; i < CBINS / RT; ++i) {
-        if (before < rule.top_k && rule.top_k <= before + c[i]) s.digit = tid * (CBINS / RT) + i;
+      for (int i = 0; i < S::CBINS / RT; ++i) {
+        if (before < rule.top_k && rule.top_k <= before + c[i]) s.digit = tid * (S::CBINS / RT) + i;
         before += c[i];
       }
       team.barrier();
@@ -1358,7 +1362,7 @@ __device__ void sample_row(S& s, Row<T>& r, const RowRule& rule, const Team<SOLO
 // A cluster of C blocks takes a row: block c its c-th contiguous part, each of the block's warps a
 // contiguous region of that, so that the index order is the order of (block, warp, vector, lane).
 template <class T, bool SOLO, int RT>
-__global__ void __launch_bounds__(RT, RT == 512 ? 2 : 1)
+__global__ void __launch_bounds__(RT, 1024 / RT)
     k_sample_rows(int64_t rows, int64_t n, const T* __restrict__ logits, int64_t stride,
                   const uint64_t* __restrict__ words, erc_sample_rule rule, int C,
                   int32_t* __restrict__ ids, float* __restrict__ logp, int32_t* __restrict__ kept) {
@@ -1585,6 +1589,8 @@ erc_status launch_rows(int64_t rows, int64_t n, const T* logits, int64_t stride,
   int dev = 0;
   ERC_CUDA(cudaGetDevice(&dev));
   if (dev >= 64 || !(ready.load(std::memory_order_acquire) >> dev & 1)) {
+    ERC_CUDA(cudaFuncSetAttribute(k_sample_rows<T, true, 128>,
+                                  cudaFuncAttributeMaxDynamicSharedMemorySize, ring_bytes(128)));
     ERC_CUDA(cudaFuncSetAttribute(k_sample_rows<T, true, 512>,
                                   cudaFuncAttributeMaxDynamicSharedMemorySize, ring_bytes(512)));
     ERC_CUDA(cudaFuncSetAttribute(k_sample_rows<T, false, 512>,
@@ -1599,8 +1605,10 @@ erc_status launch_rows(int64_t rows, int64_t n, const T* logits, int64_t stride,
   }
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(rows < 65535 ? rows : 65535) * C);
-  cfg.blockDim = dim3(many ? 1024 : 512);
-  cfg.dynamicSmemBytes = ring_bytes(many ? 1024 : 512);
+  const bool small = C == 1 && n <= SMALL && rows > sm_count();
+  const int threads = small ? 128 : many ? 1024 : 512;
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = ring_bytes(threads);
   cfg.stream = s;
   cudaLaunchAttribute at = {};
   at.id = cudaLaunchAttributeClusterDimension;
@@ -1608,7 +1616,8 @@ erc_status launch_rows(int64_t rows, int64_t n, const T* logits, int64_t stride,
   at.val.clusterDim.y = at.val.clusterDim.z = 1;
   cfg.attrs = &at;
   cfg.numAttrs = C > 1;
-  auto kernel = C == 1 ? k_sample_rows<T, true, 512>
+  auto kernel = small    ? k_sample_rows<T, true, 128>
+                : C == 1 ? k_sample_rows<T, true, 512>
                 : many ? k_sample_rows<T, false, 1024>
                        : k_sample_rows<T, false, 512>;
   ERC_CUDA(cudaLaunchKernelEx(&cfg, kernel, rows, n, logits, stride, words, rule, C, ids, logp, kept));

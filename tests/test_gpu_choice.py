@@ -33,14 +33,14 @@ def per_row(v, i):
     return v[i].item() if isinstance(v, np.ndarray) else v
 
 
-def check_sample(logits, words, **rule):
-    """Draws of a device matrix against the oracle, row by row."""
+def check_sample(logits, words, every=1, **rule):
+    """Draws of a device matrix against the oracle, `every`-th row by row."""
     given = {k: torch.from_numpy(v).to(dev()) if isinstance(v, np.ndarray) else v for k, v in rule.items()}
     ids, logp, kept = erc.erc_sample_rows(logits, torch.from_numpy(words).to(dev()), **given)
     assert ids.dtype == torch.int32 and logp.dtype == torch.float32 and kept.dtype == torch.int32
     ids, logp, kept = host(ids), host(logp).astype(np.float64), host(kept)
     x = f32(logits)
-    for i in range(x.shape[0]):
+    for i in range(0, x.shape[0], every):
         want = C.sample_row(x[i], words[i], **{k: per_row(v, i) for k, v in rule.items()})
         assert (ids[i], kept[i]) == (want[0], len(want[2])), (i, ids[i], kept[i], want[0], len(want[2]))
         if want[0] < 0:
@@ -67,6 +67,20 @@ def test_sample_matches_oracle(n, rule):
     x[3] = -np.inf
     for kind in TYPES.values():
         check_sample(torch.from_numpy(x).to(dev()).to(kind), words_of(rng, rows), **rule)
+
+
+@pytest.mark.parametrize("rule", RULES, ids=str)
+@pytest.mark.parametrize("n", [1025, 4099, 16384])
+def test_sample_many_rows_of_middling_length(n, rule):
+    rng = np.random.default_rng(n)
+    rows = 320
+    x = rng.normal(size=(rows, n)).astype(np.float32) * np.linspace(0.3, 3, rows, dtype=np.float32)[:, None]
+    x[::5] = np.round(x[::5] * 2) / 2  # ties
+    x[15::40, n // 3:] = -np.inf
+    x[30] = -np.inf
+    x[45] = 0.0
+    for kind in TYPES.values():
+        check_sample(torch.from_numpy(x).to(dev()).to(kind), words_of(rng, rows), every=15, **rule)
 
 
 @pytest.mark.parametrize("n,rows", [(20000, 3), (70001, 3), (169343, 2), (400003, 2)])
