@@ -515,9 +515,26 @@ __global__ void __launch_bounds__(FW * 32)
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(t));
     return t > -41.5f ? e : 0.f;
   };
+  // the row's choices, one or more a lane: their loads start before the row's
+  int place[KL];
+  float s[KL], g[KL], chosen[KL];
+#pragma unroll
+  for (int i = 0; i < KL; ++i) {
+    const int c = at + i * L;
+    place[i] = c < k && live ? __ldg(experts + row * k + c) : -1;
+    g[i] = c < k && live ? __ldg(dweights + row * k + c) * rule.scale : 0.f;
+  }
   float v[V], m = 0.f, inv = 0.f;
+  if (!SIGMOID) load_scores<T, V>(x, first, E, wide, live, v);
+#pragma unroll
+  for (int i = 0; i < KL; ++i) {
+    if (place[i] < 0 || place[i] >= E) {
+      place[i] = -1;
+      g[i] = 0.f;
+    }
+    chosen[i] = place[i] >= 0 ? clean_score(to_f32(x[place[i]])) : -INFINITY;
+  }
   if (!SIGMOID) {
-    load_scores<T, V>(x, first, E, wide, live, v);
     m = v[0];
 #pragma unroll
     for (int j = 1; j < V; ++j) m = fmaxf(m, v[j]);
@@ -532,29 +549,17 @@ __global__ void __launch_bounds__(FW * 32)
     z = lanes_sum<L>(z);
     inv = z > 0.f ? __frcp_rn(z) : 0.f;
   }
-  // the row's choices, one or more a lane
-  int place[KL];
-  float s[KL], g[KL], D = 0.f;
+  float D = 0.f;
 #pragma unroll
   for (int i = 0; i < KL; ++i) {
-    const int c = at + i * L;
-    place[i] = -1;
-    s[i] = g[i] = 0.f;
-    if (c < k && live) {
-      const int e = experts[row * k + c];
-      if (e >= 0 && e < E) {
-        place[i] = e;
-        g[i] = dweights[row * k + c] * rule.scale;
-        const float l = clean_score(to_f32(x[e]));
-        if (l == -INFINITY)
-          s[i] = 0.f;
-        else if (SIGMOID) {
-          const float q = pow2_float(-__fmul_rn(fabsf(l), LOG2E), -126.f);
-          s[i] = __fdiv_rn(l >= 0.f ? 1.f : q, 1.f + q);
-        } else {
-          s[i] = power(below_max(l, m, LOG2E)) * inv;
-        }
-      }
+    const float l = chosen[i];
+    if (l == -INFINITY) {
+      s[i] = 0.f;
+    } else if (SIGMOID) {
+      const float q = pow2_float(-__fmul_rn(fabsf(l), LOG2E), -126.f);
+      s[i] = __fdiv_rn(l >= 0.f ? 1.f : q, 1.f + q);
+    } else {
+      s[i] = power(below_max(l, m, LOG2E)) * inv;
     }
     D += s[i];
   }

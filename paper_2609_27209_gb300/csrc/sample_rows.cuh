@@ -1396,8 +1396,8 @@ int blocks_of(int64_t rows, int64_t n) {
 // ------------------------------------------------------------------------------------------------
 // short rows: a warp takes a row, `q` consecutive entries a lane (odd: no bank conflicts)
 // ------------------------------------------------------------------------------------------------
-constexpr int SW = 8;          // warps of a block
-constexpr int SHORT = 1024;    // longest row
+constexpr int SW = 4;          // warps of a block
+constexpr int SHORT = 1536;    // longest row (2000 entries: a block of 128 threads is faster)
 inline int short_q(int64_t n) { return (int)((n + 31) / 32) | 1; }
 
 __device__ __forceinline__ unsigned long long warp_sum(unsigned long long v) {
@@ -1432,27 +1432,142 @@ __device__ __forceinline__ unsigned largest_key(unsigned floor, unsigned top,
   return key;
 }
 
+constexpr int SBINS = 256;  // bins of a warp's histogram, six an octave of the weights
+
+// A warp's row: its entries' keys (0: not eligible), `q` consecutive ones a lane, and 2^t of each.
+struct ShortRow {
+  unsigned* keys;
+  const float* powers;  // only where entries are weighed
+  unsigned* bins;       // 2 SBINS
+  unsigned* list;       // 32
+  int q;
+  float best, scale;  // the row's maximum and log2(e) / T
+
+  __device__ __forceinline__ int bin(unsigned key) const {
+    const float t = below_max(order_value(key), best, scale);
+    return min((int)(__float_as_uint(__fmaf_rz(t, -6.f, 8388608.f)) - BIAS), SBINS - 1);
+  }
+  __device__ __forceinline__ unsigned long long weight(int i) const {
+    unsigned hi[2], lo[2];
+    split_weights(pair(powers[i], powers[i]), hi, lo);
+    return join_parts(hi[0], lo[0]);
+  }
+  // The key at which the running count (MASS: weight) over the keys above `below`, largest first,
+  // reaches `left`, which it does; `left` becomes what is still wanted from the entries at that
+  // key.  A histogram gives the bin, and the bin's entries, one a lane, the key; more than 32 of them
+  // are searched bit by bit.  A bin's parts of weights are sums of at most 2048: 32 bits hold them.
+  template <bool MASS>
+  __device__ unsigned find(unsigned below, unsigned long long& left) const {
+    const int lane = threadIdx.x & 31;
+    constexpr int P = SBINS / 32;
+    for (int b = lane; b < (MASS ? 2 : 1) * SBINS; b += 32) bins[b] = 0;
+    __syncwarp();
+    for (int i = lane * q; i < (lane + 1) * q; ++i) {
+      const unsigned k = keys[i];
+      if (k <= below) continue;
+      const int b = bin(k);
+      if (MASS) {
+        unsigned hi[2], lo[2];
+        split_weights(pair(powers[i], powers[i]), hi, lo);
+        atomicAdd(&bins[b], hi[0] - BIAS);
+        atomicAdd(&bins[SBINS + b], lo[0] - BIAS);
+      } else {
+        atomicAdd(&bins[b], 1u);
+      }
+    }
+    __syncwarp();
+    unsigned long long v[P], sum = 0;
+#pragma unroll
+    for (int j = 0; j < P; ++j) {
+      v[j] = bins[lane * P + j];
+      if (MASS) v[j] = (v[j] << 20) + bins[SBINS + lane * P + j];
+      sum += v[j];
+    }
+    unsigned long long before = warp_inclusive(sum) - sum, rest = 0;
+    int mine = -1;
+#pragma unroll
+    for (int j = 0; j < P; ++j) {
+      if (before < left && left <= before + v[j]) {
+        mine = lane * P + j;
+        rest = left - before;
+      }
+      before += v[j];
+    }
+    const int owner = __ffs(__ballot_sync(0xffffffffu, mine >= 0)) - 1;
+    const int at = __shfl_sync(0xffffffffu, mine, owner);
+    left = __shfl_sync(0xffffffffu, rest, owner);
+    // the bin's entries
+    unsigned number = 0, low = 0xffffffffu, high = 0;
+    for (int i = lane * q; i < (lane + 1) * q; ++i) {
+      const unsigned k = keys[i];
+      const bool in = k > below && bin(k) == at;
+      const unsigned who = __ballot_sync(0xffffffffu, in);
+      const unsigned p = number + __popc(who & ((1u << lane) - 1));
+      if (in) {
+        if (p < 32) list[p] = i;
+        low = min(low, k);
+        high = max(high, k);
+      }
+      number += __popc(who);
+    }
+    __syncwarp();
+    if (number <= 32) {
+      const int i = (unsigned)lane < number ? (int)list[lane] : -1;
+      const unsigned k = i >= 0 ? keys[i] : 0u;
+      const unsigned long long w = i >= 0 ? (MASS ? weight(i) : 1ull) : 0ull;
+      unsigned long long over = 0, same = 0;
+      for (unsigned j = 0; j < number; ++j) {
+        const unsigned ok = __shfl_sync(0xffffffffu, k, j);
+        const unsigned long long ow = __shfl_sync(0xffffffffu, w, j);
+        if (ok > k) over += ow;
+        if (ok == k) same += ow;
+      }
+      const bool hit = i >= 0 && over < left && left <= over + same;
+      const int who = __ffs(__ballot_sync(0xffffffffu, hit)) - 1;
+      left -= __shfl_sync(0xffffffffu, over, who);
+      return __shfl_sync(0xffffffffu, k, who);
+    }
+    low = __reduce_min_sync(0xffffffffu, low);
+    high = __reduce_max_sync(0xffffffffu, high);
+    auto sum_from = [&](unsigned from) {
+      unsigned long long some = 0;
+      for (int i = lane * q; i < (lane + 1) * q; ++i)
+        if (keys[i] >= from && keys[i] <= high) some += MASS ? weight(i) : 1ull;
+      return warp_sum(some);
+    };
+    const unsigned key = largest_key(low, high, left, sum_from);
+    if (key < high) left -= sum_from(key + 1);
+    return key;
+  }
+};
+// words of a warp's shared memory: keys, 2^t where weights are needed, bins and list where entries may
+// be filtered
+__host__ __device__ inline int short_words(int q, bool mass, bool filters) {
+  return q * 32 * (mass ? 2 : 1) + (filters ? 2 * SBINS + 32 : 0);
+}
+
 template <class T, bool MASS>
 __global__ void __launch_bounds__(SW * 32)
-    k_sample_short(int64_t rows, int n, int q, const T* __restrict__ logits, int64_t stride,
+    k_sample_short(int64_t rows, int n, int q, bool filters, const T* __restrict__ logits, int64_t stride,
                    const uint64_t* __restrict__ words, erc_sample_rule rule,
                    int32_t* __restrict__ ids, float* __restrict__ logp,
                    int32_t* __restrict__ kept) {
-  extern __shared__ uint64_t short_buffer[];
+  extern __shared__ unsigned short_buffer[];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  uint64_t* weights = short_buffer + (MASS ? warp * q * 32 : 0);  // MASS only
-  unsigned* keys = reinterpret_cast<unsigned*>(short_buffer + (MASS ? SW * q * 32 : 0)) + warp * q * 32;
+  unsigned* keys = short_buffer + warp * short_words(q, MASS, filters);
+  float* powers = reinterpret_cast<float*>(keys + q * 32);  // MASS only
+  unsigned* bins = keys + (MASS ? 2 : 1) * q * 32;
   for (int64_t row = (int64_t)blockIdx.x * SW + warp; row < rows; row += (int64_t)gridDim.x * SW) {
     const T* x = logits + row * stride;
     const RowRule r = row_rule(rule, row);
     float m = -INFINITY;
+#pragma unroll 4
     for (int i = lane; i < q * 32; i += 32) {
       const float l = i < n ? clean_score(to_f32(x[i])) : -INFINITY;
       m = fmaxf(m, l);
       keys[i] = __float_as_uint(l);
     }
-    const unsigned top = __reduce_max_sync(0xffffffffu, order_key(__fadd_rn(m, 0.f)));
-    m = order_value(top);
+    m = order_value(__reduce_max_sync(0xffffffffu, order_key(__fadd_rn(m, 0.f))));
     if (m == -INFINITY) {
       if (lane == 0) {
         ids[row] = -1;
@@ -1462,71 +1577,71 @@ __global__ void __launch_bounds__(SW * 32)
       __syncwarp();
       continue;
     }
+    const ShortRow sr = {keys, powers, bins, bins + 2 * SBINS, q, m, r.scale};
     const float least_t = r.least <= 1 ? -41.5f : log2f((float)r.least - 0.5f) - 40.01f;
     __syncwarp();
-    // a lane's own entries: keys (0: not eligible) and their weights
+    // a lane's own entries
     unsigned* mine = keys + lane * q;
     unsigned long long mass = 0;
-    unsigned above = 0, low = 0xffffffffu;
+    unsigned above = 0;
     for (int i = 0; i < q; ++i) {
       const float l = __uint_as_float(mine[i]);
       const float t = l == -INFINITY ? -INFINITY : below_max(l, m, r.scale);
       unsigned long long w = 0;
+      float v = 0.f;
       if (t >= least_t) {
-        w = fixed_weight(t);
+        v = t > -41.5f ? pow2_float(t, -41.f) : 0.f;
+        unsigned hi[2], lo[2];
+        split_weights(pair(v, v), hi, lo);
+        w = join_parts(hi[0], lo[0]);
         if (w < r.least) w = 0;
       }
-      const unsigned k = w ? order_key(l) : 0u;
-      mine[i] = k;
-      if (MASS) weights[lane * q + i] = w;
+      mine[i] = w ? order_key(l) : 0u;
+      if (MASS) powers[lane * q + i] = v;
       mass += w;
       above += w != 0;
-      if (w) low = min(low, k);
     }
+    __syncwarp();
     auto weight_of = [&](unsigned k) {
       return k ? fixed_weight(below_max(order_value(k), m, r.scale)) : 0ull;
     };
     unsigned theta = 0, ties = 0xffffffffu, tied = 0;
     unsigned number = __reduce_add_sync(0xffffffffu, above);
-    const bool by_k = r.top_k < number;
-    if (by_k || (MASS && r.part != 0xffffffffu)) {
-      low = __reduce_min_sync(0xffffffffu, low);
-      auto count = [&](unsigned k) {
-        unsigned c = 0;
-        for (int i = 0; i < q; ++i) c += mine[i] >= k;
-        return __reduce_add_sync(0xffffffffu, c);
-      };
-      auto mass_of = [&](unsigned k) {
-        unsigned long long s = 0;
-        for (int i = 0; i < q; ++i)
-          if (mine[i] >= k) s += weights[lane * q + i];
-        return warp_sum(s);
-      };
+    const bool by_k = r.top_k < number, by_p = MASS && r.part != 0xffffffffu;
+    if (by_k) {
+      unsigned long long left = r.top_k;
+      theta = sr.find<false>(0u, left);
+      ties = (unsigned)left;
+      number = r.top_k;
+    }
+    if (by_p) {
+      unsigned long long over = mass;
       if (by_k) {
-        theta = largest_key(low, top, r.top_k, [&](unsigned k) { return (unsigned long long)count(k); });
-        ties = r.top_k - (theta == 0xffffffffu ? 0u : count(theta + 1));
-        number = r.top_k;
+        over = 0;
+        for (int i = 0; i < q; ++i)
+          if (mine[i] > theta) over += sr.weight(lane * q + i);
       }
-      if (MASS && r.part != 0xffffffffu) {
-        const unsigned long long wt = by_k ? weight_of(theta) : 0ull;
-        const unsigned long long over = by_k ? mass_of(theta + 1) : warp_sum(mass);
-        const unsigned long long total = over + (by_k ? ties * wt : 0ull);
-        unsigned long long target =
-            (total >> 31) * r.part + (((total & 0x7fffffffull) * r.part) >> 31);
-        if (!target) target = 1;
-        if (over < target) {
-          ties = (unsigned)((target - over + wt - 1) / wt);
-        } else {
-          theta = largest_key(by_k ? theta + 1 : low, top, target, mass_of);
-          const unsigned long long more = mass_of(theta + 1), w = weight_of(theta);
-          ties = (unsigned)((target - more + w - 1) / w);
-        }
-        number = count(theta + 1) + ties;
+      over = warp_sum(over);
+      const unsigned long long wt = weight_of(theta);
+      const unsigned long long total = over + (by_k ? ties * wt : 0ull);
+      unsigned long long target = (total >> 31) * r.part + (((total & 0x7fffffffull) * r.part) >> 31);
+      if (!target) target = 1;
+      if (over < target) {
+        ties = (unsigned)((target - over + wt - 1) / wt);
+      } else {
+        theta = sr.find<MASS>(theta, target);
+        const unsigned long long w = weight_of(theta);
+        ties = (unsigned)((target + w - 1) / w);
       }
+      number = 0;
+      for (int i = 0; i < q; ++i) number += mine[i] > theta;
+      number = __reduce_add_sync(0xffffffffu, number) + ties;
+    }
+    if (by_k || by_p) {
       mass = 0;
       const unsigned long long wt = weight_of(theta);
       for (int i = 0; i < q; ++i) {
-        if (mine[i] > theta) mass += MASS ? weights[lane * q + i] : weight_of(mine[i]);
+        if (mine[i] > theta) mass += MASS ? sr.weight(lane * q + i) : weight_of(mine[i]);
         tied += mine[i] == theta;
       }
       const unsigned earlier = warp_inclusive(tied) - tied;
@@ -1539,11 +1654,11 @@ __global__ void __launch_bounds__(SW * 32)
     const int owner = 31 - __clz(__ballot_sync(0xffffffffu, to - mass <= at && mass));
     unsigned long long before = __shfl_sync(0xffffffffu, to - mass, owner);
     unsigned left = __shfl_sync(0xffffffffu, tied, owner);  // ties of the owner's that are kept
-    __syncwarp();
     for (int i0 = 0; i0 < q; i0 += 32) {  // the owner's entries, one a lane
       const unsigned k = i0 + lane < q ? keys[owner * q + i0 + lane] : 0u;
       const bool tie = theta && k == theta;
-      const unsigned earlier = __popc(__ballot_sync(0xffffffffu, tie) & ((1u << lane) - 1));
+      const unsigned tie_lanes = __ballot_sync(0xffffffffu, tie);
+      const unsigned earlier = __popc(tie_lanes & ((1u << lane) - 1));
       const unsigned long long w = k > theta || (tie && earlier < left) ? weight_of(k) : 0ull;
       const unsigned long long in = before + warp_inclusive(w);
       if (at < in && in - w <= at) {
@@ -1553,7 +1668,7 @@ __global__ void __launch_bounds__(SW * 32)
         logp[row] = w > rest ? log1pf(-__fdiv_rn(__ull2float_rn(rest), __ull2float_rn(total)))
                              : logf(__fdiv_rn(__ull2float_rn(w), __ull2float_rn(total)));
       }
-      left -= min(left, (unsigned)__popc(__ballot_sync(0xffffffffu, tie)));
+      left -= min(left, (unsigned)__popc(tie_lanes));
       before = __shfl_sync(0xffffffffu, in, 31);
     }
     __syncwarp();
@@ -1567,16 +1682,19 @@ template <class T>
 erc_status launch_rows(int64_t rows, int64_t n, const T* logits, int64_t stride,
                        const uint64_t* words, const erc_sample_rule& rule, int32_t* ids,
                        float* logp, int32_t* kept, cudaStream_t s) {
-  if (n <= SHORT) {
+  // a warp a row, but a whole block for few rows (1 x 1000, top-k: 27 us by a warp, 19 by a block)
+  if (n <= 256 || (n <= SHORT && rows > 2 * sm_count())) {
     const int q = short_q(n);
     const bool mass = rule.top_p < 1.f || rule.top_p_rows;
-    const size_t bytes = (size_t)SW * q * 32 * (mass ? 12 : 4);
+    const bool filters = mass || rule.top_k > 0 || rule.top_k_rows || !(rule.temperature > 0.f) ||
+                         rule.temperature_rows;
+    const size_t bytes = (size_t)SW * short_words(q, mass, filters) * 4;
     auto kernel = mass ? k_sample_short<T, true> : k_sample_short<T, false>;
     if (bytes > 48 * 1024)
       ERC_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes));
     const int64_t blocks = (rows + SW - 1) / SW;
     kernel<<<(unsigned)(blocks < 0x7fffffff ? blocks : 0x7fffffff), SW * 32, bytes, s>>>(
-        rows, (int)n, q, logits, stride, words, rule, ids, logp, kept);
+        rows, (int)n, q, filters, logits, stride, words, rule, ids, logp, kept);
     count_launches(1);
     ERC_CUDA(cudaGetLastError());
     return ERC_OK;

@@ -223,6 +223,14 @@ def test_sample_on_another_stream_and_twice():
         assert torch.equal(u, v)
 
 
+def test_sample_more_rows_than_a_grid():
+    rng = np.random.default_rng(13)
+    n, rows = 2100, 70001
+    base = torch.from_numpy(rng.normal(size=n + rows).astype(np.float32)).to(dev()).to(torch.bfloat16)
+    x = base.as_strided((rows, n), (1, 1))  # row i starts at entry i
+    check_sample(x, words_of(rng, rows), every=7777, top_p=0.9)
+
+
 def test_sample_draws_follow_the_probabilities():
     x = np.array([0.0, 1.0, 2.0, -1.0], np.float32)
     rows = 1 << 16
