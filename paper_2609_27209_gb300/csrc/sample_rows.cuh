@@ -118,6 +118,42 @@ __device__ __forceinline__ V block_exclusive(V v, V (&part)[RW], V* total) {
   return (warp ? base : V(0)) + x - v;
 }
 
+// The same for several values of each thread, in the order (value, thread); v becomes the sums before.
+template <class V, int SEG, int RW>
+__device__ __forceinline__ V block_exclusive(V (&v)[SEG], V (&part)[SEG][RW]) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  V x[SEG];
+#pragma unroll
+  for (int g = 0; g < SEG; ++g) {
+    x[g] = v[g];
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const V y = __shfl_up_sync(0xffffffffu, x[g], o);
+      if (lane >= o) x[g] += y;
+    }
+  }
+  __syncthreads();
+  if (lane == 31) {
+#pragma unroll
+    for (int g = 0; g < SEG; ++g) part[g][warp] = x[g];
+  }
+  __syncthreads();
+  V run = 0;
+#pragma unroll
+  for (int g = 0; g < SEG; ++g) {
+    V s = lane < RW ? part[g][lane] : V(0);
+#pragma unroll
+    for (int o = 1; o < RW; o <<= 1) {
+      const V y = __shfl_up_sync(0xffffffffu, s, o);
+      if (lane >= o) s += y;
+    }
+    const V base = __shfl_sync(0xffffffffu, s, warp ? warp - 1 : 0);
+    v[g] = run + (warp ? base : V(0)) + x[g] - v[g];
+    run += __shfl_sync(0xffffffffu, s, RW - 1);
+  }
+  return run;
+}
+
 struct Part {  // what a stretch of the row holds: mass and number above theta, entries at theta
   unsigned long long mass;
   unsigned above, tied;
@@ -147,6 +183,9 @@ struct Shared {
   unsigned first_bin, last_bin;  // of the weights' histogram
   unsigned long long over;    // a level's sum before that bin
   unsigned odd;               // entries that the code table has no place for
+  static constexpr int SEG = LARGE ? CODES / (4 * RT) : 1;  // fours of places of a thread
+  unsigned long long seg64[SEG][RW];
+  unsigned seg32[SEG][RW];
   union {
     struct {
       union {
@@ -911,8 +950,8 @@ __device__ bool tally(S& s, const Row<T>& r, const RowRule& rule, const Team<SOL
 // ------------------------------------------------------------------------------------------------
 // The 16 bits of a score say its weight, so one pass that counts the row's entries by code holds all
 // that the filters need: a place of the table for every magnitude in [2^-24, 2^7) of either sign, and
-// for 0, in descending order of the scores.  Each thread takes 16 places, weighs those that have
-// entries, and running sums over the threads give theta and its ties exactly.  A second pass adds up
+// for 0, in descending order of the scores.  Each thread takes fours of places, weighs those that
+// have entries, and running sums over the threads give theta and its ties exactly.  A second pass adds up
 // the kept weights of each region, read from the table (as 2^t, whose parts give the integer).
 // Returns 1, or 0 for a row with nothing to draw, or -1 where entries without a place of their own
 // could change the result.
@@ -939,7 +978,7 @@ template <class T, bool SOLO, class S>
 __device__ int by_codes(S& s, Row<T>& r, const RowRule& rule, const Team<SOLO>& team,
                         float& theta, unsigned& ties, Measured& m) {
   constexpr int RT = S::RT;
-  constexpr int P = CODES / RT;
+  constexpr int SEG = S::SEG, P = 4 * SEG;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   for (int b = tid; b < CODES; b += RT) s.codes[b] = 0;
   if (tid == 0) {
@@ -949,6 +988,7 @@ __device__ int by_codes(S& s, Row<T>& r, const RowRule& rule, const Team<SOLO>& 
     s.some = 0;
   }
   __syncthreads();
+  auto place_of = [&](int i) { return (i / 4) * 4 * RT + tid * 4 + i % 4; };  // ascending in i
   const unsigned table = (unsigned)__cvta_generic_to_shared(s.codes);
   bool odd = false, tiny = false;
   each_vector(r, r.begin(warp), r.end(warp), [&](uint4 u) {
@@ -979,7 +1019,7 @@ __device__ int by_codes(S& s, Row<T>& r, const RowRule& rule, const Team<SOLO>& 
   for (int c = 0; c < team.size(); ++c)
 #pragma unroll
     for (int i = 0; i < P; i += 4) {
-      const uint4 q = team.load(reinterpret_cast<const uint4*>(&s.codes[tid * P + i]), c);
+      const uint4 q = team.load(reinterpret_cast<const uint4*>(&s.codes[place_of(i)]), c);
       count[i] += q.x;
       count[i + 1] += q.y;
       count[i + 2] += q.z;
@@ -988,7 +1028,7 @@ __device__ int by_codes(S& s, Row<T>& r, const RowRule& rule, const Team<SOLO>& 
   unsigned first = CODES;
 #pragma unroll
   for (int i = P - 1; i >= 0; --i)
-    if (count[i]) first = tid * P + i;
+    if (count[i]) first = place_of(i);
   first = __reduce_min_sync(0xffffffffu, first);
   if (lane == 0) atomicMin(&s.top, first);
   team.barrier();  // the counts have been read everywhere
@@ -1009,36 +1049,39 @@ __device__ int by_codes(S& s, Row<T>& r, const RowRule& rule, const Team<SOLO>& 
     split_weights(pair(x, x), hi, lo);
     return join_parts(hi[0], lo[0]);
   };
-  unsigned entries = 0, all;
+  unsigned entries[SEG] = {};
 #pragma unroll
   for (int i = 0; i < P; ++i)
     if (count[i]) {
-      const float t = r.scaled(place_value(tid * P + i));
+      const float t = r.scaled(place_value(place_of(i)));
       v[i] = t > -41.5f ? pow2_float(t, -41.f) : 0.f;
       if (weight(v[i]) < r.least) count[i] = 0;
-      entries += count[i];
+      entries[i / 4] += count[i];
     }
-  const unsigned entries_before = block_exclusive(entries, s.part32, &all);
+  block_exclusive(entries, s.seg32);
   auto left_by_k = [&](unsigned before, unsigned n) {
     return before < rule.top_k ? min(n, rule.top_k - before) : 0u;
   };
-  unsigned before = entries_before;
-  unsigned long long mass = 0, total;
+  unsigned long long mass[SEG] = {};
 #pragma unroll
   for (int i = 0; i < P; ++i) {
-    if (count[i]) mass += left_by_k(before, count[i]) * weight(v[i]);
+    unsigned& before = entries[i / 4];
+    if (count[i]) mass[i / 4] += left_by_k(before, count[i]) * weight(v[i]);
     before += count[i];
   }
-  unsigned long long mass_before = block_exclusive(mass, s.part64, &total);
+  const unsigned long long total = block_exclusive(mass, s.seg64);
   unsigned long long target = ~0ull;
   if (rule.part != 0xffffffffu) {
     target = (total >> 31) * rule.part + (((total & 0x7fffffffull) * rule.part) >> 31);
     if (!target) target = 1;
   }
   unsigned number = 0, last = 0;
-  before = entries_before;
 #pragma unroll
   for (int i = 0; i < P; ++i) {
+    if (i % 4 == 0)  // back to the sums before the four places
+      entries[i / 4] -= count[i] + count[i + 1] + count[i + 2] + count[i + 3];
+    unsigned& before = entries[i / 4];
+    unsigned long long& mass_before = mass[i / 4];
     const unsigned n = left_by_k(before, count[i]);
     float keep = 0.f;
     if (n && mass_before < target) {
@@ -1050,11 +1093,11 @@ __device__ int by_codes(S& s, Row<T>& r, const RowRule& rule, const Team<SOLO>& 
       else
         keep = v[i];
       number += kept;
-      last = tid * P + i;
+      last = place_of(i);
       mass_before += n * w;
     }
     before += count[i];
-    s.codes[tid * P + i] = __float_as_uint(keep);
+    s.codes[place_of(i)] = __float_as_uint(keep);
   }
   last = __reduce_max_sync(0xffffffffu, last);
   if (lane == 0) atomicMax(&s.last_bin, last);
