@@ -93,8 +93,8 @@ uint64_t erc_kernel_launches(void);
  * its status (the outputs are then undefined).  `polls` sets the number of polls every such
  * wait makes before it gives up, for all later calls of the process; 0 (the initial state)
  * restores each wait's default, which is seconds of waiting.  Waits of work already enqueued keep
- * the limit they were enqueued with.  The hardware cluster barriers of the cluster CG solver are
- * not polled and take no limit. */
+ * the limit they were enqueued with.  The hardware cluster barriers of the cluster CG solver and of
+ * erc_sample_rows are not polled and take no limit. */
 void erc_set_wait_limit(uint32_t polls);
 
 /* ---------------------------------------------------------------------------------------------

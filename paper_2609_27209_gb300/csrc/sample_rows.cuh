@@ -167,6 +167,7 @@ struct Shared {
   static constexpr bool LARGE = THREADS > 128;
   static constexpr int LIST = LARGE ? 8192 : 2048;   // candidates listed in a block's memory
   static constexpr int RANK = LARGE ? 4096 : 1024;   // candidates of a row that one block ranks
+  static constexpr int TINY = LARGE ? 256 : 128;     // candidates drawn from one a thread
   static constexpr int BIN_BITS = LARGE ? 10 : 9;    // of the bins of one level of the descent
   static constexpr int BINS = 1 << BIN_BITS;
   static constexpr int STEPS = LARGE ? 128 : 16;     // bins an octave of the weights' histogram
@@ -237,7 +238,7 @@ struct Row {
   }
 };
 
-// f(vector) for vectors [from, to) of the row, 32 at a time (lanes past the end get masked vectors).
+// f(vector, its number) for vectors [from, to) of the row, 32 at a time (lanes past the end get masked vectors).
 // Each lane's vectors arrive in the warp's ring of shared memory, DEPTH - 1 ahead, and are read by
 // that lane alone.
 template <class T, class F>
@@ -248,7 +249,7 @@ __device__ __forceinline__ void each_vector(const Row<T>& r, int from, int to, F
     return make_uint4(w, w, w, w);
   };
   if (from == 0 && r.view.skew) {  // the first vector is shared with the row before
-    f(lane < to ? r.view.fetch(lane) : masked());
+    f(lane < to ? r.view.fetch(lane) : masked(), lane);
     from = 32;
   }
   const int whole = min(to, r.view.whole());  // vectors up to here are the row's own
@@ -272,7 +273,7 @@ __device__ __forceinline__ void each_vector(const Row<T>& r, int from, int to, F
       u = *reinterpret_cast<const uint4*>(reinterpret_cast<const char*>(mine) + stage);
     else
       u = base + lane < to ? r.view.fetch(base + lane) : masked();
-    f(u);
+    f(u, base + lane);
     last = stage;
     stage = stage == (DEPTH - 1) * 512 ? 0 : stage + 512;
   }
@@ -287,7 +288,7 @@ __device__ Part measure(const Row<T>& r, int from, int to, float theta) {
   unsigned hi = 0, lo = 0, parts = 0;
   if (r.least == 1 && theta == -INFINITY && !r.odd) {
     const uint64_t m2 = pair(-r.max, -r.max), s2 = pair(r.scale, r.scale);
-    each_vector(r, from, to, [&](uint4 u) {
+    each_vector(r, from, to, [&](uint4 u, int) {
       uint64_t l[N / 2];
       unpack_pairs<T>(u, l);
 #pragma unroll
@@ -303,7 +304,7 @@ __device__ Part measure(const Row<T>& r, int from, int to, float theta) {
       parts += N;
     });
   } else {
-    each_vector(r, from, to, [&](uint4 u) {
+    each_vector(r, from, to, [&](uint4 u, int) {
       const float best = max_score(u, T());
       if (!(best >= theta) || !(r.scaled(best) >= r.tmin)) return;
       float l[N];
@@ -401,7 +402,7 @@ __device__ __forceinline__ void each_score(const S& s, const Row<T>& r, float fl
     }
     return;
   }
-  each_vector(r, r.begin(warp), r.end(warp), [&](uint4 u) {
+  each_vector(r, r.begin(warp), r.end(warp), [&](uint4 u, int) {
     if (max_score(u, T()) >= floor) {
       float l[N];
       r.scores(u, l);
@@ -498,21 +499,87 @@ __device__ bool descend(S& s, const Row<T>& r, const Team<SOLO>& team, unsigned 
   }
 }
 
-// Ranks at most RANK candidates in block 0: top-k, then top-p, to (theta, ties).  Returns false,
-// with nothing decided, where there are more.  Candidates are the eligible entries whose distance
-// from the maximum is below `reach` (all of them: reach = inf).
+struct RowOut {  // where a row's result goes, and its word
+  uint64_t word;
+  int32_t* id;
+  float* logp;
+  int32_t* kept;
+  __device__ __forceinline__ void set(int index, unsigned long long w, unsigned long long total,
+                                      unsigned number) const {
+    const unsigned long long rest = total - w;
+    *id = index;
+    *kept = (int32_t)number;
+    *logp = w > rest ? log1pf(-__fdiv_rn(__ull2float_rn(rest), __ull2float_rn(total)))
+                     : logf(__fdiv_rn(__ull2float_rn(w), __ull2float_rn(total)));
+  }
+  __device__ __forceinline__ void none() const {
+    *id = -1;
+    *logp = -INFINITY;
+    *kept = 0;
+  }
+};
+
+// The draw from at most TINY candidates, one a thread: ranked by counting, filtered in that order,
+// and drawn by counting again in the order of their indices.
+template <class T, class S>
+__device__ void draw_tiny(S& s, const Row<T>& r, const RowRule& rule, unsigned all,
+                          const RowOut& out) {
+  const unsigned tid = threadIdx.x;
+  unsigned long long* order = reinterpret_cast<unsigned long long*>(s.wbins);  // (key, ~index)
+  unsigned long long* weights = order + S::TINY;                              // by rank
+  unsigned* index = reinterpret_cast<unsigned*>(weights + S::TINY);
+  const unsigned mine = tid < all ? s.list[S::RANK + tid] : 0u;
+  const unsigned long long own =
+      tid < all ? (unsigned long long)s.list[tid] << 32 | (0xffffffffu - mine) : 0ull;
+  if (tid < all) order[tid] = own;
+  __syncthreads();
+  if (tid < all) {
+    unsigned rank = 0;
+    for (unsigned j = 0; j < all; ++j) rank += order[j] > own;
+    weights[rank] = r.weight(order_value((unsigned)(own >> 32)));
+    index[rank] = mine;
+  }
+  __syncthreads();
+  const unsigned keep = min(all, rule.top_k);
+  const unsigned long long w = tid < keep ? weights[tid] : 0ull;
+  unsigned long long total;
+  const unsigned long long before = block_exclusive(w, s.part64, &total);
+  unsigned long long target = ~0ull;
+  if (rule.part != 0xffffffffu) {
+    target = (total >> 31) * rule.part + (((total & 0x7fffffffull) * rule.part) >> 31);
+    if (!target) target = 1;
+  }
+  const bool in = w && before < target;
+  const unsigned number = __syncthreads_count(in);  // the first `number` ranks
+  if (in && tid == number - 1) s.over = before + w;
+  __syncthreads();
+  if (in) {
+    const unsigned long long at = __umul64hi(out.word, s.over);
+    unsigned long long earlier = 0;
+    const unsigned here = index[tid];
+    for (unsigned j = 0; j < number; ++j)
+      if (index[j] < here) earlier += weights[j];
+    if (at >= earlier && at - earlier < w) out.set((int)here, w, s.over, number);
+  }
+}
+
+// Ranks at most RANK candidates in block 0: top-k, then top-p, to (theta, ties).  Candidates are the
+// eligible entries whose distance from the maximum is below `reach` (all of them: reach = inf).
+// At most TINY of them are drawn from right there, which ends the row.
+enum Ranked { TOO_MANY, RANKED, DRAWN };
 template <class T, bool SOLO, class S>
-__device__ bool rank_list(S& s, const Row<T>& r, const RowRule& rule,
-                          const Team<SOLO>& team, float inv, float reach, float& theta,
-                          unsigned& ties) {
+__device__ Ranked rank_list(S& s, const Row<T>& r, const RowRule& rule, const Team<SOLO>& team,
+                            float inv, float reach, float& theta, unsigned& ties,
+                            const RowOut& out) {
   constexpr int RT = S::RT;
+  constexpr int N = Row<T>::N;
   const int C = team.size();
   const unsigned rank = team.rank;
-  constexpr int N = Row<T>::N;
   const int tid = threadIdx.x, warp = tid >> 5;
+  unsigned* index = s.list + S::RANK;  // of the candidates
   if (tid == 0) s.number = 0;
   __syncthreads();
-  each_vector(r, r.begin(warp), r.end(warp), [&](uint4 u) {
+  each_vector(r, r.begin(warp), r.end(warp), [&](uint4 u, int at) {
     const float best = max_score(u, T());
     if (!(__fmul_rn(__fsub_rn(r.max, best), inv) < reach)) return;
     float l[N];
@@ -521,7 +588,10 @@ __device__ bool rank_list(S& s, const Row<T>& r, const RowRule& rule,
     for (int i = 0; i < N; ++i)
       if (__fmul_rn(__fsub_rn(r.max, l[i]), inv) < reach && r.eligible(l[i])) {
         const unsigned p = atomicAdd(&s.number, 1u);
-        if (p < S::RANK) s.list[p] = order_key(__fadd_rn(l[i], 0.f));
+        if (p < S::RANK) {
+          s.list[p] = order_key(__fadd_rn(l[i], 0.f));
+          index[p] = at * N - r.view.skew + i;
+        }
       }
   });
   team.barrier();
@@ -533,15 +603,25 @@ __device__ bool rank_list(S& s, const Row<T>& r, const RowRule& rule,
   }
   if (all > S::RANK) {
     team.barrier();
-    return false;
+    return TOO_MANY;
   }
   if (rank == 0) {
     unsigned at = mine;
     for (int c = 1; c < C; ++c) {
       const unsigned q = team.load(&s.number, c);
-      for (unsigned i = tid; i < q; i += RT) s.list[at + i] = team.load(&s.list[i], c);
+      for (unsigned i = tid; i < q; i += RT) {
+        s.list[at + i] = team.load(&s.list[i], c);
+        index[at + i] = team.load(&index[i], c);
+      }
       at += q;
     }
+    __syncthreads();
+  }
+  if (all <= S::TINY) {
+    if (rank == 0) draw_tiny(s, r, rule, all, out);
+    return DRAWN;
+  }
+  if (rank == 0) {
     unsigned size = 2;
     while (size < all) size *= 2;
     for (unsigned i = all + tid; i < size; i += RT) s.list[i] = 0;
@@ -597,7 +677,7 @@ __device__ bool rank_list(S& s, const Row<T>& r, const RowRule& rule,
   team.barrier();
   theta = order_value(team.load(&s.theta, 0));
   ties = team.load(&s.ties, 0);
-  return true;
+  return RANKED;
 }
 
 // Sum over the cluster of a value of each thread.
@@ -677,7 +757,7 @@ __device__ void nucleus(S& s, const Row<T>& r, const RowRule& rule, const Team<S
   if (r.least <= 1) {
     const unsigned bins = (unsigned)__cvta_generic_to_shared(s.wbins) - (BIAS << 2);
     unsigned hi = 0, lo = 0, parts = 0;
-    each_vector(r, r.begin(warp), stop, [&](uint4 u) {
+    each_vector(r, r.begin(warp), stop, [&](uint4 u, int) {
       uint64_t l[N / 2];
       unpack_pairs<T>(u, l);
 #pragma unroll
@@ -701,7 +781,7 @@ __device__ void nucleus(S& s, const Row<T>& r, const RowRule& rule, const Team<S
     });
     if (parts) mass = join_sums(hi, lo, parts);
   } else {
-    each_vector(r, r.begin(warp), stop, [&](uint4 u) {
+    each_vector(r, r.begin(warp), stop, [&](uint4 u, int) {
       const float best = max_score(u, T());
       if (!(r.scaled(best) > low)) return;
       float l[N];
@@ -777,7 +857,7 @@ __device__ void nucleus(S& s, const Row<T>& r, const RowRule& rule, const Team<S
   Part p = {0, 0, 0};
   {
     unsigned hi = 0, lo = 0, parts = 0;
-    each_vector(r, r.begin(warp), stop, [&](uint4 u) {
+    each_vector(r, r.begin(warp), stop, [&](uint4 u, int) {
       uint64_t l[N / 2];
       float t[N], best = -INFINITY;
       unpack_pairs<T>(u, l);
@@ -861,11 +941,11 @@ __device__ void nucleus(S& s, const Row<T>& r, const RowRule& rule, const Team<S
 
 // Top-k with more entries than the threads' maxima can bound: a pass counts the entries by the bins
 // of nucleus(), which gives the bin of the top_k-th exactly.  Where the entries down to that bin
-// can be ranked, they are (done: true).  Else the bin's entries are listed and theta found among
-// them, without top-p (limited).  Neither, where fewer than top_k entries lie in the bins.
+// can be ranked, they are.  Else the bin's entries are listed and theta found among them (limited),
+// which leaves top-p to the caller (TOO_MANY), as where fewer than top_k entries lie in the bins.
 template <class T, bool SOLO, class S>
-__device__ bool tally(S& s, const Row<T>& r, const RowRule& rule, const Team<SOLO>& team,
-                      float& theta, unsigned& ties, bool& limited) {
+__device__ Ranked tally(S& s, const Row<T>& r, const RowRule& rule, const Team<SOLO>& team,
+                        float& theta, unsigned& ties, bool& limited, const RowOut& out) {
   constexpr int RT = S::RT;
   constexpr int N = Row<T>::N;
   constexpr int P = S::WBINS / RT;
@@ -875,7 +955,7 @@ __device__ bool tally(S& s, const Row<T>& r, const RowRule& rule, const Team<SOL
   for (int b = tid; b < S::WBINS; b += RT) s.wbins[b] = 0;
   if (tid == 0) s.number = 0;
   __syncthreads();
-  each_vector(r, r.begin(warp), r.end(warp), [&](uint4 u) {
+  each_vector(r, r.begin(warp), r.end(warp), [&](uint4 u, int) {
     float l[N];
     r.scores(u, l);
 #pragma unroll
@@ -912,15 +992,16 @@ __device__ bool tally(S& s, const Row<T>& r, const RowRule& rule, const Team<SOL
   team.barrier();
   if (all < rule.top_k) {
     // every eligible entry, where all of them lie in the bins and can be ranked
-    return r.tmin - 1.f > -(float)S::WBINS / S::STEPS && all <= S::RANK &&
-           rank_list(s, r, rule, team, r.scale, -low, theta, ties);
+    if (r.tmin - 1.f <= -(float)S::WBINS / S::STEPS || all > S::RANK) return TOO_MANY;
+    return rank_list(s, r, rule, team, r.scale, -low, theta, ties, out);
   }
   const unsigned bin = s.first_bin;
   const float from_t = -(float)bin * (1.f / S::STEPS), to_t = -(float)(bin + 1) * (1.f / S::STEPS);
   unsigned long long left = rule.top_k - s.some;
-  if (s.some + s.digit <= S::RANK) return rank_list(s, r, rule, team, r.scale, -to_t, theta, ties);
+  if (s.some + s.digit <= S::RANK)
+    return rank_list(s, r, rule, team, r.scale, -to_t, theta, ties, out);
   __syncthreads();
-  each_vector(r, r.begin(warp), r.end(warp), [&](uint4 u) {
+  each_vector(r, r.begin(warp), r.end(warp), [&](uint4 u, int) {
     float l[N];
     r.scores(u, l);
 #pragma unroll
@@ -942,7 +1023,7 @@ __device__ bool tally(S& s, const Row<T>& r, const RowRule& rule, const Team<SOL
   theta = order_value(khi);
   ties = (unsigned)left;
   limited = true;
-  return rule.part == 0xffffffffu;
+  return rule.part == 0xffffffffu ? RANKED : TOO_MANY;
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -991,7 +1072,7 @@ __device__ int by_codes(S& s, Row<T>& r, const RowRule& rule, const Team<SOLO>& 
   auto place_of = [&](int i) { return (i / 4) * 4 * RT + tid * 4 + i % 4; };  // ascending in i
   const unsigned table = (unsigned)__cvta_generic_to_shared(s.codes);
   bool odd = false, tiny = false;
-  each_vector(r, r.begin(warp), r.end(warp), [&](uint4 u) {
+  each_vector(r, r.begin(warp), r.end(warp), [&](uint4 u, int) {
     const unsigned w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
@@ -1114,7 +1195,7 @@ __device__ int by_codes(S& s, Row<T>& r, const RowRule& rule, const Team<SOLO>& 
   const int theta4 = s.some ? (int)s.last_bin << 2 : -1;
   Part p = {0, 0, 0};
   unsigned hi = 0, lo = 0, parts = 0;
-  each_vector(r, r.begin(warp), r.end(warp), [&](uint4 u) {
+  each_vector(r, r.begin(warp), r.end(warp), [&](uint4 u, int) {
     const unsigned w[4] = {u.x, u.y, u.z, u.w};
     const float best = max_score(u, T());
     if (!(best >= theta)) return;
@@ -1152,13 +1233,13 @@ __device__ int by_codes(S& s, Row<T>& r, const RowRule& rule, const Team<SOLO>& 
 // vector.
 template <class T, bool SOLO, class S>
 __device__ void draw(S& s, const Row<T>& r, const Team<SOLO>& team, float theta, unsigned ties,
-                     const Measured& m, uint64_t word, int32_t* id, float* logp, int32_t* kept) {
+                     const Measured& m, const RowOut& out) {
   constexpr int RW = S::RW;
   constexpr int N = Row<T>::N;
   const int C = team.size();
   const unsigned rank = team.rank;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const unsigned long long at = __umul64hi(word, m.total);
+  const unsigned long long at = __umul64hi(out.word, m.total);
   if (tid < C * RW && at >= m.before && at - m.before < m.kept) {
     s.digit = tid;
     s.over = m.before;
@@ -1221,13 +1302,7 @@ __device__ void draw(S& s, const Row<T>& r, const Team<SOLO>& team, float theta,
           for (int i = 0; i < N; ++i) {
             unsigned long long w = l[i] >= theta ? r.weight(l[i]) : 0ull;
             if (w && l[i] == theta && mine_before++ >= ties) w = 0;
-            if (at >= b && at - b < w) {
-              const unsigned long long rest = m.total - w;
-              *id = (v0 + lane) * N - r.view.skew + i;
-              *kept = (int32_t)m.number;
-              *logp = w > rest ? log1pf(-__fdiv_rn(__ull2float_rn(rest), __ull2float_rn(m.total)))
-                               : logf(__fdiv_rn(__ull2float_rn(w), __ull2float_rn(m.total)));
-            }
+            if (at >= b && at - b < w) out.set((v0 + lane) * N - r.view.skew + i, w, m.total, m.number);
             b += w;
           }
         }
@@ -1241,7 +1316,7 @@ __device__ void draw(S& s, const Row<T>& r, const Team<SOLO>& team, float theta,
 
 template <class T, bool SOLO, class S>
 __device__ void sample_row(S& s, Row<T>& r, const RowRule& rule, const Team<SOLO>& team,
-                           uint64_t word, int32_t* id, float* logp, int32_t* kept) {
+                           const RowOut& out) {
   constexpr int RT = S::RT, RW = S::RW;
   const int C = team.size();
   const unsigned rank = team.rank;
@@ -1256,15 +1331,11 @@ __device__ void sample_row(S& s, Row<T>& r, const RowRule& rule, const Team<SOLO
     if (r.view.n >= CODES_FROM && (by_k || by_p) && !k_by_maxima) {
       const int found = by_codes(s, r, rule, team, theta, ties, m);
       if (found == 0) {
-        if (rank == 0 && tid == 0) {
-          *id = -1;
-          *logp = -INFINITY;
-          *kept = 0;
-        }
+        if (rank == 0 && tid == 0) out.none();
         return;
       }
       if (found > 0) {
-        draw(s, r, team, theta, ties, m, word, id, logp, kept);
+        draw(s, r, team, theta, ties, m, out);
         return;
       }
     }
@@ -1275,7 +1346,7 @@ __device__ void sample_row(S& s, Row<T>& r, const RowRule& rule, const Team<SOLO
 #pragma unroll
   for (int k = 0; k < TM; ++k) tm[k] = -INFINITY;
   {
-    each_vector(r, r.begin(warp), r.end(warp), [&](uint4 u) {
+    each_vector(r, r.begin(warp), r.end(warp), [&](uint4 u, int) {
       const float best = fmaxf(tm[0], max_score(u, T()));
 #pragma unroll
       for (int i = 1; i < TM; ++i) tm[i - 1] = tm[i];  // each fourth vector's maximum
@@ -1317,11 +1388,7 @@ __device__ void sample_row(S& s, Row<T>& r, const RowRule& rule, const Team<SOLO
   }
   r.max = order_value(top);
   if (r.max == -INFINITY) {  // the same in every block of the cluster
-    if (rank == 0 && tid == 0) {
-      *id = -1;
-      *logp = -INFINITY;
-      *kept = 0;
-    }
+    if (rank == 0 && tid == 0) out.none();
     return;
   }
   r.rules(rule);
@@ -1330,6 +1397,7 @@ __device__ void sample_row(S& s, Row<T>& r, const RowRule& rule, const Team<SOLO
   if (by_k && !r.odd) {
     // At least top_k entries lie no lower than the top_k-th best of the threads' maxima: those down
     // to its bin are the candidates.
+    Ranked ranked = TOO_MANY;
     const float inv = __fdiv_rn((float)(S::CBINS - 1), __fsub_rn(r.max, order_value(low)));
     if (inv < 1e30f && rule.top_k <= (unsigned)(RT * TM / 4 * C)) {
 #pragma unroll
@@ -1355,9 +1423,11 @@ __device__ void sample_row(S& s, Row<T>& r, const RowRule& rule, const Team<SOLO
       }
       team.barrier();
       if (all >= rule.top_k)
-        done = rank_list(s, r, rule, team, inv, (float)s.digit + 1.f, theta, ties);
+        ranked = rank_list(s, r, rule, team, inv, (float)s.digit + 1.f, theta, ties, out);
     }
-    if (!done) done = tally(s, r, rule, team, theta, ties, limited);
+    if (ranked == TOO_MANY) ranked = tally(s, r, rule, team, theta, ties, limited, out);
+    if (ranked == DRAWN) return;
+    done = ranked == RANKED;
   }
   if (!by_k && by_p && !r.odd) {
     nucleus(s, r, rule, team, theta, ties, m);
@@ -1399,7 +1469,7 @@ __device__ void sample_row(S& s, Row<T>& r, const RowRule& rule, const Team<SOLO
   }
 
   if (!measured) m = measure_row(s, r, team, theta, ties);
-  draw(s, r, team, theta, ties, m, word, id, logp, kept);
+  draw(s, r, team, theta, ties, m, out);
 }
 
 // A cluster of C blocks takes a row: block c its c-th contiguous part, each of the block's warps a
@@ -1420,7 +1490,8 @@ __global__ void __launch_bounds__(RT, 1024 / RT)
     r.first = min(r.view.vectors, (int)team.rank * part);
     r.last = min(r.view.vectors, r.first + part);
     r.region = (part + RT - 1) / RT * 32;
-    sample_row(s, r, row_rule(rule, row), team, words[row], &ids[row], &logp[row], &kept[row]);
+    const RowOut out = {words[row], &ids[row], &logp[row], &kept[row]};
+    sample_row(s, r, row_rule(rule, row), team, out);
     team.barrier();
   }
 }
