@@ -73,10 +73,11 @@ __global__ void __launch_bounds__(PT) k_plan_scan(int32_t* __restrict__ tile, in
 }
 
 // A pair's slot: its expert's offset, the expert's pairs in earlier tiles, in earlier warps of its
-// tile, and before it in its warp.  Every block adds up the experts' totals (one tile: its own).
+// tile, and before it in its warp.  Every block adds up the experts' totals (one tile: its own).  A
+// warp's pairs stay in registers between its counting and its placing, eight loads in flight.
 //
-// 169,343 x 8 pairs, 256 experts: the pairs of a warp stay in registers between
-// its counting and its placing, eight loads in flight.
+// 169,343 x 8 pairs, 256 experts: count, scan and place take 25 to 31 us for 16 MB, 2.4 us of copying;
+// bound by the three launches, each a chain of dependent steps.
 __global__ void __launch_bounds__(PT) k_plan_place(const int32_t* __restrict__ experts,
                                                    int64_t pairs, int E, int tiles,
                                                    const int32_t* __restrict__ tile,
@@ -191,7 +192,8 @@ union Piece {
 constexpr int XT = 256;  // threads of a block
 
 // A thread takes a piece of a row, K of the row's pairs in flight and the next row's slots and
-// weights on their way: the combined row is written once and every y row read once.
+// weights on their way: the combined row is written once and every y row read once.  Bound by
+// memory: 20,000 rows of 512 bf16, 4 experts each: 18.4 us, 5.6 TB/s.
 template <class T, int B, int K>
 __global__ void __launch_bounds__(XT) k_combine(int64_t rows, int k, int pieces, int wide,
                                                 const T* __restrict__ y,
@@ -286,7 +288,7 @@ __global__ void __launch_bounds__(XT) k_gather(int64_t rows, int k, int pieces, 
 
 // dy[slot] = weight dout[row] and dweights = dout[row] . y[slot]: a warp takes a row, KG of its pairs
 // at a time, so dout is read once (from L1 for more pairs) and each y row is read where its dy row is
-// written.
+// written.  Bound by memory: 32,768 rows of 1024 bf16, 8 experts each: 177 us, 6.5 TB/s.
 template <class T, int B, int KG>
 __global__ void __launch_bounds__(XT) k_combine_backward(
     int64_t rows, int k, int pieces, const T* __restrict__ dout, const T* __restrict__ y,

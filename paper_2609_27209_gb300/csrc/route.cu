@@ -401,8 +401,8 @@ __device__ __forceinline__ int candidates(const float* c, int k, int first, floa
 //
 // A warp takes rows in turn, its biases in registers and the next row on its way.
 //
-// E = 256, k = 8, four of eight groups, sigmoid with bias, 32,768 rows of bf16: k rounds over exact
-// scores took 55 us (1505 instructions a row, issue-bound).
+// E = 256, k = 8, four of eight groups, sigmoid with bias, 32,768 rows of bf16: 31 us, issue-bound at
+// about 750 instructions a row; k rounds over exact scores took 55 us (1505 instructions).
 template <class T, int V, bool SIGMOID>
 __global__ void __launch_bounds__(FW * 32, V == 8 ? 4 : V == 16 ? 2 : 1)
     k_route_warp(int64_t rows, const T* __restrict__ logits, int64_t stride,
@@ -498,6 +498,9 @@ __global__ void __launch_bounds__(FW * 32, V == 8 ? 4 : V == 16 ? 2 : 1)
 // gs = sum ds s (0 in exact arithmetic when renormalised), and 0 for sigmoid, whose rows are then not
 // read at all; the lanes that hold a chosen expert's gradient store it over that.  Results here are
 // rounded to the output's type, so the exponential is the hardware's.
+//
+// 169,343 rows of 64 f32, two experts each, softmax: 24 us, 3.8 TB/s; the chain of a row (choices,
+// scores, two reductions) at full occupancy is what is left.
 template <class T, int L, int V, bool SIGMOID>
 __global__ void __launch_bounds__(FW * 32)
     k_route_lanes_backward(int64_t rows, const T* __restrict__ logits, int64_t stride,
