@@ -238,7 +238,8 @@ struct Row {
   }
 };
 
-// f(vector, its number) for vectors [from, to) of the row, 32 at a time (lanes past the end get masked vectors).
+// f(vector, its number) for vectors [from, to) of the row, 32 at a time (lanes past the end get masked
+// vectors).
 // Each lane's vectors arrive in the warp's ring of shared memory, DEPTH - 1 ahead, and are read by
 // that lane alone.
 template <class T, class F>
@@ -253,29 +254,34 @@ __device__ __forceinline__ void each_vector(const Row<T>& r, int from, int to, F
     from = 32;
   }
   const int whole = min(to, r.view.whole());  // vectors up to here are the row's own
-  const uint4* src = reinterpret_cast<const uint4*>(r.view.base) + lane;
-  uint4* mine = r.ring + (threadIdx.x >> 5) * (DEPTH * 32) + lane;
-  const unsigned dst = (unsigned)__cvta_generic_to_shared(mine);
-  auto issue = [&](int base, unsigned stage) {
-    if (base + 32 <= whole || base + lane < whole)
-      asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + stage), "l"(src + base)
-                   : "memory");
+  const uint4* src = reinterpret_cast<const uint4*>(r.view.base) + (from + lane);
+  const unsigned ring = (unsigned)__cvta_generic_to_shared(
+      r.ring + (threadIdx.x >> 5) * (DEPTH * 32) + lane);
+  const int ahead = whole - 32 * (DEPTH - 1);
+  auto issue = [&](bool own, unsigned at, const uint4* p) {
+    if (own) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(at), "l"(p) : "memory");
     asm volatile("cp.async.commit_group;" ::: "memory");
   };
 #pragma unroll
-  for (int d = 0; d < DEPTH - 1; ++d) issue(from + 32 * d, d * 512);
-  unsigned stage = 0, last = (DEPTH - 1) * 512;
-  for (int base = from; base < to; base += 32) {
-    issue(base + 32 * (DEPTH - 1), last);
+  for (int d = 0; d < DEPTH - 1; ++d)
+    issue(from + lane + 32 * d < whole, ring + d * 512, src + 32 * d);
+  unsigned stage = ring, last = ring + (DEPTH - 1) * 512;
+  src += 32 * (DEPTH - 1);
+  int v = from + lane;
+  for (int left = to - from; left > 0; left -= 32, v += 32, src += 32) {
+    issue(v < ahead, last, src);
     asm volatile("cp.async.wait_group %0;" ::"n"(DEPTH - 1) : "memory");
     uint4 u;
-    if (base + 32 <= whole || base + lane < whole)
-      u = *reinterpret_cast<const uint4*>(reinterpret_cast<const char*>(mine) + stage);
+    if (v < whole)
+      asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
+                   : "=r"(u.x), "=r"(u.y), "=r"(u.z), "=r"(u.w)
+                   : "r"(stage)
+                   : "memory");
     else
-      u = base + lane < to ? r.view.fetch(base + lane) : masked();
-    f(u, base + lane);
+      u = v < to ? r.view.fetch(v) : masked();
+    f(u, v);
     last = stage;
-    stage = stage == (DEPTH - 1) * 512 ? 0 : stage + 512;
+    stage = stage == ring + (DEPTH - 1) * 512 ? ring : stage + 512;
   }
   asm volatile("cp.async.wait_group 0;" ::: "memory");
 }
@@ -1037,7 +1043,7 @@ __device__ Ranked tally(S& s, const Row<T>& r, const RowRule& rule, const Team<S
 // Returns 1, or 0 for a row with nothing to draw, or -1 where entries without a place of their own
 // could change the result.
 //
-// 256 rows of 232,965, top-p: 264 us by weighing every entry twice, 146 us so (57 instructions an
+// 256 rows of 232,965, top-p: 264 us by weighing every entry twice, 142 us so (57 instructions an
 // entry over both passes).
 
 // four times the place of the bfloat16 in the upper half of `t` (a: its magnitude): 0's for magnitudes
@@ -1476,10 +1482,10 @@ __device__ void sample_row(S& s, Row<T>& r, const RowRule& rule, const Team<SOLO
 // contiguous region of that, so that the index order is the order of (block, warp, vector, lane) and a
 // draw is found from the regions' sums without a scan over the row.
 //
-// Issue-bound, not memory-bound.  256 rows of 232,965 bf16, top-p 0.95: 146 us, 0.82 TB/s of the
+// Issue-bound, not memory-bound.  256 rows of 232,965 bf16, top-p 0.95: 142 us, 0.84 TB/s of the
 // row's bytes; 57 instructions an entry over both passes.  Schedulers issue in 69% of their active
 // cycles, and 256 blocks leave a sixth of the machine's 304 places empty.
-// 64 rows of 169,343 bf16, mixed rules: 51 us.  One row of 20,000 f32, top-k 50 and top-p: 18 us,
+// 64 rows of 169,343 bf16, mixed rules: 52 us.  One row of 20,000 f32, top-k 50 and top-p: 18 us,
 // latency of the call, the block scans and the cluster's barriers.
 template <class T, bool SOLO, int RT>
 __global__ void __launch_bounds__(RT, 1024 / RT)
