@@ -163,6 +163,18 @@ def test_sample_ties(rule):
         check_sample(torch.from_numpy(x).to(dev()), words_of(rng, 5), **rule)
 
 
+@pytest.mark.parametrize("high", [127, 128, 129, 255, 256, 257])
+@pytest.mark.parametrize("rule", [dict(top_k=100), dict(top_k=60, top_p=0.6), dict(top_k=120, min_p=0.7)], ids=str)
+def test_sample_few_candidates_with_ties_among_them(high, rule):
+    rng = np.random.default_rng(high)
+    for rows, n in [(3, 20001), (200, 5001)]:  # a cluster, and a small block, a row
+        x = rng.normal(size=(rows, n)).astype(np.float32) - 20
+        for row in x:
+            row[rng.choice(n, high, replace=False)] = np.repeat([1.0, 0.75, 0.5], (30, 40, high - 70))
+        for kind in TYPES.values():
+            check_sample(torch.from_numpy(x).to(dev()).to(kind), words_of(rng, rows), every=max(1, rows // 8), **rule)
+
+
 def test_sample_infinities_nan_and_lowest_values():
     low = float(np.finfo(np.float32).min)
     x = np.array([[np.nan] * 5, [np.inf, 1, np.inf, np.nan, -np.inf], [low] * 5, [low, low, 3, -np.inf, 2],
