@@ -187,6 +187,12 @@ __device__ __forceinline__ float one_score(float l, const RowScale& r) {
   return __fdiv_rn(l >= 0.f ? 1.f : e, __fadd_rn(1.f, e));
 }
 
+// 2^k for the sum k + 1.5 2^23 that pow2_pair gives, k in [-126, 0].  A product with it may be subnormal
+// (k = -126), which adding k to the other factor's exponent bits could not give.
+__device__ __forceinline__ float two_to(float k_shifted) {
+  return __uint_as_float((__float_as_uint(k_shifted) << 23) + 0x3f800000u);
+}
+
 // the scores s_j of a lane's logits, -1 where masked
 template <int L, int V, bool SIGMOID>
 __device__ __forceinline__ RowScale lane_scores(const float* l, float* s) {
@@ -201,9 +207,7 @@ __device__ __forceinline__ RowScale lane_scores(const float* l, float* s) {
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         const float x = l[j + i];
-        const float e = t[i] >= -126.5f
-                            ? __uint_as_float(__float_as_uint(p[i]) + (__float_as_uint(k[i]) << 23))
-                            : 0.f;
+        const float e = t[i] >= -126.5f ? __fmul_rn(p[i], two_to(k[i])) : 0.f;
         s[j + i] = x == -INFINITY ? -1.f : __fdiv_rn(x >= 0.f ? 1.f : e, __fadd_rn(1.f, e));
       }
     }
