@@ -266,9 +266,11 @@ __device__ __forceinline__ float lanes_max(float v) {
   }
 }
 
-// the score of a lane's group (a power of two of lanes): its best choice, or the sum of its best two
+// the score of a lane's group (a power of two of lanes): its best choice, or the sum of its best two;
+// `terms`: the sum of their magnitudes, 0 where there is no choice
 template <int V>
-__device__ __forceinline__ float group_score(const erc_route_rule& rule, int span, const float* c) {
+__device__ __forceinline__ float group_score(const erc_route_rule& rule, int span, const float* c,
+                                             float& terms) {
   float a = -INFINITY, b = -INFINITY;
 #pragma unroll
   for (int j = 0; j < V; ++j) {
@@ -280,14 +282,17 @@ __device__ __forceinline__ float group_score(const erc_route_rule& rule, int spa
     b = fmaxf(fmaxf(b, b2), fminf(a, a2));
     a = fmaxf(a, a2);
   }
-  return b > -INFINITY && rule.group_best == 2 ? __fadd_rn(a, b) : a;
+  const bool two = b > -INFINITY && rule.group_best == 2;
+  terms = two ? fabsf(a) + fabsf(b) : a > -INFINITY ? fabsf(a) : 0.f;
+  return two ? __fadd_rn(a, b) : a;
 }
 
 // The choices of the groups passed over become -inf; ties go to the lowest group.
 template <int L, int V>
 __device__ __forceinline__ void keep_groups(const erc_route_rule& rule, int lane, float* c) {
   const int at = lane % L, span = rule.experts / rule.groups / V;
-  const float mine = group_score<V>(rule, span, c);
+  float terms;
+  const float mine = group_score<V>(rule, span, c, terms);
   int better = 0;
   for (int o = 0; o < rule.groups; ++o) {
     const float other = __shfl_sync(0xffffffffu, mine, lane - at + o * span);
@@ -400,8 +405,11 @@ __device__ __forceinline__ int candidates(const float* c, int k, int first, floa
 // lane, by their exact choices.  For sigmoid scores the candidates come from the hardware's
 // exponential and reciprocal: with |t| as computed here their scores are within 1.1e-6 of the exact
 // ones (2^-22 for ex2, 1.9e-7 for the polynomial, an ulp for rcp, three roundings), so 4e-6 (1 + |c|)
-// covers twice that and the rounding of the sum with the bias.  Rows whose groups are not told apart
-// by twice as much, or with more candidates, take exact choices and, if need be, k rounds.
+// covers twice that and the rounding of the sum with the bias (2^-23 |c| between two choices).  A group's
+// score adds two such errors and its own rounding, all in proportion to its terms, which may be far
+// larger than their sum: 2.2e-6 + 2.4e-7 (|a| + |b|), and for two groups less than 8e-6 (1 + the largest
+// |a| + |b| of the row).  Rows whose groups are not told apart by that, or with more candidates, take
+// exact choices and, if need be, k rounds.
 //
 // A warp takes rows in turn, its biases in registers and the next row on its way.
 //
@@ -443,15 +451,17 @@ __global__ void __launch_bounds__(FW * 32, V == 8 ? 4 : V == 16 ? 2 : 1)
       bool clear = true;
       if (grouped) {
         // the top_groups distinct best groups' scores, and the best of the rest
-        const float mine = group_score<V>(rule, span, c);
-        float rest = mine, worst = -INFINITY;
+        float terms, worst = -INFINITY;
+        const float mine = group_score<V>(rule, span, c, terms);
+        float rest = mine;
+        terms = lanes_max<32>(terms);
         for (int i = 0; i < rule.top_groups; ++i) {
           worst = lanes_max<32>(rest);
           if (rest == worst) rest = -INFINITY;
         }
         rest = lanes_max<32>(rest);
         const int in = __popc(__ballot_sync(0xffffffffu, mine >= worst && first < E));
-        clear = in == rule.top_groups * span && worst - rest > 8e-6f * (1.f + fabsf(worst));
+        clear = in == rule.top_groups * span && worst - rest > 8e-6f * (1.f + terms);
         if (mine < worst) {
 #pragma unroll
           for (int j = 0; j < V; ++j) c[j] = -INFINITY;

@@ -6,7 +6,7 @@ import torch
 
 from oracle import choice_oracle as C
 
-from ._gpu import dev
+from ._gpu import dev, host
 from .test_gpu_choice import TYPES, check_route
 
 pytestmark = pytest.mark.gpu
@@ -27,3 +27,35 @@ def test_sigmoid_scores_around_the_smallest_normal_float(E, groups, renorm):
     for t in TYPES.values():
         check_route(torch.from_numpy(x).to(dev()).to(t), min(8, E), kind="sigmoid", groups=groups,
                     top_groups=max(1, groups // 2), renorm=renorm)
+
+
+def just_below(points):
+    """float32 logits whose float32 sigmoids are the largest below `points` that 65 neighbours hold."""
+    l = np.log(points / (1 - points)).astype(np.float32)[:, None]
+    near = (l.view(np.int32) + np.arange(-32, 33, dtype=np.int32)).view(np.float32)
+    s, _ = C.route_scores(near, "sigmoid")
+    s = np.where(s.astype(np.float64) < points[:, None], s, -1)
+    best = s.argmax(1)[:, None]
+    return np.take_along_axis(near, best, 1)[:, 0], np.take_along_axis(s, best, 1)[:, 0].astype(np.float64)
+
+
+@pytest.mark.parametrize("E,big", [(256, 512.0), (256, 1024.0), (512, 1024.0), (1024, 65536.0)])
+def test_groups_whose_two_best_cancel(E, big):
+    # One expert of a group has the bias `big`, the others -big: the choices are rounded to steps of
+    # ulp(big), a group's score is near 1.  The last group's best score lies just below the middle of
+    # such a step, the first group's well inside it: they tie, so the first is taken.
+    rows, size = 4096, 32
+    step = np.spacing(np.float32(big)).astype(np.float64)
+    j = np.floor(np.linspace(0.5, 0.9, rows) / step)
+    x = np.full((rows, E), -np.inf, np.float32)
+    x[:, :size] = x[:, -size:] = -1.0
+    x[:, 0], low = just_below((j + 0.25) * step)
+    x[:, E - size], high = just_below((j + 0.5) * step)
+    keep = (low > 0) & (high > 0) & ((j + 0.5) * step < 0.95)
+    x = x[keep]
+    assert len(x) > 4
+    bias = np.full(E, -big, np.float32)
+    bias[::size] = big
+    experts, _ = check_route(torch.from_numpy(x).to(dev()), 2, kind="sigmoid", bias=bias, groups=E // size,
+                             top_groups=1)
+    assert (host(experts) == [0, 1]).all()
