@@ -267,7 +267,7 @@ __device__ __forceinline__ float lanes_max(float v) {
 }
 
 // the score of a lane's group (a power of two of lanes): its best choice, or the sum of its best two;
-// `terms`: the sum of their magnitudes, 0 where there is no choice
+// `terms`: the sum of their magnitudes, -1 where there is no choice
 template <int V>
 __device__ __forceinline__ float group_score(const erc_route_rule& rule, int span, const float* c,
                                              float& terms) {
@@ -283,19 +283,21 @@ __device__ __forceinline__ float group_score(const erc_route_rule& rule, int spa
     a = fmaxf(a, a2);
   }
   const bool two = b > -INFINITY && rule.group_best == 2;
-  terms = two ? fabsf(a) + fabsf(b) : a > -INFINITY ? fabsf(a) : 0.f;
+  terms = two ? fabsf(a) + fabsf(b) : a > -INFINITY ? fabsf(a) : -1.f;
   return two ? __fadd_rn(a, b) : a;
 }
 
-// The choices of the groups passed over become -inf; ties go to the lowest group.
+// The choices of the groups passed over become -inf; ties go to the lowest group.  Scores are compared
+// as keys, with 0 for a group with no choice: a sum of two may be -inf, and that is still above none.
 template <int L, int V>
 __device__ __forceinline__ void keep_groups(const erc_route_rule& rule, int lane, float* c) {
   const int at = lane % L, span = rule.experts / rule.groups / V;
   float terms;
-  const float mine = group_score<V>(rule, span, c, terms);
+  const float score = group_score<V>(rule, span, c, terms);
+  const unsigned mine = terms < 0.f ? 0u : order_key(score);
   int better = 0;
   for (int o = 0; o < rule.groups; ++o) {
-    const float other = __shfl_sync(0xffffffffu, mine, lane - at + o * span);
+    const unsigned other = __shfl_sync(0xffffffffu, mine, lane - at + o * span);
     better += other > mine || (other == mine && o < at / span);
   }
   if (better >= rule.top_groups) {

@@ -59,3 +59,16 @@ def test_groups_whose_two_best_cancel(E, big):
     experts, _ = check_route(torch.from_numpy(x).to(dev()), 2, kind="sigmoid", bias=bias, groups=E // size,
                              top_groups=1)
     assert (host(experts) == [0, 1]).all()
+
+
+@pytest.mark.parametrize("E", [64, 128, 60, 256, 1024])
+@pytest.mark.parametrize("kind", ["softmax", "sigmoid"])
+def test_groups_whose_sum_overflows_are_not_empty_groups(E, kind):
+    x = np.random.default_rng(E).normal(size=(9, E)).astype(np.float32)
+    x[:, : E // 4] = -np.inf  # a group with nothing to choose comes first, groups of -inf = -3e38 - 3e38 follow
+    x[4, : 3 * E // 4] = -np.inf
+    bias = np.full(E, -3e38, np.float32)
+    for top in (1, 2, 3):
+        with np.errstate(over="ignore"):  # the oracle's sums
+            experts, _ = check_route(torch.from_numpy(x).to(dev()), 3, kind=kind, bias=bias, groups=4, top_groups=top)
+        assert (host(experts) >= E // 4).all()
