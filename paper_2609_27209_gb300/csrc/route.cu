@@ -536,7 +536,7 @@ __global__ void __launch_bounds__(FW * 32)
   };
   // the row's choices, one or more a lane: their loads start before the row's
   int place[KL];
-  float s[KL], g[KL], chosen[KL];
+  float s[KL], g[KL], chosen[KL], share[KL];
 #pragma unroll
   for (int i = 0; i < KL; ++i) {
     const int c = at + i * L;
@@ -580,17 +580,21 @@ __global__ void __launch_bounds__(FW * 32)
     } else {
       s[i] = power(below_max(l, m, LOG2E)) * inv;
     }
+    share[i] = s[i];
     D += s[i];
   }
   if (rule.renorm) {
+    // with the weight p = s / D in place of s, since (g - gp) / D alone overflows where D is tiny
     D = lanes_sum<L>(D);
-    const float r = D > 0.f ? __frcp_rn(D) : 0.f;
     float gp = 0.f;
 #pragma unroll
-    for (int i = 0; i < KL; ++i) gp += g[i] * (D > 0.f ? __fdiv_rn(s[i], D) : 0.f);
+    for (int i = 0; i < KL; ++i) {
+      share[i] = D > 0.f ? __fdiv_rn(s[i], D) : 0.f;
+      gp += g[i] * share[i];
+    }
     gp = lanes_sum<L>(gp);
 #pragma unroll
-    for (int i = 0; i < KL; ++i) g[i] = place[i] >= 0 ? (g[i] - gp) * r : 0.f;
+    for (int i = 0; i < KL; ++i) g[i] -= gp;
   }
   float gs = 0.f;
   if (!SIGMOID && !rule.renorm) {
@@ -622,7 +626,7 @@ __global__ void __launch_bounds__(FW * 32)
 #pragma unroll
   for (int i = 0; i < KL; ++i)
     if (place[i] >= 0)
-      out[place[i]] = from_f32<T>(SIGMOID ? g[i] * s[i] * (1.f - s[i]) : s[i] * (g[i] - gs));
+      out[place[i]] = from_f32<T>(SIGMOID ? g[i] * share[i] * (1.f - s[i]) : share[i] * (g[i] - gs));
 }
 
 // calls f(L, V) for the fewest lanes that hold E experts, eight a lane up to 256

@@ -5,9 +5,10 @@ import pytest
 import torch
 
 from oracle import choice_oracle as C
+from paper_2609_27209_gb300 import erc
 
 from ._gpu import dev, host
-from .test_gpu_choice import TYPES, check_route
+from .test_gpu_choice import TYPES, U, check_route, f32
 
 pytestmark = pytest.mark.gpu
 
@@ -72,3 +73,25 @@ def test_groups_whose_sum_overflows_are_not_empty_groups(E, kind):
         with np.errstate(over="ignore"):  # the oracle's sums
             experts, _ = check_route(torch.from_numpy(x).to(dev()), 3, kind=kind, bias=bias, groups=4, top_groups=top)
         assert (host(experts) >= E // 4).all()
+
+
+@pytest.mark.parametrize("E", [2, 64, 128, 200, 1024])
+def test_sigmoid_gradient_where_the_chosen_scores_are_tiny(E):
+    # (g - mean) / D alone overflows for D below 1e-35; times s it is an ordinary number
+    rng = np.random.default_rng(E)
+    k = min(4, E)
+    x = rng.uniform(-87.2, -84, (20, E)).astype(np.float32)
+    e, _ = C.route(x, k, "sigmoid")
+    for size in (1.0, 1e3, 1e6):
+        g = (rng.normal(size=e.shape) * size).astype(np.float32)
+        got = erc.erc_route_backward(torch.from_numpy(x).to(dev()), torch.from_numpy(e.astype(np.int32)).to(dev()),
+                                     torch.from_numpy(g).to(dev()), score=erc.ERC_SCORE_SIGMOID)
+        assert np.isfinite(f32(got)).all()
+        s = C.scores64(x, "sigmoid")
+        v = np.take_along_axis(s, e, 1)
+        want = C.route_gradient(x, e, g, "sigmoid", True, 1.0)
+        # scores within delta of themselves (|t| <= 126 moved by 2.5 U |t| ln 2, the rest 5 U, and half of
+        # 2^-149 against at least 2^-126), in five factors; k terms are summed
+        delta = 126 * 2.5 * U * np.log(2) + 5 * U + 2.0**-24
+        bound = s / v.sum(1, keepdims=True) * 2 * np.abs(g).sum(1, keepdims=True) * (5 * delta + (k + 8) * U)
+        assert np.all(np.abs(f32(got) - want) <= bound)
