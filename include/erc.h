@@ -355,11 +355,12 @@ typedef struct erc_route_rule {
  * erc_route -- k experts for each row of scores, with their weights.
  *
  * s_i is the softmax over the row (2^t divided by the sum of the row's integer weights, as
- * 2^t (1 / Z), T = 1) or the sigmoid ((l >= 0 ? 1 : e) / (1 + e), e = 2^(-|l| log2(e)), 0 below
- * 2^-126).  Experts are chosen by s_i + bias_i (bias [E] float32 or NULL; it balances the load
- * and has no part in the weights): first the top_groups best groups, then the k best experts in
- * them, ties to the lowest index.  A masked score, or a choice that is -inf or NaN, is never
- * chosen, and neither is a group with no other; a group's missing second best adds nothing.
+ * 2^t (1 / Z), T = 1, with 2^t kept where e >= -126, further than the integers reach) or the
+ * sigmoid ((l >= 0 ? 1 : v) / (1 + v), v = 2^(-|l| log2(e)), kept as far).  Experts are chosen by
+ * s_i + bias_i (bias [E] float32 or NULL; it balances the load and has no part in the weights):
+ * first the top_groups best groups, then the k best experts in them, ties to the lowest index.  A
+ * masked score, or a choice that is -inf or NaN, is never chosen, and neither is a group with no
+ * other; a group's missing second best adds nothing.
  * Out: experts [rows x k] int32, best first, -1 where fewer than k can be chosen; weights
  *      [rows x k] float32: scale s_i, or scale s_i / (sum of the row's chosen s) with renorm (0
  *      where that sum is 0); 0 for -1.

@@ -115,7 +115,7 @@ def route_scores(logits, kind):
             z = int(fixed_weights(x[r], LOG2E).sum())
             inv = F(1) / (F(z) * F(2.0**-40))
             p, e = _split(_below(x[r], m, LOG2E))
-            live = e >= -41
+            live = e >= -126
             s[r] = np.where(live, np.where(live, p, F(0)) * np.exp2(np.where(live, e, 0).astype(F)), F(0)).astype(F) * inv
     assert s.dtype == F
     return np.where(masked, F(0), s), masked

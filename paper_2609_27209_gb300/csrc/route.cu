@@ -2,7 +2,8 @@
 //
 // s = softmax(l) or 1 / (1 + exp(-l)) with choice.cuh's exponential: the softmax normaliser is a sum
 // of integer weights, every other step one rounded float32 operation, so the choice s + bias and
-// with it the chosen experts have the same bits on every machine.
+// with it the chosen experts have the same bits on every machine.  2^t is kept down to rint(t) = -126, so
+// that experts far below the best keep their order and their weights; only the integers end at 2^-41.
 #include "choice.cuh"
 
 namespace erc {
@@ -34,7 +35,7 @@ __device__ __forceinline__ void row_scores(const T* x, int E, int score, float* 
     const float inv = __frcp_rn(__fmul_rn(__ull2float_rn(z ? z : 1ull), 9.094947017729282e-13f));
     for (int i = lane; i < E; i += 32) {
       const float l = clean_score(to_f32(x[i]));
-      sc[i] = l == -INFINITY ? -1.f : __fmul_rn(pow2_float(below_max(l, m, LOG2E), -41.f), inv);
+      sc[i] = l == -INFINITY ? -1.f : __fmul_rn(pow2_float(below_max(l, m, LOG2E), -126.f), inv);
     }
   }
   __syncwarp();
@@ -182,7 +183,7 @@ struct RowScale {  // of a softmax row: its maximum and 1 / Z
 template <bool SIGMOID>
 __device__ __forceinline__ float one_score(float l, const RowScale& r) {
   if (l == -INFINITY) return -1.f;
-  if (!SIGMOID) return __fmul_rn(pow2_float(below_max(l, r.max, LOG2E), -41.f), r.inv);
+  if (!SIGMOID) return __fmul_rn(pow2_float(below_max(l, r.max, LOG2E), -126.f), r.inv);
   const float e = pow2_float(-__fmul_rn(fabsf(l), LOG2E), -126.f);
   return __fdiv_rn(l >= 0.f ? 1.f : e, __fadd_rn(1.f, e));
 }
@@ -219,16 +220,17 @@ __device__ __forceinline__ RowScale lane_scores(const float* l, float* s) {
     unsigned hi = 0, lo = 0;
 #pragma unroll
     for (int j = 0; j < V; j += 2) {
-      float t[2];
+      float t[2], p[2], k[2];
       unsigned h[2], w[2];
 #pragma unroll
-      for (int i = 0; i < 2; ++i) t[i] = l[j + i] == -INFINITY ? -60.f : below_max(l[j + i], m, LOG2E);
-      weight_parts(t[0], t[1], h, w, s + j);
+      for (int i = 0; i < 2; ++i)
+        t[i] = l[j + i] == -INFINITY ? -200.f : fmaxf(below_max(l[j + i], m, LOG2E), -200.f);
+      pow2_pair(t[0], t[1], p, k);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) s[j + i] = t[i] >= -126.5f ? __fmul_rn(p[i], two_to(k[i])) : 0.f;
+      split_weights(pair(s[j], s[j + 1]), h, w);
       hi += h[0] + h[1];
       lo += w[0] + w[1];
-#pragma unroll
-      for (int i = 0; i < 2; ++i)
-        if (!(t[i] > -41.5f)) s[j + i] = 0.f;
     }
     hi = lanes_sum<L>(hi - V * BIAS);
     lo = lanes_sum<L>(lo - V * BIAS);
@@ -529,10 +531,10 @@ __global__ void __launch_bounds__(FW * 32)
   const bool live = row < rows;
   const T* x = logits + (live ? row : 0) * stride;
   const int first = at * V;
-  auto power = [](float t) {  // 2^t, 0 where the forward pass has 0
+  auto power = [](float t) {  // 2^t, 0 below 2^-126
     float e;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(t));
-    return t > -41.5f ? e : 0.f;
+    return e;
   };
   // the row's choices, one or more a lane: their loads start before the row's
   int place[KL];
@@ -578,7 +580,7 @@ __global__ void __launch_bounds__(FW * 32)
       const float q = pow2_float(-__fmul_rn(fabsf(l), LOG2E), -126.f);
       s[i] = __fdiv_rn(l >= 0.f ? 1.f : q, 1.f + q);
     } else {
-      s[i] = power(below_max(l, m, LOG2E)) * inv;
+      s[i] = pow2_float(below_max(l, m, LOG2E), -126.f) * inv;
     }
     share[i] = s[i];
     D += s[i];

@@ -95,3 +95,44 @@ def test_sigmoid_gradient_where_the_chosen_scores_are_tiny(E):
         delta = 126 * 2.5 * U * np.log(2) + 5 * U + 2.0**-24
         bound = s / v.sum(1, keepdims=True) * 2 * np.abs(g).sum(1, keepdims=True) * (5 * delta + (k + 8) * U)
         assert np.all(np.abs(f32(got) - want) <= bound)
+
+
+@pytest.mark.parametrize("E,groups", KERNELS)
+def test_softmax_orders_experts_far_below_the_best(E, groups):
+    # the scores of whole-number logits within 80 of the best are distinct normal floats: the order of the
+    # experts is the order of the logits, and nothing of them is lost
+    rng = np.random.default_rng(E)
+    x = np.stack([rng.permutation(np.resize(-rng.permutation(81), E)) for _ in range(30)]).astype(np.float32)
+    x[:, 0] = 0
+    x[0, 1:8] = [-40, -30, -50, -35, -60, -45, -70]
+    x[0, 8:] = -np.inf
+    k = min(6, E)
+    for renorm in (True, False):
+        experts, weights = erc.erc_route(torch.from_numpy(x).to(dev()), k, groups=groups, top_groups=groups, renorm=renorm)
+        want = np.argsort(-x, 1, kind="stable")[:, :k]
+        np.testing.assert_array_equal(host(experts), want)
+        w = C.weights64(x, want, "softmax", renorm, 1.0)
+        # |t| <= 116 moved by 2.5 U |t| ln 2; the polynomial, the sum, its reciprocal, a product and a quotient
+        np.testing.assert_allclose(host(weights), w, rtol=116 * 2.5 * U * np.log(2) + (k + 12) * U, atol=0)
+
+
+@pytest.mark.parametrize("E", [8, 64, 128, 200, 1024])
+@pytest.mark.parametrize("renorm", [True, False])
+def test_softmax_gradient_of_experts_far_below_the_best(E, renorm):
+    # experts that a bias chose: their scores are down to e^-86 of the best one's
+    rng = np.random.default_rng(E)
+    k = min(4, E - 1)
+    x = rng.uniform(-86, -60, (20, E)).astype(np.float32)
+    x[:, -1] = 0
+    x[::2, :k] = rng.uniform(-86, -85, (10, k))
+    e = np.tile(np.arange(k), (20, 1))
+    g = (rng.normal(size=e.shape) * 1e4).astype(np.float32)
+    got = f32(erc.erc_route_backward(torch.from_numpy(x).to(dev()), torch.from_numpy(e.astype(np.int32)).to(dev()),
+                                     torch.from_numpy(g).to(dev()), renorm=renorm))
+    s = C.scores64(x, "softmax")
+    want = C.route_gradient(x, e, g, "softmax", renorm, 1.0)
+    d = np.take_along_axis(s, e, 1).sum(1, keepdims=True) if renorm else 1.0
+    delta = 126 * 2.5 * U * np.log(2) + 5 * U
+    bound = s / d * 2 * np.abs(g).sum(1, keepdims=True) * (5 * delta + (k + 8) * U)
+    # renormalised weights do not depend on the other logits at all; results below 2^-126 may be rounded to 0
+    assert np.all(np.abs(got - want) <= bound + 2.0**-126)
