@@ -1525,7 +1525,7 @@ int blocks_of(int64_t rows, int64_t n) {
 // ------------------------------------------------------------------------------------------------
 constexpr int SW = 4;          // warps of a block
 constexpr int SHORT = 1536;    // longest row (2000 entries: a block of 128 threads is faster)
-inline int short_q(int64_t n) { return (int)((n + 31) / 32) | 1; }
+constexpr int short_q(int64_t n) { return (int)((n + 31) / 32) | 1; }
 
 __device__ __forceinline__ unsigned long long warp_sum(unsigned long long v) {
 #pragma unroll
@@ -1669,7 +1669,7 @@ struct ShortRow {
 };
 // words of a warp's shared memory: keys, 2^t where weights are needed, bins and list where entries may
 // be filtered
-__host__ __device__ inline int short_words(int q, bool mass, bool filters) {
+__host__ __device__ constexpr int short_words(int q, bool mass, bool filters) {
   return q * 32 * (mass ? 2 : 1) + (filters ? 2 * SBINS + 32 : 0);
 }
 
@@ -1817,8 +1817,11 @@ erc_status launch_rows(int64_t rows, int64_t n, const T* logits, int64_t stride,
                          rule.temperature_rows;
     const size_t bytes = (size_t)SW * short_words(q, mass, filters) * 4;
     auto kernel = mass ? k_sample_short<T, true> : k_sample_short<T, false>;
+    // the longest row's, whatever this one's: a limit of its own could undercut another thread's call
+    // between its setting and its launch
+    constexpr int most = SW * 4 * short_words(short_q(SHORT), true, true);
     if (bytes > 48 * 1024)
-      ERC_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes));
+      ERC_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, most));
     const int64_t blocks = (rows + SW - 1) / SW;
     kernel<<<(unsigned)(blocks < 0x7fffffff ? blocks : 0x7fffffff), SW * 32, bytes, s>>>(
         rows, (int)n, q, filters, logits, stride, words, rule, ids, logp, kept);

@@ -1,5 +1,8 @@
 """The row-wise choices at the ends of their ranges: scores below 2^-126, sums that cancel or overflow,
 calls from several threads, and arguments that do not fit."""
+import ctypes
+import threading
+
 import numpy as np
 import pytest
 import torch
@@ -8,7 +11,7 @@ from oracle import choice_oracle as C
 from paper_2609_27209_gb300 import erc
 
 from ._gpu import dev, host
-from .test_gpu_choice import TYPES, U, check_route, f32
+from .test_gpu_choice import TYPES, U, check_route, f32, words_of
 
 pytestmark = pytest.mark.gpu
 
@@ -136,3 +139,34 @@ def test_softmax_gradient_of_experts_far_below_the_best(E, renorm):
     bound = s / d * 2 * np.abs(g).sum(1, keepdims=True) * (5 * delta + (k + 8) * U)
     # renormalised weights do not depend on the other logits at all; results below 2^-126 may be rounded to 0
     assert np.all(np.abs(got - want) <= bound + 2.0**-126)
+
+
+def test_calls_from_several_threads():
+    # Rows of 1249 entries and more need more shared memory for top-p than a kernel has without asking.
+    # The library's calls alone, without the binding's work around them, meet most often.
+    rng = np.random.default_rng(3)
+    rows, jobs, errors = 320, [], []
+    rule = erc.ErcSampleRuleC(1.0, 0, 0.9, 0.0)
+    for n in (1536, 1300, 1249, 1400):
+        x = torch.from_numpy(rng.normal(size=(rows, n)).astype(np.float32)).to(dev())
+        w = torch.from_numpy(words_of(rng, rows)).to(dev())
+        jobs.append((x, w, erc.erc_sample_rows(x, w, top_p=0.9), torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    call = erc.lib().erc_sample_rows
+
+    def work(x, w, want, stream):
+        got = [torch.empty_like(t) for t in want]
+        torch.cuda.synchronize()
+        args = (rows, x.shape[1], x.data_ptr(), erc.ERC_F32, x.shape[1], w.data_ptr(), ctypes.byref(rule),
+                *(t.data_ptr() for t in got), stream.cuda_stream)
+        failed = sum(call(*args) != erc.ERC_OK for _ in range(5000))
+        stream.synchronize()
+        if failed or not all(torch.equal(a, b) for a, b in zip(got, want)):
+            errors.append(failed)
+
+    threads = [threading.Thread(target=work, args=job) for job in jobs]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not errors
