@@ -489,7 +489,8 @@ def erc_run_host(n, src, dst, w, params, ws=None, out=None):
 
 # ------------------------------------------------------------------------------------------------
 # row-wise choices: the argument checks that need the tensors' types, shapes and devices are made
-# here (the C entry points see raw pointers), and raise ErcError with ERC_ERR_INVALID_ARG
+# here (the C entry points see raw pointers), and raise ErcError with ERC_ERR_INVALID_ARG.  All tensors
+# are on the current device
 # ------------------------------------------------------------------------------------------------
 ERC_F32, ERC_BF16, ERC_F16 = 0, 1, 2
 ERC_SCORE_SOFTMAX, ERC_SCORE_SIGMOID = 0, 1
@@ -507,11 +508,18 @@ def _need(t, name, dtype, shape, device):
         _refuse(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)} on {device}")
 
 
+def _on_current_device(t, name):
+    """The library launches on the current device, whichever device a pointer or a stream belongs to."""
+    if t.device.index != torch.cuda.current_device():
+        _refuse(f"{name} is on {t.device}, which is not the current device")
+
+
 def _rows_of(t, name):
     """(rows, n, type, row stride) of a matrix of scores with unit element stride."""
     kind = _TYPES.get(t.dtype) if isinstance(t, torch.Tensor) and t.is_cuda else None
     if kind is None or t.dim() != 2:
         _refuse(f"{name} must be a 2-d float32, bfloat16 or float16 CUDA tensor")
+    _on_current_device(t, name)
     rows, n = t.shape
     stride, unit = t.stride()
     if n > 1 and unit != 1:
@@ -592,6 +600,7 @@ def erc_expert_plan(experts, n_experts, ws=None):
     [n_experts + 1], order int32 [rows * k], slot int32 [rows, k])."""
     if not (isinstance(experts, torch.Tensor) and experts.is_cuda and experts.dim() == 2):
         _refuse("experts must be a CUDA tensor [rows, k]")
+    _on_current_device(experts, "experts")
     rows, k = experts.shape
     dev = experts.device
     _need(experts, "experts", torch.int32, (rows, k), dev)
@@ -613,6 +622,7 @@ def _matrix(t, name):
     kind = _TYPES.get(t.dtype) if isinstance(t, torch.Tensor) and t.is_cuda else None
     if kind is None or t.dim() != 2 or not t.is_contiguous():
         _refuse(f"{name} must be a contiguous 2-d float32, bfloat16 or float16 CUDA tensor")
+    _on_current_device(t, name)
     return t.shape[0], t.shape[1], kind
 
 

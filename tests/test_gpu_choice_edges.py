@@ -11,7 +11,7 @@ from oracle import choice_oracle as C
 from paper_2609_27209_gb300 import erc
 
 from ._gpu import dev, host
-from .test_gpu_choice import TYPES, U, check_route, f32, words_of
+from .test_gpu_choice import TYPES, U, check_route, f32, refused, words_of
 
 pytestmark = pytest.mark.gpu
 
@@ -170,3 +170,28 @@ def test_calls_from_several_threads():
     for t in threads:
         t.join()
     assert not errors
+
+
+def every_call():
+    """Each operator with arguments that fit: (its name, the call)."""
+    x, w = torch.zeros(4, 8, device=dev()), torch.zeros(4, dtype=torch.int64, device=dev())
+    experts, weights = erc.erc_route(x, 2)
+    offsets, _, slot = erc.erc_expert_plan(experts, 8)
+    y = torch.zeros(8, 8, device=dev())
+    return [("sample_rows", lambda: erc.erc_sample_rows(x, w)),
+            ("route", lambda: erc.erc_route(x, 2)),
+            ("route_backward", lambda: erc.erc_route_backward(x, experts, weights)),
+            ("plan", lambda: erc.erc_expert_plan(experts, 8)),
+            ("gather", lambda: erc.erc_expert_gather(x, slot, offsets)),
+            ("combine", lambda: erc.erc_expert_combine(y, slot)),
+            ("combine_backward", lambda: erc.erc_expert_combine_backward(x, y, slot, offsets, weights))]
+
+
+def test_tensors_of_a_device_that_is_not_current_are_refused(monkeypatch):
+    calls = every_call()
+    for _, call in calls:
+        call()
+    torch.cuda.synchronize()
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
+    for _, call in calls:
+        refused(call)
