@@ -597,7 +597,8 @@ def erc_route_backward(logits, experts, dweights, score=ERC_SCORE_SOFTMAX, renor
 
 def erc_expert_plan(experts, n_experts, ws=None):
     """The pairs of experts int32 [rows, k] in expert order (see include/erc.h): (offsets int64
-    [n_experts + 1], order int32 [rows * k], slot int32 [rows, k])."""
+    [n_experts + 1], order int32 [rows * k], slot int32 [rows, k]).  ws: a uint8 workspace of
+    erc_expert_plan_workspace_size bytes, or None."""
     if not (isinstance(experts, torch.Tensor) and experts.is_cuda and experts.dim() == 2):
         _refuse("experts must be a CUDA tensor [rows, k]")
     _on_current_device(experts, "experts")
@@ -612,6 +613,9 @@ def erc_expert_plan(experts, n_experts, ws=None):
     if ws is None:
         need = lib().erc_expert_plan_workspace_size(rows, k, n_experts)
         ws = _workspace(need, dev) if need else None
+    elif not (isinstance(ws, torch.Tensor) and ws.dtype is torch.uint8 and ws.device == dev
+              and ws.is_contiguous()):
+        _refuse(f"ws must be a contiguous uint8 tensor on {dev}")
     _check(lib().erc_expert_plan(rows, k, n_experts, experts.data_ptr(), offsets.data_ptr(),
                                  order.data_ptr(), slot.data_ptr(), _ptr(ws),
                                  0 if ws is None else ws.numel(), _stream_of(experts)))

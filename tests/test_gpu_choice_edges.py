@@ -195,3 +195,11 @@ def test_tensors_of_a_device_that_is_not_current_are_refused(monkeypatch):
     monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
     for _, call in calls:
         refused(call)
+
+
+def test_plan_workspaces_that_do_not_fit_are_refused():
+    e = torch.zeros(4, 2, dtype=torch.int32, device=dev())  # so few pairs need no workspace: none is touched
+    erc.erc_expert_plan(e, 3, ws=torch.empty(64, dtype=torch.uint8, device=dev()))
+    for ws in (torch.empty(64, dtype=torch.uint8), torch.empty(64, device=dev()),
+               torch.empty(64, dtype=torch.uint8, device=dev())[::2], 64):
+        refused(lambda: erc.erc_expert_plan(e, 3, ws=ws))
