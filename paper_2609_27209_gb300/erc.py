@@ -508,6 +508,19 @@ def _need(t, name, dtype, shape, device):
         _refuse(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)} on {device}")
 
 
+def _whole(v, name):
+    """`v` as an int32; a ctypes field would wrap a number that does not fit."""
+    if type(v) is int and -2**31 <= v < 2**31:
+        return v
+    try:
+        n = int(v)
+    except (TypeError, ValueError, OverflowError):
+        n = None
+    if n is None or n != v or not -2**31 <= n < 2**31:
+        _refuse(f"{name} must be a whole number of 32 bits")
+    return n
+
+
 def _on_current_device(t, name):
     """The library launches on the current device, whichever device a pointer or a stream belongs to."""
     if t.device.index != torch.cuda.current_device():
@@ -550,7 +563,7 @@ def erc_sample_rows(logits, words, temperature=1.0, top_k=0, top_p=1.0, min_p=0.
             _need(v, name, dtype, (rows,), dev)
             setattr(rule, name + "_rows", v.data_ptr())
         elif name == "top_k":
-            rule.top_k = min(int(v), 2**31 - 1)
+            rule.top_k = _whole(2**31 - 1 if v >= 2**31 else v, name)
         else:
             setattr(rule, name, float(v))
     ids = torch.empty(rows, dtype=torch.int32, device=dev)
@@ -570,7 +583,10 @@ def erc_route(logits, k, score=ERC_SCORE_SOFTMAX, bias=None, groups=1, top_group
     dev = logits.device
     if bias is not None:
         _need(bias, "bias", torch.float32, (E,), dev)
-    rule = ErcRouteRuleC(E, k, score, groups, top_groups, group_best, int(bool(renorm)), scale)
+    k = _whole(k, "k")
+    rule = ErcRouteRuleC(_whole(E, "E"), k, _whole(score, "score"), _whole(groups, "groups"),
+                         _whole(top_groups, "top_groups"), _whole(group_best, "group_best"),
+                         int(bool(renorm)), scale)
     experts = torch.empty(rows, max(k, 0), dtype=torch.int32, device=dev)
     weights = torch.empty(rows, max(k, 0), dtype=torch.float32, device=dev)
     _check(lib().erc_route(rows, logits.data_ptr(), kind, stride, _ptr(bias), ctypes.byref(rule),
@@ -587,7 +603,7 @@ def erc_route_backward(logits, experts, dweights, score=ERC_SCORE_SOFTMAX, renor
     k = experts.shape[1]
     _need(experts, "experts", torch.int32, (rows, k), dev)
     _need(dweights, "dweights", torch.float32, (rows, k), dev)
-    rule = ErcRouteRuleC(E, k, score, 1, 1, 1, int(bool(renorm)), scale)
+    rule = ErcRouteRuleC(_whole(E, "E"), _whole(k, "k"), _whole(score, "score"), 1, 1, 1, int(bool(renorm)), scale)
     dlogits = torch.empty(rows, E, dtype=logits.dtype, device=dev)
     _check(lib().erc_route_backward(rows, logits.data_ptr(), kind, stride, experts.data_ptr(),
                                     dweights.data_ptr(), ctypes.byref(rule), dlogits.data_ptr(),
@@ -605,7 +621,8 @@ def erc_expert_plan(experts, n_experts, ws=None):
     rows, k = experts.shape
     dev = experts.device
     _need(experts, "experts", torch.int32, (rows, k), dev)
-    if not 0 < n_experts < 2**31:
+    k, n_experts = _whole(k, "k"), _whole(n_experts, "n_experts")
+    if n_experts < 1:
         _refuse("n_experts out of range")
     offsets = torch.empty(n_experts + 1, dtype=torch.int64, device=dev)
     order = torch.empty(rows * k, dtype=torch.int32, device=dev)
@@ -635,7 +652,7 @@ def _slots(slot, rows, dev):
         _refuse("slot must be [rows, k]")
     rows = slot.shape[0] if rows is None else rows
     _need(slot, "slot", torch.int32, (rows, slot.shape[1]), dev)
-    return rows, slot.shape[1]
+    return rows, _whole(slot.shape[1], "k")
 
 
 def _placed(offsets, dev):

@@ -203,3 +203,17 @@ def test_plan_workspaces_that_do_not_fit_are_refused():
     for ws in (torch.empty(64, dtype=torch.uint8), torch.empty(64, device=dev()),
                torch.empty(64, dtype=torch.uint8, device=dev())[::2], 64):
         refused(lambda: erc.erc_expert_plan(e, 3, ws=ws))
+
+
+def test_whole_numbers_that_do_not_fit_are_refused():
+    x, w = torch.zeros(4, 8, device=dev()), torch.zeros(4, dtype=torch.int64, device=dev())
+    for top_k in (-1, -(2**31), -(2**32), -(2**32) + 5, 0.5, float("nan")):
+        refused(lambda: erc.erc_sample_rows(x, w, top_k=top_k))
+    assert host(erc.erc_sample_rows(x, w, top_k=2**40)[2]).tolist() == [8] * 4  # more than there are: all
+    assert host(erc.erc_sample_rows(x, w, top_k=3.0)[2]).tolist() == [3] * 4
+    for bad in (dict(score=2**32), dict(groups=2**32 + 1), dict(groups=2, top_groups=2**32 + 1),
+                dict(group_best=2**32 + 1), dict(groups=1.5)):
+        refused(lambda: erc.erc_route(x, 2, **bad))
+    refused(lambda: erc.erc_route(x[:0], 2**32 + 2))
+    experts, weights = erc.erc_route(x, 2)
+    refused(lambda: erc.erc_route_backward(x, experts, weights, score=2**32 + 1))
