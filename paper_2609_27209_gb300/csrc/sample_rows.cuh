@@ -789,15 +789,15 @@ __device__ void nucleus(S& s, const Row<T>& r, const RowRule& rule, const Team<S
   } else {
     each_vector(r, r.begin(warp), stop, [&](uint4 u, int) {
       const float best = max_score(u, T());
-      if (!(r.scaled(best) > low)) return;
+      if (!(r.scaled(best) >= r.tmin)) return;
       float l[N];
       r.scores(u, l);
 #pragma unroll
       for (int i = 0; i < N; ++i) {
         const float t = r.scaled(l[i]);
-        const unsigned long long w = t > low ? r.weight(l[i]) : 0ull;
-        mass += w;
-        if (w) atomicAdd(&s.wbins[__float_as_uint(__fmaf_rz(t, -(float)S::STEPS, 8388608.f)) - BIAS], 1u);
+        const unsigned long long w = t >= r.tmin ? r.weight(l[i]) : 0ull;
+        mass += w;  // what is too light to be counted belongs to the sum all the same
+        if (w && t > low) atomicAdd(&s.wbins[__float_as_uint(__fmaf_rz(t, -(float)S::STEPS, 8388608.f)) - BIAS], 1u);
       }
     });
   }

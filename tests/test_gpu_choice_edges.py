@@ -11,7 +11,7 @@ from oracle import choice_oracle as C
 from paper_2609_27209_gb300 import erc
 
 from ._gpu import dev, host
-from .test_gpu_choice import TYPES, U, check_route, f32, refused, words_of
+from .test_gpu_choice import TYPES, U, check_route, check_sample, f32, refused, words_of
 
 pytestmark = pytest.mark.gpu
 
@@ -139,6 +139,23 @@ def test_softmax_gradient_of_experts_far_below_the_best(E, renorm):
     bound = s / d * 2 * np.abs(g).sum(1, keepdims=True) * (5 * delta + (k + 8) * U)
     # renormalised weights do not depend on the other logits at all; results below 2^-126 may be rounded to 0
     assert np.all(np.abs(got - want) <= bound + 2.0**-126)
+
+
+@pytest.mark.parametrize("rows,n", [(3, 4100), (200, 4100), (400, 1500), (2, 70001)])
+@pytest.mark.parametrize("kind", list(TYPES))
+def test_top_p_counts_what_a_small_min_p_keeps(rows, n, kind):
+    # One entry of weight 1, 2000 (or half the row) of 2^-12, the rest far lighter, each below an eighth of
+    # (1 - top_p) / n but well above min_p: together they move top_p's target by tens of the second kind.
+    rng = np.random.default_rng(n)
+    p = 0.8
+    light = np.log2((1 - p) / n) - 3.6
+    x = np.full((rows, n), light * np.log(2), np.float32)
+    for row in x:
+        at = rng.permutation(n)
+        row[at[: min(2000, n // 2)]] = -12 * np.log(2)
+        row[at[0]] = 0
+    check_sample(torch.from_numpy(x).to(dev()).to(TYPES[kind]), words_of(rng, rows), every=max(1, rows // 4),
+                 top_p=p, min_p=1e-9)
 
 
 def test_calls_from_several_threads():
