@@ -1205,8 +1205,6 @@ __device__ int by_codes(S& s, Row<T>& r, const RowRule& rule, const Team<SOLO>& 
     const unsigned w[4] = {u.x, u.y, u.z, u.w};
     const float best = max_score(u, T());
     if (!(best >= theta)) return;
-    float l[8];
-    r.scores(u, l);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       int a;
