@@ -394,6 +394,7 @@ erc_status erc_route_backward(int64_t rows, const void* logits, int32_t type, in
  *      NULL: 1), summed in float32 in the order of j and rounded once; 0 for a row without pairs.
  * erc_expert_combine_backward -- dy[slot[t, j]] = weights[t, j] dout[t], zeros from *placed on, and
  *      dweights[t, j] = dout[t] . y[slot[t, j]] (float32 sums; 0 for no pair).
+ *      Without weights the gradient of erc_expert_combine is erc_expert_gather of dout.
  * slot must come from erc_expert_plan (every value below rows * k, none twice).  Row-major dense
  * arrays of `type`; weights and dweights float32.  Errors: INVALID_ARG.  Deterministic.
  * ------------------------------------------------------------------------------------------- */

@@ -417,8 +417,8 @@ __device__ __forceinline__ int candidates(const float* c, int k, int first, floa
 //
 // A warp takes rows in turn, its biases in registers and the next row on its way.
 //
-// E = 256, k = 8, four of eight groups, sigmoid with bias, 32,768 rows of bf16: 31 us, issue-bound at
-// about 750 instructions a row; k rounds over exact scores took 55 us (1505 instructions).
+// E = 256, k = 8, four of eight groups, sigmoid with bias, 32,768 rows of bf16: 32 us, 761 instructions a
+// row, issued in 0.60 of the cycles; k rounds over exact scores took 55 us (1505 instructions).
 template <class T, int V, bool SIGMOID>
 __global__ void __launch_bounds__(FW * 32, V == 8 ? 4 : V == 16 ? 2 : 1)
     k_route_warp(int64_t rows, const T* __restrict__ logits, int64_t stride,
@@ -514,11 +514,12 @@ __global__ void __launch_bounds__(FW * 32, V == 8 ? 4 : V == 16 ? 2 : 1)
 
 // The gradient of the row's weights.  Where nothing is chosen it is -s_i gs for softmax, with
 // gs = sum ds s (0 in exact arithmetic when renormalised), and 0 for sigmoid, whose rows are then not
-// read at all; the lanes that hold a chosen expert's gradient store it over that.  Results here are
-// rounded to the output's type, so the exponential is the hardware's.
+// read at all; the lanes that hold a chosen expert's gradient store it over that.  The chosen experts'
+// 2^t is the forward pass's; the others', and Z, take the hardware's exponential (2^-22 of itself) and
+// float32 sums.  169,343 x 64 f32: relative error 1.9e-7 against 64 bits, 1.2e-7 for plain float32 steps.
 //
-// 169,343 rows of 64 f32, two experts each, softmax: 24 us, 3.8 TB/s; the chain of a row (choices,
-// scores, two reductions) at full occupancy is what is left.
+// 169,343 rows of 64 f32, two experts each, softmax: 22.5 us, 4.0 TB/s; the chain of a row (choices,
+// scores, two reductions) is what is left.
 template <class T, int L, int V, bool SIGMOID>
 __global__ void __launch_bounds__(FW * 32)
     k_route_lanes_backward(int64_t rows, const T* __restrict__ logits, int64_t stride,

@@ -490,7 +490,8 @@ def erc_run_host(n, src, dst, w, params, ws=None, out=None):
 # ------------------------------------------------------------------------------------------------
 # row-wise choices: the argument checks that need the tensors' types, shapes and devices are made
 # here (the C entry points see raw pointers), and raise ErcError with ERC_ERR_INVALID_ARG.  All tensors
-# are on the current device
+# are on the current device.  Results carry no autograd history: a caller that differentiates wraps
+# a call and its gradient in a torch.autograd.Function
 # ------------------------------------------------------------------------------------------------
 ERC_F32, ERC_BF16, ERC_F16 = 0, 1, 2
 ERC_SCORE_SOFTMAX, ERC_SCORE_SIGMOID = 0, 1
@@ -674,7 +675,8 @@ def erc_expert_gather(x, slot, offsets):
 
 
 def erc_expert_combine(y, slot, weights=None):
-    """The weighted sum over each row's pairs of y [rows * k, width]: out [rows, width]."""
+    """The weighted sum over each row's pairs of y [rows * k, width]: out [rows, width].  The gradient
+    is erc_expert_combine_backward, or erc_expert_gather(dout, slot, offsets) where weights is None."""
     slots, width, kind = _matrix(y, "y")
     rows, k = _slots(slot, None, y.device)
     if slots != rows * k:
