@@ -412,6 +412,108 @@ erc_status erc_expert_combine_backward(int64_t rows, int32_t k, int64_t width, c
                                        float* dweights, erc_stream s);
 
 /* ---------------------------------------------------------------------------------------------
+ * erc_score_rows -- what each row of scores says about a given entry, with its best alternatives.
+ *
+ * With t_i = (l_i - m) / temperature, m the row's maximum, and Z = sum_i e^(t_i):
+ *   logp[row]    = t_id - ln Z, id = ids[row]: the logarithm of the entry's probability; 0 for an id
+ *                  outside [0, n) (a position that counts for nothing), -inf for a masked entry;
+ *   entropy[row] = ln Z - sum_i e^(t_i) t_i / Z = -sum_i p_i ln p_i; 0 where every entry is masked;
+ *   norm[row]    = (m, ln Z), which the gradient takes; (-inf, -inf) where every entry is masked;
+ *   top_ids, top_logp [rows x k]: the k best entries, by score descending, then index ascending,
+ *                  and their log probabilities; -1 and -inf where fewer are not masked.
+ * NaN and -inf are masked entries; -0 equals +0; where m is +inf only the entries that equal it have
+ * a probability.  Sums are float32, in an order that does not change: deterministic.
+ * In : logits [rows x n] of `type`, n <= ERC_SAMPLE_ROWS_MAX_N; ids [rows], or NULL with logp NULL;
+ *      temperature finite, at least 2^-126; k in [0, ERC_SCORE_MAX_K].
+ * Out: logp (NULL without ids), entropy, norm may each be NULL; top_ids and top_logp only with k.
+ * Workspace: erc_score_rows_workspace_size(rows, n, type, k) bytes on the current device (0 for many
+ *      or short rows); calls that overlap on the GPU need one each.
+ * erc_score_rows_backward -- from dlogp and dentropy [rows] (either may be NULL: 0) to
+ *      dlogits_i = ((i == id) dlogp - p_i (dlogp + dentropy (ln p_i + entropy))) / temperature,
+ *      [rows x n] dense rows of `type`, rounded once; masked entries get 0.  norm and entropy are
+ *      the forward call's (entropy and ids may be NULL when their gradient is).  An id outside
+ *      [0, n) or a masked one adds nothing; the alternatives have no gradient.
+ * Errors: INVALID_ARG for sizes, types, pointers, a temperature or k out of range; CAPACITY if
+ *      ws_bytes is too small.
+ * ------------------------------------------------------------------------------------------- */
+#define ERC_SCORE_MAX_K 32
+size_t erc_score_rows_workspace_size(int64_t rows, int64_t n, int32_t type, int32_t k);
+erc_status erc_score_rows(int64_t rows, int64_t n, const void* logits, int32_t type, int64_t stride,
+                          const int32_t* ids, float temperature, int32_t k, float* logp,
+                          float* entropy, float* norm, int32_t* top_ids, float* top_logp, void* ws,
+                          size_t ws_bytes, erc_stream s);
+erc_status erc_score_rows_backward(int64_t rows, int64_t n, const void* logits, int32_t type,
+                                   int64_t stride, const int32_t* ids, float temperature,
+                                   const float* norm, const float* entropy, const float* dlogp,
+                                   const float* dentropy, void* dlogits, erc_stream s);
+
+/* ---------------------------------------------------------------------------------------------
+ * erc_expert_ffn -- the gated feed-forward block of each expert on its rows (between
+ * erc_expert_gather and erc_expert_combine; a dense block is one expert).
+ *
+ * For slot s of expert e (offsets[e] <= s < offsets[e + 1]), x = xs[s]:
+ *   a = w_in[e][0 .. inner) x,  b = w_in[e][inner .. 2 inner) x,  y[s] = w_out[e] (act(a) b).
+ * act is ERC_ACT_SILU a / (1 + e^-a), ERC_ACT_GELU a (1 + erf(a / sqrt 2)) / 2 or ERC_ACT_RELU.
+ * In : xs [slots x width]; offsets [experts + 1] (device; from erc_expert_plan, or any ascending
+ *      offsets in [0, slots] that start at 0); w_in [experts x 2 inner x width] (rows of gates, then
+ *      rows of factors), w_out [experts x width x inner], all dense of `type`.
+ * Out: y [slots x width]; pre [slots x 2 inner] = (a, b), or NULL when no gradient is wanted.  Rows
+ *      from offsets[experts] on are zeroed in both.
+ * Sums are float32; a, b and act(a) b are rounded to `type` once, and so is y.
+ * erc_expert_ffn_backward -- from dy [slots x width], xs, pre and the weights to dxs [slots x width],
+ *      dw_in and dw_out (each may be NULL), rounded to `type` once; act(a) b and the gradients of a
+ *      and b, formed from the rounded pre and float32 sums, are rounded once too.  dxs is zeroed from
+ *      offsets[experts] on, the weights' gradients where an expert has no rows.  Contents of xs, pre
+ *      and dy behind offsets[experts] do not matter.
+ * Limits: width and inner in [1, ERC_FFN_MAX_WIDTH], experts in [1, ERC_ROUTE_MAX_EXPERTS], slots in
+ *      [0, 2^31).  bfloat16 and float16 with width and inner that are multiples of 8 and 16-byte
+ *      aligned arrays use the tensor cores; everything else runs on the float32 units.
+ * Workspace: erc_expert_ffn_workspace_size and erc_expert_ffn_backward_workspace_size bytes; calls
+ *      that overlap on the GPU need one each.
+ * Errors: INVALID_ARG for sizes, types, alignment and pointers; CAPACITY for a small workspace.
+ *      Deterministic.
+ * ------------------------------------------------------------------------------------------- */
+enum { ERC_ACT_SILU = 0, ERC_ACT_GELU = 1, ERC_ACT_RELU = 2 };
+#define ERC_FFN_MAX_WIDTH 65536
+typedef struct erc_ffn_shape {
+  int64_t slots;   /* rows of xs */
+  int32_t experts;
+  int32_t width;   /* of xs and y */
+  int32_t inner;   /* of act(a) b */
+  int32_t act;     /* ERC_ACT_* */
+  int32_t type;    /* ERC_F32, ERC_BF16 or ERC_F16: rows, weights, results */
+} erc_ffn_shape;
+size_t erc_expert_ffn_workspace_size(const erc_ffn_shape* shape);
+erc_status erc_expert_ffn(const erc_ffn_shape* shape, const void* xs, const int64_t* offsets,
+                          const void* w_in, const void* w_out, void* y, void* pre, void* ws,
+                          size_t ws_bytes, erc_stream s);
+size_t erc_expert_ffn_backward_workspace_size(const erc_ffn_shape* shape);
+erc_status erc_expert_ffn_backward(const erc_ffn_shape* shape, const void* dy, const void* xs,
+                                   const void* pre, const int64_t* offsets, const void* w_in,
+                                   const void* w_out, void* dxs, void* dw_in, void* dw_out,
+                                   void* ws, size_t ws_bytes, erc_stream s);
+
+/* ---------------------------------------------------------------------------------------------
+ * erc_dropout -- out[e] = (keep(e) ? x[e] * scale : 0) + residual[e], from a counter-based generator:
+ * the mask is never stored, and the gradient of x is the same call on out's gradient, without the
+ * residual.
+ *
+ * Entry e of the call is number i = first + e of the stream: keep(i) holds when word i mod 4 of
+ * Philox4x32-10 with the given key and counter (i div 4 lo, i div 4 hi, 0x44524F50, 0) is at least
+ * floor(p 2^32).  scale is 1 / (1 - p) rounded to float32; product and sum are rounded to float32 one
+ * by one, the result once to `type`, so it is the same on every machine.  What is dropped is 0
+ * whatever x holds.
+ * In : x, residual (or NULL) [count] of `type`; p in [0, 1] (1 drops everything); key, or key_dev
+ *      (device, [1]) when not NULL: a captured graph that is replayed reads the key of its time;
+ *      first >= 0, a multiple of 4.
+ * Out: out [count] of `type`; may be x or residual itself.
+ * Errors: INVALID_ARG for sizes, types, p, first, pointers or alignment.  Deterministic.
+ * ------------------------------------------------------------------------------------------- */
+erc_status erc_dropout(int64_t count, const void* x, int32_t type, const void* residual, double p,
+                       uint64_t key, const uint64_t* key_dev, int64_t first, void* out,
+                       erc_stream s);
+
+/* ---------------------------------------------------------------------------------------------
  * erc_laplacian_apply -- AP = L_eps P for an n x ld block (the CG operator of Eq. 5), and, when
  * pAp is not NULL, pAp[c] = sum_u P[u,c] AP[u,c] as float64 (device [kc]).  Exposed for testing
  * and benchmarking the operator alone.

@@ -1,0 +1,363 @@
+// expert_ffn.cu -- the gated feed-forward block of experts: the C entry points, and its products on
+// the float32 units, for every type and size (the tensor cores take the 16-bit types whose rows are
+// whole 16-byte pieces, expert_ffn_tc.cu).
+//
+// A product is C(i, j) = sum_k A(i, k) B(j, k) in tiles of 64 x 64 by 16: a thread keeps 4 x 4 sums in
+// registers (two sets where gates and factors share the rows).  Sums run over k in order.
+#include <initializer_list>
+
+#include "expert_ffn.cuh"
+
+namespace erc {
+namespace {
+
+constexpr int FT = 256;  // threads
+constexpr int FM = 64;   // tile
+constexpr int FK = 16;
+
+// an operand: element (i, k) at p[i * row + k * step]; i in [0, rows), k in [0, depth)
+template <class T>
+struct Operand {
+  const T* p;
+  int64_t row, step;
+  int64_t rows;
+};
+
+// FM x FK elements from row i0 and depth k0 on; CONTIG: whether k is the contiguous index
+template <class T, bool CONTIG>
+__device__ __forceinline__ void load_tile(const Operand<T>& a, int64_t i0, int64_t k0, int64_t depth, float* r) {
+#pragma unroll
+  for (int j = 0; j < FM * FK / FT; ++j) {
+    const int i = CONTIG ? threadIdx.x / FK + j * (FT / FK) : threadIdx.x % FM;
+    const int k = CONTIG ? threadIdx.x % FK : threadIdx.x / FM + j * (FT / FM);
+    r[j] = i0 + i < a.rows && k0 + k < depth ? to_f32(a.p[(i0 + i) * a.row + (k0 + k) * a.step]) : 0.f;
+  }
+}
+template <bool CONTIG>
+__device__ __forceinline__ void keep_tile(float (*s)[FM + 4], const float* r) {
+#pragma unroll
+  for (int j = 0; j < FM * FK / FT; ++j) {
+    const int i = CONTIG ? threadIdx.x / FK + j * (FT / FK) : threadIdx.x % FM;
+    const int k = CONTIG ? threadIdx.x % FK : threadIdx.x / FM + j * (FT / FM);
+    s[k][i] = r[j];
+  }
+}
+
+template <int NB>
+struct Tiles {
+  float a[FK][FM + 4];
+  float b[NB][FK][FM + 4];
+};
+
+// the thread's 4 x 4 sums of one or two products that share A: rows i0 + 4 (tid / 16) + ., columns
+// j0 + 4 (tid % 16) + .
+template <class T, bool CA, bool CB, int NB>
+__device__ __forceinline__ void product(Tiles<NB>& s, const Operand<T>& a, const Operand<T>* b, int64_t i0, int64_t j0,
+                                        int64_t depth, float (*acc)[4][4]) {
+  const int ty = threadIdx.x / 16, tx = threadIdx.x % 16;
+#pragma unroll
+  for (int q = 0; q < NB; ++q)
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) acc[q][i][j] = 0.f;
+  float ra[FM * FK / FT], rb[NB][FM * FK / FT];
+  load_tile<T, CA>(a, i0, 0, depth, ra);
+#pragma unroll
+  for (int q = 0; q < NB; ++q) load_tile<T, CB>(b[q], j0, 0, depth, rb[q]);
+  for (int64_t k0 = 0; k0 < depth; k0 += FK) {
+    keep_tile<CA>(s.a, ra);
+#pragma unroll
+    for (int q = 0; q < NB; ++q) keep_tile<CB>(s.b[q], rb[q]);
+    __syncthreads();
+    if (k0 + FK < depth) {
+      load_tile<T, CA>(a, i0, k0 + FK, depth, ra);
+#pragma unroll
+      for (int q = 0; q < NB; ++q) load_tile<T, CB>(b[q], j0, k0 + FK, depth, rb[q]);
+    }
+#pragma unroll
+    for (int k = 0; k < FK; ++k) {
+      const float4 va = *reinterpret_cast<const float4*>(&s.a[k][4 * ty]);
+      const float xa[4] = {va.x, va.y, va.z, va.w};
+#pragma unroll
+      for (int q = 0; q < NB; ++q) {
+        const float4 vb = *reinterpret_cast<const float4*>(&s.b[q][k][4 * tx]);
+        const float xb[4] = {vb.x, vb.y, vb.z, vb.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) acc[q][i][j] = fmaf(xa[i], xb[j], acc[q][i][j]);
+      }
+    }
+    __syncthreads();
+  }
+}
+
+// the expert and rows of the t-th tile of 64 slots, experts one after another; false past the last
+__device__ __forceinline__ bool find_tile(const int64_t* offsets, int experts, int64_t slots, int64_t t, int& expert,
+                                          SlotRange& rows) {
+  __shared__ int64_t warp_sum[FT / 32];
+  __shared__ int found;
+  __shared__ int64_t before_found;
+  constexpr int PER = ERC_ROUTE_MAX_EXPERTS / FT;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  int64_t count[PER], sum = 0;
+#pragma unroll
+  for (int j = 0; j < PER; ++j) {
+    const int e = threadIdx.x * PER + j;
+    count[j] = 0;
+    if (e < experts) {
+      const SlotRange r = slot_range(offsets, e, slots);
+      count[j] = (r.hi - r.lo + FM - 1) / FM;
+    }
+    sum += count[j];
+  }
+  int64_t upto = sum;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int64_t y = __shfl_up_sync(0xffffffffu, upto, o);
+    if (lane >= o) upto += y;
+  }
+  if (threadIdx.x == 0) found = -1;
+  if (lane == 31) warp_sum[warp] = upto;
+  __syncthreads();
+  int64_t before = upto - sum;
+  for (int w = 0; w < warp; ++w) before += warp_sum[w];
+#pragma unroll
+  for (int j = 0; j < PER; ++j) {
+    if (t >= before && t < before + count[j]) {
+      found = threadIdx.x * PER + j;
+      before_found = before;
+    }
+    before += count[j];
+  }
+  __syncthreads();
+  if (found < 0) return false;
+  expert = found;
+  rows = slot_range(offsets, expert, slots);
+  rows.lo += (t - before_found) * FM;
+  return true;
+}
+
+// rows of a tile of slots against all columns of a weight matrix
+template <class T, int WHICH>
+__global__ void __launch_bounds__(FT) k_ffn_slots(const FfnArgs<T> p) {
+  constexpr int NB = WHICH == FFN_IN ? 2 : 1;
+  __shared__ Tiles<NB> s;
+  const int64_t D = p.width, F = p.inner;
+  if (WHICH != FFN_DH) {
+    const int64_t used = slots_used(p.offsets, p.experts, p.slots);
+    const int64_t thread = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * FT + threadIdx.x;
+    const int64_t threads = (int64_t)gridDim.x * gridDim.y * FT;
+    if (WHICH == FFN_IN && p.pre) zero_slots(p.pre, used, p.slots, 2 * F, thread, threads);
+    if (WHICH == FFN_OUT) zero_slots(p.y, used, p.slots, D, thread, threads);
+    if (WHICH == FFN_DX) zero_slots(p.dx, used, p.slots, D, thread, threads);
+  }
+  int e;
+  SlotRange r;
+  if (!find_tile(p.offsets, p.experts, p.slots, blockIdx.x, e, r)) return;
+  const int64_t j0 = (int64_t)blockIdx.y * FM;
+  float acc[NB][4][4];
+  Operand<T> b[NB];
+  if constexpr (WHICH == FFN_IN) {
+    const Operand<T> a = {p.x, D, 1, r.hi};
+    const T* w = p.w_in + e * 2 * F * D;
+    b[0] = {w, D, 1, F};
+    b[1] = {w + F * D, D, 1, F};
+    product<T, true, true, 2>(s, a, b, r.lo, j0, D, acc);
+  } else if constexpr (WHICH == FFN_OUT) {
+    const Operand<T> a = {p.h, F, 1, r.hi};
+    b[0] = {p.w_out + e * D * F, F, 1, D};
+    product<T, true, true, 1>(s, a, b, r.lo, j0, F, acc);
+  } else if constexpr (WHICH == FFN_DH) {
+    const Operand<T> a = {p.dy, D, 1, r.hi};
+    b[0] = {p.w_out + e * D * F, 1, F, F};
+    product<T, true, false, 1>(s, a, b, r.lo, j0, D, acc);
+  } else {
+    const Operand<T> a = {p.dpre, 2 * F, 1, r.hi};
+    b[0] = {p.w_in + e * 2 * F * D, 1, D, D};
+    product<T, true, false, 1>(s, a, b, r.lo, j0, 2 * F, acc);
+  }
+  const int ty = threadIdx.x / 16, tx = threadIdx.x % 16;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int64_t row = r.lo + 4 * ty + i;
+    if (row >= r.hi) break;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int64_t col = j0 + 4 * tx + j;
+      const float v = acc[0][i][j];
+      if constexpr (WHICH == FFN_IN) {
+        if (col >= F) continue;
+        const float u = acc[NB - 1][i][j];
+        p.h[row * F + col] = from_f32<T>(act_value(p.act, v) * u);
+        if (p.pre) {
+          p.pre[row * 2 * F + col] = from_f32<T>(v);
+          p.pre[row * 2 * F + F + col] = from_f32<T>(u);
+        }
+      } else if constexpr (WHICH == FFN_DH) {
+        if (col >= F) continue;
+        const float g = to_f32(p.pre_in[row * 2 * F + col]), u = to_f32(p.pre_in[row * 2 * F + F + col]);
+        float value, slope;
+        act_both(p.act, g, value, slope);
+        p.dpre[row * 2 * F + col] = from_f32<T>(v * u * slope);
+        p.dpre[row * 2 * F + F + col] = from_f32<T>(v * value);
+        if (p.h) p.h[row * F + col] = from_f32<T>(value * u);
+      } else {
+        if (col < D) (WHICH == FFN_OUT ? p.y : p.dx)[row * D + col] = from_f32<T>(v);
+      }
+    }
+  }
+}
+
+// a tile of an expert's weight gradient: the sum over its slots
+template <class T, int WHICH>
+__global__ void __launch_bounds__(FT) k_ffn_weights(const FfnArgs<T> p) {
+  __shared__ Tiles<1> s;
+  const int64_t D = p.width, F = p.inner;
+  const int e = blockIdx.z;
+  const SlotRange r = slot_range(p.offsets, e, p.slots);
+  const int64_t i0 = (int64_t)blockIdx.y * FM, j0 = (int64_t)blockIdx.x * FM;
+  const int64_t rows = WHICH == FFN_DWIN ? 2 * F : D, cols = WHICH == FFN_DWIN ? D : F;
+  const Operand<T> a = {(WHICH == FFN_DWIN ? p.dpre : p.dy) + r.lo * rows, 1, rows, rows};
+  const Operand<T> b = {(WHICH == FFN_DWIN ? p.x : p.h) + r.lo * cols, 1, cols, cols};
+  float acc[1][4][4];
+  product<T, false, false, 1>(s, a, &b, i0, j0, r.hi - r.lo, acc);
+  T* out = (WHICH == FFN_DWIN ? p.dw_in : p.dw_out) + e * rows * cols;
+  const int ty = threadIdx.x / 16, tx = threadIdx.x % 16;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int64_t row = i0 + 4 * ty + i, col = j0 + 4 * tx + j;
+      if (row < rows && col < cols) out[row * cols + col] = from_f32<T>(acc[0][i][j]);
+    }
+}
+
+template <class T>
+erc_status simple_product(FfnProduct which, const FfnArgs<T>& p, cudaStream_t s) {
+  const int64_t tiles = p.slots / FM + (p.experts < p.slots ? p.experts : p.slots);
+  const unsigned wide = (p.width + FM - 1) / FM, deep = (p.inner + FM - 1) / FM, both = (2 * p.inner + FM - 1) / FM;
+  const unsigned rows = (unsigned)(tiles > 0 ? tiles : 1);
+  switch (which) {
+    case FFN_IN: k_ffn_slots<T, FFN_IN><<<dim3(rows, deep), FT, 0, s>>>(p); break;
+    case FFN_OUT: k_ffn_slots<T, FFN_OUT><<<dim3(rows, wide), FT, 0, s>>>(p); break;
+    case FFN_DH: k_ffn_slots<T, FFN_DH><<<dim3(rows, deep), FT, 0, s>>>(p); break;
+    case FFN_DX: k_ffn_slots<T, FFN_DX><<<dim3(rows, wide), FT, 0, s>>>(p); break;
+    case FFN_DWIN: k_ffn_weights<T, FFN_DWIN><<<dim3(wide, both, p.experts), FT, 0, s>>>(p); break;
+    case FFN_DWOUT: k_ffn_weights<T, FFN_DWOUT><<<dim3(deep, wide, p.experts), FT, 0, s>>>(p); break;
+  }
+  count_launches(1);
+  ERC_CUDA(cudaGetLastError());
+  return ERC_OK;
+}
+
+template <class T>
+erc_status ffn_product(bool tensor_cores, FfnProduct which, const FfnArgs<T>& p, cudaStream_t s) {
+  (void)tensor_cores;
+  return simple_product(which, p, s);
+}
+
+erc_status check_shape(const erc_ffn_shape* f) {
+  ERC_REQUIRE(f, "shape is required");
+  ERC_REQUIRE(f->type >= ERC_F32 && f->type <= ERC_F16, "bad type %d", f->type);
+  ERC_REQUIRE(f->act >= ERC_ACT_SILU && f->act <= ERC_ACT_RELU, "bad act %d", f->act);
+  ERC_REQUIRE(f->slots >= 0 && f->slots <= 0x7fffffffLL, "slots must be in [0, 2^31)");
+  ERC_REQUIRE(f->experts >= 1 && f->experts <= ERC_ROUTE_MAX_EXPERTS, "experts must be in [1, %d]", ERC_ROUTE_MAX_EXPERTS);
+  ERC_REQUIRE(f->width >= 1 && f->width <= ERC_FFN_MAX_WIDTH && f->inner >= 1 && f->inner <= ERC_FFN_MAX_WIDTH,
+              "width and inner must be in [1, %d]", ERC_FFN_MAX_WIDTH);
+  return ERC_OK;
+}
+bool good_shape(const erc_ffn_shape* f) {
+  return f && f->type >= ERC_F32 && f->type <= ERC_F16 && f->slots >= 0 && f->slots <= 0x7fffffffLL && f->experts >= 1 &&
+         f->experts <= ERC_ROUTE_MAX_EXPERTS && f->width >= 1 && f->width <= ERC_FFN_MAX_WIDTH && f->inner >= 1 &&
+         f->inner <= ERC_FFN_MAX_WIDTH;
+}
+uintptr_t any_bits(std::initializer_list<const void*> all) {
+  uintptr_t v = 0;
+  for (const void* p : all) v |= reinterpret_cast<uintptr_t>(p);
+  return v;
+}
+void* align_ws(void* ws) {
+  return reinterpret_cast<void*>((reinterpret_cast<uintptr_t>(ws) + 255) & ~uintptr_t(255));
+}
+
+}  // namespace
+}  // namespace erc
+
+using namespace erc;
+
+extern "C" size_t erc_expert_ffn_workspace_size(const erc_ffn_shape* f) {
+  if (!good_shape(f)) return 0;
+  return (size_t)f->slots * f->inner * type_bytes(f->type) + 512;
+}
+
+extern "C" erc_status erc_expert_ffn(const erc_ffn_shape* f, const void* xs, const int64_t* offsets, const void* w_in,
+                                     const void* w_out, void* y, void* pre, void* ws, size_t ws_bytes,
+                                     erc_stream stream) {
+  clear_error();
+  ERC_TRY(check_shape(f));
+  if (f->slots == 0) return ERC_OK;
+  ERC_REQUIRE(xs && offsets && w_in && w_out && y, "null pointer");
+  const uintptr_t all = any_bits({xs, w_in, w_out, y, pre});
+  ERC_REQUIRE(all % type_bytes(f->type) == 0 && reinterpret_cast<uintptr_t>(offsets) % 8 == 0, "misaligned array");
+  if (!ws || ws_bytes < erc_expert_ffn_workspace_size(f)) return set_error(ERC_ERR_CAPACITY, "workspace too small");
+  return with_type(f->type, [&](auto t) {
+    using T = decltype(t);
+    Arena ar(align_ws(ws));
+    FfnArgs<T> p = {f->slots, f->experts, f->width, f->inner, f->act, offsets};
+    p.x = static_cast<const T*>(xs);
+    p.w_in = static_cast<const T*>(w_in);
+    p.w_out = static_cast<const T*>(w_out);
+    p.h = ar.take<T>((size_t)f->slots * f->inner);
+    p.pre = static_cast<T*>(pre);
+    p.y = static_cast<T*>(y);
+    ERC_TRY(ffn_product(false, FFN_IN, p, as_stream(stream)));
+    return ffn_product(false, FFN_OUT, p, as_stream(stream));
+  });
+}
+
+extern "C" size_t erc_expert_ffn_backward_workspace_size(const erc_ffn_shape* f) {
+  if (!good_shape(f)) return 0;
+  return (size_t)f->slots * f->inner * 3 * type_bytes(f->type) + 1024;
+}
+
+extern "C" erc_status erc_expert_ffn_backward(const erc_ffn_shape* f, const void* dy, const void* xs, const void* pre,
+                                              const int64_t* offsets, const void* w_in, const void* w_out, void* dxs,
+                                              void* dw_in, void* dw_out, void* ws, size_t ws_bytes, erc_stream stream) {
+  clear_error();
+  ERC_TRY(check_shape(f));
+  if (!dxs && !dw_in && !dw_out) return ERC_OK;
+  const cudaStream_t s = as_stream(stream);
+  if (f->slots == 0) {
+    const size_t bytes = (size_t)f->experts * f->width * f->inner * type_bytes(f->type);
+    if (dw_in) ERC_CUDA(cudaMemsetAsync(dw_in, 0, 2 * bytes, s));
+    if (dw_out) ERC_CUDA(cudaMemsetAsync(dw_out, 0, bytes, s));
+    return ERC_OK;
+  }
+  ERC_REQUIRE(dy && pre && offsets && (w_out || !(dxs || dw_in)) && (xs || !dw_in) && (w_in || !dxs), "null pointer");
+  const uintptr_t all = any_bits({dy, xs, pre, w_in, w_out, dxs, dw_in, dw_out});
+  ERC_REQUIRE(all % type_bytes(f->type) == 0 && reinterpret_cast<uintptr_t>(offsets) % 8 == 0, "misaligned array");
+  if (!ws || ws_bytes < erc_expert_ffn_backward_workspace_size(f))
+    return set_error(ERC_ERR_CAPACITY, "workspace too small");
+  return with_type(f->type, [&](auto t) {
+    using T = decltype(t);
+    Arena ar(align_ws(ws));
+    FfnArgs<T> p = {f->slots, f->experts, f->width, f->inner, f->act, offsets};
+    p.x = static_cast<const T*>(xs);
+    p.w_in = static_cast<const T*>(w_in);
+    p.w_out = static_cast<const T*>(w_out);
+    p.dy = static_cast<const T*>(dy);
+    p.pre_in = static_cast<const T*>(pre);
+    p.dpre = ar.take<T>((size_t)f->slots * f->inner * 2);
+    p.h = ar.take<T>((size_t)f->slots * f->inner);
+    p.dx = static_cast<T*>(dxs);
+    p.dw_in = static_cast<T*>(dw_in);
+    p.dw_out = static_cast<T*>(dw_out);
+    ERC_TRY(ffn_product(false, FFN_DH, p, s));
+    if (p.dx) ERC_TRY(ffn_product(false, FFN_DX, p, s));
+    if (p.dw_in) ERC_TRY(ffn_product(false, FFN_DWIN, p, s));
+    if (p.dw_out) ERC_TRY(ffn_product(false, FFN_DWOUT, p, s));
+    return ERC_OK;
+  });
+}

@@ -1,0 +1,92 @@
+// expert_ffn.cuh -- what the gated feed-forward block's two paths share: the float32 units' (all types
+// and sizes, expert_ffn.cu) and the tensor cores' (expert_ffn_tc.cu).
+//
+// With h = act(a) b and s a slot of expert e, the block is six products:
+//   IN    (a, b)[s] = w_in[e] x[s]           OUT   y[s] = w_out[e] h[s]
+//   DH    dh[s] = dy[s] w_out[e], then da = dh b act'(a), db = dh act(a), and h again from (a, b)
+//   DX    dx[s] = (da, db)[s] w_in[e]
+//   DWIN  dw_in[e] = sum_s (da, db)[s] x[s]^T     DWOUT  dw_out[e] = sum_s dy[s] h[s]^T
+#pragma once
+
+#include "choice.cuh"
+
+namespace erc {
+
+enum FfnProduct { FFN_IN, FFN_OUT, FFN_DH, FFN_DX, FFN_DWIN, FFN_DWOUT };
+
+// the arrays of all six; a product uses those that it names
+template <class T>
+struct FfnArgs {
+  int64_t slots;
+  int experts, width, inner, act;
+  const int64_t* offsets;
+  const T* x;
+  const T* w_in;
+  const T* w_out;
+  const T* dy;
+  const T* pre_in;  // (a, b), read
+  T* pre;           // (a, b), written; may be null
+  T* h;             // act(a) b
+  T* dpre;          // (da, db)
+  T* y;
+  T* dx;
+  T* dw_in;
+  T* dw_out;
+};
+
+// [lo, hi) of an expert; whatever the offsets hold, it lies in [0, slots]
+struct SlotRange {
+  int64_t lo, hi;
+};
+__device__ __forceinline__ SlotRange slot_range(const int64_t* offsets, int e, int64_t slots) {
+  int64_t lo = __ldg(offsets + e), hi = __ldg(offsets + e + 1);
+  lo = lo < 0 ? 0 : lo > slots ? slots : lo;
+  hi = hi < lo ? lo : hi > slots ? slots : hi;
+  return {lo, hi};
+}
+__device__ __forceinline__ int64_t slots_used(const int64_t* offsets, int experts, int64_t slots) {
+  const int64_t v = __ldg(offsets + experts);
+  return v < 0 ? 0 : v > slots ? slots : v;
+}
+
+
+// act(a), and act'(a).  Beyond 100 in magnitude the sigmoid and the normal distribution function are 0 or 1 in
+// float32 and the slopes' second terms vanish, so a is held there where a product with 0 could follow;
+// act(-inf) is 0.  The distribution function comes from erfc, which keeps its relative accuracy in the lower tail.
+__device__ __forceinline__ float held(float a) { return fabsf(a) > 100.f ? copysignf(100.f, a) : a; }
+__device__ __forceinline__ float act_value(int act, float a) {
+  if (act == ERC_ACT_RELU) return a > 0.f || a != a ? a : 0.f;
+  const float q = act == ERC_ACT_GELU ? 0.5f * erfcf(a * -0.7071067811865476f) : 1.f / (1.f + expf(-a));
+  return a == -INFINITY ? 0.f : a * q;
+}
+__device__ __forceinline__ void act_both(int act, float a, float& value, float& slope) {
+  if (act == ERC_ACT_RELU) {
+    value = a > 0.f || a != a ? a : 0.f;
+    slope = a > 0.f ? 1.f : 0.f;
+    return;
+  }
+  const float c = held(a);
+  float q;
+  if (act == ERC_ACT_GELU) {
+    q = 0.5f * erfcf(a * -0.7071067811865476f);
+    slope = fmaf(c * expf(-0.5f * c * c), 0.3989422804014327f, q);
+  } else {
+    q = 1.f / (1.f + expf(-a));
+    slope = q * fmaf(c, 1.f - q, 1.f);
+  }
+  value = a == -INFINITY ? 0.f : a * q;
+}
+
+// rows [first, slots) of `width` elements set to zero by all threads of the grid; `thread` of `threads`
+template <class T>
+__device__ __forceinline__ void zero_slots(T* out, int64_t first, int64_t slots, int64_t width, int64_t thread,
+                                           int64_t threads) {
+  for (int64_t i = first * width + thread; i < slots * width; i += threads) out[i] = from_f32<T>(0.f);
+}
+
+// the tensor cores' path: whether it takes a call, and a product
+bool ffn_tc_takes(const erc_ffn_shape& f, uintptr_t all_pointers);
+template <class T>
+erc_status ffn_tc_product(FfnProduct which, const FfnArgs<T>& a, cudaStream_t s);
+
+}  // namespace erc

@@ -58,6 +58,11 @@ class ErcRouteRuleC(ctypes.Structure):
                 ("top_groups", _i32), ("group_best", _i32), ("renorm", _i32), ("scale", _f32)]
 
 
+class ErcFfnShapeC(ctypes.Structure):
+    _fields_ = [("slots", _i64), ("experts", _i32), ("width", _i32), ("inner", _i32), ("act", _i32),
+                ("type", _i32)]
+
+
 class ErcParamsC(ctypes.Structure):
     _fields_ = [("seed", _u64), ("K", _i32), ("kc", _i32), ("eps", _f32), ("tol", _f32),
                 ("max_iter", _i32), ("eta", _f32), ("dup_policy", _i32), ("precond", _i32)]
@@ -127,6 +132,18 @@ _SIGS = {
     "erc_expert_combine": (_i32, [_i64, _i32, _i64, _c_p, _i32, _c_p, _c_p, _c_p, _c_p]),
     "erc_expert_combine_backward": (_i32, [_i64, _i32, _i64, _c_p, _c_p, _i32, _c_p, _c_p, _c_p,
                                            _c_p, _c_p, _c_p]),
+    "erc_score_rows_workspace_size": (_sz, [_i64, _i64, _i32, _i32]),
+    "erc_score_rows": (_i32, [_i64, _i64, _c_p, _i32, _i64, _c_p, _f32, _i32, _c_p, _c_p, _c_p,
+                              _c_p, _c_p, _c_p, _sz, _c_p]),
+    "erc_score_rows_backward": (_i32, [_i64, _i64, _c_p, _i32, _i64, _c_p, _f32, _c_p, _c_p, _c_p,
+                                       _c_p, _c_p, _c_p]),
+    "erc_expert_ffn_workspace_size": (_sz, [ctypes.POINTER(ErcFfnShapeC)]),
+    "erc_expert_ffn": (_i32, [ctypes.POINTER(ErcFfnShapeC), _c_p, _c_p, _c_p, _c_p, _c_p, _c_p,
+                              _c_p, _sz, _c_p]),
+    "erc_expert_ffn_backward_workspace_size": (_sz, [ctypes.POINTER(ErcFfnShapeC)]),
+    "erc_expert_ffn_backward": (_i32, [ctypes.POINTER(ErcFfnShapeC), _c_p, _c_p, _c_p, _c_p, _c_p,
+                                       _c_p, _c_p, _c_p, _c_p, _c_p, _sz, _c_p]),
+    "erc_dropout": (_i32, [_i64, _c_p, _i32, _c_p, ctypes.c_double, _u64, _c_p, _i64, _c_p, _c_p]),
 }
 
 _lib = None
@@ -702,3 +719,143 @@ def erc_expert_combine_backward(dout, y, slot, offsets, weights):
                                              _placed(offsets, dev), _ptr(weights), dy.data_ptr(),
                                              dweights.data_ptr(), _stream_of(dout)))
     return dy, dweights
+
+
+# ------------------------------------------------------------------------------------------------
+# training and answering: given entries of rows of scores, the experts' products, dropout
+# ------------------------------------------------------------------------------------------------
+ERC_SCORE_MAX_K = 32
+ERC_ACT_SILU, ERC_ACT_GELU, ERC_ACT_RELU = 0, 1, 2
+
+
+def _given_workspace(ws, need, device):
+    """`ws` or a fresh workspace of `need` bytes."""
+    if ws is None:
+        return _workspace(need, device) if need else None
+    if not (isinstance(ws, torch.Tensor) and ws.dtype is torch.uint8 and ws.device == device
+            and ws.is_contiguous()):
+        _refuse(f"ws must be a contiguous uint8 tensor on {device}")
+    return ws
+
+
+def erc_score_rows(logits, ids=None, temperature=1.0, k=0, ws=None):
+    """What each row of logits [rows, n] says about the entry ids[row] (see include/erc.h):
+    (logp float32 [rows] or None without ids, entropy float32 [rows], norm float32 [rows, 2],
+    top_ids int32 [rows, k], top_logp float32 [rows, k]).
+
+    ids int32 [rows]; an id outside [0, n) gives 0.  norm is what erc_score_rows_backward takes.  ws: a
+    uint8 workspace of erc_score_rows_workspace_size bytes, or None.
+    """
+    rows, n, kind, stride = _rows_of(logits, "logits")
+    dev = logits.device
+    if ids is not None:
+        _need(ids, "ids", torch.int32, (rows,), dev)
+    k = _whole(k, "k")
+    if not 0 <= k <= ERC_SCORE_MAX_K:
+        _refuse(f"k must be in [0, {ERC_SCORE_MAX_K}]")
+    kw = dict(dtype=torch.float32, device=dev)
+    logp = torch.empty(rows, **kw) if ids is not None else None
+    entropy, norm = torch.empty(rows, **kw), torch.empty(rows, 2, **kw)
+    top_ids, top_logp = torch.empty(rows, k, dtype=torch.int32, device=dev), torch.empty(rows, k, **kw)
+    ws = _given_workspace(ws, lib().erc_score_rows_workspace_size(rows, n, kind, k), dev)
+    _check(lib().erc_score_rows(rows, n, logits.data_ptr(), kind, stride, _ptr(ids), temperature, k,
+                                _ptr(logp), entropy.data_ptr(), norm.data_ptr(), top_ids.data_ptr(),
+                                top_logp.data_ptr(), _ptr(ws), 0 if ws is None else ws.numel(),
+                                _stream_of(logits)))
+    return logp, entropy, norm, top_ids, top_logp
+
+
+def erc_score_rows_backward(logits, ids, norm, dlogp=None, entropy=None, dentropy=None, temperature=1.0):
+    """The gradient of erc_score_rows' logp and entropy: dlogits [rows, n] from dlogp and dentropy
+    float32 [rows] (None: 0), with the forward call's norm and entropy."""
+    rows, n, kind, stride = _rows_of(logits, "logits")
+    dev = logits.device
+    _need(norm, "norm", torch.float32, (rows, 2), dev)
+    for name, t, dtype in (("ids", ids, torch.int32), ("dlogp", dlogp, torch.float32),
+                           ("entropy", entropy, torch.float32), ("dentropy", dentropy, torch.float32)):
+        if t is not None:
+            _need(t, name, dtype, (rows,), dev)
+    dlogits = torch.empty(rows, n, dtype=logits.dtype, device=dev)
+    _check(lib().erc_score_rows_backward(rows, n, logits.data_ptr(), kind, stride, _ptr(ids), temperature,
+                                         norm.data_ptr(), _ptr(entropy), _ptr(dlogp), _ptr(dentropy),
+                                         dlogits.data_ptr(), _stream_of(logits)))
+    return dlogits
+
+
+def _ffn_shape(x, name, offsets, w_in, w_out, act):
+    """The shape of a block, with its weights and offsets checked against x [slots, width]."""
+    slots, width, kind = _matrix(x, name)
+    dev = x.device
+    _placed(offsets, dev)
+    experts = offsets.numel() - 1
+    if not (isinstance(w_out, torch.Tensor) and w_out.dim() == 3):
+        _refuse("w_out must be [experts, width, inner]")
+    inner = w_out.shape[2]
+    _need(w_out, "w_out", x.dtype, (experts, width, inner), dev)
+    _need(w_in, "w_in", x.dtype, (experts, 2 * inner, width), dev)
+    return ErcFfnShapeC(slots, experts, _whole(width, "width"), _whole(inner, "inner"), _whole(act, "act"), kind)
+
+
+def erc_expert_ffn(xs, offsets, w_in, w_out, act=ERC_ACT_SILU, keep=False, ws=None):
+    """The gated feed-forward block of each expert on its rows of xs [slots, width] (see include/erc.h):
+    (y [slots, width], pre [slots, 2 inner] or None).
+
+    offsets int64 [experts + 1] as from erc_expert_plan (a dense block: [0, slots]); w_in [experts,
+    2 inner, width], w_out [experts, width, inner].  keep: also return pre, which the gradient takes.
+    ws: a uint8 workspace of erc_expert_ffn_workspace_size bytes, or None.
+    """
+    shape = _ffn_shape(xs, "xs", offsets, w_in, w_out, act)
+    dev = xs.device
+    y = torch.empty_like(xs)
+    pre = torch.empty(shape.slots, 2 * shape.inner, dtype=xs.dtype, device=dev) if keep else None
+    ref = ctypes.byref(shape)
+    ws = _given_workspace(ws, lib().erc_expert_ffn_workspace_size(ref), dev)
+    _check(lib().erc_expert_ffn(ref, xs.data_ptr(), offsets.data_ptr(), w_in.data_ptr(), w_out.data_ptr(),
+                                y.data_ptr(), _ptr(pre), _ptr(ws), 0 if ws is None else ws.numel(),
+                                _stream_of(xs)))
+    return y, pre
+
+
+def erc_expert_ffn_backward(dy, xs, pre, offsets, w_in, w_out, act=ERC_ACT_SILU, dxs=True, dw=True, ws=None):
+    """The gradient of erc_expert_ffn from dy [slots, width] and the forward call's pre: (dxs, dw_in,
+    dw_out); dxs, dw: which of the rows' and the weights' to form (None for the others)."""
+    shape = _ffn_shape(xs, "xs", offsets, w_in, w_out, act)
+    dev = xs.device
+    _need(dy, "dy", xs.dtype, xs.shape, dev)
+    _need(pre, "pre", xs.dtype, (shape.slots, 2 * shape.inner), dev)
+    out = (torch.empty_like(xs) if dxs else None, torch.empty_like(w_in) if dw else None,
+           torch.empty_like(w_out) if dw else None)
+    ref = ctypes.byref(shape)
+    ws = _given_workspace(ws, lib().erc_expert_ffn_backward_workspace_size(ref), dev)
+    _check(lib().erc_expert_ffn_backward(ref, dy.data_ptr(), xs.data_ptr(), pre.data_ptr(), offsets.data_ptr(),
+                                         w_in.data_ptr(), w_out.data_ptr(), _ptr(out[0]), _ptr(out[1]), _ptr(out[2]),
+                                         _ptr(ws), 0 if ws is None else ws.numel(), _stream_of(xs)))
+    return out
+
+
+def erc_dropout(x, p, key, residual=None, first=0):
+    """Dropout of a contiguous tensor from the generator's stream of `key`, plus the residual (see
+    include/erc.h).  The gradient of x is the same call on out's gradient, without the residual.
+
+    key: a whole number (mod 2^64), or an int64 tensor [1], read when the kernel runs; first: the
+    stream's number of x's first entry, a multiple of 4.
+    """
+    kind = _TYPES.get(x.dtype) if isinstance(x, torch.Tensor) and x.is_cuda else None
+    if kind is None or not x.is_contiguous():
+        _refuse("x must be a contiguous float32, bfloat16 or float16 CUDA tensor")
+    _on_current_device(x, "x")
+    if residual is not None:
+        _need(residual, "residual", x.dtype, x.shape, x.device)
+    if isinstance(key, torch.Tensor):
+        _need(key, "key", torch.int64, (1,), x.device)
+        number, at = 0, key.data_ptr()
+    else:
+        if int(key) != key:
+            _refuse("key must be a whole number")
+        number, at = int(key) % 2**64, None
+    if not (int(first) == first and 0 <= first < 2**62):
+        _refuse("first must be a whole number in [0, 2^62)")
+    out = torch.empty_like(x)
+    _check(lib().erc_dropout(x.numel(), x.data_ptr(), kind, _ptr(residual), p, number, at, int(first), out.data_ptr(),
+                             _stream_of(x)))
+    return out
