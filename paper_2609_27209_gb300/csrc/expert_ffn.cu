@@ -252,9 +252,17 @@ erc_status simple_product(FfnProduct which, const FfnArgs<T>& p, cudaStream_t s)
   return ERC_OK;
 }
 
+// whether the tensor cores take a call
+bool on_tensor_cores(const erc_ffn_shape* f, uintptr_t all) {
+  return f->type != ERC_F32 && f->width % 8 == 0 && f->inner % 8 == 0 && all % 16 == 0;
+}
+
 template <class T>
-erc_status ffn_product(bool tensor_cores, FfnProduct which, const FfnArgs<T>& p, cudaStream_t s) {
-  (void)tensor_cores;
+erc_status ffn_product(bool tensor_cores, FfnProduct which, const FfnArgs<T>& p, int* status, cudaStream_t s) {
+  if constexpr (sizeof(T) == 2) {
+    if (tensor_cores) return ffn_tc_product<T>(which, p, status, s);
+  }
+  if (which == FFN_IN || which == FFN_DH) ERC_CUDA(cudaMemsetAsync(status, 0, sizeof(int), s));
   return simple_product(which, p, s);
 }
 
@@ -289,7 +297,7 @@ using namespace erc;
 
 extern "C" size_t erc_expert_ffn_workspace_size(const erc_ffn_shape* f) {
   if (!good_shape(f)) return 0;
-  return (size_t)f->slots * f->inner * type_bytes(f->type) + 512;
+  return (size_t)f->slots * f->inner * type_bytes(f->type) + 1024;
 }
 
 extern "C" erc_status erc_expert_ffn(const erc_ffn_shape* f, const void* xs, const int64_t* offsets, const void* w_in,
@@ -302,9 +310,11 @@ extern "C" erc_status erc_expert_ffn(const erc_ffn_shape* f, const void* xs, con
   const uintptr_t all = any_bits({xs, w_in, w_out, y, pre});
   ERC_REQUIRE(all % type_bytes(f->type) == 0 && reinterpret_cast<uintptr_t>(offsets) % 8 == 0, "misaligned array");
   if (!ws || ws_bytes < erc_expert_ffn_workspace_size(f)) return set_error(ERC_ERR_CAPACITY, "workspace too small");
+  const bool fast = on_tensor_cores(f, all);
   return with_type(f->type, [&](auto t) {
     using T = decltype(t);
     Arena ar(align_ws(ws));
+    int* status = ar.take<int>(1);
     FfnArgs<T> p = {f->slots, f->experts, f->width, f->inner, f->act, offsets};
     p.x = static_cast<const T*>(xs);
     p.w_in = static_cast<const T*>(w_in);
@@ -312,14 +322,14 @@ extern "C" erc_status erc_expert_ffn(const erc_ffn_shape* f, const void* xs, con
     p.h = ar.take<T>((size_t)f->slots * f->inner);
     p.pre = static_cast<T*>(pre);
     p.y = static_cast<T*>(y);
-    ERC_TRY(ffn_product(false, FFN_IN, p, as_stream(stream)));
-    return ffn_product(false, FFN_OUT, p, as_stream(stream));
+    ERC_TRY(ffn_product(fast, FFN_IN, p, status, as_stream(stream)));
+    return ffn_product(fast, FFN_OUT, p, status, as_stream(stream));
   });
 }
 
 extern "C" size_t erc_expert_ffn_backward_workspace_size(const erc_ffn_shape* f) {
   if (!good_shape(f)) return 0;
-  return (size_t)f->slots * f->inner * 3 * type_bytes(f->type) + 1024;
+  return (size_t)f->slots * f->inner * 3 * type_bytes(f->type) + 1536;
 }
 
 extern "C" erc_status erc_expert_ffn_backward(const erc_ffn_shape* f, const void* dy, const void* xs, const void* pre,
@@ -340,9 +350,11 @@ extern "C" erc_status erc_expert_ffn_backward(const erc_ffn_shape* f, const void
   ERC_REQUIRE(all % type_bytes(f->type) == 0 && reinterpret_cast<uintptr_t>(offsets) % 8 == 0, "misaligned array");
   if (!ws || ws_bytes < erc_expert_ffn_backward_workspace_size(f))
     return set_error(ERC_ERR_CAPACITY, "workspace too small");
+  const bool fast = on_tensor_cores(f, all);
   return with_type(f->type, [&](auto t) {
     using T = decltype(t);
     Arena ar(align_ws(ws));
+    int* status = ar.take<int>(1);
     FfnArgs<T> p = {f->slots, f->experts, f->width, f->inner, f->act, offsets};
     p.x = static_cast<const T*>(xs);
     p.w_in = static_cast<const T*>(w_in);
@@ -354,10 +366,10 @@ extern "C" erc_status erc_expert_ffn_backward(const erc_ffn_shape* f, const void
     p.dx = static_cast<T*>(dxs);
     p.dw_in = static_cast<T*>(dw_in);
     p.dw_out = static_cast<T*>(dw_out);
-    ERC_TRY(ffn_product(false, FFN_DH, p, s));
-    if (p.dx) ERC_TRY(ffn_product(false, FFN_DX, p, s));
-    if (p.dw_in) ERC_TRY(ffn_product(false, FFN_DWIN, p, s));
-    if (p.dw_out) ERC_TRY(ffn_product(false, FFN_DWOUT, p, s));
+    ERC_TRY(ffn_product(fast, FFN_DH, p, status, s));
+    if (p.dx) ERC_TRY(ffn_product(fast, FFN_DX, p, status, s));
+    if (p.dw_in) ERC_TRY(ffn_product(fast, FFN_DWIN, p, status, s));
+    if (p.dw_out) ERC_TRY(ffn_product(fast, FFN_DWOUT, p, status, s));
     return ERC_OK;
   });
 }

@@ -53,10 +53,16 @@ __device__ __forceinline__ int64_t slots_used(const int64_t* offsets, int expert
 // act(a), and act'(a).  Beyond 100 in magnitude the sigmoid and the normal distribution function are 0 or 1 in
 // float32 and the slopes' second terms vanish, so a is held there where a product with 0 could follow;
 // act(-inf) is 0.  The distribution function comes from erfc, which keeps its relative accuracy in the lower tail.
+__device__ __forceinline__ float sigmoid(float a) {  // the hardware's 2^x and 1 / x: a few units in the last place, more with |a|
+  float e, q;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(a * -LOG2E));
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(q) : "f"(1.f + e));
+  return q;
+}
 __device__ __forceinline__ float held(float a) { return fabsf(a) > 100.f ? copysignf(100.f, a) : a; }
 __device__ __forceinline__ float act_value(int act, float a) {
   if (act == ERC_ACT_RELU) return a > 0.f || a != a ? a : 0.f;
-  const float q = act == ERC_ACT_GELU ? 0.5f * erfcf(a * -0.7071067811865476f) : 1.f / (1.f + expf(-a));
+  const float q = act == ERC_ACT_GELU ? 0.5f * erfcf(a * -0.7071067811865476f) : sigmoid(a);
   return a == -INFINITY ? 0.f : a * q;
 }
 __device__ __forceinline__ void act_both(int act, float a, float& value, float& slope) {
@@ -71,7 +77,7 @@ __device__ __forceinline__ void act_both(int act, float a, float& value, float& 
     q = 0.5f * erfcf(a * -0.7071067811865476f);
     slope = fmaf(c * expf(-0.5f * c * c), 0.3989422804014327f, q);
   } else {
-    q = 1.f / (1.f + expf(-a));
+    q = sigmoid(a);
     slope = q * fmaf(c, 1.f - q, 1.f);
   }
   value = a == -INFINITY ? 0.f : a * q;
@@ -84,9 +90,13 @@ __device__ __forceinline__ void zero_slots(T* out, int64_t first, int64_t slots,
   for (int64_t i = first * width + thread; i < slots * width; i += threads) out[i] = from_f32<T>(0.f);
 }
 
-// the tensor cores' path: whether it takes a call, and a product
-bool ffn_tc_takes(const erc_ffn_shape& f, uintptr_t all_pointers);
+// a product on the tensor cores (bfloat16 and float16 whose rows are whole 16-byte pieces); `status` (device) gets
+// ERC_OK at the start of IN and DH, and ERC_ERR_TIMEOUT where a wait ran out
 template <class T>
-erc_status ffn_tc_product(FfnProduct which, const FfnArgs<T>& a, cudaStream_t s);
+erc_status ffn_tc_product(FfnProduct which, const FfnArgs<T>& p, int* status, cudaStream_t s);
+template <>
+erc_status ffn_tc_product(FfnProduct which, const FfnArgs<__nv_bfloat16>& p, int* status, cudaStream_t s);
+template <>
+erc_status ffn_tc_product(FfnProduct which, const FfnArgs<__half>& p, int* status, cudaStream_t s);
 
 }  // namespace erc

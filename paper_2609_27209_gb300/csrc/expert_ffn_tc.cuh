@@ -1,0 +1,605 @@
+// expert_ffn_tc.cuh -- the block's products on the tensor cores (tcgen05), bfloat16 and float16.
+//
+// Every product is D(m, n) = sum_k A(m, k) B(n, k) with m the index that is contiguous in the result, so
+// that a warp, whose lanes hold neighbouring m, writes whole sectors:
+//
+//   product   m       n      k      A                            B
+//   IN        gate/up slot   width  w_in, rows of width          x, rows of width
+//   OUT       width   slot   inner  w_out, rows of inner         h
+//   DH        inner   slot   width  w_out, columns               dy
+//   DX        width   slot   2 inner  w_in, columns              (da, db)
+//   DWIN      width   2 inner  slot x, columns                   (da, db), columns
+//   DWOUT     inner   width  slot   h, columns                   dy, columns
+//
+// A pair of blocks (a cluster of two) takes a tile of 256 x N, N <= 256: each block holds half of A and
+// half of B in shared memory and accumulates its 128 rows of m, one a lane, in tensor memory; the first
+// block's thread issues the products of both.  Slots are n, so that a tile at the end of an expert's rows
+// costs N = 32, 64, .. columns and not 256, and rows of another expert never mix.  In IN gates and
+// factors of the same 8 features alternate in m (the copy's box does that), so that a lane and the lane 8
+// further hold a and b of one feature.
+//
+// Persistent blocks of 12 warps: copies (TMA), products, a warp that passes on what has landed, one that
+// zeroes the rows behind the last expert's, and 8 that read tensor memory and write results while the next
+// tile runs in its other half.
+//
+// Every wait on a barrier ends: after WAIT_LIMIT polls it gives up, the block's roles stop, copies and
+// products in flight are waited for (with the same limit), tensor memory is freed and the status word is
+// set to ERC_ERR_TIMEOUT.
+#pragma once
+
+#include <cuda.h>
+
+#include "expert_ffn.cuh"
+
+namespace erc {
+
+constexpr int TC_STAGES = 6;
+constexpr int TC_K = 64;                    // depth of a stage: 128 bytes, one row of the swizzle
+constexpr int TC_HALF = 128;                // rows of A and of B that a block holds
+constexpr int TC_OPERAND = TC_HALF * TC_K * 2;
+constexpr int TC_STAGE = 2 * TC_OPERAND;
+constexpr int TC_SMEM = TC_STAGES * TC_STAGE + 1024;
+constexpr int TC_THREADS = 384;
+constexpr int TC_EPILOGUE = 8;              // warps that write results
+constexpr unsigned TC_WAIT_LIMIT = 1u << 22;
+
+__device__ __forceinline__ uint32_t smem_at(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ uint32_t cluster_rank() {
+  uint32_t r;
+  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ uint32_t peer_address(uint32_t local, uint32_t rank) {
+  uint32_t r;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(local), "r"(rank));
+  return r;
+}
+__device__ __forceinline__ void cluster_arrive_wait() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void bar_init(uint32_t bar, uint32_t count) {
+  asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
+}
+__device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes) {
+  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void bar_arrive_cluster(uint32_t cluster_bar) {
+  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
+}
+__device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
+  uint32_t done;
+  asm volatile(
+      "{\n.reg .pred p;\nmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}"
+      : "=r"(done)
+      : "r"(bar), "r"(parity)
+      : "memory");
+  return done;
+}
+// false when the wait ran out, here or in another role of the block
+__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile int* failed) {
+  for (unsigned i = 0; i < TC_WAIT_LIMIT; ++i) {
+    if (bar_try(bar, parity)) return true;
+    if (*failed) return false;
+  }
+  *failed = 1;
+  return false;
+}
+__device__ __forceinline__ void bar_drain(uint32_t bar, uint32_t parity) {
+  for (unsigned i = 0; i < TC_WAIT_LIMIT; ++i)
+    if (bar_try(bar, parity)) return;
+}
+
+__device__ __forceinline__ void copy_2d(uint32_t dst, const CUtensorMap* map, uint32_t bar, int x, int y) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];" ::"r"(dst),
+      "l"(map), "r"(bar), "r"(x), "r"(y)
+      : "memory");
+}
+__device__ __forceinline__ void copy_3d(uint32_t dst, const CUtensorMap* map, uint32_t bar, int x, int y, int z) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(
+          dst),
+      "l"(map), "r"(bar), "r"(x), "r"(y), "r"(z)
+      : "memory");
+}
+__device__ __forceinline__ void copy_5d(uint32_t dst, const CUtensorMap* map, uint32_t bar, int a, int b, int c, int d, int e) {
+  asm volatile(
+      "cp.async.bulk.tensor.5d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6, %7}], [%2];" ::
+          "r"(dst),
+      "l"(map), "r"(bar), "r"(a), "r"(b), "r"(c), "r"(d), "r"(e)
+      : "memory");
+}
+
+// Shared-memory descriptor of an operand in 128-byte swizzle, 1024-byte aligned atoms.  K contiguous: 8 rows of 128
+// bytes an atom, atoms 1024 bytes apart.  M or N contiguous: 64 of them by 8 k an atom, 1024 bytes to the next 8 k and
+// 8192 (a box of the copy) to the next 64.
+__device__ __forceinline__ uint64_t operand_desc(uint32_t addr, bool k_contiguous) {
+  uint64_t d = (uint64_t)((addr & 0x3ffff) >> 4);
+  d |= (uint64_t)(k_contiguous ? 1 : 8192 >> 4) << 16;
+  d |= (uint64_t)(1024 >> 4) << 32;
+  d |= (uint64_t)1 << 46;
+  d |= (uint64_t)2 << 61;
+  return d;
+}
+__device__ __forceinline__ void mma_pair(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add) {
+  asm volatile(
+      "{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\ntcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(d), "l"(a),
+      "l"(b), "r"(idesc), "r"((uint32_t)add)
+      : "memory");
+}
+// arrives at the barrier of this offset in both blocks once the products issued so far are done
+__device__ __forceinline__ void commit_pair(uint32_t bar) {
+  asm volatile(
+      "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar),
+      "h"((uint16_t)3)
+      : "memory");
+}
+__device__ __forceinline__ void read_tmem(uint32_t addr, float* v) {
+  uint32_t* r = reinterpret_cast<uint32_t*>(v);
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, "
+      "%18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+        "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]),
+        "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]),
+        "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+      : "r"(addr)
+      : "memory");
+}
+__device__ __forceinline__ void read_tmem_done() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+
+template <class T>
+struct Half2;
+template <>
+struct Half2<__nv_bfloat16> {
+  static constexpr uint32_t FORMAT = 1;
+  static __device__ __forceinline__ uint32_t pack(float a, float b) {
+    const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&v);
+  }
+  static __device__ __forceinline__ float2 unpack(uint32_t v) {
+    return make_float2(__uint_as_float(v << 16), __uint_as_float(v & 0xffff0000u));
+  }
+};
+template <>
+struct Half2<__half> {
+  static constexpr uint32_t FORMAT = 0;
+  static __device__ __forceinline__ uint32_t pack(float a, float b) {
+    const __half2 v = __floats2half2_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&v);
+  }
+  static __device__ __forceinline__ float2 unpack(uint32_t v) { return __half22float2(*reinterpret_cast<const __half2*>(&v)); }
+};
+
+// a tile: rows of m from m0 on (of both blocks), n columns from n0 on of which `valid` are written, k blocks
+struct TcTile {
+  int expert, m0, n, valid, blocks;
+  int64_t n0;       // slot, or row of a weight gradient
+  int64_t k0, k1;   // slots of a weight gradient
+};
+
+// which tiles a product has, from the experts' slots
+template <int WHICH>
+struct TcTiles {
+  static constexpr bool SLOTS = WHICH <= FFN_DX;
+  int m_tiles, n_tiles, depth;  // n_tiles: of a weight gradient
+  int n_total, wide;            // a weight gradient's n, and its columns a tile
+  int64_t total;
+  __device__ __forceinline__ void init(int D, int F) {
+    const int m = WHICH == FFN_IN ? 2 * F : WHICH == FFN_DH || WHICH == FFN_DWOUT ? F : D;
+    m_tiles = (m + 255) / 256;
+    depth = WHICH == FFN_IN || WHICH == FFN_DH ? D : WHICH == FFN_OUT ? F : 2 * F;
+    n_total = WHICH == FFN_DWIN ? 2 * F : D;
+    wide = n_total <= 128 ? 128 : 256;
+    n_tiles = (n_total + wide - 1) / wide;
+  }
+  // prefix[e]: tiles of 256 slots of the experts before e
+  __device__ __forceinline__ TcTile at(int64_t t, const int* prefix, const int64_t* offsets, int experts, int64_t slots) const {
+    TcTile r;
+    if (SLOTS) {
+      const int of = (int)(t / m_tiles);
+      r.m0 = (int)(t - (int64_t)of * m_tiles) * 256;
+      int lo = 0, hi = experts;  // the last expert with prefix[e] <= of
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (prefix[mid] <= of) lo = mid; else hi = mid;
+      }
+      r.expert = lo;
+      const SlotRange s = slot_range(offsets, lo, slots);
+      r.n0 = s.lo + (int64_t)(of - prefix[lo]) * 256;
+      const int64_t left = s.hi - r.n0;
+      r.valid = left < 256 ? (int)left : 256;
+      r.n = (r.valid + 31) & ~31;  // a pair's products take multiples of 32
+      r.k0 = r.k1 = 0;
+      r.blocks = (depth + TC_K - 1) / TC_K;
+    } else {
+      const int each = m_tiles * n_tiles;
+      r.expert = (int)(t / each);
+      const int rest = (int)(t - (int64_t)r.expert * each);
+      r.m0 = rest % m_tiles * 256;
+      r.n0 = rest / m_tiles * wide;
+      r.n = wide;
+      r.valid = n_total - r.n0 < wide ? (int)(n_total - r.n0) : wide;
+      const SlotRange s = slot_range(offsets, r.expert, slots);
+      r.k0 = s.lo;
+      r.k1 = s.hi;
+      r.blocks = (int)((s.hi - s.lo + TC_K - 1) / TC_K);
+    }
+    return r;
+  }
+};
+
+// results of 32 columns of a tile, two at a time: a lane and its neighbour swap, so that even lanes hold rows m, m + 1
+// of column c and odd lanes rows m - 1, m of column c + 1
+template <class T>
+__device__ __forceinline__ void pair_up(float a, float b, int lane, float& lo, float& hi) {
+  const float give = lane & 1 ? a : b, keep = lane & 1 ? b : a;
+  const float got = __shfl_xor_sync(0xffffffffu, give, 1);
+  lo = lane & 1 ? got : keep;
+  hi = lane & 1 ? keep : got;
+}
+
+template <class T, int WHICH>
+__device__ __forceinline__ void write_columns(const FfnArgs<T>& p, const TcTile& t, const float* v, int c0, int m_block, int lane,
+                                              int quad) {
+  using H = Half2<T>;
+  const int64_t D = p.width, F = p.inner;
+  if constexpr (WHICH == FFN_IN) {
+    // lane: gates where bit 3 is clear, factors where it is set, of feature f
+    const bool up = lane & 8;
+    const int f = (t.m0 + m_block) / 2 + quad * 16 + (lane >> 4) * 8 + (lane & 7);
+    const int odd = lane & 1;
+#pragma unroll
+    for (int j = 0; j < 32; j += 4) {
+      float g[2], u[2], h[2];
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        const float a = v[j + 2 * q], b = v[j + 2 * q + 1];
+        const float got = __shfl_xor_sync(0xffffffffu, up ? a : b, 8);
+        g[q] = up ? got : a;
+        u[q] = up ? b : got;
+        h[q] = act_value(p.act, g[q]) * u[q];
+      }
+      // columns j (even lanes) and j + 2 (odd lanes), one further for lanes of factors
+      float h0, h1, g0, g1, u0, u1;
+      pair_up<T>(h[0], h[1], lane, h0, h1);
+      const int col = c0 + j + 2 * odd + (up ? 1 : 0);
+      const bool live = col < t.valid && f < F;
+      const int64_t row = t.n0 + col;
+      const int at = f - odd;
+      if (live) *reinterpret_cast<uint32_t*>(p.h + row * F + at) = H::pack(h0, h1);
+      if (p.pre) {
+        pair_up<T>(g[0], g[1], lane, g0, g1);
+        pair_up<T>(u[0], u[1], lane, u0, u1);
+        if (live) {
+          *reinterpret_cast<uint32_t*>(p.pre + row * 2 * F + at) = H::pack(g0, g1);
+          *reinterpret_cast<uint32_t*>(p.pre + row * 2 * F + F + at) = H::pack(u0, u1);
+        }
+      }
+    }
+  } else {
+    const int m = t.m0 + m_block + quad * 32 + lane, odd = lane & 1, at = m - odd;
+    const int64_t ld = WHICH == FFN_DH || WHICH == FFN_DWOUT ? F : D;
+    uint32_t pa[16], pb[16];
+    if constexpr (WHICH == FFN_DH) {
+#pragma unroll
+      for (int j = 0; j < 32; j += 2) {
+        const int col = c0 + j + odd;
+        pa[j / 2] = pb[j / 2] = 0;
+        if (col < t.valid && m < ld) {
+          const T* pre = p.pre_in + (t.n0 + col) * 2 * F + at;
+          pa[j / 2] = __ldg(reinterpret_cast<const uint32_t*>(pre));
+          pb[j / 2] = __ldg(reinterpret_cast<const uint32_t*>(pre + F));
+        }
+      }
+    }
+    T* out = WHICH == FFN_OUT ? p.y : WHICH == FFN_DX ? p.dx : WHICH == FFN_DWIN ? p.dw_in : p.dw_out;
+    if constexpr (WHICH == FFN_DWIN) out += (int64_t)t.expert * 2 * F * D;
+    if constexpr (WHICH == FFN_DWOUT) out += (int64_t)t.expert * D * F;
+#pragma unroll
+    for (int j = 0; j < 32; j += 2) {
+      float lo, hi;
+      pair_up<T>(v[j], v[j + 1], lane, lo, hi);
+      const int col = c0 + j + odd;
+      const bool live = col < t.valid && m < ld;
+      const int64_t row = t.n0 + col;
+      if constexpr (WHICH == FFN_DH) {
+        const float2 a = H::unpack(pa[j / 2]), b = H::unpack(pb[j / 2]);
+        float v0, v1, s0, s1;
+        act_both(p.act, a.x, v0, s0);
+        act_both(p.act, a.y, v1, s1);
+        if (live) {
+          *reinterpret_cast<uint32_t*>(p.dpre + row * 2 * F + at) = H::pack(lo * b.x * s0, hi * b.y * s1);
+          *reinterpret_cast<uint32_t*>(p.dpre + row * 2 * F + F + at) = H::pack(lo * v0, hi * v1);
+          *reinterpret_cast<uint32_t*>(p.h + row * F + at) = H::pack(v0 * b.x, v1 * b.y);
+        }
+      } else if (live) {
+        *reinterpret_cast<uint32_t*>(out + row * ld + at) = H::pack(lo, hi);
+      }
+    }
+  }
+}
+
+template <class T, int WHICH>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(TC_THREADS, 1)
+    k_ffn_tc(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const FfnArgs<T> p,
+             int* __restrict__ status) {
+  constexpr bool SLOTS = TcTiles<WHICH>::SLOTS;
+  constexpr bool A_K = WHICH == FFN_IN || WHICH == FFN_OUT, B_K = SLOTS;
+  extern __shared__ char raw[];
+  __shared__ __align__(8) uint64_t bars[3 * TC_STAGES + 5];
+  __shared__ int prefix[ERC_ROUTE_MAX_EXPERTS + 1];
+  __shared__ uint32_t tmem_base;
+  __shared__ volatile int failed;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t rank = cluster_rank();
+  const uint32_t stages = (smem_at(raw) + 1023) & ~1023u;
+  const uint32_t bar0 = smem_at(bars);
+  auto land = [&](int s) { return bar0 + 8u * s; };                       // this block's copies of a stage
+  auto ready = [&](int s) { return bar0 + 8u * (TC_STAGES + s); };        // first block: both blocks' copies
+  auto empty = [&](int s) { return bar0 + 8u * (2 * TC_STAGES + s); };    // the products have read a stage
+  auto full = [&](int a) { return bar0 + 8u * (3 * TC_STAGES + a); };     // a tile's sums are complete
+  auto taken = [&](int a) { return bar0 + 8u * (3 * TC_STAGES + 2 + a); };  // first block: both have read them
+  const uint32_t done = bar0 + 8u * (3 * TC_STAGES + 4);
+
+  if (threadIdx.x == 0) {
+    failed = 0;
+    for (int s = 0; s < TC_STAGES; ++s) {
+      bar_init(land(s), 1);
+      bar_init(ready(s), 2);
+      bar_init(empty(s), 1);
+    }
+    for (int a = 0; a < 2; ++a) {
+      bar_init(full(a), 1);
+      bar_init(taken(a), 2 * TC_EPILOGUE);
+    }
+    bar_init(done, 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 3) {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_at(&tmem_base)) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
+  }
+  TcTiles<WHICH> tiles;
+  tiles.init(p.width, p.inner);
+  if (SLOTS) {
+    for (int e = threadIdx.x; e < p.experts; e += TC_THREADS) {
+      const SlotRange r = slot_range(p.offsets, e, p.slots);
+      prefix[e + 1] = (int)((r.hi - r.lo + 255) / 256);
+    }
+    __syncthreads();
+    if (warp == 0) {
+      int before = 0;
+      for (int e0 = 0; e0 < p.experts; e0 += 32) {
+        int x = e0 + lane < p.experts ? prefix[e0 + lane + 1] : 0;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+          const int y = __shfl_up_sync(0xffffffffu, x, o);
+          if (lane >= o) x += y;
+        }
+        if (e0 + lane < p.experts) prefix[e0 + lane + 1] = before + x;
+        before += __shfl_sync(0xffffffffu, x, 31);
+      }
+      if (lane == 0) prefix[0] = 0;
+    }
+  }
+  if (blockIdx.x == 0 && threadIdx.x == 0 && (WHICH == FFN_IN || WHICH == FFN_DH)) *status = ERC_OK;
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  __syncthreads();
+  cluster_arrive_wait();
+  asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+  const uint32_t tmem = tmem_base;
+  const int64_t total = SLOTS ? (int64_t)prefix[p.experts] * tiles.m_tiles
+                              : (int64_t)p.experts * tiles.m_tiles * tiles.n_tiles;
+  const int64_t first = blockIdx.x >> 1, step = gridDim.x >> 1;
+  const int m_block = rank * TC_HALF;
+
+  if (warp == 0) {
+    if (lane == 0) {  // copies
+      int s = 0;
+      uint32_t phase = 0, issued = 0;
+      bool ok = true;
+      for (int64_t at = first; ok && at < total; at += step) {
+        const TcTile t = tiles.at(at, prefix, p.offsets, p.experts, p.slots);
+        const int m = t.m0 + m_block, n_half = t.n / 2;
+        for (int b = 0; b < t.blocks; ++b) {
+          if (!(ok = bar_wait(empty(s), phase ^ 1, &failed))) break;
+          const uint32_t dst = stages + s * TC_STAGE, bar = land(s);
+          const int k = b * TC_K;
+          bar_expect(bar, TC_OPERAND + (B_K ? TC_OPERAND : n_half * TC_K * 2));
+          if constexpr (WHICH == FFN_IN) {
+            copy_5d(dst, &map_a, bar, k, 0, 0, m / 16, t.expert);
+          } else if constexpr (WHICH == FFN_OUT) {
+            copy_3d(dst, &map_a, bar, k, m, t.expert);
+          } else if constexpr (SLOTS) {
+            copy_3d(dst, &map_a, bar, m, k, t.expert);
+            copy_3d(dst + 8192, &map_a, bar, m + 64, k, t.expert);
+          } else {
+            copy_2d(dst, &map_a, bar, m, (int)(t.k0 + k));
+            copy_2d(dst + 8192, &map_a, bar, m + 64, (int)(t.k0 + k));
+          }
+          if constexpr (B_K) {
+            copy_2d(dst + TC_OPERAND, &map_b, bar, k, (int)(t.n0 + rank * n_half));
+          } else {
+            const int n = (int)t.n0 + rank * n_half;
+            copy_2d(dst + TC_OPERAND, &map_b, bar, n, (int)(t.k0 + k));
+            if (n_half > 64) copy_2d(dst + TC_OPERAND + 8192, &map_b, bar, n + 64, (int)(t.k0 + k));
+          }
+          ++issued;
+          if (++s == TC_STAGES) s = 0, phase ^= 1;
+        }
+      }
+      if (failed)  // copies in flight write shared memory: none may be left
+        for (int i = 0; i < TC_STAGES && issued > 0; ++i, --issued) {
+          if (s-- == 0) s = TC_STAGES - 1, phase ^= 1;
+          bar_drain(land(s), phase);
+        }
+    }
+  } else if (warp == 1) {
+    if (lane == 0 && rank == 0) {  // products
+      int s = 0, a = 0;
+      uint32_t phase = 0, a_phase = 0;
+      bool ok = true;
+      for (int64_t at = first; ok && at < total; at += step) {
+        const TcTile t = tiles.at(at, prefix, p.offsets, p.experts, p.slots);
+        if (t.blocks == 0) continue;
+        const uint32_t idesc = (1u << 4) | (Half2<T>::FORMAT << 7) | (Half2<T>::FORMAT << 10) | ((A_K ? 0u : 1u) << 15) |
+                               ((B_K ? 0u : 1u) << 16) | ((uint32_t)(t.n >> 3) << 17) | ((256u >> 4) << 24);
+        if (!(ok = bar_wait(taken(a), a_phase ^ 1, &failed))) break;
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        const uint32_t d = tmem + a * 256;
+        for (int b = 0; b < t.blocks; ++b) {
+          if (!(ok = bar_wait(ready(s), phase, &failed))) break;
+          asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+          const uint64_t da = operand_desc(stages + s * TC_STAGE, A_K), db = operand_desc(stages + s * TC_STAGE + TC_OPERAND, B_K);
+#pragma unroll
+          for (int k = 0; k < TC_K / 16; ++k)
+            mma_pair(d, da + k * (A_K ? 32 >> 4 : 2048 >> 4), db + k * (B_K ? 32 >> 4 : 2048 >> 4), idesc, b > 0 || k > 0);
+          commit_pair(empty(s));
+          if (++s == TC_STAGES) s = 0, phase ^= 1;
+        }
+        if (!ok) break;
+        commit_pair(full(a));
+        if (++a == 2) a = 0, a_phase ^= 1;
+      }
+      if (failed) {
+        commit_pair(done);
+        bar_drain(done, 0);
+      }
+    }
+  } else if (warp == 2) {  // what has landed is passed on to the first block
+    int s = 0;
+    uint32_t phase = 0;
+    bool ok = true;
+    for (int64_t at = first; ok && at < total; at += step) {
+      const TcTile t = tiles.at(at, prefix, p.offsets, p.experts, p.slots);
+      for (int b = 0; b < t.blocks; ++b) {
+        if (!(ok = __all_sync(0xffffffffu, bar_wait(land(s), phase, &failed)))) break;
+        if (!SLOTS && t.k0 + (b + 1) * TC_K > t.k1) {
+          // the last slots of an expert: the rows of the box behind them belong to others
+          const int live = (int)(t.k1 - t.k0 - (int64_t)b * TC_K);
+          const uint32_t base = stages + s * TC_STAGE;
+          const int boxes = t.n > 128 ? 4 : 3;
+          for (int x = 0; x < boxes; ++x)
+            for (int i = live * 8 + lane; i < 512; i += 32)
+              asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(base + x * 8192 + i * 16), "r"(0) : "memory");
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        }
+        __syncwarp();
+        if (lane == 0) bar_arrive_cluster(peer_address(ready(s), 0));
+        if (++s == TC_STAGES) s = 0, phase ^= 1;
+      }
+    }
+  } else if (warp == 3) {  // rows behind the last expert's
+    if constexpr (WHICH == FFN_IN || WHICH == FFN_OUT || WHICH == FFN_DX) {
+      T* out = WHICH == FFN_IN ? p.pre : WHICH == FFN_OUT ? p.y : p.dx;
+      const int64_t row = (WHICH == FFN_IN ? 2 * (int64_t)p.inner : p.width) * sizeof(T) / 16;
+      if (out)
+        for (int64_t i = slots_used(p.offsets, p.experts, p.slots) * row + blockIdx.x * 32 + lane; i < p.slots * row;
+             i += gridDim.x * 32)
+          reinterpret_cast<uint4*>(out)[i] = make_uint4(0, 0, 0, 0);
+    }
+  } else {  // results
+    const int quad = warp & 3, part = (warp - 4) >> 2;
+    int a = 0;
+    uint32_t a_phase = 0;
+    bool ok = true;
+    for (int64_t at = first; ok && at < total; at += step) {
+      const TcTile t = tiles.at(at, prefix, p.offsets, p.experts, p.slots);
+      const int c1 = min(t.n, (part + 1) * 128);
+      float v[32];
+      if (t.blocks == 0) {
+#pragma unroll
+        for (int i = 0; i < 32; ++i) v[i] = 0.f;
+        for (int c = part * 128; c < c1; c += 32) write_columns<T, WHICH>(p, t, v, c, m_block, lane, quad);
+        continue;
+      }
+      ok = __all_sync(0xffffffffu, bar_wait(full(a), a_phase, &failed));
+      if (!ok) break;
+      asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+      const uint32_t src = tmem + a * 256 + ((uint32_t)(quad * 32) << 16);
+      for (int c = part * 128; c < c1; c += 32) {
+        read_tmem(src + c, v);
+        read_tmem_done();
+        if (c + 32 >= c1) {
+          asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+          __syncwarp();
+          if (lane == 0) bar_arrive_cluster(peer_address(taken(a), 0));
+        }
+        write_columns<T, WHICH>(p, t, v, c, m_block, lane, quad);
+      }
+      if (part * 128 >= c1) {
+        __syncwarp();
+        if (lane == 0) bar_arrive_cluster(peer_address(taken(a), 0));
+      }
+      if (++a == 2) a = 0, a_phase ^= 1;
+    }
+  }
+  __syncwarp();
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  __syncthreads();
+  cluster_arrive_wait();
+  asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+  if (warp == 3) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(tmem));
+  if (threadIdx.x == 0 && failed) *status = ERC_ERR_TIMEOUT;
+}
+
+// ---- host side
+// a tensor map of 16-bit elements; dims, strides (bytes, of all but the first) and box as given.  False when refused.
+bool tc_encode(CUtensorMap* map, bool bf16, const void* base, int rank, const uint64_t* dims, const uint64_t* strides,
+               const uint32_t* box);
+
+template <class T, int WHICH>
+erc_status ffn_tc_launch(const FfnArgs<T>& p, int* status, cudaStream_t s) {
+  const uint64_t D = p.width, F = p.inner, E = p.experts, S = p.slots;
+  constexpr bool BF = std::is_same<T, __nv_bfloat16>::value;
+  CUtensorMap a, b;
+  bool good = true;
+  if constexpr (WHICH == FFN_IN) {
+    // features in groups of 8, gates and factors of a group next to each other
+    const uint64_t dims[5] = {D, 8, 2, F / 8, E}, strides[4] = {2 * D, 2 * D * F, 16 * D, 4 * D * F};
+    const uint32_t box[5] = {TC_K, 8, 2, 8, 1};
+    good = tc_encode(&a, BF, p.w_in, 5, dims, strides, box);
+  } else if constexpr (WHICH == FFN_OUT || WHICH == FFN_DH) {
+    const uint64_t dims[3] = {F, D, E}, strides[2] = {2 * F, 2 * D * F};
+    const uint32_t box[3] = {TC_K, WHICH == FFN_OUT ? (uint32_t)TC_HALF : (uint32_t)TC_K, 1};
+    good = tc_encode(&a, BF, p.w_out, 3, dims, strides, box);
+  } else if constexpr (WHICH == FFN_DX) {
+    const uint64_t dims[3] = {D, 2 * F, E}, strides[2] = {2 * D, 4 * D * F};
+    const uint32_t box[3] = {TC_K, TC_K, 1};
+    good = tc_encode(&a, BF, p.w_in, 3, dims, strides, box);
+  } else {
+    const uint64_t width = WHICH == FFN_DWIN ? D : F;
+    const uint64_t dims[2] = {width, S}, strides[1] = {2 * width};
+    const uint32_t box[2] = {TC_K, TC_K};
+    good = tc_encode(&a, BF, WHICH == FFN_DWIN ? p.x : p.h, 2, dims, strides, box);
+  }
+  const uint64_t row = WHICH == FFN_IN || WHICH == FFN_DH || WHICH == FFN_DWOUT ? D : WHICH == FFN_OUT ? F : 2 * F;
+  const void* from = WHICH == FFN_IN ? p.x : WHICH == FFN_OUT ? p.h : WHICH == FFN_DH || WHICH == FFN_DWOUT ? p.dy : p.dpre;
+  const uint64_t dims[2] = {row, S}, strides[1] = {2 * row};
+  const uint32_t box[2] = {TC_K, WHICH <= FFN_DX ? (uint32_t)TC_HALF : (uint32_t)TC_K};
+  good = good && tc_encode(&b, BF, from, 2, dims, strides, box);
+  if (!good) return set_error(ERC_ERR_CUDA, "a tensor map of the expert products was refused");
+  auto kernel = k_ffn_tc<T, WHICH>;
+  ERC_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, TC_SMEM));
+  kernel<<<sm_count() / 2 * 2, TC_THREADS, TC_SMEM, s>>>(a, b, p, status);
+  count_launches(1);
+  ERC_CUDA(cudaGetLastError());
+  return ERC_OK;
+}
+
+// the products of a type, in a translation unit of their own
+#define ERC_FFN_TC_PRODUCTS(T)                                                                             \
+  template <>                                                                                              \
+  erc_status ffn_tc_product<T>(FfnProduct which, const FfnArgs<T>& p, int* status, cudaStream_t s) {       \
+    switch (which) {                                                                                       \
+      case FFN_IN: return ffn_tc_launch<T, FFN_IN>(p, status, s);                                          \
+      case FFN_OUT: return ffn_tc_launch<T, FFN_OUT>(p, status, s);                                        \
+      case FFN_DH: return ffn_tc_launch<T, FFN_DH>(p, status, s);                                          \
+      case FFN_DX: return ffn_tc_launch<T, FFN_DX>(p, status, s);                                          \
+      case FFN_DWIN: return ffn_tc_launch<T, FFN_DWIN>(p, status, s);                                      \
+      default: return ffn_tc_launch<T, FFN_DWOUT>(p, status, s);                                           \
+    }                                                                                                      \
+  }
+
+}  // namespace erc
