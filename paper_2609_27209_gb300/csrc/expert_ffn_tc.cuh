@@ -41,6 +41,7 @@ constexpr int TC_STAGE = 2 * TC_OPERAND;
 constexpr int TC_SMEM = TC_STAGES * TC_STAGE + 1024;
 constexpr int TC_THREADS = 384;
 constexpr int TC_EPILOGUE = 8;              // warps that write results
+constexpr int TC_COLS = 16;                 // columns that a lane holds at a time
 constexpr unsigned TC_WAIT_LIMIT = 1u << 22;
 
 __device__ __forceinline__ uint32_t smem_at(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
@@ -64,12 +65,12 @@ __device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes) {
   asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
 }
 __device__ __forceinline__ void bar_arrive_cluster(uint32_t cluster_bar) {
-  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
+  asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
 }
 __device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
   uint32_t done;
   asm volatile(
-      "{\n.reg .pred p;\nmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}"
+      "{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}"
       : "=r"(done)
       : "r"(bar), "r"(parity)
       : "memory");
@@ -137,12 +138,9 @@ __device__ __forceinline__ void commit_pair(uint32_t bar) {
 __device__ __forceinline__ void read_tmem(uint32_t addr, float* v) {
   uint32_t* r = reinterpret_cast<uint32_t*>(v);
   asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, "
-      "%18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
       : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
-        "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]),
-        "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]),
-        "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
       : "r"(addr)
       : "memory");
 }
@@ -229,7 +227,7 @@ struct TcTiles {
   }
 };
 
-// results of 32 columns of a tile, two at a time: a lane and its neighbour swap, so that even lanes hold rows m, m + 1
+// results of TC_COLS columns of a tile, two at a time: a lane and its neighbour swap, so that even lanes hold rows m, m + 1
 // of column c and odd lanes rows m - 1, m of column c + 1
 template <class T>
 __device__ __forceinline__ void pair_up(float a, float b, int lane, float& lo, float& hi) {
@@ -239,9 +237,28 @@ __device__ __forceinline__ void pair_up(float a, float b, int lane, float& lo, f
   hi = lane & 1 ? keep : got;
 }
 
-template <class T, int WHICH>
-__device__ __forceinline__ void write_columns(const FfnArgs<T>& p, const TcTile& t, const float* v, int c0, int m_block, int lane,
-                                              int quad) {
+// DH: the pairs (a, a') and (b, b') of TC_COLS columns that a lane needs, read while the tile before them is at work
+struct PrePairs {
+  uint32_t a[TC_COLS / 2], b[TC_COLS / 2];
+};
+template <class T>
+__device__ __forceinline__ void read_pre(const FfnArgs<T>& p, const TcTile& t, int c0, int m_block, int lane, int quad, PrePairs& r) {
+  const int64_t F = p.inner;
+  const int m = t.m0 + m_block + quad * 32 + lane, odd = lane & 1;
+  const T* pre = p.pre_in + (t.n0 + c0 + odd) * 2 * F + m - odd;
+#pragma unroll
+  for (int j = 0; j < TC_COLS / 2; ++j) {
+    r.a[j] = r.b[j] = 0;
+    if (c0 + 2 * j + odd < t.valid && m < F) {
+      r.a[j] = __ldg(reinterpret_cast<const uint32_t*>(pre + 4 * j * F));
+      r.b[j] = __ldg(reinterpret_cast<const uint32_t*>(pre + (4 * j + 1) * F));
+    }
+  }
+}
+
+template <class T, int WHICH, int ACT>
+__device__ __forceinline__ void write_columns(const FfnArgs<T>& p, const TcTile& t, const float* v, const PrePairs& pre, int c0,
+                                              int m_block, int lane, int quad) {
   using H = Half2<T>;
   const int64_t D = p.width, F = p.inner;
   if constexpr (WHICH == FFN_IN) {
@@ -250,7 +267,7 @@ __device__ __forceinline__ void write_columns(const FfnArgs<T>& p, const TcTile&
     const int f = (t.m0 + m_block) / 2 + quad * 16 + (lane >> 4) * 8 + (lane & 7);
     const int odd = lane & 1;
 #pragma unroll
-    for (int j = 0; j < 32; j += 4) {
+    for (int j = 0; j < TC_COLS; j += 4) {
       float g[2], u[2], h[2];
 #pragma unroll
       for (int q = 0; q < 2; ++q) {
@@ -258,7 +275,7 @@ __device__ __forceinline__ void write_columns(const FfnArgs<T>& p, const TcTile&
         const float got = __shfl_xor_sync(0xffffffffu, up ? a : b, 8);
         g[q] = up ? got : a;
         u[q] = up ? b : got;
-        h[q] = act_value(p.act, g[q]) * u[q];
+        h[q] = act_value(ACT, g[q]) * u[q];
       }
       // columns j (even lanes) and j + 2 (odd lanes), one further for lanes of factors
       float h0, h1, g0, g1, u0, u1;
@@ -280,34 +297,21 @@ __device__ __forceinline__ void write_columns(const FfnArgs<T>& p, const TcTile&
   } else {
     const int m = t.m0 + m_block + quad * 32 + lane, odd = lane & 1, at = m - odd;
     const int64_t ld = WHICH == FFN_DH || WHICH == FFN_DWOUT ? F : D;
-    uint32_t pa[16], pb[16];
-    if constexpr (WHICH == FFN_DH) {
-#pragma unroll
-      for (int j = 0; j < 32; j += 2) {
-        const int col = c0 + j + odd;
-        pa[j / 2] = pb[j / 2] = 0;
-        if (col < t.valid && m < ld) {
-          const T* pre = p.pre_in + (t.n0 + col) * 2 * F + at;
-          pa[j / 2] = __ldg(reinterpret_cast<const uint32_t*>(pre));
-          pb[j / 2] = __ldg(reinterpret_cast<const uint32_t*>(pre + F));
-        }
-      }
-    }
     T* out = WHICH == FFN_OUT ? p.y : WHICH == FFN_DX ? p.dx : WHICH == FFN_DWIN ? p.dw_in : p.dw_out;
     if constexpr (WHICH == FFN_DWIN) out += (int64_t)t.expert * 2 * F * D;
     if constexpr (WHICH == FFN_DWOUT) out += (int64_t)t.expert * D * F;
 #pragma unroll
-    for (int j = 0; j < 32; j += 2) {
+    for (int j = 0; j < TC_COLS; j += 2) {
       float lo, hi;
       pair_up<T>(v[j], v[j + 1], lane, lo, hi);
       const int col = c0 + j + odd;
       const bool live = col < t.valid && m < ld;
       const int64_t row = t.n0 + col;
       if constexpr (WHICH == FFN_DH) {
-        const float2 a = H::unpack(pa[j / 2]), b = H::unpack(pb[j / 2]);
+        const float2 a = H::unpack(pre.a[j / 2]), b = H::unpack(pre.b[j / 2]);
         float v0, v1, s0, s1;
-        act_both(p.act, a.x, v0, s0);
-        act_both(p.act, a.y, v1, s1);
+        act_both(ACT, a.x, v0, s0);
+        act_both(ACT, a.y, v1, s1);
         if (live) {
           *reinterpret_cast<uint32_t*>(p.dpre + row * 2 * F + at) = H::pack(lo * b.x * s0, hi * b.y * s1);
           *reinterpret_cast<uint32_t*>(p.dpre + row * 2 * F + F + at) = H::pack(lo * v0, hi * v1);
@@ -320,7 +324,7 @@ __device__ __forceinline__ void write_columns(const FfnArgs<T>& p, const TcTile&
   }
 }
 
-template <class T, int WHICH>
+template <class T, int WHICH, int ACT>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(TC_THREADS, 1)
     k_ffn_tc(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const FfnArgs<T> p,
              int* __restrict__ status) {
@@ -483,7 +487,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(TC_THREADS, 1)
           for (int x = 0; x < boxes; ++x)
             for (int i = live * 8 + lane; i < 512; i += 32)
               asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(base + x * 8192 + i * 16), "r"(0) : "memory");
-          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          asm volatile("fence.proxy.async.shared::cta;\nfence.acq_rel.cluster;" ::: "memory");
         }
         __syncwarp();
         if (lane == 0) bar_arrive_cluster(peer_address(ready(s), 0));
@@ -507,26 +511,36 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(TC_THREADS, 1)
     for (int64_t at = first; ok && at < total; at += step) {
       const TcTile t = tiles.at(at, prefix, p.offsets, p.experts, p.slots);
       const int c1 = min(t.n, (part + 1) * 128);
-      float v[32];
+      float v[TC_COLS];
+      PrePairs pre, next;
       if (t.blocks == 0) {
 #pragma unroll
-        for (int i = 0; i < 32; ++i) v[i] = 0.f;
-        for (int c = part * 128; c < c1; c += 32) write_columns<T, WHICH>(p, t, v, c, m_block, lane, quad);
+        for (int i = 0; i < TC_COLS; ++i) v[i] = 0.f;
+#pragma unroll 1
+        for (int c = part * 128; c < c1; c += TC_COLS) write_columns<T, WHICH, ACT>(p, t, v, pre, c, m_block, lane, quad);
         continue;
+      }
+      if constexpr (WHICH == FFN_DH) {
+        if (part * 128 < c1) read_pre(p, t, part * 128, m_block, lane, quad, next);
       }
       ok = __all_sync(0xffffffffu, bar_wait(full(a), a_phase, &failed));
       if (!ok) break;
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
       const uint32_t src = tmem + a * 256 + ((uint32_t)(quad * 32) << 16);
-      for (int c = part * 128; c < c1; c += 32) {
+#pragma unroll 1
+      for (int c = part * 128; c < c1; c += TC_COLS) {
         read_tmem(src + c, v);
+        if constexpr (WHICH == FFN_DH) {
+          pre = next;
+          if (c + TC_COLS < c1) read_pre(p, t, c + TC_COLS, m_block, lane, quad, next);
+        }
         read_tmem_done();
-        if (c + 32 >= c1) {
+        if (c + TC_COLS >= c1) {
           asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
           __syncwarp();
           if (lane == 0) bar_arrive_cluster(peer_address(taken(a), 0));
         }
-        write_columns<T, WHICH>(p, t, v, c, m_block, lane, quad);
+        write_columns<T, WHICH, ACT>(p, t, v, pre, c, m_block, lane, quad);
       }
       if (part * 128 >= c1) {
         __syncwarp();
@@ -580,7 +594,14 @@ erc_status ffn_tc_launch(const FfnArgs<T>& p, int* status, cudaStream_t s) {
   const uint32_t box[2] = {TC_K, WHICH <= FFN_DX ? (uint32_t)TC_HALF : (uint32_t)TC_K};
   good = good && tc_encode(&b, BF, from, 2, dims, strides, box);
   if (!good) return set_error(ERC_ERR_CUDA, "a tensor map of the expert products was refused");
-  auto kernel = k_ffn_tc<T, WHICH>;
+  // the activation is fixed at compile time: with all three in one kernel the unrolled columns do not fit the
+  // instruction cache (DH of 80000 slots, 64 experts, 512 x 1024: 1048 us)
+  constexpr bool ACTS = WHICH == FFN_IN || WHICH == FFN_DH;
+  auto kernel = k_ffn_tc<T, WHICH, ERC_ACT_SILU>;
+  if constexpr (ACTS) {
+    if (p.act == ERC_ACT_GELU) kernel = k_ffn_tc<T, WHICH, ERC_ACT_GELU>;
+    if (p.act == ERC_ACT_RELU) kernel = k_ffn_tc<T, WHICH, ERC_ACT_RELU>;
+  }
   ERC_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, TC_SMEM));
   kernel<<<sm_count() / 2 * 2, TC_THREADS, TC_SMEM, s>>>(a, b, p, status);
   count_launches(1);
