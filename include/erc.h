@@ -503,7 +503,7 @@ erc_status erc_expert_ffn_backward(const erc_ffn_shape* shape, const void* dy, c
  * floor(p 2^32).  scale is 1 / (1 - p) rounded to float32; product and sum are rounded to float32 one
  * by one, the result once to `type`, so it is the same on every machine.  What is dropped is 0
  * whatever x holds.
- * In : x, residual (or NULL) [count] of `type`; p in [0, 1] (1 drops everything); key, or key_dev
+ * In : x, residual (or NULL) [count] of `type`, count <= 2^40; p in [0, 1] (1 drops everything); key, or key_dev
  *      (device, [1]) when not NULL: a captured graph that is replayed reads the key of its time;
  *      first >= 0, a multiple of 4.
  * Out: out [count] of `type`; may be x or residual itself.

@@ -252,15 +252,23 @@ erc_status simple_product(FfnProduct which, const FfnArgs<T>& p, cudaStream_t s)
   return ERC_OK;
 }
 
-// whether the tensor cores take a call
-bool on_tensor_cores(const erc_ffn_shape* f, uintptr_t all) {
-  return f->type != ERC_F32 && f->width % 8 == 0 && f->inner % 8 == 0 && all % 16 == 0;
+// how a call's products run
+enum FfnWay { FFN_SIMPLE, FFN_FEW, FFN_TENSOR };
+constexpr int64_t FEW_SLOTS = 32;  // measured: see expert_ffn_few.cu
+
+// `all`: the bits of every pointer
+FfnWay ffn_way(const erc_ffn_shape* f, uintptr_t all, bool forward) {
+  const int piece = 16 / type_bytes(f->type);
+  if (all % 16 != 0 || f->width % piece != 0 || f->inner % piece != 0) return FFN_SIMPLE;
+  if (forward && f->slots <= FEW_SLOTS) return FFN_FEW;
+  return f->type == ERC_F32 ? FFN_SIMPLE : FFN_TENSOR;
 }
 
 template <class T>
-erc_status ffn_product(bool tensor_cores, FfnProduct which, const FfnArgs<T>& p, int* status, cudaStream_t s) {
+erc_status ffn_product(FfnWay way, FfnProduct which, const FfnArgs<T>& p, int* status, cudaStream_t s) {
+  if (way == FFN_FEW) return ffn_few_product<T>(which, p, status, s);
   if constexpr (sizeof(T) == 2) {
-    if (tensor_cores) return ffn_tc_product<T>(which, p, status, s);
+    if (way == FFN_TENSOR) return ffn_tc_product<T>(which, p, status, s);
   }
   if (which == FFN_IN || which == FFN_DH) ERC_CUDA(cudaMemsetAsync(status, 0, sizeof(int), s));
   return simple_product(which, p, s);
@@ -310,7 +318,7 @@ extern "C" erc_status erc_expert_ffn(const erc_ffn_shape* f, const void* xs, con
   const uintptr_t all = any_bits({xs, w_in, w_out, y, pre});
   ERC_REQUIRE(all % type_bytes(f->type) == 0 && reinterpret_cast<uintptr_t>(offsets) % 8 == 0, "misaligned array");
   if (!ws || ws_bytes < erc_expert_ffn_workspace_size(f)) return set_error(ERC_ERR_CAPACITY, "workspace too small");
-  const bool fast = on_tensor_cores(f, all);
+  const FfnWay way = ffn_way(f, all, true);
   return with_type(f->type, [&](auto t) {
     using T = decltype(t);
     Arena ar(align_ws(ws));
@@ -322,8 +330,8 @@ extern "C" erc_status erc_expert_ffn(const erc_ffn_shape* f, const void* xs, con
     p.h = ar.take<T>((size_t)f->slots * f->inner);
     p.pre = static_cast<T*>(pre);
     p.y = static_cast<T*>(y);
-    ERC_TRY(ffn_product(fast, FFN_IN, p, status, as_stream(stream)));
-    return ffn_product(fast, FFN_OUT, p, status, as_stream(stream));
+    ERC_TRY(ffn_product(way, FFN_IN, p, status, as_stream(stream)));
+    return ffn_product(way, FFN_OUT, p, status, as_stream(stream));
   });
 }
 
@@ -350,7 +358,7 @@ extern "C" erc_status erc_expert_ffn_backward(const erc_ffn_shape* f, const void
   ERC_REQUIRE(all % type_bytes(f->type) == 0 && reinterpret_cast<uintptr_t>(offsets) % 8 == 0, "misaligned array");
   if (!ws || ws_bytes < erc_expert_ffn_backward_workspace_size(f))
     return set_error(ERC_ERR_CAPACITY, "workspace too small");
-  const bool fast = on_tensor_cores(f, all);
+  const FfnWay way = ffn_way(f, all, false);
   return with_type(f->type, [&](auto t) {
     using T = decltype(t);
     Arena ar(align_ws(ws));
@@ -366,10 +374,10 @@ extern "C" erc_status erc_expert_ffn_backward(const erc_ffn_shape* f, const void
     p.dx = static_cast<T*>(dxs);
     p.dw_in = static_cast<T*>(dw_in);
     p.dw_out = static_cast<T*>(dw_out);
-    ERC_TRY(ffn_product(fast, FFN_DH, p, status, s));
-    if (p.dx) ERC_TRY(ffn_product(fast, FFN_DX, p, status, s));
-    if (p.dw_in) ERC_TRY(ffn_product(fast, FFN_DWIN, p, status, s));
-    if (p.dw_out) ERC_TRY(ffn_product(fast, FFN_DWOUT, p, status, s));
+    ERC_TRY(ffn_product(way, FFN_DH, p, status, s));
+    if (p.dx) ERC_TRY(ffn_product(way, FFN_DX, p, status, s));
+    if (p.dw_in) ERC_TRY(ffn_product(way, FFN_DWIN, p, status, s));
+    if (p.dw_out) ERC_TRY(ffn_product(way, FFN_DWOUT, p, status, s));
     return ERC_OK;
   });
 }

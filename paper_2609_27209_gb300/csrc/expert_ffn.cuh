@@ -90,6 +90,10 @@ __device__ __forceinline__ void zero_slots(T* out, int64_t first, int64_t slots,
   for (int64_t i = first * width + thread; i < slots * width; i += threads) out[i] = from_f32<T>(0.f);
 }
 
+// IN or OUT for a handful of slots (expert_ffn_few.cu); rows of whole 16-byte pieces, 16-byte aligned arrays
+template <class T>
+erc_status ffn_few_product(FfnProduct which, const FfnArgs<T>& p, int* status, cudaStream_t s);
+
 // a product on the tensor cores (bfloat16 and float16 whose rows are whole 16-byte pieces); `status` (device) gets
 // ERC_OK at the start of IN and DH, and ERC_ERR_TIMEOUT where a wait ran out
 template <class T>

@@ -176,13 +176,18 @@ struct TcTile {
   int64_t k0, k1;   // slots of a weight gradient
 };
 
-// which tiles a product has, from the experts' slots
+// the experts' slots, and the tiles of 256 slots before each, in shared memory
+struct TcRanges {
+  int lo[ERC_ROUTE_MAX_EXPERTS], hi[ERC_ROUTE_MAX_EXPERTS];
+  int prefix[ERC_ROUTE_MAX_EXPERTS + 1];
+};
+
+// which tiles a product has
 template <int WHICH>
 struct TcTiles {
   static constexpr bool SLOTS = WHICH <= FFN_DX;
   int m_tiles, n_tiles, depth;  // n_tiles: of a weight gradient
   int n_total, wide;            // a weight gradient's n, and its columns a tile
-  int64_t total;
   __device__ __forceinline__ void init(int D, int F) {
     const int m = WHICH == FFN_IN ? 2 * F : WHICH == FFN_DH || WHICH == FFN_DWOUT ? F : D;
     m_tiles = (m + 255) / 256;
@@ -191,37 +196,33 @@ struct TcTiles {
     wide = n_total <= 128 ? 128 : 256;
     n_tiles = (n_total + wide - 1) / wide;
   }
-  // prefix[e]: tiles of 256 slots of the experts before e
-  __device__ __forceinline__ TcTile at(int64_t t, const int* prefix, const int64_t* offsets, int experts, int64_t slots) const {
+  __device__ __forceinline__ TcTile at(int t, const TcRanges& of, int experts) const {
     TcTile r;
     if (SLOTS) {
-      const int of = (int)(t / m_tiles);
-      r.m0 = (int)(t - (int64_t)of * m_tiles) * 256;
-      int lo = 0, hi = experts;  // the last expert with prefix[e] <= of
+      const int block = t / m_tiles;
+      r.m0 = (t - block * m_tiles) * 256;
+      int lo = 0, hi = experts;  // the last expert with prefix[e] <= block
       while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
-        if (prefix[mid] <= of) lo = mid; else hi = mid;
+        if (of.prefix[mid] <= block) lo = mid; else hi = mid;
       }
       r.expert = lo;
-      const SlotRange s = slot_range(offsets, lo, slots);
-      r.n0 = s.lo + (int64_t)(of - prefix[lo]) * 256;
-      const int64_t left = s.hi - r.n0;
-      r.valid = left < 256 ? (int)left : 256;
+      r.n0 = of.lo[lo] + (block - of.prefix[lo]) * 256;
+      r.valid = min(of.hi[lo] - (int)r.n0, 256);
       r.n = (r.valid + 31) & ~31;  // a pair's products take multiples of 32
       r.k0 = r.k1 = 0;
       r.blocks = (depth + TC_K - 1) / TC_K;
     } else {
       const int each = m_tiles * n_tiles;
-      r.expert = (int)(t / each);
-      const int rest = (int)(t - (int64_t)r.expert * each);
+      r.expert = t / each;
+      const int rest = t - r.expert * each;
       r.m0 = rest % m_tiles * 256;
       r.n0 = rest / m_tiles * wide;
       r.n = wide;
-      r.valid = n_total - r.n0 < wide ? (int)(n_total - r.n0) : wide;
-      const SlotRange s = slot_range(offsets, r.expert, slots);
-      r.k0 = s.lo;
-      r.k1 = s.hi;
-      r.blocks = (int)((s.hi - s.lo + TC_K - 1) / TC_K);
+      r.valid = min(n_total - (int)r.n0, wide);
+      r.k0 = of.lo[r.expert];
+      r.k1 = of.hi[r.expert];
+      r.blocks = (int)((r.k1 - r.k0 + TC_K - 1) / TC_K);
     }
     return r;
   }
@@ -332,7 +333,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(TC_THREADS, 1)
   constexpr bool A_K = WHICH == FFN_IN || WHICH == FFN_OUT, B_K = SLOTS;
   extern __shared__ char raw[];
   __shared__ __align__(8) uint64_t bars[3 * TC_STAGES + 5];
-  __shared__ int prefix[ERC_ROUTE_MAX_EXPERTS + 1];
+  __shared__ TcRanges of;
   __shared__ uint32_t tmem_base;
   __shared__ volatile int failed;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -366,25 +367,32 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(TC_THREADS, 1)
   }
   TcTiles<WHICH> tiles;
   tiles.init(p.width, p.inner);
+  if constexpr (WHICH != FFN_IN && WHICH != FFN_DH) {
+    // everything before this point overlaps the product before, whose results are read from here on
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+  }
+  asm volatile("griddepcontrol.launch_dependents;");
+  for (int e = threadIdx.x; e < p.experts; e += TC_THREADS) {
+    const SlotRange r = slot_range(p.offsets, e, p.slots);
+    of.lo[e] = (int)r.lo;
+    of.hi[e] = (int)r.hi;
+    of.prefix[e + 1] = (int)((r.hi - r.lo + 255) / 256);
+  }
   if (SLOTS) {
-    for (int e = threadIdx.x; e < p.experts; e += TC_THREADS) {
-      const SlotRange r = slot_range(p.offsets, e, p.slots);
-      prefix[e + 1] = (int)((r.hi - r.lo + 255) / 256);
-    }
     __syncthreads();
     if (warp == 0) {
       int before = 0;
       for (int e0 = 0; e0 < p.experts; e0 += 32) {
-        int x = e0 + lane < p.experts ? prefix[e0 + lane + 1] : 0;
+        int x = e0 + lane < p.experts ? of.prefix[e0 + lane + 1] : 0;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
           const int y = __shfl_up_sync(0xffffffffu, x, o);
           if (lane >= o) x += y;
         }
-        if (e0 + lane < p.experts) prefix[e0 + lane + 1] = before + x;
+        if (e0 + lane < p.experts) of.prefix[e0 + lane + 1] = before + x;
         before += __shfl_sync(0xffffffffu, x, 31);
       }
-      if (lane == 0) prefix[0] = 0;
+      if (lane == 0) of.prefix[0] = 0;
     }
   }
   if (blockIdx.x == 0 && threadIdx.x == 0 && (WHICH == FFN_IN || WHICH == FFN_DH)) *status = ERC_OK;
@@ -393,9 +401,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(TC_THREADS, 1)
   cluster_arrive_wait();
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
   const uint32_t tmem = tmem_base;
-  const int64_t total = SLOTS ? (int64_t)prefix[p.experts] * tiles.m_tiles
-                              : (int64_t)p.experts * tiles.m_tiles * tiles.n_tiles;
-  const int64_t first = blockIdx.x >> 1, step = gridDim.x >> 1;
+  const int total = SLOTS ? of.prefix[p.experts] * tiles.m_tiles : p.experts * tiles.m_tiles * tiles.n_tiles;
+  const int first = blockIdx.x >> 1, step = gridDim.x >> 1;
   const int m_block = rank * TC_HALF;
 
   if (warp == 0) {
@@ -403,8 +410,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(TC_THREADS, 1)
       int s = 0;
       uint32_t phase = 0, issued = 0;
       bool ok = true;
-      for (int64_t at = first; ok && at < total; at += step) {
-        const TcTile t = tiles.at(at, prefix, p.offsets, p.experts, p.slots);
+      for (int at = first; ok && at < total; at += step) {
+        const TcTile t = tiles.at(at, of, p.experts);
         const int m = t.m0 + m_block, n_half = t.n / 2;
         for (int b = 0; b < t.blocks; ++b) {
           if (!(ok = bar_wait(empty(s), phase ^ 1, &failed))) break;
@@ -444,8 +451,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(TC_THREADS, 1)
       int s = 0, a = 0;
       uint32_t phase = 0, a_phase = 0;
       bool ok = true;
-      for (int64_t at = first; ok && at < total; at += step) {
-        const TcTile t = tiles.at(at, prefix, p.offsets, p.experts, p.slots);
+      for (int at = first; ok && at < total; at += step) {
+        const TcTile t = tiles.at(at, of, p.experts);
         if (t.blocks == 0) continue;
         const uint32_t idesc = (1u << 4) | (Half2<T>::FORMAT << 7) | (Half2<T>::FORMAT << 10) | ((A_K ? 0u : 1u) << 15) |
                                ((B_K ? 0u : 1u) << 16) | ((uint32_t)(t.n >> 3) << 17) | ((256u >> 4) << 24);
@@ -475,8 +482,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(TC_THREADS, 1)
     int s = 0;
     uint32_t phase = 0;
     bool ok = true;
-    for (int64_t at = first; ok && at < total; at += step) {
-      const TcTile t = tiles.at(at, prefix, p.offsets, p.experts, p.slots);
+    for (int at = first; ok && at < total; at += step) {
+      const TcTile t = tiles.at(at, of, p.experts);
       for (int b = 0; b < t.blocks; ++b) {
         if (!(ok = __all_sync(0xffffffffu, bar_wait(land(s), phase, &failed)))) break;
         if (!SLOTS && t.k0 + (b + 1) * TC_K > t.k1) {
@@ -508,8 +515,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(TC_THREADS, 1)
     int a = 0;
     uint32_t a_phase = 0;
     bool ok = true;
-    for (int64_t at = first; ok && at < total; at += step) {
-      const TcTile t = tiles.at(at, prefix, p.offsets, p.experts, p.slots);
+    for (int at = first; ok && at < total; at += step) {
+      const TcTile t = tiles.at(at, of, p.experts);
       const int c1 = min(t.n, (part + 1) * 128);
       float v[TC_COLS];
       PrePairs pre, next;
@@ -603,9 +610,18 @@ erc_status ffn_tc_launch(const FfnArgs<T>& p, int* status, cudaStream_t s) {
     if (p.act == ERC_ACT_RELU) kernel = k_ffn_tc<T, WHICH, ERC_ACT_RELU>;
   }
   ERC_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, TC_SMEM));
-  kernel<<<sm_count() / 2 * 2, TC_THREADS, TC_SMEM, s>>>(a, b, p, status);
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(sm_count() / 2 * 2);
+  cfg.blockDim = dim3(TC_THREADS);
+  cfg.dynamicSmemBytes = TC_SMEM;
+  cfg.stream = s;
+  cudaLaunchAttribute after[1];
+  after[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  after[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = after;
+  cfg.numAttrs = ACTS ? 0 : 1;  // the first product of a call starts when the work before the call is done
+  ERC_CUDA(cudaLaunchKernelEx(&cfg, kernel, a, b, p, status));
   count_launches(1);
-  ERC_CUDA(cudaGetLastError());
   return ERC_OK;
 }
 
