@@ -254,13 +254,16 @@ erc_status simple_product(FfnProduct which, const FfnArgs<T>& p, cudaStream_t s)
 
 // how a call's products run
 enum FfnWay { FFN_SIMPLE, FFN_FEW, FFN_TENSOR };
-constexpr int64_t FEW_SLOTS = 32;  // measured: see expert_ffn_few.cu
+// Few slots read the weights without the tensor cores.  IN + OUT, both ways (us; bfloat16): one expert of 2048 x 2048, 8
+// slots 23 / 39, 16 slots 43 / 39; 8 experts of 512 x 1024, 16 slots 18 / 27, 32 slots 19 / 27; 64 experts of
+// 1024 x 512, 32 slots 42 / 45.
+bool few_slots(const erc_ffn_shape* f) { return f->slots <= 8 || (f->slots <= 32 && f->slots <= 4 * f->experts); }
 
 // `all`: the bits of every pointer
 FfnWay ffn_way(const erc_ffn_shape* f, uintptr_t all, bool forward) {
   const int piece = 16 / type_bytes(f->type);
   if (all % 16 != 0 || f->width % piece != 0 || f->inner % piece != 0) return FFN_SIMPLE;
-  if (forward && f->slots <= FEW_SLOTS) return FFN_FEW;
+  if (forward && few_slots(f)) return FFN_FEW;
   return f->type == ERC_F32 ? FFN_SIMPLE : FFN_TENSOR;
 }
 

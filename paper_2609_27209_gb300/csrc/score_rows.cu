@@ -7,9 +7,9 @@
 // exponential and no part scales its sums.  Parts join by d = (m_part - m) c: u <- 2^d (u + d T), T <- 2^d T.
 // t is kept above -1000, where 2^t is 0, so that no product of 0 and infinity appears.
 //
-// The best entries need no pass of their own: the first one notes the largest score of each 32 vectors
-// (a segment, 512 bytes).  The k segments with the best maxima (ties to the first) hold the k best
-// entries: an entry elsewhere is behind the k maxima.  Only these are searched, in shared memory.
+// The best entries: the k-th largest of the threads' maxima (found bit by bit, 20 bits) bounds the k-th best entry from
+// below, so only the few entries from it on are ranked.  Where many are equal, the k-th best key and the last index
+// that belongs are found the same way among all entries.
 //
 // Up to 8 parts are a cluster, whose first block joins them through distributed shared memory; more go
 // through a workspace and a second kernel.
@@ -53,6 +53,15 @@ __device__ __forceinline__ Sum join(Sum a, Sum b, float c) {
   raise(b, m, c);
   return {m, a.T + b.T, a.u + b.u};
 }
+// the parts of `width` neighbouring lanes joined
+__device__ __forceinline__ Sum lane_join(Sum a, float c, int width) {
+  for (int o = width / 2; o; o >>= 1) {
+    const Sum b = {__shfl_xor_sync(0xffffffffu, a.m, o), __shfl_xor_sync(0xffffffffu, a.T, o),
+                   __shfl_xor_sync(0xffffffffu, a.u, o)};
+    a = join(a, b, c);  // the same on both sides: sums and maxima commute
+  }
+  return a;
+}
 // the largest score of a warp, and a sum over it
 __device__ __forceinline__ float warp_max(float v) {
   return order_value(__reduce_max_sync(0xffffffffu, order_key(v)));
@@ -63,17 +72,99 @@ __device__ __forceinline__ float warp_sum(float v) {
   return v;
 }
 
-// the terms of a vector, with the maximum known
-template <class T>
-__device__ __forceinline__ void add_vector(Sum& a, uint4 v, float c) {
-  float l[ScoreVec<T>::N];
-  unpack_scores(v, l, T());
-#pragma unroll
-  for (int i = 0; i < ScoreVec<T>::N; ++i) {
-    const float t = scaled(l[i], a.m, c), e = exp2_fast(t);
-    a.T += e;
-    a.u = fmaf(e, t, a.u);
+// The terms of entries whose maximum m is known.  t = l c - fl(m c) is one fma, for two entries at once; the
+// rounding of m c moves every t by the same d = m c - fl(m c) (t is d at the maximum), which `settle` takes out
+// again.  Masked entries and NaN are raised to `low`, about 1000 / c below m, where 2^t is 0: one maximum of the
+// stored type.  Rows where that does not hold (a maximum or a scale that is infinite, far from 0 or out of the type's
+// range) take the terms one by one.
+struct Scale {
+  float m, c, minus_mc, low;
+  bool plain;  // packed terms do
+  __device__ __forceinline__ Scale(float m_, float c_) : m(m_), c(c_) {
+    minus_mc = -__fmul_rn(m, c);
+    low = m - __fdividef(1000.f, c);
+    plain = fabsf(minus_mc) < 1e4f && c > 0.1f && c < 1e4f && low > -6e4f;
   }
+};
+// a vector's entries, raised to low, as pairs
+__device__ __forceinline__ void raised_pairs(uint4 v, float low, uint64_t* p, float) {
+  p[0] = pair(fmaxf(__uint_as_float(v.x), low), fmaxf(__uint_as_float(v.y), low));
+  p[1] = pair(fmaxf(__uint_as_float(v.z), low), fmaxf(__uint_as_float(v.w), low));
+}
+__device__ __forceinline__ void raised_pairs(uint4 v, float low, uint64_t* p, __nv_bfloat16) {
+  const __nv_bfloat162 l = __float2bfloat162_rn(low);
+  const unsigned w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const __nv_bfloat162 h = __hmax2(*reinterpret_cast<const __nv_bfloat162*>(&w[i]), l);
+    const unsigned b = *reinterpret_cast<const unsigned*>(&h);
+    p[i] = pair(__uint_as_float(b << 16), __uint_as_float(b & 0xffff0000u));
+  }
+}
+__device__ __forceinline__ void raised_pairs(uint4 v, float low, uint64_t* p, __half) {
+  const __half2 l = __float2half2_rn(low);
+  const unsigned w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float2 f = __half22float2(__hmax2(*reinterpret_cast<const __half2*>(&w[i]), l));
+    p[i] = pair(f.x, f.y);
+  }
+}
+struct Terms {
+  uint64_t T = 0, u = 0;  // two sums each
+};
+template <class T>
+__device__ __forceinline__ void add_vector(Terms& a, uint4 v, const Scale& s) {
+  constexpr int P = ScoreVec<T>::N / 2;
+  if (s.plain) {
+    uint64_t l[P];
+    raised_pairs(v, s.low, l, T());
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+      const uint64_t t = fma2(l[i], pair(s.c, s.c), pair(s.minus_mc, s.minus_mc));
+      float t0, t1;
+      unpair(t, t0, t1);
+      const uint64_t e = pair(exp2_fast(t0), exp2_fast(t1));
+      a.T = add2(a.T, e);
+      a.u = fma2(e, t, a.u);
+    }
+  } else {
+    float l[2 * P];
+    unpack_scores(v, l, T());
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+      const float t0 = scaled(l[2 * i], s.m, s.c), t1 = scaled(l[2 * i + 1], s.m, s.c);
+      const uint64_t e = pair(exp2_fast(t0), exp2_fast(t1));
+      a.T = add2(a.T, e);
+      a.u = fma2(e, pair(t0, t1), a.u);
+    }
+  }
+}
+// the terms of two entries, masked ones -inf
+__device__ __forceinline__ void add_pair(Terms& a, float l0, float l1, const Scale& s) {
+  float t0, t1;
+  if (s.plain) {
+    t0 = fmaf(fmaxf(l0, s.low), s.c, s.minus_mc);
+    t1 = fmaf(fmaxf(l1, s.low), s.c, s.minus_mc);
+  } else {
+    t0 = scaled(l0, s.m, s.c);
+    t1 = scaled(l1, s.m, s.c);
+  }
+  const uint64_t e = pair(exp2_fast(t0), exp2_fast(t1));
+  a.T = add2(a.T, e);
+  a.u = fma2(e, pair(t0, t1), a.u);
+}
+// the sums over a warp's or a group's lanes, with d taken out: 2^-d (T, u - d T)
+__device__ __forceinline__ Sum settle(Sum a, const Scale& s) {
+  if (!s.plain) return a;
+  const float d = fmaf(s.m, s.c, s.minus_mc), f = exp2_fast(-d);
+  return {a.m, f * a.T, f * fmaf(-d, a.T, a.u)};
+}
+__device__ __forceinline__ Sum sum_of(const Terms& a, float m) {
+  float T0, T1, u0, u1;
+  unpair(a.T, T0, T1);
+  unpair(a.u, u0, u1);
+  return {m, T0 + T1, u0 + u1};
 }
 
 struct ScoreOut {
@@ -124,73 +215,78 @@ __device__ __forceinline__ bool ahead(unsigned ka, unsigned ia, unsigned kb, uns
   return ka > kb || (ka == kb && ia < ib);
 }
 
+constexpr int CAP = 256;  // entries that are ranked at once
 struct TopScratch {
-  unsigned seg[MAX_PARTS];  // best key of each segment
-  int chosen[KMAX];         // the k best segments, best first
-  unsigned least;           // the key of the last of them
-  int segments, found;
-  Best list[KMAX * KMAX];   // what they hold from `least` on, at most k of each
+  Best list[CAP];
+  int found, sum;
 };
 
-// The k best of the entries behind s.seg[0 .. nseg): fetch(segment, lane, e, keys, ids) gives the
-// e-th of a lane's ENTRIES of a segment.  put(rank, key, id) takes the results.
-template <int ENTRIES, class Fetch, class Put>
-__device__ __forceinline__ void select_top(TopScratch& s, int nseg, int k, Fetch&& fetch, Put&& put) {
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  if (tid == 0) s.segments = s.found = 0, s.least = 0;
+// the sum of a count over the block's threads
+__device__ __forceinline__ int block_count(TopScratch& s, int mine) {
+  mine = __reduce_add_sync(0xffffffffu, mine);
+  if ((threadIdx.x & 31) == 0) atomicAdd(&s.sum, mine);
   __syncthreads();
-  for (int i = tid; i < nseg; i += ST) {
-    const unsigned mine = s.seg[i];
-    if (mine <= MASKED_KEY) continue;
-    int before = 0;
-    for (int j = 0; j < nseg; ++j) before += ahead(s.seg[j], j, mine, i);
-    if (before < k) {
-      s.chosen[before] = i;
-      atomicMax(&s.segments, before + 1);
-      if (before == k - 1) s.least = mine;
-    }
+  const int v = s.sum;
+  __syncthreads();
+  if (threadIdx.x == 0) s.sum = 0;
+  __syncthreads();
+  return v;
+}
+
+// The k best of a block's entries: each(least, f) calls f(key, id) for the thread's entries of at least that key, or for
+// more; `mine` is the largest key of the thread's entries (0: none).  put(rank, key, id) takes the results, (0, 0) where
+// there are fewer than k.
+template <class Each, class Put>
+__device__ __forceinline__ void block_top(TopScratch& s, unsigned mine, int k, Each&& each, Put&& put) {
+  const int tid = threadIdx.x;
+  if (mine <= MASKED_KEY) mine = 0;
+  unsigned least = 0;
+  if (tid == 0) s.found = s.sum = 0;
+  for (int bit = 31; bit >= 12; --bit) {
+    const unsigned t = least | (1u << bit);
+    if (__syncthreads_count(mine >= t) >= k) least = t;
   }
+  least = max(least, MASKED_KEY + 1);
+  each(least, [&](unsigned key, unsigned id) {
+    if (key < least) return;
+    const int at = atomicAdd(&s.found, 1);
+    if (at < CAP) s.list[at] = {key, id};
+  });
   __syncthreads();
-  const unsigned least = max(s.least, MASKED_KEY + 1);
-  for (int j = warp; j < s.segments; j += SW) {
-    unsigned key[ENTRIES], id[ENTRIES];
-    int mine = 0;
-    fetch(s.chosen[j], lane, key, id);
-#pragma unroll
-    for (int i = 0; i < ENTRIES; ++i) {
-      if (key[i] < least) key[i] = 0;
-      mine += key[i] != 0;
+  int found = s.found;
+  if (found > CAP) {
+    unsigned edge = 0, last = 0;  // the k-th best key, and the last index that belongs among those equal to it
+    for (int bit = 31; bit >= 0; --bit) {
+      const unsigned t = edge | (1u << bit);
+      int c = 0;
+      each(t, [&](unsigned key, unsigned) { c += key >= t; });
+      if (block_count(s, c) >= k) edge = t;
     }
-    const int all = __reduce_add_sync(0xffffffffu, mine);
-    if (all <= k) {
-      int at = mine ? atomicAdd(&s.found, mine) : 0;
-#pragma unroll
-      for (int i = 0; i < ENTRIES; ++i)
-        if (key[i]) s.list[at++] = {key[i], id[i]};
-    } else {  // many equal ones: the first k of the segment, one after another
-      for (int r = 0; r < k; ++r) {
-        unsigned bk = 0, bi = 0xffffffffu;
-#pragma unroll
-        for (int i = 0; i < ENTRIES; ++i)
-          if (key[i] && ahead(key[i], id[i], bk, bi)) bk = key[i], bi = id[i];
-        const unsigned top = __reduce_max_sync(0xffffffffu, bk);
-        const unsigned first = __reduce_min_sync(0xffffffffu, bk == top ? bi : 0xffffffffu);
-        if (lane == 0) s.list[atomicAdd(&s.found, 1)] = {top, first};
-#pragma unroll
-        for (int i = 0; i < ENTRIES; ++i)
-          if (id[i] == first) key[i] = 0;
-      }
+    int above = 0;
+    each(edge, [&](unsigned key, unsigned) { above += key > edge; });
+    const int need = k - block_count(s, above);
+    for (int bit = 22; bit >= 0; --bit) {
+      const unsigned t = last | (1u << bit);
+      int c = 0;
+      each(edge, [&](unsigned key, unsigned id) { c += key == edge && id < t; });
+      if (block_count(s, c) < need) last = t;
     }
+    if (tid == 0) s.found = 0;
+    __syncthreads();
+    each(edge, [&](unsigned key, unsigned id) {
+      if (key > edge || (key == edge && id <= last)) s.list[atomicAdd(&s.found, 1)] = {key, id};
+    });
+    __syncthreads();
+    found = s.found;
   }
-  __syncthreads();
-  const int found = s.found;
-  for (int i = tid; i < found; i += ST) {
-    const Best b = s.list[i];
+  if (tid < found) {
+    const Best b = s.list[tid];
     int before = 0;
     for (int j = 0; j < found; ++j) before += ahead(s.list[j].key, s.list[j].id, b.key, b.id);
     if (before < k) put(before, b.key, b.id);
   }
-  for (int r = found + tid; r < k; r += ST) put(r, 0u, 0u);  // fewer than k
+  if (tid >= found && tid < k) put(tid, 0u, 0u);
+  __syncthreads();
 }
 
 __device__ __forceinline__ void put_best(const ScoreOut& o, int64_t row, Sum a, float lnT, int rank, unsigned key,
@@ -239,8 +335,7 @@ __device__ __forceinline__ bool landed(uint32_t bar, uint32_t parity) {
   return false;
 }
 
-template <class T>
-constexpr int part_smem(bool top) { return SEGS * 512 + (top ? (int)sizeof(TopScratch) : 0); }
+constexpr int part_smem(int per, bool top) { return per * 16 + (top ? (int)sizeof(TopScratch) : 0); }
 
 // A block takes one of the `parts` of a row, `per` vectors each (a multiple of 32).  CLUSTERED: the parts of a row are a
 // cluster.  Blocks start with a task and take every gridDim.x-th one.
@@ -249,15 +344,14 @@ __global__ void __launch_bounds__(ST) k_score_part(int64_t rows, int64_t n, cons
                                                    int parts, int per, ScoreOut o, Sum* __restrict__ sums,
                                                    Best* __restrict__ best) {
   constexpr int N = ScoreVec<T>::N;
-  constexpr unsigned NONE = 0xffffffffu;
-  __shared__ Sum part[SW];
+    __shared__ Sum part[SW];
   __shared__ Sum joined;
   __shared__ float top_of[SW];
-  __shared__ Best mine[KMAX];
+  __shared__ Best kept[KMAX];
   __shared__ __align__(8) uint64_t bar_word;
   extern __shared__ __align__(16) char smem[];
   uint4* held = reinterpret_cast<uint4*>(smem);
-  TopScratch& top = *reinterpret_cast<TopScratch*>(smem + SEGS * 512);
+  TopScratch& top = *reinterpret_cast<TopScratch*>(smem + per * 16);
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const uint32_t bar = shared_at(&bar_word);
   if (tid == 0) {
@@ -300,45 +394,38 @@ __global__ void __launch_bounds__(ST) k_score_part(int64_t rows, int64_t n, cons
     }
     ok = __syncthreads_and(ok);
 
-    float m = LOWEST;
-    for (int v0 = warp * 32; v0 < count; v0 += ST) {
-      const int at = v0 + lane;
-      const float here = at < count ? max_score(held[at], T()) : -INFINITY;
-      if (TOP) {
-        const unsigned key = __reduce_max_sync(NONE, order_key(__fadd_rn(here, 0.f)));
-        if (lane == 0) top.seg[v0 / 32] = key;
-      }
-      m = fmaxf(m, here);
-    }
+    float m = -INFINITY;
+    for (int at = tid; at < count; at += ST) m = fmaxf(m, max_score(held[at], T()));
+    const unsigned mine = order_key(__fadd_rn(m, 0.f));
+    m = fmaxf(m, LOWEST);
     m = warp_max(m);
     if (lane == 0) top_of[warp] = m;
     __syncthreads();
 #pragma unroll
     for (int w = 0; w < SW; ++w) m = fmaxf(m, top_of[w]);
-    Sum a = {m, 0.f, 0.f};
-    for (int at = tid; at < count; at += ST) add_vector<T>(a, held[at], o.c);
-    a = block_sum(a, part);
+    const Scale scale(m, o.c);
+    Terms terms;
+    for (int at = tid; at < count; at += ST) add_vector<T>(terms, held[at], scale);
+    Sum a = settle(block_sum(sum_of(terms, m), part), scale);
     if (!ok) a = {NAN, NAN, NAN};
     if (TOP) {
       const bool alone = !CLUSTERED && parts == 1;
       const float lnT = alone && a.T > 0.f ? logf(a.T) : -INFINITY;
-      select_top<N>(
-          top, (count + 31) / 32, o.k,
-          [&](int seg, int l, unsigned* key, unsigned* id) {
-            const int at = seg * 32 + l;
-            float s[N];
-            uint4 v = make_uint4(masked_word<T>(), masked_word<T>(), masked_word<T>(), masked_word<T>());
-            if (at < count) v = held[at];
-            unpack_scores(v, s, T());
+      block_top(
+          top, mine, o.k,
+          [&](unsigned least, auto&& f) {
+            for (int at = tid; at < count; at += ST) {
+              const uint4 v = held[at];
+              if (order_key(__fadd_rn(max_score(v, T()), 0.f)) < least) continue;
+              float s[N];
+              unpack_scores(v, s, T());
 #pragma unroll
-            for (int i = 0; i < N; ++i) {
-              key[i] = order_key(__fadd_rn(s[i], 0.f));
-              id[i] = (unsigned)((first + at) * N + i - view.skew);
+              for (int i = 0; i < N; ++i) f(order_key(__fadd_rn(s[i], 0.f)), (unsigned)((first + at) * N + i - view.skew));
             }
           },
           [&](int rank, unsigned key, unsigned id) {
             if (CLUSTERED)
-              mine[rank] = {key, id};
+              kept[rank] = {key, id};
             else if (alone)
               put_best(o, row, a, lnT, rank, key, id);
             else
@@ -349,28 +436,23 @@ __global__ void __launch_bounds__(ST) k_score_part(int64_t rows, int64_t n, cons
       if (tid == 0) joined = a;
       cluster_sync_all();
       if (which == 0) {
-        Sum all = a;
-        for (int p = 1; p < parts; ++p) {
-          const uint32_t at = of_block(shared_at(&joined), p);
-          const Sum other = {__uint_as_float(peer_word(at)), __uint_as_float(peer_word(at + 4)),
-                             __uint_as_float(peer_word(at + 8))};
-          all = join(all, other, o.c);
+        Sum all = {LOWEST, 0.f, 0.f};
+        if (lane < parts) {
+          const uint32_t at = of_block(shared_at(&joined), lane);
+          all = {__uint_as_float(peer_word(at)), __uint_as_float(peer_word(at + 4)), __uint_as_float(peer_word(at + 8))};
         }
+        all = lane_join(all, o.c, CLUSTER);
+        all = {__shfl_sync(0xffffffffu, all.m, 0), __shfl_sync(0xffffffffu, all.T, 0), __shfl_sync(0xffffffffu, all.u, 0)};
         if (tid == 0) finish_row(o, row, g, all);
         if (TOP) {
           const float lnT = all.T > 0.f ? logf(all.T) : -INFINITY;
-          if (tid < parts) top.seg[tid] = peer_word(of_block(shared_at(&mine[0].key), tid));
-          __syncthreads();
-          select_top<1>(
-              top, parts, o.k,
-              [&](int p, int l, unsigned* key, unsigned* id) {
-                key[0] = id[0] = 0;
-                if (l < o.k) {
-                  const uint32_t at = of_block(shared_at(&mine[l]), p);
-                  key[0] = peer_word(at);
-                  id[0] = peer_word(at + 4);
-                }
-              },
+          Best one = {0u, 0u};  // parts * k entries, at most one a thread
+          if (tid < parts * o.k) {
+            const uint32_t at = of_block(shared_at(&kept[tid % o.k]), tid / o.k);
+            one = {peer_word(at), peer_word(at + 4)};
+          }
+          block_top(
+              top, one.key, o.k, [&](unsigned, auto&& f) { f(one.key, one.id); },
               [&](int rank, unsigned key, unsigned id) { put_best(o, row, all, lnT, rank, key, id); });
         }
       }
@@ -400,15 +482,7 @@ __global__ void __launch_bounds__(ST) k_score_join(int64_t rows, int64_t n, cons
     if (threadIdx.x == 0) g = given_of(o, row, logits + row * stride, n);
     Sum a = {LOWEST, 0.f, 0.f};
     for (int p = threadIdx.x; p < parts; p += ST) a = join(a, sums[row * parts + p], o.c);
-    const Best* mine = best + row * parts * o.k;
-    if (TOP)
-      for (int p = threadIdx.x; p < parts; p += ST) top.seg[p] = mine[p * o.k].key;
-#pragma unroll
-    for (int w = 16; w; w >>= 1) {
-      const Sum b = {__shfl_xor_sync(0xffffffffu, a.m, w), __shfl_xor_sync(0xffffffffu, a.T, w),
-                     __shfl_xor_sync(0xffffffffu, a.u, w)};
-      a = join(a, b, o.c);  // the same on both sides: sums and maxima commute
-    }
+    a = lane_join(a, o.c, 32);
     if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = a;
     __syncthreads();
     a = part[0];
@@ -417,12 +491,16 @@ __global__ void __launch_bounds__(ST) k_score_join(int64_t rows, int64_t n, cons
     if (threadIdx.x == 0) finish_row(o, row, g, a);
     if (TOP) {
       const float lnT = a.T > 0.f ? logf(a.T) : -INFINITY;
-      select_top<1>(
-          top, parts, o.k,
-          [&](int p, int l, unsigned* key, unsigned* id) {
-            const Best b = l < o.k ? mine[p * o.k + l] : Best{0u, 0u};
-            key[0] = b.key;
-            id[0] = b.id;
+      const Best* from = best + row * parts * o.k;
+      unsigned mine = 0;
+      for (int i = threadIdx.x; i < parts * o.k; i += ST) mine = max(mine, from[i].key);
+      block_top(
+          top, mine, o.k,
+          [&](unsigned, auto&& f) {
+            for (int i = threadIdx.x; i < parts * o.k; i += ST) {
+              const Best b = from[i];
+              f(b.key, b.id);
+            }
           },
           [&](int rank, unsigned key, unsigned id) { put_best(o, row, a, lnT, rank, key, id); });
     }
@@ -430,56 +508,144 @@ __global__ void __launch_bounds__(ST) k_score_join(int64_t rows, int64_t n, cons
   }
 }
 
-// a warp takes a row of at most 32 VPL vectors
-template <class T, int VPL, bool TOP>
-__global__ void __launch_bounds__(ST) k_score_short(int64_t rows, int64_t n, const T* __restrict__ logits, int64_t stride,
-                                                    ScoreOut o) {
+// a row as whole aligned vectors, and the few entries before and behind them
+template <class T>
+struct ShortRow {
+  const uint4* whole;
+  int vectors, head, tail, tail_at;  // entries before the vectors, behind them, and where those start
+  __device__ __forceinline__ ShortRow(const T* row, int n) {
+    constexpr int N = ScoreVec<T>::N;
+    const int skew = (int)((reinterpret_cast<uintptr_t>(row) & 15) / sizeof(T));
+    head = skew ? min(N - skew, n) : 0;
+    vectors = (n - head) / N;
+    tail_at = head + vectors * N;
+    tail = n - tail_at;
+    whole = reinterpret_cast<const uint4*>(row + head);
+  }
+};
+
+constexpr int SHORT_CAP = 128;
+
+// LANES neighbouring lanes take a row of at most LANES VPL whole vectors (LANES = 32 with TOP)
+template <class T, int LANES, int VPL, bool TOP>
+__global__ void __launch_bounds__(ST, TOP ? 3 : 4) k_score_short(int64_t rows, int64_t n, const T* __restrict__ logits,
+                                                                 int64_t stride, ScoreOut o) {
   constexpr int N = ScoreVec<T>::N;
-  const int lane = threadIdx.x & 31;
-  for (int64_t row = ((int64_t)blockIdx.x * ST + threadIdx.x) >> 5; row < rows; row += (int64_t)gridDim.x * SW) {
+  constexpr int EACH = ST / LANES;  // rows of a block
+  constexpr unsigned ALL = 0xffffffffu;
+  __shared__ Best list[TOP ? SW : 1][SHORT_CAP];
+  __shared__ int found[SW];
+  const int at0 = threadIdx.x % LANES, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  for (int64_t row0 = (int64_t)blockIdx.x * EACH; row0 < rows; row0 += (int64_t)gridDim.x * EACH) {
+    const int64_t row = min(row0 + threadIdx.x / LANES, rows - 1);  // a group without a row of its own repeats the last
+    const bool mine = row0 + threadIdx.x / LANES < rows;
     const T* x = logits + row * stride;
-    const RowView<T> view(x, n);
+    const ShortRow<T> view(x, (int)n);
     uint4 v[VPL];
-    float m = LOWEST;
 #pragma unroll
     for (int j = 0; j < VPL; ++j) {
-      const int at = j * 32 + lane;
-      if (at < view.vectors)
-        v[j] = view.fetch(at);
-      else
-        v[j] = make_uint4(masked_word<T>(), masked_word<T>(), masked_word<T>(), masked_word<T>());
+      const int at = j * LANES + at0;
+      v[j] = at < view.vectors ? __ldg(view.whole + at)
+                               : make_uint4(masked_word<T>(), masked_word<T>(), masked_word<T>(), masked_word<T>());
     }
+    const float head = at0 < view.head ? clean_score(to_f32(x[at0])) : -INFINITY;
+    const float tail = at0 < view.tail ? clean_score(to_f32(x[view.tail_at + at0])) : -INFINITY;
     Given g = {-1, 0.f};
-    if (lane == 0) g = given_of(o, row, x, n);
+    if (at0 == 0) g = given_of(o, row, x, n);
+    float m = fmaxf(fmaxf(head, tail), LOWEST);
 #pragma unroll
     for (int j = 0; j < VPL; ++j) m = fmaxf(m, max_score(v[j], T()));
-    Sum a = {warp_max(m), 0.f, 0.f};
 #pragma unroll
-    for (int j = 0; j < VPL; ++j) add_vector<T>(a, v[j], o.c);
-    a.T = warp_sum(a.T);
-    a.u = warp_sum(a.u);
-    if (lane == 0) finish_row(o, row, g, a);
-    if (TOP) {
+    for (int w = LANES / 2; w; w >>= 1) m = fmaxf(m, __shfl_xor_sync(ALL, m, w));
+    const Scale scale(m, o.c);
+    Terms terms;
+#pragma unroll
+    for (int j = 0; j < VPL; ++j) add_vector<T>(terms, v[j], scale);
+    add_pair(terms, head, tail, scale);
+    Sum a = sum_of(terms, m);
+#pragma unroll
+    for (int w = LANES / 2; w; w >>= 1) {
+      a.T += __shfl_xor_sync(ALL, a.T, w);
+      a.u += __shfl_xor_sync(ALL, a.u, w);
+    }
+    a = settle(a, scale);
+    if (at0 == 0 && mine) finish_row(o, row, g, a);
+    if constexpr (TOP) {
+      // a vector is as good as its best entry; short rows have too few vectors and take every entry
+      constexpr bool ENTRIES = VPL <= 2;
+      constexpr int UNITS = (ENTRIES ? VPL * N : VPL) + 2;
       const float lnT = a.T > 0.f ? logf(a.T) : -INFINITY;
-      unsigned pk = 0xffffffffu, pi = 0;  // the one found last
-      for (int r = 0; r < o.k; ++r) {
-        unsigned bk = 0, bi = 0xffffffffu;
+      const unsigned hk = order_key(head), tk = order_key(tail);
+      unsigned unit[UNITS];
 #pragma unroll
-        for (int j = 0; j < VPL; ++j) {
+      for (int j = 0; j < VPL; ++j) {
+        if (ENTRIES) {
           float s[N];
           unpack_scores(v[j], s, T());
 #pragma unroll
-          for (int i = 0; i < N; ++i) {
-            const unsigned key = order_key(__fadd_rn(s[i], 0.f)), id = (unsigned)((j * 32 + lane) * N + i - view.skew);
-            if (key > MASKED_KEY && ahead(pk, pi, key, id) && ahead(key, id, bk, bi)) bk = key, bi = id;
-          }
+          for (int i = 0; i < N; ++i) unit[j * N + i] = order_key(__fadd_rn(s[i], 0.f));
+        } else {
+          unit[j] = order_key(__fadd_rn(max_score(v[j], T()), 0.f));
         }
-        pk = __reduce_max_sync(0xffffffffu, bk);
-        pi = __reduce_min_sync(0xffffffffu, bk == pk ? bi : 0xffffffffu);
-        if (lane == 0) put_best(o, row, a, lnT, r, pk, pi);
-        if (pk == 0) {
-          for (int q = r + 1 + lane; q < o.k; q += 32) put_best(o, row, a, lnT, q, 0u, 0u);
-          break;
+      }
+      unit[UNITS - 2] = hk;
+      unit[UNITS - 1] = tk;
+      unsigned least = 0;
+      for (int bit = 31; bit >= 12; --bit) {
+        const unsigned t = least | (1u << bit);
+        int c = 0;
+#pragma unroll
+        for (int i = 0; i < UNITS; ++i) c += unit[i] >= t;
+        if (__reduce_add_sync(ALL, c) >= o.k) least = t;
+      }
+      least = max(least, MASKED_KEY + 1);
+      __syncwarp();
+      if (lane == 0) found[warp] = 0;
+      __syncwarp();
+      auto offer = [&](unsigned key, unsigned id) {
+        if (key < least) return;
+        const int at = atomicAdd(&found[warp], 1);
+        if (at < SHORT_CAP) list[warp][at] = {key, id};
+      };
+#pragma unroll
+      for (int j = 0; j < VPL; ++j) {
+        if (!ENTRIES && unit[j] < least) continue;
+        float s[N];
+        unpack_scores(v[j], s, T());
+#pragma unroll
+        for (int i = 0; i < N; ++i) offer(order_key(__fadd_rn(s[i], 0.f)), (unsigned)(view.head + (j * 32 + lane) * N + i));
+      }
+      offer(hk, (unsigned)lane);
+      offer(tk, (unsigned)(view.tail_at + lane));
+      __syncwarp();
+      const int many = found[warp];
+      if (many <= SHORT_CAP) {
+        for (int i = lane; i < many; i += 32) {
+          const Best b = list[warp][i];
+          int before = 0;
+          for (int j = 0; j < many; ++j) before += ahead(list[warp][j].key, list[warp][j].id, b.key, b.id);
+          if (before < o.k && mine) put_best(o, row, a, lnT, before, b.key, b.id);
+        }
+        if (lane >= many && lane < o.k && mine) put_best(o, row, a, lnT, lane, 0u, 0u);
+      } else {  // many equal ones: the best that are left, one after another
+        unsigned pk = ALL, pi = 0;
+        for (int r = 0; r < o.k; ++r) {
+          unsigned bk = 0, bi = ALL;
+          auto better = [&](unsigned key, unsigned id) {
+            if (key > MASKED_KEY && ahead(pk, pi, key, id) && ahead(key, id, bk, bi)) bk = key, bi = id;
+          };
+#pragma unroll
+          for (int j = 0; j < VPL; ++j) {
+            float s[N];
+            unpack_scores(v[j], s, T());
+#pragma unroll
+            for (int i = 0; i < N; ++i) better(order_key(__fadd_rn(s[i], 0.f)), (unsigned)(view.head + (j * 32 + lane) * N + i));
+          }
+          better(hk, (unsigned)lane);
+          better(tk, (unsigned)(view.tail_at + lane));
+          pk = __reduce_max_sync(ALL, bk);
+          pi = __reduce_min_sync(ALL, bk == pk ? bi : ALL);
+          if (lane == 0 && mine) put_best(o, row, a, lnT, r, pk, pi);
         }
       }
     }
@@ -495,64 +661,151 @@ struct ScoreGrad {
   const float* dentropy;
   float temperature, c;
 };
+// With t = l c - fl(m c + ln Z log2(e)), which is log2 p but for the rounding r of the constant (the same for all
+// entries), an entry's gradient is 2^t (A t + B), and g / temperature more at the given entry.
 struct RowGrad {
-  float m, lnZ, shift, g, gh, H, inv;
+  Scale scale;
+  float shift, A, B, lnZ, g, gh, H, inv;
   int id;
-  __device__ __forceinline__ float operator()(float l, int i, float c) const {
+  // one entry, any row
+  __device__ __forceinline__ float one(float l, int i) const {
     if (l == -INFINITY) return 0.f;
-    const float t = scaled(l, m, c), lp = fmaf(t, LN2, -lnZ);
-    const float p = exp2_fast(t - shift);
-    float v = -p * fmaf(gh, lp + H, g);
+    const float t = scaled(l, scale.m, scale.c), lp = fmaf(t, LN2, -lnZ);
+    float v = -exp2_fast(fmaf(lnZ, -LOG2E, t)) * fmaf(gh, lp + H, g);
     if (i == id) v += g;
     return v * inv;
   }
 };
-
+__device__ __forceinline__ uint32_t pack_pair(float a, float b, __nv_bfloat16) {
+  const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+__device__ __forceinline__ uint32_t pack_pair(float a, float b, __half) {
+  const __half2 v = __floats2half2_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
 template <class T>
-__global__ void __launch_bounds__(ST) k_score_backward(int64_t rows, int64_t n, const T* __restrict__ logits,
-                                                       int64_t stride, int parts, ScoreGrad o, T* __restrict__ dlogits) {
+__device__ __forceinline__ uint4 grad_vector(uint4 v, const RowGrad& r) {
+  constexpr int P = ScoreVec<T>::N / 2;
+  uint64_t l[P];
+  raised_pairs(v, r.scale.low, l, T());
+  uint32_t w[4];
+#pragma unroll
+  for (int i = 0; i < P; ++i) {
+    const uint64_t t = fma2(l[i], pair(r.scale.c, r.scale.c), pair(r.shift, r.shift));
+    float t0, t1, q0, q1;
+    unpair(t, t0, t1);
+    unpair(fma2(t, pair(r.A, r.A), pair(r.B, r.B)), q0, q1);
+    q0 *= exp2_fast(t0);
+    q1 *= exp2_fast(t1);
+    if constexpr (sizeof(T) == 4) {
+      w[2 * i] = __float_as_uint(q0);
+      w[2 * i + 1] = __float_as_uint(q1);
+    } else {
+      w[i] = pack_pair(q0, q1, T());
+    }
+  }
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// bytes `by` .. by + 15 (a multiple of the type's size) of two vectors
+__device__ __forceinline__ uint4 shifted(uint4 a, uint4 b, int by) {
+  uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+  if (by & 8)
+#pragma unroll
+    for (int i = 0; i < 6; ++i) w[i] = w[i + 2];
+  if (by & 4)
+#pragma unroll
+    for (int i = 0; i < 5; ++i) w[i] = w[i + 1];
+  const int bits = (by & 3) * 8;
+  return make_uint4(__funnelshift_r(w[0], w[1], bits), __funnelshift_r(w[1], w[2], bits), __funnelshift_r(w[2], w[3], bits),
+                    __funnelshift_r(w[3], w[4], bits));
+}
+
+// A warp takes `each` vectors of a row's result (a multiple of 31 SV).  Where the result's rows are aligned otherwise than
+// the scores', a result vector is two neighbouring lanes' shifted together, and 32 lanes give 31.
+template <class T>
+__global__ void __launch_bounds__(ST) k_score_backward(int64_t rows, int64_t n, const T* __restrict__ logits, int64_t stride,
+                                                       int parts, int each, ScoreGrad o, T* __restrict__ dlogits) {
   constexpr int N = ScoreVec<T>::N;
+  const int lane = threadIdx.x & 31;
   const int64_t tasks = rows * parts;
-  for (int64_t task = blockIdx.x; task < tasks; task += gridDim.x) {
+  for (int64_t task = ((int64_t)blockIdx.x * ST + threadIdx.x) >> 5; task < tasks; task += (int64_t)gridDim.x * SW) {
     const int64_t row = task / parts;
     const int which = (int)(task - row * parts);
     const T* x = logits + row * stride;
     T* out = dlogits + row * n;
     const RowView<T> view(x, n);
-    RowGrad r;
-    r.m = o.norm[2 * row];
+    const int skew = (int)((reinterpret_cast<uintptr_t>(out) & 15) / sizeof(T));  // of the result
+    const int vectors = (skew + (int)n + N - 1) / N;
+    // result vector u starts with entry u N - skew: entry `by` of score vector u - back
+    const int delta = view.skew - skew, back = delta < 0 ? 1 : 0, by = delta < 0 ? delta + N : delta;
+    const int wide = by ? 31 : 32;
+    const int first = which * each, last = min(first + each, vectors);
+    uint4 v[SV];
+    auto load = [&](int u0) {
+#pragma unroll
+      for (int j = 0; j < SV; ++j) {
+        const int at = u0 + j * wide + lane - back;
+        if (at >= 0 && at < view.vectors && u0 + j * wide < last)
+          v[j] = view.fetch(at);
+        else
+          v[j] = make_uint4(masked_word<T>(), masked_word<T>(), masked_word<T>(), masked_word<T>());
+      }
+    };
+    load(first);
+    RowGrad r = {Scale(o.norm[2 * row], o.c)};
     r.lnZ = o.norm[2 * row + 1];
-    r.shift = r.lnZ * LOG2E;
     r.id = o.ids ? o.ids[row] : -1;
-    r.g = o.dlogp && r.id >= 0 && r.id < n && clean_score(to_f32(x[r.id])) != -INFINITY ? o.dlogp[row] : 0.f;
+    const float here = r.id >= 0 && r.id < n ? clean_score(to_f32(x[r.id])) : -INFINITY;
+    r.g = o.dlogp && here != -INFINITY ? o.dlogp[row] : 0.f;
     r.gh = o.dentropy ? o.dentropy[row] : 0.f;
     r.H = o.dentropy ? o.entropy[row] : 0.f;
     r.inv = __frcp_rn(o.temperature);
-    const bool same = ((reinterpret_cast<uintptr_t>(x) ^ reinterpret_cast<uintptr_t>(out)) & 15) == 0;
-    T* shifted = out - view.skew;
-    for (int v0 = which * ST * SV; v0 < view.vectors; v0 += parts * ST * SV) {
-      uint4 v[SV];
+    {
+      // shift = -(m c + Z2) rounded, Z2 = ln Z log2(e); t - rest is log2 p, rest = m c + Z2 + shift
+      const float mc = -r.scale.minus_mc, Z2 = r.lnZ * LOG2E, sum = mc + Z2;
+      r.shift = -sum;
+      const float part = sum - mc, lost = (mc - (sum - part)) + (Z2 - part);
+      const float rest = fmaf(r.scale.m, r.scale.c, -mc) + lost + fmaf(r.lnZ, LOG2E, -Z2);
+      const float f = exp2_fast(-rest) * r.inv;
+      r.A = -f * r.gh * LN2;
+      r.B = -f * fmaf(r.gh, fmaf(-rest, LN2, r.H), r.g);
+    }
+    for (int u0 = first; u0 < last; u0 += SV * wide) {
+      if (u0 > first) load(u0);
 #pragma unroll
       for (int j = 0; j < SV; ++j) {
-        const int at = v0 + j * ST + threadIdx.x;
-        if (at < view.vectors) v[j] = view.fetch(at);
-      }
-#pragma unroll
-      for (int j = 0; j < SV; ++j) {
-        const int at = v0 + j * ST + threadIdx.x;
-        if (at >= view.vectors) continue;
-        float l[N];
-        unpack_scores(v[j], l, T());
+        if (u0 + j * wide >= last) break;
         union Piece {
           uint4 raw;
           T t[N];
           __device__ Piece() {}
         } q;
-        const int e = at * N - view.skew;
+        const int at = u0 + j * wide + lane - back, e0 = at * N - view.skew;
+        if (r.scale.plain) {
+          q.raw = grad_vector<T>(v[j], r);
+          if (r.g != 0.f && r.id >= e0 && r.id < e0 + N) {
+            const T mine = from_f32<T>(r.one(here, r.id));
 #pragma unroll
-        for (int i = 0; i < N; ++i) q.t[i] = from_f32<T>(r(l[i], e + i, o.c));
-        if (same && e >= 0 && e + N <= n) {
-          reinterpret_cast<uint4*>(shifted)[at] = q.raw;
+            for (int i = 0; i < N; ++i)
+              if (e0 + i == r.id) q.t[i] = mine;
+          }
+        } else {
+          float l[N];
+          unpack_scores(v[j], l, T());
+#pragma unroll
+          for (int i = 0; i < N; ++i) q.t[i] = from_f32<T>(r.one(l[i], e0 + i));
+        }
+        if (by) {
+          const uint4 next = make_uint4(__shfl_down_sync(0xffffffffu, q.raw.x, 1), __shfl_down_sync(0xffffffffu, q.raw.y, 1),
+                                        __shfl_down_sync(0xffffffffu, q.raw.z, 1), __shfl_down_sync(0xffffffffu, q.raw.w, 1));
+          q.raw = shifted(q.raw, next, by * (int)sizeof(T));
+        }
+        const int u = u0 + j * wide + lane, e = u * N - skew;
+        if (lane >= wide || u >= last) continue;
+        if (e >= 0 && e + N <= n) {
+          *reinterpret_cast<uint4*>(out + e) = q.raw;
         } else {
 #pragma unroll
           for (int i = 0; i < N; ++i)
@@ -581,7 +834,7 @@ Split split_rows(int64_t rows, int64_t n, int32_t type) {
   const int64_t each = (segments + parts - 1) / parts;
   return {(int)((segments + each - 1) / each), (int)each * 32};
 }
-bool short_rows(int64_t n, int32_t type) { return n / (16 / type_bytes(type)) + 2 <= 256; }
+bool short_rows(int64_t n, int32_t type) { return n / (16 / type_bytes(type)) <= 32 * 8; }
 
 erc_status check_scores(int64_t rows, int64_t n, int32_t type, int64_t stride) {
   ERC_REQUIRE(rows >= 0 && rows <= 0x7fffffffLL, "rows must be in [0, 2^31)");
@@ -644,28 +897,37 @@ extern "C" erc_status erc_score_rows(int64_t rows, int64_t n, const void* logits
     using T = decltype(t);
     const T* x = static_cast<const T*>(logits);
     if (brief) {
-      const int64_t vectors = n / ScoreVec<T>::N + 2, blocks = (rows + SW - 1) / SW, most = (int64_t)sm_count() * 64;
-      const unsigned grid = (unsigned)(blocks < most ? blocks : most);
-      auto launch = [&](auto vpl) {
-        constexpr int V = decltype(vpl)::value;
-        (k ? k_score_short<T, V, true> : k_score_short<T, V, false>)<<<grid, ST, 0, s>>>(rows, n, x, stride, o);
+      const int64_t vectors = n / ScoreVec<T>::N, most = (int64_t)sm_count() * 64;
+      auto launch = [&](auto kernel, int lanes) {
+        const int64_t blocks = (rows + ST / lanes - 1) / (ST / lanes);
+        kernel<<<(unsigned)(blocks < most ? blocks : most), ST, 0, s>>>(rows, n, x, stride, o);
       };
-      if (vectors <= 32)
-        launch(ic<1>());
+      if (k && vectors <= 32)
+        launch(k_score_short<T, 32, 1, true>, 32);
+      else if (k && vectors <= 64)
+        launch(k_score_short<T, 32, 2, true>, 32);
+      else if (k && vectors <= 128)
+        launch(k_score_short<T, 32, 4, true>, 32);
+      else if (k)
+        launch(k_score_short<T, 32, 8, true>, 32);
+      else if (vectors <= 16)
+        launch(k_score_short<T, 8, 2, false>, 8);
+      else if (vectors <= 32)
+        launch(k_score_short<T, 8, 4, false>, 8);
       else if (vectors <= 64)
-        launch(ic<2>());
+        launch(k_score_short<T, 8, 8, false>, 8);
       else if (vectors <= 128)
-        launch(ic<4>());
+        launch(k_score_short<T, 16, 8, false>, 16);
       else
-        launch(ic<8>());
+        launch(k_score_short<T, 32, 8, false>, 32);
       count_launches(1);
     } else {
-      const int smem = part_smem<T>(k > 0);
+      const int smem = part_smem(sp.per, k > 0);
       const int64_t tasks = rows * sp.parts;
       const bool together = sp.parts > 1 && sp.parts <= CLUSTER;
       auto kernel = together ? (k ? k_score_part<T, true, true> : k_score_part<T, false, true>)
                              : (k ? k_score_part<T, true, false> : k_score_part<T, false, false>);
-      ERC_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+      ERC_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, part_smem(SEGS * 32, true)));
       // a grid is a whole number of clusters; blocks take further tasks a grid apart, so a cluster's stay together
       const int64_t most = (int64_t)sm_count() * 64 / sp.parts * sp.parts;
       cudaLaunchConfig_t cfg = {};
@@ -708,12 +970,14 @@ extern "C" erc_status erc_score_rows_backward(int64_t rows, int64_t n, const voi
   const ScoreGrad o = {ids, norm, entropy, dlogp, dentropy, temperature, LOG2E / temperature};
   return with_type(type, [&](auto t) {
     using T = decltype(t);
-    const int64_t vectors = n / ScoreVec<T>::N + 2, steps = (vectors + ST * SV - 1) / (ST * SV);
-    const int64_t wanted = ((int64_t)sm_count() * 8 + rows - 1) / rows;
-    const int parts = (int)(steps < wanted ? steps : wanted);
-    const int64_t tasks = rows * parts, most = (int64_t)sm_count() * 64;
-    k_score_backward<T><<<(unsigned)(tasks < most ? tasks : most), ST, 0, as_stream(stream)>>>(
-        rows, n, static_cast<const T*>(logits), stride, parts, o, static_cast<T*>(dlogits));
+    // a warp's share: a few steps of 31 SV vectors, fewer where rows are few
+    const int64_t vectors = n / ScoreVec<T>::N + 2, steps = (vectors + 31 * SV - 1) / (31 * SV);
+    const int64_t warps = (int64_t)sm_count() * 64, wanted = (warps + rows - 1) / rows;
+    const int64_t share = steps <= wanted ? 1 : steps / wanted < 4 ? steps / wanted : 4;
+    const int parts = (int)((steps + share - 1) / share);
+    const int64_t blocks = (rows * parts + SW - 1) / SW, most = (int64_t)sm_count() * 256;
+    k_score_backward<T><<<(unsigned)(blocks < most ? blocks : most), ST, 0, as_stream(stream)>>>(
+        rows, n, static_cast<const T*>(logits), stride, parts, (int)share * 31 * SV, o, static_cast<T*>(dlogits));
     count_launches(1);
     ERC_CUDA(cudaGetLastError());
     return ERC_OK;
