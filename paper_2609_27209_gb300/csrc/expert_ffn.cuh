@@ -50,37 +50,32 @@ __device__ __forceinline__ int64_t slots_used(const int64_t* offsets, int expert
 }
 
 
-// act(a), and act'(a).  Beyond 100 in magnitude the sigmoid and the normal distribution function are 0 or 1 in
-// float32 and the slopes' second terms vanish, so a is held there where a product with 0 could follow;
-// act(-inf) is 0.  The distribution function comes from erfc, which keeps its relative accuracy in the lower tail.
-__device__ __forceinline__ float sigmoid(float a) {  // the hardware's 2^x and 1 / x: a few units in the last place, more with |a|
+// act(a), and act'(a).  The normal distribution function comes from erfc, which keeps its relative accuracy in the lower
+// tail; the sigmoid from the hardware's 2^x and 1 / x (a few units in the last place, more with |a|).  Far from 0 both are
+// 0 or 1 and nothing overflows for finite a.
+__device__ __forceinline__ float sigmoid(float a) {
   float e, q;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(a * -LOG2E));
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(q) : "f"(1.f + e));
   return q;
 }
-__device__ __forceinline__ float held(float a) { return fabsf(a) > 100.f ? copysignf(100.f, a) : a; }
 __device__ __forceinline__ float act_value(int act, float a) {
   if (act == ERC_ACT_RELU) return a > 0.f || a != a ? a : 0.f;
-  const float q = act == ERC_ACT_GELU ? 0.5f * erfcf(a * -0.7071067811865476f) : sigmoid(a);
-  return a == -INFINITY ? 0.f : a * q;
+  return a * (act == ERC_ACT_GELU ? 0.5f * erfcf(a * -0.7071067811865476f) : sigmoid(a));
 }
 __device__ __forceinline__ void act_both(int act, float a, float& value, float& slope) {
   if (act == ERC_ACT_RELU) {
     value = a > 0.f || a != a ? a : 0.f;
     slope = a > 0.f ? 1.f : 0.f;
-    return;
-  }
-  const float c = held(a);
-  float q;
-  if (act == ERC_ACT_GELU) {
-    q = 0.5f * erfcf(a * -0.7071067811865476f);
-    slope = fmaf(c * expf(-0.5f * c * c), 0.3989422804014327f, q);
+  } else if (act == ERC_ACT_GELU) {
+    const float q = 0.5f * erfcf(a * -0.7071067811865476f);
+    value = a * q;
+    slope = fmaf(a * expf(-0.5f * a * a), 0.3989422804014327f, q);
   } else {
-    q = sigmoid(a);
-    slope = q * fmaf(c, 1.f - q, 1.f);
+    const float q = sigmoid(a);
+    value = a * q;
+    slope = fmaf(value, 1.f - q, q);
   }
-  value = a == -INFINITY ? 0.f : a * q;
 }
 
 // rows [first, slots) of `width` elements set to zero by all threads of the grid; `thread` of `threads`

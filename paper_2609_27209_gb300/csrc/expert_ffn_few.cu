@@ -39,9 +39,9 @@ union FewPiece {
   __device__ FewPiece() {}
 };
 
-// lane l gets sum (slot l / 4 mod R, weight row l mod 4) over `depth` elements
+// lane l gets sum (slot l / 4 mod R, weight row l mod 4) over `depth` elements; of slots from `rows` on the last one's
 template <class T, int R>
-__device__ __forceinline__ float few_sums(const T* const* w, const T* x, int64_t ld, int depth, int lane) {
+__device__ __forceinline__ float few_sums(const T* const* w, const T* x, int rows, int depth, int lane) {
   constexpr int N = 16 / sizeof(T);
   float acc[R * WR];
 #pragma unroll
@@ -54,7 +54,7 @@ __device__ __forceinline__ float few_sums(const T* const* w, const T* x, int64_t
 #pragma unroll
     for (int r = 0; r < R; ++r) {
       FewPiece<T> b;
-      b.raw = *reinterpret_cast<const uint4*>(x + r * ld + k);
+      b.raw = *reinterpret_cast<const uint4*>(x + (int64_t)min(r, rows - 1) * depth + k);
 #pragma unroll
       for (int i = 0; i < N; ++i) {
         const float xv = to_f32(b.t[i]);
@@ -104,13 +104,12 @@ __global__ void __launch_bounds__(WT) k_ffn_few(const FfnArgs<T> p, int* __restr
   if (!some) return;
   const T* x = WHICH == FFN_IN ? p.x : p.h;
   for (int64_t r0 = s.lo; r0 < s.hi;) {
-    const int64_t left = s.hi - r0;
-    const int R = left >= 8 ? 8 : left >= 4 ? 4 : left >= 2 ? 2 : 1;
+    const int R = (int)min(s.hi - r0, (int64_t)8);
     const T* from = x + r0 * depth;
-    const float sum = R == 8   ? few_sums<T, 8>(w, from, depth, depth, lane)
-                      : R == 4 ? few_sums<T, 4>(w, from, depth, depth, lane)
-                      : R == 2 ? few_sums<T, 2>(w, from, depth, depth, lane)
-                               : few_sums<T, 1>(w, from, depth, depth, lane);
+    const float sum = R > 4    ? few_sums<T, 8>(w, from, R, depth, lane)
+                      : R > 2  ? few_sums<T, 4>(w, from, R, depth, lane)
+                      : R == 2 ? few_sums<T, 2>(w, from, R, depth, lane)
+                               : few_sums<T, 1>(w, from, R, depth, lane);
     const int64_t row = r0 + lane / WR;
     const int j = lane % WR;
     if constexpr (WHICH == FFN_IN) {

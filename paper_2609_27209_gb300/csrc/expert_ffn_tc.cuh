@@ -176,9 +176,11 @@ struct TcTile {
   int64_t k0, k1;   // slots of a weight gradient
 };
 
-// the experts' slots, and the tiles of 256 slots before each, in shared memory
+// the experts' slots, the slots of a tile (an expert's tiles are of one size, the last perhaps smaller), and the tiles before
+// each expert, in shared memory
 struct TcRanges {
   int lo[ERC_ROUTE_MAX_EXPERTS], hi[ERC_ROUTE_MAX_EXPERTS];
+  short wide[ERC_ROUTE_MAX_EXPERTS];
   int prefix[ERC_ROUTE_MAX_EXPERTS + 1];
 };
 
@@ -207,8 +209,9 @@ struct TcTiles {
         if (of.prefix[mid] <= block) lo = mid; else hi = mid;
       }
       r.expert = lo;
-      r.n0 = of.lo[lo] + (block - of.prefix[lo]) * 256;
-      r.valid = min(of.hi[lo] - (int)r.n0, 256);
+      const int wide = of.wide[lo];
+      r.n0 = of.lo[lo] + (int64_t)(block - of.prefix[lo]) * wide;
+      r.valid = min(of.hi[lo] - (int)r.n0, wide);
       r.n = (r.valid + 31) & ~31;  // a pair's products take multiples of 32
       r.k0 = r.k1 = 0;
       r.blocks = (depth + TC_K - 1) / TC_K;
@@ -228,99 +231,195 @@ struct TcTiles {
   }
 };
 
-// results of TC_COLS columns of a tile, two at a time: a lane and its neighbour swap, so that even lanes hold rows m, m + 1
-// of column c and odd lanes rows m - 1, m of column c + 1
-template <class T>
-__device__ __forceinline__ void pair_up(float a, float b, int lane, float& lo, float& hi) {
-  const float give = lane & 1 ? a : b, keep = lane & 1 ? b : a;
-  const float got = __shfl_xor_sync(0xffffffffu, give, 1);
-  lo = lane & 1 ? got : keep;
-  hi = lane & 1 ? keep : got;
+// A lane holds row m of two columns, rounded and packed; its neighbour holds m + 1 or m - 1.  They swap: even lanes get
+// rows m, m + 1 of the first column, odd lanes rows m - 1, m of the second.
+__device__ __forceinline__ uint32_t pair_up(uint32_t own, uint32_t pick) {
+  const uint32_t other = __shfl_xor_sync(0xffffffffu, own, 1);
+  return __byte_perm(own, other, pick);
 }
+__device__ __forceinline__ uint32_t pair_pick(int lane) { return lane & 1 ? 0x3276u : 0x5410u; }
 
-// DH: the pairs (a, a') and (b, b') of TC_COLS columns that a lane needs, read while the tile before them is at work
-struct PrePairs {
-  uint32_t a[TC_COLS / 2], b[TC_COLS / 2];
-};
-template <class T>
-__device__ __forceinline__ void read_pre(const FfnArgs<T>& p, const TcTile& t, int c0, int m_block, int lane, int quad, PrePairs& r) {
-  const int64_t F = p.inner;
-  const int m = t.m0 + m_block + quad * 32 + lane, odd = lane & 1;
-  const T* pre = p.pre_in + (t.n0 + c0 + odd) * 2 * F + m - odd;
-#pragma unroll
-  for (int j = 0; j < TC_COLS / 2; ++j) {
-    r.a[j] = r.b[j] = 0;
-    if (c0 + 2 * j + odd < t.valid && m < F) {
-      r.a[j] = __ldg(reinterpret_cast<const uint32_t*>(pre + 4 * j * F));
-      r.b[j] = __ldg(reinterpret_cast<const uint32_t*>(pre + (4 * j + 1) * F));
+// two activations, and their slopes, with the packed instructions: what act_both computes, for arguments that are finite
+template <int ACT>
+__device__ __forceinline__ void act_pair(uint64_t a, uint64_t& value, uint64_t& slope) {
+  float a0, a1;
+  unpair(a, a0, a1);
+  if constexpr (ACT == ERC_ACT_SILU) {
+    float t0, t1;
+    unpair(mul2(a, pair(-LOG2E, -LOG2E)), t0, t1);
+    uint64_t e;
+    {
+      float e0, e1;
+      asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e0) : "f"(t0));
+      asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e1) : "f"(t1));
+      e = add2(pair(e0, e1), pair(1.f, 1.f));
     }
+    float d0, d1, q0, q1;
+    unpair(e, d0, d1);
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(q0) : "f"(d0));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(q1) : "f"(d1));
+    const uint64_t q = pair(q0, q1), less = add2(pair(1.f, 1.f), q ^ 0x8000000080000000ull);
+    value = mul2(a, q);
+    slope = fma2(value, less, q);
+  } else {
+    float v0, v1, s0, s1;
+    act_both(ACT, a0, v0, s0);
+    act_both(ACT, a1, v1, s1);
+    value = pair(v0, v1);
+    slope = pair(s0, s1);
   }
 }
 
-template <class T, int WHICH, int ACT>
-__device__ __forceinline__ void write_columns(const FfnArgs<T>& p, const TcTile& t, const float* v, const PrePairs& pre, int c0,
-                                              int m_block, int lane, int quad) {
-  using H = Half2<T>;
+// DH: the pairs (a, a') and (b, b') of TC_COLS columns that a lane needs, read while the columns before them are at work
+struct PrePairs {
+  uint32_t a[TC_COLS / 2], b[TC_COLS / 2];
+};
+// `at`: the lane's byte offset of its first column's row; `two`: bytes of two rows; columns from `live` on are not read
+__device__ __forceinline__ void read_pre(const char* a, const char* b, uint32_t at, uint32_t two, int c, int live, PrePairs& r) {
+#pragma unroll
+  for (int j = 0; j < TC_COLS / 2; ++j) {
+    r.a[j] = r.b[j] = 0;
+    if (c + 2 * j < live) {
+      r.a[j] = __ldg(reinterpret_cast<const uint32_t*>(a + at));
+      r.b[j] = __ldg(reinterpret_cast<const uint32_t*>(b + at));
+    }
+    at += two;
+  }
+}
+
+// asks for the pieces of (a, b) that a warp will read of a tile: 64 bytes of each of its columns' rows
+template <class T>
+__device__ __forceinline__ void ask_for_pre(const FfnArgs<T>& p, const TcTile& t, int m_block, int lane, int quad, int part) {
+  const int64_t F = p.inner;
+  const int m = t.m0 + m_block + quad * 32;
+  if (m >= F) return;
+  const uint32_t bytes = (uint32_t)min((int)F - m, 32) * sizeof(T);
+  for (int c = part * 128 + lane; c < min(t.valid, (part + 1) * 128); c += 32) {
+    const T* at = p.pre_in + (t.n0 + c) * 2 * F + m;
+    asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(at), "r"(bytes) : "memory");
+    asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(at + F), "r"(bytes) : "memory");
+  }
+}
+
+// where a lane's results of a tile go: byte offsets from the tile's first row, which 32 bits hold (256 rows of at most
+// 2^18 bytes), and the first column that is not its to write
+struct TcOut {
+  char *first, *second, *third;  // IN: h, gates, factors; DH: (da), (db), h; else the result
+  const char *pre_a, *pre_b;
+  uint32_t at, at_h, two, two_h;  // offsets of the lane's first column, and of two columns; _h: in rows of inner
+  int live, col;                  // col: the lane's column of each pair (IN: of each four)
+};
+template <class T, int WHICH>
+__device__ __forceinline__ TcOut tile_out(const FfnArgs<T>& p, const TcTile& t, int m_block, int lane, int quad) {
   const int64_t D = p.width, F = p.inner;
+  const int odd = lane & 1;
+  TcOut o;
   if constexpr (WHICH == FFN_IN) {
-    // lane: gates where bit 3 is clear, factors where it is set, of feature f
-    const bool up = lane & 8;
     const int f = (t.m0 + m_block) / 2 + quad * 16 + (lane >> 4) * 8 + (lane & 7);
-    const int odd = lane & 1;
+    o.col = 2 * odd + ((lane >> 3) & 1);
+    o.live = f < F ? t.valid : 0;
+    o.first = reinterpret_cast<char*>(p.h + t.n0 * F + f - odd);
+    o.second = reinterpret_cast<char*>(p.pre + t.n0 * 2 * F + f - odd);
+    o.third = o.second + F * sizeof(T);
+    o.two = 4 * (uint32_t)F * sizeof(T);
+    o.two_h = 2 * (uint32_t)F * sizeof(T);
+  } else {
+    const int m = t.m0 + m_block + quad * 32 + lane;
+    const int64_t ld = WHICH == FFN_DH || WHICH == FFN_DWOUT ? F : D;
+    o.col = odd;
+    o.live = m < ld ? t.valid : 0;
+    if constexpr (WHICH == FFN_DH) {
+      const int64_t row = t.n0 * 2 * F + m - odd;
+      o.first = reinterpret_cast<char*>(p.dpre + row);
+      o.second = o.first + F * sizeof(T);
+      o.third = reinterpret_cast<char*>(p.h + t.n0 * F + m - odd);
+      o.pre_a = reinterpret_cast<const char*>(p.pre_in + row);
+      o.pre_b = o.pre_a + F * sizeof(T);
+      o.two = 4 * (uint32_t)F * sizeof(T);
+      o.two_h = 2 * (uint32_t)F * sizeof(T);
+    } else {
+      T* out = WHICH == FFN_OUT ? p.y : WHICH == FFN_DX ? p.dx : WHICH == FFN_DWIN ? p.dw_in : p.dw_out;
+      if constexpr (WHICH == FFN_DWIN) out += (int64_t)t.expert * 2 * F * D;
+      if constexpr (WHICH == FFN_DWOUT) out += (int64_t)t.expert * D * F;
+      o.first = reinterpret_cast<char*>(out + t.n0 * ld + m - odd);
+      o.two = o.two_h = 2 * (uint32_t)ld * sizeof(T);
+    }
+  }
+  o.at = o.two / 2 * (uint32_t)o.col;
+  o.at_h = o.two_h / 2 * (uint32_t)o.col;
+  return o;
+}
+
+// TC_COLS columns of a tile from column c on
+template <class T, int WHICH, int ACT>
+__device__ __forceinline__ void write_columns(const TcOut& o, const float* v, const PrePairs& pre, int c, int lane, bool keep) {
+  using H = Half2<T>;
+  const uint32_t pick = pair_pick(lane);
+  const int live = o.live - o.col;
+  uint32_t at = o.at + (uint32_t)c / 2 * o.two, at_h = o.at_h + (uint32_t)c / 2 * o.two_h;
+  if constexpr (WHICH == FFN_IN) {
+    // gates where bit 3 of the lane is clear, factors of the same features 8 lanes further: of columns j and j + 1 the
+    // gates' lanes keep the first, the factors' lanes the second
+    const bool up = lane & 8;
 #pragma unroll
     for (int j = 0; j < TC_COLS; j += 4) {
-      float g[2], u[2], h[2];
+      float g[2], u[2];
 #pragma unroll
       for (int q = 0; q < 2; ++q) {
         const float a = v[j + 2 * q], b = v[j + 2 * q + 1];
         const float got = __shfl_xor_sync(0xffffffffu, up ? a : b, 8);
         g[q] = up ? got : a;
         u[q] = up ? b : got;
-        h[q] = act_value(ACT, g[q]) * u[q];
       }
-      // columns j (even lanes) and j + 2 (odd lanes), one further for lanes of factors
-      float h0, h1, g0, g1, u0, u1;
-      pair_up<T>(h[0], h[1], lane, h0, h1);
-      const int col = c0 + j + 2 * odd + (up ? 1 : 0);
-      const bool live = col < t.valid && f < F;
-      const int64_t row = t.n0 + col;
-      const int at = f - odd;
-      if (live) *reinterpret_cast<uint32_t*>(p.h + row * F + at) = H::pack(h0, h1);
-      if (p.pre) {
-        pair_up<T>(g[0], g[1], lane, g0, g1);
-        pair_up<T>(u[0], u[1], lane, u0, u1);
-        if (live) {
-          *reinterpret_cast<uint32_t*>(p.pre + row * 2 * F + at) = H::pack(g0, g1);
-          *reinterpret_cast<uint32_t*>(p.pre + row * 2 * F + F + at) = H::pack(u0, u1);
+      float h0, h1;
+      if constexpr (ACT == ERC_ACT_SILU) {
+        uint64_t value, slope;
+        act_pair<ACT>(pair(g[0], g[1]), value, slope);
+        unpair(mul2(value, pair(u[0], u[1])), h0, h1);
+      } else {
+        h0 = act_value(ACT, g[0]) * u[0];
+        h1 = act_value(ACT, g[1]) * u[1];
+      }
+      const uint32_t h = pair_up(H::pack(h0, h1), pick);
+      const bool mine = c + j < live;
+      if (mine) *reinterpret_cast<uint32_t*>(o.first + at_h) = h;
+      if (keep) {
+        const uint32_t gg = pair_up(H::pack(g[0], g[1]), pick), uu = pair_up(H::pack(u[0], u[1]), pick);
+        if (mine) {
+          *reinterpret_cast<uint32_t*>(o.second + at) = gg;
+          *reinterpret_cast<uint32_t*>(o.third + at) = uu;
         }
       }
+      at += 2 * o.two;
+      at_h += 2 * o.two_h;
     }
   } else {
-    const int m = t.m0 + m_block + quad * 32 + lane, odd = lane & 1, at = m - odd;
-    const int64_t ld = WHICH == FFN_DH || WHICH == FFN_DWOUT ? F : D;
-    T* out = WHICH == FFN_OUT ? p.y : WHICH == FFN_DX ? p.dx : WHICH == FFN_DWIN ? p.dw_in : p.dw_out;
-    if constexpr (WHICH == FFN_DWIN) out += (int64_t)t.expert * 2 * F * D;
-    if constexpr (WHICH == FFN_DWOUT) out += (int64_t)t.expert * D * F;
 #pragma unroll
     for (int j = 0; j < TC_COLS; j += 2) {
-      float lo, hi;
-      pair_up<T>(v[j], v[j + 1], lane, lo, hi);
-      const int col = c0 + j + odd;
-      const bool live = col < t.valid && m < ld;
-      const int64_t row = t.n0 + col;
+      const bool mine = c + j < live;
       if constexpr (WHICH == FFN_DH) {
+        const bool odd = lane & 1;
+        const float got = __shfl_xor_sync(0xffffffffu, odd ? v[j] : v[j + 1], 1);
+        const uint64_t dh = pair(odd ? got : v[j], odd ? v[j + 1] : got);
         const float2 a = H::unpack(pre.a[j / 2]), b = H::unpack(pre.b[j / 2]);
-        float v0, v1, s0, s1;
-        act_both(ACT, a.x, v0, s0);
-        act_both(ACT, a.y, v1, s1);
-        if (live) {
-          *reinterpret_cast<uint32_t*>(p.dpre + row * 2 * F + at) = H::pack(lo * b.x * s0, hi * b.y * s1);
-          *reinterpret_cast<uint32_t*>(p.dpre + row * 2 * F + F + at) = H::pack(lo * v0, hi * v1);
-          *reinterpret_cast<uint32_t*>(p.h + row * F + at) = H::pack(v0 * b.x, v1 * b.y);
+        const uint64_t bb = pair(b.x, b.y);
+        uint64_t value, slope;
+        act_pair<ACT>(pair(a.x, a.y), value, slope);
+        float x0, x1, y0, y1, z0, z1;
+        unpair(mul2(mul2(dh, bb), slope), x0, x1);
+        unpair(mul2(dh, value), y0, y1);
+        unpair(mul2(value, bb), z0, z1);
+        if (mine) {
+          *reinterpret_cast<uint32_t*>(o.first + at) = H::pack(x0, x1);
+          *reinterpret_cast<uint32_t*>(o.second + at) = H::pack(y0, y1);
+          *reinterpret_cast<uint32_t*>(o.third + at_h) = H::pack(z0, z1);
         }
-      } else if (live) {
-        *reinterpret_cast<uint32_t*>(out + row * ld + at) = H::pack(lo, hi);
+      } else {
+        const uint32_t w = pair_up(H::pack(v[j], v[j + 1]), pick);
+        if (mine) *reinterpret_cast<uint32_t*>(o.first + at) = w;
       }
+      at += o.two;
+      at_h += o.two_h;
     }
   }
 }
@@ -376,7 +475,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(TC_THREADS, 1)
     const SlotRange r = slot_range(p.offsets, e, p.slots);
     of.lo[e] = (int)r.lo;
     of.hi[e] = (int)r.hi;
-    of.prefix[e + 1] = (int)((r.hi - r.lo + 255) / 256);
+    const int rows = of.hi[e] - of.lo[e], count = (int)(((unsigned)rows + 255u) / 256u);
+    const int wide = count > 1 ? ((rows + count - 1) / count + 31) & ~31 : 256;
+    of.wide[e] = (short)wide;
+    of.prefix[e + 1] = (int)(((unsigned)rows + wide - 1) / wide);
   }
   if (SLOTS) {
     __syncthreads();
@@ -515,20 +617,28 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(TC_THREADS, 1)
     int a = 0;
     uint32_t a_phase = 0;
     bool ok = true;
+    if constexpr (WHICH == FFN_DH) {
+      if (first < total) ask_for_pre(p, tiles.at(first, of, p.experts), m_block, lane, quad, part);
+    }
     for (int at = first; ok && at < total; at += step) {
       const TcTile t = tiles.at(at, of, p.experts);
       const int c1 = min(t.n, (part + 1) * 128);
+      if constexpr (WHICH == FFN_DH) {
+        if (at + step < total) ask_for_pre(p, tiles.at(at + step, of, p.experts), m_block, lane, quad, part);
+      }
+      const TcOut out = tile_out<T, WHICH>(p, t, m_block, lane, quad);
+      const bool keep = p.pre != nullptr;
       float v[TC_COLS];
       PrePairs pre, next;
       if (t.blocks == 0) {
 #pragma unroll
         for (int i = 0; i < TC_COLS; ++i) v[i] = 0.f;
 #pragma unroll 1
-        for (int c = part * 128; c < c1; c += TC_COLS) write_columns<T, WHICH, ACT>(p, t, v, pre, c, m_block, lane, quad);
+        for (int c = part * 128; c < c1; c += TC_COLS) write_columns<T, WHICH, ACT>(out, v, pre, c, lane, keep);
         continue;
       }
       if constexpr (WHICH == FFN_DH) {
-        if (part * 128 < c1) read_pre(p, t, part * 128, m_block, lane, quad, next);
+        if (part * 128 < c1) read_pre(out.pre_a, out.pre_b, out.at + part * 64 * out.two, out.two, part * 128, out.live - out.col, next);
       }
       ok = __all_sync(0xffffffffu, bar_wait(full(a), a_phase, &failed));
       if (!ok) break;
@@ -539,7 +649,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(TC_THREADS, 1)
         read_tmem(src + c, v);
         if constexpr (WHICH == FFN_DH) {
           pre = next;
-          if (c + TC_COLS < c1) read_pre(p, t, c + TC_COLS, m_block, lane, quad, next);
+          if (c + TC_COLS < c1)
+            read_pre(out.pre_a, out.pre_b, out.at + (uint32_t)(c + TC_COLS) / 2 * out.two, out.two, c + TC_COLS,
+                     out.live - out.col, next);
         }
         read_tmem_done();
         if (c + TC_COLS >= c1) {
@@ -547,7 +659,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(TC_THREADS, 1)
           __syncwarp();
           if (lane == 0) bar_arrive_cluster(peer_address(taken(a), 0));
         }
-        write_columns<T, WHICH, ACT>(p, t, v, pre, c, m_block, lane, quad);
+        write_columns<T, WHICH, ACT>(out, v, pre, c, lane, keep);
       }
       if (part * 128 >= c1) {
         __syncwarp();

@@ -7,7 +7,7 @@
 // exponential and no part scales its sums.  Parts join by d = (m_part - m) c: u <- 2^d (u + d T), T <- 2^d T.
 // t is kept above -1000, where 2^t is 0, so that no product of 0 and infinity appears.
 //
-// The best entries: the k-th largest of the threads' maxima (found bit by bit, 20 bits) bounds the k-th best entry from
+// The best entries: the k-th largest of the threads' maxima, found by halving, bounds the k-th best entry from
 // below, so only the few entries from it on are ranked.  Where many are equal, the k-th best key and the last index
 // that belongs are found the same way among all entries.
 //
@@ -218,8 +218,41 @@ __device__ __forceinline__ bool ahead(unsigned ka, unsigned ia, unsigned kb, uns
 constexpr int CAP = 256;  // entries that are ranked at once
 struct TopScratch {
   Best list[CAP];
+  unsigned unit[ST];  // the threads' largest keys
+  unsigned least;
   int found, sum;
 };
+
+// A key that at least k of a warp's units reach (UNITS a lane; 0: none), close to the largest such one: steps down from the
+// largest unit double until k are reached, six halvings follow.  MASKED_KEY + 1 where there are fewer than k.
+template <int UNITS>
+__device__ __forceinline__ unsigned reached_by(const unsigned* unit, int k) {
+  constexpr unsigned ALL = 0xffffffffu;
+  unsigned top = 0;
+#pragma unroll
+  for (int i = 0; i < UNITS; ++i) top = max(top, unit[i]);
+  top = __reduce_max_sync(ALL, top);
+  if (k == 1 || top <= MASKED_KEY) return max(top, MASKED_KEY + 1);
+  auto enough = [&](unsigned t) {
+    int c = 0;
+#pragma unroll
+    for (int i = 0; i < UNITS; ++i) c += unit[i] >= t;
+    return __reduce_add_sync(ALL, c) >= k;
+  };
+  unsigned lo, hi = top + 1;
+  for (unsigned step = 1u << 18;; step <<= 1) {
+    lo = top - MASKED_KEY - 1 > step && step != 0 ? top - step : MASKED_KEY + 1;
+    if (lo == MASKED_KEY + 1 || enough(lo)) break;
+    hi = lo;
+  }
+  if (lo == MASKED_KEY + 1 && !enough(lo)) return lo;
+#pragma unroll 1
+  for (int i = 0; i < 6; ++i) {
+    const unsigned mid = lo + (hi - lo) / 2;
+    if (enough(mid)) lo = mid; else hi = mid;
+  }
+  return lo;
+}
 
 // the sum of a count over the block's threads
 __device__ __forceinline__ int block_count(TopScratch& s, int mine) {
@@ -239,14 +272,18 @@ __device__ __forceinline__ int block_count(TopScratch& s, int mine) {
 template <class Each, class Put>
 __device__ __forceinline__ void block_top(TopScratch& s, unsigned mine, int k, Each&& each, Put&& put) {
   const int tid = threadIdx.x;
-  if (mine <= MASKED_KEY) mine = 0;
-  unsigned least = 0;
+  s.unit[tid] = mine;
   if (tid == 0) s.found = s.sum = 0;
-  for (int bit = 31; bit >= 12; --bit) {
-    const unsigned t = least | (1u << bit);
-    if (__syncthreads_count(mine >= t) >= k) least = t;
+  __syncthreads();
+  if (tid < 32) {
+    unsigned unit[SW];
+#pragma unroll
+    for (int w = 0; w < SW; ++w) unit[w] = s.unit[w * 32 + tid];
+    const unsigned v = reached_by<SW>(unit, k);
+    if (tid == 0) s.least = v;
   }
-  least = max(least, MASKED_KEY + 1);
+  __syncthreads();
+  const unsigned least = s.least;
   each(least, [&](unsigned key, unsigned id) {
     if (key < least) return;
     const int at = atomicAdd(&s.found, 1);
@@ -493,13 +530,17 @@ __global__ void __launch_bounds__(ST) k_score_join(int64_t rows, int64_t n, cons
       const float lnT = a.T > 0.f ? logf(a.T) : -INFINITY;
       const Best* from = best + row * parts * o.k;
       unsigned mine = 0;
+#pragma unroll 8
       for (int i = threadIdx.x; i < parts * o.k; i += ST) mine = max(mine, from[i].key);
       block_top(
           top, mine, o.k,
           [&](unsigned, auto&& f) {
-            for (int i = threadIdx.x; i < parts * o.k; i += ST) {
-              const Best b = from[i];
-              f(b.key, b.id);
+            for (int i0 = threadIdx.x; i0 < parts * o.k; i0 += 8 * ST) {  // eight reads in flight
+              Best b[8];
+#pragma unroll
+              for (int j = 0; j < 8; ++j) b[j] = i0 + j * ST < parts * o.k ? from[i0 + j * ST] : Best{0u, 0u};
+#pragma unroll
+              for (int j = 0; j < 8; ++j) f(b[j].key, b[j].id);
             }
           },
           [&](int rank, unsigned key, unsigned id) { put_best(o, row, a, lnT, rank, key, id); });
@@ -590,15 +631,7 @@ __global__ void __launch_bounds__(ST, TOP ? 3 : 4) k_score_short(int64_t rows, i
       }
       unit[UNITS - 2] = hk;
       unit[UNITS - 1] = tk;
-      unsigned least = 0;
-      for (int bit = 31; bit >= 12; --bit) {
-        const unsigned t = least | (1u << bit);
-        int c = 0;
-#pragma unroll
-        for (int i = 0; i < UNITS; ++i) c += unit[i] >= t;
-        if (__reduce_add_sync(ALL, c) >= o.k) least = t;
-      }
-      least = max(least, MASKED_KEY + 1);
+      const unsigned least = reached_by<UNITS>(unit, o.k);
       __syncwarp();
       if (lane == 0) found[warp] = 0;
       __syncwarp();
@@ -722,15 +755,15 @@ __device__ __forceinline__ uint4 shifted(uint4 a, uint4 b, int by) {
                     __funnelshift_r(w[3], w[4], bits));
 }
 
-// A warp takes `each` vectors of a row's result (a multiple of 31 SV).  Where the result's rows are aligned otherwise than
+// WARPS warps (a block, or one) take `each` vectors of a row's result, SV steps of 31 WARPS or 32 WARPS at a time.  Where the result's rows are aligned otherwise than
 // the scores', a result vector is two neighbouring lanes' shifted together, and 32 lanes give 31.
-template <class T>
-__global__ void __launch_bounds__(ST) k_score_backward(int64_t rows, int64_t n, const T* __restrict__ logits, int64_t stride,
+template <class T, int WARPS>
+__global__ void __launch_bounds__(ST, 4) k_score_backward(int64_t rows, int64_t n, const T* __restrict__ logits, int64_t stride,
                                                        int parts, int each, ScoreGrad o, T* __restrict__ dlogits) {
   constexpr int N = ScoreVec<T>::N;
-  const int lane = threadIdx.x & 31;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, part_warp = warp % WARPS;
   const int64_t tasks = rows * parts;
-  for (int64_t task = ((int64_t)blockIdx.x * ST + threadIdx.x) >> 5; task < tasks; task += (int64_t)gridDim.x * SW) {
+  for (int64_t task = (int64_t)blockIdx.x * (SW / WARPS) + warp / WARPS; task < tasks; task += (int64_t)gridDim.x * (SW / WARPS)) {
     const int64_t row = task / parts;
     const int which = (int)(task - row * parts);
     const T* x = logits + row * stride;
@@ -740,14 +773,14 @@ __global__ void __launch_bounds__(ST) k_score_backward(int64_t rows, int64_t n, 
     const int vectors = (skew + (int)n + N - 1) / N;
     // result vector u starts with entry u N - skew: entry `by` of score vector u - back
     const int delta = view.skew - skew, back = delta < 0 ? 1 : 0, by = delta < 0 ? delta + N : delta;
-    const int wide = by ? 31 : 32;
+    const int wide = by ? 31 : 32, step = wide * WARPS, off = part_warp * wide;
     const int first = which * each, last = min(first + each, vectors);
     uint4 v[SV];
     auto load = [&](int u0) {
 #pragma unroll
       for (int j = 0; j < SV; ++j) {
-        const int at = u0 + j * wide + lane - back;
-        if (at >= 0 && at < view.vectors && u0 + j * wide < last)
+        const int at = u0 + j * step + off + lane - back;
+        if (at >= 0 && at < view.vectors && u0 + j * step + off < last)
           v[j] = view.fetch(at);
         else
           v[j] = make_uint4(masked_word<T>(), masked_word<T>(), masked_word<T>(), masked_word<T>());
@@ -772,17 +805,17 @@ __global__ void __launch_bounds__(ST) k_score_backward(int64_t rows, int64_t n, 
       r.A = -f * r.gh * LN2;
       r.B = -f * fmaf(r.gh, fmaf(-rest, LN2, r.H), r.g);
     }
-    for (int u0 = first; u0 < last; u0 += SV * wide) {
+    for (int u0 = first; u0 < last; u0 += SV * step) {
       if (u0 > first) load(u0);
 #pragma unroll
       for (int j = 0; j < SV; ++j) {
-        if (u0 + j * wide >= last) break;
+        if (u0 + j * step + off >= last) break;
         union Piece {
           uint4 raw;
           T t[N];
           __device__ Piece() {}
         } q;
-        const int at = u0 + j * wide + lane - back, e0 = at * N - view.skew;
+        const int at = u0 + j * step + off + lane - back, e0 = at * N - view.skew;
         if (r.scale.plain) {
           q.raw = grad_vector<T>(v[j], r);
           if (r.g != 0.f && r.id >= e0 && r.id < e0 + N) {
@@ -802,7 +835,7 @@ __global__ void __launch_bounds__(ST) k_score_backward(int64_t rows, int64_t n, 
                                         __shfl_down_sync(0xffffffffu, q.raw.z, 1), __shfl_down_sync(0xffffffffu, q.raw.w, 1));
           q.raw = shifted(q.raw, next, by * (int)sizeof(T));
         }
-        const int u = u0 + j * wide + lane, e = u * N - skew;
+        const int u = u0 + j * step + off + lane, e = u * N - skew;
         if (lane >= wide || u >= last) continue;
         if (e >= 0 && e + N <= n) {
           *reinterpret_cast<uint4*>(out + e) = q.raw;
@@ -825,7 +858,7 @@ Split split_rows(int64_t rows, int64_t n, int32_t type) {
   const int N = 16 / type_bytes(type);
   const int64_t vectors = n / N + 2;  // a row that starts inside a vector ends in one more
   const int64_t segments = (vectors + 31) / 32, least = (segments + SEGS - 1) / SEGS;
-  const int64_t wanted = ((int64_t)sm_count() * 4 + rows - 1) / rows;
+  const int64_t wanted = rows < (int64_t)sm_count() * 4 ? (int64_t)sm_count() * 4 / rows : 1;
   const int64_t most = (segments + 2 * SW - 1) / (2 * SW);  // two vectors a thread at least
   int64_t parts = wanted < most ? wanted : most;
   if (parts < least) parts = least;
@@ -970,14 +1003,16 @@ extern "C" erc_status erc_score_rows_backward(int64_t rows, int64_t n, const voi
   const ScoreGrad o = {ids, norm, entropy, dlogp, dentropy, temperature, LOG2E / temperature};
   return with_type(type, [&](auto t) {
     using T = decltype(t);
-    // a warp's share: a few steps of 31 SV vectors, fewer where rows are few
-    const int64_t vectors = n / ScoreVec<T>::N + 2, steps = (vectors + 31 * SV - 1) / (31 * SV);
-    const int64_t warps = (int64_t)sm_count() * 64, wanted = (warps + rows - 1) / rows;
-    const int64_t share = steps <= wanted ? 1 : steps / wanted < 4 ? steps / wanted : 4;
-    const int parts = (int)((steps + share - 1) / share);
-    const int64_t blocks = (rows * parts + SW - 1) / SW, most = (int64_t)sm_count() * 256;
-    k_score_backward<T><<<(unsigned)(blocks < most ? blocks : most), ST, 0, as_stream(stream)>>>(
-        rows, n, static_cast<const T*>(logits), stride, parts, (int)share * 31 * SV, o, static_cast<T*>(dlogits));
+    // a block takes a row, or a share of one where rows are few; a warp takes a short one
+    const int64_t vectors = n / ScoreVec<T>::N + 2;
+    const bool wide = vectors > 31 * SV * 2;
+    const int64_t unit = 31 * SV * (wide ? SW : 1), steps = (vectors + unit - 1) / unit;
+    const int64_t wanted = ((int64_t)sm_count() * 8 + rows - 1) / rows;
+    const int64_t parts = steps < wanted ? steps : wanted, each = (steps + parts - 1) / parts * unit;
+    const int64_t tasks = rows * parts, blocks = wide ? tasks : (tasks + SW - 1) / SW, most = (int64_t)sm_count() * 256;
+    (wide ? k_score_backward<T, SW> : k_score_backward<T, 1>)<<<(unsigned)(blocks < most ? blocks : most), ST, 0,
+                                                                as_stream(stream)>>>(
+        rows, n, static_cast<const T*>(logits), stride, (int)parts, (int)each, o, static_cast<T*>(dlogits));
     count_launches(1);
     ERC_CUDA(cudaGetLastError());
     return ERC_OK;
