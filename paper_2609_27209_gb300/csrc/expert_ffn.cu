@@ -1,9 +1,10 @@
 // expert_ffn.cu -- the gated feed-forward block of experts: the C entry points, and its products on
 // the float32 units, for every type and size (the tensor cores take the 16-bit types whose rows are
-// whole 16-byte pieces, expert_ffn_tc.cu).
+// whole 16-byte pieces, expert_ffn_tc.cuh).
 //
-// A product is C(i, j) = sum_k A(i, k) B(j, k) in tiles of 64 x 64 by 16: a thread keeps 4 x 4 sums in
-// registers (two sets where gates and factors share the rows).  Sums run over k in order.
+// A product is C(i, j) = sum_k A(i, k) B(j, k) in tiles of 64 or 128 rows and columns by a depth of 16, twice
+// buffered in shared memory.  A thread keeps 4 x 4 or 8 x 8 sums in registers, as groups of 4 rows and 4 columns 64
+// apart.  In IN the second group of columns holds the factors of the first one's features.  Sums run over k in order.
 #include <initializer_list>
 
 #include "expert_ffn.cuh"
@@ -12,89 +13,131 @@ namespace erc {
 namespace {
 
 constexpr int FT = 256;  // threads
-constexpr int FM = 64;   // tile
+constexpr int FM = 64;   // rows of a group: 16 threads by 4
 constexpr int FK = 16;
 
-// an operand: element (i, k) at p[i * row + k * step]; i in [0, rows), k in [0, depth)
+// an operand: element (i, k) at p[i * row + k * step], i < rows.  One of row and step is 1.  With `twin` rows from FM of a
+// tile on are those of the first FM, `twin` elements further (the factors of IN).
 template <class T>
 struct Operand {
   const T* p;
   int64_t row, step;
   int64_t rows;
+  int64_t twin;
 };
 
-// FM x FK elements from row i0 and depth k0 on; CONTIG: whether k is the contiguous index
-template <class T, bool CONTIG>
-__device__ __forceinline__ void load_tile(const Operand<T>& a, int64_t i0, int64_t k0, int64_t depth, float* r) {
-#pragma unroll
-  for (int j = 0; j < FM * FK / FT; ++j) {
-    const int i = CONTIG ? threadIdx.x / FK + j * (FT / FK) : threadIdx.x % FM;
-    const int k = CONTIG ? threadIdx.x % FK : threadIdx.x / FM + j * (FT / FM);
-    r[j] = i0 + i < a.rows && k0 + k < depth ? to_f32(a.p[(i0 + i) * a.row + (k0 + k) * a.step]) : 0.f;
+// E neighbouring elements of an operand's tile (GROUPS * FM rows by FK) for each thread; CONTIG: k is the contiguous index
+template <int GROUPS, bool CONTIG>
+struct Slice {
+  static constexpr int E = GROUPS * FM * FK / FT;
+  int i, k;
+  __device__ __forceinline__ Slice() {
+    if (CONTIG) {
+      i = threadIdx.x / (FK / E);
+      k = threadIdx.x % (FK / E) * E;
+    } else {
+      k = threadIdx.x / (GROUPS * FM / E);
+      i = threadIdx.x % (GROUPS * FM / E) * E;
+    }
   }
-}
-template <bool CONTIG>
-__device__ __forceinline__ void keep_tile(float (*s)[FM + 4], const float* r) {
+  template <class T>
+  __device__ __forceinline__ void load(const Operand<T>& a, int64_t i0, int64_t k0, int64_t depth, float* r) const {
+    int64_t row = i0 + i, shift = 0;
+    if (a.twin && i >= FM) row -= FM, shift = a.twin;
+    const int64_t at = k0 + k;
+    const T* p = a.p + shift + row * a.row + at * a.step;
+    constexpr int BYTES = E * sizeof(T) < 16 ? E * sizeof(T) : 16, PER = BYTES / sizeof(T);
+    const bool whole = CONTIG ? row < a.rows && at + E <= depth : row + E <= a.rows && at < depth;
+    if (whole && reinterpret_cast<uintptr_t>(p) % BYTES == 0) {
 #pragma unroll
-  for (int j = 0; j < FM * FK / FT; ++j) {
-    const int i = CONTIG ? threadIdx.x / FK + j * (FT / FK) : threadIdx.x % FM;
-    const int k = CONTIG ? threadIdx.x % FK : threadIdx.x / FM + j * (FT / FM);
-    s[k][i] = r[j];
+      for (int j = 0; j < E; j += PER) {
+        union Piece {
+          uint4 q;
+          uint2 d;
+          T t[16 / sizeof(T)];
+          __device__ Piece() {}
+        } v;
+        if constexpr (BYTES == 16)
+          v.q = __ldg(reinterpret_cast<const uint4*>(p + j));
+        else
+          v.d = __ldg(reinterpret_cast<const uint2*>(p + j));
+#pragma unroll
+        for (int q = 0; q < PER; ++q) r[j + q] = to_f32(v.t[q]);
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < E; ++j) {
+        const bool in = CONTIG ? row < a.rows && at + j < depth : row + j < a.rows && at < depth;
+        r[j] = in ? to_f32(p[j]) : 0.f;
+      }
+    }
   }
-}
+  __device__ __forceinline__ void keep(float (*s)[GROUPS * FM + 4], const float* r) const {
+#pragma unroll
+    for (int j = 0; j < E; ++j) {
+      if (CONTIG)
+        s[k + j][i] = r[j];
+      else
+        s[k][i + j] = r[j];
+    }
+  }
+};
 
-template <int NB>
+template <int RG, int CG>
 struct Tiles {
-  float a[FK][FM + 4];
-  float b[NB][FK][FM + 4];
+  float a[2][FK][RG * FM + 4];
+  float b[2][FK][CG * FM + 4];
 };
 
-// the thread's 4 x 4 sums of one or two products that share A: rows i0 + 4 (tid / 16) + ., columns
-// j0 + 4 (tid % 16) + .
-template <class T, bool CA, bool CB, int NB>
-__device__ __forceinline__ void product(Tiles<NB>& s, const Operand<T>& a, const Operand<T>* b, int64_t i0, int64_t j0,
-                                        int64_t depth, float (*acc)[4][4]) {
+// the thread's sums: rows i0 + 64 g + 4 (tid / 16) + ., columns j0 + 64 q + 4 (tid % 16) + .
+template <class T, bool CA, bool CB, int RG, int CG>
+__device__ __forceinline__ void product(Tiles<RG, CG>& s, const Operand<T>& a, const Operand<T>& b, int64_t i0, int64_t j0,
+                                        int64_t depth, float (*acc)[4 * CG]) {
   const int ty = threadIdx.x / 16, tx = threadIdx.x % 16;
+  const Slice<RG, CA> sa;
+  const Slice<CG, CB> sb;
 #pragma unroll
-  for (int q = 0; q < NB; ++q)
+  for (int i = 0; i < 4 * RG; ++i)
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) acc[q][i][j] = 0.f;
-  float ra[FM * FK / FT], rb[NB][FM * FK / FT];
-  load_tile<T, CA>(a, i0, 0, depth, ra);
-#pragma unroll
-  for (int q = 0; q < NB; ++q) load_tile<T, CB>(b[q], j0, 0, depth, rb[q]);
+    for (int j = 0; j < 4 * CG; ++j) acc[i][j] = 0.f;
+  float ra[Slice<RG, CA>::E], rb[Slice<CG, CB>::E];
+  sa.load(a, i0, 0, depth, ra);
+  sb.load(b, j0, 0, depth, rb);
+  sa.keep(s.a[0], ra);
+  sb.keep(s.b[0], rb);
+  __syncthreads();
+  int at = 0;
   for (int64_t k0 = 0; k0 < depth; k0 += FK) {
-    keep_tile<CA>(s.a, ra);
-#pragma unroll
-    for (int q = 0; q < NB; ++q) keep_tile<CB>(s.b[q], rb[q]);
-    __syncthreads();
-    if (k0 + FK < depth) {
-      load_tile<T, CA>(a, i0, k0 + FK, depth, ra);
-#pragma unroll
-      for (int q = 0; q < NB; ++q) load_tile<T, CB>(b[q], j0, k0 + FK, depth, rb[q]);
+    const bool more = k0 + FK < depth;
+    if (more) {
+      sa.load(a, i0, k0 + FK, depth, ra);
+      sb.load(b, j0, k0 + FK, depth, rb);
     }
 #pragma unroll
     for (int k = 0; k < FK; ++k) {
-      const float4 va = *reinterpret_cast<const float4*>(&s.a[k][4 * ty]);
-      const float xa[4] = {va.x, va.y, va.z, va.w};
+      float xa[4 * RG], xb[4 * CG];
 #pragma unroll
-      for (int q = 0; q < NB; ++q) {
-        const float4 vb = *reinterpret_cast<const float4*>(&s.b[q][k][4 * tx]);
-        const float xb[4] = {vb.x, vb.y, vb.z, vb.w};
+      for (int g = 0; g < RG; ++g)
+        *reinterpret_cast<float4*>(xa + 4 * g) = *reinterpret_cast<const float4*>(&s.a[at][k][FM * g + 4 * ty]);
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+      for (int g = 0; g < CG; ++g)
+        *reinterpret_cast<float4*>(xb + 4 * g) = *reinterpret_cast<const float4*>(&s.b[at][k][FM * g + 4 * tx]);
 #pragma unroll
-          for (int j = 0; j < 4; ++j) acc[q][i][j] = fmaf(xa[i], xb[j], acc[q][i][j]);
-      }
+      for (int i = 0; i < 4 * RG; ++i)
+#pragma unroll
+        for (int j = 0; j < 4 * CG; ++j) acc[i][j] = fmaf(xa[i], xb[j], acc[i][j]);
+    }
+    if (more) {
+      sa.keep(s.a[at ^ 1], ra);
+      sb.keep(s.b[at ^ 1], rb);
     }
     __syncthreads();
+    at ^= 1;
   }
 }
 
-// the expert and rows of the t-th tile of 64 slots, experts one after another; false past the last
-__device__ __forceinline__ bool find_tile(const int64_t* offsets, int experts, int64_t slots, int64_t t, int& expert,
+// the expert and rows of the t-th tile of `high` slots, experts one after another; false past the last
+__device__ __forceinline__ bool find_tile(const int64_t* offsets, int experts, int64_t slots, int high, int64_t t, int& expert,
                                           SlotRange& rows) {
   __shared__ int64_t warp_sum[FT / 32];
   __shared__ int found;
@@ -108,7 +151,7 @@ __device__ __forceinline__ bool find_tile(const int64_t* offsets, int experts, i
     count[j] = 0;
     if (e < experts) {
       const SlotRange r = slot_range(offsets, e, slots);
-      count[j] = (r.hi - r.lo + FM - 1) / FM;
+      count[j] = (r.hi - r.lo + high - 1) / high;
     }
     sum += count[j];
   }
@@ -135,15 +178,14 @@ __device__ __forceinline__ bool find_tile(const int64_t* offsets, int experts, i
   if (found < 0) return false;
   expert = found;
   rows = slot_range(offsets, expert, slots);
-  rows.lo += (t - before_found) * FM;
+  rows.lo += (t - before_found) * high;
   return true;
 }
 
-// rows of a tile of slots against all columns of a weight matrix
-template <class T, int WHICH>
+// rows of a tile of slots against columns of a weight matrix
+template <class T, int WHICH, int RG, int CG>
 __global__ void __launch_bounds__(FT) k_ffn_slots(const FfnArgs<T> p) {
-  constexpr int NB = WHICH == FFN_IN ? 2 : 1;
-  __shared__ Tiles<NB> s;
+  __shared__ Tiles<RG, CG> s;
   const int64_t D = p.width, F = p.inner;
   if (WHICH != FFN_DH) {
     const int64_t used = slots_used(p.offsets, p.experts, p.slots);
@@ -155,41 +197,34 @@ __global__ void __launch_bounds__(FT) k_ffn_slots(const FfnArgs<T> p) {
   }
   int e;
   SlotRange r;
-  if (!find_tile(p.offsets, p.experts, p.slots, blockIdx.x, e, r)) return;
-  const int64_t j0 = (int64_t)blockIdx.y * FM;
-  float acc[NB][4][4];
-  Operand<T> b[NB];
+  if (!find_tile(p.offsets, p.experts, p.slots, RG * FM, blockIdx.x, e, r)) return;
+  const int64_t j0 = (int64_t)blockIdx.y * (WHICH == FFN_IN ? FM : CG * FM);
+  float acc[4 * RG][4 * CG];
   if constexpr (WHICH == FFN_IN) {
-    const Operand<T> a = {p.x, D, 1, r.hi};
-    const T* w = p.w_in + e * 2 * F * D;
-    b[0] = {w, D, 1, F};
-    b[1] = {w + F * D, D, 1, F};
-    product<T, true, true, 2>(s, a, b, r.lo, j0, D, acc);
+    const Operand<T> a = {p.x, D, 1, r.hi, 0}, b = {p.w_in + e * 2 * F * D, D, 1, F, F * D};
+    product<T, true, true, RG, CG>(s, a, b, r.lo, j0, D, acc);
   } else if constexpr (WHICH == FFN_OUT) {
-    const Operand<T> a = {p.h, F, 1, r.hi};
-    b[0] = {p.w_out + e * D * F, F, 1, D};
-    product<T, true, true, 1>(s, a, b, r.lo, j0, F, acc);
+    const Operand<T> a = {p.h, F, 1, r.hi, 0}, b = {p.w_out + e * D * F, F, 1, D, 0};
+    product<T, true, true, RG, CG>(s, a, b, r.lo, j0, F, acc);
   } else if constexpr (WHICH == FFN_DH) {
-    const Operand<T> a = {p.dy, D, 1, r.hi};
-    b[0] = {p.w_out + e * D * F, 1, F, F};
-    product<T, true, false, 1>(s, a, b, r.lo, j0, D, acc);
+    const Operand<T> a = {p.dy, D, 1, r.hi, 0}, b = {p.w_out + e * D * F, 1, F, F, 0};
+    product<T, true, false, RG, CG>(s, a, b, r.lo, j0, D, acc);
   } else {
-    const Operand<T> a = {p.dpre, 2 * F, 1, r.hi};
-    b[0] = {p.w_in + e * 2 * F * D, 1, D, D};
-    product<T, true, false, 1>(s, a, b, r.lo, j0, 2 * F, acc);
+    const Operand<T> a = {p.dpre, 2 * F, 1, r.hi, 0}, b = {p.w_in + e * 2 * F * D, 1, D, D, 0};
+    product<T, true, false, RG, CG>(s, a, b, r.lo, j0, 2 * F, acc);
   }
   const int ty = threadIdx.x / 16, tx = threadIdx.x % 16;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int64_t row = r.lo + 4 * ty + i;
-    if (row >= r.hi) break;
+  for (int i = 0; i < 4 * RG; ++i) {
+    const int64_t row = r.lo + FM * (i / 4) + 4 * ty + i % 4;
+    if (row >= r.hi) continue;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int64_t col = j0 + 4 * tx + j;
-      const float v = acc[0][i][j];
+    for (int j = 0; j < (WHICH == FFN_IN ? 4 : 4 * CG); ++j) {
+      const int64_t col = j0 + FM * (j / 4) + 4 * tx + j % 4;
+      const float v = acc[i][j];
       if constexpr (WHICH == FFN_IN) {
         if (col >= F) continue;
-        const float u = acc[NB - 1][i][j];
+        const float u = acc[i][4 + j];
         p.h[row * F + col] = from_f32<T>(act_value(p.act, v) * u);
         if (p.pre) {
           p.pre[row * 2 * F + col] = from_f32<T>(v);
@@ -202,7 +237,7 @@ __global__ void __launch_bounds__(FT) k_ffn_slots(const FfnArgs<T> p) {
         act_both(p.act, g, value, slope);
         p.dpre[row * 2 * F + col] = from_f32<T>(v * u * slope);
         p.dpre[row * 2 * F + F + col] = from_f32<T>(v * value);
-        if (p.h) p.h[row * F + col] = from_f32<T>(value * u);
+        p.h[row * F + col] = from_f32<T>(value * u);
       } else {
         if (col < D) (WHICH == FFN_OUT ? p.y : p.dx)[row * D + col] = from_f32<T>(v);
       }
@@ -211,45 +246,68 @@ __global__ void __launch_bounds__(FT) k_ffn_slots(const FfnArgs<T> p) {
 }
 
 // a tile of an expert's weight gradient: the sum over its slots
-template <class T, int WHICH>
+template <class T, int WHICH, int RG, int CG>
 __global__ void __launch_bounds__(FT) k_ffn_weights(const FfnArgs<T> p) {
-  __shared__ Tiles<1> s;
+  __shared__ Tiles<RG, CG> s;
   const int64_t D = p.width, F = p.inner;
   const int e = blockIdx.z;
   const SlotRange r = slot_range(p.offsets, e, p.slots);
-  const int64_t i0 = (int64_t)blockIdx.y * FM, j0 = (int64_t)blockIdx.x * FM;
+  const int64_t i0 = (int64_t)blockIdx.y * (RG * FM), j0 = (int64_t)blockIdx.x * (CG * FM);
   const int64_t rows = WHICH == FFN_DWIN ? 2 * F : D, cols = WHICH == FFN_DWIN ? D : F;
-  const Operand<T> a = {(WHICH == FFN_DWIN ? p.dpre : p.dy) + r.lo * rows, 1, rows, rows};
-  const Operand<T> b = {(WHICH == FFN_DWIN ? p.x : p.h) + r.lo * cols, 1, cols, cols};
-  float acc[1][4][4];
-  product<T, false, false, 1>(s, a, &b, i0, j0, r.hi - r.lo, acc);
+  const Operand<T> a = {(WHICH == FFN_DWIN ? p.dpre : p.dy) + r.lo * rows, 1, rows, rows, 0};
+  const Operand<T> b = {(WHICH == FFN_DWIN ? p.x : p.h) + r.lo * cols, 1, cols, cols, 0};
+  float acc[4 * RG][4 * CG];
+  product<T, false, false, RG, CG>(s, a, b, i0, j0, r.hi - r.lo, acc);
   T* out = (WHICH == FFN_DWIN ? p.dw_in : p.dw_out) + e * rows * cols;
   const int ty = threadIdx.x / 16, tx = threadIdx.x % 16;
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
+  for (int i = 0; i < 4 * RG; ++i)
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int64_t row = i0 + 4 * ty + i, col = j0 + 4 * tx + j;
-      if (row < rows && col < cols) out[row * cols + col] = from_f32<T>(acc[0][i][j]);
+    for (int j = 0; j < 4 * CG; ++j) {
+      const int64_t row = i0 + FM * (i / 4) + 4 * ty + i % 4, col = j0 + FM * (j / 4) + 4 * tx + j % 4;
+      if (row < rows && col < cols) out[row * cols + col] = from_f32<T>(acc[i][j]);
     }
 }
 
-template <class T>
-erc_status simple_product(FfnProduct which, const FfnArgs<T>& p, cudaStream_t s) {
-  const int64_t tiles = p.slots / FM + (p.experts < p.slots ? p.experts : p.slots);
-  const unsigned wide = (p.width + FM - 1) / FM, deep = (p.inner + FM - 1) / FM, both = (2 * p.inner + FM - 1) / FM;
-  const unsigned rows = (unsigned)(tiles > 0 ? tiles : 1);
-  switch (which) {
-    case FFN_IN: k_ffn_slots<T, FFN_IN><<<dim3(rows, deep), FT, 0, s>>>(p); break;
-    case FFN_OUT: k_ffn_slots<T, FFN_OUT><<<dim3(rows, wide), FT, 0, s>>>(p); break;
-    case FFN_DH: k_ffn_slots<T, FFN_DH><<<dim3(rows, deep), FT, 0, s>>>(p); break;
-    case FFN_DX: k_ffn_slots<T, FFN_DX><<<dim3(rows, wide), FT, 0, s>>>(p); break;
-    case FFN_DWIN: k_ffn_weights<T, FFN_DWIN><<<dim3(wide, both, p.experts), FT, 0, s>>>(p); break;
-    case FFN_DWOUT: k_ffn_weights<T, FFN_DWOUT><<<dim3(deep, wide, p.experts), FT, 0, s>>>(p); break;
+// tiles of 128 rows and columns where they keep every SM busy twice, else of 64: a thread's 64 sums take half the
+// shared-memory reads a product that 16 take, but few large tiles leave SMs idle
+template <class T, int WHICH>
+erc_status simple_launch(const FfnArgs<T>& p, cudaStream_t s) {
+  const int64_t least = p.experts < p.slots ? p.experts : p.slots, busy = (int64_t)sm_count();
+  if constexpr (WHICH <= FFN_DX) {
+    const int64_t cols = WHICH == FFN_IN || WHICH == FFN_DH ? p.inner : p.width;
+    const int64_t wide = WHICH == FFN_IN ? FM : 2 * FM;  // columns of a large tile
+    const int64_t large = (p.slots / (2 * FM) + 1) * ((cols + wide - 1) / wide);
+    if (large >= busy) {
+      const int64_t tiles = p.slots / (2 * FM) + least;
+      k_ffn_slots<T, WHICH, 2, 2><<<dim3((unsigned)tiles, (unsigned)((cols + wide - 1) / wide)), FT, 0, s>>>(p);
+    } else {
+      const int64_t tiles = p.slots / FM + least;
+      k_ffn_slots<T, WHICH, 1, WHICH == FFN_IN ? 2 : 1><<<dim3((unsigned)tiles, (unsigned)((cols + FM - 1) / FM)), FT, 0, s>>>(p);
+    }
+  } else {
+    const int64_t rows = WHICH == FFN_DWIN ? 2 * (int64_t)p.inner : p.width, cols = WHICH == FFN_DWIN ? p.width : p.inner;
+    const int64_t r2 = (rows + 2 * FM - 1) / (2 * FM), c2 = (cols + 2 * FM - 1) / (2 * FM);
+    if (r2 * c2 * p.experts >= busy)
+      k_ffn_weights<T, WHICH, 2, 2><<<dim3((unsigned)c2, (unsigned)r2, p.experts), FT, 0, s>>>(p);
+    else
+      k_ffn_weights<T, WHICH, 1, 1><<<dim3((unsigned)((cols + FM - 1) / FM), (unsigned)((rows + FM - 1) / FM), p.experts), FT, 0,
+                                      s>>>(p);
   }
   count_launches(1);
   ERC_CUDA(cudaGetLastError());
   return ERC_OK;
+}
+template <class T>
+erc_status simple_product(FfnProduct which, const FfnArgs<T>& p, cudaStream_t s) {
+  switch (which) {
+    case FFN_IN: return simple_launch<T, FFN_IN>(p, s);
+    case FFN_OUT: return simple_launch<T, FFN_OUT>(p, s);
+    case FFN_DH: return simple_launch<T, FFN_DH>(p, s);
+    case FFN_DX: return simple_launch<T, FFN_DX>(p, s);
+    case FFN_DWIN: return simple_launch<T, FFN_DWIN>(p, s);
+    default: return simple_launch<T, FFN_DWOUT>(p, s);
+  }
 }
 
 // how a call's products run

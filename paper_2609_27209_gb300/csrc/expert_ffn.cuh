@@ -50,27 +50,54 @@ __device__ __forceinline__ int64_t slots_used(const int64_t* offsets, int expert
 }
 
 
-// act(a), and act'(a).  The normal distribution function comes from erfc, which keeps its relative accuracy in the lower
-// tail; the sigmoid from the hardware's 2^x and 1 / x (a few units in the last place, more with |a|).  Far from 0 both are
-// 0 or 1 and nothing overflows for finite a.
-__device__ __forceinline__ float sigmoid(float a) {
-  float e, q;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(a * -LOG2E));
-  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(q) : "f"(1.f + e));
+// act(a), and act'(a).  The sigmoid takes the hardware's 2^x and 1 / x (a few units in the last place, more with |a|).  The
+// normal distribution function of -|a| is e^(-a^2 / 2) G(1 / (1 + 0.34 |a|)), G a polynomial without a constant term
+// fitted to e^(a^2 / 2) erfc(|a| / sqrt 2) / 2 for the smallest relative error on [0, 14.5] (4e-8; 4e-7 with the rounding
+// of its float32 evaluation), so its lower tail keeps its relative accuracy.  Far from 0 both functions are 0 or 1 and
+// nothing overflows for finite a.
+__device__ __forceinline__ float exp2_hw(float t) {
+  float e;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(t));
+  return e;
+}
+__device__ __forceinline__ float recip_hw(float t) {
+  float q;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(q) : "f"(t));
   return q;
+}
+__device__ __forceinline__ float sigmoid(float a) { return recip_hw(1.f + exp2_hw(a * -LOG2E)); }
+
+constexpr float HALF_LOG2E = 0.72134752f;
+constexpr float TAIL_STEP = 0.34f;
+__host__ __device__ constexpr float tail_coef(int i) {
+  constexpr float c[9] = {0.135621578f, 0.136092216f, 0.115351841f, 0.114712983f, 
+                          -0.0431046113f, 0.199714825f, -0.270868301f, 0.138355583f, -0.0258760974f};
+  return c[i];
+}
+// the normal distribution function of a, and e^(-a^2 / 2)
+__device__ __forceinline__ float normal_below(float a, float& e) {
+  const float t = recip_hw(fmaf(TAIL_STEP, fabsf(a), 1.f));
+  float g = tail_coef(8);
+#pragma unroll
+  for (int i = 7; i >= 0; --i) g = fmaf(g, t, tail_coef(i));
+  e = exp2_hw(a * a * -HALF_LOG2E);
+  const float q = g * t * e;
+  return a < 0.f ? q : 1.f - q;
 }
 __device__ __forceinline__ float act_value(int act, float a) {
   if (act == ERC_ACT_RELU) return a > 0.f || a != a ? a : 0.f;
-  return a * (act == ERC_ACT_GELU ? 0.5f * erfcf(a * -0.7071067811865476f) : sigmoid(a));
+  float e;
+  return a * (act == ERC_ACT_GELU ? normal_below(a, e) : sigmoid(a));
 }
 __device__ __forceinline__ void act_both(int act, float a, float& value, float& slope) {
   if (act == ERC_ACT_RELU) {
     value = a > 0.f || a != a ? a : 0.f;
     slope = a > 0.f ? 1.f : 0.f;
   } else if (act == ERC_ACT_GELU) {
-    const float q = 0.5f * erfcf(a * -0.7071067811865476f);
+    float e;
+    const float q = normal_below(a, e);
     value = a * q;
-    slope = fmaf(a * expf(-0.5f * a * a), 0.3989422804014327f, q);
+    slope = fmaf(a * e, 0.3989422804014327f, q);
   } else {
     const float q = sigmoid(a);
     value = a * q;

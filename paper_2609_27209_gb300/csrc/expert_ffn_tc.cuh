@@ -42,6 +42,7 @@ constexpr int TC_SMEM = TC_STAGES * TC_STAGE + 1024;
 constexpr int TC_THREADS = 384;
 constexpr int TC_EPILOGUE = 8;              // warps that write results
 constexpr int TC_COLS = 16;                 // columns that a lane holds at a time
+constexpr int TC_AHEAD = 3;
 constexpr unsigned TC_WAIT_LIMIT = 1u << 22;
 
 __device__ __forceinline__ uint32_t smem_at(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
@@ -242,31 +243,32 @@ __device__ __forceinline__ uint32_t pair_pick(int lane) { return lane & 1 ? 0x32
 // two activations, and their slopes, with the packed instructions: what act_both computes, for arguments that are finite
 template <int ACT>
 __device__ __forceinline__ void act_pair(uint64_t a, uint64_t& value, uint64_t& slope) {
-  float a0, a1;
+  float a0, a1, x0, x1;
   unpair(a, a0, a1);
+  const uint64_t one = pair(1.f, 1.f), minus = 0x8000000080000000ull;
   if constexpr (ACT == ERC_ACT_SILU) {
-    float t0, t1;
-    unpair(mul2(a, pair(-LOG2E, -LOG2E)), t0, t1);
-    uint64_t e;
-    {
-      float e0, e1;
-      asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e0) : "f"(t0));
-      asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e1) : "f"(t1));
-      e = add2(pair(e0, e1), pair(1.f, 1.f));
-    }
-    float d0, d1, q0, q1;
-    unpair(e, d0, d1);
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(q0) : "f"(d0));
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(q1) : "f"(d1));
-    const uint64_t q = pair(q0, q1), less = add2(pair(1.f, 1.f), q ^ 0x8000000080000000ull);
+    unpair(mul2(a, pair(-LOG2E, -LOG2E)), x0, x1);
+    unpair(add2(pair(exp2_hw(x0), exp2_hw(x1)), one), x0, x1);
+    const uint64_t q = pair(recip_hw(x0), recip_hw(x1));
     value = mul2(a, q);
-    slope = fma2(value, less, q);
+    slope = fma2(value, add2(one, q ^ minus), q);
+  } else if constexpr (ACT == ERC_ACT_GELU) {
+    unpair(fma2(pair(TAIL_STEP, TAIL_STEP), a & 0x7fffffff7fffffffull, one), x0, x1);
+    const uint64_t t = pair(recip_hw(x0), recip_hw(x1));
+    uint64_t g = pair(tail_coef(8), tail_coef(8));
+#pragma unroll
+    for (int i = 7; i >= 0; --i) g = fma2(g, t, pair(tail_coef(i), tail_coef(i)));
+    unpair(mul2(mul2(a, a), pair(-HALF_LOG2E, -HALF_LOG2E)), x0, x1);
+    const uint64_t e = pair(exp2_hw(x0), exp2_hw(x1)), q = mul2(mul2(g, t), e);
+    float q0, q1, r0, r1;
+    unpair(q, q0, q1);
+    unpair(add2(one, q ^ minus), r0, r1);
+    const uint64_t below = pair(a0 < 0.f ? q0 : r0, a1 < 0.f ? q1 : r1);
+    value = mul2(a, below);
+    slope = fma2(mul2(a, e), pair(0.3989422804014327f, 0.3989422804014327f), below);
   } else {
-    float v0, v1, s0, s1;
-    act_both(ACT, a0, v0, s0);
-    act_both(ACT, a1, v1, s1);
-    value = pair(v0, v1);
-    slope = pair(s0, s1);
+    value = pair(a0 > 0.f || a0 != a0 ? a0 : 0.f, a1 > 0.f || a1 != a1 ? a1 : 0.f);
+    slope = pair(a0 > 0.f ? 1.f : 0.f, a1 > 0.f ? 1.f : 0.f);
   }
 }
 
@@ -284,20 +286,6 @@ __device__ __forceinline__ void read_pre(const char* a, const char* b, uint32_t 
       r.b[j] = __ldg(reinterpret_cast<const uint32_t*>(b + at));
     }
     at += two;
-  }
-}
-
-// asks for the pieces of (a, b) that a warp will read of a tile: 64 bytes of each of its columns' rows
-template <class T>
-__device__ __forceinline__ void ask_for_pre(const FfnArgs<T>& p, const TcTile& t, int m_block, int lane, int quad, int part) {
-  const int64_t F = p.inner;
-  const int m = t.m0 + m_block + quad * 32;
-  if (m >= F) return;
-  const uint32_t bytes = (uint32_t)min((int)F - m, 32) * sizeof(T);
-  for (int c = part * 128 + lane; c < min(t.valid, (part + 1) * 128); c += 32) {
-    const T* at = p.pre_in + (t.n0 + c) * 2 * F + m;
-    asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(at), "r"(bytes) : "memory");
-    asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(at + F), "r"(bytes) : "memory");
   }
 }
 
@@ -372,14 +360,9 @@ __device__ __forceinline__ void write_columns(const TcOut& o, const float* v, co
         u[q] = up ? b : got;
       }
       float h0, h1;
-      if constexpr (ACT == ERC_ACT_SILU) {
-        uint64_t value, slope;
-        act_pair<ACT>(pair(g[0], g[1]), value, slope);
-        unpair(mul2(value, pair(u[0], u[1])), h0, h1);
-      } else {
-        h0 = act_value(ACT, g[0]) * u[0];
-        h1 = act_value(ACT, g[1]) * u[1];
-      }
+      uint64_t value, slope;
+      act_pair<ACT>(pair(g[0], g[1]), value, slope);
+      unpair(mul2(value, pair(u[0], u[1])), h0, h1);
       const uint32_t h = pair_up(H::pack(h0, h1), pick);
       const bool mine = c + j < live;
       if (mine) *reinterpret_cast<uint32_t*>(o.first + at_h) = h;
@@ -617,19 +600,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(TC_THREADS, 1)
     int a = 0;
     uint32_t a_phase = 0;
     bool ok = true;
-    if constexpr (WHICH == FFN_DH) {
-      if (first < total) ask_for_pre(p, tiles.at(first, of, p.experts), m_block, lane, quad, part);
-    }
     for (int at = first; ok && at < total; at += step) {
       const TcTile t = tiles.at(at, of, p.experts);
       const int c1 = min(t.n, (part + 1) * 128);
-      if constexpr (WHICH == FFN_DH) {
-        if (at + step < total) ask_for_pre(p, tiles.at(at + step, of, p.experts), m_block, lane, quad, part);
-      }
       const TcOut out = tile_out<T, WHICH>(p, t, m_block, lane, quad);
       const bool keep = p.pre != nullptr;
       float v[TC_COLS];
-      PrePairs pre, next;
+      PrePairs pre, next[TC_AHEAD];  // DH: read TC_AHEAD steps before their use
       if (t.blocks == 0) {
 #pragma unroll
         for (int i = 0; i < TC_COLS; ++i) v[i] = 0.f;
@@ -637,8 +614,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(TC_THREADS, 1)
         for (int c = part * 128; c < c1; c += TC_COLS) write_columns<T, WHICH, ACT>(out, v, pre, c, lane, keep);
         continue;
       }
+      auto read_ahead = [&](int c, PrePairs& r) {
+        read_pre(out.pre_a, out.pre_b, out.at + (uint32_t)c / 2 * out.two, out.two, c, c < c1 ? out.live - out.col : 0, r);
+      };
       if constexpr (WHICH == FFN_DH) {
-        if (part * 128 < c1) read_pre(out.pre_a, out.pre_b, out.at + part * 64 * out.two, out.two, part * 128, out.live - out.col, next);
+#pragma unroll
+        for (int i = 0; i < TC_AHEAD; ++i) read_ahead(part * 128 + i * TC_COLS, next[i]);
       }
       ok = __all_sync(0xffffffffu, bar_wait(full(a), a_phase, &failed));
       if (!ok) break;
@@ -648,10 +629,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(TC_THREADS, 1)
       for (int c = part * 128; c < c1; c += TC_COLS) {
         read_tmem(src + c, v);
         if constexpr (WHICH == FFN_DH) {
-          pre = next;
-          if (c + TC_COLS < c1)
-            read_pre(out.pre_a, out.pre_b, out.at + (uint32_t)(c + TC_COLS) / 2 * out.two, out.two, c + TC_COLS,
-                     out.live - out.col, next);
+          pre = next[0];
+#pragma unroll
+          for (int i = 0; i + 1 < TC_AHEAD; ++i) next[i] = next[i + 1];
+          read_ahead(c + TC_AHEAD * TC_COLS, next[TC_AHEAD - 1]);
         }
         read_tmem_done();
         if (c + TC_COLS >= c1) {
