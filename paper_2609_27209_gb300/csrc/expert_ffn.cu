@@ -250,8 +250,8 @@ template <class T, int WHICH, int RG, int CG>
 __global__ void __launch_bounds__(FT) k_ffn_weights(const FfnArgs<T> p) {
   __shared__ Tiles<RG, CG> s;
   const int64_t D = p.width, F = p.inner;
-  const int e = blockIdx.z;
-  const SlotRange r = slot_range(p.offsets, e, p.slots);
+  const int e = blockIdx.z / p.splits, part = blockIdx.z - e * p.splits;
+  const SlotRange r = split_range(slot_range(p.offsets, e, p.slots), part, p.splits);
   const int64_t i0 = (int64_t)blockIdx.y * (RG * FM), j0 = (int64_t)blockIdx.x * (CG * FM);
   const int64_t rows = WHICH == FFN_DWIN ? 2 * F : D, cols = WHICH == FFN_DWIN ? D : F;
   const Operand<T> a = {(WHICH == FFN_DWIN ? p.dpre : p.dy) + r.lo * rows, 1, rows, rows, 0};
@@ -259,13 +259,19 @@ __global__ void __launch_bounds__(FT) k_ffn_weights(const FfnArgs<T> p) {
   float acc[4 * RG][4 * CG];
   product<T, false, false, RG, CG>(s, a, b, i0, j0, r.hi - r.lo, acc);
   T* out = (WHICH == FFN_DWIN ? p.dw_in : p.dw_out) + e * rows * cols;
+  float* sums = p.splits > 1 ? p.partial + ((int64_t)part * p.experts + e) * rows * cols : nullptr;
   const int ty = threadIdx.x / 16, tx = threadIdx.x % 16;
 #pragma unroll
   for (int i = 0; i < 4 * RG; ++i)
 #pragma unroll
     for (int j = 0; j < 4 * CG; ++j) {
       const int64_t row = i0 + FM * (i / 4) + 4 * ty + i % 4, col = j0 + FM * (j / 4) + 4 * tx + j % 4;
-      if (row < rows && col < cols) out[row * cols + col] = from_f32<T>(acc[i][j]);
+      if (row < rows && col < cols) {
+        if (sums)
+          sums[row * cols + col] = acc[i][j];
+        else
+          out[row * cols + col] = from_f32<T>(acc[i][j]);
+      }
     }
 }
 
@@ -288,11 +294,11 @@ erc_status simple_launch(const FfnArgs<T>& p, cudaStream_t s) {
   } else {
     const int64_t rows = WHICH == FFN_DWIN ? 2 * (int64_t)p.inner : p.width, cols = WHICH == FFN_DWIN ? p.width : p.inner;
     const int64_t r2 = (rows + 2 * FM - 1) / (2 * FM), c2 = (cols + 2 * FM - 1) / (2 * FM);
+    const unsigned deep = (unsigned)p.experts * p.splits;
     if (r2 * c2 * p.experts >= busy)
-      k_ffn_weights<T, WHICH, 2, 2><<<dim3((unsigned)c2, (unsigned)r2, p.experts), FT, 0, s>>>(p);
+      k_ffn_weights<T, WHICH, 2, 2><<<dim3((unsigned)c2, (unsigned)r2, deep), FT, 0, s>>>(p);
     else
-      k_ffn_weights<T, WHICH, 1, 1><<<dim3((unsigned)((cols + FM - 1) / FM), (unsigned)((rows + FM - 1) / FM), p.experts), FT, 0,
-                                      s>>>(p);
+      k_ffn_weights<T, WHICH, 1, 1><<<dim3((unsigned)((cols + FM - 1) / FM), (unsigned)((rows + FM - 1) / FM), deep), FT, 0, s>>>(p);
   }
   count_launches(1);
   ERC_CUDA(cudaGetLastError());
@@ -310,29 +316,158 @@ erc_status simple_product(FfnProduct which, const FfnArgs<T>& p, cudaStream_t s)
   }
 }
 
-// how a call's products run
+// ---- how a call's products run
 enum FfnWay { FFN_SIMPLE, FFN_FEW, FFN_TENSOR };
+
 // Few slots read the weights without the tensor cores.  IN + OUT, both ways (us; bfloat16): one expert of 2048 x 2048, 8
 // slots 23 / 39, 16 slots 43 / 39; 8 experts of 512 x 1024, 16 slots 18 / 27, 32 slots 19 / 27; 64 experts of
 // 1024 x 512, 32 slots 42 / 45.
 bool few_slots(const erc_ffn_shape* f) { return f->slots <= 8 || (f->slots <= 32 && f->slots <= 4 * f->experts); }
-
+bool whole_pieces(const erc_ffn_shape* f) {
+  const int piece = 16 / type_bytes(f->type);
+  return f->width % piece == 0 && f->inner % piece == 0;
+}
+// Rows that are not whole pieces are copied into rows that are, for the tensor cores' sake, where that pays: the copies
+// cost some 20 us and three times the weights' bytes.
+bool worth_padding(const erc_ffn_shape* f) {
+  return f->type != ERC_F32 && !whole_pieces(f) && f->slots >= 32 * (int64_t)f->experts &&
+         (double)f->slots * f->width * f->inner >= 1e8;
+}
 // `all`: the bits of every pointer
 FfnWay ffn_way(const erc_ffn_shape* f, uintptr_t all, bool forward) {
-  const int piece = 16 / type_bytes(f->type);
-  if (all % 16 != 0 || f->width % piece != 0 || f->inner % piece != 0) return FFN_SIMPLE;
+  if (worth_padding(f)) return FFN_TENSOR;
+  if (all % 16 != 0 || !whole_pieces(f)) return FFN_SIMPLE;
   if (forward && few_slots(f)) return FFN_FEW;
   return f->type == ERC_F32 ? FFN_SIMPLE : FFN_TENSOR;
+}
+
+// Parts of an expert's slots in a weight gradient of rows x cols: few tiles would leave most SMs idle over a long sum.
+int weight_splits(const erc_ffn_shape* f, int64_t rows, int64_t cols, bool tensor) {
+  const int64_t side = tensor ? 256 : FM, most = tensor ? sm_count() / 2 : 2 * sm_count();
+  const int64_t tiles = f->experts * ((rows + side - 1) / side) * ((cols + side - 1) / side);
+  int64_t n = most / (tiles > 0 ? tiles : 1);
+  const int64_t deep = f->slots / ((int64_t)f->experts * 512);
+  if (n > deep) n = deep;
+  return (int)(n < 1 ? 1 : n > 64 ? 64 : n);
+}
+
+// the splits' sums, added in order and rounded once
+template <class T>
+__global__ void __launch_bounds__(FT) k_ffn_sum(const float* __restrict__ partial, int splits, int64_t count, T* __restrict__ out) {
+  for (int64_t i = (int64_t)blockIdx.x * FT + threadIdx.x; i < count; i += (int64_t)gridDim.x * FT) {
+    float s = 0.f;
+#pragma unroll 8
+    for (int k = 0; k < splits; ++k) s += __ldcg(partial + k * count + i);
+    out[i] = from_f32<T>(s);
+  }
+}
+
+// dst [groups][rows_to][cols_to] from src [groups][rows_from][cols_from], zeros where src has none; several at once
+template <class T>
+struct Recast {
+  const T* src;
+  T* dst;
+  int64_t groups;
+  int rows_from, cols_from, rows_to, cols_to;
+};
+template <class T>
+struct Recasts {
+  Recast<T> job[5];
+  int jobs = 0;
+  void add(const T* src, T* dst, int64_t groups, int rows_from, int cols_from, int rows_to, int cols_to) {
+    if (src && dst) job[jobs++] = {src, dst, groups, rows_from, cols_from, rows_to, cols_to};
+  }
+};
+template <class T>
+__global__ void __launch_bounds__(FT) k_ffn_recast(const Recasts<T> all) {
+  const Recast<T> j = all.job[blockIdx.y];
+  const int64_t rows = j.groups * j.rows_to;
+  const int lane = threadIdx.x & 31;
+  for (int64_t r = ((int64_t)blockIdx.x * FT + threadIdx.x) >> 5; r < rows; r += (int64_t)gridDim.x * (FT / 32)) {
+    const int64_t g = r / j.rows_to;
+    const int i = (int)(r - g * j.rows_to);
+    const T* from = j.src + (g * j.rows_from + i) * j.cols_from;
+    const int some = i < j.rows_from ? j.cols_from : 0;
+#pragma unroll 4
+    for (int c = lane; c < j.cols_to; c += 32) j.dst[r * j.cols_to + c] = c < some ? from[c] : from_f32<T>(0.f);
+  }
+}
+template <class T>
+erc_status recast(const Recasts<T>& all, cudaStream_t s) {
+  if (all.jobs == 0) return ERC_OK;
+  k_ffn_recast<T><<<dim3(sm_count() * 8, all.jobs), FT, 0, s>>>(all);
+  count_launches(1);
+  ERC_CUDA(cudaGetLastError());
+  return ERC_OK;
 }
 
 template <class T>
 erc_status ffn_product(FfnWay way, FfnProduct which, const FfnArgs<T>& p, int* status, cudaStream_t s) {
   if (way == FFN_FEW) return ffn_few_product<T>(which, p, status, s);
-  if constexpr (sizeof(T) == 2) {
-    if (way == FFN_TENSOR) return ffn_tc_product<T>(which, p, status, s);
+  if (way == FFN_TENSOR) {
+    if constexpr (sizeof(T) == 2) ERC_TRY(ffn_tc_product<T>(which, p, status, s));
+  } else {
+    if (which == FFN_IN || which == FFN_DH) ERC_CUDA(cudaMemsetAsync(status, 0, sizeof(int), s));
+    ERC_TRY(simple_product(which, p, s));
   }
-  if (which == FFN_IN || which == FFN_DH) ERC_CUDA(cudaMemsetAsync(status, 0, sizeof(int), s));
-  return simple_product(which, p, s);
+  if (which >= FFN_DWIN && p.splits > 1) {
+    const int64_t count = (int64_t)p.experts * p.width * p.inner * (which == FFN_DWIN ? 2 : 1);
+    const int64_t blocks = (count + FT - 1) / FT, most = (int64_t)sm_count() * 8;
+    k_ffn_sum<T><<<(unsigned)(blocks < most ? blocks : most), FT, 0, s>>>(p.partial, p.splits, count,
+                                                                         which == FFN_DWIN ? p.dw_in : p.dw_out);
+    count_launches(1);
+    ERC_CUDA(cudaGetLastError());
+  }
+  return ERC_OK;
+}
+
+// what a call keeps in its workspace
+template <class T>
+struct FfnSpace {
+  int* status;
+  T *h, *dpre;
+  float* partial;
+  T *x, *dy, *pre, *w_in, *w_out, *y, *dx, *dw_in, *dw_out;  // rows of whole pieces
+};
+template <class T>
+void plan_space(Arena& a, FfnSpace<T>& w, const erc_ffn_shape* f, bool backward) {
+  const bool pad = worth_padding(f);
+  const size_t S = f->slots, E = f->experts, D = pad ? (f->width + 7) / 8 * 8 : f->width, F = pad ? (f->inner + 7) / 8 * 8 : f->inner;
+  w = {};
+  w.status = a.take<int>(1);
+  w.h = a.take<T>(S * F);
+  if (backward) {
+    w.dpre = a.take<T>(S * 2 * F);
+    size_t sums = 0;
+    for (int tensor = 0; tensor < 2; ++tensor) {
+      const size_t in = weight_splits(f, 2 * F, D, tensor), out = weight_splits(f, D, F, tensor);
+      if (in > 1 && sums < in * E * 2 * F * D) sums = in * E * 2 * F * D;
+      if (out > 1 && sums < out * E * F * D) sums = out * E * F * D;
+    }
+    w.partial = a.take<float>(sums);
+  }
+  if (!pad) return;
+  w.x = a.take<T>(S * D);
+  w.pre = a.take<T>(S * 2 * F);
+  w.w_in = a.take<T>(E * 2 * F * D);
+  w.w_out = a.take<T>(E * D * F);
+  w.y = a.take<T>(S * D);
+  if (!backward) return;
+  w.dy = w.y;
+  w.dx = a.take<T>(S * D);
+  w.dw_in = a.take<T>(E * 2 * F * D);
+  w.dw_out = a.take<T>(E * D * F);
+}
+size_t space_bytes(const erc_ffn_shape* f, bool backward) {
+  Arena a(nullptr);
+  if (f->type == ERC_F32) {
+    FfnSpace<float> w;
+    plan_space(a, w, f, backward);
+  } else {
+    FfnSpace<__half> w;
+    plan_space(a, w, f, backward);
+  }
+  return a.used + 256;
 }
 
 erc_status check_shape(const erc_ffn_shape* f) {
@@ -364,10 +499,7 @@ void* align_ws(void* ws) {
 
 using namespace erc;
 
-extern "C" size_t erc_expert_ffn_workspace_size(const erc_ffn_shape* f) {
-  if (!good_shape(f)) return 0;
-  return (size_t)f->slots * f->inner * type_bytes(f->type) + 1024;
-}
+extern "C" size_t erc_expert_ffn_workspace_size(const erc_ffn_shape* f) { return good_shape(f) ? space_bytes(f, false) : 0; }
 
 extern "C" erc_status erc_expert_ffn(const erc_ffn_shape* f, const void* xs, const int64_t* offsets, const void* w_in,
                                      const void* w_out, void* y, void* pre, void* ws, size_t ws_bytes,
@@ -378,27 +510,49 @@ extern "C" erc_status erc_expert_ffn(const erc_ffn_shape* f, const void* xs, con
   ERC_REQUIRE(xs && offsets && w_in && w_out && y, "null pointer");
   const uintptr_t all = any_bits({xs, w_in, w_out, y, pre});
   ERC_REQUIRE(all % type_bytes(f->type) == 0 && reinterpret_cast<uintptr_t>(offsets) % 8 == 0, "misaligned array");
-  if (!ws || ws_bytes < erc_expert_ffn_workspace_size(f)) return set_error(ERC_ERR_CAPACITY, "workspace too small");
+  if (!ws || ws_bytes < space_bytes(f, false)) return set_error(ERC_ERR_CAPACITY, "workspace too small");
   const FfnWay way = ffn_way(f, all, true);
+  const cudaStream_t s = as_stream(stream);
   return with_type(f->type, [&](auto t) {
     using T = decltype(t);
     Arena ar(align_ws(ws));
-    int* status = ar.take<int>(1);
+    FfnSpace<T> w;
+    plan_space(ar, w, f, false);
     FfnArgs<T> p = {f->slots, f->experts, f->width, f->inner, f->act, offsets};
     p.x = static_cast<const T*>(xs);
     p.w_in = static_cast<const T*>(w_in);
     p.w_out = static_cast<const T*>(w_out);
-    p.h = ar.take<T>((size_t)f->slots * f->inner);
+    p.h = w.h;
     p.pre = static_cast<T*>(pre);
     p.y = static_cast<T*>(y);
-    ERC_TRY(ffn_product(way, FFN_IN, p, status, as_stream(stream)));
-    return ffn_product(way, FFN_OUT, p, status, as_stream(stream));
+    p.splits = 1;
+    const int D = p.width, F = p.inner, E = p.experts;
+    if (w.x) {
+      p.width = (D + 7) / 8 * 8;
+      p.inner = (F + 7) / 8 * 8;
+      Recasts<T> to;
+      to.add(p.x, w.x, 1, (int)p.slots, D, (int)p.slots, p.width);
+      to.add(p.w_in, w.w_in, 2 * E, F, D, p.inner, p.width);
+      to.add(p.w_out, w.w_out, E, D, F, p.width, p.inner);
+      ERC_TRY(recast(to, s));
+      p.x = w.x;
+      p.w_in = w.w_in;
+      p.w_out = w.w_out;
+      p.pre = pre ? w.pre : nullptr;
+      p.y = w.y;
+    }
+    ERC_TRY(ffn_product(way, FFN_IN, p, w.status, s));
+    ERC_TRY(ffn_product(way, FFN_OUT, p, w.status, s));
+    if (!w.x) return ERC_OK;
+    Recasts<T> back;
+    back.add(w.y, static_cast<T*>(y), 1, (int)p.slots, p.width, (int)p.slots, D);
+    back.add(w.pre, static_cast<T*>(pre), 2 * p.slots, 1, p.inner, 1, F);
+    return recast(back, s);
   });
 }
 
 extern "C" size_t erc_expert_ffn_backward_workspace_size(const erc_ffn_shape* f) {
-  if (!good_shape(f)) return 0;
-  return (size_t)f->slots * f->inner * 3 * type_bytes(f->type) + 1536;
+  return good_shape(f) ? space_bytes(f, true) : 0;
 }
 
 extern "C" erc_status erc_expert_ffn_backward(const erc_ffn_shape* f, const void* dy, const void* xs, const void* pre,
@@ -414,31 +568,60 @@ extern "C" erc_status erc_expert_ffn_backward(const erc_ffn_shape* f, const void
     if (dw_out) ERC_CUDA(cudaMemsetAsync(dw_out, 0, bytes, s));
     return ERC_OK;
   }
-  ERC_REQUIRE(dy && pre && offsets && (w_out || !(dxs || dw_in)) && (xs || !dw_in) && (w_in || !dxs), "null pointer");
+  ERC_REQUIRE(dy && pre && offsets && w_out && (xs || !dw_in) && (w_in || !dxs), "null pointer");
   const uintptr_t all = any_bits({dy, xs, pre, w_in, w_out, dxs, dw_in, dw_out});
   ERC_REQUIRE(all % type_bytes(f->type) == 0 && reinterpret_cast<uintptr_t>(offsets) % 8 == 0, "misaligned array");
-  if (!ws || ws_bytes < erc_expert_ffn_backward_workspace_size(f))
-    return set_error(ERC_ERR_CAPACITY, "workspace too small");
+  if (!ws || ws_bytes < space_bytes(f, true)) return set_error(ERC_ERR_CAPACITY, "workspace too small");
   const FfnWay way = ffn_way(f, all, false);
   return with_type(f->type, [&](auto t) {
     using T = decltype(t);
     Arena ar(align_ws(ws));
-    int* status = ar.take<int>(1);
+    FfnSpace<T> w;
+    plan_space(ar, w, f, true);
     FfnArgs<T> p = {f->slots, f->experts, f->width, f->inner, f->act, offsets};
     p.x = static_cast<const T*>(xs);
     p.w_in = static_cast<const T*>(w_in);
     p.w_out = static_cast<const T*>(w_out);
     p.dy = static_cast<const T*>(dy);
     p.pre_in = static_cast<const T*>(pre);
-    p.dpre = ar.take<T>((size_t)f->slots * f->inner * 2);
-    p.h = ar.take<T>((size_t)f->slots * f->inner);
+    p.dpre = w.dpre;
+    p.h = w.h;
     p.dx = static_cast<T*>(dxs);
     p.dw_in = static_cast<T*>(dw_in);
     p.dw_out = static_cast<T*>(dw_out);
-    ERC_TRY(ffn_product(way, FFN_DH, p, status, s));
-    if (p.dx) ERC_TRY(ffn_product(way, FFN_DX, p, status, s));
-    if (p.dw_in) ERC_TRY(ffn_product(way, FFN_DWIN, p, status, s));
-    if (p.dw_out) ERC_TRY(ffn_product(way, FFN_DWOUT, p, status, s));
-    return ERC_OK;
+    p.partial = w.partial;
+    p.splits = 1;
+    const int D = p.width, F = p.inner, E = p.experts;
+    if (w.x) {
+      p.width = (D + 7) / 8 * 8;
+      p.inner = (F + 7) / 8 * 8;
+      Recasts<T> to;
+      to.add(p.dy, w.dy, 1, (int)p.slots, D, (int)p.slots, p.width);
+      to.add(p.pre_in, w.pre, 2 * p.slots, 1, F, 1, p.inner);
+      to.add(p.w_out, w.w_out, E, D, F, p.width, p.inner);
+      if (dw_in) to.add(p.x, w.x, 1, (int)p.slots, D, (int)p.slots, p.width);
+      if (dxs) to.add(p.w_in, w.w_in, 2 * E, F, D, p.inner, p.width);
+      ERC_TRY(recast(to, s));
+      p.dy = w.dy;
+      p.pre_in = w.pre;
+      p.x = w.x;
+      p.w_in = w.w_in;
+      p.w_out = w.w_out;
+      p.dx = dxs ? w.dx : nullptr;
+      p.dw_in = dw_in ? w.dw_in : nullptr;
+      p.dw_out = dw_out ? w.dw_out : nullptr;
+    }
+    ERC_TRY(ffn_product(way, FFN_DH, p, w.status, s));
+    if (p.dx) ERC_TRY(ffn_product(way, FFN_DX, p, w.status, s));
+    p.splits = weight_splits(f, 2 * p.inner, p.width, way == FFN_TENSOR);
+    if (p.dw_in) ERC_TRY(ffn_product(way, FFN_DWIN, p, w.status, s));
+    p.splits = weight_splits(f, p.width, p.inner, way == FFN_TENSOR);
+    if (p.dw_out) ERC_TRY(ffn_product(way, FFN_DWOUT, p, w.status, s));
+    if (!w.x) return ERC_OK;
+    Recasts<T> back;
+    back.add(w.dx, static_cast<T*>(dxs), 1, (int)p.slots, p.width, (int)p.slots, D);
+    back.add(w.dw_in, static_cast<T*>(dw_in), 2 * E, p.inner, p.width, F, D);
+    back.add(w.dw_out, static_cast<T*>(dw_out), E, p.width, p.inner, D, F);
+    return recast(back, s);
   });
 }

@@ -32,8 +32,10 @@ struct FfnArgs {
   T* dx;
   T* dw_in;
   T* dw_out;
+  // DWIN and DWOUT: the slots of an expert in `splits` parts, whose sums go to partial [splits][experts][rows][columns]
+  int splits;
+  float* partial;
 };
-
 // [lo, hi) of an expert; whatever the offsets hold, it lies in [0, slots]
 struct SlotRange {
   int64_t lo, hi;
@@ -44,6 +46,14 @@ __device__ __forceinline__ SlotRange slot_range(const int64_t* offsets, int e, i
   hi = hi < lo ? lo : hi > slots ? slots : hi;
   return {lo, hi};
 }
+// the slots of part `s` of an expert's [lo, hi)
+__device__ __forceinline__ SlotRange split_range(SlotRange r, int s, int splits) {
+  if (splits == 1) return r;
+  const int64_t each = ((r.hi - r.lo + splits - 1) / splits + 63) & ~int64_t(63);
+  const int64_t lo = r.lo + s * each, hi = lo + each;
+  return {lo < r.hi ? lo : r.hi, hi < r.hi ? hi : r.hi};
+}
+
 __device__ __forceinline__ int64_t slots_used(const int64_t* offsets, int experts, int64_t slots) {
   const int64_t v = __ldg(offsets + experts);
   return v < 0 ? 0 : v > slots ? slots : v;

@@ -42,7 +42,7 @@ constexpr int TC_SMEM = TC_STAGES * TC_STAGE + 1024;
 constexpr int TC_THREADS = 384;
 constexpr int TC_EPILOGUE = 8;              // warps that write results
 constexpr int TC_COLS = 16;                 // columns that a lane holds at a time
-constexpr int TC_AHEAD = 3;
+constexpr int TC_AHEAD = 1;
 constexpr unsigned TC_WAIT_LIMIT = 1u << 22;
 
 __device__ __forceinline__ uint32_t smem_at(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
@@ -172,7 +172,7 @@ struct Half2<__half> {
 
 // a tile: rows of m from m0 on (of both blocks), n columns from n0 on of which `valid` are written, k blocks
 struct TcTile {
-  int expert, m0, n, valid, blocks;
+  int expert, m0, n, valid, blocks, split;
   int64_t n0;       // slot, or row of a weight gradient
   int64_t k0, k1;   // slots of a weight gradient
 };
@@ -190,8 +190,9 @@ template <int WHICH>
 struct TcTiles {
   static constexpr bool SLOTS = WHICH <= FFN_DX;
   int m_tiles, n_tiles, depth;  // n_tiles: of a weight gradient
-  int n_total, wide;            // a weight gradient's n, and its columns a tile
-  __device__ __forceinline__ void init(int D, int F) {
+  int n_total, wide, splits;    // a weight gradient's n, its columns a tile, parts of its slots
+  __device__ __forceinline__ void init(int D, int F, int splits_) {
+    splits = splits_;
     const int m = WHICH == FFN_IN ? 2 * F : WHICH == FFN_DH || WHICH == FFN_DWOUT ? F : D;
     m_tiles = (m + 255) / 256;
     depth = WHICH == FFN_IN || WHICH == FFN_DH ? D : WHICH == FFN_OUT ? F : 2 * F;
@@ -217,15 +218,17 @@ struct TcTiles {
       r.k0 = r.k1 = 0;
       r.blocks = (depth + TC_K - 1) / TC_K;
     } else {
-      const int each = m_tiles * n_tiles;
-      r.expert = t / each;
-      const int rest = t - r.expert * each;
+      const int each = m_tiles * n_tiles, of_split = t / each;
+      r.expert = of_split / splits;
+      r.split = of_split - r.expert * splits;
+      const int rest = t - of_split * each;
       r.m0 = rest % m_tiles * 256;
       r.n0 = rest / m_tiles * wide;
       r.n = wide;
       r.valid = min(n_total - (int)r.n0, wide);
-      r.k0 = of.lo[r.expert];
-      r.k1 = of.hi[r.expert];
+      const SlotRange s = split_range({of.lo[r.expert], of.hi[r.expert]}, r.split, splits);
+      r.k0 = s.lo;
+      r.k1 = s.hi;
       r.blocks = (int)((r.k1 - r.k0 + TC_K - 1) / TC_K);
     }
     return r;
@@ -296,12 +299,14 @@ struct TcOut {
   const char *pre_a, *pre_b;
   uint32_t at, at_h, two, two_h;  // offsets of the lane's first column, and of two columns; _h: in rows of inner
   int live, col;                  // col: the lane's column of each pair (IN: of each four)
+  bool partial;                   // float32 sums of a part of the slots, one lane a row
 };
 template <class T, int WHICH>
 __device__ __forceinline__ TcOut tile_out(const FfnArgs<T>& p, const TcTile& t, int m_block, int lane, int quad) {
   const int64_t D = p.width, F = p.inner;
   const int odd = lane & 1;
   TcOut o;
+  o.partial = false;
   if constexpr (WHICH == FFN_IN) {
     const int f = (t.m0 + m_block) / 2 + quad * 16 + (lane >> 4) * 8 + (lane & 7);
     o.col = 2 * odd + ((lane >> 3) & 1);
@@ -326,6 +331,15 @@ __device__ __forceinline__ TcOut tile_out(const FfnArgs<T>& p, const TcTile& t, 
       o.two = 4 * (uint32_t)F * sizeof(T);
       o.two_h = 2 * (uint32_t)F * sizeof(T);
     } else {
+      if (WHICH >= FFN_DWIN && p.splits > 1) {
+        const int64_t rows = WHICH == FFN_DWIN ? 2 * F : D;
+        o.partial = true;
+        o.col = 0;
+        o.first = reinterpret_cast<char*>(p.partial + (((int64_t)t.split * p.experts + t.expert) * rows + t.n0) * ld + m);
+        o.two = o.two_h = 2 * (uint32_t)ld * sizeof(float);
+        o.at = o.at_h = 0;
+        return o;
+      }
       T* out = WHICH == FFN_OUT ? p.y : WHICH == FFN_DX ? p.dx : WHICH == FFN_DWIN ? p.dw_in : p.dw_out;
       if constexpr (WHICH == FFN_DWIN) out += (int64_t)t.expert * 2 * F * D;
       if constexpr (WHICH == FFN_DWOUT) out += (int64_t)t.expert * D * F;
@@ -375,6 +389,12 @@ __device__ __forceinline__ void write_columns(const TcOut& o, const float* v, co
       }
       at += 2 * o.two;
       at_h += 2 * o.two_h;
+    }
+  } else if (WHICH >= FFN_DWIN && o.partial) {
+#pragma unroll
+    for (int j = 0; j < TC_COLS; ++j) {
+      if (c + j < live) *reinterpret_cast<float*>(o.first + at) = v[j];
+      at += o.two / 2;
     }
   } else {
 #pragma unroll
@@ -448,7 +468,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(TC_THREADS, 1)
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
   }
   TcTiles<WHICH> tiles;
-  tiles.init(p.width, p.inner);
+  tiles.init(p.width, p.inner, SLOTS ? 1 : p.splits);
   if constexpr (WHICH != FFN_IN && WHICH != FFN_DH) {
     // everything before this point overlaps the product before, whose results are read from here on
     asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -486,7 +506,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(TC_THREADS, 1)
   cluster_arrive_wait();
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
   const uint32_t tmem = tmem_base;
-  const int total = SLOTS ? of.prefix[p.experts] * tiles.m_tiles : p.experts * tiles.m_tiles * tiles.n_tiles;
+  const int total = SLOTS ? of.prefix[p.experts] * tiles.m_tiles : p.experts * tiles.splits * tiles.m_tiles * tiles.n_tiles;
   const int first = blockIdx.x >> 1, step = gridDim.x >> 1;
   const int m_block = rank * TC_HALF;
 

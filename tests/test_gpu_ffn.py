@@ -142,6 +142,29 @@ def test_a_dense_block_of_many_rows():
     check(*inputs(6, [3001], 0, 128, 192, "bf16"), act=1)
 
 
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("width,inner", [(24, 16), (17, 40), (264, 8)])
+@pytest.mark.parametrize("counts", [[9000], [4001, 0, 5003]], ids=str)
+def test_long_sums_of_small_weights(kind, width, inner, counts):
+    """The weights' gradients are few tiles over many slots: summed in parts, which are then added."""
+    check(*inputs(13, counts, 4, width, inner, kind), act=0)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+@pytest.mark.parametrize("width,inner", [(201, 203), (200, 203), (203, 200)])
+def test_odd_widths_of_many_rows(kind, width, inner):
+    """16-bit rows that are not whole 16-byte pieces are copied into rows that are."""
+    check(*inputs(14, [2500, 0, 131], 7, width, inner, kind), act=1)
+    offsets, x, dy, w_in, w_out = inputs(15, [2900], 3, width, inner, kind)
+    at = torch.from_numpy(offsets).to(dev())
+    y, pre = erc.erc_expert_ffn(x, at, w_in, w_out, keep=True)
+    full = erc.erc_expert_ffn_backward(dy, x, pre, at, w_in, w_out)
+    rows = erc.erc_expert_ffn_backward(dy, x, pre, at, w_in, w_out, dw=False)
+    weights = erc.erc_expert_ffn_backward(dy, x, pre, at, w_in, w_out, dxs=False)
+    assert torch.equal(rows[0], full[0]) and torch.equal(weights[1], full[1]) and torch.equal(weights[2], full[2])
+    assert torch.equal(erc.erc_expert_ffn(x, at, w_in, w_out)[0], y)
+
+
 def test_rows_that_hold_infinities_stay_by_themselves():
     offsets, x, dy, w_in, w_out = inputs(7, [70, 60], 0, 64, 64, "bf16")
     at = torch.from_numpy(offsets).to(dev())
