@@ -18,8 +18,8 @@
 // factors of the same 8 features alternate in m (the copy's box does that), so that a lane and the lane 8
 // further hold a and b of one feature.
 //
-// Persistent blocks of 12 warps: copies (TMA), products, a warp that passes on what has landed, one that
-// zeroes the rows behind the last expert's, and 8 that read tensor memory and write results while the next
+// Persistent blocks of 20 warps: copies (TMA), products, a warp that passes on what has landed, one that
+// zeroes the rows behind the last expert's, and 16 that read tensor memory and write results while the next
 // tile runs in its other half.
 //
 // Every wait on a barrier ends: after WAIT_LIMIT polls it gives up, the block's roles stop, copies and
@@ -39,10 +39,10 @@ constexpr int TC_HALF = 128;                // rows of A and of B that a block h
 constexpr int TC_OPERAND = TC_HALF * TC_K * 2;
 constexpr int TC_STAGE = 2 * TC_OPERAND;
 constexpr int TC_SMEM = TC_STAGES * TC_STAGE + 1024;
-constexpr int TC_THREADS = 384;
-constexpr int TC_EPILOGUE = 8;              // warps that write results
-constexpr int TC_COLS = 16;                 // columns that a lane holds at a time
-constexpr int TC_AHEAD = 1;
+constexpr int TC_EPILOGUE = 16;             // warps that write results: a quarter of the rows and of the columns each
+constexpr int TC_PART = 256 / (TC_EPILOGUE / 4);
+constexpr int TC_THREADS = 128 + 32 * TC_EPILOGUE;
+constexpr int tc_cols(int which) { return which == FFN_DH ? 8 : 16; }  // columns that a lane holds at a time
 constexpr unsigned TC_WAIT_LIMIT = 1u << 22;
 
 __device__ __forceinline__ uint32_t smem_at(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
@@ -136,14 +136,21 @@ __device__ __forceinline__ void commit_pair(uint32_t bar) {
       "h"((uint16_t)3)
       : "memory");
 }
+template <int COLS>
 __device__ __forceinline__ void read_tmem(uint32_t addr, float* v) {
   uint32_t* r = reinterpret_cast<uint32_t*>(v);
-  asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
-      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
-        "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
-      : "r"(addr)
-      : "memory");
+  if constexpr (COLS == 8)
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+                 : "r"(addr)
+                 : "memory");
+  else
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(addr)
+        : "memory");
 }
 __device__ __forceinline__ void read_tmem_done() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 
@@ -275,14 +282,15 @@ __device__ __forceinline__ void act_pair(uint64_t a, uint64_t& value, uint64_t& 
   }
 }
 
-// DH: the pairs (a, a') and (b, b') of TC_COLS columns that a lane needs, read while the columns before them are at work
+// DH: the pairs (a, a') and (b, b') of the columns that a lane needs, read while the columns before them are at work
+constexpr int PRE_PAIRS = tc_cols(FFN_DH) / 2;
 struct PrePairs {
-  uint32_t a[TC_COLS / 2], b[TC_COLS / 2];
+  uint32_t a[PRE_PAIRS], b[PRE_PAIRS];
 };
 // `at`: the lane's byte offset of its first column's row; `two`: bytes of two rows; columns from `live` on are not read
 __device__ __forceinline__ void read_pre(const char* a, const char* b, uint32_t at, uint32_t two, int c, int live, PrePairs& r) {
 #pragma unroll
-  for (int j = 0; j < TC_COLS / 2; ++j) {
+  for (int j = 0; j < PRE_PAIRS; ++j) {
     r.a[j] = r.b[j] = 0;
     if (c + 2 * j < live) {
       r.a[j] = __ldg(reinterpret_cast<const uint32_t*>(a + at));
@@ -352,10 +360,11 @@ __device__ __forceinline__ TcOut tile_out(const FfnArgs<T>& p, const TcTile& t, 
   return o;
 }
 
-// TC_COLS columns of a tile from column c on
+// a lane's columns of a tile from column c on
 template <class T, int WHICH, int ACT>
 __device__ __forceinline__ void write_columns(const TcOut& o, const float* v, const PrePairs& pre, int c, int lane, bool keep) {
   using H = Half2<T>;
+  constexpr int COLS = tc_cols(WHICH);
   const uint32_t pick = pair_pick(lane);
   const int live = o.live - o.col;
   uint32_t at = o.at + (uint32_t)c / 2 * o.two, at_h = o.at_h + (uint32_t)c / 2 * o.two_h;
@@ -364,7 +373,7 @@ __device__ __forceinline__ void write_columns(const TcOut& o, const float* v, co
     // gates' lanes keep the first, the factors' lanes the second
     const bool up = lane & 8;
 #pragma unroll
-    for (int j = 0; j < TC_COLS; j += 4) {
+    for (int j = 0; j < COLS; j += 4) {
       float g[2], u[2];
 #pragma unroll
       for (int q = 0; q < 2; ++q) {
@@ -392,13 +401,13 @@ __device__ __forceinline__ void write_columns(const TcOut& o, const float* v, co
     }
   } else if (WHICH >= FFN_DWIN && o.partial) {
 #pragma unroll
-    for (int j = 0; j < TC_COLS; ++j) {
+    for (int j = 0; j < COLS; ++j) {
       if (c + j < live) *reinterpret_cast<float*>(o.first + at) = v[j];
       at += o.two / 2;
     }
   } else {
 #pragma unroll
-    for (int j = 0; j < TC_COLS; j += 2) {
+    for (int j = 0; j < COLS; j += 2) {
       const bool mine = c + j < live;
       if constexpr (WHICH == FFN_DH) {
         const bool odd = lane & 1;
@@ -616,53 +625,47 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(TC_THREADS, 1)
           reinterpret_cast<uint4*>(out)[i] = make_uint4(0, 0, 0, 0);
     }
   } else {  // results
-    const int quad = warp & 3, part = (warp - 4) >> 2;
+    constexpr int COLS = tc_cols(WHICH);
+    const int quad = warp & 3, c0 = (warp - 4) / 4 * TC_PART;
+    const bool keep = p.pre != nullptr;
     int a = 0;
     uint32_t a_phase = 0;
-    bool ok = true;
-    for (int at = first; ok && at < total; at += step) {
+    for (int at = first; at < total; at += step) {
       const TcTile t = tiles.at(at, of, p.experts);
-      const int c1 = min(t.n, (part + 1) * 128);
+      const int c1 = min(t.n, c0 + TC_PART);
       const TcOut out = tile_out<T, WHICH>(p, t, m_block, lane, quad);
-      const bool keep = p.pre != nullptr;
-      float v[TC_COLS];
-      PrePairs pre, next[TC_AHEAD];  // DH: read TC_AHEAD steps before their use
+      float v[COLS];
+      PrePairs pre, next;
       if (t.blocks == 0) {
 #pragma unroll
-        for (int i = 0; i < TC_COLS; ++i) v[i] = 0.f;
+        for (int i = 0; i < COLS; ++i) v[i] = 0.f;
 #pragma unroll 1
-        for (int c = part * 128; c < c1; c += TC_COLS) write_columns<T, WHICH, ACT>(out, v, pre, c, lane, keep);
+        for (int c = c0; c < c1; c += COLS) write_columns<T, WHICH, ACT>(out, v, pre, c, lane, keep);
         continue;
       }
-      auto read_ahead = [&](int c, PrePairs& r) {
-        read_pre(out.pre_a, out.pre_b, out.at + (uint32_t)c / 2 * out.two, out.two, c, c < c1 ? out.live - out.col : 0, r);
+      auto read_ahead = [&](int c) {
+        read_pre(out.pre_a, out.pre_b, out.at + (uint32_t)c / 2 * out.two, out.two, c, c < c1 ? out.live - out.col : 0, next);
       };
-      if constexpr (WHICH == FFN_DH) {
-#pragma unroll
-        for (int i = 0; i < TC_AHEAD; ++i) read_ahead(part * 128 + i * TC_COLS, next[i]);
-      }
-      ok = __all_sync(0xffffffffu, bar_wait(full(a), a_phase, &failed));
-      if (!ok) break;
+      if constexpr (WHICH == FFN_DH) read_ahead(c0);
+      if (!__all_sync(0xffffffffu, bar_wait(full(a), a_phase, &failed))) break;
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
       const uint32_t src = tmem + a * 256 + ((uint32_t)(quad * 32) << 16);
 #pragma unroll 1
-      for (int c = part * 128; c < c1; c += TC_COLS) {
-        read_tmem(src + c, v);
+      for (int c = c0; c < c1; c += COLS) {
+        read_tmem<COLS>(src + c, v);
         if constexpr (WHICH == FFN_DH) {
-          pre = next[0];
-#pragma unroll
-          for (int i = 0; i + 1 < TC_AHEAD; ++i) next[i] = next[i + 1];
-          read_ahead(c + TC_AHEAD * TC_COLS, next[TC_AHEAD - 1]);
+          pre = next;
+          read_ahead(c + COLS);
         }
         read_tmem_done();
-        if (c + TC_COLS >= c1) {
+        if (c + COLS >= c1) {
           asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
           __syncwarp();
           if (lane == 0) bar_arrive_cluster(peer_address(taken(a), 0));
         }
         write_columns<T, WHICH, ACT>(out, v, pre, c, lane, keep);
       }
-      if (part * 128 >= c1) {
+      if (c0 >= c1) {
         __syncwarp();
         if (lane == 0) bar_arrive_cluster(peer_address(taken(a), 0));
       }
