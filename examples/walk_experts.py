@@ -6,7 +6,11 @@ predict the next node of a walk, its nodes routed to experts (erc_route, erc_exp
 erc_expert_gather, erc_expert_combine, with their gradients); at the end nodes are drawn from the
 model's scores over all nodes, one row a walker (erc_sample_rows again, as a decoder uses it).
 
-    python examples/walk_experts.py [--steps 60] [--walkers 512]
+With --gated the experts are gated feed-forward blocks whose result is dropped out and added to the
+nodes' rows (erc_expert_ffn, erc_dropout), and the loss is the steps' log probability with a little
+entropy (erc_score_rows): no product of the experts and no row of scores leaves the library.
+
+    python examples/walk_experts.py [--steps 60] [--walkers 512] [--gated]
 """
 from __future__ import annotations
 
@@ -89,6 +93,73 @@ class Experts(torch.nn.Module):
         return Combine.apply(y, weights, slot, offsets)
 
 
+class Block(torch.autograd.Function):
+    """The gated feed-forward block of each expert on its rows."""
+
+    @staticmethod
+    def forward(ctx, xs, w_in, w_out, offsets, act):
+        y, pre = erc.erc_expert_ffn(xs, offsets, w_in, w_out, act=act, keep=True)
+        ctx.save_for_backward(xs, pre, offsets, w_in, w_out)
+        ctx.act = act
+        return y
+
+    @staticmethod
+    def backward(ctx, dy):
+        xs, pre, offsets, w_in, w_out = ctx.saved_tensors
+        return *erc.erc_expert_ffn_backward(dy.contiguous(), xs, pre, offsets, w_in, w_out, act=ctx.act), None, None
+
+
+class Dropout(torch.autograd.Function):
+    """residual + dropout(x): the gradient is the same call on the gradient."""
+
+    @staticmethod
+    def forward(ctx, x, residual, p, key):
+        ctx.p, ctx.key = p, key
+        return erc.erc_dropout(x, p, key, residual=residual)
+
+    @staticmethod
+    def backward(ctx, dout):
+        dout = dout.contiguous()
+        return erc.erc_dropout(dout, ctx.p, ctx.key), dout, None, None
+
+
+class Scored(torch.autograd.Function):
+    """(log probability of the given entries, entropy) of rows of scores."""
+
+    @staticmethod
+    def forward(ctx, logits, ids):
+        logp, entropy, norm, _, _ = erc.erc_score_rows(logits, ids)
+        ctx.save_for_backward(logits, ids, norm, entropy)
+        return logp, entropy
+
+    @staticmethod
+    def backward(ctx, dlogp, dentropy):
+        logits, ids, norm, entropy = ctx.saved_tensors
+        return erc.erc_score_rows_backward(logits, ids, norm, dlogp.contiguous(), entropy, dentropy.contiguous()), None
+
+
+class GatedExperts(torch.nn.Module):
+    """out[t] = x[t] + dropout(sum_j w[t, j] O_e (act(G_e x[t]) U_e x[t])), e the j-th expert of row t."""
+
+    def __init__(self, width, n_experts, k, inner=None, p=0.1, act=erc.ERC_ACT_SILU):
+        super().__init__()
+        inner = inner or 2 * width
+        self.n_experts, self.k, self.p, self.act = n_experts, k, p, act
+        self.router = torch.nn.Parameter(torch.randn(width, n_experts) * width**-0.5)
+        self.w_in = torch.nn.Parameter(torch.randn(n_experts, 2 * inner, width) * width**-0.5)
+        self.w_out = torch.nn.Parameter(torch.randn(n_experts, width, inner) * inner**-0.5)
+        self.key = 0  # of the next step's dropout
+
+    def forward(self, x):
+        experts, weights = Route.apply(x @ self.router, self.k, erc.ERC_SCORE_SOFTMAX, None)
+        offsets, _, slot = erc.erc_expert_plan(experts, self.n_experts)
+        y = Block.apply(Gather.apply(x, slot, offsets), self.w_in, self.w_out, offsets, self.act)
+        out = Combine.apply(y, weights, slot, offsets)
+        if self.training:
+            self.key += 1
+        return Dropout.apply(out, x, self.p if self.training else 0.0, self.key)
+
+
 def neighbour_scores(n, src, dst, w, dev):
     """Padded (ids, scores) of every node's neighbours: Eq. 8's edge weight as a logarithm, -inf where
     a node has no more neighbours."""
@@ -118,13 +189,13 @@ def walk(table, start, steps, generator, temperature=0.7, top_p=0.95):
     return torch.stack(nodes, 1)
 
 
-def main(steps=60, walkers=512, width=64, n_experts=8, k=2, seed=0, n=400):
+def main(steps=60, walkers=512, width=64, n_experts=8, k=2, seed=0, n=400, gated=False):
     dev = torch.device("cuda:0")
     torch.manual_seed(seed)
     generator = torch.Generator(device=dev).manual_seed(seed)
     table = neighbour_scores(*synth.random_connected(n, 4 * n, seed=seed + 11, weighted=True), dev)
     embed = torch.nn.Embedding(n, width).to(dev)
-    model = Experts(width, n_experts, k).to(dev)
+    model = (GatedExperts if gated else Experts)(width, n_experts, k).to(dev)
     answer = torch.nn.Linear(width, n).to(dev)
     optimiser = torch.optim.Adam([*embed.parameters(), *model.parameters(), *answer.parameters()], lr=1e-2)
     losses = []
@@ -132,7 +203,11 @@ def main(steps=60, walkers=512, width=64, n_experts=8, k=2, seed=0, n=400):
         start = torch.randint(0, n, (walkers,), generator=generator, device=dev)
         nodes = walk(table, start, 4, generator)
         scores = answer(model(embed(nodes[:, :-1].reshape(-1))))
-        loss = torch.nn.functional.cross_entropy(scores, nodes[:, 1:].reshape(-1))
+        if gated:
+            logp, entropy = Scored.apply(scores, nodes[:, 1:].reshape(-1).to(torch.int32))
+            loss = -(logp + 0.001 * entropy).mean()
+        else:
+            loss = torch.nn.functional.cross_entropy(scores, nodes[:, 1:].reshape(-1))
         optimiser.zero_grad()
         loss.backward()
         optimiser.step()
@@ -150,7 +225,8 @@ if __name__ == "__main__":
     parser = argparse.ArgumentParser()
     parser.add_argument("--steps", type=int, default=60)
     parser.add_argument("--walkers", type=int, default=512)
+    parser.add_argument("--gated", action="store_true")
     args = parser.parse_args()
-    r = main(args.steps, args.walkers)
+    r = main(args.steps, args.walkers, gated=args.gated)
     print(f"loss {r['losses'][0]:.3f} -> {r['losses'][-1]:.3f}; drawn nodes that are neighbours: "
           f"{100 * r['on_an_edge']:.0f}%; kept entries a row: {r['kept'].float().mean().item():.1f}")

@@ -94,7 +94,10 @@ uint64_t erc_kernel_launches(void);
  * wait makes before it gives up, for all later calls of the process; 0 (the initial state)
  * restores each wait's default, which is seconds of waiting.  Waits of work already enqueued keep
  * the limit they were enqueued with.  The hardware cluster barriers of the cluster CG solver and of
- * erc_sample_rows are not polled and take no limit. */
+ * erc_sample_rows are not polled and take no limit.  The waits of erc_score_rows and erc_expert_ffn for
+ * copies and products within a thread block or a pair of them keep fixed limits of their own, seconds
+ * of waiting: a row of scores whose copy did not land has NaN as its results, and erc_expert_ffn says
+ * so in its workspace. */
 void erc_set_wait_limit(uint32_t polls);
 
 /* ---------------------------------------------------------------------------------------------
@@ -467,9 +470,12 @@ erc_status erc_score_rows_backward(int64_t rows, int64_t n, const void* logits, 
  *      and dy behind offsets[experts] do not matter.
  * Limits: width and inner in [1, ERC_FFN_MAX_WIDTH], experts in [1, ERC_ROUTE_MAX_EXPERTS], slots in
  *      [0, 2^31).  bfloat16 and float16 with width and inner that are multiples of 8 and 16-byte
- *      aligned arrays use the tensor cores; everything else runs on the float32 units.
- * Workspace: erc_expert_ffn_workspace_size and erc_expert_ffn_backward_workspace_size bytes; calls
- *      that overlap on the GPU need one each.
+ *      aligned arrays use the tensor cores, and so do many rows of other widths, by way of copies in the
+ *      workspace; everything else runs on the float32 units.
+ * Workspace: erc_expert_ffn_workspace_size and erc_expert_ffn_backward_workspace_size bytes on the
+ *      current device; calls that overlap on the GPU need one each.  The int32 at its first 256-byte
+ *      boundary is ERC_OK once the work is done, or ERC_ERR_TIMEOUT where a wait on the device ran out
+ *      (the results are then undefined).
  * Errors: INVALID_ARG for sizes, types, alignment and pointers; CAPACITY for a small workspace.
  *      Deterministic.
  * ------------------------------------------------------------------------------------------- */

@@ -42,6 +42,7 @@ constexpr int TC_SMEM = TC_STAGES * TC_STAGE + 1024;
 constexpr int TC_EPILOGUE = 16;             // warps that write results: a quarter of the rows and of the columns each
 constexpr int TC_PART = 256 / (TC_EPILOGUE / 4);
 constexpr int TC_THREADS = 128 + 32 * TC_EPILOGUE;
+constexpr int TC_AHEAD = 1;
 constexpr int tc_cols(int which) { return which == FFN_DH ? 8 : 16; }  // columns that a lane holds at a time
 constexpr unsigned TC_WAIT_LIMIT = 1u << 22;
 
@@ -445,6 +446,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(TC_THREADS, 1)
   extern __shared__ char raw[];
   __shared__ __align__(8) uint64_t bars[3 * TC_STAGES + 5];
   __shared__ TcRanges of;
+  __shared__ float cost_of[4];
   __shared__ uint32_t tmem_base;
   __shared__ volatile int failed;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -487,10 +489,30 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(TC_THREADS, 1)
     const SlotRange r = slot_range(p.offsets, e, p.slots);
     of.lo[e] = (int)r.lo;
     of.hi[e] = (int)r.hi;
-    const int rows = of.hi[e] - of.lo[e], count = (int)(((unsigned)rows + 255u) / 256u);
-    const int wide = count > 1 ? ((rows + count - 1) / count + 31) & ~31 : 256;
-    of.wide[e] = (short)wide;
-    of.prefix[e + 1] = (int)(((unsigned)rows + wide - 1) / wide);
+  }
+  if (SLOTS) {
+    // The widest tile that costs least: the pairs' last tiles may leave most of them idle, so that narrower ones end
+    // sooner.  A tile costs its columns and a share for A, which is read whatever they are.
+    __syncthreads();
+    if (warp < 4) {
+      const int wide = 256 - 32 * warp;
+      int count = 0;
+      for (int e = lane; e < p.experts; e += 32) count += ((unsigned)(of.hi[e] - of.lo[e]) + wide - 1) / wide;
+      count = __reduce_add_sync(0xffffffffu, count);
+      const int pairs = gridDim.x / 2;
+      if (lane == 0) cost_of[warp] = (float)((count * tiles.m_tiles + pairs - 1) / pairs) * (wide + 85);
+    }
+    __syncthreads();
+    int most = 256;
+    float least = cost_of[0];
+    for (int i = 1; i < 4; ++i)
+      if (cost_of[i] < 0.97f * least) least = cost_of[i], most = 256 - 32 * i;
+    for (int e = threadIdx.x; e < p.experts; e += TC_THREADS) {
+      const int rows = of.hi[e] - of.lo[e], count = (int)(((unsigned)rows + most - 1) / most);
+      const int wide = count > 1 ? ((rows + count - 1) / count + 31) & ~31 : 256;
+      of.wide[e] = (short)wide;
+      of.prefix[e + 1] = (int)(((unsigned)rows + wide - 1) / wide);
+    }
   }
   if (SLOTS) {
     __syncthreads();
@@ -635,7 +657,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(TC_THREADS, 1)
       const int c1 = min(t.n, c0 + TC_PART);
       const TcOut out = tile_out<T, WHICH>(p, t, m_block, lane, quad);
       float v[COLS];
-      PrePairs pre, next;
+      PrePairs pre, next[TC_AHEAD];  // DH: read TC_AHEAD steps before their use
       if (t.blocks == 0) {
 #pragma unroll
         for (int i = 0; i < COLS; ++i) v[i] = 0.f;
@@ -643,10 +665,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(TC_THREADS, 1)
         for (int c = c0; c < c1; c += COLS) write_columns<T, WHICH, ACT>(out, v, pre, c, lane, keep);
         continue;
       }
-      auto read_ahead = [&](int c) {
-        read_pre(out.pre_a, out.pre_b, out.at + (uint32_t)c / 2 * out.two, out.two, c, c < c1 ? out.live - out.col : 0, next);
+      auto read_ahead = [&](int c, PrePairs& r) {
+        read_pre(out.pre_a, out.pre_b, out.at + (uint32_t)c / 2 * out.two, out.two, c, c < c1 ? out.live - out.col : 0, r);
       };
-      if constexpr (WHICH == FFN_DH) read_ahead(c0);
+      if constexpr (WHICH == FFN_DH) {
+#pragma unroll
+        for (int i = 0; i < TC_AHEAD; ++i) read_ahead(c0 + i * COLS, next[i]);
+      }
       if (!__all_sync(0xffffffffu, bar_wait(full(a), a_phase, &failed))) break;
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
       const uint32_t src = tmem + a * 256 + ((uint32_t)(quad * 32) << 16);
@@ -654,8 +679,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(TC_THREADS, 1)
       for (int c = c0; c < c1; c += COLS) {
         read_tmem<COLS>(src + c, v);
         if constexpr (WHICH == FFN_DH) {
-          pre = next;
-          read_ahead(c + COLS);
+          pre = next[0];
+#pragma unroll
+          for (int i = 0; i + 1 < TC_AHEAD; ++i) next[i] = next[i + 1];
+          read_ahead(c + TC_AHEAD * COLS, next[TC_AHEAD - 1]);
         }
         read_tmem_done();
         if (c + COLS >= c1) {

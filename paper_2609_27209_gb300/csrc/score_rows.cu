@@ -528,17 +528,19 @@ __global__ void __launch_bounds__(ST) k_score_join(int64_t rows, int64_t n, cons
     if (threadIdx.x == 0) finish_row(o, row, g, a);
     if (TOP) {
       const float lnT = a.T > 0.f ? logf(a.T) : -INFINITY;
+      // the parts' best first, then their second best, ..: a thread's largest is some part's best, or nearly so
       const Best* from = best + row * parts * o.k;
+      auto nth = [&](int i) { return from[i % parts * o.k + i / parts]; };
       unsigned mine = 0;
 #pragma unroll 8
-      for (int i = threadIdx.x; i < parts * o.k; i += ST) mine = max(mine, from[i].key);
+      for (int i = threadIdx.x; i < parts * o.k; i += ST) mine = max(mine, nth(i).key);
       block_top(
           top, mine, o.k,
           [&](unsigned, auto&& f) {
             for (int i0 = threadIdx.x; i0 < parts * o.k; i0 += 8 * ST) {  // eight reads in flight
               Best b[8];
 #pragma unroll
-              for (int j = 0; j < 8; ++j) b[j] = i0 + j * ST < parts * o.k ? from[i0 + j * ST] : Best{0u, 0u};
+              for (int j = 0; j < 8; ++j) b[j] = i0 + j * ST < parts * o.k ? nth(i0 + j * ST) : Best{0u, 0u};
 #pragma unroll
               for (int j = 0; j < 8; ++j) f(b[j].key, b[j].id);
             }
@@ -757,8 +759,9 @@ __device__ __forceinline__ uint4 shifted(uint4 a, uint4 b, int by) {
 
 // WARPS warps (a block, or one) take `each` vectors of a row's result, SV steps of 31 WARPS or 32 WARPS at a time.  Where the result's rows are aligned otherwise than
 // the scores', a result vector is two neighbouring lanes' shifted together, and 32 lanes give 31.
-template <class T, int WARPS>
-__global__ void __launch_bounds__(ST, 4) k_score_backward(int64_t rows, int64_t n, const T* __restrict__ logits, int64_t stride,
+// SHIFT: some rows may be aligned otherwise.
+template <class T, int WARPS, bool SHIFT>
+__global__ void __launch_bounds__(ST, SHIFT ? 4 : 5) k_score_backward(int64_t rows, int64_t n, const T* __restrict__ logits, int64_t stride,
                                                        int parts, int each, ScoreGrad o, T* __restrict__ dlogits) {
   constexpr int N = ScoreVec<T>::N;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, part_warp = warp % WARPS;
@@ -772,7 +775,7 @@ __global__ void __launch_bounds__(ST, 4) k_score_backward(int64_t rows, int64_t 
     const int skew = (int)((reinterpret_cast<uintptr_t>(out) & 15) / sizeof(T));  // of the result
     const int vectors = (skew + (int)n + N - 1) / N;
     // result vector u starts with entry u N - skew: entry `by` of score vector u - back
-    const int delta = view.skew - skew, back = delta < 0 ? 1 : 0, by = delta < 0 ? delta + N : delta;
+    const int delta = SHIFT ? view.skew - skew : 0, back = delta < 0 ? 1 : 0, by = delta < 0 ? delta + N : delta;
     const int wide = by ? 31 : 32, step = wide * WARPS, off = part_warp * wide;
     const int first = which * each, last = min(first + each, vectors);
     uint4 v[SV];
@@ -830,7 +833,7 @@ __global__ void __launch_bounds__(ST, 4) k_score_backward(int64_t rows, int64_t 
 #pragma unroll
           for (int i = 0; i < N; ++i) q.t[i] = from_f32<T>(r.one(l[i], e0 + i));
         }
-        if (by) {
+        if (SHIFT && by) {
           const uint4 next = make_uint4(__shfl_down_sync(0xffffffffu, q.raw.x, 1), __shfl_down_sync(0xffffffffu, q.raw.y, 1),
                                         __shfl_down_sync(0xffffffffu, q.raw.z, 1), __shfl_down_sync(0xffffffffu, q.raw.w, 1));
           q.raw = shifted(q.raw, next, by * (int)sizeof(T));
@@ -960,7 +963,8 @@ extern "C" erc_status erc_score_rows(int64_t rows, int64_t n, const void* logits
       const bool together = sp.parts > 1 && sp.parts <= CLUSTER;
       auto kernel = together ? (k ? k_score_part<T, true, true> : k_score_part<T, false, true>)
                              : (k ? k_score_part<T, true, false> : k_score_part<T, false, false>);
-      ERC_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, part_smem(SEGS * 32, true)));
+      if (smem > 40960)
+        ERC_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, part_smem(SEGS * 32, true)));
       // a grid is a whole number of clusters; blocks take further tasks a grid apart, so a cluster's stay together
       const int64_t most = (int64_t)sm_count() * 64 / sp.parts * sp.parts;
       cudaLaunchConfig_t cfg = {};
@@ -1010,8 +1014,11 @@ extern "C" erc_status erc_score_rows_backward(int64_t rows, int64_t n, const voi
     const int64_t wanted = ((int64_t)sm_count() * 8 + rows - 1) / rows;
     const int64_t parts = steps < wanted ? steps : wanted, each = (steps + parts - 1) / parts * unit;
     const int64_t tasks = rows * parts, blocks = wide ? tasks : (tasks + SW - 1) / SW, most = (int64_t)sm_count() * 256;
-    (wide ? k_score_backward<T, SW> : k_score_backward<T, 1>)<<<(unsigned)(blocks < most ? blocks : most), ST, 0,
-                                                                as_stream(stream)>>>(
+    const uintptr_t apart = reinterpret_cast<uintptr_t>(logits) ^ reinterpret_cast<uintptr_t>(dlogits);
+    const bool shift = apart % 16 != 0 || (rows > 1 && (stride - n) * (int64_t)sizeof(T) % 16 != 0);
+    auto kernel = wide ? (shift ? k_score_backward<T, SW, true> : k_score_backward<T, SW, false>)
+                       : (shift ? k_score_backward<T, 1, true> : k_score_backward<T, 1, false>);
+    kernel<<<(unsigned)(blocks < most ? blocks : most), ST, 0, as_stream(stream)>>>(
         rows, n, static_cast<const T*>(logits), stride, (int)parts, (int)each, o, static_cast<T*>(dlogits));
     count_launches(1);
     ERC_CUDA(cudaGetLastError());

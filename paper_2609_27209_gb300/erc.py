@@ -740,8 +740,8 @@ def _given_workspace(ws, need, device):
 
 def erc_score_rows(logits, ids=None, temperature=1.0, k=0, ws=None):
     """What each row of logits [rows, n] says about the entry ids[row] (see include/erc.h):
-    (logp float32 [rows] or None without ids, entropy float32 [rows], norm float32 [rows, 2],
-    top_ids int32 [rows, k], top_logp float32 [rows, k]).
+    (logp float32 [rows], entropy float32 [rows], norm float32 [rows, 2], top_ids int32 [rows, k],
+    top_logp float32 [rows, k]); logp is None without ids, the last two without k.
 
     ids int32 [rows]; an id outside [0, n) gives 0.  norm is what erc_score_rows_backward takes.  ws: a
     uint8 workspace of erc_score_rows_workspace_size bytes, or None.
@@ -753,14 +753,17 @@ def erc_score_rows(logits, ids=None, temperature=1.0, k=0, ws=None):
     k = _whole(k, "k")
     if not 0 <= k <= ERC_SCORE_MAX_K:
         _refuse(f"k must be in [0, {ERC_SCORE_MAX_K}]")
-    kw = dict(dtype=torch.float32, device=dev)
-    logp = torch.empty(rows, **kw) if ids is not None else None
-    entropy, norm = torch.empty(rows, **kw), torch.empty(rows, 2, **kw)
-    top_ids, top_logp = torch.empty(rows, k, dtype=torch.int32, device=dev), torch.empty(rows, k, **kw)
-    ws = _given_workspace(ws, lib().erc_score_rows_workspace_size(rows, n, kind, k), dev)
+    logp = torch.empty(rows, dtype=torch.float32, device=dev) if ids is not None else None
+    entropy = torch.empty(rows, dtype=torch.float32, device=dev)
+    norm = torch.empty((rows, 2), dtype=torch.float32, device=dev)
+    top_ids = torch.empty((rows, k), dtype=torch.int32, device=dev) if k else None
+    top_logp = torch.empty((rows, k), dtype=torch.float32, device=dev) if k else None
+    need = lib().erc_score_rows_workspace_size(rows, n, kind, k)
+    if need or ws is not None:
+        ws = _given_workspace(ws, need, dev)
     _check(lib().erc_score_rows(rows, n, logits.data_ptr(), kind, stride, _ptr(ids), temperature, k,
-                                _ptr(logp), entropy.data_ptr(), norm.data_ptr(), top_ids.data_ptr(),
-                                top_logp.data_ptr(), _ptr(ws), 0 if ws is None else ws.numel(),
+                                _ptr(logp), entropy.data_ptr(), norm.data_ptr(), _ptr(top_ids),
+                                _ptr(top_logp), _ptr(ws), 0 if ws is None else ws.numel(),
                                 _stream_of(logits)))
     return logp, entropy, norm, top_ids, top_logp
 

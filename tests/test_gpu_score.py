@@ -43,7 +43,11 @@ def check(logits, ids, temperature=1.0, k=0, every=1):
     """Forward and gradient of a device matrix against the oracle, every `every`-th row."""
     rows, n = logits.shape
     logp, entropy, norm, top_ids, top_logp = erc.erc_score_rows(logits, torch.from_numpy(ids).to(dev()), temperature, k)
-    assert top_ids.shape == top_logp.shape == (rows, k) and top_ids.dtype == torch.int32
+    if k:
+        assert top_ids.shape == top_logp.shape == (rows, k) and top_ids.dtype == torch.int32
+    else:
+        assert top_ids is None and top_logp is None
+        top_ids, top_logp = torch.empty(rows, 0, dtype=torch.int32), torch.empty(rows, 0)
     rng = np.random.default_rng(rows * 1000 + n)
     dlogp, dentropy = (rng.normal(size=rows).astype(np.float32) for _ in range(2))
     grad = erc.erc_score_rows_backward(logits, torch.from_numpy(ids).to(dev()), norm, torch.from_numpy(dlogp).to(dev()),
@@ -182,7 +186,7 @@ def test_optional_parts():
     ids = torch.tensor([3, 4, -1, 299], dtype=torch.int32, device=dev())
     logp, entropy, norm, top, _ = erc.erc_score_rows(x, ids)
     none, entropy2, norm2, _, _ = erc.erc_score_rows(x)
-    assert none is None and torch.equal(entropy, entropy2) and torch.equal(norm, norm2) and top.shape == (4, 0)
+    assert none is None and torch.equal(entropy, entropy2) and torch.equal(norm, norm2) and top is None
     g, h = torch.randn(2, 4, device=dev())
     zero = torch.zeros(4, device=dev())
     a = erc.erc_score_rows_backward(x, ids, norm, g)
