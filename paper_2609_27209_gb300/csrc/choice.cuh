@@ -221,6 +221,22 @@ __device__ __forceinline__ void unpack_pairs(uint4 u, uint64_t* p) {
 #pragma unroll
   for (int i = 0; i < ScoreVec<T>::N / 2; ++i) p[i] = pair(l[2 * i], l[2 * i + 1]);
 }
+// two values rounded to a 16-bit type, the first in the low half: one instruction, where two single conversions and a
+// merge take more
+__device__ __forceinline__ uint32_t pack_pair(float a, float b, __nv_bfloat16) {
+  const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+__device__ __forceinline__ uint32_t pack_pair(float a, float b, __half) {
+  const __half2 v = __floats2half2_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+// and back
+__device__ __forceinline__ float2 unpack_pair(uint32_t v, __nv_bfloat16) {
+  return make_float2(__uint_as_float(v << 16), __uint_as_float(v & 0xffff0000u));
+}
+__device__ __forceinline__ float2 unpack_pair(uint32_t v, __half) { return __half22float2(*reinterpret_cast<const __half2*>(&v)); }
+
 // the pattern of -inf in each lane of a 32-bit word
 template <class T>
 __device__ __forceinline__ unsigned masked_word();

@@ -12,8 +12,8 @@ constexpr int DT = 256;
 constexpr uint32_t DROP = 0x44524F50u;
 
 struct DropRule {
-  uint32_t most;  // words up to it are dropped; nothing is when `all`
-  bool all;
+  uint32_t most;  // words up to it are dropped
+  bool all;       // everything stays: p below 2^-32 (most is 0 then, and no words are drawn)
   float scale;
   uint64_t key, first;  // first: of the call's first entry, in blocks of 4
 };
@@ -37,12 +37,31 @@ __device__ __forceinline__ void drop_words(uint64_t block, uint64_t key, uint32_
   }
 }
 
-template <class T>
-union DropPiece {
-  uint4 raw;
-  T t[16 / sizeof(T)];
-  __device__ DropPiece() {}
-};
+// a piece of 16 bytes, the first entry's words in w
+template <class T, bool RESIDUAL>
+__device__ __forceinline__ uint4 drop_piece(uint4 x, uint4 r, const uint32_t* w, const DropRule& d) {
+  uint32_t v[4] = {x.x, x.y, x.z, x.w};
+  const uint32_t q[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (sizeof(T) == 4) {
+      float f = w[i] > d.most ? __fmul_rn(__uint_as_float(v[i]), d.scale) : 0.f;
+      if (RESIDUAL) f = __fadd_rn(f, __uint_as_float(q[i]));
+      v[i] = __float_as_uint(f);
+    } else {
+      float2 f = unpack_pair(v[i], T());
+      f.x = w[2 * i] > d.most ? __fmul_rn(f.x, d.scale) : 0.f;
+      f.y = w[2 * i + 1] > d.most ? __fmul_rn(f.y, d.scale) : 0.f;
+      if (RESIDUAL) {
+        const float2 g = unpack_pair(q[i], T());
+        f.x = __fadd_rn(f.x, g.x);
+        f.y = __fadd_rn(f.y, g.y);
+      }
+      v[i] = pack_pair(f.x, f.y, T());
+    }
+  }
+  return make_uint4(v[0], v[1], v[2], v[3]);
+}
 
 // all arrays are 16-byte aligned; a block takes 2 DT pieces of 16 bytes, the last one perhaps not whole
 template <class T, bool RESIDUAL>
@@ -51,34 +70,32 @@ __global__ void __launch_bounds__(DT) k_dropout(int64_t count, const T* x, const
   if (key_dev) d.key = *key_dev;
   constexpr int N = 16 / sizeof(T);
   int64_t v[2];
-  DropPiece<T> a[2], r[2];
+  uint4 a[2] = {}, r[2] = {};
 #pragma unroll
   for (int j = 0; j < 2; ++j) {
     v[j] = ((int64_t)blockIdx.x * 2 + j) * DT + threadIdx.x;
     if ((v[j] + 1) * N <= count) {
-      a[j].raw = reinterpret_cast<const uint4*>(x)[v[j]];
-      if (RESIDUAL) r[j].raw = reinterpret_cast<const uint4*>(residual)[v[j]];
-    } else {
-#pragma unroll
-      for (int i = 0; i < N; ++i)
-        if (v[j] * N + i < count) {
-          a[j].t[i] = x[v[j] * N + i];
-          if (RESIDUAL) r[j].t[i] = residual[v[j] * N + i];
-        }
+      a[j] = reinterpret_cast<const uint4*>(x)[v[j]];
+      if (RESIDUAL) r[j] = reinterpret_cast<const uint4*>(residual)[v[j]];
     }
   }
 #pragma unroll
   for (int j = 0; j < 2; ++j) {
     uint32_t w[N];
-    drop_words<N / 4>(d.first + (uint64_t)v[j] * (N / 4), d.key, w);
+    if (d.all) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) a[j].t[i] = drop_one(a[j].t[i], RESIDUAL ? &r[j].t[i] : nullptr, d.all || w[i] > d.most, d);
+      for (int i = 0; i < N; ++i) w[i] = ~0u;
+    } else {
+      drop_words<N / 4>(d.first + (uint64_t)v[j] * (N / 4), d.key, w);
+    }
     if ((v[j] + 1) * N <= count) {
-      reinterpret_cast<uint4*>(out)[v[j]] = a[j].raw;
+      reinterpret_cast<uint4*>(out)[v[j]] = drop_piece<T, RESIDUAL>(a[j], r[j], w, d);
     } else {
 #pragma unroll
-      for (int i = 0; i < N; ++i)
-        if (v[j] * N + i < count) out[v[j] * N + i] = a[j].t[i];
+      for (int i = 0; i < N; ++i) {
+        const int64_t e = v[j] * N + i;
+        if (e < count) out[e] = drop_one(x[e], RESIDUAL ? residual + e : nullptr, w[i] > d.most, d);
+      }
     }
   }
 }
@@ -121,7 +138,7 @@ extern "C" erc_status erc_dropout(int64_t count, const void* x, int32_t type, co
   const uint64_t least = (uint64_t)(p * 4294967296.);
   DropRule d;
   d.all = least == 0;
-  d.most = (uint32_t)(least - 1);
+  d.most = d.all ? 0u : (uint32_t)(least - 1);
   d.scale = p < 1. ? (float)(1. / (1. - p)) : 0.f;
   d.key = key;
   d.first = (uint64_t)first / 4;

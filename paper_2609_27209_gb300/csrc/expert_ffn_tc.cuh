@@ -156,26 +156,10 @@ __device__ __forceinline__ void read_tmem(uint32_t addr, float* v) {
 __device__ __forceinline__ void read_tmem_done() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 
 template <class T>
-struct Half2;
-template <>
-struct Half2<__nv_bfloat16> {
-  static constexpr uint32_t FORMAT = 1;
-  static __device__ __forceinline__ uint32_t pack(float a, float b) {
-    const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
-    return *reinterpret_cast<const uint32_t*>(&v);
-  }
-  static __device__ __forceinline__ float2 unpack(uint32_t v) {
-    return make_float2(__uint_as_float(v << 16), __uint_as_float(v & 0xffff0000u));
-  }
-};
-template <>
-struct Half2<__half> {
-  static constexpr uint32_t FORMAT = 0;
-  static __device__ __forceinline__ uint32_t pack(float a, float b) {
-    const __half2 v = __floats2half2_rn(a, b);
-    return *reinterpret_cast<const uint32_t*>(&v);
-  }
-  static __device__ __forceinline__ float2 unpack(uint32_t v) { return __half22float2(*reinterpret_cast<const __half2*>(&v)); }
+struct Half2 {
+  static constexpr uint32_t FORMAT = std::is_same<T, __nv_bfloat16>::value ? 1 : 0;  // of an operand, in the instruction
+  static __device__ __forceinline__ uint32_t pack(float a, float b) { return pack_pair(a, b, T()); }
+  static __device__ __forceinline__ float2 unpack(uint32_t v) { return unpack_pair(v, T()); }
 };
 
 // a tile: rows of m from m0 on (of both blocks), n columns from n0 on of which `valid` are written, k blocks

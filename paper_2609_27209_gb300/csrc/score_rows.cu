@@ -711,14 +711,6 @@ struct RowGrad {
     return v * inv;
   }
 };
-__device__ __forceinline__ uint32_t pack_pair(float a, float b, __nv_bfloat16) {
-  const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
-  return *reinterpret_cast<const uint32_t*>(&v);
-}
-__device__ __forceinline__ uint32_t pack_pair(float a, float b, __half) {
-  const __half2 v = __floats2half2_rn(a, b);
-  return *reinterpret_cast<const uint32_t*>(&v);
-}
 template <class T>
 __device__ __forceinline__ uint4 grad_vector(uint4 v, const RowGrad& r) {
   constexpr int P = ScoreVec<T>::N / 2;
