@@ -18,13 +18,12 @@
 // factors of the same 8 features alternate in m (the copy's box does that), so that a lane and the lane 8
 // further hold a and b of one feature.
 //
-// Persistent blocks of 20 warps: copies (TMA), products, a warp that passes on what has landed, one that
-// zeroes the rows behind the last expert's, and 16 that read tensor memory and write results while the next
+// Persistent blocks of 20 warps: copies (TMA), products, a warp that zeroes what weight gradients' last copies
+// bring of other experts, one that zeroes the rows behind the last expert's, and 16 that read tensor memory and write results while the next
 // tile runs in its other half.
 //
-// Every wait on a barrier ends: after WAIT_LIMIT polls it gives up, the block's roles stop, copies and
-// products in flight are waited for (with the same limit), tensor memory is freed and the status word is
-// set to ERC_ERR_TIMEOUT.
+// Every wait on a barrier ends: after TC_WAIT it gives up, the block's roles stop, copies and products in flight
+// are waited for (with limits), tensor memory is freed and the status word is set to ERC_ERR_TIMEOUT.
 #pragma once
 
 #include <cuda.h>
@@ -44,7 +43,8 @@ constexpr int TC_PART = 256 / (TC_EPILOGUE / 4);
 constexpr int TC_THREADS = 128 + 32 * TC_EPILOGUE;
 constexpr int TC_AHEAD = 1;
 constexpr int tc_cols(int which) { return which == FFN_DH ? 8 : 16; }  // columns that a lane holds at a time
-constexpr unsigned TC_WAIT_LIMIT = 1u << 22;
+constexpr uint64_t TC_WAIT = 20000000000ull;   // nanoseconds: the sum over the slots of one expert is a tile's longest wait
+constexpr uint64_t TC_COPIES = 2000000ull;     // far longer than copies take that are in flight
 
 __device__ __forceinline__ uint32_t smem_at(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
 __device__ __forceinline__ uint32_t cluster_rank() {
@@ -78,37 +78,59 @@ __device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
       : "memory");
   return done;
 }
+__device__ __forceinline__ uint64_t nanoseconds() {
+  uint64_t t;
+  asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
+  return t;
+}
+// polls a barrier, for `limit` nanoseconds at most; the clock is looked at every 256 polls
+__device__ __forceinline__ bool bar_poll(uint32_t bar, uint32_t parity, uint64_t limit, volatile int* failed) {
+  uint64_t start = 0;
+  for (unsigned i = 0; i < 0x7fffffffu; ++i) {
+    if (bar_try(bar, parity)) return true;
+    if (failed && *failed) return false;
+    if (i % 256 == 255) {
+      const uint64_t now = nanoseconds();
+      if (start == 0) start = now;
+      if (now - start > limit) return false;
+    }
+  }
+  return false;
+}
 // false when the wait ran out, here or in another role of the block
 __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile int* failed) {
-  for (unsigned i = 0; i < TC_WAIT_LIMIT; ++i) {
-    if (bar_try(bar, parity)) return true;
-    if (*failed) return false;
-  }
+  if (bar_poll(bar, parity, TC_WAIT, failed)) return true;
   *failed = 1;
   return false;
 }
-__device__ __forceinline__ void bar_drain(uint32_t bar, uint32_t parity) {
-  for (unsigned i = 0; i < TC_WAIT_LIMIT; ++i)
-    if (bar_try(bar, parity)) return;
-}
 
+// A box into this block's shared memory.  PAIR: `bar` is of either block of the pair (a cluster address), else of this one.
+template <bool PAIR>
 __device__ __forceinline__ void copy_2d(uint32_t dst, const CUtensorMap* map, uint32_t bar, int x, int y) {
-  asm volatile(
-      "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];" ::"r"(dst),
-      "l"(map), "r"(bar), "r"(x), "r"(y)
-      : "memory");
+  if constexpr (PAIR)
+    asm volatile(
+        "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], "
+        "[%2];" ::"r"(dst),
+        "l"(map), "r"(bar), "r"(x), "r"(y)
+        : "memory");
+  else
+    asm volatile(
+        "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];" ::"r"(
+            dst),
+        "l"(map), "r"(bar), "r"(x), "r"(y)
+        : "memory");
 }
 __device__ __forceinline__ void copy_3d(uint32_t dst, const CUtensorMap* map, uint32_t bar, int x, int y, int z) {
   asm volatile(
-      "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(
-          dst),
+      "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], "
+      "[%2];" ::"r"(dst),
       "l"(map), "r"(bar), "r"(x), "r"(y), "r"(z)
       : "memory");
 }
 __device__ __forceinline__ void copy_5d(uint32_t dst, const CUtensorMap* map, uint32_t bar, int a, int b, int c, int d, int e) {
   asm volatile(
-      "cp.async.bulk.tensor.5d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6, %7}], [%2];" ::
-          "r"(dst),
+      "cp.async.bulk.tensor.5d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, "
+      "%6, %7}], [%2];" ::"r"(dst),
       "l"(map), "r"(bar), "r"(a), "r"(b), "r"(c), "r"(d), "r"(e)
       : "memory");
 }
@@ -428,7 +450,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(TC_THREADS, 1)
   constexpr bool SLOTS = TcTiles<WHICH>::SLOTS;
   constexpr bool A_K = WHICH == FFN_IN || WHICH == FFN_OUT, B_K = SLOTS;
   extern __shared__ char raw[];
-  __shared__ __align__(8) uint64_t bars[3 * TC_STAGES + 5];
+  __shared__ __align__(8) uint64_t bars[3 * TC_STAGES + 6];
   __shared__ TcRanges of;
   __shared__ float cost_of[4];
   __shared__ uint32_t tmem_base;
@@ -437,18 +459,18 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(TC_THREADS, 1)
   const uint32_t rank = cluster_rank();
   const uint32_t stages = (smem_at(raw) + 1023) & ~1023u;
   const uint32_t bar0 = smem_at(bars);
-  auto land = [&](int s) { return bar0 + 8u * s; };                       // this block's copies of a stage
-  auto ready = [&](int s) { return bar0 + 8u * (TC_STAGES + s); };        // first block: both blocks' copies
+  auto land = [&](int s) { return bar0 + 8u * s; };                       // this block's copies of a stage with a ragged end
+  auto ready = [&](int s) { return bar0 + 8u * (TC_STAGES + s); };        // first block: both blocks' stages are complete
   auto empty = [&](int s) { return bar0 + 8u * (2 * TC_STAGES + s); };    // the products have read a stage
   auto full = [&](int a) { return bar0 + 8u * (3 * TC_STAGES + a); };     // a tile's sums are complete
   auto taken = [&](int a) { return bar0 + 8u * (3 * TC_STAGES + 2 + a); };  // first block: both have read them
-  const uint32_t done = bar0 + 8u * (3 * TC_STAGES + 4);
+  const uint32_t done = bar0 + 8u * (3 * TC_STAGES + 4), never = done + 8u;
 
   if (threadIdx.x == 0) {
     failed = 0;
     for (int s = 0; s < TC_STAGES; ++s) {
       bar_init(land(s), 1);
-      bar_init(ready(s), 2);
+      bar_init(ready(s), SLOTS ? 1 : 2);
       bar_init(empty(s), 1);
     }
     for (int a = 0; a < 2; ++a) {
@@ -456,6 +478,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(TC_THREADS, 1)
       bar_init(taken(a), 2 * TC_EPILOGUE);
     }
     bar_init(done, 1);
+    bar_init(never, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == 3) {
@@ -528,43 +551,54 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(TC_THREADS, 1)
   if (warp == 0) {
     if (lane == 0) {  // copies
       int s = 0;
-      uint32_t phase = 0, issued = 0;
+      uint32_t phase = 0;
       bool ok = true;
       for (int at = first; ok && at < total; at += step) {
         const TcTile t = tiles.at(at, of, p.experts);
         const int m = t.m0 + m_block, n_half = t.n / 2;
+        const uint32_t bytes = TC_OPERAND + (B_K ? TC_OPERAND : n_half * TC_K * 2);
         for (int b = 0; b < t.blocks; ++b) {
           if (!(ok = bar_wait(empty(s), phase ^ 1, &failed))) break;
-          const uint32_t dst = stages + s * TC_STAGE, bar = land(s);
+          const uint32_t dst = stages + s * TC_STAGE;
           const int k = b * TC_K;
-          bar_expect(bar, TC_OPERAND + (B_K ? TC_OPERAND : n_half * TC_K * 2));
-          if constexpr (WHICH == FFN_IN) {
-            copy_5d(dst, &map_a, bar, k, 0, 0, m / 16, t.expert);
-          } else if constexpr (WHICH == FFN_OUT) {
-            copy_3d(dst, &map_a, bar, k, m, t.expert);
-          } else if constexpr (SLOTS) {
-            copy_3d(dst, &map_a, bar, m, k, t.expert);
-            copy_3d(dst + 8192, &map_a, bar, m + 64, k, t.expert);
+          if constexpr (SLOTS) {
+            const uint32_t bar = peer_address(ready(s), 0);
+            if (rank == 0) bar_expect(ready(s), 2 * bytes);
+            if constexpr (WHICH == FFN_IN) {
+              copy_5d(dst, &map_a, bar, k, 0, 0, m / 16, t.expert);
+            } else if constexpr (WHICH == FFN_OUT) {
+              copy_3d(dst, &map_a, bar, k, m, t.expert);
+            } else {
+              copy_3d(dst, &map_a, bar, m, k, t.expert);
+              copy_3d(dst + 8192, &map_a, bar, m + 64, k, t.expert);
+            }
+            copy_2d<true>(dst + TC_OPERAND, &map_b, bar, k, (int)(t.n0 + rank * n_half));
           } else {
-            copy_2d(dst, &map_a, bar, m, (int)(t.k0 + k));
-            copy_2d(dst + 8192, &map_a, bar, m + 64, (int)(t.k0 + k));
+            // all but a ragged end go to the first block's barrier; that one is passed on when its rows are in order
+            const int n = (int)t.n0 + rank * n_half, row = (int)(t.k0 + k);
+            auto boxes = [&](auto pair, uint32_t bar) {
+              constexpr bool PAIR = decltype(pair)::value;
+              copy_2d<PAIR>(dst, &map_a, bar, m, row);
+              copy_2d<PAIR>(dst + 8192, &map_a, bar, m + 64, row);
+              copy_2d<PAIR>(dst + TC_OPERAND, &map_b, bar, n, row);
+              if (n_half > 64) copy_2d<PAIR>(dst + TC_OPERAND + 8192, &map_b, bar, n + 64, row);
+            };
+            if (t.k0 + k + TC_K > t.k1) {
+              bar_expect(land(s), bytes);
+              boxes(std::false_type(), land(s));
+            } else {
+              if (rank == 0) {
+                bar_expect(ready(s), 2 * bytes);
+                bar_arrive_cluster(peer_address(ready(s), 0));
+              }
+              boxes(std::true_type(), peer_address(ready(s), 0));
+            }
           }
-          if constexpr (B_K) {
-            copy_2d(dst + TC_OPERAND, &map_b, bar, k, (int)(t.n0 + rank * n_half));
-          } else {
-            const int n = (int)t.n0 + rank * n_half;
-            copy_2d(dst + TC_OPERAND, &map_b, bar, n, (int)(t.k0 + k));
-            if (n_half > 64) copy_2d(dst + TC_OPERAND + 8192, &map_b, bar, n + 64, (int)(t.k0 + k));
-          }
-          ++issued;
           if (++s == TC_STAGES) s = 0, phase ^= 1;
         }
       }
-      if (failed)  // copies in flight write shared memory: none may be left
-        for (int i = 0; i < TC_STAGES && issued > 0; ++i, --issued) {
-          if (s-- == 0) s = TC_STAGES - 1, phase ^= 1;
-          bar_drain(land(s), phase);
-        }
+      // copies in flight write shared memory, and none may be left: nothing arrives at this barrier, so this is a pause
+      if (failed) bar_poll(never, 0, TC_COPIES, nullptr);
     }
   } else if (warp == 1) {
     if (lane == 0 && rank == 0) {  // products
@@ -595,30 +629,32 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(TC_THREADS, 1)
       }
       if (failed) {
         commit_pair(done);
-        bar_drain(done, 0);
+        bar_poll(done, 0, TC_WAIT, nullptr);
       }
     }
-  } else if (warp == 2) {  // what has landed is passed on to the first block
-    int s = 0;
-    uint32_t phase = 0;
-    bool ok = true;
-    for (int at = first; ok && at < total; at += step) {
-      const TcTile t = tiles.at(at, of, p.experts);
-      for (int b = 0; b < t.blocks; ++b) {
-        if (!(ok = __all_sync(0xffffffffu, bar_wait(land(s), phase, &failed)))) break;
-        if (!SLOTS && t.k0 + (b + 1) * TC_K > t.k1) {
-          // the last slots of an expert: the rows of the box behind them belong to others
-          const int live = (int)(t.k1 - t.k0 - (int64_t)b * TC_K);
+  } else if (warp == 2) {
+    // the ends of weight gradients: the rows of a box behind an expert's last slots belong to others, and become zeros
+    if constexpr (!SLOTS) {
+      int s = 0;
+      uint32_t used = 0;  // bit s: the phase of land(s)
+      for (int at = first; at < total; at += step) {
+        const TcTile t = tiles.at(at, of, p.experts);
+        if (t.blocks == 0) continue;
+        s = (s + t.blocks - 1) % TC_STAGES;
+        const int live = (int)(t.k1 - t.k0 - (int64_t)(t.blocks - 1) * TC_K);
+        if (live < TC_K) {
+          if (!__all_sync(0xffffffffu, bar_wait(land(s), used >> s & 1, &failed))) break;
+          used ^= 1u << s;
           const uint32_t base = stages + s * TC_STAGE;
           const int boxes = t.n > 128 ? 4 : 3;
           for (int x = 0; x < boxes; ++x)
             for (int i = live * 8 + lane; i < 512; i += 32)
               asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(base + x * 8192 + i * 16), "r"(0) : "memory");
           asm volatile("fence.proxy.async.shared::cta;\nfence.acq_rel.cluster;" ::: "memory");
+          __syncwarp();
+          if (lane == 0) bar_arrive_cluster(peer_address(ready(s), 0));
         }
-        __syncwarp();
-        if (lane == 0) bar_arrive_cluster(peer_address(ready(s), 0));
-        if (++s == TC_STAGES) s = 0, phase ^= 1;
+        s = (s + 1) % TC_STAGES;
       }
     }
   } else if (warp == 3) {  // rows behind the last expert's
