@@ -434,7 +434,8 @@ erc_status erc_expert_combine_backward(int64_t rows, int32_t k, int64_t width, c
  * erc_score_rows_backward -- from dlogp and dentropy [rows] (either may be NULL: 0) to
  *      dlogits_i = ((i == id) dlogp - p_i (dlogp + dentropy (ln p_i + entropy))) / temperature,
  *      [rows x n] dense rows of `type`, rounded once; masked entries get 0.  norm and entropy are
- *      the forward call's (entropy and ids may be NULL when their gradient is).  An id outside
+ *      the forward call's (entropy and ids may be NULL when their gradient is); dlogits does not
+ *      overlap logits.  An id outside
  *      [0, n) or a masked one adds nothing; the alternatives have no gradient.
  * Errors: INVALID_ARG for sizes, types, pointers, a temperature or k out of range; CAPACITY if
  *      ws_bytes is too small.
@@ -467,7 +468,7 @@ erc_status erc_score_rows_backward(int64_t rows, int64_t n, const void* logits, 
  *      dw_in and dw_out (each may be NULL), rounded to `type` once; act(a) b and the gradients of a
  *      and b, formed from the rounded pre and float32 sums, are rounded once too.  dxs is zeroed from
  *      offsets[experts] on, the weights' gradients where an expert has no rows.  Contents of xs, pre
- *      and dy behind offsets[experts] do not matter.
+ *      and dy behind offsets[experts] do not matter.  No array that is written overlaps another.
  * Limits: width and inner in [1, ERC_FFN_MAX_WIDTH], experts in [1, ERC_ROUTE_MAX_EXPERTS], slots in
  *      [0, 2^31).  bfloat16 and float16 with width and inner that are multiples of 8 and 16-byte
  *      aligned arrays use the tensor cores, and so do many rows of other widths, by way of copies in the

@@ -5,6 +5,8 @@
 // A product is C(i, j) = sum_k A(i, k) B(j, k) in tiles of 64 or 128 rows and columns by a depth of 16, twice
 // buffered in shared memory.  A thread keeps 4 x 4 or 8 x 8 sums in registers, as groups of 4 rows and 4 columns 64
 // apart.  In IN the second group of columns holds the factors of the first one's features.  Sums run over k in order.
+// Bound by the float32 units and by the tiles' rounds: 8192 slots of 1024 x 1024 float32, 44 TFLOP/s forward and 38
+// backward (a library product: 45 and 50).
 #include <initializer_list>
 
 #include "expert_ffn.cuh"
@@ -328,7 +330,8 @@ bool whole_pieces(const erc_ffn_shape* f) {
   return f->width % piece == 0 && f->inner % piece == 0;
 }
 // Rows that are not whole pieces are copied into rows that are, for the tensor cores' sake, where that pays: the copies
-// cost some 20 us and three times the weights' bytes.
+// cost some 20 us and three times the weights' bytes.  8192 slots of 1021 x 1023 bfloat16: forward 1440 us on the float32
+// units, 104 this way; gradient 3750 and 216.
 bool worth_padding(const erc_ffn_shape* f) {
   return f->type != ERC_F32 && !whole_pieces(f) && f->slots >= 32 * (int64_t)f->experts &&
          (double)f->slots * f->width * f->inner >= 1e8;
@@ -341,7 +344,8 @@ FfnWay ffn_way(const erc_ffn_shape* f, uintptr_t all, bool forward) {
   return f->type == ERC_F32 ? FFN_SIMPLE : FFN_TENSOR;
 }
 
-// Parts of an expert's slots in a weight gradient of rows x cols: few tiles would leave most SMs idle over a long sum.
+// Parts of an expert's slots in a weight gradient of rows x cols: few tiles would leave most SMs idle over a long sum
+// (100000 slots of 32 x 64 bfloat16, the whole gradient: 986 us in one part, 126 in 64).
 int weight_splits(const erc_ffn_shape* f, int64_t rows, int64_t cols, bool tensor) {
   const int64_t side = tensor ? 256 : FM, most = tensor ? sm_count() / 2 : 2 * sm_count();
   const int64_t tiles = f->experts * ((rows + side - 1) / side) * ((cols + side - 1) / side);

@@ -5,6 +5,10 @@
 // a time.  A lane multiplies its 16-byte pieces of the weights with the slots' pieces (from L1), so 32 lanes end
 // with parts of up to 32 sums; halving steps leave sum i in lane i (31 shuffles for 32 sums).  OUT asks for its
 // weights while IN still runs, and waits for h only then.
+//
+// 14 slots over 8 experts of 512 x 1024 bf16 (16 MB of weights, 2.3 us of copying): IN 8.6 us, OUT 5.3; a call takes 19 to
+// 21, which is the binding's and the launches' time.  Both are latency: offsets, weights, slots and the halving steps
+// follow each other, and half the blocks have no slots.
 #include "expert_ffn.cuh"
 
 namespace erc {

@@ -19,8 +19,20 @@
 // further hold a and b of one feature.
 //
 // Persistent blocks of 20 warps: copies (TMA), products, a warp that zeroes what weight gradients' last copies
-// bring of other experts, one that zeroes the rows behind the last expert's, and 16 that read tensor memory and write results while the next
-// tile runs in its other half.
+// bring of other experts, one that zeroes the rows behind the last expert's, and 16 that read tensor memory and
+// write results while the next tile runs in its other half.
+//
+// Why this tile: a stage of 64 k brings a block 32 KB for 512 clocks of products, and an SM takes in about 64 bytes a
+// clock, so 256 x 256 a pair is where copies and products balance; with a quarter of the products left out 8192 x 2048
+// x 4096 still takes 0.77 of its time.  Two accumulators fill tensor memory.  What it reaches (8192 slots, one expert,
+// 2048 x 4096): IN 159 to 167 us, 1640 to 1730 TFLOP/s (0.87 to 0.91 of the measured burst rate); OUT 94 to 100 us,
+// 1370 to 1450, 256 tiles on 76 pairs being 3.4 rounds.  Experts of a few hundred slots are bound by memory and by the
+// rounds: 64 x 512 slots of 1024 x 512, IN 59 to 64 us, OUT 45.  DH also reads (a, b) and writes (da, db) and h, 0.9 GB for
+// 80000 slots of 1024: 198 us, 4.7 TB/s.
+//
+// What was tried and did not pay: asking for DH's rows ahead (prefetches into L2: 215 -> 240 us, by bulk requests 345;
+// reading two or three steps ahead: no change); 8 result warps instead of 16 (DH 209 instead of 200); passing every
+// stage on through a warp of each block (the same).  Releases at cluster scope on the way cost a microsecond a stage.
 //
 // Every wait on a barrier ends: after TC_WAIT it gives up, the block's roles stop, copies and products in flight
 // are waited for (with limits), tensor memory is freed and the status word is set to ERC_ERR_TIMEOUT.

@@ -12,7 +12,16 @@
 // that belongs are found the same way among all entries.
 //
 // Up to 8 parts are a cluster, whose first block joins them through distributed shared memory; more go
-// through a workspace and a second kernel.
+// through a workspace and a second kernel.  Short rows take 8 to 32 lanes each, rows by the thousand without best
+// entries a warp each, all in registers.
+//
+// What bounds them: an entry costs 3 to 4 instructions and one of the 16 exponentials an SM makes a clock, which is
+// 0.37 of the copy rate for bfloat16 rows if nothing else waits; a few long rows are latency (launch, copy, two
+// passes, the search, two cluster barriers).  Device time (us) and floor at 6767 GB/s:
+//   64 x 169343 bf16, 20 best  17.6 / 3.2, none 11.8 / 3.2; 1 x 20000 f32, 5 best 7.6, none 4.1; 16384 x 257 f32, none
+//   8.7 / 2.5, 32 best 28.5; 4096 x 20000 bf16, none 38.5 / 24.2; 8 x 2449029 f32, none 22 / 11.6, 32 best 45 / 11.6.
+// The gradient reads and writes each entry once: 4096 x 20000 bf16 52 to 55 us, 0.87 to 0.93 of the copy rate; rows whose
+// result is aligned otherwise than the scores (4096 x 19999) 69 us.
 #include "choice.cuh"
 
 namespace erc {
@@ -551,6 +560,51 @@ __global__ void __launch_bounds__(ST) k_score_join(int64_t rows, int64_t n, cons
   }
 }
 
+// A warp takes a row of any length, 8 vectors a lane in flight, without a barrier: a higher maximum settles what was
+// summed below the one before.  No best entries.
+template <class T>
+__global__ void __launch_bounds__(ST, 4) k_score_stream(int64_t rows, int64_t n, const T* __restrict__ logits, int64_t stride,
+                                                        ScoreOut o) {
+  constexpr int V = 8;
+  const int lane = threadIdx.x & 31;
+  for (int64_t row = ((int64_t)blockIdx.x * ST + threadIdx.x) >> 5; row < rows; row += (int64_t)gridDim.x * SW) {
+    const T* x = logits + row * stride;
+    const RowView<T> view(x, n);
+    Given g = {-1, 0.f};
+    if (lane == 0) g = given_of(o, row, x, n);
+    Sum a = {LOWEST, 0.f, 0.f};  // what was settled
+    Scale scale(LOWEST, o.c);
+    Terms terms;
+    for (int v0 = 0; v0 < view.vectors; v0 += 32 * V) {
+      uint4 v[V];
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        const int at = v0 + j * 32 + lane;
+        v[j] = at < view.vectors ? view.fetch(at)
+                                 : make_uint4(masked_word<T>(), masked_word<T>(), masked_word<T>(), masked_word<T>());
+      }
+      float m = scale.m;
+#pragma unroll
+      for (int j = 0; j < V; ++j) m = fmaxf(m, max_score(v[j], T()));
+      m = warp_max(m);
+      if (m > scale.m) {
+        const Sum s = settle(sum_of(terms, scale.m), scale);
+        a.T += s.T;
+        a.u += s.u;
+        raise(a, m, o.c);
+        scale = Scale(m, o.c);
+        terms = Terms();
+      }
+#pragma unroll
+      for (int j = 0; j < V; ++j) add_vector<T>(terms, v[j], scale);
+    }
+    const Sum s = settle(sum_of(terms, scale.m), scale);
+    a.T = warp_sum(a.T + s.T);
+    a.u = warp_sum(a.u + s.u);
+    if (lane == 0) finish_row(o, row, g, a);
+  }
+}
+
 // a row as whole aligned vectors, and the few entries before and behind them
 template <class T>
 struct ShortRow {
@@ -751,7 +805,8 @@ __device__ __forceinline__ uint4 shifted(uint4 a, uint4 b, int by) {
 
 // WARPS warps (a block, or one) take `each` vectors of a row's result, SV steps of 31 WARPS or 32 WARPS at a time.  Where the result's rows are aligned otherwise than
 // the scores', a result vector is two neighbouring lanes' shifted together, and 32 lanes give 31.
-// SHIFT: some rows may be aligned otherwise.
+// SHIFT: some rows may be aligned otherwise (71 registers and not 48, so it is left out where none can be: 63 -> 55 us for
+// 4096 x 20000 bf16).
 template <class T, int WARPS, bool SHIFT>
 __global__ void __launch_bounds__(ST, SHIFT ? 4 : 5) k_score_backward(int64_t rows, int64_t n, const T* __restrict__ logits, int64_t stride,
                                                        int parts, int each, ScoreGrad o, T* __restrict__ dlogits) {
@@ -862,6 +917,10 @@ Split split_rows(int64_t rows, int64_t n, int32_t type) {
   const int64_t each = (segments + parts - 1) / parts;
   return {(int)((segments + each - 1) / each), (int)each * 32};
 }
+// Rows enough to keep the machine busy with a warp each.  A warp a row against a block a row (us, k 0): 10000 x 5001 float16
+// 32 / 39, 4096 x 20001 float32 69 / 79, 3000 x 3000 bfloat16 9.4 / 12.2; fewer rows leave SMs without loads in flight:
+// 2500 x 20000 bfloat16 29.6 / 27.3, 1900 x 20000 25.6 / 21.9.
+bool many_rows(int64_t rows) { return rows >= (int64_t)sm_count() * 18; }
 bool short_rows(int64_t n, int32_t type) { return n / (16 / type_bytes(type)) <= 32 * 8; }
 
 erc_status check_scores(int64_t rows, int64_t n, int32_t type, int64_t stride) {
@@ -891,7 +950,7 @@ extern "C" size_t erc_score_rows_workspace_size(int64_t rows, int64_t n, int32_t
       k < 0 || k > ERC_SCORE_MAX_K || short_rows(n, type))
     return 0;
   const Split sp = split_rows(rows, n, type);
-  if (sp.parts <= CLUSTER) return 0;
+  if (sp.parts <= CLUSTER || (k == 0 && many_rows(rows))) return 0;
   Arena a(nullptr);
   ScorePlan p;
   plan_scores(a, p, rows, sp.parts, k);
@@ -914,8 +973,9 @@ extern "C" erc_status erc_score_rows(int64_t rows, int64_t n, const void* logits
   const cudaStream_t s = as_stream(stream);
   const bool brief = short_rows(n, type);
   const Split sp = brief ? Split{1, 0} : split_rows(rows, n, type);
+  const bool stream_rows = !brief && k == 0 && many_rows(rows);
   ScorePlan p = {};
-  if (sp.parts > CLUSTER) {
+  if (sp.parts > CLUSTER && !stream_rows) {
     if (!ws || ws_bytes < erc_score_rows_workspace_size(rows, n, type, k))
       return set_error(ERC_ERR_CAPACITY, "workspace too small");
     Arena ar(reinterpret_cast<void*>((reinterpret_cast<uintptr_t>(ws) + 255) & ~uintptr_t(255)));
@@ -948,6 +1008,10 @@ extern "C" erc_status erc_score_rows(int64_t rows, int64_t n, const void* logits
         launch(k_score_short<T, 16, 8, false>, 16);
       else
         launch(k_score_short<T, 32, 8, false>, 32);
+      count_launches(1);
+    } else if (stream_rows) {
+      const int64_t blocks = (rows + SW - 1) / SW, most = (int64_t)sm_count() * 64;
+      k_score_stream<T><<<(unsigned)(blocks < most ? blocks : most), ST, 0, s>>>(rows, n, x, stride, o);
       count_launches(1);
     } else {
       const int smem = part_smem(sp.per, k > 0);
