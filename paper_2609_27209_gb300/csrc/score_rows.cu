@@ -29,7 +29,7 @@ namespace {
 
 constexpr int ST = 256;          // threads of a block
 constexpr int SW = ST / 32;      // its warps
-constexpr int SV = 4;            // vectors a thread holds at a time
+constexpr int SV = 4;            // vectors a lane holds at a time in the gradient
 constexpr int SEGS = 96;         // segments of a block's part of a row, at most
 constexpr int MAX_PARTS = 512;   // parts of a row, at most
 constexpr int CLUSTER = 8;       // parts that a cluster joins, at most
@@ -390,7 +390,7 @@ __global__ void __launch_bounds__(ST) k_score_part(int64_t rows, int64_t n, cons
                                                    int parts, int per, ScoreOut o, Sum* __restrict__ sums,
                                                    Best* __restrict__ best) {
   constexpr int N = ScoreVec<T>::N;
-    __shared__ Sum part[SW];
+  __shared__ Sum part[SW];
   __shared__ Sum joined;
   __shared__ float top_of[SW];
   __shared__ Best kept[KMAX];
