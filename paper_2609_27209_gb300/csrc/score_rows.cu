@@ -1,10 +1,10 @@
 // score_rows.cu -- log probability of a given entry of each row of scores, the row's entropy and its
 // best entries, and the scores' gradient.
 //
-// With c = log2(e) / temperature, m the largest score and t = (l - m) c, T = sum 2^t and u = sum 2^t t
-// give ln Z = ln T and the entropy ln T - ln2 u / T.  A part of a row (at most 48 KB) arrives in shared
+// With c = log2(e) / temperature, m the largest score and t = (l - m) c, Z = sum 2^t and u = sum 2^t t
+// give ln Z and the entropy ln Z - ln2 u / Z.  A part of a row (at most 48 KB) arrives in shared
 // memory by one asynchronous copy; a first pass finds its maximum, a second its sums, so an entry costs one
-// exponential and no part scales its sums.  Parts join by d = (m_part - m) c: u <- 2^d (u + d T), T <- 2^d T.
+// exponential and no part scales its sums.  Parts join by d = (m_part - m) c: u <- 2^d (u + d Z), Z <- 2^d Z.
 // t is kept above -1000, where 2^t is 0, so that no product of 0 and infinity appears.
 //
 // The best entries: the k-th largest of the threads' maxima, found by halving, bounds the k-th best entry from
@@ -47,28 +47,35 @@ __device__ __forceinline__ float scaled(float l, float m, float c) {
   return l == m ? 0.f : fmaxf((l - m) * c, -1000.f);
 }
 
+// Entries met so far: `top` of them equal the largest, m (LOWEST where nothing was met); X is the sum of 2^t and u that of
+// 2^t t over the others.  Z = top + X: kept apart, so that ln Z, which is X where one entry has nearly all of
+// the probability, keeps its relative accuracy.
 struct Sum {
-  float m, T, u;  // m: LOWEST where nothing was met (T = 0)
+  float m, X, u, top;
 };
+__device__ __forceinline__ float log_sum(const Sum& a) { return a.top > 0.f ? log1pf(a.X + (a.top - 1.f)) : -INFINITY; }
 __device__ __forceinline__ void raise(Sum& a, float m, float c) {
-  const float d = scaled(a.m, m, c), f = exp2_fast(d);
-  a.u = f * fmaf(d, a.T, a.u);
-  a.T *= f;
+  if (a.m == m) return;
+  const float d = scaled(a.m, m, c), f = exp2_fast(d), Z = a.X + a.top;
+  a.u = f * fmaf(d, Z, a.u);
+  a.X = f * Z;
+  a.top = 0.f;
   a.m = m;
 }
 __device__ __forceinline__ Sum join(Sum a, Sum b, float c) {
   const float m = fmaxf(a.m, b.m);
   raise(a, m, c);
   raise(b, m, c);
-  return {m, a.T + b.T, a.u + b.u};
+  return {m, a.X + b.X, a.u + b.u, a.top + b.top};
+}
+__device__ __forceinline__ Sum from_lane(const Sum& a, int lane) {
+  return {__shfl_sync(0xffffffffu, a.m, lane), __shfl_sync(0xffffffffu, a.X, lane), __shfl_sync(0xffffffffu, a.u, lane),
+          __shfl_sync(0xffffffffu, a.top, lane)};
 }
 // the parts of `width` neighbouring lanes joined
 __device__ __forceinline__ Sum lane_join(Sum a, float c, int width) {
-  for (int o = width / 2; o; o >>= 1) {
-    const Sum b = {__shfl_xor_sync(0xffffffffu, a.m, o), __shfl_xor_sync(0xffffffffu, a.T, o),
-                   __shfl_xor_sync(0xffffffffu, a.u, o)};
-    a = join(a, b, c);  // the same on both sides: sums and maxima commute
-  }
+  for (int o = width / 2; o; o >>= 1)
+    a = join(a, from_lane(a, (threadIdx.x & 31) ^ o), c);  // the same on both sides: sums and maxima commute
   return a;
 }
 // the largest score of a warp, and a sum over it
@@ -82,8 +89,7 @@ __device__ __forceinline__ float warp_sum(float v) {
 }
 
 // The terms of entries whose maximum m is known.  t = l c - fl(m c) is one fma, for two entries at once; the
-// rounding of m c moves every t by the same d = m c - fl(m c) (t is d at the maximum), which `settle` takes out
-// again.  Masked entries and NaN are raised to `low`, about 1000 / c below m, where 2^t is 0: one maximum of the
+// rounding of m c moves every t by the same d = m c - fl(m c), which `settle` takes out again.  Masked entries and NaN are raised to `low`, about 1000 / c below m, where 2^t is 0: one maximum of the
 // stored type.  Rows where that does not hold (a maximum or a scale that is infinite, far from 0 or out of the type's
 // range) take the terms one by one.
 struct Scale {
@@ -120,12 +126,23 @@ __device__ __forceinline__ void raised_pairs(uint4 v, float low, uint64_t* p, __
   }
 }
 struct Terms {
-  uint64_t T = 0, u = 0;  // two sums each
+  uint64_t X = 0, u = 0;  // two sums each
+  float top = 0.f;
 };
+// one entry, which may be a largest one; masked: -inf
+__device__ __forceinline__ void add_entry(Terms& a, float l, const Scale& s) {
+  const bool largest = l == s.m;
+  const float t = s.plain ? fmaf(fmaxf(l, s.low), s.c, s.minus_mc) : scaled(l, s.m, s.c);
+  const float e = largest ? 0.f : exp2_fast(t);
+  a.top += largest ? 1.f : 0.f;
+  a.X = add2(a.X, pair(e, 0.f));
+  a.u = fma2(pair(e, 0.f), pair(t, 0.f), a.u);
+}
+// holds_top: a largest entry may be among them
 template <class T>
-__device__ __forceinline__ void add_vector(Terms& a, uint4 v, const Scale& s) {
+__device__ __forceinline__ void add_vector(Terms& a, uint4 v, const Scale& s, bool holds_top) {
   constexpr int P = ScoreVec<T>::N / 2;
-  if (s.plain) {
+  if (s.plain && !holds_top) {
     uint64_t l[P];
     raised_pairs(v, s.low, l, T());
 #pragma unroll
@@ -134,46 +151,27 @@ __device__ __forceinline__ void add_vector(Terms& a, uint4 v, const Scale& s) {
       float t0, t1;
       unpair(t, t0, t1);
       const uint64_t e = pair(exp2_fast(t0), exp2_fast(t1));
-      a.T = add2(a.T, e);
+      a.X = add2(a.X, e);
       a.u = fma2(e, t, a.u);
     }
   } else {
     float l[2 * P];
     unpack_scores(v, l, T());
 #pragma unroll
-    for (int i = 0; i < P; ++i) {
-      const float t0 = scaled(l[2 * i], s.m, s.c), t1 = scaled(l[2 * i + 1], s.m, s.c);
-      const uint64_t e = pair(exp2_fast(t0), exp2_fast(t1));
-      a.T = add2(a.T, e);
-      a.u = fma2(e, pair(t0, t1), a.u);
-    }
+    for (int i = 0; i < 2 * P; ++i) add_entry(a, l[i], s);
   }
 }
-// the terms of two entries, masked ones -inf
-__device__ __forceinline__ void add_pair(Terms& a, float l0, float l1, const Scale& s) {
-  float t0, t1;
-  if (s.plain) {
-    t0 = fmaf(fmaxf(l0, s.low), s.c, s.minus_mc);
-    t1 = fmaf(fmaxf(l1, s.low), s.c, s.minus_mc);
-  } else {
-    t0 = scaled(l0, s.m, s.c);
-    t1 = scaled(l1, s.m, s.c);
-  }
-  const uint64_t e = pair(exp2_fast(t0), exp2_fast(t1));
-  a.T = add2(a.T, e);
-  a.u = fma2(e, pair(t0, t1), a.u);
-}
-// the sums over a warp's or a group's lanes, with d taken out: 2^-d (T, u - d T)
+// the sums of a lane, or of several, with d taken out: 2^-d (X, u - d X)
 __device__ __forceinline__ Sum settle(Sum a, const Scale& s) {
   if (!s.plain) return a;
   const float d = fmaf(s.m, s.c, s.minus_mc), f = exp2_fast(-d);
-  return {a.m, f * a.T, f * fmaf(-d, a.T, a.u)};
+  return {a.m, f * a.X, f * fmaf(-d, a.X, a.u), a.top};
 }
 __device__ __forceinline__ Sum sum_of(const Terms& a, float m) {
-  float T0, T1, u0, u1;
-  unpair(a.T, T0, T1);
+  float X0, X1, u0, u1;
+  unpair(a.X, X0, X1);
   unpair(a.u, u0, u1);
-  return {m, T0 + T1, u0 + u1};
+  return {m, X0 + X1, u0 + u1, a.top};
 }
 
 struct ScoreOut {
@@ -187,8 +185,8 @@ struct ScoreOut {
   int k;
 };
 
-__device__ __forceinline__ float log_p(float l, float m, float lnT, float temperature) {
-  return l == -INFINITY ? -INFINITY : (l == m ? 0.f : __fdiv_rn(l - m, temperature)) - lnT;
+__device__ __forceinline__ float log_p(float l, float m, float lnZ, float temperature) {
+  return l == -INFINITY ? -INFINITY : (l == m ? 0.f : __fdiv_rn(l - m, temperature)) - lnZ;
 }
 
 // a row's id, and its score (read before the sums are known)
@@ -206,14 +204,14 @@ __device__ __forceinline__ Given given_of(const ScoreOut& o, int64_t row, const 
   return g;
 }
 __device__ __forceinline__ void finish_row(const ScoreOut& o, int64_t row, Given g, Sum a) {
-  const bool some = !(a.T <= 0.f);  // NaN: a copy that did not land
-  const float lnT = some ? logf(a.T) : -INFINITY, entropy = some ? lnT - LN2 * (a.u / a.T) : 0.f;
+  const bool some = !(a.top <= 0.f);  // NaN: a copy that did not land
+  const float lnZ = some ? log1pf(a.X + (a.top - 1.f)) : -INFINITY, entropy = some ? lnZ - LN2 * (a.u / (a.X + a.top)) : 0.f;
   if (o.entropy) o.entropy[row] = entropy < 0.f ? 0.f : entropy;
   if (o.norm) {
     o.norm[2 * row] = some ? a.m : -INFINITY;
-    o.norm[2 * row + 1] = lnT;
+    o.norm[2 * row + 1] = lnZ;
   }
-  if (o.logp) o.logp[row] = g.id < 0 ? 0.f : some ? log_p(g.l, a.m, lnT, o.temperature) : -INFINITY;
+  if (o.logp) o.logp[row] = g.id < 0 ? 0.f : some ? log_p(g.l, a.m, lnZ, o.temperature) : -INFINITY;
 }
 
 // an entry of a row's part in the workspace
@@ -335,21 +333,22 @@ __device__ __forceinline__ void block_top(TopScratch& s, unsigned mine, int k, E
   __syncthreads();
 }
 
-__device__ __forceinline__ void put_best(const ScoreOut& o, int64_t row, Sum a, float lnT, int rank, unsigned key,
+__device__ __forceinline__ void put_best(const ScoreOut& o, int64_t row, Sum a, float lnZ, int rank, unsigned key,
                                          unsigned id) {
   o.top_ids[row * o.k + rank] = key ? (int32_t)id : -1;
-  o.top_logp[row * o.k + rank] = key ? log_p(order_value(key), a.m, lnT, o.temperature) : -INFINITY;
+  o.top_logp[row * o.k + rank] = key ? log_p(order_value(key), a.m, lnZ, o.temperature) : -INFINITY;
 }
 
 // the sums of a block whose threads share a maximum, in the order of its warps
 __device__ __forceinline__ Sum block_sum(Sum a, Sum* part) {
-  a.T = warp_sum(a.T);
+  a.X = warp_sum(a.X);
   a.u = warp_sum(a.u);
+  a.top = warp_sum(a.top);
   if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = a;
   __syncthreads();
   Sum all = part[0];
 #pragma unroll
-  for (int w = 1; w < SW; ++w) all.T += part[w].T, all.u += part[w].u;
+  for (int w = 1; w < SW; ++w) all.X += part[w].X, all.u += part[w].u, all.top += part[w].top;
   return all;
 }
 
@@ -443,20 +442,20 @@ __global__ void __launch_bounds__(ST) k_score_part(int64_t rows, int64_t n, cons
     float m = -INFINITY;
     for (int at = tid; at < count; at += ST) m = fmaxf(m, max_score(held[at], T()));
     const unsigned mine = order_key(__fadd_rn(m, 0.f));
-    m = fmaxf(m, LOWEST);
-    m = warp_max(m);
+    const float own = m;
+    m = warp_max(fmaxf(m, LOWEST));
     if (lane == 0) top_of[warp] = m;
     __syncthreads();
 #pragma unroll
     for (int w = 0; w < SW; ++w) m = fmaxf(m, top_of[w]);
     const Scale scale(m, o.c);
     Terms terms;
-    for (int at = tid; at < count; at += ST) add_vector<T>(terms, held[at], scale);
+    for (int at = tid; at < count; at += ST) add_vector<T>(terms, held[at], scale, own == m);
     Sum a = settle(block_sum(sum_of(terms, m), part), scale);
-    if (!ok) a = {NAN, NAN, NAN};
+    if (!ok) a = {NAN, NAN, NAN, NAN};
     if (TOP) {
       const bool alone = !CLUSTERED && parts == 1;
-      const float lnT = alone && a.T > 0.f ? logf(a.T) : -INFINITY;
+      const float lnZ = alone ? log_sum(a) : 0.f;
       block_top(
           top, mine, o.k,
           [&](unsigned least, auto&& f) {
@@ -473,7 +472,7 @@ __global__ void __launch_bounds__(ST) k_score_part(int64_t rows, int64_t n, cons
             if (CLUSTERED)
               kept[rank] = {key, id};
             else if (alone)
-              put_best(o, row, a, lnT, rank, key, id);
+              put_best(o, row, a, lnZ, rank, key, id);
             else
               best[task * o.k + rank] = {key, id};
           });
@@ -482,16 +481,16 @@ __global__ void __launch_bounds__(ST) k_score_part(int64_t rows, int64_t n, cons
       if (tid == 0) joined = a;
       cluster_sync_all();
       if (which == 0) {
-        Sum all = {LOWEST, 0.f, 0.f};
+        Sum all = {LOWEST, 0.f, 0.f, 0.f};
         if (lane < parts) {
           const uint32_t at = of_block(shared_at(&joined), lane);
-          all = {__uint_as_float(peer_word(at)), __uint_as_float(peer_word(at + 4)), __uint_as_float(peer_word(at + 8))};
+          all = {__uint_as_float(peer_word(at)), __uint_as_float(peer_word(at + 4)), __uint_as_float(peer_word(at + 8)),
+                 __uint_as_float(peer_word(at + 12))};
         }
-        all = lane_join(all, o.c, CLUSTER);
-        all = {__shfl_sync(0xffffffffu, all.m, 0), __shfl_sync(0xffffffffu, all.T, 0), __shfl_sync(0xffffffffu, all.u, 0)};
+        all = from_lane(lane_join(all, o.c, CLUSTER), 0);
         if (tid == 0) finish_row(o, row, g, all);
         if (TOP) {
-          const float lnT = all.T > 0.f ? logf(all.T) : -INFINITY;
+          const float lnZ = log_sum(all);
           Best one = {0u, 0u};  // parts * k entries, at most one a thread
           if (tid < parts * o.k) {
             const uint32_t at = of_block(shared_at(&kept[tid % o.k]), tid / o.k);
@@ -499,7 +498,7 @@ __global__ void __launch_bounds__(ST) k_score_part(int64_t rows, int64_t n, cons
           }
           block_top(
               top, one.key, o.k, [&](unsigned, auto&& f) { f(one.key, one.id); },
-              [&](int rank, unsigned key, unsigned id) { put_best(o, row, all, lnT, rank, key, id); });
+              [&](int rank, unsigned key, unsigned id) { put_best(o, row, all, lnZ, rank, key, id); });
         }
       }
       cluster_sync_all();
@@ -526,7 +525,7 @@ __global__ void __launch_bounds__(ST) k_score_join(int64_t rows, int64_t n, cons
   for (int64_t row = blockIdx.x; row < rows; row += gridDim.x) {
     Given g = {-1, 0.f};
     if (threadIdx.x == 0) g = given_of(o, row, logits + row * stride, n);
-    Sum a = {LOWEST, 0.f, 0.f};
+    Sum a = {LOWEST, 0.f, 0.f, 0.f};
     for (int p = threadIdx.x; p < parts; p += ST) a = join(a, sums[row * parts + p], o.c);
     a = lane_join(a, o.c, 32);
     if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = a;
@@ -536,7 +535,7 @@ __global__ void __launch_bounds__(ST) k_score_join(int64_t rows, int64_t n, cons
     for (int w = 1; w < SW; ++w) a = join(a, part[w], o.c);
     if (threadIdx.x == 0) finish_row(o, row, g, a);
     if (TOP) {
-      const float lnT = a.T > 0.f ? logf(a.T) : -INFINITY;
+      const float lnZ = log_sum(a);
       // the parts' best first, then their second best, ..: a thread's largest is some part's best, or nearly so
       const Best* from = best + row * parts * o.k;
       auto nth = [&](int i) { return from[i % parts * o.k + i / parts]; };
@@ -554,7 +553,7 @@ __global__ void __launch_bounds__(ST) k_score_join(int64_t rows, int64_t n, cons
               for (int j = 0; j < 8; ++j) f(b[j].key, b[j].id);
             }
           },
-          [&](int rank, unsigned key, unsigned id) { put_best(o, row, a, lnT, rank, key, id); });
+          [&](int rank, unsigned key, unsigned id) { put_best(o, row, a, lnZ, rank, key, id); });
     }
     __syncthreads();
   }
@@ -572,7 +571,7 @@ __global__ void __launch_bounds__(ST, 4) k_score_stream(int64_t rows, int64_t n,
     const RowView<T> view(x, n);
     Given g = {-1, 0.f};
     if (lane == 0) g = given_of(o, row, x, n);
-    Sum a = {LOWEST, 0.f, 0.f};  // what was settled
+    Sum a = {LOWEST, 0.f, 0.f, 0.f};  // what was settled
     Scale scale(LOWEST, o.c);
     Terms terms;
     for (int v0 = 0; v0 < view.vectors; v0 += 32 * V) {
@@ -583,24 +582,27 @@ __global__ void __launch_bounds__(ST, 4) k_score_stream(int64_t rows, int64_t n,
         v[j] = at < view.vectors ? view.fetch(at)
                                  : make_uint4(masked_word<T>(), masked_word<T>(), masked_word<T>(), masked_word<T>());
       }
-      float m = scale.m;
+      float m = scale.m, best[V];
 #pragma unroll
-      for (int j = 0; j < V; ++j) m = fmaxf(m, max_score(v[j], T()));
+      for (int j = 0; j < V; ++j) {
+        best[j] = max_score(v[j], T());
+        m = fmaxf(m, best[j]);
+      }
       m = warp_max(m);
       if (m > scale.m) {
         const Sum s = settle(sum_of(terms, scale.m), scale);
-        a.T += s.T;
-        a.u += s.u;
+        a = {scale.m, a.X + s.X, a.u + s.u, a.top + s.top};
         raise(a, m, o.c);
         scale = Scale(m, o.c);
         terms = Terms();
       }
 #pragma unroll
-      for (int j = 0; j < V; ++j) add_vector<T>(terms, v[j], scale);
+      for (int j = 0; j < V; ++j) add_vector<T>(terms, v[j], scale, best[j] == m);
     }
     const Sum s = settle(sum_of(terms, scale.m), scale);
-    a.T = warp_sum(a.T + s.T);
+    a.X = warp_sum(a.X + s.X);
     a.u = warp_sum(a.u + s.u);
+    a.top = warp_sum(a.top + s.top);
     if (lane == 0) finish_row(o, row, g, a);
   }
 }
@@ -649,21 +651,26 @@ __global__ void __launch_bounds__(ST, TOP ? 3 : 4) k_score_short(int64_t rows, i
     const float tail = at0 < view.tail ? clean_score(to_f32(x[view.tail_at + at0])) : -INFINITY;
     Given g = {-1, 0.f};
     if (at0 == 0) g = given_of(o, row, x, n);
-    float m = fmaxf(fmaxf(head, tail), LOWEST);
+    float m = fmaxf(fmaxf(head, tail), LOWEST), peak[VPL];
 #pragma unroll
-    for (int j = 0; j < VPL; ++j) m = fmaxf(m, max_score(v[j], T()));
+    for (int j = 0; j < VPL; ++j) {
+      peak[j] = max_score(v[j], T());
+      m = fmaxf(m, peak[j]);
+    }
 #pragma unroll
     for (int w = LANES / 2; w; w >>= 1) m = fmaxf(m, __shfl_xor_sync(ALL, m, w));
     const Scale scale(m, o.c);
     Terms terms;
 #pragma unroll
-    for (int j = 0; j < VPL; ++j) add_vector<T>(terms, v[j], scale);
-    add_pair(terms, head, tail, scale);
+    for (int j = 0; j < VPL; ++j) add_vector<T>(terms, v[j], scale, peak[j] == m);
+    add_entry(terms, head, scale);
+    add_entry(terms, tail, scale);
     Sum a = sum_of(terms, m);
 #pragma unroll
     for (int w = LANES / 2; w; w >>= 1) {
-      a.T += __shfl_xor_sync(ALL, a.T, w);
+      a.X += __shfl_xor_sync(ALL, a.X, w);
       a.u += __shfl_xor_sync(ALL, a.u, w);
+      a.top += __shfl_xor_sync(ALL, a.top, w);
     }
     a = settle(a, scale);
     if (at0 == 0 && mine) finish_row(o, row, g, a);
@@ -671,7 +678,7 @@ __global__ void __launch_bounds__(ST, TOP ? 3 : 4) k_score_short(int64_t rows, i
       // a vector is as good as its best entry; short rows have too few vectors and take every entry
       constexpr bool ENTRIES = VPL <= 2;
       constexpr int UNITS = (ENTRIES ? VPL * N : VPL) + 2;
-      const float lnT = a.T > 0.f ? logf(a.T) : -INFINITY;
+      const float lnZ = log_sum(a);
       const unsigned hk = order_key(head), tk = order_key(tail);
       unsigned unit[UNITS];
 #pragma unroll
@@ -713,9 +720,9 @@ __global__ void __launch_bounds__(ST, TOP ? 3 : 4) k_score_short(int64_t rows, i
           const Best b = list[warp][i];
           int before = 0;
           for (int j = 0; j < many; ++j) before += ahead(list[warp][j].key, list[warp][j].id, b.key, b.id);
-          if (before < o.k && mine) put_best(o, row, a, lnT, before, b.key, b.id);
+          if (before < o.k && mine) put_best(o, row, a, lnZ, before, b.key, b.id);
         }
-        if (lane >= many && lane < o.k && mine) put_best(o, row, a, lnT, lane, 0u, 0u);
+        if (lane >= many && lane < o.k && mine) put_best(o, row, a, lnZ, lane, 0u, 0u);
       } else {  // many equal ones: the best that are left, one after another
         unsigned pk = ALL, pi = 0;
         for (int r = 0; r < o.k; ++r) {
@@ -734,7 +741,7 @@ __global__ void __launch_bounds__(ST, TOP ? 3 : 4) k_score_short(int64_t rows, i
           better(tk, (unsigned)(view.tail_at + lane));
           pk = __reduce_max_sync(ALL, bk);
           pi = __reduce_min_sync(ALL, bk == pk ? bi : ALL);
-          if (lane == 0 && mine) put_best(o, row, a, lnT, r, pk, pi);
+          if (lane == 0 && mine) put_best(o, row, a, lnZ, r, pk, pi);
         }
       }
     }
@@ -760,9 +767,9 @@ struct RowGrad {
   __device__ __forceinline__ float one(float l, int i) const {
     if (l == -INFINITY) return 0.f;
     const float t = scaled(l, scale.m, scale.c), lp = fmaf(t, LN2, -lnZ);
-    float v = -exp2_fast(fmaf(lnZ, -LOG2E, t)) * fmaf(gh, lp + H, g);
-    if (i == id) v += g;
-    return v * inv;
+    const float p = exp2_fast(fmaf(lnZ, -LOG2E, t));
+    // at the given entry g (1 - p) = -g (e^lp - 1), which does not cancel where p is near 1
+    return i == id ? inv * fmaf(-g, expm1f(lp), -p * gh * (lp + H)) : inv * (-p * fmaf(gh, lp + H, g));
   }
 };
 template <class T>

@@ -148,6 +148,36 @@ def test_the_longest_row():
     assert abs(logp.item() - want[0]) <= 2 * SUM + 32 * U * 20 and abs(entropy.item() - want[1]) <= 2 * SUM * 16 + 32 * U * 20
 
 
+@pytest.mark.parametrize("rows,n", [(3, 50), (3, 260), (3, 1000), (3, 9001), (3, 120001), (3000, 3001)])
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+def test_rows_with_one_sure_entry_keep_their_relative_accuracy(rows, n, kind):
+    """ln Z and 1 - p come from the sum without the largest entry, not from a number next to 1."""
+    rng = np.random.default_rng(n)
+    lead = rng.choice([5.0, 15.0, 25.0], rows)
+    x = torch.from_numpy(rng.normal(size=(rows, n)).astype(np.float32)).to(TYPES[kind])
+    best = torch.from_numpy(rng.integers(0, n, rows))
+    x[torch.arange(rows), best] = x.amax(1) + torch.from_numpy(lead).to(TYPES[kind])
+    logits, ids = x.to(dev()), best.to(torch.int32).to(dev())
+    logp, entropy, norm, _, top = erc.erc_score_rows(logits, ids, k=0 if rows > 100 else 1)
+    one, zero = torch.ones(rows, device=dev()), torch.zeros(rows, device=dev())
+    grad = erc.erc_score_rows_backward(logits, ids, norm, one, entropy, zero)
+    for r in range(0, rows, max(1, rows // 5)):
+        l = f32(logits[r]).astype(np.float64)
+        t = np.delete(l, best[r].item()) - l.max()
+        rest = np.exp(t).sum()
+        # as SUM, and every t within 4 U |t| of its value
+        bound = SUM + 4 * U * np.abs(t).max() + 16 * U
+        assert abs(logp[r].item() + np.log1p(rest)) <= bound * rest
+        assert top is None or top[r, 0].item() == logp[r].item()
+        want = np.log1p(rest) - (np.exp(t) * t).sum() / (1 + rest)
+        assert abs(entropy[r].item() - want) <= 2 * bound * want
+        g = grad[r].double().cpu().numpy()
+        half = half_ulp(TYPES[kind])
+        assert abs(g[best[r].item()] - rest / (1 + rest)) <= (bound + half) * rest
+        others = -np.exp(t) / (1 + rest)
+        assert np.all(np.abs(np.delete(g, best[r].item()) - others) <= (bound + half) * np.abs(others))
+
+
 @pytest.mark.parametrize("n", [300, 5000, 40000])
 def test_all_equal_rows_give_the_first_entries(n):
     for value in (0.0, -0.0, 7.0, -3e38):
