@@ -142,17 +142,32 @@ __device__ __forceinline__ void add_entry(Terms& a, float l, const Scale& s) {
 template <class T>
 __device__ __forceinline__ void add_vector(Terms& a, uint4 v, const Scale& s, bool holds_top) {
   constexpr int P = ScoreVec<T>::N / 2;
-  if (s.plain && !holds_top) {
+  if (s.plain) {
     uint64_t l[P];
     raised_pairs(v, s.low, l, T());
+    if (holds_top) {
 #pragma unroll
-    for (int i = 0; i < P; ++i) {
-      const uint64_t t = fma2(l[i], pair(s.c, s.c), pair(s.minus_mc, s.minus_mc));
-      float t0, t1;
-      unpair(t, t0, t1);
-      const uint64_t e = pair(exp2_fast(t0), exp2_fast(t1));
-      a.X = add2(a.X, e);
-      a.u = fma2(e, t, a.u);
+      for (int i = 0; i < P; ++i) {
+        const uint64_t t = fma2(l[i], pair(s.c, s.c), pair(s.minus_mc, s.minus_mc));
+        float t0, t1, l0, l1;
+        unpair(t, t0, t1);
+        unpair(l[i], l0, l1);
+        const bool top0 = l0 == s.m, top1 = l1 == s.m;
+        const uint64_t e = pair(top0 ? 0.f : exp2_fast(t0), top1 ? 0.f : exp2_fast(t1));
+        a.top += (top0 ? 1.f : 0.f) + (top1 ? 1.f : 0.f);
+        a.X = add2(a.X, e);
+        a.u = fma2(e, t, a.u);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < P; ++i) {
+        const uint64_t t = fma2(l[i], pair(s.c, s.c), pair(s.minus_mc, s.minus_mc));
+        float t0, t1;
+        unpair(t, t0, t1);
+        const uint64_t e = pair(exp2_fast(t0), exp2_fast(t1));
+        a.X = add2(a.X, e);
+        a.u = fma2(e, t, a.u);
+      }
     }
   } else {
     float l[2 * P];
@@ -450,7 +465,10 @@ __global__ void __launch_bounds__(ST) k_score_part(int64_t rows, int64_t n, cons
     for (int w = 0; w < SW; ++w) m = fmaxf(m, top_of[w]);
     const Scale scale(m, o.c);
     Terms terms;
-    for (int at = tid; at < count; at += ST) add_vector<T>(terms, held[at], scale, own == m);
+    for (int at = tid; at < count; at += ST) {
+      const uint4 v = held[at];
+      add_vector<T>(terms, v, scale, own == m && max_score(v, T()) == m);
+    }
     Sum a = settle(block_sum(sum_of(terms, m), part), scale);
     if (!ok) a = {NAN, NAN, NAN, NAN};
     if (TOP) {
