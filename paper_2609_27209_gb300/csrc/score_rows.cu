@@ -18,10 +18,10 @@
 // What bounds them: an entry costs 3 to 4 instructions and one of the 16 exponentials an SM makes a clock, which is
 // 0.37 of the copy rate for bfloat16 rows if nothing else waits; a few long rows are latency (launch, copy, two
 // passes, the search, two cluster barriers).  Device time (us) and floor at 6767 GB/s:
-//   64 x 169343 bf16, 20 best  17.6 / 3.2, none 11.8 / 3.2; 1 x 20000 f32, 5 best 7.6, none 4.1; 16384 x 257 f32, none
-//   8.7 / 2.5, 32 best 28.5; 4096 x 20000 bf16, none 38.5 / 24.2; 8 x 2449029 f32, none 22 / 11.6, 32 best 45 / 11.6.
-// The gradient reads and writes each entry once: 4096 x 20000 bf16 52 to 55 us, 0.87 to 0.93 of the copy rate; rows whose
-// result is aligned otherwise than the scores (4096 x 19999) 69 us.
+//   64 x 169343 bf16, 20 best  18.7 / 3.2, none 12.4 / 3.2; 1 x 20000 f32, 5 best 8.3, none 4.6; 16384 x 257 f32, none
+//   10.2 / 2.5, 32 best 30; 4096 x 20000 bf16, none 42 / 24.2; 8 x 2449029 f32, none 24 / 11.6, 32 best 47 / 11.6.
+// The gradient reads and writes each entry once: 4096 x 20000 bf16 53 to 56 us, 0.87 to 0.92 of the copy rate; rows whose
+// result is aligned otherwise than the scores (4096 x 19999) 71 us.
 #include "choice.cuh"
 
 namespace erc {
@@ -943,8 +943,8 @@ Split split_rows(int64_t rows, int64_t n, int32_t type) {
   return {(int)((segments + each - 1) / each), (int)each * 32};
 }
 // Rows enough to keep the machine busy with a warp each.  A warp a row against a block a row (us, k 0): 10000 x 5001 float16
-// 32 / 39, 4096 x 20001 float32 69 / 79, 3000 x 3000 bfloat16 9.4 / 12.2; fewer rows leave SMs without loads in flight:
-// 2500 x 20000 bfloat16 29.6 / 27.3, 1900 x 20000 25.6 / 21.9.
+// 35 / 45, 4096 x 20001 float32 71 / 85, 3000 x 3000 bfloat16 10.3 / 14.1; fewer rows leave SMs without loads in flight:
+// 2500 x 20000 bfloat16 30 / 28, 1900 x 20000 26 / 23.
 bool many_rows(int64_t rows) { return rows >= (int64_t)sm_count() * 18; }
 bool short_rows(int64_t n, int32_t type) { return n / (16 / type_bytes(type)) <= 32 * 8; }
 
