@@ -4,15 +4,15 @@
 // An entry's word is one of the four of its Philox block.  A thread takes two pieces of 16 bytes of
 // each array, one block of the generator a piece for float32 and two for the 16-bit types.
 //
-// 169343 x 512 bf16 with a residual: 87 us, 0.88 of the copy rate.  Without one the 16-bit types are bound by
-// instructions: 21 an entry, most of them the generator's on the half-rate integer units; 20000 x 1001 f16 takes 19 us for
-// a floor of 11.8.
+// 169343 x 512 bf16 with a residual: 78 to 80 us, 0.96 to 0.99 of the copy rate.  Without one the 16-bit types are bound by
+// the generator's instructions on the half-rate integer units: 20000 x 1001 f16 takes 19 us for a floor of 11.8 (blocks of
+// 256 threads 19.9, one piece a thread 20.9, four 22.5).
 #include "choice.cuh"
 
 namespace erc {
 namespace {
 
-constexpr int DT = 256;
+constexpr int DT = 128;
 constexpr uint32_t DROP = 0x44524F50u;
 
 struct DropRule {
@@ -67,39 +67,45 @@ __device__ __forceinline__ uint4 drop_piece(uint4 x, uint4 r, const uint32_t* w,
   return make_uint4(v[0], v[1], v[2], v[3]);
 }
 
-// all arrays are 16-byte aligned; a block takes 2 DT pieces of 16 bytes, the last one perhaps not whole
+// all arrays are 16-byte aligned; a block takes 2 DT pieces of 16 bytes, the last block perhaps fewer
 template <class T, bool RESIDUAL>
 __global__ void __launch_bounds__(DT) k_dropout(int64_t count, const T* x, const T* residual, DropRule d,
                                                 const uint64_t* key_dev, T* out) {
   if (key_dev) d.key = *key_dev;
   constexpr int N = 16 / sizeof(T);
-  int64_t v[2];
-  uint4 a[2] = {}, r[2] = {};
+  const int64_t from = (int64_t)blockIdx.x * (2 * DT * N) + threadIdx.x * N;  // the thread's entries: N here, N from DT N on
+  const uint64_t block = d.first + (uint64_t)from / 4;
+  x += from;
+  out += from;
+  if (RESIDUAL) residual += from;
+  if (((int64_t)blockIdx.x + 1) * (2 * DT * N) <= count) {
+    uint4 a[2], r[2] = {};
 #pragma unroll
-  for (int j = 0; j < 2; ++j) {
-    v[j] = ((int64_t)blockIdx.x * 2 + j) * DT + threadIdx.x;
-    if ((v[j] + 1) * N <= count) {
-      a[j] = reinterpret_cast<const uint4*>(x)[v[j]];
-      if (RESIDUAL) r[j] = reinterpret_cast<const uint4*>(residual)[v[j]];
+    for (int j = 0; j < 2; ++j) {
+      a[j] = reinterpret_cast<const uint4*>(x)[j * DT];
+      if (RESIDUAL) r[j] = reinterpret_cast<const uint4*>(residual)[j * DT];
     }
-  }
 #pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      uint32_t w[N];
+      if (d.all) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) w[i] = ~0u;
+      } else {
+        drop_words<N / 4>(block + j * (DT * N / 4), d.key, w);
+      }
+      reinterpret_cast<uint4*>(out)[j * DT] = drop_piece<T, RESIDUAL>(a[j], r[j], w, d);
+    }
+    return;
+  }
+#pragma unroll 1
   for (int j = 0; j < 2; ++j) {
     uint32_t w[N];
-    if (d.all) {
+    drop_words<N / 4>(block + j * (DT * N / 4), d.key, w);
 #pragma unroll
-      for (int i = 0; i < N; ++i) w[i] = ~0u;
-    } else {
-      drop_words<N / 4>(d.first + (uint64_t)v[j] * (N / 4), d.key, w);
-    }
-    if ((v[j] + 1) * N <= count) {
-      reinterpret_cast<uint4*>(out)[v[j]] = drop_piece<T, RESIDUAL>(a[j], r[j], w, d);
-    } else {
-#pragma unroll
-      for (int i = 0; i < N; ++i) {
-        const int64_t e = v[j] * N + i;
-        if (e < count) out[e] = drop_one(x[e], RESIDUAL ? residual + e : nullptr, w[i] > d.most, d);
-      }
+    for (int i = 0; i < N; ++i) {
+      const int at = j * DT * N + i;
+      if (from + at < count) out[at] = drop_one(x[at], RESIDUAL ? residual + at : nullptr, d.all || w[i] > d.most, d);
     }
   }
 }
