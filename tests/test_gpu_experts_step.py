@@ -169,3 +169,65 @@ def test_the_gated_example_runs(example):
     r = example.main(steps=3, walkers=64, gated=True)
     assert len(r["losses"]) == 3 and np.isfinite(r["losses"]).all()
     assert (r["ids"] >= 0).all() and torch.isfinite(r["logp"]).all()
+
+
+def every_call():
+    x = torch.randn(8, 16, device=dev())
+    ids = torch.zeros(8, dtype=torch.int32, device=dev())
+    at = torch.tensor([0, 5, 8], device=dev())
+    w_in, w_out = torch.randn(2, 24, 16, device=dev()), torch.randn(2, 16, 12, device=dev())
+    pre = torch.randn(8, 24, device=dev())
+    norm, one = torch.zeros(8, 2, device=dev()), torch.ones(8, device=dev())
+    return [lambda **kw: erc.erc_score_rows(x, ids, k=2, **kw), lambda **kw: erc.erc_expert_ffn(x, at, w_in, w_out, **kw),
+            lambda **kw: erc.erc_expert_ffn_backward(x, x, pre, at, w_in, w_out, **kw),
+            lambda: erc.erc_score_rows_backward(x, ids, norm, one), lambda: erc.erc_dropout(x, 0.5, 3)]
+
+
+def refused(call, **kw):
+    with pytest.raises(erc.ErcError) as e:
+        call(**kw)
+    assert e.value.status == erc.ERC_ERR_INVALID_ARG
+
+
+def test_tensors_of_a_device_that_is_not_current_are_refused(monkeypatch):
+    calls = every_call()
+    for call in calls:
+        call()
+    torch.cuda.synchronize()
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
+    for call in calls:
+        refused(call)
+
+
+def test_workspaces_of_another_type_device_or_layout_are_refused():
+    for call in every_call()[:3]:
+        call(ws=torch.empty(1 << 20, dtype=torch.uint8, device=dev()))
+        for ws in (torch.empty(1 << 20, dtype=torch.uint8), torch.empty(1 << 20, device=dev()),
+                   torch.empty(1 << 20, dtype=torch.uint8, device=dev())[::2], 1 << 20):
+            refused(call, ws=ws)
+
+
+def test_a_workspace_may_start_anywhere_and_says_that_the_work_ended_well():
+    offsets = torch.tensor([0, 100, 260], device=dev())
+    w_in, w_out = torch.randn(2, 64, 48, device=dev()).half(), torch.randn(2, 48, 32, device=dev()).half()
+    x = torch.randn(260, 48, device=dev()).half()
+    want, _ = erc.erc_expert_ffn(x, offsets, w_in, w_out)
+    need = erc.lib().erc_expert_ffn_workspace_size(erc.ctypes.byref(erc._ffn_shape(x, "xs", offsets, w_in, w_out, 0)))
+    for lead in (0, 1, 8, 255):
+        buffer = torch.full((need + 256,), 77, dtype=torch.uint8, device=dev())
+        ws = buffer[lead:lead + need]
+        got, _ = erc.erc_expert_ffn(x, offsets, w_in, w_out, ws=ws)
+        assert torch.equal(got, want)
+        first = -ws.data_ptr() % 256 + lead  # the first 256-byte boundary
+        assert not buffer[first:first + 4].any()
+        assert (buffer[:lead] == 77).all() and (buffer[lead + need:] == 77).all()
+
+
+def test_numbers_that_do_not_fit_are_refused():
+    x = torch.randn(4, 16, device=dev())
+    ids = torch.zeros(4, dtype=torch.int32, device=dev())
+    at = torch.tensor([0, 4], device=dev())
+    w_in, w_out = torch.randn(1, 24, 16, device=dev()), torch.randn(1, 16, 12, device=dev())
+    for call in (lambda: erc.erc_score_rows(x, ids, k=2**32), lambda: erc.erc_expert_ffn(x, at, w_in, w_out, act=2**32),
+                 lambda: erc.erc_dropout(x, 0.5, 1, first=2**62), lambda: erc.erc_dropout(x, 0.5, 1, first=0.5)):
+        refused(call)
