@@ -5,8 +5,8 @@
 // A product is C(i, j) = sum_k A(i, k) B(j, k) in tiles of 64 or 128 rows and columns by a depth of 16, twice
 // buffered in shared memory.  A thread keeps 4 x 4 or 8 x 8 sums in registers, as groups of 4 rows and 4 columns 64
 // apart.  In IN the second group of columns holds the factors of the first one's features.  Sums run over k in order.
-// Bound by the float32 units and by the tiles' rounds: 8192 slots of 1024 x 1024 float32, 44 TFLOP/s forward and 38
-// backward (a library product: 45 and 50).
+// Bound by the float32 units and by the tiles' rounds: 8192 slots of 1024 x 1024 float32, 44 TFLOP/s forward and 42
+// backward (library products: 45 and 50).
 #include <initializer_list>
 
 #include "expert_ffn.cuh"
@@ -277,7 +277,15 @@ __global__ void __launch_bounds__(FT) k_ffn_weights(const FfnArgs<T> p) {
     }
 }
 
-// tiles of 128 rows and columns where they keep every SM busy twice, else of 64: a thread's 64 sums take half the
+// whether a weight gradient of rows x cols takes tiles of 128: enough of them for every SM, or slots enough to split their
+// sums until there are (8192 slots of 1024 x 1024 float32, 128 tiles and 64: the whole gradient 2744 -> 2426 us)
+bool large_weights(int64_t slots, int experts, int64_t rows, int64_t cols) {
+  const int64_t tiles = ((rows + 2 * FM - 1) / (2 * FM)) * ((cols + 2 * FM - 1) / (2 * FM)) * experts;
+  if (tiles >= sm_count()) return true;
+  return rows >= 96 && cols >= 96 && slots >= (int64_t)experts * 1024 && tiles * (slots / ((int64_t)experts * 512)) >= sm_count();
+}
+
+// tiles of 128 rows and columns where there is one for every SM, else of 64: a thread's 64 sums take half the
 // shared-memory reads a product that 16 take, but few large tiles leave SMs idle
 template <class T, int WHICH>
 erc_status simple_launch(const FfnArgs<T>& p, cudaStream_t s) {
@@ -297,7 +305,7 @@ erc_status simple_launch(const FfnArgs<T>& p, cudaStream_t s) {
     const int64_t rows = WHICH == FFN_DWIN ? 2 * (int64_t)p.inner : p.width, cols = WHICH == FFN_DWIN ? p.width : p.inner;
     const int64_t r2 = (rows + 2 * FM - 1) / (2 * FM), c2 = (cols + 2 * FM - 1) / (2 * FM);
     const unsigned deep = (unsigned)p.experts * p.splits;
-    if (r2 * c2 * p.experts >= busy)
+    if (large_weights(p.slots, p.experts, rows, cols))
       k_ffn_weights<T, WHICH, 2, 2><<<dim3((unsigned)c2, (unsigned)r2, deep), FT, 0, s>>>(p);
     else
       k_ffn_weights<T, WHICH, 1, 1><<<dim3((unsigned)((cols + FM - 1) / FM), (unsigned)((rows + FM - 1) / FM), deep), FT, 0, s>>>(p);
@@ -345,9 +353,10 @@ FfnWay ffn_way(const erc_ffn_shape* f, uintptr_t all, bool forward) {
 }
 
 // Parts of an expert's slots in a weight gradient of rows x cols: few tiles would leave most SMs idle over a long sum
-// (100000 slots of 32 x 64 bfloat16, the whole gradient: 986 us in one part, 126 in 64).
+// (100000 slots of 32 x 64 bfloat16, the whole gradient: 986 us in one part, 111 to 126 in 64).
 int weight_splits(const erc_ffn_shape* f, int64_t rows, int64_t cols, bool tensor) {
-  const int64_t side = tensor ? 256 : FM, most = tensor ? sm_count() / 2 : 2 * sm_count();
+  const int64_t side = tensor ? 256 : large_weights(f->slots, f->experts, rows, cols) ? 2 * FM : FM;
+  const int64_t most = tensor ? sm_count() / 2 : 2 * sm_count();
   const int64_t tiles = f->experts * ((rows + side - 1) / side) * ((cols + side - 1) / side);
   int64_t n = most / (tiles > 0 ? tiles : 1);
   const int64_t deep = f->slots / ((int64_t)f->experts * 512);

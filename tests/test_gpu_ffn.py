@@ -143,7 +143,7 @@ def test_a_dense_block_of_many_rows():
 
 
 @pytest.mark.parametrize("kind", TYPES)
-@pytest.mark.parametrize("width,inner", [(24, 16), (17, 40), (264, 8)])
+@pytest.mark.parametrize("width,inner", [(24, 16), (17, 40), (264, 8), (264, 136)])
 @pytest.mark.parametrize("counts", [[9000], [4001, 0, 5003]], ids=str)
 def test_long_sums_of_small_weights(kind, width, inner, counts):
     """The weights' gradients are few tiles over many slots: summed in parts, which are then added."""
