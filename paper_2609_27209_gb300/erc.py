@@ -731,11 +731,16 @@ ERC_ACT_SILU, ERC_ACT_GELU, ERC_ACT_RELU = 0, 1, 2
 def _given_workspace(ws, need, device):
     """`ws` or a fresh workspace of `need` bytes."""
     if ws is None:
-        return _workspace(need, device) if need else None
+        return torch.empty(need, dtype=torch.uint8, device=device) if need else None
     if not (isinstance(ws, torch.Tensor) and ws.dtype is torch.uint8 and ws.device == device
             and ws.is_contiguous()):
         _refuse(f"ws must be a contiguous uint8 tensor on {device}")
     return ws
+
+
+def _at(t):
+    """The address of a tensor as a plain number, which ctypes takes faster than a c_void_p; None is NULL."""
+    return None if t is None else t.data_ptr()
 
 
 def erc_score_rows(logits, ids=None, temperature=1.0, k=0, ws=None):
@@ -758,13 +763,15 @@ def erc_score_rows(logits, ids=None, temperature=1.0, k=0, ws=None):
     norm = torch.empty((rows, 2), dtype=torch.float32, device=dev)
     top_ids = torch.empty((rows, k), dtype=torch.int32, device=dev) if k else None
     top_logp = torch.empty((rows, k), dtype=torch.float32, device=dev) if k else None
-    need = lib().erc_score_rows_workspace_size(rows, n, kind, k)
+    L = lib()
+    need = L.erc_score_rows_workspace_size(rows, n, kind, k)
     if need or ws is not None:
         ws = _given_workspace(ws, need, dev)
-    _check(lib().erc_score_rows(rows, n, logits.data_ptr(), kind, stride, _ptr(ids), temperature, k,
-                                _ptr(logp), entropy.data_ptr(), norm.data_ptr(), _ptr(top_ids),
-                                _ptr(top_logp), _ptr(ws), 0 if ws is None else ws.numel(),
-                                _stream_of(logits)))
+    status = L.erc_score_rows(rows, n, logits.data_ptr(), kind, stride, _at(ids), temperature, k, _at(logp),
+                              entropy.data_ptr(), norm.data_ptr(), _at(top_ids), _at(top_logp), _at(ws),
+                              0 if ws is None else ws.numel(), _stream_of(logits))
+    if status:
+        _check(status)
     return logp, entropy, norm, top_ids, top_logp
 
 
@@ -779,8 +786,8 @@ def erc_score_rows_backward(logits, ids, norm, dlogp=None, entropy=None, dentrop
         if t is not None:
             _need(t, name, dtype, (rows,), dev)
     dlogits = torch.empty(rows, n, dtype=logits.dtype, device=dev)
-    _check(lib().erc_score_rows_backward(rows, n, logits.data_ptr(), kind, stride, _ptr(ids), temperature,
-                                         norm.data_ptr(), _ptr(entropy), _ptr(dlogp), _ptr(dentropy),
+    _check(lib().erc_score_rows_backward(rows, n, logits.data_ptr(), kind, stride, _at(ids), temperature,
+                                         norm.data_ptr(), _at(entropy), _at(dlogp), _at(dentropy),
                                          dlogits.data_ptr(), _stream_of(logits)))
     return dlogits
 
@@ -788,14 +795,16 @@ def erc_score_rows_backward(logits, ids, norm, dlogp=None, entropy=None, dentrop
 def _ffn_shape(x, name, offsets, w_in, w_out, act):
     """The shape of a block, with its weights and offsets checked against x [slots, width]."""
     slots, width, kind = _matrix(x, name)
-    dev = x.device
-    _placed(offsets, dev)
+    dev, dtype = x.device, x.dtype
+    if not (isinstance(offsets, torch.Tensor) and offsets.dtype is torch.int64 and offsets.dim() == 1
+            and offsets.device == dev and offsets.is_contiguous() and offsets.numel() > 0):
+        _refuse(f"offsets must be a contiguous int64 tensor [n_experts + 1] on {dev}")
     experts = offsets.numel() - 1
     if not (isinstance(w_out, torch.Tensor) and w_out.dim() == 3):
         _refuse("w_out must be [experts, width, inner]")
     inner = w_out.shape[2]
-    _need(w_out, "w_out", x.dtype, (experts, width, inner), dev)
-    _need(w_in, "w_in", x.dtype, (experts, 2 * inner, width), dev)
+    _need(w_out, "w_out", dtype, (experts, width, inner), dev)
+    _need(w_in, "w_in", dtype, (experts, 2 * inner, width), dev)
     return ErcFfnShapeC(slots, experts, _whole(width, "width"), _whole(inner, "inner"), _whole(act, "act"), kind)
 
 
@@ -811,11 +820,12 @@ def erc_expert_ffn(xs, offsets, w_in, w_out, act=ERC_ACT_SILU, keep=False, ws=No
     dev = xs.device
     y = torch.empty_like(xs)
     pre = torch.empty(shape.slots, 2 * shape.inner, dtype=xs.dtype, device=dev) if keep else None
-    ref = ctypes.byref(shape)
-    ws = _given_workspace(ws, lib().erc_expert_ffn_workspace_size(ref), dev)
-    _check(lib().erc_expert_ffn(ref, xs.data_ptr(), offsets.data_ptr(), w_in.data_ptr(), w_out.data_ptr(),
-                                y.data_ptr(), _ptr(pre), _ptr(ws), 0 if ws is None else ws.numel(),
-                                _stream_of(xs)))
+    L, ref = lib(), ctypes.byref(shape)
+    ws = _given_workspace(ws, L.erc_expert_ffn_workspace_size(ref), dev)
+    status = L.erc_expert_ffn(ref, xs.data_ptr(), offsets.data_ptr(), w_in.data_ptr(), w_out.data_ptr(), y.data_ptr(),
+                              _at(pre), _at(ws), 0 if ws is None else ws.numel(), _stream_of(xs))
+    if status:
+        _check(status)
     return y, pre
 
 
@@ -828,11 +838,11 @@ def erc_expert_ffn_backward(dy, xs, pre, offsets, w_in, w_out, act=ERC_ACT_SILU,
     _need(pre, "pre", xs.dtype, (shape.slots, 2 * shape.inner), dev)
     out = (torch.empty_like(xs) if dxs else None, torch.empty_like(w_in) if dw else None,
            torch.empty_like(w_out) if dw else None)
-    ref = ctypes.byref(shape)
-    ws = _given_workspace(ws, lib().erc_expert_ffn_backward_workspace_size(ref), dev)
-    _check(lib().erc_expert_ffn_backward(ref, dy.data_ptr(), xs.data_ptr(), pre.data_ptr(), offsets.data_ptr(),
-                                         w_in.data_ptr(), w_out.data_ptr(), _ptr(out[0]), _ptr(out[1]), _ptr(out[2]),
-                                         _ptr(ws), 0 if ws is None else ws.numel(), _stream_of(xs)))
+    L, ref = lib(), ctypes.byref(shape)
+    ws = _given_workspace(ws, L.erc_expert_ffn_backward_workspace_size(ref), dev)
+    _check(L.erc_expert_ffn_backward(ref, dy.data_ptr(), xs.data_ptr(), pre.data_ptr(), offsets.data_ptr(),
+                                     w_in.data_ptr(), w_out.data_ptr(), _at(out[0]), _at(out[1]), _at(out[2]),
+                                     _at(ws), 0 if ws is None else ws.numel(), _stream_of(xs)))
     return out
 
 
@@ -859,6 +869,8 @@ def erc_dropout(x, p, key, residual=None, first=0):
     if not (int(first) == first and 0 <= first < 2**62):
         _refuse("first must be a whole number in [0, 2^62)")
     out = torch.empty_like(x)
-    _check(lib().erc_dropout(x.numel(), x.data_ptr(), kind, _ptr(residual), p, number, at, int(first), out.data_ptr(),
-                             _stream_of(x)))
+    status = lib().erc_dropout(x.numel(), x.data_ptr(), kind, _at(residual), p, number, at, int(first), out.data_ptr(),
+                               _stream_of(x))
+    if status:
+        _check(status)
     return out
