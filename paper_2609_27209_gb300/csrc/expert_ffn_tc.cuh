@@ -23,15 +23,16 @@
 // write results while the next tile runs in its other half.
 //
 // Why this tile: a stage of 64 k brings a block 32 KB for 512 clocks of products, and an SM takes in about 64 bytes a
-// clock, so 256 x 256 a pair is where copies and products balance; with a quarter of the products left out 8192 x 2048
-// x 4096 still takes 0.77 of its time.  Two accumulators fill tensor memory.  What it reaches (8192 slots, one expert,
+// clock, so 256 x 256 a pair is where copies and products balance; with three quarters of the products left out 8192 x
+// 2048 x 4096 still takes 0.77 of its time.  Two accumulators fill tensor memory.  What it reaches (8192 slots, one expert,
 // 2048 x 4096): IN 159 to 167 us, 1640 to 1730 TFLOP/s (0.87 to 0.91 of the measured burst rate); OUT 94 to 100 us,
 // 1370 to 1450, 256 tiles on 76 pairs being 3.4 rounds.  Experts of a few hundred slots are bound by memory and by the
 // rounds: 64 x 512 slots of 1024 x 512, IN 59 to 64 us, OUT 45.  DH also reads (a, b) and writes (da, db) and h, 0.9 GB for
 // 80000 slots of 1024: 198 us, 4.7 TB/s.
 //
 // What was tried and did not pay: asking for DH's rows ahead (prefetches into L2: 215 -> 240 us, by bulk requests 345;
-// reading two or three steps ahead: no change); 8 result warps instead of 16 (DH 209 instead of 200); passing every
+// reading two or three steps ahead: no change); passing what DH reads and writes through shared memory by tensor copies,
+// with 4 stages instead of 6 (200 -> 191 us at a depth of 512, 108 -> 117 at 2048); 8 result warps instead of 16 (DH 209 instead of 200); passing every
 // stage on through a warp of each block (the same).  Releases at cluster scope on the way cost a microsecond a stage.
 //
 // Every wait on a barrier ends: after TC_WAIT it gives up, the block's roles stop, copies and products in flight
@@ -53,7 +54,6 @@ constexpr int TC_SMEM = TC_STAGES * TC_STAGE + 1024;
 constexpr int TC_EPILOGUE = 16;             // warps that write results: a quarter of the rows and of the columns each
 constexpr int TC_PART = 256 / (TC_EPILOGUE / 4);
 constexpr int TC_THREADS = 128 + 32 * TC_EPILOGUE;
-constexpr int TC_AHEAD = 1;
 constexpr int tc_cols(int which) { return which == FFN_DH ? 8 : 16; }  // columns that a lane holds at a time
 constexpr uint64_t TC_WAIT = 20000000000ull;   // nanoseconds: the sum over the slots of one expert is a tile's longest wait
 constexpr uint64_t TC_COPIES = 2000000ull;     // far longer than copies take that are in flight
@@ -689,7 +689,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(TC_THREADS, 1)
       const int c1 = min(t.n, c0 + TC_PART);
       const TcOut out = tile_out<T, WHICH>(p, t, m_block, lane, quad);
       float v[COLS];
-      PrePairs pre, next[TC_AHEAD];  // DH: read TC_AHEAD steps before their use
+      PrePairs pre, next;  // DH: read a step before their use
       if (t.blocks == 0) {
 #pragma unroll
         for (int i = 0; i < COLS; ++i) v[i] = 0.f;
@@ -697,13 +697,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(TC_THREADS, 1)
         for (int c = c0; c < c1; c += COLS) write_columns<T, WHICH, ACT>(out, v, pre, c, lane, keep);
         continue;
       }
-      auto read_ahead = [&](int c, PrePairs& r) {
-        read_pre(out.pre_a, out.pre_b, out.at + (uint32_t)c / 2 * out.two, out.two, c, c < c1 ? out.live - out.col : 0, r);
+      auto read_ahead = [&](int c) {
+        read_pre(out.pre_a, out.pre_b, out.at + (uint32_t)c / 2 * out.two, out.two, c, c < c1 ? out.live - out.col : 0, next);
       };
-      if constexpr (WHICH == FFN_DH) {
-#pragma unroll
-        for (int i = 0; i < TC_AHEAD; ++i) read_ahead(c0 + i * COLS, next[i]);
-      }
+      if constexpr (WHICH == FFN_DH) read_ahead(c0);
       if (!__all_sync(0xffffffffu, bar_wait(full(a), a_phase, &failed))) break;
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
       const uint32_t src = tmem + a * 256 + ((uint32_t)(quad * 32) << 16);
@@ -711,10 +708,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(TC_THREADS, 1)
       for (int c = c0; c < c1; c += COLS) {
         read_tmem<COLS>(src + c, v);
         if constexpr (WHICH == FFN_DH) {
-          pre = next[0];
-#pragma unroll
-          for (int i = 0; i + 1 < TC_AHEAD; ++i) next[i] = next[i + 1];
-          read_ahead(c + TC_AHEAD * COLS, next[TC_AHEAD - 1]);
+          pre = next;
+          read_ahead(c + COLS);
         }
         read_tmem_done();
         if (c + COLS >= c1) {
