@@ -4,8 +4,9 @@
 //
 // A product is C(i, j) = sum_k A(i, k) B(j, k) in tiles of 64 or 128 rows and columns by a depth of 16, twice
 // buffered in shared memory.  A thread keeps 4 x 4 or 8 x 8 sums in registers, as groups of 4 rows and 4 columns 64
-// apart.  In IN the second group of columns holds the factors of the first one's features.  Sums run over k in order.
-// Bound by the float32 units and by the tiles' rounds: 8192 slots of 1024 x 1024 float32, 44 TFLOP/s forward and 42
+// apart.  In IN the second group of columns holds the factors of the first one's features.  Sums run over k in order,
+// 256 at a time.
+// Bound by the float32 units and by the tiles' rounds: 8192 slots of 1024 x 1024 float32, 42 TFLOP/s forward and 41
 // backward (library products: 45 and 50).
 #include <initializer_list>
 
@@ -85,10 +86,18 @@ struct Slice {
   }
 };
 
+// Sums of FLUSH products go to a second set of sums.  Terms of mixed signs leave a sum of n of them off by some
+// 2^-24 sqrt(n / 6) of its size, and so off by no more than that of 256 (2000 slots of 900 x 1000, three experts, the
+// gradient of x: 9.7e-7 -> 4.1e-7 of its norm; 8192 x 1024 x 1024: forward 1186 -> 1218 us, gradient 2426 -> 2519 us).
+// 64 sums a thread leave no registers for a second set, so theirs lies in shared memory.
+constexpr int FLUSH = 256;
 template <int RG, int CG>
 struct Tiles {
+  static constexpr int SUMS = 16 * RG * CG;
+  static constexpr bool OUTSIDE = SUMS > 32;
   float a[2][FK][RG * FM + 4];
   float b[2][FK][CG * FM + 4];
+  float held[OUTSIDE ? SUMS : 1][OUTSIDE ? FT : 1];
 };
 
 // the thread's sums: rows i0 + 64 g + 4 (tid / 16) + ., columns j0 + 64 q + 4 (tid % 16) + .
@@ -102,6 +111,15 @@ __device__ __forceinline__ void product(Tiles<RG, CG>& s, const Operand<T>& a, c
   for (int i = 0; i < 4 * RG; ++i)
 #pragma unroll
     for (int j = 0; j < 4 * CG; ++j) acc[i][j] = 0.f;
+  constexpr bool OUTSIDE = Tiles<RG, CG>::OUTSIDE;
+  float held[OUTSIDE ? 1 : Tiles<RG, CG>::SUMS];
+  bool flushed = false;
+  auto second = [&](int i, int j) -> float& {
+    if constexpr (OUTSIDE)
+      return s.held[i * 4 * CG + j][threadIdx.x];
+    else
+      return held[i * 4 * CG + j];
+  };
   float ra[Slice<RG, CA>::E], rb[Slice<CG, CB>::E];
   sa.load(a, i0, 0, depth, ra);
   sb.load(b, j0, 0, depth, rb);
@@ -135,6 +153,35 @@ __device__ __forceinline__ void product(Tiles<RG, CG>& s, const Operand<T>& a, c
     }
     __syncthreads();
     at ^= 1;
+    if (more && (k0 / FK + 1) % (FLUSH / FK) == 0) {
+#pragma unroll
+      for (int i = 0; i < 4 * RG; ++i)
+#pragma unroll
+        for (int j = 0; j < 4 * CG; ++j) {
+          second(i, j) = flushed ? second(i, j) + acc[i][j] : acc[i][j];
+          acc[i][j] = 0.f;
+        }
+      flushed = true;
+    }
+  }
+  if (flushed)
+#pragma unroll
+    for (int i = 0; i < 4 * RG; ++i)
+#pragma unroll
+      for (int j = 0; j < 4 * CG; ++j) acc[i][j] += second(i, j);
+}
+
+// the shared memory of a kernel, dynamic where it is more than a static array may be
+template <int RG, int CG>
+constexpr size_t tiles_bytes() { return Tiles<RG, CG>::OUTSIDE ? sizeof(Tiles<RG, CG>) : 0; }
+template <int RG, int CG>
+__device__ __forceinline__ Tiles<RG, CG>& tiles_of() {
+  if constexpr (Tiles<RG, CG>::OUTSIDE) {
+    extern __shared__ __align__(16) char outside[];
+    return *reinterpret_cast<Tiles<RG, CG>*>(outside);
+  } else {
+    __shared__ Tiles<RG, CG> inside;
+    return inside;
   }
 }
 
@@ -187,7 +234,7 @@ __device__ __forceinline__ bool find_tile(const int64_t* offsets, int experts, i
 // rows of a tile of slots against columns of a weight matrix
 template <class T, int WHICH, int RG, int CG>
 __global__ void __launch_bounds__(FT) k_ffn_slots(const FfnArgs<T> p) {
-  __shared__ Tiles<RG, CG> s;
+  Tiles<RG, CG>& s = tiles_of<RG, CG>();
   const int64_t D = p.width, F = p.inner;
   if (WHICH != FFN_DH) {
     const int64_t used = slots_used(p.offsets, p.experts, p.slots);
@@ -250,7 +297,7 @@ __global__ void __launch_bounds__(FT) k_ffn_slots(const FfnArgs<T> p) {
 // a tile of an expert's weight gradient: the sum over its slots
 template <class T, int WHICH, int RG, int CG>
 __global__ void __launch_bounds__(FT) k_ffn_weights(const FfnArgs<T> p) {
-  __shared__ Tiles<RG, CG> s;
+  Tiles<RG, CG>& s = tiles_of<RG, CG>();
   const int64_t D = p.width, F = p.inner;
   const int e = blockIdx.z / p.splits, part = blockIdx.z - e * p.splits;
   const SlotRange r = split_range(slot_range(p.offsets, e, p.slots), part, p.splits);
@@ -285,6 +332,14 @@ bool large_weights(int64_t slots, int experts, int64_t rows, int64_t cols) {
   return rows >= 96 && cols >= 96 && slots >= (int64_t)experts * 1024 && tiles * (slots / ((int64_t)experts * 512)) >= sm_count();
 }
 
+template <int RG, int CG, class K, class P>
+erc_status launch_tiles(K kernel, dim3 grid, const P& p, cudaStream_t s) {
+  constexpr size_t bytes = tiles_bytes<RG, CG>();
+  if (bytes) ERC_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes));
+  kernel<<<grid, FT, bytes, s>>>(p);
+  return ERC_OK;
+}
+
 // tiles of 128 rows and columns where there is one for every SM, else of 64: a thread's 64 sums take half the
 // shared-memory reads a product that 16 take, but few large tiles leave SMs idle
 template <class T, int WHICH>
@@ -296,19 +351,21 @@ erc_status simple_launch(const FfnArgs<T>& p, cudaStream_t s) {
     const int64_t large = (p.slots / (2 * FM) + 1) * ((cols + wide - 1) / wide);
     if (large >= busy) {
       const int64_t tiles = p.slots / (2 * FM) + least;
-      k_ffn_slots<T, WHICH, 2, 2><<<dim3((unsigned)tiles, (unsigned)((cols + wide - 1) / wide)), FT, 0, s>>>(p);
+      ERC_TRY((launch_tiles<2, 2>(k_ffn_slots<T, WHICH, 2, 2>, dim3((unsigned)tiles, (unsigned)((cols + wide - 1) / wide)), p, s)));
     } else {
       const int64_t tiles = p.slots / FM + least;
-      k_ffn_slots<T, WHICH, 1, WHICH == FFN_IN ? 2 : 1><<<dim3((unsigned)tiles, (unsigned)((cols + FM - 1) / FM)), FT, 0, s>>>(p);
+      constexpr int CG = WHICH == FFN_IN ? 2 : 1;
+      ERC_TRY((launch_tiles<1, CG>(k_ffn_slots<T, WHICH, 1, CG>, dim3((unsigned)tiles, (unsigned)((cols + FM - 1) / FM)), p, s)));
     }
   } else {
     const int64_t rows = WHICH == FFN_DWIN ? 2 * (int64_t)p.inner : p.width, cols = WHICH == FFN_DWIN ? p.width : p.inner;
     const int64_t r2 = (rows + 2 * FM - 1) / (2 * FM), c2 = (cols + 2 * FM - 1) / (2 * FM);
     const unsigned deep = (unsigned)p.experts * p.splits;
     if (large_weights(p.slots, p.experts, rows, cols))
-      k_ffn_weights<T, WHICH, 2, 2><<<dim3((unsigned)c2, (unsigned)r2, deep), FT, 0, s>>>(p);
+      ERC_TRY((launch_tiles<2, 2>(k_ffn_weights<T, WHICH, 2, 2>, dim3((unsigned)c2, (unsigned)r2, deep), p, s)));
     else
-      k_ffn_weights<T, WHICH, 1, 1><<<dim3((unsigned)((cols + FM - 1) / FM), (unsigned)((rows + FM - 1) / FM), deep), FT, 0, s>>>(p);
+      ERC_TRY((launch_tiles<1, 1>(k_ffn_weights<T, WHICH, 1, 1>,
+                                  dim3((unsigned)((cols + FM - 1) / FM), (unsigned)((rows + FM - 1) / FM), deep), p, s)));
   }
   count_launches(1);
   ERC_CUDA(cudaGetLastError());

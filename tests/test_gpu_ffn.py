@@ -286,3 +286,16 @@ def test_refusals():
         with pytest.raises(erc.ErcError) as e:
             call(x, at, w_in, w_out, ws=torch.empty(16, dtype=torch.uint8, device=dev()))
         assert e.value.status == erc.ERC_ERR_CAPACITY
+
+
+@pytest.mark.parametrize("slots,width,inner", [(300, 8192, 64), (2000, 4096, 640)])
+def test_long_float32_sums_keep_their_last_bits(slots, width, inner):
+    """n terms of mixed signs, summed 256 at a time: the k-th partial sum's square is k of a term's, its rounding's at
+    most U^2 / 3 of that, so the sums of 256 add 256 U^2 / 6 and the sum of those n / 256 U^2 / 6 to the squared error.
+    A single sum in order would add n U^2 / 6."""
+    offsets, x, _, w_in, w_out = inputs(31, [slots], 0, width, inner, "f32")
+    at = torch.from_numpy(offsets).to(dev())
+    _, pre = erc.erc_expert_ffn(x, at, w_in, w_out, act=erc.ERC_ACT_SILU, keep=True)
+    want = f64(x) @ f64(w_in[0]).T
+    error = np.linalg.norm(f64(pre) - want) / np.linalg.norm(want)
+    assert error <= U * np.sqrt((256 + width / 256) / 6), error / U
