@@ -6,7 +6,7 @@
 // buffered in shared memory.  A thread keeps 4 x 4 or 8 x 8 sums in registers, as groups of 4 rows and 4 columns 64
 // apart.  In IN the second group of columns holds the factors of the first one's features.  Sums run over k in order,
 // 256 at a time.
-// Bound by the float32 units and by the tiles' rounds: 8192 slots of 1024 x 1024 float32, 42 TFLOP/s forward and 41
+// Bound by the float32 units and by the tiles' rounds: 8192 slots of 1024 x 1024 float32, 44 TFLOP/s forward and 41
 // backward (library products: 45 and 50).
 #include <initializer_list>
 
@@ -88,16 +88,15 @@ struct Slice {
 
 // Sums of FLUSH products go to a second set of sums.  Terms of mixed signs leave a sum of n of them off by some
 // 2^-24 sqrt(n / 6) of its size, and so off by no more than that of 256 (2000 slots of 900 x 1000, three experts, the
-// gradient of x: 9.7e-7 -> 4.1e-7 of its norm; 8192 x 1024 x 1024: forward 1186 -> 1218 us, gradient 2426 -> 2519 us).
-// 64 sums a thread leave no registers for a second set, so theirs lies in shared memory.
+// gradient of x: 9.7e-7 -> 4.1e-7 of its norm; 8192 x 1024 x 1024: forward 1186 -> 1170 us, gradient 2426 -> 2518 us).
+// It lies in shared memory: in registers it would leave room for fewer blocks (1000 slots of 500 x 300, gradient: 193
+// instead of 155 us).
 constexpr int FLUSH = 256;
 template <int RG, int CG>
 struct Tiles {
-  static constexpr int SUMS = 16 * RG * CG;
-  static constexpr bool OUTSIDE = SUMS > 32;
   float a[2][FK][RG * FM + 4];
   float b[2][FK][CG * FM + 4];
-  float held[OUTSIDE ? SUMS : 1][OUTSIDE ? FT : 1];
+  float held[16 * RG * CG][FT];
 };
 
 // the thread's sums: rows i0 + 64 g + 4 (tid / 16) + ., columns j0 + 64 q + 4 (tid % 16) + .
@@ -111,15 +110,10 @@ __device__ __forceinline__ void product(Tiles<RG, CG>& s, const Operand<T>& a, c
   for (int i = 0; i < 4 * RG; ++i)
 #pragma unroll
     for (int j = 0; j < 4 * CG; ++j) acc[i][j] = 0.f;
-  constexpr bool OUTSIDE = Tiles<RG, CG>::OUTSIDE;
-  float held[OUTSIDE ? 1 : Tiles<RG, CG>::SUMS];
-  bool flushed = false;
-  auto second = [&](int i, int j) -> float& {
-    if constexpr (OUTSIDE)
-      return s.held[i * 4 * CG + j][threadIdx.x];
-    else
-      return held[i * 4 * CG + j];
-  };
+  const bool flushes = depth > FLUSH;
+  if (flushes)
+#pragma unroll
+    for (int i = 0; i < 16 * RG * CG; ++i) s.held[i][threadIdx.x] = 0.f;
   float ra[Slice<RG, CA>::E], rb[Slice<CG, CB>::E];
   sa.load(a, i0, 0, depth, ra);
   sb.load(b, j0, 0, depth, rb);
@@ -153,36 +147,27 @@ __device__ __forceinline__ void product(Tiles<RG, CG>& s, const Operand<T>& a, c
     }
     __syncthreads();
     at ^= 1;
-    if (more && (k0 / FK + 1) % (FLUSH / FK) == 0) {
+    if (flushes && (k0 / FK + 1) % (FLUSH / FK) == 0) {
 #pragma unroll
       for (int i = 0; i < 4 * RG; ++i)
 #pragma unroll
         for (int j = 0; j < 4 * CG; ++j) {
-          second(i, j) = flushed ? second(i, j) + acc[i][j] : acc[i][j];
+          s.held[i * 4 * CG + j][threadIdx.x] += acc[i][j];
           acc[i][j] = 0.f;
         }
-      flushed = true;
     }
   }
-  if (flushed)
+  if (flushes)
 #pragma unroll
     for (int i = 0; i < 4 * RG; ++i)
 #pragma unroll
-      for (int j = 0; j < 4 * CG; ++j) acc[i][j] += second(i, j);
+      for (int j = 0; j < 4 * CG; ++j) acc[i][j] += s.held[i * 4 * CG + j][threadIdx.x];
 }
 
-// the shared memory of a kernel, dynamic where it is more than a static array may be
-template <int RG, int CG>
-constexpr size_t tiles_bytes() { return Tiles<RG, CG>::OUTSIDE ? sizeof(Tiles<RG, CG>) : 0; }
 template <int RG, int CG>
 __device__ __forceinline__ Tiles<RG, CG>& tiles_of() {
-  if constexpr (Tiles<RG, CG>::OUTSIDE) {
-    extern __shared__ __align__(16) char outside[];
-    return *reinterpret_cast<Tiles<RG, CG>*>(outside);
-  } else {
-    __shared__ Tiles<RG, CG> inside;
-    return inside;
-  }
+  extern __shared__ __align__(16) char tiles[];
+  return *reinterpret_cast<Tiles<RG, CG>*>(tiles);
 }
 
 // the expert and rows of the t-th tile of `high` slots, experts one after another; false past the last
@@ -334,8 +319,10 @@ bool large_weights(int64_t slots, int experts, int64_t rows, int64_t cols) {
 
 template <int RG, int CG, class K, class P>
 erc_status launch_tiles(K kernel, dim3 grid, const P& p, cudaStream_t s) {
-  constexpr size_t bytes = tiles_bytes<RG, CG>();
-  if (bytes) ERC_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes));
+  constexpr size_t bytes = sizeof(Tiles<RG, CG>);
+  // small calls are bound by the host, and what every launch may have needs no asking
+  if constexpr (bytes > 48 * 1024)
+    ERC_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes));
   kernel<<<grid, FT, bytes, s>>>(p);
   return ERC_OK;
 }
