@@ -53,7 +53,11 @@ __device__ __forceinline__ float scaled(float l, float m, float c) {
 struct Sum {
   float m, X, u, top;
 };
-__device__ __forceinline__ float log_sum(const Sum& a) { return a.top > 0.f ? log1pf(a.X + (a.top - 1.f)) : -INFINITY; }
+// X is NaN where a copy did not land, and stays so however parts join: everything about the row is NaN then.
+__device__ __forceinline__ bool lost_row(const Sum& a) { return a.X != a.X; }
+__device__ __forceinline__ float log_sum(const Sum& a) {
+  return a.top > 0.f || lost_row(a) ? log1pf(a.X + (a.top - 1.f)) : -INFINITY;
+}
 __device__ __forceinline__ void raise(Sum& a, float m, float c) {
   if (a.m == m) return;
   const float d = scaled(a.m, m, c), f = exp2_fast(d), Z = a.X + a.top;
@@ -198,6 +202,7 @@ struct ScoreOut {
   float* top_logp;
   float temperature, c;
   int k;
+  unsigned polls;  // looks at a copy before its block gives up (0: a second or so)
 };
 
 __device__ __forceinline__ float log_p(float l, float m, float lnZ, float temperature) {
@@ -219,14 +224,14 @@ __device__ __forceinline__ Given given_of(const ScoreOut& o, int64_t row, const 
   return g;
 }
 __device__ __forceinline__ void finish_row(const ScoreOut& o, int64_t row, Given g, Sum a) {
-  const bool some = !(a.top <= 0.f);  // NaN: a copy that did not land
-  const float lnZ = some ? log1pf(a.X + (a.top - 1.f)) : -INFINITY, entropy = some ? lnZ - LN2 * (a.u / (a.X + a.top)) : 0.f;
+  const bool lost = lost_row(a), some = lost || a.top > 0.f;
+  const float lnZ = log_sum(a), entropy = some ? lnZ - LN2 * (a.u / (a.X + a.top)) : 0.f;
   if (o.entropy) o.entropy[row] = entropy < 0.f ? 0.f : entropy;
   if (o.norm) {
-    o.norm[2 * row] = some ? a.m : -INFINITY;
+    o.norm[2 * row] = lost ? NAN : some ? a.m : -INFINITY;
     o.norm[2 * row + 1] = lnZ;
   }
-  if (o.logp) o.logp[row] = g.id < 0 ? 0.f : some ? log_p(g.l, a.m, lnZ, o.temperature) : -INFINITY;
+  if (o.logp) o.logp[row] = lost ? NAN : g.id < 0 ? 0.f : some ? log_p(g.l, a.m, lnZ, o.temperature) : -INFINITY;
 }
 
 // an entry of a row's part in the workspace
@@ -350,8 +355,9 @@ __device__ __forceinline__ void block_top(TopScratch& s, unsigned mine, int k, E
 
 __device__ __forceinline__ void put_best(const ScoreOut& o, int64_t row, Sum a, float lnZ, int rank, unsigned key,
                                          unsigned id) {
-  o.top_ids[row * o.k + rank] = key ? (int32_t)id : -1;
-  o.top_logp[row * o.k + rank] = key ? log_p(order_value(key), a.m, lnZ, o.temperature) : -INFINITY;
+  const bool lost = lnZ != lnZ;
+  o.top_ids[row * o.k + rank] = key && !lost ? (int32_t)id : -1;
+  o.top_logp[row * o.k + rank] = lost ? NAN : key ? log_p(order_value(key), a.m, lnZ, o.temperature) : -INFINITY;
 }
 
 // the sums of a block whose threads share a maximum, in the order of its warps
@@ -382,23 +388,32 @@ __device__ __forceinline__ void cluster_sync_all() {
   asm volatile("barrier.cluster.arrive.release;\nbarrier.cluster.wait.acquire;" ::: "memory");
 }
 
-// waits for a copy into shared memory; false when a second or so was not enough (the row's results are NaN then)
-__device__ __forceinline__ bool landed(uint32_t bar, uint32_t parity) {
-  for (unsigned i = 0; i < (1u << 22); ++i) {
-    uint32_t done;
-    asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}"
-                 : "=r"(done)
-                 : "r"(bar), "r"(parity)
-                 : "memory");
-    if (done) return true;
+// Waits for a copy into shared memory; false when it did not land in `polls` looks at its barrier, or, with 0, in a second
+// or so of waiting.
+__device__ __forceinline__ bool landed(uint32_t bar, uint32_t parity, unsigned polls) {
+  uint32_t done = 0;
+  if (polls == 0) {
+    for (unsigned i = 0; i < (1u << 22) && !done; ++i)  // each may sleep for a while
+      asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}"
+                   : "=r"(done)
+                   : "r"(bar), "r"(parity)
+                   : "memory");
+  } else {
+    for (unsigned i = 0; i < polls && !done; ++i)
+      asm volatile("{\n.reg .pred p;\nmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}"
+                   : "=r"(done)
+                   : "r"(bar), "r"(parity)
+                   : "memory");
   }
-  return false;
+  return done;
 }
 
 constexpr int part_smem(int per, bool top) { return per * 16 + (top ? (int)sizeof(TopScratch) : 0); }
 
 // A block takes one of the `parts` of a row, `per` vectors each (a multiple of 32).  CLUSTERED: the parts of a row are a
-// cluster.  Blocks start with a task and take every gridDim.x-th one.
+// cluster.  Blocks start with a task and take every gridDim.x-th one.  Once a copy did not land in time the block starts
+// no more and gives NaN for this and its later tasks: that copy may still write the shared memory, and its barrier's
+// phase is open.  The block waits for it, with a limit, before it ends.
 template <class T, bool TOP, bool CLUSTERED>
 __global__ void __launch_bounds__(ST) k_score_part(int64_t rows, int64_t n, const T* __restrict__ logits, int64_t stride,
                                                    int parts, int per, ScoreOut o, Sum* __restrict__ sums,
@@ -420,6 +435,7 @@ __global__ void __launch_bounds__(ST) k_score_part(int64_t rows, int64_t n, cons
   }
   __syncthreads();
   uint32_t parity = 0;
+  bool ok = true;  // the same for all threads
   const int64_t tasks = rows * parts;
   for (int64_t task = blockIdx.x; task < tasks; task += gridDim.x) {
     const int64_t row = task / parts;
@@ -429,7 +445,7 @@ __global__ void __launch_bounds__(ST) k_score_part(int64_t rows, int64_t n, cons
     const int first = which * per, count = max(min(per, view.vectors - first), 0);
     // whole vectors arrive by the copy, those that the row shares with its neighbours element by element
     const int lo = min(first == 0 && view.skew ? 1 : 0, count), hi = max(min(first + count, view.whole()) - first, lo);
-    if (tid == 0) {
+    if (ok && tid == 0) {
       if (hi > lo) {
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // the part before was written and read by threads
         asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"((hi - lo) * 16) : "memory");
@@ -441,21 +457,21 @@ __global__ void __launch_bounds__(ST) k_score_part(int64_t rows, int64_t n, cons
       if (lo == 1) held[0] = view.fetch(first);
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
-    if (tid == 32) {
+    if (ok && tid == 32) {
       for (int v = hi; v < count; ++v) held[v] = view.fetch(first + v);
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
     Given g = {-1, 0.f};
     if (tid == 0 && (CLUSTERED ? which == 0 : parts == 1)) g = given_of(o, row, x, n);
-    bool ok = true;
-    if (hi > lo) {
-      ok = landed(bar, parity);
+    if (ok && hi > lo) {
+      ok = landed(bar, parity, o.polls);
       parity ^= 1;
     }
     ok = __syncthreads_and(ok);
 
+    const int live = ok ? count : 0;
     float m = -INFINITY;
-    for (int at = tid; at < count; at += ST) m = fmaxf(m, max_score(held[at], T()));
+    for (int at = tid; at < live; at += ST) m = fmaxf(m, max_score(held[at], T()));
     const unsigned mine = order_key(__fadd_rn(m, 0.f));
     const float own = m;
     m = warp_max(fmaxf(m, LOWEST));
@@ -465,19 +481,19 @@ __global__ void __launch_bounds__(ST) k_score_part(int64_t rows, int64_t n, cons
     for (int w = 0; w < SW; ++w) m = fmaxf(m, top_of[w]);
     const Scale scale(m, o.c);
     Terms terms;
-    for (int at = tid; at < count; at += ST) {
+    for (int at = tid; at < live; at += ST) {
       const uint4 v = held[at];
       add_vector<T>(terms, v, scale, own == m && max_score(v, T()) == m);
     }
     Sum a = settle(block_sum(sum_of(terms, m), part), scale);
-    if (!ok) a = {NAN, NAN, NAN, NAN};
+    if (!ok) a = {m, NAN, NAN, NAN};
     if (TOP) {
       const bool alone = !CLUSTERED && parts == 1;
       const float lnZ = alone ? log_sum(a) : 0.f;
       block_top(
           top, mine, o.k,
           [&](unsigned least, auto&& f) {
-            for (int at = tid; at < count; at += ST) {
+            for (int at = tid; at < live; at += ST) {
               const uint4 v = held[at];
               if (order_key(__fadd_rn(max_score(v, T()), 0.f)) < least) continue;
               float s[N];
@@ -530,6 +546,7 @@ __global__ void __launch_bounds__(ST) k_score_part(int64_t rows, int64_t n, cons
       __syncthreads();
     }
   }
+  if (!ok) landed(bar, parity ^ 1, 0);
 }
 
 // a block joins the parts of a row
@@ -994,7 +1011,8 @@ extern "C" erc_status erc_score_rows(int64_t rows, int64_t n, const void* logits
   if (rows == 0) return ERC_OK;
   ERC_REQUIRE((n == 0 || logits) && (!ids == !logp) && (k == 0 || (top_ids && top_logp)), "null pointer");
   ERC_REQUIRE(reinterpret_cast<uintptr_t>(logits) % type_bytes(type) == 0, "misaligned logits");
-  const ScoreOut o = {ids, logp, entropy, norm, top_ids, top_logp, temperature, LOG2E / temperature, k};
+  const ScoreOut o = {ids, logp, entropy, norm, top_ids, top_logp, temperature, LOG2E / temperature, k,
+                      wait_limit(0)};
   const cudaStream_t s = as_stream(stream);
   const bool brief = short_rows(n, type);
   const Split sp = brief ? Split{1, 0} : split_rows(rows, n, type);
