@@ -95,12 +95,11 @@ uint64_t erc_kernel_launches(void);
  * restores each wait's default, which is seconds of waiting.  Waits of work already enqueued keep
  * the limit they were enqueued with.  The hardware cluster barriers of the cluster CG solver and of
  * erc_sample_rows are not polled and take no limit.
- * erc_score_rows waits for copies within a thread block, under the same limit (by default a second or
- * so) but without a status, because the call does not wait for the GPU: a row whose copy did not land in
- * time has NaN as its results and -1 as its best entries, and so have the rows that its block would have
- * taken after it.
- * The waits of erc_expert_ffn for copies and products within a pair of thread blocks keep a fixed limit of
- * their own, seconds of waiting; it says in its workspace that one ran out. */
+ * erc_score_rows and erc_expert_ffn wait for copies and products within a thread block or a pair of
+ * them, under the same limit (by default a second or so, and 20 seconds), but return before the GPU is done,
+ * so not with a status: a row of scores whose copy did not land in time has NaN as its results and -1 as its best
+ * entries, and so have the rows that its block would have taken after it; erc_expert_ffn and its gradient say
+ * so in their workspace. */
 void erc_set_wait_limit(uint32_t polls);
 
 /* ---------------------------------------------------------------------------------------------

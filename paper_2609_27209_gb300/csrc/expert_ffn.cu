@@ -481,7 +481,7 @@ erc_status ffn_product(FfnWay way, FfnProduct which, const FfnArgs<T>& p, int* s
 // what a call keeps in its workspace
 template <class T>
 struct FfnSpace {
-  int* status;
+  int *status, *lost;
   T *h, *dpre;
   float* partial;
   T *x, *dy, *pre, *w_in, *w_out, *y, *dx, *dw_in, *dw_out;  // rows of whole pieces
@@ -492,6 +492,7 @@ void plan_space(Arena& a, FfnSpace<T>& w, const erc_ffn_shape* f, bool backward)
   const size_t S = f->slots, E = f->experts, D = pad ? (f->width + 7) / 8 * 8 : f->width, F = pad ? (f->inner + 7) / 8 * 8 : f->inner;
   w = {};
   w.status = a.take<int>(1);
+  w.lost = a.take<int>(tc_blocks());
   w.h = a.take<T>(S * F);
   if (backward) {
     w.dpre = a.take<T>(S * 2 * F);
@@ -583,6 +584,8 @@ extern "C" erc_status erc_expert_ffn(const erc_ffn_shape* f, const void* xs, con
     p.pre = static_cast<T*>(pre);
     p.y = static_cast<T*>(y);
     p.splits = 1;
+    p.polls = wait_limit(0);
+    p.lost = w.lost;
     const int D = p.width, F = p.inner, E = p.experts;
     if (w.x) {
       p.width = (D + 7) / 8 * 8;
@@ -648,6 +651,8 @@ extern "C" erc_status erc_expert_ffn_backward(const erc_ffn_shape* f, const void
     p.dw_out = static_cast<T*>(dw_out);
     p.partial = w.partial;
     p.splits = 1;
+    p.polls = wait_limit(0);
+    p.lost = w.lost;
     const int D = p.width, F = p.inner, E = p.experts;
     if (w.x) {
       p.width = (D + 7) / 8 * 8;

@@ -35,6 +35,9 @@ struct FfnArgs {
   // DWIN and DWOUT: the slots of an expert in `splits` parts, whose sums go to partial [splits][experts][rows][columns]
   int splits;
   float* partial;
+  // on the tensor cores: looks at a barrier before a wait gives up (0: TC_WAIT), and which blocks of IN or DH gave up
+  unsigned polls;
+  int* lost;
 };
 // [lo, hi) of an expert; whatever the offsets hold, it lies in [0, slots]
 struct SlotRange {
@@ -122,12 +125,16 @@ __device__ __forceinline__ void zero_slots(T* out, int64_t first, int64_t slots,
   for (int64_t i = first * width + thread; i < slots * width; i += threads) out[i] = from_f32<T>(0.f);
 }
 
+// blocks of every product on the tensor cores
+inline int tc_blocks() { return sm_count() / 2 * 2; }
+
 // IN or OUT for a handful of slots (expert_ffn_few.cu); rows of whole 16-byte pieces, 16-byte aligned arrays
 template <class T>
 erc_status ffn_few_product(FfnProduct which, const FfnArgs<T>& p, int* status, cudaStream_t s);
 
 // a product on the tensor cores (bfloat16 and float16 whose rows are whole 16-byte pieces); `status` (device) gets
-// ERC_OK at the start of IN and DH, and ERC_ERR_TIMEOUT where a wait ran out
+// ERC_OK at the start of IN and DH, and ERC_ERR_TIMEOUT where a wait ran out: IN and DH leave word in `lost`, which the
+// products after them pass on, so that none can undo it
 template <class T>
 erc_status ffn_tc_product(FfnProduct which, const FfnArgs<T>& p, int* status, cudaStream_t s);
 template <>

@@ -35,8 +35,11 @@
 // with 4 stages instead of 6 (200 -> 191 us at a depth of 512, 108 -> 117 at 2048); 8 result warps instead of 16 (DH 209 instead of 200); passing every
 // stage on through a warp of each block (the same).  Releases at cluster scope on the way cost a microsecond a stage.
 //
-// Every wait on a barrier ends: after TC_WAIT it gives up, the block's roles stop, copies and products in flight
-// are waited for (with limits), tensor memory is freed and the status word is set to ERC_ERR_TIMEOUT.
+// Every wait on a barrier ends: after TC_WAIT, or a given number of looks, it gives up.  The block's other roles then
+// stop at their next wait; once all have, products and copies in flight are waited for (with limits), tensor memory
+// is freed and the status is ERC_ERR_TIMEOUT.  Products may still read, and copies still write, what either block of a
+// pair holds: the two end together, and where the products' thread gave up, the results of that tile wait in vain in
+// both, so that both pause.  Where it did not, every copy has landed.
 #pragma once
 
 #include <cuda.h>
@@ -109,9 +112,23 @@ __device__ __forceinline__ bool bar_poll(uint32_t bar, uint32_t parity, uint64_t
   }
   return false;
 }
+// looks at a barrier `polls` times
+__device__ __forceinline__ bool bar_look(uint32_t bar, uint32_t parity, unsigned polls, volatile int* failed) {
+  for (unsigned i = 0; i < polls; ++i) {
+    uint32_t done;
+    asm volatile(
+        "{\n.reg .pred p;\nmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}"
+        : "=r"(done)
+        : "r"(bar), "r"(parity)
+        : "memory");
+    if (done) return true;
+    if (*failed) return false;
+  }
+  return false;
+}
 // false when the wait ran out, here or in another role of the block
-__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile int* failed) {
-  if (bar_poll(bar, parity, TC_WAIT, failed)) return true;
+__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile int* failed, unsigned polls) {
+  if (polls ? bar_look(bar, parity, polls, failed) : bar_poll(bar, parity, TC_WAIT, failed)) return true;
   *failed = 1;
   return false;
 }
@@ -570,7 +587,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(TC_THREADS, 1)
         const int m = t.m0 + m_block, n_half = t.n / 2;
         const uint32_t bytes = TC_OPERAND + (B_K ? TC_OPERAND : n_half * TC_K * 2);
         for (int b = 0; b < t.blocks; ++b) {
-          if (!(ok = bar_wait(empty(s), phase ^ 1, &failed))) break;
+          if (!(ok = bar_wait(empty(s), phase ^ 1, &failed, p.polls))) break;
           const uint32_t dst = stages + s * TC_STAGE;
           const int k = b * TC_K;
           if constexpr (SLOTS) {
@@ -609,8 +626,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(TC_THREADS, 1)
           if (++s == TC_STAGES) s = 0, phase ^= 1;
         }
       }
-      // copies in flight write shared memory, and none may be left: nothing arrives at this barrier, so this is a pause
-      if (failed) bar_poll(never, 0, TC_COPIES, nullptr);
     }
   } else if (warp == 1) {
     if (lane == 0 && rank == 0) {  // products
@@ -622,11 +637,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(TC_THREADS, 1)
         if (t.blocks == 0) continue;
         const uint32_t idesc = (1u << 4) | (Half2<T>::FORMAT << 7) | (Half2<T>::FORMAT << 10) | ((A_K ? 0u : 1u) << 15) |
                                ((B_K ? 0u : 1u) << 16) | ((uint32_t)(t.n >> 3) << 17) | ((256u >> 4) << 24);
-        if (!(ok = bar_wait(taken(a), a_phase ^ 1, &failed))) break;
+        if (!(ok = bar_wait(taken(a), a_phase ^ 1, &failed, p.polls))) break;
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         const uint32_t d = tmem + a * 256;
         for (int b = 0; b < t.blocks; ++b) {
-          if (!(ok = bar_wait(ready(s), phase, &failed))) break;
+          if (!(ok = bar_wait(ready(s), phase, &failed, p.polls))) break;
           asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
           const uint64_t da = operand_desc(stages + s * TC_STAGE, A_K), db = operand_desc(stages + s * TC_STAGE + TC_OPERAND, B_K);
 #pragma unroll
@@ -638,10 +653,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(TC_THREADS, 1)
         if (!ok) break;
         commit_pair(full(a));
         if (++a == 2) a = 0, a_phase ^= 1;
-      }
-      if (failed) {
-        commit_pair(done);
-        bar_poll(done, 0, TC_WAIT, nullptr);
       }
     }
   } else if (warp == 2) {
@@ -655,7 +666,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(TC_THREADS, 1)
         s = (s + t.blocks - 1) % TC_STAGES;
         const int live = (int)(t.k1 - t.k0 - (int64_t)(t.blocks - 1) * TC_K);
         if (live < TC_K) {
-          if (!__all_sync(0xffffffffu, bar_wait(land(s), used >> s & 1, &failed))) break;
+          if (!__all_sync(0xffffffffu, bar_wait(land(s), used >> s & 1, &failed, p.polls))) break;
           used ^= 1u << s;
           const uint32_t base = stages + s * TC_STAGE;
           const int boxes = t.n > 128 ? 4 : 3;
@@ -669,7 +680,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(TC_THREADS, 1)
         s = (s + 1) % TC_STAGES;
       }
     }
-  } else if (warp == 3) {  // rows behind the last expert's
+  } else if (warp == 3) {  // rows behind the last expert's, and what the first product left word of
+    if constexpr (WHICH != FFN_IN && WHICH != FFN_DH) {
+      if (blockIdx.x == 0) {
+        int lost = 0;
+        for (int i = lane; i < gridDim.x; i += 32) lost |= __ldcg(p.lost + i);
+        if (lost) *status = ERC_ERR_TIMEOUT;
+      }
+    }
     if constexpr (WHICH == FFN_IN || WHICH == FFN_OUT || WHICH == FFN_DX) {
       T* out = WHICH == FFN_IN ? p.pre : WHICH == FFN_OUT ? p.y : p.dx;
       const int64_t row = (WHICH == FFN_IN ? 2 * (int64_t)p.inner : p.width) * sizeof(T) / 16;
@@ -701,7 +719,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(TC_THREADS, 1)
         read_pre(out.pre_a, out.pre_b, out.at + (uint32_t)c / 2 * out.two, out.two, c, c < c1 ? out.live - out.col : 0, next);
       };
       if constexpr (WHICH == FFN_DH) read_ahead(c0);
-      if (!__all_sync(0xffffffffu, bar_wait(full(a), a_phase, &failed))) break;
+      if (!__all_sync(0xffffffffu, bar_wait(full(a), a_phase, &failed, p.polls))) break;
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
       const uint32_t src = tmem + a * 256 + ((uint32_t)(quad * 32) << 16);
 #pragma unroll 1
@@ -729,10 +747,24 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(TC_THREADS, 1)
   __syncwarp();
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
   __syncthreads();
+  if (failed) {
+    if (threadIdx.x == 32 && rank == 0) {  // the thread that issued the products
+      commit_pair(done);
+      bar_poll(done, 0, TC_WAIT, nullptr);
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) bar_poll(never, 0, TC_COPIES, nullptr);  // nothing arrives here, so this is a pause for the copies
+    __syncthreads();
+  }
   cluster_arrive_wait();
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
   if (warp == 3) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(tmem));
-  if (threadIdx.x == 0 && failed) *status = ERC_ERR_TIMEOUT;
+  if (threadIdx.x == 0) {
+    if (WHICH == FFN_IN || WHICH == FFN_DH)
+      p.lost[blockIdx.x] = failed;
+    else if (failed)
+      *status = ERC_ERR_TIMEOUT;
+  }
 }
 
 // ---- host side
@@ -781,7 +813,7 @@ erc_status ffn_tc_launch(const FfnArgs<T>& p, int* status, cudaStream_t s) {
   }
   ERC_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, TC_SMEM));
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(sm_count() / 2 * 2);
+  cfg.gridDim = dim3(tc_blocks());
   cfg.blockDim = dim3(TC_THREADS);
   cfg.dynamicSmemBytes = TC_SMEM;
   cfg.stream = s;
