@@ -99,7 +99,7 @@ uint64_t erc_kernel_launches(void);
  * them, under the same limit (by default a second or so, and 20 seconds), but return before the GPU is done,
  * so not with a status: a row of scores whose copy did not land in time has NaN as its results and -1 as its best
  * entries, and so have the rows that its block would have taken after it; erc_expert_ffn and its gradient say
- * so in their workspace. */
+ * so in their workspace, and their results are right or NaN. */
 void erc_set_wait_limit(uint32_t polls);
 
 /* ---------------------------------------------------------------------------------------------
@@ -477,8 +477,8 @@ erc_status erc_score_rows_backward(int64_t rows, int64_t n, const void* logits, 
  *      workspace; everything else runs on the float32 units.
  * Workspace: erc_expert_ffn_workspace_size and erc_expert_ffn_backward_workspace_size bytes on the
  *      current device; calls that overlap on the GPU need one each.  The int32 at its first 256-byte
- *      boundary is ERC_OK once the work is done, or ERC_ERR_TIMEOUT where a wait on the device ran out
- *      (the results are then undefined).
+ *      boundary is ERC_OK once the work is done, or ERC_ERR_TIMEOUT where a wait on the device ran out:
+ *      results that were not reached are NaN then, the others right.  A call without slots leaves it as it is.
  * Errors: INVALID_ARG for sizes, types, alignment and pointers; CAPACITY for a small workspace.
  *      Deterministic.
  * ------------------------------------------------------------------------------------------- */

@@ -39,7 +39,7 @@
 // stop at their next wait; once all have, products and copies in flight are waited for (with limits), tensor memory
 // is freed and the status is ERC_ERR_TIMEOUT.  Products may still read, and copies still write, what either block of a
 // pair holds: the two end together, and where the products' thread gave up, the results of that tile wait in vain in
-// both, so that both pause.  Where it did not, every copy has landed.
+// both, so that both pause.  Where it did not, every copy has landed.  Results that were not reached are NaN.
 #pragma once
 
 #include <cuda.h>
@@ -702,6 +702,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(TC_THREADS, 1)
     const bool keep = p.pre != nullptr;
     int a = 0;
     uint32_t a_phase = 0;
+    bool ok = true;  // once a wait gave up this tile and the warp's later ones are NaN, and so is all that is made of them
     for (int at = first; at < total; at += step) {
       const TcTile t = tiles.at(at, of, p.experts);
       const int c1 = min(t.n, c0 + TC_PART);
@@ -719,12 +720,17 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(TC_THREADS, 1)
         read_pre(out.pre_a, out.pre_b, out.at + (uint32_t)c / 2 * out.two, out.two, c, c < c1 ? out.live - out.col : 0, next);
       };
       if constexpr (WHICH == FFN_DH) read_ahead(c0);
-      if (!__all_sync(0xffffffffu, bar_wait(full(a), a_phase, &failed, p.polls))) break;
+      if (ok) ok = __all_sync(0xffffffffu, bar_wait(full(a), a_phase, &failed, p.polls));
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
       const uint32_t src = tmem + a * 256 + ((uint32_t)(quad * 32) << 16);
 #pragma unroll 1
       for (int c = c0; c < c1; c += COLS) {
-        read_tmem<COLS>(src + c, v);
+        if (ok) {
+          read_tmem<COLS>(src + c, v);
+        } else {
+#pragma unroll
+          for (int i = 0; i < COLS; ++i) v[i] = NAN;
+        }
         if constexpr (WHICH == FFN_DH) {
           pre = next;
           read_ahead(c + COLS);
@@ -733,13 +739,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(TC_THREADS, 1)
         if (c + COLS >= c1) {
           asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
           __syncwarp();
-          if (lane == 0) bar_arrive_cluster(peer_address(taken(a), 0));
+          if (ok && lane == 0) bar_arrive_cluster(peer_address(taken(a), 0));
         }
         write_columns<T, WHICH, ACT>(out, v, pre, c, lane, keep);
       }
       if (c0 >= c1) {
         __syncwarp();
-        if (lane == 0) bar_arrive_cluster(peer_address(taken(a), 0));
+        if (ok && lane == 0) bar_arrive_cluster(peer_address(taken(a), 0));
       }
       if (++a == 2) a = 0, a_phase ^= 1;
     }

@@ -814,7 +814,8 @@ def erc_expert_ffn(xs, offsets, w_in, w_out, act=ERC_ACT_SILU, keep=False, ws=No
 
     offsets int64 [experts + 1] as from erc_expert_plan (a dense block: [0, slots]); w_in [experts,
     2 inner, width], w_out [experts, width, inner].  keep: also return pre, which the gradient takes.
-    ws: a uint8 workspace of erc_expert_ffn_workspace_size bytes, or None.
+    ws: a uint8 workspace of erc_expert_ffn_workspace_size bytes, or None; it holds the status of the
+    device's waits.  Where one ran out, results that were not reached are NaN.
     """
     shape = _ffn_shape(xs, "xs", offsets, w_in, w_out, act)
     dev = xs.device

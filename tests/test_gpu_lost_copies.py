@@ -88,3 +88,23 @@ def test_a_wait_of_the_block_that_gave_up_is_in_its_status(counts, width, inner,
     erc.erc_set_wait_limit(0)
     for (got, status), (right, _) in zip(block_steps(at, x, dy, w_in, w_out, pre), want):
         assert status == erc.ERC_OK and all(torch.equal(a, b) for a, b in zip(got, right))
+
+
+@pytest.mark.parametrize("counts,width,inner", BLOCKS.values(), ids=BLOCKS)
+@pytest.mark.parametrize("kind", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("act", [0, 1, 2])
+@pytest.mark.parametrize("polls", [1, 30, 300])
+def test_results_that_a_block_did_not_reach_are_nan(counts, width, inner, kind, act, polls):
+    at, x, dy, w_in, w_out = block_inputs(width + polls + act, counts, width, inner, kind)
+    pre = erc.erc_expert_ffn(x, at, w_in, w_out, act, keep=True)[1]
+    want = block_steps(at, x, dy, w_in, w_out, pre, act)
+    erc.erc_set_wait_limit(polls)
+    for _ in range(TRIES):
+        for (got, status), (right, _) in zip(block_steps(at, x, dy, w_in, w_out, pre, act), want):
+            missing = [torch.isnan(a) for a in got]
+            for a, b, none in zip(got, right, missing):
+                assert torch.equal(torch.where(none, b, a), b)
+            # a block that gave up may have had no rows of its own (those from `inner` on), so only one way
+            some = any(bool(none.any()) for none in missing)
+            assert status == erc.ERC_ERR_TIMEOUT or (status == erc.ERC_OK and not some)
+            assert polls > 1 or some
