@@ -584,7 +584,7 @@ extern "C" erc_status erc_expert_ffn(const erc_ffn_shape* f, const void* xs, con
     p.pre = static_cast<T*>(pre);
     p.y = static_cast<T*>(y);
     p.splits = 1;
-    p.polls = wait_limit(0);
+    p.patience = TcPatience(wait_limit(0));
     p.lost = w.lost;
     const int D = p.width, F = p.inner, E = p.experts;
     if (w.x) {
@@ -651,7 +651,7 @@ extern "C" erc_status erc_expert_ffn_backward(const erc_ffn_shape* f, const void
     p.dw_out = static_cast<T*>(dw_out);
     p.partial = w.partial;
     p.splits = 1;
-    p.polls = wait_limit(0);
+    p.patience = TcPatience(wait_limit(0));
     p.lost = w.lost;
     const int D = p.width, F = p.inner, E = p.experts;
     if (w.x) {

@@ -14,6 +14,14 @@ namespace erc {
 
 enum FfnProduct { FFN_IN, FFN_OUT, FFN_DH, FFN_DX, FFN_DWIN, FFN_DWOUT };
 
+// looks at a barrier before a wait gives up, and how many nanoseconds a look may sleep: one that is told to give up
+// early does not sleep
+struct TcPatience {
+  unsigned polls = 0x7fffffffu, nap = 1000000u;
+  TcPatience() = default;
+  __host__ __device__ explicit TcPatience(unsigned limit) { if (limit) polls = limit, nap = 0; }
+};
+
 // the arrays of all six; a product uses those that it names
 template <class T>
 struct FfnArgs {
@@ -35,8 +43,8 @@ struct FfnArgs {
   // DWIN and DWOUT: the slots of an expert in `splits` parts, whose sums go to partial [splits][experts][rows][columns]
   int splits;
   float* partial;
-  // on the tensor cores: looks at a barrier before a wait gives up (0: TC_WAIT), and which blocks of IN or DH gave up
-  unsigned polls;
+  // on the tensor cores: how long a wait lasts, and which blocks of IN or DH gave up
+  TcPatience patience;
   int* lost;
 };
 // [lo, hi) of an expert; whatever the offsets hold, it lies in [0, slots]

@@ -84,12 +84,13 @@ __device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes) {
 __device__ __forceinline__ void bar_arrive_cluster(uint32_t cluster_bar) {
   asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
 }
-__device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
+// a look at a barrier, which may sleep for up to `nap` nanoseconds
+__device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity, uint32_t nap) {
   uint32_t done;
   asm volatile(
-      "{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}"
+      "{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\nselp.u32 %0, 1, 0, p;\n}"
       : "=r"(done)
-      : "r"(bar), "r"(parity)
+      : "r"(bar), "r"(parity), "r"(nap)
       : "memory");
   return done;
 }
@@ -98,37 +99,22 @@ __device__ __forceinline__ uint64_t nanoseconds() {
   asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
   return t;
 }
-// polls a barrier, for `limit` nanoseconds at most; the clock is looked at every 256 polls
-__device__ __forceinline__ bool bar_poll(uint32_t bar, uint32_t parity, uint64_t limit, volatile int* failed) {
+// looks at a barrier `polls` times and for `limit` nanoseconds at most; the clock is read every 256 looks
+__device__ __forceinline__ bool bar_poll(uint32_t bar, uint32_t parity, TcPatience w, uint64_t limit, volatile int* failed) {
   uint64_t start = 0;
-  for (unsigned i = 0; i < 0x7fffffffu; ++i) {
-    if (bar_try(bar, parity)) return true;
-    if (failed && *failed) return false;
-    if (i % 256 == 255) {
+  for (unsigned i = 1;; ++i) {
+    if (bar_try(bar, parity, w.nap)) return true;
+    if ((failed && *failed) || i >= w.polls) return false;
+    if (i % 256 == 0) {
       const uint64_t now = nanoseconds();
       if (start == 0) start = now;
       if (now - start > limit) return false;
     }
   }
-  return false;
-}
-// looks at a barrier `polls` times
-__device__ __forceinline__ bool bar_look(uint32_t bar, uint32_t parity, unsigned polls, volatile int* failed) {
-  for (unsigned i = 0; i < polls; ++i) {
-    uint32_t done;
-    asm volatile(
-        "{\n.reg .pred p;\nmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}"
-        : "=r"(done)
-        : "r"(bar), "r"(parity)
-        : "memory");
-    if (done) return true;
-    if (*failed) return false;
-  }
-  return false;
 }
 // false when the wait ran out, here or in another role of the block
-__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile int* failed, unsigned polls) {
-  if (polls ? bar_look(bar, parity, polls, failed) : bar_poll(bar, parity, TC_WAIT, failed)) return true;
+__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile int* failed, TcPatience w) {
+  if (bar_poll(bar, parity, w, TC_WAIT, failed)) return true;
   *failed = 1;
   return false;
 }
@@ -587,7 +573,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(TC_THREADS, 1)
         const int m = t.m0 + m_block, n_half = t.n / 2;
         const uint32_t bytes = TC_OPERAND + (B_K ? TC_OPERAND : n_half * TC_K * 2);
         for (int b = 0; b < t.blocks; ++b) {
-          if (!(ok = bar_wait(empty(s), phase ^ 1, &failed, p.polls))) break;
+          if (!(ok = bar_wait(empty(s), phase ^ 1, &failed, p.patience))) break;
           const uint32_t dst = stages + s * TC_STAGE;
           const int k = b * TC_K;
           if constexpr (SLOTS) {
@@ -637,11 +623,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(TC_THREADS, 1)
         if (t.blocks == 0) continue;
         const uint32_t idesc = (1u << 4) | (Half2<T>::FORMAT << 7) | (Half2<T>::FORMAT << 10) | ((A_K ? 0u : 1u) << 15) |
                                ((B_K ? 0u : 1u) << 16) | ((uint32_t)(t.n >> 3) << 17) | ((256u >> 4) << 24);
-        if (!(ok = bar_wait(taken(a), a_phase ^ 1, &failed, p.polls))) break;
+        if (!(ok = bar_wait(taken(a), a_phase ^ 1, &failed, p.patience))) break;
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         const uint32_t d = tmem + a * 256;
         for (int b = 0; b < t.blocks; ++b) {
-          if (!(ok = bar_wait(ready(s), phase, &failed, p.polls))) break;
+          if (!(ok = bar_wait(ready(s), phase, &failed, p.patience))) break;
           asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
           const uint64_t da = operand_desc(stages + s * TC_STAGE, A_K), db = operand_desc(stages + s * TC_STAGE + TC_OPERAND, B_K);
 #pragma unroll
@@ -666,7 +652,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(TC_THREADS, 1)
         s = (s + t.blocks - 1) % TC_STAGES;
         const int live = (int)(t.k1 - t.k0 - (int64_t)(t.blocks - 1) * TC_K);
         if (live < TC_K) {
-          if (!__all_sync(0xffffffffu, bar_wait(land(s), used >> s & 1, &failed, p.polls))) break;
+          if (!__all_sync(0xffffffffu, bar_wait(land(s), used >> s & 1, &failed, p.patience))) break;
           used ^= 1u << s;
           const uint32_t base = stages + s * TC_STAGE;
           const int boxes = t.n > 128 ? 4 : 3;
@@ -720,7 +706,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(TC_THREADS, 1)
         read_pre(out.pre_a, out.pre_b, out.at + (uint32_t)c / 2 * out.two, out.two, c, c < c1 ? out.live - out.col : 0, next);
       };
       if constexpr (WHICH == FFN_DH) read_ahead(c0);
-      if (ok) ok = __all_sync(0xffffffffu, bar_wait(full(a), a_phase, &failed, p.polls));
+      if (ok) ok = __all_sync(0xffffffffu, bar_wait(full(a), a_phase, &failed, p.patience));
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
       const uint32_t src = tmem + a * 256 + ((uint32_t)(quad * 32) << 16);
 #pragma unroll 1
@@ -756,10 +742,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(TC_THREADS, 1)
   if (failed) {
     if (threadIdx.x == 32 && rank == 0) {  // the thread that issued the products
       commit_pair(done);
-      bar_poll(done, 0, TC_WAIT, nullptr);
+      bar_poll(done, 0, TcPatience(), TC_WAIT, nullptr);
     }
     __syncthreads();
-    if (threadIdx.x == 0) bar_poll(never, 0, TC_COPIES, nullptr);  // nothing arrives here, so this is a pause for the copies
+    if (threadIdx.x == 0) bar_poll(never, 0, TcPatience(0x7fffffffu), TC_COPIES, nullptr);  // nothing arrives here, so this is a pause for the copies
     __syncthreads();
   }
   cluster_arrive_wait();
