@@ -133,18 +133,18 @@ struct Terms {
   uint64_t X = 0, u = 0;  // two sums each
   float top = 0.f;
 };
-// one entry, which may be a largest one; masked: -inf
-__device__ __forceinline__ void add_entry(Terms& a, float l, const Scale& s) {
-  const bool largest = l == s.m;
+// one entry, which may equal `top`, the largest; masked: -inf
+__device__ __forceinline__ void add_entry(Terms& a, float l, const Scale& s, float top) {
+  const bool largest = l == top;
   const float t = s.plain ? fmaf(fmaxf(l, s.low), s.c, s.minus_mc) : scaled(l, s.m, s.c);
   const float e = largest ? 0.f : exp2_fast(t);
   a.top += largest ? 1.f : 0.f;
   a.X = add2(a.X, pair(e, 0.f));
   a.u = fma2(pair(e, 0.f), pair(t, 0.f), a.u);
 }
-// holds_top: a largest entry may be among them
+// holds_top: an entry that equals `top` may be among them (the largest; the anchor, where none is given)
 template <class T>
-__device__ __forceinline__ void add_vector(Terms& a, uint4 v, const Scale& s, bool holds_top) {
+__device__ __forceinline__ void add_vector(Terms& a, uint4 v, const Scale& s, bool holds_top, float top) {
   constexpr int P = ScoreVec<T>::N / 2;
   if (s.plain) {
     uint64_t l[P];
@@ -156,7 +156,7 @@ __device__ __forceinline__ void add_vector(Terms& a, uint4 v, const Scale& s, bo
         float t0, t1, l0, l1;
         unpair(t, t0, t1);
         unpair(l[i], l0, l1);
-        const bool top0 = l0 == s.m, top1 = l1 == s.m;
+        const bool top0 = l0 == top, top1 = l1 == top;
         const uint64_t e = pair(top0 ? 0.f : exp2_fast(t0), top1 ? 0.f : exp2_fast(t1));
         a.top += (top0 ? 1.f : 0.f) + (top1 ? 1.f : 0.f);
         a.X = add2(a.X, e);
@@ -177,8 +177,12 @@ __device__ __forceinline__ void add_vector(Terms& a, uint4 v, const Scale& s, bo
     float l[2 * P];
     unpack_scores(v, l, T());
 #pragma unroll
-    for (int i = 0; i < 2 * P; ++i) add_entry(a, l[i], s);
+    for (int i = 0; i < 2 * P; ++i) add_entry(a, l[i], s, top);
   }
+}
+template <class T>
+__device__ __forceinline__ void add_vector(Terms& a, uint4 v, const Scale& s, bool holds_top) {
+  add_vector<T>(a, v, s, holds_top, s.m);
 }
 // the sums of a lane, or of several, with d taken out: 2^-d (X, u - d X)
 __device__ __forceinline__ Sum settle(Sum a, const Scale& s) {
@@ -594,21 +598,35 @@ __global__ void __launch_bounds__(ST) k_score_join(int64_t rows, int64_t n, cons
   }
 }
 
-// A warp takes a row of any length, 8 vectors a lane in flight, without a barrier: a higher maximum settles what was
-// summed below the one before.  No best entries.
+// A warp takes a row of any length, 8 vectors a lane in flight, without a barrier.  No best entries.
+//
+// Terms are relative to an anchor that the largest entry so far, the peak, exceeds by at most 2^1: a higher peak turns
+// the entries that equalled the one before into terms, and only where it leaves the anchor behind are the sums scaled, by less
+// than 1/2, so that the roundings of many such steps add up to less than two.  A lane sums the terms of 4 rounds, 128 of a
+// 16-bit type, one by one; these sums go to a second one that keeps its rounding errors, so that no row is too long (4194304
+// entries would be 65536 terms to a sum: ln Z off by 5e-4).
 template <class T>
 __global__ void __launch_bounds__(ST, 4) k_score_stream(int64_t rows, int64_t n, const T* __restrict__ logits, int64_t stride,
                                                         ScoreOut o) {
-  constexpr int V = 8;
+  constexpr int V = 8, ROUNDS = 4;
+  __shared__ float4 settled[ST];  // the second sums, X and u and the roundings of both: registers are short
+  float4& held = settled[threadIdx.x];
   const int lane = threadIdx.x & 31;
   for (int64_t row = ((int64_t)blockIdx.x * ST + threadIdx.x) >> 5; row < rows; row += (int64_t)gridDim.x * SW) {
     const T* x = logits + row * stride;
     const RowView<T> view(x, n);
     Given g = {-1, 0.f};
     if (lane == 0) g = given_of(o, row, x, n);
-    Sum a = {LOWEST, 0.f, 0.f, 0.f};  // what was settled
-    Scale scale(LOWEST, o.c);
-    Terms terms;
+    held = {0.f, 0.f, 0.f, 0.f};
+    Scale scale(LOWEST, o.c);               // of the anchor
+    float peak = LOWEST;
+    Terms terms;  // its `top` counts the entries that equal the peak
+    auto put_by = [&] {
+      const Sum s = settle(sum_of(terms, scale.m), scale);
+      const float2 X = df_two_sum(held.x, s.X), u = df_two_sum(held.y, s.u);
+      held = {X.x, u.x, held.z + X.y, held.w + u.y};
+      terms.X = terms.u = 0;
+    };
     for (int v0 = 0; v0 < view.vectors; v0 += 32 * V) {
       uint4 v[V];
 #pragma unroll
@@ -617,27 +635,35 @@ __global__ void __launch_bounds__(ST, 4) k_score_stream(int64_t rows, int64_t n,
         v[j] = at < view.vectors ? view.fetch(at)
                                  : make_uint4(masked_word<T>(), masked_word<T>(), masked_word<T>(), masked_word<T>());
       }
-      float m = scale.m, best[V];
+      float m = peak, best[V];
 #pragma unroll
       for (int j = 0; j < V; ++j) {
         best[j] = max_score(v[j], T());
         m = fmaxf(m, best[j]);
       }
       m = warp_max(m);
-      if (m > scale.m) {
-        const Sum s = settle(sum_of(terms, scale.m), scale);
-        a = {scale.m, a.X + s.X, a.u + s.u, a.top + s.top};
-        raise(a, m, o.c);
-        scale = Scale(m, o.c);
-        terms = Terms();
+      if (m > peak) {
+        const float t = scale.plain ? fmaf(peak, scale.c, scale.minus_mc) : scaled(peak, scale.m, scale.c);
+        const float e = terms.top * exp2_fast(t);
+        terms.X = add2(terms.X, pair(e, 0.f));
+        terms.u = fma2(pair(e, 0.f), pair(t, 0.f), terms.u);
+        terms.top = 0.f;
+        peak = m;
+        if (!(scaled(m, scale.m, scale.c) <= 1.f)) {
+          put_by();
+          const float d = scaled(scale.m, m, scale.c), f = exp2_fast(d);
+          held = {f * held.x, f * fmaf(d, held.x, held.y), f * held.z, f * fmaf(d, held.z, held.w)};
+          scale = Scale(m, o.c);
+        }
       }
 #pragma unroll
-      for (int j = 0; j < V; ++j) add_vector<T>(terms, v[j], scale, best[j] == m);
+      for (int j = 0; j < V; ++j) add_vector<T>(terms, v[j], scale, best[j] == peak, peak);
+      if (v0 / (32 * V) % ROUNDS == ROUNDS - 1) put_by();
     }
-    const Sum s = settle(sum_of(terms, scale.m), scale);
-    a.X = warp_sum(a.X + s.X);
-    a.u = warp_sum(a.u + s.u);
-    a.top = warp_sum(a.top + s.top);
+    put_by();
+    Sum a = {scale.m, warp_sum(held.x + held.z), warp_sum(held.y + held.w), 0.f};
+    raise(a, peak, o.c);
+    a.top = warp_sum(terms.top);
     if (lane == 0) finish_row(o, row, g, a);
   }
 }
@@ -698,8 +724,8 @@ __global__ void __launch_bounds__(ST, TOP ? 3 : 4) k_score_short(int64_t rows, i
     Terms terms;
 #pragma unroll
     for (int j = 0; j < VPL; ++j) add_vector<T>(terms, v[j], scale, peak[j] == m);
-    add_entry(terms, head, scale);
-    add_entry(terms, tail, scale);
+    add_entry(terms, head, scale, m);
+    add_entry(terms, tail, scale, m);
     Sum a = sum_of(terms, m);
 #pragma unroll
     for (int w = LANES / 2; w; w >>= 1) {
