@@ -530,10 +530,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(TC_THREADS, 1)
     for (int i = 1; i < 4; ++i)
       if (cost_of[i] < 0.97f * least) least = cost_of[i], most = 256 - 32 * i;
     for (int e = threadIdx.x; e < p.experts; e += TC_THREADS) {
-      const int rows = of.hi[e] - of.lo[e], count = (int)(((unsigned)rows + most - 1) / most);
-      const int wide = count > 1 ? ((rows + count - 1) / count + 31) & ~31 : 256;
+      const unsigned rows = of.hi[e] - of.lo[e], count = (rows + most - 1) / most;  // rows + count: up to 2^31 + 2^24
+      const unsigned wide = count > 1 ? ((rows + count - 1) / count + 31) & ~31u : 256;
       of.wide[e] = (short)wide;
-      of.prefix[e + 1] = (int)(((unsigned)rows + wide - 1) / wide);
+      of.prefix[e + 1] = (int)((rows + wide - 1) / wide);
     }
   }
   if (SLOTS) {
