@@ -922,6 +922,8 @@ __global__ void __launch_bounds__(ST, SHIFT ? 4 : 5) k_score_backward(int64_t ro
       const float f = exp2_fast(-rest) * r.inv;
       r.A = -f * r.gh * LN2;
       r.B = -f * fmaf(r.gh, fmaf(-rest, LN2, r.H), r.g);
+      // a masked entry's t is finite and its 2^t is 0, so that its gradient is 0 unless A t + B is not a number
+      r.scale.plain = r.scale.plain && fabsf(r.A) < 1e30f && fabsf(r.B) < 1e30f;
     }
     for (int u0 = first; u0 < last; u0 += SV * step) {
       if (u0 > first) load(u0);
