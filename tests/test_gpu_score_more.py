@@ -33,3 +33,26 @@ def test_masked_entries_have_no_gradient_whatever_comes_from_above(kind, n, valu
     got, want = (erc.erc_score_rows_backward(x, ids, norm, d, entropy, one) for d in (dlogp, one))
     others = [0, 1, 2, 4, 5]
     assert torch.equal(got[others], want[others])
+
+
+@pytest.mark.parametrize("kind", [torch.float32, torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("rows", [1, 3])
+def test_many_equal_entries_of_rows_that_a_second_kernel_joins(rows, kind):
+    """More than 256 candidates among the parts' best: the exact search by key and index."""
+    n, k = 1400003, 32
+    equal = torch.full((rows, n), 2.5, device=dev()).to(kind)
+    ids = erc.erc_score_rows(equal, k=k)[3]
+    assert (ids == torch.arange(k, device=dev(), dtype=torch.int32)).all()
+    few = equal.clone()
+    few[:, : n // 2] = 1.0  # the best are the later half
+    best = [n - 1, n // 2 + 70000, n // 2 + 70001]
+    few[:, best] = 3.0
+    _, _, _, ids, logp = erc.erc_score_rows(few, k=k)
+    want = torch.cat([torch.tensor(sorted(best)), torch.arange(n // 2, n // 2 + k - 3)]).to(dev()).int()
+    assert torch.equal(ids, want.expand(rows, k))
+    assert (logp[:, :3] == logp[:, :1]).all() and (logp[:, 3:] == logp[:, 3:4]).all() and (logp[:, 0] > logp[:, 3]).all()
+    zeros = torch.zeros(rows, n, device=dev()).to(kind)
+    zeros[:, ::3] = -0.0  # equal to +0
+    zeros[:, 5] = -math.inf
+    want = [i for i in range(k + 1) if i != 5]
+    assert erc.erc_score_rows(zeros, k=k)[3].tolist() == [want] * rows
