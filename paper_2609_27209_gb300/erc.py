@@ -526,6 +526,19 @@ def _need(t, name, dtype, shape, device):
         _refuse(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)} on {device}")
 
 
+def _integer(v, name):
+    """`v` as an int, of any size."""
+    if type(v) is int:
+        return v
+    try:
+        n = int(v)
+    except (TypeError, ValueError, OverflowError):
+        n = None
+    if n is None or n != v:
+        _refuse(f"{name} must be a whole number")
+    return n
+
+
 def _whole(v, name):
     """`v` as an int32; a ctypes field would wrap a number that does not fit."""
     if type(v) is int and -2**31 <= v < 2**31:
@@ -864,13 +877,12 @@ def erc_dropout(x, p, key, residual=None, first=0):
         _need(key, "key", torch.int64, (1,), x.device)
         number, at = 0, key.data_ptr()
     else:
-        if int(key) != key:
-            _refuse("key must be a whole number")
-        number, at = int(key) % 2**64, None
-    if not (int(first) == first and 0 <= first < 2**62):
-        _refuse("first must be a whole number in [0, 2^62)")
+        number, at = _integer(key, "key") % 2**64, None
+    first = _integer(first, "first")
+    if not 0 <= first < 2**62:
+        _refuse("first must be in [0, 2^62)")
     out = torch.empty_like(x)
-    status = lib().erc_dropout(x.numel(), x.data_ptr(), kind, _at(residual), p, number, at, int(first), out.data_ptr(),
+    status = lib().erc_dropout(x.numel(), x.data_ptr(), kind, _at(residual), p, number, at, first, out.data_ptr(),
                                _stream_of(x))
     if status:
         _check(status)
