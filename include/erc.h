@@ -465,7 +465,9 @@ erc_status erc_score_rows_backward(int64_t rows, int64_t n, const void* logits, 
  *      rows of factors), w_out [experts x width x inner], all dense of `type`.
  * Out: y [slots x width]; pre [slots x 2 inner] = (a, b), or NULL when no gradient is wanted.  Rows
  *      from offsets[experts] on are zeroed in both.
- * Sums are float32; a, b and act(a) b are rounded to `type` once, and so is y.
+ * Sums are float32; a, b and act(a) b are rounded to `type` once, and so is y.  The second product's operands are
+ * of `type` because the tensor cores' are: in float16 an |act(a) b| of 65520 and more is infinite, whatever y would be
+ * without that rounding, and in the gradient those of a and b below 2^-25 are 0.  Scale such models, or use bfloat16.
  * erc_expert_ffn_backward -- from dy [slots x width], xs, pre and the weights to dxs [slots x width],
  *      dw_in and dw_out (each may be NULL), rounded to `type` once; act(a) b and the gradients of a
  *      and b, formed from the rounded pre and float32 sums, are rounded once too.  dxs is zeroed from

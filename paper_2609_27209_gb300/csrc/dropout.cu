@@ -4,7 +4,7 @@
 // An entry's word is one of the four of its Philox block.  A thread takes two pieces of 16 bytes of
 // each array, one block of the generator a piece for float32 and two for the 16-bit types.
 //
-// 169343 x 512 bf16 with a residual: 78 to 80 us, 0.96 to 0.99 of the copy rate.  Without one the 16-bit types are bound by
+// 169343 x 512 bf16 with a residual: 76 to 80 us, 0.96 to 1.01 of the copy rate.  Without one the 16-bit types are bound by
 // the generator's instructions on the half-rate integer units: 20000 x 1001 f16 takes 19 us for a floor of 11.8 (blocks of
 // 256 threads 19.9, one piece a thread 20.9, four 22.5).
 #include "choice.cuh"

@@ -6,8 +6,9 @@
 // buffered in shared memory.  A thread keeps 4 x 4 or 8 x 8 sums in registers, as groups of 4 rows and 4 columns 64
 // apart.  In IN the second group of columns holds the factors of the first one's features.  Sums run over k in order,
 // 256 at a time.
-// Bound by the float32 units and by the tiles' rounds: 8192 slots of 1024 x 1024 float32, 44 TFLOP/s forward and 41
-// backward (library products: 45 and 50).
+// Bound by issue (a product and its share of the shared-memory reads are instructions of their own) and by the tiles'
+// rounds: 8192 slots of 1024 x 1024 float32, 43 to 44 TFLOP/s forward and 41 backward (library products: 45 to 57, by layout,
+// and 50 to 57).
 #include <initializer_list>
 
 #include "expert_ffn.cuh"
@@ -311,8 +312,11 @@ __global__ void __launch_bounds__(FT) k_ffn_weights(const FfnArgs<T> p) {
     }
 }
 
-// whether a weight gradient of rows x cols takes tiles of 128: enough of them for every SM, or slots enough to split their
-// sums until there are (8192 slots of 1024 x 1024 float32, 128 tiles and 64: the whole gradient 2744 -> 2426 us)
+// Whether a weight gradient of rows x cols takes tiles of 128: enough of them for every SM, or slots enough to split their
+// sums until there are.  The whole float32 gradient with tiles of 64 / 128 (us).  It takes 128: one expert of 1024 x 1024,
+// 8192 slots 2939 / 2511, 1024 slots 435 / 400; 8192 of 512 x 512, 780 / 663; 20000 of 200 x 200, 491 / 450; 20000 of 8 experts,
+// 256 x 512, 1046 / 929.  It takes 64: 8192 of 96 x 96, 90 / 160; 30000 of 128 x 128, 240 / 264; 1000 of 500 x 300, 165 / 294;
+// 4096 of 8 experts, 256 x 512, 234 / 239; 515 of 5 experts, 100 x 67, 43 / 60.
 bool large_weights(int64_t slots, int experts, int64_t rows, int64_t cols) {
   const int64_t tiles = ((rows + 2 * FM - 1) / (2 * FM)) * ((cols + 2 * FM - 1) / (2 * FM)) * experts;
   if (tiles >= sm_count()) return true;
@@ -375,17 +379,21 @@ erc_status simple_product(FfnProduct which, const FfnArgs<T>& p, cudaStream_t s)
 // ---- how a call's products run
 enum FfnWay { FFN_SIMPLE, FFN_FEW, FFN_TENSOR };
 
-// Few slots read the weights without the tensor cores.  IN + OUT, both ways (us; bfloat16): one expert of 2048 x 2048, 8
-// slots 23 / 39, 16 slots 43 / 39; 8 experts of 512 x 1024, 16 slots 18 / 27, 32 slots 19 / 27; 64 experts of
-// 1024 x 512, 32 slots 42 / 45.
+// Few slots read the weights without the tensor cores.  IN + OUT, this way / by tiles (us, weights in L2):
+//   one expert of 2048 x 2048       bfloat16: 4 slots 12 / 28, 8: 19 / 28, 16: 34 / 28; float32: 8: 23 / 230, 16: 44 / 231
+//   8 experts of 512 x 1024         bfloat16: 16 slots 11 / 20, 32: 13 / 21, 64: 18 / 20; float32: 32: 15 / 87, 64: 22 / 87
+//   64 experts of 1024 x 512        bfloat16: 32 slots 40 / 36, 64: 69 / 53; float32: 32: 51 / 207, 64: 87 / 379
+// The bound is bfloat16's; float32, whose tiles are of 64 rows whatever is in them, would gain from a later one.
 bool few_slots(const erc_ffn_shape* f) { return f->slots <= 8 || (f->slots <= 32 && f->slots <= 4 * f->experts); }
 bool whole_pieces(const erc_ffn_shape* f) {
   const int piece = 16 / type_bytes(f->type);
   return f->width % piece == 0 && f->inner % piece == 0;
 }
-// Rows that are not whole pieces are copied into rows that are, for the tensor cores' sake, where that pays: the copies
-// cost some 20 us and three times the weights' bytes.  8192 slots of 1021 x 1023 bfloat16: forward 1440 us on the float32
-// units, 104 this way; gradient 3750 and 216.
+// Rows that are not whole pieces are copied into rows that are, for the tensor cores' sake: the copies cost some 20 us and
+// three times the weights' bytes.  bfloat16, on the float32 units / this way (us, forward; gradient): 8192 slots of 1021 x
+// 1023, 1440 / 86; 3750 / 189.  At the bounds: 100 slots of 1001 x 1001, 220 / 37; 334 / 66; 400 of 501 x 501, 117 / 31; 237 / 60;
+// 400 slots of 8 experts, 511 x 511, 118 / 31; 206 / 59.  Below them it would pay too, at the price of the copies'
+// workspace: 1000 slots of 201 x 201, 53 / 23; 256 / 52; 250 slots of 8 experts, 511 x 511, 109 / 29; 184 / 58.
 bool worth_padding(const erc_ffn_shape* f) {
   return f->type != ERC_F32 && !whole_pieces(f) && f->slots >= 32 * (int64_t)f->experts &&
          (double)f->slots * f->width * f->inner >= 1e8;

@@ -6,9 +6,11 @@
 // with parts of up to 32 sums; halving steps leave sum i in lane i (31 shuffles for 32 sums).  OUT asks for its
 // weights while IN still runs, and waits for h only then.
 //
-// 14 slots over 8 experts of 512 x 1024 bf16 (16 MB of weights, 2.3 us of copying): IN 8.6 us, OUT 5.3; a call takes 19 to
-// 21, which is the binding's and the launches' time.  Both are latency: offsets, weights, slots and the halving steps
-// follow each other, and half the blocks have no slots.
+// 14 slots over 8 experts of 512 x 1024 bf16 (25 MB of weights, 3.7 us of copying): 13.5 us; one slot of one expert of
+// 2048 x 2048 (25 MB) 11.5; in float32 19 and 18.7 (7.4).  A call takes 20 to 22, which is the binding's and the launches'
+// time.  What bounds them is latency: offsets, weights, slots and the halving steps follow each other, with 128 and
+// 64 blocks (2048 rows) for 152 SMs, issue active in 0.05 to 0.15 of the cycles, and, with few slots over many experts, blocks
+// without any.
 #include "expert_ffn.cuh"
 
 namespace erc {

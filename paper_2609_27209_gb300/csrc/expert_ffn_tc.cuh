@@ -24,16 +24,18 @@
 //
 // Why this tile: a stage of 64 k brings a block 32 KB for 512 clocks of products, and an SM takes in about 64 bytes a
 // clock, so 256 x 256 a pair is where copies and products balance; with three quarters of the products left out 8192 x
-// 2048 x 4096 still takes 0.77 of its time.  Two accumulators fill tensor memory.  What it reaches (8192 slots, one expert,
-// 2048 x 4096): IN 159 to 167 us, 1640 to 1730 TFLOP/s (0.87 to 0.91 of the measured burst rate); OUT 94 to 100 us,
-// 1370 to 1450, 256 tiles on 76 pairs being 3.4 rounds.  Experts of a few hundred slots are bound by memory and by the
-// rounds: 64 x 512 slots of 1024 x 512, IN 59 to 64 us, OUT 45.  DH also reads (a, b) and writes (da, db) and h, 0.9 GB for
-// 80000 slots of 1024: 198 us, 4.7 TB/s.
+// 2048 x 4096 still took 0.77 of its time.  Two accumulators fill tensor memory.  What it reaches (8192 slots, one expert,
+// 2048 x 4096 bf16): IN 147 us, 1870 TFLOP/s (0.99 of the measured burst rate); OUT 92 us, 1490, 256 tiles on 76
+// pairs being 3.4 rounds.  Experts of a few hundred slots (64 x 512 slots of 1024 x 512: IN 52 to 57 us, OUT 36 to 41) saturate
+// nothing: tensor pipe 0.57, copies into the SMs 0.56 of 64 bytes a clock, memory 0.63 of the copy rate; their 7 rounds of 16
+// stages of 512 clocks are 30 us.  Where the rest goes is not known.  DH also reads (a, b) and writes (da, db) and h, 0.9 GB
+// for 80000 slots of 1024: 187 to 190 us, 4.9 TB/s.
 //
 // What was tried and did not pay: asking for DH's rows ahead (prefetches into L2: 215 -> 240 us, by bulk requests 345;
 // reading two or three steps ahead: no change); passing what DH reads and writes through shared memory by tensor copies,
 // with 4 stages instead of 6 (200 -> 191 us at a depth of 512, 108 -> 117 at 2048); 8 result warps instead of 16 (DH 209 instead of 200); passing every
 // stage on through a warp of each block (the same).  Releases at cluster scope on the way cost a microsecond a stage.
+// A wait's look names how long it may sleep (8192 x 2048 x 4096 f16: IN 186 -> 177 us, OUT 106 -> 97 against looks that do not).
 //
 // Every wait on a barrier ends: after TC_WAIT, or a given number of looks, it gives up.  The block's other roles then
 // stop at their next wait; once all have, products and copies in flight are waited for (with limits), tensor memory

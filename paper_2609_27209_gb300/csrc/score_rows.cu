@@ -15,11 +15,12 @@
 // through a workspace and a second kernel.  Short rows take 8 to 32 lanes each, rows by the thousand without best
 // entries a warp each, all in registers.
 //
-// What bounds them: an entry costs 3 to 4 instructions and one of the 16 exponentials an SM makes a clock, which is
-// 0.37 of the copy rate for bfloat16 rows if nothing else waits; a few long rows are latency (launch, copy, two
-// passes, the search, two cluster barriers).  Device time (us) and floor at 6767 GB/s:
-//   64 x 169343 bf16, 20 best  18.7 / 3.2, none 12.4 / 3.2; 1 x 20000 f32, 5 best 8.3, none 4.6; 16384 x 257 f32, none
-//   10.2 / 2.5, 32 best 30; 4096 x 20000 bf16, none 42 / 24.2; 8 x 2449029 f32, none 24 / 11.6, 32 best 47 / 11.6.
+// What bounds them: an entry costs 3 to 4 instructions, 0.3 of the time that bfloat16 rows take to arrive, and one of the
+// 16 exponentials an SM makes a clock, 0.7 of it; a block's phases (copy, maximum, sums, search) wait for each other, and
+// a few long rows are latency (launch, copy, two passes, the search, two cluster barriers).  Device time (us) and floor at 6767 GB/s:
+//   64 x 169343 bf16, 20 best  18.4 / 3.2, none 12.4 / 3.2; 1 x 20000 f32, 5 best 8.2, none 4.8; 16384 x 257 f32, none
+//   8 to 10 / 2.5, 32 best 30; 4096 x 20000 bf16, none 42 / 24.2; 3000 x 300000 bf16, none 375 / 266; 8 x 2449029 f32, none
+//   24 / 11.6, 32 best 48 / 11.6.  A warp a row (4096 x 20000) issues in 0.49 of the cycles with 0.37 of the warps that fit.
 // The gradient reads and writes each entry once: 4096 x 20000 bf16 53 to 56 us, 0.87 to 0.92 of the copy rate; rows whose
 // result is aligned otherwise than the scores (4096 x 19999) 71 us.
 #include "choice.cuh"
@@ -988,7 +989,8 @@ Split split_rows(int64_t rows, int64_t n, int32_t type) {
   return {(int)((segments + each - 1) / each), (int)each * 32};
 }
 // Rows enough to keep the machine busy with a warp each.  A warp a row against a block a row (us, k 0): 10000 x 5001 float16
-// 35 / 45, 4096 x 20001 float32 71 / 85, 3000 x 3000 bfloat16 10.3 / 14.1; fewer rows leave SMs without loads in flight:
+// 35 / 45, 4096 x 20001 float32 71 / 85, 3000 x 3000 bfloat16 10.3 / 14.1, 4096 x 20000 bfloat16 43 / 41.5 (no difference
+// worth a rule); fewer rows leave SMs without loads in flight:
 // 2500 x 20000 bfloat16 30 / 28, 1900 x 20000 26 / 23.
 bool many_rows(int64_t rows) { return rows >= (int64_t)sm_count() * 18; }
 bool short_rows(int64_t n, int32_t type) { return n / (16 / type_bytes(type)) <= 32 * 8; }
