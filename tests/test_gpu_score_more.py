@@ -56,3 +56,23 @@ def test_many_equal_entries_of_rows_that_a_second_kernel_joins(rows, kind):
     zeros[:, 5] = -math.inf
     want = [i for i in range(k + 1) if i != 5]
     assert erc.erc_score_rows(zeros, k=k)[3].tolist() == [want] * rows
+
+
+@pytest.mark.parametrize("kind", [torch.float32, torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("rows,n", [(5, 40), (3000, 40), (5, 9001), (3000, 2500), (2, 60001), (1, 1400003)])
+def test_a_types_lowest_value_is_a_score_and_a_mask_beside_others(rows, n, kind):
+    low = torch.finfo(kind).min
+    x = torch.full((rows, n), low, dtype=kind, device=dev())
+    ids = torch.full((rows,), n - 1, dtype=torch.int32, device=dev())
+    logp, entropy, norm, _, _ = erc.erc_score_rows(x, ids)
+    # equal entries are counted, not summed: log n within its rounding and that of the logarithm
+    for v, want in ((logp, -math.log(n)), (entropy, math.log(n)), (norm[:, 1], math.log(n))):
+        assert (v - want).abs().max().item() <= 4 * 2.0**-24 * math.log(n)
+    assert (norm[:, 0] == low).all()
+    x[:, 3] = 0.0
+    logp, entropy, norm, _, _ = erc.erc_score_rows(x, ids)
+    assert (norm == 0).all() and (entropy == 0).all() and (logp == low).all()
+    grad = erc.erc_score_rows_backward(x, ids, norm, torch.ones(rows, device=dev()), entropy, torch.ones(rows, device=dev()))
+    want = torch.zeros_like(x)
+    want[:, 3], want[:, -1] = -1.0, 1.0
+    assert torch.equal(grad, want)
