@@ -733,7 +733,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(TC_THREADS, 1)
       bar_poll(done, 0, TcPatience(), TC_WAIT, nullptr);
     }
     __syncthreads();
-    if (threadIdx.x == 0) bar_poll(never, 0, TcPatience(0x7fffffffu), TC_COPIES, nullptr);  // nothing arrives here, so this is a pause for the copies
+    // nothing arrives at this barrier, so this is a pause, for the copies
+    if (threadIdx.x == 0) bar_poll(never, 0, TcPatience(0x7fffffffu), TC_COPIES, nullptr);
     __syncthreads();
   }
   cluster_arrive_wait();

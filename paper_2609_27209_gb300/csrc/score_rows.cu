@@ -93,9 +93,10 @@ __device__ __forceinline__ float warp_sum(float v) {
   return v;
 }
 
-// The terms of entries whose maximum m is known.  t = l c - fl(m c) is one fma, for two entries at once; the
-// rounding of m c moves every t by the same d = m c - fl(m c), which `settle` takes out again.  Masked entries and NaN are raised to `low`, about 1000 / c below m, where 2^t is 0: one maximum of the
-// stored type.  Rows where that does not hold (a maximum or a scale that is infinite, far from 0 or out of the type's
+// The terms of entries whose maximum m is known (a warp that streams a row: the anchor, at most 2^1 below it).
+// t = l c - fl(m c) is one fma, for two entries at once; the rounding of m c moves every t by the same d = m c - fl(m c),
+// which `settle` takes out again.  Masked entries and NaN are raised to `low`, about 1000 / c below m, where 2^t is 0: one
+// maximum of the stored type.  Rows where that does not hold (a maximum or a scale that is infinite, far from 0 or out of the type's
 // range) take the terms one by one.
 struct Scale {
   float m, c, minus_mc, low;
